@@ -1,0 +1,178 @@
+/*
+ * gett_matrix.h -- matrix operators for training and serving in 4 bits.
+ *
+ * Beside the tensor contraction of gett.h the library carries the matrix
+ * operators of a model whose products run in microscaled 4-bit floating point
+ * and whose weight updates are made orthogonal before they are applied:
+ *
+ *   gett_mx_quantize     a float matrix -> packed 4-bit matrix (one or both
+ *                        orientations in one pass)
+ *   gett_mx_dequantize   the values a packed matrix stands for
+ *   gett_mx_contract     C <- alpha * A * B^T + beta * C, A and B packed
+ *   gett_mx_apply        the same with a float A that is quantised in the call
+ *   gett_orthogonalize   Newton-Schulz steps on a stack of matrices
+ *
+ * Element types are those of gett_dtype_t and GETT_BFLOAT16 / GETT_FLOAT16.
+ * A matrix argument is a device pointer to element [0, 0] with a stride per
+ * row and per column in elements (both >= 1, any order; the library's other
+ * entry points describe tensors the same way).
+ *
+ * Calls enqueue work on `stream` (a hipStream_t, NULL: the default stream)
+ * and return.  Errors are statuses; nothing is thrown.  Workspaces are the
+ * library's own, one per device and stream, as for gett_contract: a call that
+ * needs more than the stream's workspace holds allocates, which is refused
+ * with GETT_ERROR_NOT_SUPPORTED, nothing enqueued, while `stream` captures a
+ * graph (run the call eagerly on that stream first).
+ *
+ * The packed format ("MX4").  A matrix of `rows` x `cols` is packed along its
+ * columns, the direction a product sums over.  Each run of 32 neighbours
+ * x_0..x_31 of one row shares the scale
+ *
+ *     s = 2^(floor(log2(max |x_i|)) - 2)          (2^-127 at least)
+ *
+ * and holds q_i = x_i / s rounded to the nearest of
+ * 0, 0.5, 1, 1.5, 2, 3, 4, 6 (and their negatives), ties to the value whose
+ * code is even; magnitudes above 6 become 6.  A run that holds an infinity
+ * or a NaN gets the NaN scale and stands for 32 NaNs.  Columns are padded with
+ * zeros to T = ceil(cols / 256) tiles of 256.
+ *
+ *   codes   rows x 128 T bytes, row after row: two codes (sign, two exponent
+ *           bits, one mantissa bit) a byte, the even column in the low half.
+ *   scales  T x 4 x R x 2 bytes, R = rows rounded up to 16: byte
+ *           ((t * 4 + b / 2) * R + row) * 2 + b % 2 is the scale of block b
+ *           (columns 256 t + 32 b and 31 more) of `row`, as exponent + 127;
+ *           255 is NaN.  The bytes of rows >= `rows` may hold anything.
+ *
+ * Both pointers are aligned to 16 bytes.  The scales lie in the order in
+ * which a wavefront takes them: the scales of one lane's rows and blocks are
+ * neighbours, so they reach its registers in one load per tile.
+ */
+#ifndef GETT_MATRIX_H
+#define GETT_MATRIX_H
+
+#include "gett.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/* Element types of these operators only, values of gett_dtype_t beside
+ * GETT_FLOAT32; the contraction's entry points refuse them. */
+#define GETT_BFLOAT16 ((gett_dtype_t)2)
+#define GETT_FLOAT16 ((gett_dtype_t)3)
+
+/*
+ * gett_mx_size -- bytes of the codes and scales of a packed rows x cols
+ * matrix.  GETT_ERROR_INVALID_VALUE for a null pointer or a negative extent,
+ * GETT_ERROR_NOT_SUPPORTED for rows of 2^30 or cols of 2^24 and more.
+ */
+gett_status_t gett_mx_size(int64_t rows, int64_t cols, uint64_t *code_bytes,
+                           uint64_t *scale_bytes);
+
+/*
+ * gett_mx_quantize -- pack X, its transpose, or both, in one pass over X.
+ *
+ *   dtype            GETT_FLOAT32, GETT_BFLOAT16 or GETT_FLOAT16.
+ *   codes, scales    X packed along its columns (gett_mx_size(rows, cols)),
+ *                    or both NULL.
+ *   codes_t, scales_t  X^T, a cols x rows matrix, packed along X's rows
+ *                    (gett_mx_size(cols, rows)), or both NULL.
+ *
+ * Errors: GETT_ERROR_INVALID_VALUE (unknown dtype, negative extent, stride
+ * < 1, no output, half of an output, a null or misaligned pointer, an output
+ * that overlaps X or another output), GETT_ERROR_NOT_SUPPORTED (extents
+ * beyond gett_mx_size's), GETT_ERROR_HIP.  An empty X enqueues nothing and its
+ * pointers are not looked at.
+ */
+gett_status_t gett_mx_quantize(gett_dtype_t dtype, int64_t rows, int64_t cols, const void *X,
+                               int64_t stride_row, int64_t stride_col, void *codes, void *scales,
+                               void *codes_t, void *scales_t, void *stream);
+
+/*
+ * gett_mx_dequantize -- the values of a packed rows x cols matrix, written to
+ * X in `dtype` (rounded where it cannot hold them: GETT_FLOAT16 only).
+ * Strides that map two elements to one address are refused
+ * (GETT_ERROR_NOT_SUPPORTED); other errors as for gett_mx_quantize.
+ */
+gett_status_t gett_mx_dequantize(gett_dtype_t dtype, int64_t rows, int64_t cols,
+                                 const void *codes, const void *scales, void *X,
+                                 int64_t stride_row, int64_t stride_col, void *stream);
+
+/*
+ * gett_mx_contract -- C[m, n] <- alpha * sum_k A[m, k] B[n, k] + beta * C[m, n].
+ *
+ *   codes_A, scales_A   a packed m x k matrix;
+ *   codes_B, scales_B   a packed n x k matrix.
+ *   dtype, C            C's element type and data.  Sums are held in 32 bits;
+ *                       alpha, beta and the sum are combined in 32 bits and
+ *                       rounded once.  beta == 0: C is not read; alpha == 0
+ *                       or k == 0: A and B are not read.
+ *
+ * Repeated calls give identical results.  Errors: GETT_ERROR_INVALID_VALUE
+ * (unknown dtype, negative extent, stride < 1, null or misaligned pointer, C
+ * overlapping an operand), GETT_ERROR_NOT_SUPPORTED (extents beyond
+ * gett_mx_size's; strides that map two elements of C to one address),
+ * GETT_ERROR_HIP.
+ */
+gett_status_t gett_mx_contract(int64_t m, int64_t n, int64_t k, double alpha,
+                               const void *codes_A, const void *scales_A, const void *codes_B,
+                               const void *scales_B, double beta, gett_dtype_t dtype, void *C,
+                               int64_t stride_m, int64_t stride_n, void *stream);
+
+/*
+ * gett_mx_apply -- gett_mx_contract with a float A, quantised in the call.
+ *
+ *   dtype_A, A, stride_am, stride_ak   an m x k matrix in 16 or 32 bits; the
+ *            result is that of gett_mx_quantize and gett_mx_contract.
+ *
+ * For few rows (single tokens) A is quantised on its way into the product,
+ * in the same launch; for more, into the stream's workspace first.
+ */
+gett_status_t gett_mx_apply(int64_t m, int64_t n, int64_t k, double alpha, gett_dtype_t dtype_A,
+                            const void *A, int64_t stride_am, int64_t stride_ak,
+                            const void *codes_B, const void *scales_B, double beta,
+                            gett_dtype_t dtype, void *C, int64_t stride_m, int64_t stride_n,
+                            void *stream);
+
+/*
+ * gett_orthogonalize -- O <- the Newton-Schulz iterate of G, per matrix.
+ *
+ *     X_0 = G / (|G|_F + eps)            |G|_F summed in 64 bits
+ *     X_{i+1} = a X_i + (b S + c S^2) X_i,   S = X_i X_i^T,   i < steps
+ *     O = X_steps                         (S = X^T X where rows > cols)
+ *
+ * The singular vectors of G stay and each singular value s moves by
+ * s <- a s + b s^3 + c s^5; with (3.4445, -4.7750, 2.0315) and five steps
+ * those above about 1e-3 |G|_F end between 0.7 and 1.2.
+ *
+ *   dtype     of G and O: GETT_FLOAT32, GETT_BFLOAT16 or GETT_FLOAT16.
+ *   batch     matrices in the stack (stride_batch between them, >= 1; any
+ *             value when batch is 1).
+ *   a, b, c   the polynomial.  Coefficients for which a singular value may
+ *             pass 3, or b s^2 + c s^4 may pass 15, within the steps
+ *             are refused (GETT_ERROR_NOT_SUPPORTED): the iterates are kept
+ *             in 16-bit parts that hold such values.
+ *   steps     0 to 1000.
+ *
+ * O may be G itself (same pointer and strides); otherwise they must not
+ * overlap.  Products are formed from 16-bit parts with sums in 32 bits: two
+ * parts (22 bits) for GETT_FLOAT32 and GETT_FLOAT16, one part (11 bits) for
+ * GETT_BFLOAT16, whose own 8 bits are coarser.  A NaN or an infinity in a
+ * matrix makes that matrix NaN.  Errors: GETT_ERROR_INVALID_VALUE (unknown
+ * dtype, negative extent or steps, stride < 1, eps negative or NaN, a
+ * coefficient that is not finite, null or misaligned pointer, overlap),
+ * GETT_ERROR_NOT_SUPPORTED (see above; rows or cols of 2^20 and more, steps above 1000; strides
+ * that map two elements to one address; batch x tiles beyond a launch),
+ * GETT_ERROR_HIP.
+ */
+gett_status_t gett_orthogonalize(gett_dtype_t dtype, int64_t batch, int64_t rows, int64_t cols,
+                                 const void *G, int64_t stride_batch, int64_t stride_row,
+                                 int64_t stride_col, double a, double b, double c, double eps,
+                                 int steps, void *O, int64_t ostride_batch, int64_t ostride_row,
+                                 int64_t ostride_col, void *stream);
+
+#ifdef __cplusplus
+}
+#endif
+
+#endif /* GETT_MATRIX_H */

@@ -1,0 +1,362 @@
+// mx_pack.hip -- microscaled 4-bit packing and its inverse.
+//
+// A block of 32 values x_i becomes s = 2^(floor(log2 max|x|) - 2) and the
+// codes of x_i / s (gett_matrix.h has the format).  The maximum is taken on
+// the magnitudes' bits as integers, which order as the floats do and put
+// infinities and NaNs above everything; the exponent is a field of those
+// bits, so the scale is exact.  The division by a power of two, the rounding
+// (to nearest, ties to the even code) and the saturation at 6 are one
+// conversion instruction for two values.
+//
+// Bound: memory.  X is read once, also where both orientations are packed: a
+// workgroup takes a 128 x 128 tile; each lane loads eight neighbours of a
+// row, four lanes hold a block, and the maximum crosses them in two
+// exchanges.  For the transposed packing the tile passes through LDS
+// (unrounded, in X's own type) and a lane takes 32 rows of one column; four
+// lanes take one column's four blocks, so 64 bytes of a row of codes_t leave
+// together.  Scales are gathered in LDS and leave in runs of 256 bytes.
+#include "matrix.hpp"
+
+namespace gett {
+namespace {
+
+constexpr int kT = 128;         // tile edge
+constexpr int kThreads = 256;
+constexpr int kChunk = 8;       // neighbours of a row one lane takes
+constexpr int kRowsPass = kThreads / (kT / kChunk);   // 16 rows per pass
+constexpr int kPasses = kT / kRowsPass;
+
+__device__ __forceinline__ uint32_t quad_max(uint32_t v)
+{
+    // the other lane of the pair, then the other pair of the four
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xF, 0xF, true));
+    return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xF, 0xF, true));
+}
+
+__device__ __forceinline__ uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+
+// LDS address (elements) of tile element (r, c): rows follow one another,
+// with 32 bytes of skew after every 32 rows, so that the lanes that read four
+// blocks of one column fall on different banks.
+template <typename T> __device__ __forceinline__ int tile_at(int r, int c)
+{
+    return r * kT + (r >> 5) * (32 / (int)sizeof(T)) + c;
+}
+
+// `wide`: columns are neighbours in memory (stride_col 1).
+template <typename T, bool ROWS, bool COLS>
+__global__ __launch_bounds__(kThreads) void mx_quantize_kernel(
+    const T *__restrict__ X, int64_t sr, int64_t sc, int rows, int cols, int tilesC, bool wide,
+    uint8_t *__restrict__ codes, uint8_t *__restrict__ scales, uint8_t *__restrict__ codesT,
+    uint8_t *__restrict__ scalesT)
+{
+    __shared__ __attribute__((aligned(16))) T tile[COLS ? kT * kT + 3 * (32 / sizeof(T)) : 1];
+    // [pair of blocks][row or column][block of the pair]
+    __shared__ __attribute__((aligned(16))) uint8_t sRow[ROWS ? 2 : 1][kT][2];
+    __shared__ __attribute__((aligned(16))) uint8_t sCol[COLS ? 2 : 1][kT][2];
+
+    const int tid = (int)threadIdx.x;
+    const int tr = (int)blockIdx.x / tilesC, tc = (int)blockIdx.x % tilesC;
+    const int row0 = tr * kT, col0 = tc * kT;
+    const int tilesK = (int)mx_tiles(cols), tilesKT = (int)mx_tiles(rows);
+    // this tile's columns (rows) lie inside the padded row of codes (codes_t)
+    const bool inRow = ROWS && col0 < tilesK * kTileK, inCol = COLS && row0 < tilesKT * kTileK;
+
+    const int c8 = (tid % (kT / kChunk)) * kChunk, r0 = tid / (kT / kChunk);
+    const int left = cols - (col0 + c8);   // columns of this lane's chunk inside X
+    T x[kPasses][kChunk];
+#pragma unroll
+    for (int p = 0; p < kPasses; ++p) {
+        const int r = row0 + r0 + p * kRowsPass;
+        const T *src = X + (int64_t)r * sr + (int64_t)(col0 + c8) * sc;
+        if (r < rows && left >= kChunk && wide) {
+            const Run<T, kChunk> v = *reinterpret_cast<const Run<T, kChunk> *>(src);
+#pragma unroll
+            for (int i = 0; i < kChunk; ++i) x[p][i] = v.v[i];
+        } else {
+#pragma unroll
+            for (int i = 0; i < kChunk; ++i) x[p][i] = from_float<T>(0.0f);
+            if (r < rows)
+#pragma unroll
+                for (int i = 0; i < kChunk; ++i)
+                    if (i < left) x[p][i] = src[i * sc];
+        }
+    }
+#pragma unroll
+    for (int p = 0; p < kPasses; ++p) {
+        const int lr = r0 + p * kRowsPass;
+        if constexpr (COLS) {
+#pragma unroll
+            for (int i = 0; i < kChunk; ++i) tile[tile_at<T>(lr, c8) + i] = x[p][i];
+        }
+        if constexpr (ROWS) {
+            float f[kChunk];
+            uint32_t top = 0;
+#pragma unroll
+            for (int i = 0; i < kChunk; ++i) {
+                f[i] = to_float(x[p][i]);
+                top = max(top, magnitude(f[i]));
+            }
+            const uint32_t sb = scale_byte(quad_max(top));
+            const uint32_t q = codes8(f, scale_value(sb));
+            if (inRow && row0 + lr < rows)
+                *reinterpret_cast<uint32_t *>(codes + (int64_t)(row0 + lr) * tilesK * kTileBytes +
+                                              (col0 + c8) / 2) = q;
+            if ((tid & 3) == 0) sRow[(c8 >> 6)][lr][(c8 >> 5) & 1] = (uint8_t)sb;
+        }
+    }
+    __syncthreads();
+    if constexpr (COLS) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int c = j * (kT / 2) + (tid >> 2), b = tid & 3;   // column, block of 32 rows
+            float f[32];
+            uint32_t top = 0;
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+                f[i] = to_float(tile[tile_at<T>(b * 32 + i, c)]);
+                top = max(top, magnitude(f[i]));
+            }
+            const uint32_t sb = scale_byte(top);
+            const float s = scale_value(sb);
+            i4 q;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) q[i] = (int)codes8(f + 8 * i, s);
+            if (inCol && col0 + c < cols)
+                *reinterpret_cast<i4 *>(codesT + (int64_t)(col0 + c) * tilesKT * kTileBytes +
+                                        row0 / 2 + b * 16) = q;
+            sCol[b >> 1][c][b & 1] = (uint8_t)sb;
+        }
+        __syncthreads();
+    }
+    // scales: two runs of 128 pairs, one 16-byte piece (eight rows) a thread
+    if constexpr (ROWS) {
+        const int h = tid >> 4, r = (tid & 15) * 8;
+        const int R = (int)mx_scale_rows(rows);
+        if (tid < 32 && inRow && row0 + r < R) {
+            const int t = col0 / kTileK, q = (col0 % kTileK) / 64 + h;
+            *reinterpret_cast<i4 *>(scales + (((int64_t)t * 4 + q) * R + row0 + r) * 2) =
+                *reinterpret_cast<const i4 *>(&sRow[h][r][0]);
+        }
+    }
+    if constexpr (COLS) {
+        const int u = tid - 64;   // another wavefront than the rows'
+        const int h = u >> 4, c = (u & 15) * 8;
+        const int R = (int)mx_scale_rows(cols);
+        if (u >= 0 && u < 32 && inCol && col0 + c < R) {
+            const int t = row0 / kTileK, q = (row0 % kTileK) / 64 + h;
+            *reinterpret_cast<i4 *>(scalesT + (((int64_t)t * 4 + q) * R + col0 + c) * 2) =
+                *reinterpret_cast<const i4 *>(&sCol[h][c][0]);
+        }
+    }
+}
+
+// A workgroup writes a 128 x 128 tile of values; `wide` as above.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void mx_dequantize_kernel(
+    const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales, int rows, int cols,
+    int tilesC, bool wide, T *__restrict__ X, int64_t sr, int64_t sc)
+{
+    __shared__ __attribute__((aligned(16))) uint8_t sRow[2][kT][2];
+    const int tid = (int)threadIdx.x;
+    const int row0 = (int)blockIdx.x / tilesC * kT, col0 = (int)blockIdx.x % tilesC * kT;
+    const int tilesK = (int)mx_tiles(cols), R = (int)mx_scale_rows(rows);
+    const int c8 = (tid % (kT / kChunk)) * kChunk, r0 = tid / (kT / kChunk);
+    const int left = cols - (col0 + c8);
+    uint32_t q[kPasses];
+#pragma unroll
+    for (int p = 0; p < kPasses; ++p) {
+        const int r = row0 + r0 + p * kRowsPass;
+        q[p] = 0;
+        if (r < rows && left > 0)
+            q[p] = *reinterpret_cast<const uint32_t *>(codes + (int64_t)r * tilesK * kTileBytes +
+                                                       (col0 + c8) / 2);
+    }
+    {
+        const int h = tid >> 4, r = (tid & 15) * 8;
+        if (tid < 32 && row0 + r < R) {
+            const int t = col0 / kTileK, b = (col0 % kTileK) / 64 + h;
+            *reinterpret_cast<i4 *>(&sRow[h][r][0]) =
+                *reinterpret_cast<const i4 *>(scales + (((int64_t)t * 4 + b) * R + row0 + r) * 2);
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int p = 0; p < kPasses; ++p) {
+        const int lr = r0 + p * kRowsPass, r = row0 + lr;
+        if (r >= rows || left <= 0) continue;
+        const uint32_t sb = sRow[c8 >> 6][lr][(c8 >> 5) & 1];
+        const float s = scale_value(sb);
+        float f[kChunk];
+        const f2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q[p], s, 0);
+        const f2 b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q[p], s, 1);
+        const f2 c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q[p], s, 2);
+        const f2 d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q[p], s, 3);
+        f[0] = a[0], f[1] = a[1], f[2] = b[0], f[3] = b[1];
+        f[4] = c[0], f[5] = c[1], f[6] = d[0], f[7] = d[1];
+        Run<T, kChunk> v;
+#pragma unroll
+        for (int i = 0; i < kChunk; ++i)
+            v.v[i] = from_float<T>(sb == 255 ? __uint_as_float(0x7fc00000u) : f[i]);
+        T *dst = X + (int64_t)r * sr + (int64_t)(col0 + c8) * sc;
+        if (wide && left >= kChunk) {
+            *reinterpret_cast<Run<T, kChunk> *>(dst) = v;
+        } else {
+#pragma unroll
+            for (int i = 0; i < kChunk; ++i)
+                if (i < left) dst[i * sc] = v.v[i];
+        }
+    }
+}
+
+template <typename T>
+hipError_t quantize_typed(int64_t rows, int64_t cols, const void *X, int64_t sr, int64_t sc,
+                          uint8_t *codes, uint8_t *scales, uint8_t *codesT, uint8_t *scalesT,
+                          unsigned blocks, int tilesC, hipStream_t stream)
+{
+    const T *x = static_cast<const T *>(X);
+    const int r = (int)rows, c = (int)cols;
+    const bool wide = sc == 1;
+    if (codes && codesT)
+        hipLaunchKernelGGL((mx_quantize_kernel<T, true, true>), dim3(blocks), dim3(kThreads), 0,
+                           stream, x, sr, sc, r, c, tilesC, wide, codes, scales, codesT, scalesT);
+    else if (codes)
+        hipLaunchKernelGGL((mx_quantize_kernel<T, true, false>), dim3(blocks), dim3(kThreads), 0,
+                           stream, x, sr, sc, r, c, tilesC, wide, codes, scales, codesT, scalesT);
+    else
+        hipLaunchKernelGGL((mx_quantize_kernel<T, false, true>), dim3(blocks), dim3(kThreads), 0,
+                           stream, x, sr, sc, r, c, tilesC, wide, codes, scales, codesT, scalesT);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t dequantize_typed(int64_t rows, int64_t cols, const void *codes, const void *scales,
+                            void *X, int64_t sr, int64_t sc, unsigned blocks, int tilesC,
+                            hipStream_t stream)
+{
+    hipLaunchKernelGGL((mx_dequantize_kernel<T>), dim3(blocks), dim3(kThreads), 0, stream,
+                       static_cast<const uint8_t *>(codes), static_cast<const uint8_t *>(scales),
+                       (int)rows, (int)cols, tilesC, sc == 1, static_cast<T *>(X), sr, sc);
+    return hipGetLastError();
+}
+
+// status of a matrix argument: extents, strides, pointer
+gett_status_t matrix_ok(gett_dtype_t dtype, int64_t rows, int64_t cols, const void *X, int64_t sr,
+                        int64_t sc)
+{
+    if (!float_type(dtype) || rows < 0 || cols < 0 || sr < 1 || sc < 1)
+        return GETT_ERROR_INVALID_VALUE;
+    if (rows > 0 && cols > 0 && (!X || (uintptr_t)X % type_size(dtype)))
+        return GETT_ERROR_INVALID_VALUE;
+    return GETT_SUCCESS;
+}
+
+}  // namespace
+
+bool packed_ok(const void *codes, const void *scales)
+{
+    return codes && scales && (uintptr_t)codes % 16 == 0 && (uintptr_t)scales % 16 == 0;
+}
+
+gett_status_t quantize_launch(gett_dtype_t dtype, int64_t rows, int64_t cols, const void *X,
+                              int64_t sr, int64_t sc, void *codes, void *scales, void *codesT,
+                              void *scalesT, hipStream_t stream)
+{
+    if (rows == 0 || cols == 0) return GETT_SUCCESS;
+    if (sr == 1 && sc != 1) {   // the transpose is read along its rows
+        std::swap(rows, cols);
+        std::swap(sr, sc);
+        std::swap(codes, codesT);
+        std::swap(scales, scalesT);
+    }
+    // enough tiles for X and for the padding of the packed rows
+    const int64_t tilesR = codesT ? 2 * mx_tiles(rows) : (rows + kT - 1) / kT;
+    const int64_t tilesC = codes ? 2 * mx_tiles(cols) : (cols + kT - 1) / kT;
+    if (tilesR * tilesC >= INT32_MAX) return GETT_ERROR_NOT_SUPPORTED;
+    const unsigned blocks = (unsigned)(tilesR * tilesC);
+    uint8_t *c = static_cast<uint8_t *>(codes), *s = static_cast<uint8_t *>(scales);
+    uint8_t *ct = static_cast<uint8_t *>(codesT), *st = static_cast<uint8_t *>(scalesT);
+    hipError_t e;
+    if (dtype == GETT_FLOAT32)
+        e = quantize_typed<float>(rows, cols, X, sr, sc, c, s, ct, st, blocks, (int)tilesC, stream);
+    else if (dtype == GETT_BFLOAT16)
+        e = quantize_typed<bf16>(rows, cols, X, sr, sc, c, s, ct, st, blocks, (int)tilesC, stream);
+    else
+        e = quantize_typed<_Float16>(rows, cols, X, sr, sc, c, s, ct, st, blocks, (int)tilesC,
+                                     stream);
+    return e == hipSuccess ? GETT_SUCCESS : GETT_ERROR_HIP;
+}
+
+}  // namespace gett
+
+extern "C" {
+
+gett_status_t gett_mx_size(int64_t rows, int64_t cols, uint64_t *code_bytes, uint64_t *scale_bytes)
+{
+    if (!code_bytes || !scale_bytes || rows < 0 || cols < 0) return GETT_ERROR_INVALID_VALUE;
+    if (rows >= gett::kMaxRows || cols >= gett::kMaxCols) return GETT_ERROR_NOT_SUPPORTED;
+    *code_bytes = (uint64_t)gett::mx_code_bytes(rows, cols);
+    *scale_bytes = (uint64_t)gett::mx_scale_bytes(rows, cols);
+    return GETT_SUCCESS;
+}
+
+gett_status_t gett_mx_quantize(gett_dtype_t dtype, int64_t rows, int64_t cols, const void *X,
+                               int64_t stride_row, int64_t stride_col, void *codes, void *scales,
+                               void *codes_t, void *scales_t, void *stream)
+{
+    using namespace gett;
+    const gett_status_t st = matrix_ok(dtype, rows, cols, X, stride_row, stride_col);
+    if (st != GETT_SUCCESS) return st;
+    const bool along = codes || scales, across = codes_t || scales_t;
+    if (rows >= kMaxRows || cols >= kMaxRows || (along && cols >= kMaxCols) ||
+        (across && rows >= kMaxCols))
+        return GETT_ERROR_NOT_SUPPORTED;
+    if (rows == 0 || cols == 0) return GETT_SUCCESS;
+    if ((!along && !across) || (along && !packed_ok(codes, scales)) ||
+        (across && !packed_ok(codes_t, scales_t)))
+        return GETT_ERROR_INVALID_VALUE;
+    const int64_t span = span_bytes(rows, cols, stride_row, stride_col, type_size(dtype));
+    if (span < 0) return GETT_ERROR_NOT_SUPPORTED;
+    const void *p[5] = {X, codes, scales, codes_t, scales_t};
+    const int64_t n[5] = {span, mx_code_bytes(rows, cols), mx_scale_bytes(rows, cols),
+                          mx_code_bytes(cols, rows), mx_scale_bytes(cols, rows)};
+    for (int i = 0; i < 5; ++i)
+        for (int j = i + 1; j < 5; ++j)
+            if (p[i] && p[j] && overlaps(p[i], n[i], p[j], n[j])) return GETT_ERROR_INVALID_VALUE;
+    return quantize_launch(dtype, rows, cols, X, stride_row, stride_col, codes, scales, codes_t,
+                           scales_t, static_cast<hipStream_t>(stream));
+}
+
+gett_status_t gett_mx_dequantize(gett_dtype_t dtype, int64_t rows, int64_t cols,
+                                 const void *codes, const void *scales, void *X,
+                                 int64_t stride_row, int64_t stride_col, void *stream)
+{
+    using namespace gett;
+    const gett_status_t st = matrix_ok(dtype, rows, cols, X, stride_row, stride_col);
+    if (st != GETT_SUCCESS) return st;
+    if (rows >= kMaxRows || cols >= kMaxCols) return GETT_ERROR_NOT_SUPPORTED;
+    if (rows == 0 || cols == 0) return GETT_SUCCESS;
+    if (!packed_ok(codes, scales)) return GETT_ERROR_INVALID_VALUE;
+    const int64_t span = span_bytes(rows, cols, stride_row, stride_col, type_size(dtype));
+    if (span < 0 || !matrix_injective(rows, cols, stride_row, stride_col))
+        return GETT_ERROR_NOT_SUPPORTED;
+    if (overlaps(X, span, codes, mx_code_bytes(rows, cols)) ||
+        overlaps(X, span, scales, mx_scale_bytes(rows, cols)))
+        return GETT_ERROR_INVALID_VALUE;
+    const int64_t tilesC = (cols + kT - 1) / kT, tiles = (rows + kT - 1) / kT * tilesC;
+    if (tiles >= INT32_MAX) return GETT_ERROR_NOT_SUPPORTED;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    hipError_t e;
+    if (dtype == GETT_FLOAT32)
+        e = dequantize_typed<float>(rows, cols, codes, scales, X, stride_row, stride_col,
+                                    (unsigned)tiles, (int)tilesC, s);
+    else if (dtype == GETT_BFLOAT16)
+        e = dequantize_typed<bf16>(rows, cols, codes, scales, X, stride_row, stride_col,
+                                   (unsigned)tiles, (int)tilesC, s);
+    else
+        e = dequantize_typed<_Float16>(rows, cols, codes, scales, X, stride_row, stride_col,
+                                       (unsigned)tiles, (int)tilesC, s);
+    return e == hipSuccess ? GETT_SUCCESS : GETT_ERROR_HIP;
+}
+
+}  // extern "C"
