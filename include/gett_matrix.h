@@ -38,8 +38,8 @@
  *
  *   codes   rows x 128 T bytes, row after row: two codes (sign, two exponent
  *           bits, one mantissa bit) a byte, the even column in the low half.
- *   scales  T x 4 x R x 2 bytes, R = rows rounded up to 16: byte
- *           ((t * 4 + b / 2) * R + row) * 2 + b % 2 is the scale of block b
+ *   scales  T x 2 x R x 4 bytes, R = rows rounded up to 16: byte
+ *           ((t * 2 + b / 4) * R + row) * 4 + b % 4 is the scale of block b
  *           (columns 256 t + 32 b and 31 more) of `row`, as exponent + 127;
  *           255 is NaN.  The bytes of rows >= `rows` may hold anything.
  *

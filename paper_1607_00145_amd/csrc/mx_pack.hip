@@ -14,7 +14,7 @@
 // exchanges.  For the transposed packing the tile passes through LDS
 // (unrounded, in X's own type) and a lane takes 32 rows of one column; four
 // lanes take one column's four blocks, so 64 bytes of a row of codes_t leave
-// together.  Scales are gathered in LDS and leave in runs of 256 bytes.
+// together.  Scales are gathered in LDS and leave in runs of 512 bytes.
 #include "matrix.hpp"
 
 namespace gett {
@@ -51,9 +51,9 @@ __global__ __launch_bounds__(kThreads) void mx_quantize_kernel(
     uint8_t *__restrict__ scalesT)
 {
     __shared__ __attribute__((aligned(16))) T tile[COLS ? kT * kT + 3 * (32 / sizeof(T)) : 1];
-    // [pair of blocks][row or column][block of the pair]
-    __shared__ __attribute__((aligned(16))) uint8_t sRow[ROWS ? 2 : 1][kT][2];
-    __shared__ __attribute__((aligned(16))) uint8_t sCol[COLS ? 2 : 1][kT][2];
+    // [row or column][block]
+    __shared__ __attribute__((aligned(16))) uint8_t sRow[ROWS ? kT : 1][4];
+    __shared__ __attribute__((aligned(16))) uint8_t sCol[COLS ? kT : 1][4];
 
     const int tid = (int)threadIdx.x;
     const int tr = (int)blockIdx.x / tilesC, tc = (int)blockIdx.x % tilesC;
@@ -102,7 +102,7 @@ __global__ __launch_bounds__(kThreads) void mx_quantize_kernel(
             if (inRow && row0 + lr < rows)
                 *reinterpret_cast<uint32_t *>(codes + (int64_t)(row0 + lr) * tilesK * kTileBytes +
                                               (col0 + c8) / 2) = q;
-            if ((tid & 3) == 0) sRow[(c8 >> 6)][lr][(c8 >> 5) & 1] = (uint8_t)sb;
+            if ((tid & 3) == 0) sRow[lr][c8 >> 5] = (uint8_t)sb;
         }
     }
     __syncthreads();
@@ -125,29 +125,22 @@ __global__ __launch_bounds__(kThreads) void mx_quantize_kernel(
             if (inCol && col0 + c < cols)
                 *reinterpret_cast<i4 *>(codesT + (int64_t)(col0 + c) * tilesKT * kTileBytes +
                                         row0 / 2 + b * 16) = q;
-            sCol[b >> 1][c][b & 1] = (uint8_t)sb;
+            sCol[c][b] = (uint8_t)sb;
         }
         __syncthreads();
     }
-    // scales: two runs of 128 pairs, one 16-byte piece (eight rows) a thread
+    // scales: a run of 512 bytes, one 16-byte piece (four rows) a thread
     if constexpr (ROWS) {
-        const int h = tid >> 4, r = (tid & 15) * 8;
-        const int R = (int)mx_scale_rows(rows);
-        if (tid < 32 && inRow && row0 + r < R) {
-            const int t = col0 / kTileK, q = (col0 % kTileK) / 64 + h;
-            *reinterpret_cast<i4 *>(scales + (((int64_t)t * 4 + q) * R + row0 + r) * 2) =
-                *reinterpret_cast<const i4 *>(&sRow[h][r][0]);
-        }
+        const int r = tid * 4, R = (int)mx_scale_rows(rows);
+        if (tid < 32 && inRow && row0 + r < R)
+            *reinterpret_cast<i4 *>(scales + ((int64_t)(col0 / kT) * R + row0 + r) * 4) =
+                *reinterpret_cast<const i4 *>(&sRow[r][0]);
     }
     if constexpr (COLS) {
-        const int u = tid - 64;   // another wavefront than the rows'
-        const int h = u >> 4, c = (u & 15) * 8;
-        const int R = (int)mx_scale_rows(cols);
-        if (u >= 0 && u < 32 && inCol && col0 + c < R) {
-            const int t = row0 / kTileK, q = (row0 % kTileK) / 64 + h;
-            *reinterpret_cast<i4 *>(scalesT + (((int64_t)t * 4 + q) * R + col0 + c) * 2) =
-                *reinterpret_cast<const i4 *>(&sCol[h][c][0]);
-        }
+        const int c = (tid - 64) * 4, R = (int)mx_scale_rows(cols);   // another wavefront
+        if (c >= 0 && c < kT && inCol && col0 + c < R)
+            *reinterpret_cast<i4 *>(scalesT + ((int64_t)(row0 / kT) * R + col0 + c) * 4) =
+                *reinterpret_cast<const i4 *>(&sCol[c][0]);
     }
 }
 
@@ -157,7 +150,7 @@ __global__ __launch_bounds__(kThreads) void mx_dequantize_kernel(
     const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales, int rows, int cols,
     int tilesC, bool wide, T *__restrict__ X, int64_t sr, int64_t sc)
 {
-    __shared__ __attribute__((aligned(16))) uint8_t sRow[2][kT][2];
+    __shared__ __attribute__((aligned(16))) uint8_t sRow[kT][4];
     const int tid = (int)threadIdx.x;
     const int row0 = (int)blockIdx.x / tilesC * kT, col0 = (int)blockIdx.x % tilesC * kT;
     const int tilesK = (int)mx_tiles(cols), R = (int)mx_scale_rows(rows);
@@ -172,20 +165,15 @@ __global__ __launch_bounds__(kThreads) void mx_dequantize_kernel(
             q[p] = *reinterpret_cast<const uint32_t *>(codes + (int64_t)r * tilesK * kTileBytes +
                                                        (col0 + c8) / 2);
     }
-    {
-        const int h = tid >> 4, r = (tid & 15) * 8;
-        if (tid < 32 && row0 + r < R) {
-            const int t = col0 / kTileK, b = (col0 % kTileK) / 64 + h;
-            *reinterpret_cast<i4 *>(&sRow[h][r][0]) =
-                *reinterpret_cast<const i4 *>(scales + (((int64_t)t * 4 + b) * R + row0 + r) * 2);
-        }
-    }
+    if (tid < 32 && row0 + tid * 4 < R)
+        *reinterpret_cast<i4 *>(&sRow[tid * 4][0]) =
+            *reinterpret_cast<const i4 *>(scales + ((int64_t)(col0 / kT) * R + row0 + tid * 4) * 4);
     __syncthreads();
 #pragma unroll
     for (int p = 0; p < kPasses; ++p) {
         const int lr = r0 + p * kRowsPass, r = row0 + lr;
         if (r >= rows || left <= 0) continue;
-        const uint32_t sb = sRow[c8 >> 6][lr][(c8 >> 5) & 1];
+        const uint32_t sb = sRow[lr][c8 >> 5];
         const float s = scale_value(sb);
         float f[kChunk];
         const f2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q[p], s, 0);

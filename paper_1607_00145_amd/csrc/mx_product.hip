@@ -73,7 +73,7 @@ __global__ __launch_bounds__(S::THREADS) void mx_tile_kernel(PanelOperand A, Pan
     p.init();
     p.run(dyn_lds, A, B, 0, panels);
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
+    for (int e = 0; e < 16; ++e)
 #pragma unroll
         for (int i = 0; i < S::FM; ++i) {
             float v[S::FN];
@@ -120,7 +120,8 @@ template <int FM> struct FewPacked {
                                                        q * 32);
             f.v[i][0] = p[0];
             f.v[i][1] = p[1];
-            f.s[i] = *reinterpret_cast<const uint16_t *>(scales + ((t * 4 + q) * R + row) * 2);
+            f.s[i] = *reinterpret_cast<const uint16_t *>(
+                scales + ((t * 2 + (q >> 1)) * R + row) * 4 + (q & 1) * 2);
         }
     }
 };
@@ -184,12 +185,11 @@ __global__ __launch_bounds__(kFewWaves * 64) void mx_few_kernel(LA A, const uint
         const int row = col0 + FN * r + j < o.n ? col0 + FN * r + j : o.n - 1;
         pb[j] = codesB + (int64_t)row * panels * kTileBytes + q * 32;
     }
-    int64_t rs = col0 + FN * r;
-    rs = rs < R - FN ? rs : R - FN;
+    const int64_t rs = col0 + FN * r < R ? col0 + FN * r : R - FN;
     f4 acc[FM][FN] = {};
     for (int t0 = wave; t0 < panels; t0 += kFewWaves * DEEP) {
         i4 b[DEEP][FN][2];
-        int sb[DEEP];
+        f2 sb[DEEP];   // a word of four scales per row
         typename LA::Frag a[DEEP];
 #pragma unroll
         for (int u = 0; u < DEEP; ++u) {
@@ -201,7 +201,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void mx_few_kernel(LA A, const uint
                     b[u][j][0] = p[0];
                     b[u][j][1] = p[1];
                 }
-                sb[u] = *reinterpret_cast<const int *>(scalesB + ((t * 4 + q) * R + rs) * 2);
+                sb[u] = *reinterpret_cast<const f2 *>(scalesB + ((t * 2 + (q >> 1)) * R + rs) * 4);
             }
         }
 #pragma unroll
@@ -212,12 +212,15 @@ __global__ __launch_bounds__(kFewWaves * 64) void mx_few_kernel(LA A, const uint
 #pragma unroll
         for (int u = 0; u < DEEP; ++u) {
             if (t0 + u * kFewWaves >= panels) break;
+            // this lane group's two scales of the word
+            const int s0 = (int)(__float_as_uint(sb[u][0]) >> ((q & 1) * 16));
+            const int s1 = (int)(__float_as_uint(sb[u][1]) >> ((q & 1) * 16));
 #pragma unroll
             for (int i = 0; i < FM; ++i) {
-                acc[i][0] = mfma_mx<0, 0>(a[u].v[i][0], b[u][0][0], acc[i][0], a[u].s[i], sb[u]);
-                acc[i][0] = mfma_mx<1, 1>(a[u].v[i][1], b[u][0][1], acc[i][0], a[u].s[i], sb[u]);
-                acc[i][1] = mfma_mx<0, 2>(a[u].v[i][0], b[u][1][0], acc[i][1], a[u].s[i], sb[u]);
-                acc[i][1] = mfma_mx<1, 3>(a[u].v[i][1], b[u][1][1], acc[i][1], a[u].s[i], sb[u]);
+                acc[i][0] = mfma_mx16<0, 0>(a[u].v[i][0], b[u][0][0], acc[i][0], a[u].s[i], s0);
+                acc[i][0] = mfma_mx16<1, 1>(a[u].v[i][1], b[u][0][1], acc[i][0], a[u].s[i], s0);
+                acc[i][1] = mfma_mx16<0, 0>(a[u].v[i][0], b[u][1][0], acc[i][1], a[u].s[i], s1);
+                acc[i][1] = mfma_mx16<1, 1>(a[u].v[i][1], b[u][1][1], acc[i][1], a[u].s[i], s1);
             }
         }
     }
@@ -282,9 +285,9 @@ hipError_t contract_typed(Packed A, Packed B, int64_t k, const Result<T> &out, h
     const PanelOperand pb = {cb, sb, (int64_t)panels * kTileBytes, o.n, 0};
     const int64_t big = (int64_t)((o.m + 255) / 256) * ((o.n + 255) / 256);
     const int64_t mid = (int64_t)((o.m + 127) / 128) * ((o.n + 127) / 128);
-    if (big >= 256) return tile_launch<T, PanelShape<8, 4, 2, 4>>(pa, pb, panels, o, stream);
-    if (mid >= 256) return tile_launch<T, PanelShape<4, 4, 2, 2>>(pa, pb, panels, o, stream);
-    return tile_launch<T, PanelShape<2, 2, 2, 2>>(pa, pb, panels, o, stream);
+    if (big >= 256) return tile_launch<T, PanelShape<2, 4, 4, 2>>(pa, pb, panels, o, stream);
+    if (mid >= 256) return tile_launch<T, PanelShape<2, 2, 2, 2>>(pa, pb, panels, o, stream);
+    return tile_launch<T, PanelShape<1, 1, 2, 2>>(pa, pb, panels, o, stream);
 }
 
 template <typename T>

@@ -239,7 +239,7 @@ __global__ __launch_bounds__(S::THREADS) void orth_product_kernel(ProductArgs d,
     char *out = d.out + z * d.stackOut;
     const char *addend = STEP == kGram ? nullptr : d.addend + z * d.stackOut;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
+    for (int e = 0; e < 16; ++e) {
         const int row0 = A.row0 + p.row(0, e);   // FM neighbouring rows
 #pragma unroll
         for (int i = 0; i < FM; ++i) {
@@ -327,9 +327,9 @@ hipError_t product_launch(ProductArgs d, const Stack<T> &O, int64_t batch, hipSt
 }
 
 // Square tiles (the symmetric products mirror them).
-typedef PanelShape<8, 4, 2, 4> Big;
-typedef PanelShape<4, 4, 2, 2> Mid;
-typedef PanelShape<2, 2, 2, 2> Small;
+typedef PanelShape<2, 4, 4, 2> Big;
+typedef PanelShape<2, 2, 2, 2> Mid;
+typedef PanelShape<1, 1, 2, 2> Small;
 
 template <int KIND, int STEP, typename T>
 hipError_t product(const ProductArgs &d, const Stack<T> &O, int64_t batch, hipStream_t stream)
