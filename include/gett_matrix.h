@@ -36,16 +36,18 @@
  * or a NaN gets the NaN scale and stands for 32 NaNs.  Columns are padded with
  * zeros to T = ceil(cols / 256) tiles of 256.
  *
- *   codes   rows x 128 T bytes, row after row: two codes (sign, two exponent
- *           bits, one mantissa bit) a byte, the even column in the low half.
+ *   codes   T x rows x 128 bytes, tile after tile and in it row after row: two
+ *           codes (sign, two exponent bits, one mantissa bit) a byte, the even
+ *           column in the low half.
  *   scales  T x 2 x R x 4 bytes, R = rows rounded up to 16: byte
  *           ((t * 2 + b / 4) * R + row) * 4 + b % 4 is the scale of block b
  *           (columns 256 t + 32 b and 31 more) of `row`, as exponent + 127;
  *           255 is NaN.  The bytes of rows >= `rows` may hold anything.
  *
- * Both pointers are aligned to 16 bytes.  The scales lie in the order in
- * which a wavefront takes them: the scales of one lane's rows and blocks are
- * neighbours, so they reach its registers in one load per tile.
+ * Both pointers are aligned to 16 bytes.  A product takes one tile of columns
+ * of many rows at a time: tile after tile these are neighbours in memory (row
+ * after row they would lie a power of two apart, on few memory channels), and
+ * the scales of one lane's rows and blocks reach its registers in one load.
  */
 #ifndef GETT_MATRIX_H
 #define GETT_MATRIX_H

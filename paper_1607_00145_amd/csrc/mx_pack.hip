@@ -35,6 +35,12 @@ __device__ __forceinline__ uint32_t quad_max(uint32_t v)
 
 __device__ __forceinline__ uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
 
+// the byte of column c of row r among the codes
+__device__ __forceinline__ int64_t code_offset(int rows, int r, int c)
+{
+    return ((int64_t)(c / kTileK) * rows + r) * kTileBytes + (c % kTileK) / 2;
+}
+
 // LDS address (elements) of tile element (r, c): rows follow one another,
 // with 32 bytes of skew after every 32 rows, so that the lanes that read four
 // blocks of one column fall on different banks.
@@ -100,8 +106,7 @@ __global__ __launch_bounds__(kThreads) void mx_quantize_kernel(
             const uint32_t sb = scale_byte(quad_max(top));
             const uint32_t q = codes8(f, scale_value(sb));
             if (inRow && row0 + lr < rows)
-                *reinterpret_cast<uint32_t *>(codes + (int64_t)(row0 + lr) * tilesK * kTileBytes +
-                                              (col0 + c8) / 2) = q;
+                *reinterpret_cast<uint32_t *>(codes + code_offset(rows, row0 + lr, col0 + c8)) = q;
             if ((tid & 3) == 0) sRow[lr][c8 >> 5] = (uint8_t)sb;
         }
     }
@@ -123,8 +128,7 @@ __global__ __launch_bounds__(kThreads) void mx_quantize_kernel(
 #pragma unroll
             for (int i = 0; i < 4; ++i) q[i] = (int)codes8(f + 8 * i, s);
             if (inCol && col0 + c < cols)
-                *reinterpret_cast<i4 *>(codesT + (int64_t)(col0 + c) * tilesKT * kTileBytes +
-                                        row0 / 2 + b * 16) = q;
+                *reinterpret_cast<i4 *>(codesT + code_offset(cols, col0 + c, row0 + b * 32)) = q;
             sCol[c][b] = (uint8_t)sb;
         }
         __syncthreads();
@@ -153,7 +157,7 @@ __global__ __launch_bounds__(kThreads) void mx_dequantize_kernel(
     __shared__ __attribute__((aligned(16))) uint8_t sRow[kT][4];
     const int tid = (int)threadIdx.x;
     const int row0 = (int)blockIdx.x / tilesC * kT, col0 = (int)blockIdx.x % tilesC * kT;
-    const int tilesK = (int)mx_tiles(cols), R = (int)mx_scale_rows(rows);
+    const int R = (int)mx_scale_rows(rows);
     const int c8 = (tid % (kT / kChunk)) * kChunk, r0 = tid / (kT / kChunk);
     const int left = cols - (col0 + c8);
     uint32_t q[kPasses];
@@ -162,8 +166,7 @@ __global__ __launch_bounds__(kThreads) void mx_dequantize_kernel(
         const int r = row0 + r0 + p * kRowsPass;
         q[p] = 0;
         if (r < rows && left > 0)
-            q[p] = *reinterpret_cast<const uint32_t *>(codes + (int64_t)r * tilesK * kTileBytes +
-                                                       (col0 + c8) / 2);
+            q[p] = *reinterpret_cast<const uint32_t *>(codes + code_offset(rows, r, col0 + c8));
     }
     if (tid < 32 && row0 + tid * 4 < R)
         *reinterpret_cast<i4 *>(&sRow[tid * 4][0]) =

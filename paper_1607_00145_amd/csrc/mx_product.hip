@@ -105,7 +105,7 @@ constexpr int kFewCols = 32;
 // A's side of one panel: FM fragments of two pieces, and their scales
 template <int FM> struct FewPacked {
     const uint8_t *codes, *scales;
-    int m, panels;
+    int m;
     struct Frag {
         i4 v[FM][2];
         int s[FM];   // the scales of both pieces in the low 16 bits
@@ -116,8 +116,8 @@ template <int FM> struct FewPacked {
 #pragma unroll
         for (int i = 0; i < FM; ++i) {
             const int row = FM * r + i < m ? FM * r + i : m - 1;
-            const i4 *p = reinterpret_cast<const i4 *>(codes + ((int64_t)row * panels + t) * kTileBytes +
-                                                       q * 32);
+            const i4 *p =
+                reinterpret_cast<const i4 *>(codes + ((int64_t)t * m + row) * kTileBytes + q * 32);
             f.v[i][0] = p[0];
             f.v[i][1] = p[1];
             f.s[i] = *reinterpret_cast<const uint16_t *>(
@@ -183,7 +183,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void mx_few_kernel(LA A, const uint
 #pragma unroll
     for (int j = 0; j < FN; ++j) {
         const int row = col0 + FN * r + j < o.n ? col0 + FN * r + j : o.n - 1;
-        pb[j] = codesB + (int64_t)row * panels * kTileBytes + q * 32;
+        pb[j] = codesB + (int64_t)row * kTileBytes + q * 32;
     }
     const int64_t rs = col0 + FN * r < R ? col0 + FN * r : R - FN;
     f4 acc[FM][FN] = {};
@@ -197,7 +197,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void mx_few_kernel(LA A, const uint
             if (t < panels) {
 #pragma unroll
                 for (int j = 0; j < FN; ++j) {
-                    const i4 *p = reinterpret_cast<const i4 *>(pb[j] + (int64_t)t * kTileBytes);
+                    const i4 *p = reinterpret_cast<const i4 *>(pb[j] + (int64_t)t * o.n * kTileBytes);
                     b[u][j][0] = p[0];
                     b[u][j][1] = p[1];
                 }
@@ -278,11 +278,11 @@ hipError_t contract_typed(Packed A, Packed B, int64_t k, const Result<T> &out, h
     const uint8_t *cb = static_cast<const uint8_t *>(B.codes);
     const uint8_t *sb = static_cast<const uint8_t *>(B.scales);
     if (panels > 0 && o.m <= 16)
-        return few_launch<T, FewPacked<1>, 1>({ca, sa, o.m, panels}, cb, sb, panels, o, stream);
+        return few_launch<T, FewPacked<1>, 1>({ca, sa, o.m}, cb, sb, panels, o, stream);
     if (panels > 0 && o.m <= 32)
-        return few_launch<T, FewPacked<2>, 2>({ca, sa, o.m, panels}, cb, sb, panels, o, stream);
-    const PanelOperand pa = {ca, sa, (int64_t)panels * kTileBytes, o.m, 0};
-    const PanelOperand pb = {cb, sb, (int64_t)panels * kTileBytes, o.n, 0};
+        return few_launch<T, FewPacked<2>, 2>({ca, sa, o.m}, cb, sb, panels, o, stream);
+    const PanelOperand pa = {ca, sa, o.m, 0};
+    const PanelOperand pb = {cb, sb, o.n, 0};
     const int64_t big = (int64_t)((o.m + 255) / 256) * ((o.n + 255) / 256);
     const int64_t mid = (int64_t)((o.m + 127) / 128) * ((o.n + 127) / 128);
     if (big >= 256) return tile_launch<T, PanelShape<2, 4, 4, 2>>(pa, pb, panels, o, stream);

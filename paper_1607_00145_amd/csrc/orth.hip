@@ -42,10 +42,10 @@ constexpr int kNormBlocks = 256;   // at most, per matrix; one partial sum each
 // numbers and then their low parts (slab 0 takes the even pieces of a panel,
 // slab 1 the odd ones).
 template <int KIND> __host__ __device__ inline int panel_elements() { return KIND == kPanelSplit ? 32 : 64; }
-template <int KIND> __host__ __device__ inline int64_t row_bytes(int64_t k)
+template <int KIND> inline int64_t panel_count(int64_t k)
 {
     const int e = panel_elements<KIND>();
-    return (k + e - 1) / e * 128;
+    return (k + e - 1) / e;
 }
 // columns of a row, padding included
 template <int KIND> __host__ __device__ inline int padded(int k)
@@ -53,10 +53,12 @@ template <int KIND> __host__ __device__ inline int padded(int k)
     const int e = panel_elements<KIND>();
     return (k + e - 1) / e * e;
 }
-// the byte offset of column k in its row
-template <int KIND> __device__ __forceinline__ int64_t at_col(int k)
+// the byte of column k of a row in a matrix of `rows` rows
+template <int KIND> __device__ __forceinline__ int64_t at(int rows, int row, int k)
 {
-    return KIND == kPanelSplit ? (int64_t)(k >> 3) * 32 + (k & 7) * 2 : (int64_t)k * 2;
+    const int e = panel_elements<KIND>(), in = k % e;
+    return ((int64_t)(k / e) * rows + row) * 128 +
+           (KIND == kPanelSplit ? (in >> 3) * 32 + (in & 7) * 2 : in * 2);
 }
 
 // N neighbours (N divides 8 and the column): held values are 2^12 x
@@ -158,7 +160,6 @@ __global__ __launch_bounds__(kNormThreads) void orth_start_kernel(
         tile[i][k] = v;
     }
     __syncthreads();
-    const int64_t pitch = row_bytes<KIND>(n), pitchT = row_bytes<KIND>(m);
 #pragma unroll
     for (int u = 0; u < kStart * kStart / 8 / kNormThreads; ++u) {
         const int e = u * kNormThreads + tid;
@@ -167,12 +168,12 @@ __global__ __launch_bounds__(kNormThreads) void orth_start_kernel(
         if (i0 + a < m && k0 + c < padded<KIND>(n)) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = tile[a][c + i];
-            store_run<KIND, 8>(X + z * stackX + (i0 + a) * pitch + at_col<KIND>(k0 + c), v);
+            store_run<KIND, 8>(X + z * stackX + at<KIND>(m, i0 + a, k0 + c), v);
         }
         if (k0 + a < n && i0 + c < padded<KIND>(m)) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = tile[c + i][a];
-            store_run<KIND, 8>(XT + z * stackXT + (k0 + a) * pitchT + at_col<KIND>(i0 + c), v);
+            store_run<KIND, 8>(XT + z * stackXT + at<KIND>(n, k0 + a, i0 + c), v);
         }
     }
 }
@@ -187,7 +188,7 @@ __global__ __launch_bounds__(256) void orth_copy_kernel(const char *X, int64_t s
     const int64_t z = e / ((int64_t)m * n), rest = e % ((int64_t)m * n);
     const int i = (int)(rest / n), k = (int)(rest % n);
     float v;
-    load_run<KIND, 1>(X + z * stackX + i * row_bytes<KIND>(n) + at_col<KIND>(k), &v);
+    load_run<KIND, 1>(X + z * stackX + at<KIND>(m, i, k), &v);
     O.p[z * O.sb + i * O.si + k * O.sk] = from_float<T>(v * kDown);
 }
 
@@ -197,7 +198,7 @@ enum Step { kGram, kPoly, kUpdate, kLast };
 
 struct ProductArgs {
     const char *P, *Q;          // the operands, K along their rows
-    int64_t pitch, stackP, stackQ;
+    int64_t stackP, stackQ;
     int m, n, panels;           // rows of P, rows of Q, panels of a row
     int tilesM, tilesN, tiles;  // tiles of one matrix
     const char *addend;         // Poly: S; Update, Last: X; [row][col] as `out`
@@ -225,15 +226,14 @@ __global__ __launch_bounds__(S::THREADS) void orth_product_kernel(ProductArgs d,
     constexpr bool kSymmetric = STEP == kGram || STEP == kPoly;
     if constexpr (kSymmetric) triangle_tile(t, tm, tn);
     else panel_tile(t, d.tilesM, d.tilesN, 4, tm, tn);
-    const PanelOperand A = {reinterpret_cast<const uint8_t *>(d.P) + z * d.stackP, nullptr, d.pitch,
-                            d.m, tm * S::BM};
-    const PanelOperand B = {reinterpret_cast<const uint8_t *>(d.Q) + z * d.stackQ, nullptr, d.pitch,
-                            d.n, tn * S::BN};
+    const PanelOperand A = {reinterpret_cast<const uint8_t *>(d.P) + z * d.stackP, nullptr, d.m,
+                            tm * S::BM};
+    const PanelOperand B = {reinterpret_cast<const uint8_t *>(d.Q) + z * d.stackQ, nullptr, d.n,
+                            tn * S::BN};
     Panel<KIND, S> p;
     p.init();
     p.run(dyn_lds, A, B, 0, d.panels);
 
-    const int64_t pitch = row_bytes<KIND>(d.n), pitchT = row_bytes<KIND>(d.m);
     const int padN = padded<KIND>(d.n), padM = padded<KIND>(d.m);
     const int col = B.row0 + p.col(0);
     char *out = d.out + z * d.stackOut;
@@ -249,7 +249,7 @@ __global__ __launch_bounds__(S::THREADS) void orth_product_kernel(ProductArgs d,
             for (int j = 0; j < FN; ++j) x[j] = 0.0f;
             if constexpr (STEP != kGram)
                 if (row < d.m && col < padN)
-                    load_run<KIND, FN>(addend + row * pitch + at_col<KIND>(col), x);
+                    load_run<KIND, FN>(addend + at<KIND>(d.m, row, col), x);
 #pragma unroll
             for (int j = 0; j < FN; ++j) {
                 // rows and columns of the padding are zeros
@@ -262,7 +262,7 @@ __global__ __launch_bounds__(S::THREADS) void orth_product_kernel(ProductArgs d,
 #pragma unroll
                 for (int j = 0; j < FN; ++j) v[j] = p.acc[i][j][e];
                 if (row < d.m && col < padN)
-                    store_run<KIND, FN>(out + row * pitch + at_col<KIND>(col), v);
+                    store_run<KIND, FN>(out + at<KIND>(d.m, row, col), v);
             } else if (O.si != 1 || O.sk == 1) {
                 T *o = O.p + z * O.sb + row * O.si + col * O.sk;
                 if (row < d.m && O.sk == 1 && col + FN <= d.n) {
@@ -287,7 +287,7 @@ __global__ __launch_bounds__(S::THREADS) void orth_product_kernel(ProductArgs d,
 #pragma unroll
                     for (int i = 0; i < FM; ++i) v[i] = p.acc[i][j][e];
                     if (col + j < d.n && row0 < padM)
-                        store_run<KIND, FM>(outT + (col + j) * pitchT + at_col<KIND>(row0), v);
+                        store_run<KIND, FM>(outT + at<KIND>(d.n, col + j, row0), v);
                 }
             }
         } else if (O.si == 1 && O.sk != 1) {
@@ -355,8 +355,8 @@ template <typename T, int KIND>
 gett_status_t orthogonalize_typed(const Problem &P, Stack<const T> G, Stack<T> O)
 {
     const int m = P.m, n = P.n;
-    const int64_t pitchX = row_bytes<KIND>(n), pitchS = row_bytes<KIND>(m);
-    const int64_t X = m * pitchX, XT = n * pitchS, SS = m * pitchS;
+    const int64_t panelsX = panel_count<KIND>(n), panelsS = panel_count<KIND>(m);
+    const int64_t X = m * panelsX * 128, XT = n * panelsS * 128, SS = m * panelsS * 128;
     // the norm reads along the smaller stride
     const bool along = G.sk <= G.si;
     const int outer = along ? m : n, inner = along ? n : m;
@@ -395,19 +395,17 @@ gett_status_t orthogonalize_typed(const Problem &P, Stack<const T> G, Stack<T> O
     for (int i = 0; i < P.steps; ++i) {
         ProductArgs d = {};
         d.P = d.Q = x;
-        d.pitch = pitchX;
         d.stackP = d.stackQ = X;
         d.m = d.n = m;
-        d.panels = (int)(pitchX / 128);
+        d.panels = (int)panelsX;
         d.out = d.outT = s;
         d.stackOut = d.stackOutT = SS;
         d.factor = kDown;
         e = product<KIND, kGram, T>(d, none, P.batch, P.stream);
         if (e != hipSuccess) return GETT_ERROR_HIP;
         d.P = d.Q = d.addend = s;
-        d.pitch = pitchS;
         d.stackP = d.stackQ = SS;
-        d.panels = (int)(pitchS / 128);
+        d.panels = (int)panelsS;
         d.out = d.outT = poly;
         d.scale = (float)P.b;
         d.factor = (float)(P.c * kDown);

@@ -1,8 +1,11 @@
 // panel.hpp -- the product core of the matrix operators (device code):
 // acc[i][j] = sum over K of row i of one operand times row j of another.
 //
-// Both operands lie row after row with K along the row, cut into panels of 128
-// bytes: eight 16-byte pieces, taken as four slabs of two pieces, slab s the
+// Both operands are cut along K into panels of 128 bytes a row; a panel's rows
+// follow one another in memory, panel after panel (row after row, the rows of
+// a panel would lie a power of two apart and share few L2 channels: 181 us for
+// the half-precision product 4096^3 that takes XXX this way).  A row's 128 bytes
+// are eight 16-byte pieces, taken as four slabs of two pieces, slab s the
 // pieces s and s + 4.  One MFMA 32 x 32 takes a slab of 32 rows of each operand
 // (16 bytes a lane: lane l gives row l % 32, piece 4 (l / 32) + s), whatever
 // the bytes stand for:
@@ -68,14 +71,21 @@ template <int FM_, int FN_, int WM_, int WN_> struct PanelShape {
 };
 
 // One operand of a tile: rows [row0, row0 + tile rows) of a matrix of `rows`
-// rows, `pitch` bytes apart (a multiple of 128).  Rows past the last read the
-// last one again; their results are not stored.
+// rows.  Rows past the last read the last one again; their results are not
+// stored.
 struct PanelOperand {
-    const uint8_t *data;     // row 0
+    const uint8_t *data;     // panel 0, row 0
     const uint8_t *scales;   // Mx: the packed scales
-    int64_t pitch;
     int rows, row0;
-    __device__ __forceinline__ const uint8_t *tile() const { return data + (int64_t)row0 * pitch; }
+    // rows row0 ... of panel t, and nothing behind the panel's last row
+    __device__ __forceinline__ __amdgpu_buffer_rsrc_t panel(int t) const
+    {
+        const uint8_t *p = data + ((int64_t)t * rows + row0) * 128;
+        const int64_t bytes = (int64_t)(rows - row0) * 128;
+        return __builtin_amdgcn_make_buffer_rsrc(
+            const_cast<uint8_t *>(p), 0, (int)(uint32_t)(bytes < 0xffffffffll ? bytes : 0xffffffffll),
+            0x00027000);
+    }
 };
 
 typedef float f16v __attribute__((ext_vector_type(16)));
@@ -148,13 +158,6 @@ template <int KIND, typename S> struct Panel {
     }
     __device__ __forceinline__ int col(int j) const { return wn * 32 * FN + FN * r + j; }
 
-    static __device__ __forceinline__ __amdgpu_buffer_rsrc_t resource(const PanelOperand &o)
-    {
-        const int64_t bytes = (int64_t)(o.rows - o.row0) * o.pitch;
-        return __builtin_amdgcn_make_buffer_rsrc(
-            const_cast<uint8_t *>(o.tile()), 0,
-            (int)(uint32_t)(bytes < 0xffffffffll ? bytes : 0xffffffffll), 0x00027000);
-    }
     // panels [t0, t1) of both operands; `lds` holds S::LDS bytes
     __device__ __forceinline__ void run(char *lds, const PanelOperand &A, const PanelOperand &B,
                                         int t0, int t1)
@@ -172,22 +175,20 @@ template <int KIND, typename S> struct Panel {
             const int x = 2 * pair / F;   // the lane r of the pair's rows (F = 1: of the first)
             const int p = (lane & 15) ^ (F > 1 ? x & 15 : (x >> 1) & 7);
             const int row = 2 * pair + (p >> 3), last = (isA ? A.rows - A.row0 : B.rows - B.row0) - 1;
-            off[j] = (uint32_t)(row < last ? row : last) * (uint32_t)(isA ? A.pitch : B.pitch) +
-                     (uint32_t)(p & 7) * 16;
+            off[j] = (uint32_t)(row < last ? row : last) * 128 + (uint32_t)(p & 7) * 16;
         }
-        // buffer loads: a lane's offset stays, the panel's is a scalar.  Reads
-        // past the matrix's end (none are made) would return zeros.
-        const __amdgpu_buffer_rsrc_t ra = resource(A), rb = resource(B);
-        int at = t0 * 128;
+        // buffer loads: a lane's offset stays, the panel's base is a scalar
+        int at = t0;
         auto issue = [&](int stage) {
+            const __amdgpu_buffer_rsrc_t ra = A.panel(at), rb = B.panel(at);
 #pragma unroll
             for (int j = 0; j < J; ++j) {
                 char *dst = lds + stage * S::STAGE + (j < JA ? 0 : S::BM * 128) +
                             ((j < JA ? j : j - JA) * NW + wave) * 1024;
                 __builtin_amdgcn_raw_ptr_buffer_load_lds(j < JA ? ra : rb, (matrix_lds *)dst, 16,
-                                                         (int)off[j], at, 0, 0);
+                                                         (int)off[j], 0, 0, 0);
             }
-            at += 128;
+            ++at;
         };
         // scales of panel t: a lane's are neighbours (gett_matrix.h)
         PanelScales<FM> sa, nextA;
@@ -300,11 +301,11 @@ template <int KIND, typename S> struct Panel {
                 constexpr int READS = G * (FM + FN);
                 constexpr int MFMAS = FM * FN * (KIND == kPanelSplit ? 3 : 1);
                 if constexpr (s + 1 < STEPS || more) {
-#pragma unroll
-                    for (int i = 0; i < READS && i < MFMAS; ++i) {
+                    static_for<(READS < MFMAS ? READS : MFMAS)>([](auto ic) {
+                        constexpr int i = decltype(ic)::value;
                         __builtin_amdgcn_sched_group_barrier(0x100, i + 1 < MFMAS ? 1 : READS - i, 0);
                         __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-                    }
+                    });
                 }
                 __builtin_amdgcn_sched_barrier(0);
             });
