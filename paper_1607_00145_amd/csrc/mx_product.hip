@@ -61,17 +61,19 @@ __device__ __forceinline__ void store_row(const Result<T> &o, int row, int col, 
 
 template <typename T, typename S>
 __global__ __launch_bounds__(S::THREADS) void mx_tile_kernel(PanelOperand A, PanelOperand B,
-                                                            int panels, int tilesM, int tilesN,
-                                                            Result<T> o)
+                                                            PanelGrid grid, Result<T> o)
 {
     extern __shared__ __attribute__((aligned(256))) char dyn_lds[];
     int tm, tn;
-    panel_tile((int)blockIdx.x, tilesM, tilesN, 4, tm, tn);
+    const PanelItem w = panel_item(grid, (int)blockIdx.x);
+    panel_tile(grid, w.tile, tm, tn);
     A.row0 = tm * S::BM;
     B.row0 = tn * S::BN;
     Panel<kPanelMx, S> p;
     p.init();
-    p.run(dyn_lds, A, B, 0, panels);
+    p.run(dyn_lds, A, B, w.t0, w.t1);
+    __syncthreads();
+    if (!panel_join<kPanelMx, S>(p, grid, w, dyn_lds) || p.group > 0) return;
 #pragma unroll
     for (int e = 0; e < 16; ++e)
 #pragma unroll
@@ -83,17 +85,58 @@ __global__ __launch_bounds__(S::THREADS) void mx_tile_kernel(PanelOperand A, Pan
         }
 }
 
+// Tiles, and the workgroups of each that a CU holds at once.
+typedef PanelShape<2, 4, 4, 2, 2> Big;
+typedef PanelShape<2, 2, 2, 2, 2> Mid;
+typedef PanelShape<1, 1, 2, 2, 4> Small;
+constexpr int64_t kCus = 256;
+
+struct TilePlan {
+    int shape;   // 0 Big, 1 Mid, 2 Small
+    PanelCut cut;
+    int64_t slotBytes, counters;
+};
+
+template <typename S> void consider(TilePlan &best, double &time, int shape, int64_t resident,
+                                    double perPanel, int64_t m, int64_t n, int64_t panels)
+{
+    const int64_t tiles = ((m + S::BM - 1) / S::BM) * ((n + S::BN - 1) / S::BN);
+    const int64_t slots = resident * kCus;
+    const PanelCut c = panel_cut(tiles, slots, panels);
+    double t = 0;
+    if (c.full) t += (double)((c.full + slots - 1) / slots) * panels * perPanel;
+    // a slice writes its sums past the L2, and one workgroup reads them all
+    if (c.slices > 1)
+        t += (double)panels / c.slices * perPanel + (2.0 + c.slices) * (S::TILE / 16384.0 * 3.0 + 0.5);
+    if (t >= time) return;
+    time = t;
+    const int64_t shared = c.slices > 1 ? c.blocks - c.full : 0;
+    best = {shape, c, shared * S::TILE * 4, c.slices > 1 ? shared / c.slices : 0};
+}
+
+TilePlan tile_plan(int64_t m, int64_t n, int64_t panels)
+{
+    TilePlan p = {};
+    double time = 1e300;
+    consider<Big>(p, time, 0, 1, 1.7, m, n, panels);
+    consider<Mid>(p, time, 1, 2, 1.0, m, n, panels);
+    consider<Small>(p, time, 2, 2, 0.45, m, n, panels);
+    return p;
+}
+
 template <typename T, typename S>
-hipError_t tile_launch(const PanelOperand &A, const PanelOperand &B, int panels,
-                       const Result<T> &o, hipStream_t stream)
+hipError_t tile_launch(const PanelOperand &A, const PanelOperand &B, int panels, const TilePlan &p,
+                       float *slots, int *counters, const Result<T> &o, hipStream_t stream)
 {
     constexpr auto k = mx_tile_kernel<T, S>;
-    const hipError_t e = allow_dynamic_lds<k>(S::LDS);
+    const hipError_t e = allow_dynamic_lds<k>(S::lds(kPanelMx));
     if (e != hipSuccess) return e;
-    const int64_t tm = (o.m + S::BM - 1) / S::BM, tn = (o.n + S::BN - 1) / S::BN;
-    if (tm * tn >= INT32_MAX) return hipErrorInvalidValue;
-    hipLaunchKernelGGL(k, dim3((unsigned)(tm * tn)), dim3(S::THREADS), S::LDS, stream, A, B,
-                       panels, (int)tm, (int)tn, o);
+    const int64_t tilesM = (o.m + S::BM - 1) / S::BM, tilesN = (o.n + S::BN - 1) / S::BN;
+    PanelGrid g;
+    if (!panel_grid(g, 1, tilesM, tilesN, tilesM * tilesN, p.cut, panels, slots, counters))
+        return hipErrorInvalidValue;
+    hipLaunchKernelGGL(k, dim3((unsigned)p.cut.blocks), dim3(S::THREADS), S::lds(kPanelMx), stream,
+                       A, B, g, o);
     return hipGetLastError();
 }
 
@@ -263,31 +306,28 @@ struct Packed {
     int64_t rows;
 };
 
+// Few rows go their own way; tiles get slots for shared sums behind the
+// `before` bytes of the stream's workspace that the caller has in use.
+bool few_rows(int64_t m, int64_t k) { return k > 0 && m <= 32; }
+
 template <typename T>
-hipError_t contract_typed(Packed A, Packed B, int64_t k, const Result<T> &out, hipStream_t stream)
+hipError_t contract_typed(const Packed &A, const Packed &B, int64_t k, const TilePlan &plan,
+                          float *slots, int *counters, const Result<T> &o, hipStream_t stream)
 {
-    Result<T> o = out;
     const int panels = (int)mx_tiles(k);
-    if (o.sm == 1 && o.sn != 1) {   // C's neighbours lie along m: C^T = B A^T
-        std::swap(A, B);
-        std::swap(o.sm, o.sn);
-        std::swap(o.m, o.n);
-    }
     const uint8_t *ca = static_cast<const uint8_t *>(A.codes);
     const uint8_t *sa = static_cast<const uint8_t *>(A.scales);
     const uint8_t *cb = static_cast<const uint8_t *>(B.codes);
     const uint8_t *sb = static_cast<const uint8_t *>(B.scales);
-    if (panels > 0 && o.m <= 16)
-        return few_launch<T, FewPacked<1>, 1>({ca, sa, o.m}, cb, sb, panels, o, stream);
-    if (panels > 0 && o.m <= 32)
-        return few_launch<T, FewPacked<2>, 2>({ca, sa, o.m}, cb, sb, panels, o, stream);
-    const PanelOperand pa = {ca, sa, o.m, 0};
-    const PanelOperand pb = {cb, sb, o.n, 0};
-    const int64_t big = (int64_t)((o.m + 255) / 256) * ((o.n + 255) / 256);
-    const int64_t mid = (int64_t)((o.m + 127) / 128) * ((o.n + 127) / 128);
-    if (big >= 256) return tile_launch<T, PanelShape<2, 4, 4, 2>>(pa, pb, panels, o, stream);
-    if (mid >= 256) return tile_launch<T, PanelShape<2, 2, 2, 2>>(pa, pb, panels, o, stream);
-    return tile_launch<T, PanelShape<1, 1, 2, 2>>(pa, pb, panels, o, stream);
+    if (few_rows(o.m, k))
+        return o.m <= 16 ? few_launch<T, FewPacked<1>, 1>({ca, sa, o.m}, cb, sb, panels, o, stream)
+                         : few_launch<T, FewPacked<2>, 2>({ca, sa, o.m}, cb, sb, panels, o, stream);
+    const PanelOperand pa = {ca, sa, o.m, 0}, pb = {cb, sb, o.n, 0};
+    if (plan.shape == 0)
+        return tile_launch<T, Big>(pa, pb, panels, plan, slots, counters, o, stream);
+    if (plan.shape == 1)
+        return tile_launch<T, Mid>(pa, pb, panels, plan, slots, counters, o, stream);
+    return tile_launch<T, Small>(pa, pb, panels, plan, slots, counters, o, stream);
 }
 
 template <typename T>
@@ -296,19 +336,56 @@ Result<T> result(void *C, int64_t sm, int64_t sn, int64_t m, int64_t n, double a
     return Result<T>{static_cast<T *>(C), sm, sn, (int)m, (int)n, (float)alpha, (float)beta};
 }
 
-gett_status_t contract_launch(Packed A, Packed B, int64_t k, double alpha, double beta,
-                              gett_dtype_t dtype, void *C, int64_t sm, int64_t sn,
-                              hipStream_t stream)
+// What a product of m x k by n x k needs of the workspace, with C's neighbours
+// along n (or exchanged).
+struct Need {
+    bool swapped;
+    TilePlan plan;
+};
+Need need_of(int64_t m, int64_t n, int64_t k, int64_t sm, int64_t sn)
 {
+    Need w = {};
+    w.swapped = sm == 1 && sn != 1;   // C's neighbours lie along m: C^T = B A^T
+    if (w.swapped) std::swap(m, n);
+    if (!few_rows(m, k)) w.plan = tile_plan(m, n, mx_tiles(k));
+    return w;
+}
+
+gett_status_t contract_launch(Packed A, Packed B, int64_t k, const Need &need, float *slots,
+                              int *counters, double alpha, double beta, gett_dtype_t dtype, void *C,
+                              int64_t sm, int64_t sn, hipStream_t stream)
+{
+    if (need.swapped) {
+        std::swap(A, B);
+        std::swap(sm, sn);
+    }
     const int64_t m = A.rows, n = B.rows;
     hipError_t e;
     if (dtype == GETT_FLOAT32)
-        e = contract_typed<float>(A, B, k, result<float>(C, sm, sn, m, n, alpha, beta), stream);
+        e = contract_typed<float>(A, B, k, need.plan, slots, counters,
+                                  result<float>(C, sm, sn, m, n, alpha, beta), stream);
     else if (dtype == GETT_BFLOAT16)
-        e = contract_typed<bf16>(A, B, k, result<bf16>(C, sm, sn, m, n, alpha, beta), stream);
+        e = contract_typed<bf16>(A, B, k, need.plan, slots, counters,
+                                 result<bf16>(C, sm, sn, m, n, alpha, beta), stream);
     else
-        e = contract_typed<_Float16>(A, B, k, result<_Float16>(C, sm, sn, m, n, alpha, beta), stream);
+        e = contract_typed<_Float16>(A, B, k, need.plan, slots, counters,
+                                     result<_Float16>(C, sm, sn, m, n, alpha, beta), stream);
     return e == hipSuccess ? GETT_SUCCESS : GETT_ERROR_HIP;
+}
+
+// the whole call: the product alone
+gett_status_t contract(const Packed &A, const Packed &B, int64_t k, double alpha, double beta,
+                       gett_dtype_t dtype, void *C, int64_t sm, int64_t sn, hipStream_t stream)
+{
+    const Need need = need_of(A.rows, B.rows, k, sm, sn);
+    Partials w;
+    if (need.plan.slotBytes > 0) {
+        const gett_status_t ws = stream_workspace(stream, (uint64_t)need.plan.counters,
+                                                  (uint64_t)need.plan.slotBytes, w);
+        if (ws != GETT_SUCCESS) return ws;
+    }
+    return contract_launch(A, B, k, need, static_cast<float *>(w.tiles), w.counters, alpha, beta,
+                           dtype, C, sm, sn, stream);
 }
 
 template <typename TA, typename T>
@@ -370,8 +447,8 @@ gett_status_t gett_mx_contract(int64_t m, int64_t n, int64_t k, double alpha,
             !clear_of(C, bytes, codes_B, scales_B, n, k))
             return GETT_ERROR_INVALID_VALUE;
     }
-    return contract_launch({codes_A, scales_A, m}, {codes_B, scales_B, n}, k, alpha, beta, dtype,
-                           C, stride_m, stride_n, static_cast<hipStream_t>(stream));
+    return contract({codes_A, scales_A, m}, {codes_B, scales_B, n}, k, alpha, beta, dtype, C,
+                    stride_m, stride_n, static_cast<hipStream_t>(stream));
 }
 
 gett_status_t gett_mx_apply(int64_t m, int64_t n, int64_t k, double alpha, gett_dtype_t dtype_A,
@@ -387,8 +464,8 @@ gett_status_t gett_mx_apply(int64_t m, int64_t n, int64_t k, double alpha, gett_
     if (alpha == 0.0) k = 0;
     hipStream_t s = static_cast<hipStream_t>(stream);
     if (k == 0)
-        return contract_launch({nullptr, nullptr, m}, {nullptr, nullptr, n}, 0, 0.0, beta, dtype,
-                               C, stride_m, stride_n, s);
+        return contract({nullptr, nullptr, m}, {nullptr, nullptr, n}, 0, 0.0, beta, dtype, C, stride_m,
+                        stride_n, s);
     if (!A || (uintptr_t)A % type_size(dtype_A) || !packed_ok(codes_B, scales_B))
         return GETT_ERROR_INVALID_VALUE;
     const int64_t bytesA = span_bytes(m, k, stride_am, stride_ak, type_size(dtype_A));
@@ -411,17 +488,20 @@ gett_status_t gett_mx_apply(int64_t m, int64_t n, int64_t k, double alpha, gett_
                                        s);
         return e == hipSuccess ? GETT_SUCCESS : GETT_ERROR_HIP;
     }
-    // A's packed copy: codes, then scales, in the stream's workspace.  The
-    // hold lasts until both launches are enqueued.
-    const int64_t codeBytes = mx_code_bytes(m, k);
+    // A's packed copy and the slots of shared sums, in the stream's workspace.
+    // The hold lasts until both launches are enqueued.
+    const int64_t codeBytes = mx_code_bytes(m, k), packed = codeBytes + mx_scale_bytes(m, k);
+    const Need need = need_of(m, n, k, stride_m, stride_n);
     Partials w;
-    gett_status_t ws = stream_workspace(s, 0, (uint64_t)(codeBytes + mx_scale_bytes(m, k)), w);
+    gett_status_t ws = stream_workspace(s, (uint64_t)need.plan.counters,
+                                        (uint64_t)(packed + need.plan.slotBytes), w);
     if (ws != GETT_SUCCESS) return ws;
     char *codes = static_cast<char *>(w.tiles), *scales = codes + codeBytes;
     ws = quantize_launch(dtype_A, m, k, A, stride_am, stride_ak, codes, scales, nullptr, nullptr, s);
     if (ws != GETT_SUCCESS) return ws;
-    return contract_launch({codes, scales, m}, {codes_B, scales_B, n}, k, alpha, beta, dtype, C,
-                           stride_m, stride_n, s);
+    return contract_launch({codes, scales, m}, {codes_B, scales_B, n}, k, need,
+                           reinterpret_cast<float *>(codes + packed), w.counters, alpha, beta, dtype,
+                           C, stride_m, stride_n, s);
 }
 
 }  // extern "C"

@@ -41,7 +41,7 @@ constexpr int kNormBlocks = 256;   // at most, per matrix; one partial sum each
 // Numbers of one panel: Half 64 halves; Split 32, the high parts of eight
 // numbers and then their low parts (slab 0 takes the even pieces of a panel,
 // slab 1 the odd ones).
-template <int KIND> __host__ __device__ inline int panel_elements() { return KIND == kPanelSplit ? 32 : 64; }
+template <int KIND> __host__ __device__ constexpr int panel_elements() { return KIND == kPanelSplit ? 32 : 64; }
 template <int KIND> inline int64_t panel_count(int64_t k)
 {
     const int e = panel_elements<KIND>();
@@ -200,102 +200,172 @@ struct ProductArgs {
     const char *P, *Q;          // the operands, K along their rows
     int64_t stackP, stackQ;
     int m, n, panels;           // rows of P, rows of Q, panels of a row
-    int tilesM, tilesN, tiles;  // tiles of one matrix
     const char *addend;         // Poly: S; Update, Last: X; [row][col] as `out`
     char *out, *outT;           // [row][col], and its transpose
     int64_t stackOut, stackOutT;
-    float scale, factor;        // addend's and the product's factor
+    float factor, ratio;        // out = factor * (product + ratio * addend)
 };
 
-// The t-th tile on or below the diagonal, row by row.
-__device__ __forceinline__ void triangle_tile(int t, int &tm, int &tn)
+// Writes a tile's accumulators (held values) to panels at `out`, a matrix of
+// `rows` rows and `panels` panels, as [row][col] or ACROSS as its transpose,
+// `row0` / `col0` being the tile's first row and column there.  The lanes'
+// runs are a few elements of many rows, so they are put in order in LDS, the
+// panels' image: every store of a wavefront then covers 1 KB.
+template <int KIND, typename S, bool ACROSS>
+__device__ __forceinline__ void store_panels(Panel<KIND, S> &p, char *lds, char *out,
+                                             int rows, int panels, int row0, int col0)
 {
-    tm = (int)((sqrtf(8.0f * (float)t + 1.0f) - 1.0f) * 0.5f);
-    while ((tm + 1) * (tm + 2) / 2 <= t) ++tm;
-    while (tm * (tm + 1) / 2 > t) --tm;
-    tn = t - tm * (tm + 1) / 2;
+    constexpr int E = panel_elements<KIND>();
+    constexpr int ROWS = ACROSS ? S::BN : S::BM, COLS = ACROSS ? S::BM : S::BN;
+    constexpr int FR = ACROSS ? S::FN : S::FM, FC = ACROSS ? S::FM : S::FN;   // runs of a lane
+    constexpr int FIT = S::lds(KIND) / (ROWS * 128), ALL = COLS / E, PP = FIT < ALL ? FIT : ALL;
+    static_assert(ALL % PP == 0 && (PP * E) % (32 * FC) == 0, "a wavefront's columns in one pass");
+    const int tid = (int)threadIdx.x;
+    const int mine = (ACROSS ? p.wm : p.wn) * 32 * FC;   // this wavefront's first column
+#pragma unroll
+    for (int pass = 0; pass < ALL / PP; ++pass) {
+        __syncthreads();
+        if (p.group == 0 && mine / (PP * E) == pass) {
+            // each pass rounds anew: the compiler would round all values once
+            // and keep the parts, twice the registers, in scratch memory
+#pragma unroll
+            for (int i = 0; i < S::FM; ++i)
+#pragma unroll
+                for (int j = 0; j < S::FN; ++j) asm volatile("" : "+v"(p.acc[i][j]));
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+#pragma unroll
+                for (int f = 0; f < FR; ++f) {
+                    const int row = ACROSS ? p.col(f) : p.row(f, e);
+                    const int col = (ACROSS ? p.row(0, e) : p.col(0)) - pass * PP * E;
+                    const int in = col % E;
+                    const int byte = KIND == kPanelSplit ? (in >> 3) * 32 + (in & 7) * 2 : in * 2;
+                    // pieces of a row lie by an exclusive or, so that the lanes'
+                    // rows, a power of two apart, fall on different banks
+                    const int x = row / FR & 7;
+                    char *at = lds + (col / E * ROWS + row) * 128 + ((byte >> 4 ^ x) << 4) + (byte & 15);
+                    typedef _Float16 vec __attribute__((ext_vector_type(FC)));
+                    vec hi, lo;
+#pragma unroll
+                    for (int c = 0; c < FC; ++c) {
+                        const float v = ACROSS ? p.acc[c][f][e] : p.acc[f][c][e];
+                        hi[c] = (_Float16)v;
+                        lo[c] = (_Float16)(v - (float)hi[c]);
+                    }
+                    *reinterpret_cast<vec *>(at) = hi;
+                    if constexpr (KIND == kPanelSplit)
+                        *reinterpret_cast<vec *>(lds + (col / E * ROWS + row) * 128 +
+                                                 (((byte >> 4) + 1 ^ x) << 4) + (byte & 15)) = lo;
+                }
+                __builtin_amdgcn_sched_barrier(0);   // no registers for many addresses
+            }
+        }
+        __syncthreads();
+        for (int u = tid; u < PP * ROWS * 8; u += S::THREADS) {
+            const int piece = u & 7, row = u / 8 % ROWS, panel = u / 8 / ROWS;
+            const i4 v = *reinterpret_cast<const i4 *>(lds + (panel * ROWS + row) * 128 +
+                                                       ((piece ^ (row / FR & 7)) << 4));
+            const int to = (col0 + pass * PP * E) / E + panel;
+            if (row0 + row < rows && to < panels)
+                *reinterpret_cast<i4 *>(out + ((int64_t)to * rows + row0 + row) * 128 + piece * 16) = v;
+        }
+    }
 }
 
 template <int KIND, int STEP, typename S, typename T>
-__global__ __launch_bounds__(S::THREADS) void orth_product_kernel(ProductArgs d, Stack<T> O)
+__global__ __launch_bounds__(S::THREADS) void orth_product_kernel(ProductArgs d, PanelGrid grid,
+                                                                  Stack<T> O)
 {
     extern __shared__ __attribute__((aligned(256))) char dyn_lds[];
     constexpr int FM = S::FM, FN = S::FN;
-    const int z = (int)blockIdx.x / d.tiles, t = (int)blockIdx.x % d.tiles;
-    int tm, tn;
     constexpr bool kSymmetric = STEP == kGram || STEP == kPoly;
-    if constexpr (kSymmetric) triangle_tile(t, tm, tn);
-    else panel_tile(t, d.tilesM, d.tilesN, 4, tm, tn);
+    int tm, tn;
+    const PanelItem w = panel_item(grid, (int)blockIdx.x);
+    const int z = w.z;
+    if constexpr (kSymmetric) panel_triangle(w.tile, tm, tn);
+    else panel_tile(grid, w.tile, tm, tn);
     const PanelOperand A = {reinterpret_cast<const uint8_t *>(d.P) + z * d.stackP, nullptr, d.m,
                             tm * S::BM};
     const PanelOperand B = {reinterpret_cast<const uint8_t *>(d.Q) + z * d.stackQ, nullptr, d.n,
                             tn * S::BN};
     Panel<KIND, S> p;
     p.init();
-    p.run(dyn_lds, A, B, 0, d.panels);
-
-    const int padN = padded<KIND>(d.n), padM = padded<KIND>(d.m);
-    const int col = B.row0 + p.col(0);
-    char *out = d.out + z * d.stackOut;
-    const char *addend = STEP == kGram ? nullptr : d.addend + z * d.stackOut;
+    const int col = B.row0 + p.col(0), padN = padded<KIND>(d.n);
+    if constexpr (STEP != kGram) {
+        // the sums start from the addend: its loads overlap those of the
+        // first panels and need no registers of their own
+        const char *addend = d.addend + z * d.stackOut;
+        if (w.slice == 0 && p.group == 0) {
+            // (outside the matrix any of its values will do: the results there
+            // are replaced)
+            const int c = col < padN ? col : padN - FN;
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-        const int row0 = A.row0 + p.row(0, e);   // FM neighbouring rows
+            for (int e = 0; e < 16; ++e)
 #pragma unroll
-        for (int i = 0; i < FM; ++i) {
-            const int row = row0 + i;
-            float x[FN];
+                for (int i = 0; i < FM; ++i) {
+                    const int row = A.row0 + p.row(i, e);
+                    float x[FN];
+                    load_run<KIND, FN>(addend + at<KIND>(d.m, row < d.m ? row : d.m - 1, c), x);
 #pragma unroll
-            for (int j = 0; j < FN; ++j) x[j] = 0.0f;
-            if constexpr (STEP != kGram)
-                if (row < d.m && col < padN)
-                    load_run<KIND, FN>(addend + at<KIND>(d.m, row, col), x);
-#pragma unroll
-            for (int j = 0; j < FN; ++j) {
-                // rows and columns of the padding are zeros
-                float v = d.factor * p.acc[i][j][e];
-                if constexpr (STEP != kGram) v += d.scale * x[j];
-                p.acc[i][j][e] = row < d.m && col + j < d.n ? v : 0.0f;
-            }
-            if constexpr (STEP != kLast) {
-                float v[FN];
-#pragma unroll
-                for (int j = 0; j < FN; ++j) v[j] = p.acc[i][j][e];
-                if (row < d.m && col < padN)
-                    store_run<KIND, FN>(out + at<KIND>(d.m, row, col), v);
-            } else if (O.si != 1 || O.sk == 1) {
-                T *o = O.p + z * O.sb + row * O.si + col * O.sk;
-                if (row < d.m && O.sk == 1 && col + FN <= d.n) {
-                    Run<T, FN> v;
-#pragma unroll
-                    for (int j = 0; j < FN; ++j) v.v[j] = from_float<T>(p.acc[i][j][e] * kDown);
-                    *reinterpret_cast<Run<T, FN> *>(o) = v;
-                } else if (row < d.m) {
-#pragma unroll
-                    for (int j = 0; j < FN; ++j)
-                        if (col + j < d.n) o[j * O.sk] = from_float<T>(p.acc[i][j][e] * kDown);
+                    for (int j = 0; j < FN; ++j) p.acc[i][j][e] = d.ratio * x[j];
                 }
-            }
         }
+    }
+    p.run(dyn_lds, A, B, w.t0, w.t1);
+    __syncthreads();
+    if (!panel_join<KIND, S>(p, grid, w, dyn_lds)) return;
+
+    // rows and columns of the padding become zeros
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int j = 0; j < FN; ++j)
+                p.acc[i][j][e] = A.row0 + p.row(i, e) < d.m && col + j < d.n
+                                     ? d.factor * p.acc[i][j][e]
+                                     : 0.0f;
+    if constexpr (STEP != kLast) {
+        const int panelsN = padN / panel_elements<KIND>();
+        store_panels<KIND, S, false>(p, dyn_lds, d.out + z * d.stackOut, d.m, panelsN, A.row0, B.row0);
         // the other orientation: X^T, or the mirrored tile
-        if constexpr (STEP != kLast) {
-            if (!kSymmetric || tm != tn) {
-                char *outT = d.outT + z * d.stackOutT;
+        if (!kSymmetric || tm != tn)
+            store_panels<KIND, S, true>(p, dyn_lds, d.outT + z * d.stackOutT, d.n,
+                                        padded<KIND>(d.m) / panel_elements<KIND>(), B.row0, A.row0);
+    } else if (p.group > 0) {
+    } else if (O.si != 1 || O.sk == 1) {
+        T *own = O.p + z * O.sb + (A.row0 + p.row(0, 0)) * O.si + col * O.sk;
 #pragma unroll
-                for (int j = 0; j < FN; ++j) {
-                    float v[FM];
+        for (int e = 0; e < 16; ++e) {
 #pragma unroll
-                    for (int i = 0; i < FM; ++i) v[i] = p.acc[i][j][e];
-                    if (col + j < d.n && row0 < padM)
-                        store_run<KIND, FM>(outT + at<KIND>(d.n, col + j, row0), v);
+            for (int i = 0; i < FM; ++i) {
+                const int down = p.row(i, e) - p.row(0, 0);
+                T *o = own + down * O.si;
+                if (A.row0 + p.row(i, e) < d.m) {
+                    if (O.sk == 1 && col + FN <= d.n) {
+                        Run<T, FN> v;
+#pragma unroll
+                        for (int j = 0; j < FN; ++j) v.v[j] = from_float<T>(p.acc[i][j][e] * kDown);
+                        *reinterpret_cast<Run<T, FN> *>(o) = v;
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < FN; ++j)
+                            if (col + j < d.n) o[j * O.sk] = from_float<T>(p.acc[i][j][e] * kDown);
+                    }
                 }
             }
-        } else if (O.si == 1 && O.sk != 1) {
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    } else {   // neighbours in memory run along the rows, FM of which a lane holds
+        T *own = O.p + z * O.sb + (A.row0 + p.row(0, 0)) + col * O.sk;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const int down = p.row(0, e) - p.row(0, 0), left = d.m - (A.row0 + p.row(0, e));
 #pragma unroll
             for (int j = 0; j < FN; ++j) {
                 if (col + j >= d.n) continue;
-                T *o = O.p + z * O.sb + row0 + (int64_t)(col + j) * O.sk;
-                if (row0 + FM <= d.m) {
+                T *o = own + down + j * O.sk;
+                if (left >= FM) {
                     Run<T, FM> v;
 #pragma unroll
                     for (int i = 0; i < FM; ++i) v.v[i] = from_float<T>(p.acc[i][j][e] * kDown);
@@ -303,44 +373,105 @@ __global__ __launch_bounds__(S::THREADS) void orth_product_kernel(ProductArgs d,
                 } else {
 #pragma unroll
                     for (int i = 0; i < FM; ++i)
-                        if (row0 + i < d.m) o[i] = from_float<T>(p.acc[i][j][e] * kDown);
+                        if (i < left) o[i] = from_float<T>(p.acc[i][j][e] * kDown);
                 }
             }
+            __builtin_amdgcn_sched_barrier(0);
         }
     }
 }
 
+// Square tiles (the symmetric products mirror them) and the workgroups of each
+// that a CU holds at once.
+typedef PanelShape<2, 4, 4, 2, 2> Big;
+typedef PanelShape<2, 2, 2, 2, 2> Mid;
+typedef PanelShape<1, 1, 2, 2, 4> Small;
+constexpr int kCus = 256;
+template <typename S> constexpr int64_t resident_tiles()
+{
+    return (S::BM == 256 ? 1 : 2) * kCus;
+}
+
+template <int STEP> int64_t tile_count(int64_t edge, int64_t m, int64_t n)
+{
+    const int64_t tm = (m + edge - 1) / edge, tn = (n + edge - 1) / edge;
+    return STEP == kGram || STEP == kPoly ? tm * (tm + 1) / 2 : tm * tn;
+}
+
+// us that a product takes with these tiles: rounds of whole tiles, and the
+// last round's slices with their sums
+template <int STEP, typename S>
+double product_time(int64_t batch, int64_t m, int64_t n, int64_t panels, double perPanel)
+{
+    const PanelCut c = panel_cut(batch * tile_count<STEP>(S::BM, m, n), resident_tiles<S>(), panels);
+    const int64_t slots = resident_tiles<S>();
+    double t = 0;
+    if (c.full) t += (double)((c.full + slots - 1) / slots) * panels * perPanel;
+    // a slice writes its sums past the L2, and one workgroup reads them all
+    if (c.slices > 1)
+        t += (double)panels / c.slices * perPanel + (2.0 + c.slices) * (S::TILE / 16384.0 * 3.0 + 0.5);
+    return t;
+}
+
+// what the slices of a problem's products need of the stream's workspace
+struct SliceNeed {
+    int64_t slots = 0, counters = 0;
+};
+
+template <int STEP> int pick(int64_t batch, int64_t m, int64_t n, int64_t panels)
+{
+    const double big = product_time<STEP, Big>(batch, m, n, panels, 1.7);
+    const double mid = product_time<STEP, Mid>(batch, m, n, panels, 1.0);
+    const double small = product_time<STEP, Small>(batch, m, n, panels, 0.45);
+    return small <= mid && small <= big ? 2 : mid <= big ? 1 : 0;
+}
+template <int STEP, typename S>
+void need_of(SliceNeed &w, int64_t batch, int64_t m, int64_t n, int64_t panels)
+{
+    const PanelCut c = panel_cut(batch * tile_count<STEP>(S::BM, m, n), resident_tiles<S>(), panels);
+    if (c.slices < 2) return;
+    const int64_t slots = (c.blocks - c.full) * S::TILE * 4, counters = (c.blocks - c.full) / c.slices;
+    w.slots = w.slots > slots ? w.slots : slots;
+    w.counters = w.counters > counters ? w.counters : counters;
+}
+template <int STEP> void add_need(SliceNeed &w, int64_t batch, int64_t m, int64_t n, int64_t panels)
+{
+    const int s = pick<STEP>(batch, m, n, panels);
+    if (s == 0) need_of<STEP, Big>(w, batch, m, n, panels);
+    else if (s == 1) need_of<STEP, Mid>(w, batch, m, n, panels);
+    else need_of<STEP, Small>(w, batch, m, n, panels);
+}
+
+struct Workspace {
+    float *slots;
+    int *counters;
+};
+
 template <int KIND, int STEP, typename S, typename T>
-hipError_t product_launch(ProductArgs d, const Stack<T> &O, int64_t batch, hipStream_t stream)
+hipError_t product_launch(const ProductArgs &d, const Workspace &w, const Stack<T> &O, int64_t batch,
+                          hipStream_t stream)
 {
     constexpr auto k = orth_product_kernel<KIND, STEP, S, T>;
-    const hipError_t e = allow_dynamic_lds<k>(S::LDS);
+    const hipError_t e = allow_dynamic_lds<k>(S::lds(KIND));
     if (e != hipSuccess) return e;
-    d.tilesM = (d.m + S::BM - 1) / S::BM;
-    d.tilesN = (d.n + S::BN - 1) / S::BN;
-    const int64_t tiles = STEP == kGram || STEP == kPoly ? (int64_t)d.tilesM * (d.tilesM + 1) / 2
-                                                         : (int64_t)d.tilesM * d.tilesN;
-    if (tiles * batch >= INT32_MAX) return hipErrorInvalidValue;
-    d.tiles = (int)tiles;
-    hipLaunchKernelGGL(k, dim3((unsigned)(tiles * batch)), dim3(S::THREADS), S::LDS, stream, d, O);
+    const int64_t tiles = tile_count<STEP>(S::BM, d.m, d.n);
+    const PanelCut c = panel_cut(tiles * batch, resident_tiles<S>(), d.panels);
+    PanelGrid g;
+    if (!panel_grid(g, batch, (d.m + S::BM - 1) / S::BM, (d.n + S::BN - 1) / S::BN, tiles, c,
+                    d.panels, w.slots, w.counters))
+        return hipErrorInvalidValue;
+    hipLaunchKernelGGL(k, dim3((unsigned)c.blocks), dim3(S::THREADS), S::lds(KIND), stream, d, g, O);
     return hipGetLastError();
 }
 
-// Square tiles (the symmetric products mirror them).
-typedef PanelShape<2, 4, 4, 2> Big;
-typedef PanelShape<2, 2, 2, 2> Mid;
-typedef PanelShape<1, 1, 2, 2> Small;
-
 template <int KIND, int STEP, typename T>
-hipError_t product(const ProductArgs &d, const Stack<T> &O, int64_t batch, hipStream_t stream)
+hipError_t product(const ProductArgs &d, const Workspace &w, const Stack<T> &O, int64_t batch,
+                   hipStream_t stream)
 {
-    auto tiles = [&](int64_t edge) {
-        const int64_t tm = (d.m + edge - 1) / edge, tn = (d.n + edge - 1) / edge;
-        return batch * (STEP == kGram || STEP == kPoly ? tm * (tm + 1) / 2 : tm * tn);
-    };
-    if (tiles(256) >= 256) return product_launch<KIND, STEP, Big, T>(d, O, batch, stream);
-    if (tiles(128) >= 256) return product_launch<KIND, STEP, Mid, T>(d, O, batch, stream);
-    return product_launch<KIND, STEP, Small, T>(d, O, batch, stream);
+    const int s = pick<STEP>(batch, d.m, d.n, d.panels);
+    if (s == 0) return product_launch<KIND, STEP, Big, T>(d, w, O, batch, stream);
+    if (s == 1) return product_launch<KIND, STEP, Mid, T>(d, w, O, batch, stream);
+    return product_launch<KIND, STEP, Small, T>(d, w, O, batch, stream);
 }
 
 struct Problem {
@@ -367,10 +498,17 @@ gett_status_t orthogonalize_typed(const Problem &P, Stack<const T> G, Stack<T> O
     if (P.batch * startM * startN >= INT32_MAX || P.batch * blocks >= INT32_MAX ||
         copies >= INT32_MAX)
         return GETT_ERROR_NOT_SUPPORTED;
+    SliceNeed need;
+    add_need<kGram>(need, P.batch, m, m, panelsX);
+    add_need<kPoly>(need, P.batch, m, m, panelsS);
+    add_need<kUpdate>(need, P.batch, m, n, panelsS);
     Partials w;
-    const gett_status_t ws = stream_workspace(
-        P.stream, 0, (uint64_t)(head + P.batch * (X + 2 * XT + 2 * SS)), w);
+    const int64_t matrices = head + P.batch * (X + 2 * XT + 2 * SS);
+    const gett_status_t ws = stream_workspace(P.stream, (uint64_t)need.counters,
+                                              (uint64_t)(matrices + need.slots), w);
     if (ws != GETT_SUCCESS) return ws;
+    const Workspace slots = {reinterpret_cast<float *>(static_cast<char *>(w.tiles) + matrices),
+                             w.counters};
     double *partial = static_cast<double *>(w.tiles);
     char *x = static_cast<char *>(w.tiles) + head, *xt = x + P.batch * X;
     char *xt2 = xt + P.batch * XT, *s = xt2 + P.batch * XT, *poly = s + P.batch * SS;
@@ -401,15 +539,17 @@ gett_status_t orthogonalize_typed(const Problem &P, Stack<const T> G, Stack<T> O
         d.out = d.outT = s;
         d.stackOut = d.stackOutT = SS;
         d.factor = kDown;
-        e = product<KIND, kGram, T>(d, none, P.batch, P.stream);
+        e = product<KIND, kGram, T>(d, slots, none, P.batch, P.stream);
         if (e != hipSuccess) return GETT_ERROR_HIP;
         d.P = d.Q = d.addend = s;
         d.stackP = d.stackQ = SS;
-        d.panels = (int)panelsS;
+        // without a quintic term to speak of no product is needed
+        const bool quintic = fabs(P.c) * 0x1p40 > fabs(P.b);
+        d.panels = quintic ? (int)panelsS : 0;
         d.out = d.outT = poly;
-        d.scale = (float)P.b;
-        d.factor = (float)(P.c * kDown);
-        e = product<KIND, kPoly, T>(d, none, P.batch, P.stream);
+        d.factor = (float)(quintic ? P.c * kDown : P.b);
+        d.ratio = (float)(quintic ? P.b / (P.c * kDown) : 1.0);
+        e = product<KIND, kPoly, T>(d, slots, none, P.batch, P.stream);
         if (e != hipSuccess) return GETT_ERROR_HIP;
         d.P = poly;
         d.Q = xt;
@@ -419,10 +559,11 @@ gett_status_t orthogonalize_typed(const Problem &P, Stack<const T> G, Stack<T> O
         d.outT = xt2;
         d.stackOut = X;
         d.stackOutT = XT;
-        d.scale = (float)P.a;
+        d.panels = (int)panelsS;
         d.factor = kDown;
-        e = i + 1 < P.steps ? product<KIND, kUpdate, T>(d, none, P.batch, P.stream)
-                            : product<KIND, kLast, T>(d, O, P.batch, P.stream);
+        d.ratio = (float)P.a * kUp;
+        e = i + 1 < P.steps ? product<KIND, kUpdate, T>(d, slots, none, P.batch, P.stream)
+                            : product<KIND, kLast, T>(d, slots, O, P.batch, P.stream);
         if (e != hipSuccess) return GETT_ERROR_HIP;
         std::swap(xt, xt2);
     }

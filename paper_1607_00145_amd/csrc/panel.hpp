@@ -34,15 +34,22 @@
 // different row / F, so they fall on sixteen different places: 210 bytes a
 // clock and CU, the rate of reads that follow one another being 227.
 //
-// Pipeline, two stages of LDS.  While panel t is multiplied, panel t + 1 is
-// on its way; one barrier per panel, after the last LDS read of t and before
+// Pipeline, NS stages of LDS.  While panel t is multiplied, the next NS - 1 are
+// on their way; one barrier per panel, after the last LDS read of t and before
 // its last MFMAs:
 //   read slabs g of t | MFMAs of slabs g - 1         (for each group of slabs)
-//   wait for t + 1; barrier; loads of t + 2 into t's stage
+//   wait for t + 1; barrier; loads of t + NS into t's stage
 //   read the first group of t + 1 | MFMAs of the last group of t
+// Two stages do for the large tiles (three or four: the same time within 2 %);
+// small tiles, whose panels take less than a load's latency, have four.
+//
+// The large tiles are bound by the card's power: with the instructions alone
+// and operands of random bits the clock falls until they make 6.2 PFLOP/s in
+// 4 bits and 1.6 in halves.
 #pragma once
 #include <type_traits>
 
+#include "kernel.hpp"
 #include "matrix.hpp"
 
 namespace gett {
@@ -60,14 +67,21 @@ template <int N, int I = 0, typename F> __device__ __forceinline__ void static_f
     }
 }
 
-template <int FM_, int FN_, int WM_, int WN_> struct PanelShape {
+template <int FM_, int FN_, int WM_, int WN_, int NS_, int KG_ = 1> struct PanelShape {
     static constexpr int FM = FM_, FN = FN_, WM = WM_, WN = WN_;   // fragments, wavefronts
+    static constexpr int NS = NS_;                                 // stages
     static constexpr int BM = 32 * FM * WM, BN = 32 * FN * WN;
-    static constexpr int NW = WM * WN, THREADS = 64 * NW;
-    static constexpr int STAGE = (BM + BN) * 128;
-    static constexpr int LDS = 2 * STAGE;
-    static constexpr int J = (BM + BN) / 8 / NW;   // load instructions a wavefront per panel
+    static constexpr int KG = KG_;                                 // groups that share K
+    static constexpr int NW = WM * WN, THREADS = 64 * NW * KG;     // wavefronts of a group
+    static constexpr int DATA = (BM + BN) * 128;      // bytes of a stage without scales
+    static constexpr int SCALES = (BM + BN) * 8;      // of its scales
+    static constexpr int J = DATA / 1024 / NW;        // load instructions a wavefront per panel
+    static constexpr int JS = SCALES / 256 / NW;      // and for scales
+    static constexpr int TILE = BM * BN;              // elements
     static_assert((BM / 8) % NW == 0 && (BN / 8) % NW == 0, "whole instructions per operand");
+    static_assert(SCALES % (256 * NW) == 0 && BM % 64 == 0 && BN % 64 == 0, "64 scale words each");
+    static constexpr int lds(int kind) { return KG * NS * (DATA + (kind == kPanelMx ? SCALES : 0)); }
+    static_assert(KG == 1 || (KG - 1) * TILE * 4 <= KG * NS * DATA, "the groups' sums fit");
 };
 
 // One operand of a tile: rows [row0, row0 + tile rows) of a matrix of `rows`
@@ -77,11 +91,21 @@ struct PanelOperand {
     const uint8_t *data;     // panel 0, row 0
     const uint8_t *scales;   // Mx: the packed scales
     int rows, row0;
-    // rows row0 ... of panel t, and nothing behind the panel's last row
-    __device__ __forceinline__ __amdgpu_buffer_rsrc_t panel(int t) const
+    // rows row0 ... of panel t, and nothing behind the panel's last row (of a
+    // panel that is not `there`, nothing: zeros are read); the scale words of
+    // half h likewise
+    __device__ __forceinline__ __amdgpu_buffer_rsrc_t panel(int t, bool there) const
     {
         const uint8_t *p = data + ((int64_t)t * rows + row0) * 128;
-        const int64_t bytes = (int64_t)(rows - row0) * 128;
+        const int64_t bytes = there ? (int64_t)(rows - row0) * 128 : 0;
+        return __builtin_amdgcn_make_buffer_rsrc(
+            const_cast<uint8_t *>(p), 0, (int)(uint32_t)(bytes < 0xffffffffll ? bytes : 0xffffffffll),
+            0x00027000);
+    }
+    __device__ __forceinline__ __amdgpu_buffer_rsrc_t words(int t, int half, int64_t R, bool there) const
+    {
+        const uint8_t *p = scales + (((int64_t)t * 2 + half) * R + row0) * 4;
+        const int64_t bytes = there ? (R - row0) * 4 : 0;
         return __builtin_amdgcn_make_buffer_rsrc(
             const_cast<uint8_t *>(p), 0, (int)(uint32_t)(bytes < 0xffffffffll ? bytes : 0xffffffffll),
             0x00027000);
@@ -108,22 +132,6 @@ __device__ __forceinline__ f16v mfma_half(i4 a, i4 b, f16v c)
                                                   __builtin_bit_cast(h8, b), c, 0, 0, 0);
 }
 
-// The scales of a lane's F rows and four slabs, a word per row.
-template <int F> struct PanelScales {
-    int v[F];
-    __device__ __forceinline__ void load(const uint8_t *p)
-    {
-        if constexpr (F == 1) {
-            v[0] = *reinterpret_cast<const int *>(p);
-        } else {
-            typedef int vec __attribute__((ext_vector_type(F)));
-            const vec x = *reinterpret_cast<const vec *>(p);
-#pragma unroll
-            for (int i = 0; i < F; ++i) v[i] = x[i];
-        }
-    }
-};
-
 // place of piece p (8 + p in the second row of its pair) of a row of lane r
 template <int F> __device__ __forceinline__ int panel_place(int p, int r)
 {
@@ -131,15 +139,18 @@ template <int F> __device__ __forceinline__ int panel_place(int p, int r)
 }
 
 template <int KIND, typename S> struct Panel {
-    static constexpr int FM = S::FM, FN = S::FN;
+    static constexpr int FM = S::FM, FN = S::FN, NS = S::NS;
+    static constexpr int STAGE = S::DATA + (KIND == kPanelMx ? S::SCALES : 0);
     static constexpr int G = KIND == kPanelSplit ? 2 : 1;   // slabs read together
     f16v acc[FM][FN];
-    int r, h, wm, wn;
+    int r, h, wm, wn, group;
 
     __device__ __forceinline__ void init()
     {
         const int tid = (int)threadIdx.x;
-        const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+        const int all = __builtin_amdgcn_readfirstlane(tid >> 6);
+        group = S::KG == 1 ? 0 : all / S::NW;
+        const int wave = S::KG == 1 ? all : all % S::NW;
         r = tid & 31;
         h = (tid >> 5) & 1;
         wm = wave / S::WN;
@@ -158,13 +169,17 @@ template <int KIND, typename S> struct Panel {
     }
     __device__ __forceinline__ int col(int j) const { return wn * 32 * FN + FN * r + j; }
 
-    // panels [t0, t1) of both operands; `lds` holds S::LDS bytes
-    __device__ __forceinline__ void run(char *lds, const PanelOperand &A, const PanelOperand &B,
+    // panels [t0, t1) of both operands; `lds` holds S::lds(KIND) bytes.  With
+    // several groups, group g takes panels t0 + g, t0 + g + KG, ... in stages of
+    // its own (all go through the same number of barriers), and group 0 ends
+    // with the sum; the others have nothing.
+    __device__ __forceinline__ void run(char *all, const PanelOperand &A, const PanelOperand &B,
                                         int t0, int t1)
     {
+        char *lds = all + group * NS * STAGE;
         constexpr int NW = S::NW, J = S::J, JA = S::BM / 8 / NW;
         const int lane = (int)threadIdx.x & 63;
-        const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+        const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) - group * NW;
         // this lane's piece of each load: 16 places of a pair of rows
         uint32_t off[J];
 #pragma unroll
@@ -178,40 +193,34 @@ template <int KIND, typename S> struct Panel {
             off[j] = (uint32_t)(row < last ? row : last) * 128 + (uint32_t)(p & 7) * 16;
         }
         // buffer loads: a lane's offset stays, the panel's base is a scalar
-        int at = t0;
+        int at = t0 + group;
         auto issue = [&](int stage) {
-            const __amdgpu_buffer_rsrc_t ra = A.panel(at), rb = B.panel(at);
+            const bool there = S::KG == 1 || at < t1;
+            const __amdgpu_buffer_rsrc_t ra = A.panel(at, there), rb = B.panel(at, there);
+            char *base = lds + stage * STAGE;
 #pragma unroll
             for (int j = 0; j < J; ++j) {
-                char *dst = lds + stage * S::STAGE + (j < JA ? 0 : S::BM * 128) +
-                            ((j < JA ? j : j - JA) * NW + wave) * 1024;
+                char *dst = base + (j < JA ? 0 : S::BM * 128) + ((j < JA ? j : j - JA) * NW + wave) * 1024;
                 __builtin_amdgcn_raw_ptr_buffer_load_lds(j < JA ? ra : rb, (matrix_lds *)dst, 16,
                                                          (int)off[j], 0, 0, 0);
             }
-            ++at;
-        };
-        // scales of panel t: a lane's are neighbours (gett_matrix.h)
-        PanelScales<FM> sa, nextA;
-        PanelScales<FN> sb, nextB;
-        const uint8_t *pa = nullptr, *pb = nullptr;
-        int64_t stepA = 0, stepB = 0;
-        if constexpr (KIND == kPanelMx) {
-            const int64_t RA = mx_scale_rows(A.rows), RB = mx_scale_rows(B.rows);
-            int64_t rowA = A.row0 + wm * 32 * FM + FM * r, rowB = B.row0 + wn * 32 * FN + FN * r;
-            rowA = rowA < RA - FM ? rowA : RA - FM;
-            rowB = rowB < RB - FN ? rowB : RB - FN;
-            stepA = RA * kTileBlocks;
-            stepB = RB * kTileBlocks;
-            pa = A.scales + t0 * stepA + (h * RA + rowA) * 4;
-            pb = B.scales + t0 * stepB + (h * RB + rowB) * 4;
-        }
-        auto scales = [&](PanelScales<FM> &x, PanelScales<FN> &y) {
             if constexpr (KIND == kPanelMx) {
-                x.load(pa);
-                y.load(pb);
-                pa += stepA;
-                pb += stepB;
+                // [A's rows, half 0][half 1][B's rows, half 0][half 1], 64 words
+                // an instruction; words past the last row come as zeros
+                const int64_t RA = mx_scale_rows(A.rows), RB = mx_scale_rows(B.rows);
+#pragma unroll
+                for (int j = 0; j < S::JS; ++j) {
+                    const int u = wave * S::JS + j;   // which 64 words
+                    const bool isA = u < S::BM / 32;
+                    const int v = isA ? u : u - S::BM / 32, per = (isA ? S::BM : S::BN) / 64;
+                    const int half = v / per, first = (v - half * per) * 64;
+                    const __amdgpu_buffer_rsrc_t rs =
+                        isA ? A.words(at, half, RA, there) : B.words(at, half, RB, there);
+                    __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (matrix_lds *)(base + S::DATA + u * 256),
+                                                             4, (first + lane) * 4, 0, 0, 0);
+                }
             }
+            at += S::KG;
         };
 
         // LDS reads: rows F r + i of the wavefront's part, piece 4 h + s.  The
@@ -225,9 +234,23 @@ template <int KIND, typename S> struct Panel {
         i4 a[2][G][FM], b[2][G][FN];
         int atA = ownA, atB = ownB;
         auto at_stage = [&](int stage) {
-            atA = ownA + stage * S::STAGE;
-            atB = ownB + stage * S::STAGE;
+            atA = ownA + stage * STAGE;
+            atB = ownB + stage * STAGE;
             asm volatile("" : "+v"(atA), "+v"(atB));
+        };
+        // the scale words of this lane's rows in stage `stage`
+        int sa[FM], sb[FN];
+        auto scales = [&](int stage) {
+            if constexpr (KIND == kPanelMx) {
+                const char *w = lds + stage * STAGE + S::DATA;
+                const int *pa = reinterpret_cast<const int *>(w) + h * S::BM + wm * 32 * FM + FM * r;
+                const int *pb = reinterpret_cast<const int *>(w) + 2 * S::BM + h * S::BN +
+                                wn * 32 * FN + FN * r;
+#pragma unroll
+                for (int i = 0; i < FM; ++i) sa[i] = pa[i];
+#pragma unroll
+                for (int j = 0; j < FN; ++j) sb[j] = pb[j];
+            }
         };
         auto read = [&](int set, int s) {
 #pragma unroll
@@ -249,8 +272,7 @@ template <int KIND, typename S> struct Panel {
 #pragma unroll
                 for (int j = 0; j < FN; ++j) {
                     if constexpr (KIND == kPanelMx)
-                        acc[i][j] = mfma_mx32<s>(a[set][0][i], b[set][0][j], acc[i][j], sa.v[i],
-                                                 sb.v[j]);
+                        acc[i][j] = mfma_mx32<s>(a[set][0][i], b[set][0][j], acc[i][j], sa[i], sb[j]);
                     else
                         acc[i][j] = mfma_half(a[set][0][i], b[set][0][j], acc[i][j]);
                 }
@@ -269,30 +291,39 @@ template <int KIND, typename S> struct Panel {
         };
         // no fence: a release would wait for the loads in flight as well
         auto barrier = []() { asm volatile("s_barrier" ::: "memory"); };
-        constexpr int kAllLoads = 7 << 4;   // vmcnt 0, lgkmcnt 0
         constexpr int STEPS = 4 / G;        // groups of slabs per panel
+        // s_waitcnt operands (gfx9 encoding): lgkmcnt 0 and that many loads left
+        // on their way
+        constexpr int LOADS = J + (KIND == kPanelMx ? S::JS : 0);
+        static_assert((NS - 1) * LOADS < 64, "vmcnt range");
+        auto wait_for = [](int left) constexpr { return (left & 15) | (left >> 4) << 14 | 7 << 4; };
+        constexpr int kAll = wait_for(0), kFirst = wait_for((NS - 1) * LOADS);
+        constexpr int kNext = wait_for((NS - 2) * LOADS);
 
-        const int n = t1 - t0;
+        const int n = (t1 - t0 + S::KG - 1) / S::KG;
         if (n <= 0) return;
-        issue(0);
-        scales(sa, sb);
-        __builtin_amdgcn_s_waitcnt(kAllLoads);
+#pragma unroll
+        for (int i = 0; i < NS; ++i)
+            if (i < n) issue(i);
+        if (n >= NS) __builtin_amdgcn_s_waitcnt(kFirst);
+        else __builtin_amdgcn_s_waitcnt(kAll);
         barrier();
-        if (n > 1) issue(1);
         at_stage(0);
         read(0, 0);
-        // one panel; `more`: another follows, `load`: and one after that
-        auto panel = [&](int stage, auto more, auto load) {
-            if constexpr (more) scales(nextA, nextB);
+        int stage = 0;
+        // one panel; `more`: another follows, `load`: and one is loaded
+        auto panel = [&](auto more, auto load) {
+            scales(stage);
             static_for<STEPS>([&](auto step) {
                 constexpr int s = decltype(step)::value;
                 if constexpr (s + 1 < STEPS) {
                     read((s + 1) & 1, (s + 1) * G);
                 } else if constexpr (more) {
-                    __builtin_amdgcn_s_waitcnt(kAllLoads);   // t + 1 loaded, t read
+                    __builtin_amdgcn_s_waitcnt(load ? kNext : kAll);   // t + 1 loaded, t read
                     barrier();
                     if constexpr (load) issue(stage);
-                    at_stage(stage ^ 1);
+                    stage = stage + 1 == NS ? 0 : stage + 1;
+                    at_stage(stage);
                     read((s + 1) & 1, 0);
                 }
                 mma(s & 1, std::integral_constant<int, s * G>{});
@@ -309,37 +340,196 @@ template <int KIND, typename S> struct Panel {
                 }
                 __builtin_amdgcn_sched_barrier(0);
             });
-            if constexpr (KIND == kPanelMx && more) {
-                sa = nextA;
-                sb = nextB;
-            }
         };
         const std::true_type yes;
         const std::false_type no;
         int t = 0;
-        for (; t + 2 < n; ++t) panel(t & 1, yes, yes);
-        if (t + 1 < n) {
-            panel(t & 1, yes, no);
-            ++t;
+        for (; t + NS < n; ++t) panel(yes, yes);
+        for (; t + 1 < n; ++t) panel(yes, no);
+        panel(no, no);
+        if constexpr (S::KG > 1) {
+            float *sums = reinterpret_cast<float *>(all) + ((int)threadIdx.x & (64 * NW - 1));
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < FM; ++i)
+#pragma unroll
+                for (int j = 0; j < FN; ++j)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        float *at = sums + ((i * FN + j) * 16 + e) * 64 * NW;
+                        if (group > 0) at[(group - 1) * S::TILE] = acc[i][j][e];
+                    }
+            __syncthreads();
+            if (group == 0) {
+#pragma unroll
+                for (int g = 0; g < S::KG - 1; ++g)
+#pragma unroll
+                    for (int i = 0; i < FM; ++i)
+#pragma unroll
+                        for (int j = 0; j < FN; ++j)
+#pragma unroll
+                            for (int e = 0; e < 16; ++e)
+                                acc[i][j][e] += sums[((i * FN + j) * 16 + e) * 64 * NW + g * S::TILE];
+            }
         }
-        panel(t & 1, no, no);
     }
 };
 
-// The tile of workgroup `bid` of `tilesM` x `tilesN`.  Workgroups go round
-// the eight XCDs, each with an L2 of its own: the ids of one XCD are made
-// neighbours, and they walk bands of `band` tile rows, column by column, so
-// that the tiles resident on an XCD share operand rows.
-__device__ __forceinline__ void panel_tile(int bid, int tilesM, int tilesN, int band, int &tm,
-                                           int &tn)
+// The work of a launch: the tiles of one or several matrices of results.
+//
+// Slices.  The tiles from `full` on are each shared among `slices` workgroups, a
+// run of panels each.  Their sums go to slots in device memory in lane order
+// (device-scope accesses, which pass by the XCD's own L2, so no fence writes
+// caches back), and the last to arrive adds them in slice order: results do not
+// depend on who that is.  Counters are zero between launches.
+//
+// Order.  Workgroups go round the eight XCDs, each with an L2 of its own: the
+// ids of one XCD are made neighbours, and neighbours walk bands of four tile
+// rows, column by column, so that the tiles resident on an XCD share operand
+// rows.
+//
+// Divisions are multiplications by the host's reciprocals: with the compiler's
+// own a launch began with 900 scalar instructions, a microsecond.
+struct PanelGrid {
+    int tilesM, tilesN, tiles;   // of one matrix
+    int full, slices, panels;
+    Recip tilesInv, bandInv, slicesInv;
+    float *slots;
+    int *counters;
+};
+
+struct PanelItem {
+    int z, tile;          // matrix, tile in it
+    int shared, slice;    // index among the shared tiles (-1: whole), slice
+    int t0, t1;           // panels
+};
+
+__device__ __forceinline__ PanelItem panel_item(const PanelGrid &g, int bid)
 {
-    const int total = tilesM * tilesN, per = total >> 3;
-    int id = bid;
-    if (bid < per * 8) id = (bid & 7) * per + (bid >> 3);
-    const int inBand = band * tilesN, b = id / inBand, rest = id % inBand;
-    const int height = tilesM - b * band < band ? tilesM - b * band : band;
-    tm = b * band + rest % height;
-    tn = rest / height;
+    PanelItem w = {0, 0, -1, 0, 0, g.panels};
+    int tile = bid;
+    if (bid >= g.full) {
+        const int u = bid - g.full;
+        w.shared = (int)quotient((uint32_t)u, g.slices, g.slicesInv);
+        w.slice = u - w.shared * g.slices;
+        tile = g.full + w.shared;
+        w.t0 = (int)quotient((uint32_t)(g.panels * w.slice), g.slices, g.slicesInv);
+        w.t1 = (int)quotient((uint32_t)(g.panels * (w.slice + 1)), g.slices, g.slicesInv);
+        if (g.slices == 1) w.shared = -1;
+    } else if (bid < (g.full & ~7)) {
+        tile = (bid & 7) * (g.full >> 3) + (bid >> 3);
+    }
+    w.z = (int)quotient((uint32_t)tile, g.tiles, g.tilesInv);
+    w.tile = tile - w.z * g.tiles;
+    return w;
+}
+
+constexpr int kPanelBand = 4;
+__device__ __forceinline__ void panel_tile(const PanelGrid &g, int id, int &tm, int &tn)
+{
+    const int inBand = kPanelBand * g.tilesN;
+    const int b = (int)quotient((uint32_t)id, inBand, g.bandInv), rest = id - b * inBand;
+    const int height = g.tilesM - b * kPanelBand;
+    if (height >= kPanelBand) tn = rest >> 2;
+    else if (height == 3) tn = (int)__umulhi((uint32_t)rest, 0x55555556u);
+    else tn = rest >> (height - 1);
+    tm = b * kPanelBand + rest - tn * (height < kPanelBand ? height : kPanelBand);
+}
+// the t-th tile on or below the diagonal, row by row
+__device__ __forceinline__ void panel_triangle(int t, int &tm, int &tn)
+{
+    tm = (int)((sqrtf(8.0f * (float)t + 1.0f) - 1.0f) * 0.5f);
+    while ((tm + 1) * (tm + 2) / 2 <= t) ++tm;
+    while (tm * (tm + 1) / 2 > t) --tm;
+    tn = t - tm * (tm + 1) / 2;
+}
+
+// Adds up a shared tile; true for the workgroup that holds the sum (and for a
+// tile that is not shared).  `lds` may be any LDS but is overwritten.
+template <int KIND, typename S>
+__device__ __forceinline__ bool panel_join(Panel<KIND, S> &p, const PanelGrid &d,
+                                           const PanelItem &w, char *lds)
+{
+    if (w.shared < 0) return true;
+    const int tid = (int)threadIdx.x;
+    constexpr int N = 64 * S::NW;   // threads that hold sums
+    float *first = d.slots + (int64_t)w.shared * d.slices * S::TILE + (tid & (N - 1));
+    float *own = first + (int64_t)w.slice * S::TILE;
+    if (p.group == 0)
+#pragma unroll
+        for (int i = 0; i < S::FM; ++i)
+#pragma unroll
+            for (int j = 0; j < S::FN; ++j)
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    __hip_atomic_store(own + ((i * S::FN + j) * 16 + e) * N, p.acc[i][j][e],
+                                       __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __builtin_amdgcn_s_waitcnt(7 << 4 | 15 << 8);   // vmcnt 0: the stores are done
+    __syncthreads();
+    int *last = reinterpret_cast<int *>(lds);
+    if (tid == 0)
+        *last = __hip_atomic_fetch_add(d.counters + w.shared, 1, __ATOMIC_RELAXED,
+                                       __HIP_MEMORY_SCOPE_AGENT) == d.slices - 1;
+    __syncthreads();
+    if (!*last) return false;
+    if (tid == 0)
+        __hip_atomic_store(d.counters + w.shared, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (p.group == 0)
+#pragma unroll
+        for (int i = 0; i < S::FM; ++i)
+#pragma unroll
+            for (int j = 0; j < S::FN; ++j) {
+                const float *at = first + (i * S::FN + j) * 16 * N;
+                for (int s0 = 0; s0 < d.slices; s0 += 2) {   // two slices' loads together
+                    float v[2][16];
+#pragma unroll
+                    for (int s = 0; s < 2; ++s)
+                        if (s0 + s < d.slices)
+#pragma unroll
+                            for (int e = 0; e < 16; ++e)
+                                v[s][e] = __hip_atomic_load(at + (int64_t)(s0 + s) * S::TILE + e * N,
+                                                            __ATOMIC_RELAXED,
+                                                            __HIP_MEMORY_SCOPE_AGENT);
+#pragma unroll
+                    for (int s = 0; s < 2; ++s)
+                        if (s0 + s < d.slices)
+#pragma unroll
+                            for (int e = 0; e < 16; ++e)
+                                p.acc[i][j][e] = s0 + s == 0 ? v[s][e] : p.acc[i][j][e] + v[s][e];
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+    __syncthreads();   // everyone has read `last`
+    return true;
+}
+
+// Host: how a launch of `tiles` tiles is shared, with `slots` workgroups
+// resident at once.  Whole rounds of tiles stay whole; the tiles of a last,
+// incomplete round are cut so that their slices fill it (at most eight, of two
+// panels or more each: beyond, the sums cost what the shorter runs save).
+struct PanelCut {
+    int64_t full, slices, blocks;
+};
+inline PanelCut panel_cut(int64_t tiles, int64_t slots, int64_t panels)
+{
+    const int64_t rest = tiles % slots;
+    int64_t s = rest ? slots / rest : 1;
+    s = s < panels / 2 ? s : panels / 2;
+    s = s < 8 ? s : 8;
+    if (s < 2) return {tiles, 1, tiles};
+    return {tiles - rest, s, tiles - rest + rest * s};
+}
+
+// Fills in a grid; false where it has too many workgroups for a launch.
+inline bool panel_grid(PanelGrid &g, int64_t batch, int64_t tilesM, int64_t tilesN, int64_t tiles,
+                       const PanelCut &cut, int panels, float *slots, int *counters)
+{
+    if (cut.blocks >= INT32_MAX || tiles * batch >= INT32_MAX ||
+        kPanelBand * tilesN >= INT32_MAX || (int64_t)panels * cut.slices >= INT32_MAX)
+        return false;
+    g = {(int)tilesM, (int)tilesN, (int)tiles, (int)cut.full, (int)cut.slices, panels,
+         recip(tiles), recip(kPanelBand * tilesN), recip(cut.slices), slots, counters};
+    return true;
 }
 
 }  // namespace gett
