@@ -85,11 +85,9 @@ __global__ __launch_bounds__(S::THREADS) void mx_tile_kernel(PanelOperand A, Pan
         }
 }
 
-// Tiles, and the workgroups of each that a CU holds at once.
 typedef PanelShape<2, 4, 4, 2, 2> Big;
 typedef PanelShape<2, 2, 2, 2, 2> Mid;
 typedef PanelShape<1, 1, 2, 2, 4> Small;
-constexpr int64_t kCus = 256;
 
 struct TilePlan {
     int shape;   // 0 Big, 1 Mid, 2 Small
@@ -97,30 +95,21 @@ struct TilePlan {
     int64_t slotBytes, counters;
 };
 
-template <typename S> void consider(TilePlan &best, double &time, int shape, int64_t resident,
-                                    double perPanel, int64_t m, int64_t n, int64_t panels)
+template <typename S>
+void consider(TilePlan &best, int shape, int64_t m, int64_t n, int64_t panels)
 {
     const int64_t tiles = ((m + S::BM - 1) / S::BM) * ((n + S::BN - 1) / S::BN);
-    const int64_t slots = resident * kCus;
-    const PanelCut c = panel_cut(tiles, slots, panels);
-    double t = 0;
-    if (c.full) t += (double)((c.full + slots - 1) / slots) * panels * perPanel;
-    // a slice writes its sums past the L2, and one workgroup reads them all
-    if (c.slices > 1)
-        t += (double)panels / c.slices * perPanel + (2.0 + c.slices) * (S::TILE / 16384.0 * 3.0 + 0.5);
-    if (t >= time) return;
-    time = t;
-    const int64_t shared = c.slices > 1 ? c.blocks - c.full : 0;
-    best = {shape, c, shared * S::TILE * 4, c.slices > 1 ? shared / c.slices : 0};
+    const PanelCut c = panel_cut<S>(kPanelMx, tiles, panels);
+    if (shape == 0 || c.us < best.cut.us)
+        best = {shape, c, c.shared() * c.slices * S::TILE * 4, c.shared()};
 }
 
 TilePlan tile_plan(int64_t m, int64_t n, int64_t panels)
 {
-    TilePlan p = {};
-    double time = 1e300;
-    consider<Big>(p, time, 0, 1, 1.7, m, n, panels);
-    consider<Mid>(p, time, 1, 2, 1.0, m, n, panels);
-    consider<Small>(p, time, 2, 2, 0.45, m, n, panels);
+    TilePlan p;
+    consider<Big>(p, 0, m, n, panels);
+    consider<Mid>(p, 1, m, n, panels);
+    consider<Small>(p, 2, m, n, panels);
     return p;
 }
 

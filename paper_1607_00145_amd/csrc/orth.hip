@@ -381,16 +381,10 @@ __global__ __launch_bounds__(S::THREADS) void orth_product_kernel(ProductArgs d,
     }
 }
 
-// Square tiles (the symmetric products mirror them) and the workgroups of each
-// that a CU holds at once.
+// Square tiles (the symmetric products mirror them).
 typedef PanelShape<2, 4, 4, 2, 2> Big;
 typedef PanelShape<2, 2, 2, 2, 2> Mid;
 typedef PanelShape<1, 1, 2, 2, 4> Small;
-constexpr int kCus = 256;
-template <typename S> constexpr int64_t resident_tiles()
-{
-    return (S::BM == 256 ? 1 : 2) * kCus;
-}
 
 template <int STEP> int64_t tile_count(int64_t edge, int64_t m, int64_t n)
 {
@@ -398,48 +392,23 @@ template <int STEP> int64_t tile_count(int64_t edge, int64_t m, int64_t n)
     return STEP == kGram || STEP == kPoly ? tm * (tm + 1) / 2 : tm * tn;
 }
 
-// us that a product takes with these tiles: rounds of whole tiles, and the
-// last round's slices with their sums
-template <int STEP, typename S>
-double product_time(int64_t batch, int64_t m, int64_t n, int64_t panels, double perPanel)
-{
-    const PanelCut c = panel_cut(batch * tile_count<STEP>(S::BM, m, n), resident_tiles<S>(), panels);
-    const int64_t slots = resident_tiles<S>();
-    double t = 0;
-    if (c.full) t += (double)((c.full + slots - 1) / slots) * panels * perPanel;
-    // a slice writes its sums past the L2, and one workgroup reads them all
-    if (c.slices > 1)
-        t += (double)panels / c.slices * perPanel + (2.0 + c.slices) * (S::TILE / 16384.0 * 3.0 + 0.5);
-    return t;
-}
-
-// what the slices of a problem's products need of the stream's workspace
-struct SliceNeed {
-    int64_t slots = 0, counters = 0;
+// The tiles of one product: 0 Big, 1 Mid, 2 Small, and how they are shared.
+struct Choice {
+    int shape;
+    PanelCut cut;
+    int64_t slotBytes;
 };
-
-template <int STEP> int pick(int64_t batch, int64_t m, int64_t n, int64_t panels)
+template <int KIND, int STEP> Choice choose(int64_t batch, int64_t m, int64_t n, int64_t panels)
 {
-    const double big = product_time<STEP, Big>(batch, m, n, panels, 1.7);
-    const double mid = product_time<STEP, Mid>(batch, m, n, panels, 1.0);
-    const double small = product_time<STEP, Small>(batch, m, n, panels, 0.45);
-    return small <= mid && small <= big ? 2 : mid <= big ? 1 : 0;
-}
-template <int STEP, typename S>
-void need_of(SliceNeed &w, int64_t batch, int64_t m, int64_t n, int64_t panels)
-{
-    const PanelCut c = panel_cut(batch * tile_count<STEP>(S::BM, m, n), resident_tiles<S>(), panels);
-    if (c.slices < 2) return;
-    const int64_t slots = (c.blocks - c.full) * S::TILE * 4, counters = (c.blocks - c.full) / c.slices;
-    w.slots = w.slots > slots ? w.slots : slots;
-    w.counters = w.counters > counters ? w.counters : counters;
-}
-template <int STEP> void add_need(SliceNeed &w, int64_t batch, int64_t m, int64_t n, int64_t panels)
-{
-    const int s = pick<STEP>(batch, m, n, panels);
-    if (s == 0) need_of<STEP, Big>(w, batch, m, n, panels);
-    else if (s == 1) need_of<STEP, Mid>(w, batch, m, n, panels);
-    else need_of<STEP, Small>(w, batch, m, n, panels);
+    const PanelCut c[3] = {
+        panel_cut<Big>(KIND, batch * tile_count<STEP>(Big::BM, m, n), panels),
+        panel_cut<Mid>(KIND, batch * tile_count<STEP>(Mid::BM, m, n), panels),
+        panel_cut<Small>(KIND, batch * tile_count<STEP>(Small::BM, m, n), panels)};
+    int s = 0;
+    for (int i = 1; i < 3; ++i)
+        if (c[i].us < c[s].us) s = i;
+    const int64_t tile[3] = {Big::TILE, Mid::TILE, Small::TILE};
+    return {s, c[s], c[s].shared() * c[s].slices * tile[s] * 4};
 }
 
 struct Workspace {
@@ -448,30 +417,27 @@ struct Workspace {
 };
 
 template <int KIND, int STEP, typename S, typename T>
-hipError_t product_launch(const ProductArgs &d, const Workspace &w, const Stack<T> &O, int64_t batch,
-                          hipStream_t stream)
+hipError_t product_launch(const ProductArgs &d, const PanelCut &c, const Workspace &w,
+                          const Stack<T> &O, int64_t batch, hipStream_t stream)
 {
     constexpr auto k = orth_product_kernel<KIND, STEP, S, T>;
     const hipError_t e = allow_dynamic_lds<k>(S::lds(KIND));
     if (e != hipSuccess) return e;
-    const int64_t tiles = tile_count<STEP>(S::BM, d.m, d.n);
-    const PanelCut c = panel_cut(tiles * batch, resident_tiles<S>(), d.panels);
     PanelGrid g;
-    if (!panel_grid(g, batch, (d.m + S::BM - 1) / S::BM, (d.n + S::BN - 1) / S::BN, tiles, c,
-                    d.panels, w.slots, w.counters))
+    if (!panel_grid(g, batch, (d.m + S::BM - 1) / S::BM, (d.n + S::BN - 1) / S::BN,
+                    tile_count<STEP>(S::BM, d.m, d.n), c, d.panels, w.slots, w.counters))
         return hipErrorInvalidValue;
     hipLaunchKernelGGL(k, dim3((unsigned)c.blocks), dim3(S::THREADS), S::lds(KIND), stream, d, g, O);
     return hipGetLastError();
 }
 
 template <int KIND, int STEP, typename T>
-hipError_t product(const ProductArgs &d, const Workspace &w, const Stack<T> &O, int64_t batch,
-                   hipStream_t stream)
+hipError_t product(const ProductArgs &d, const Choice &c, const Workspace &w, const Stack<T> &O,
+                   int64_t batch, hipStream_t stream)
 {
-    const int s = pick<STEP>(batch, d.m, d.n, d.panels);
-    if (s == 0) return product_launch<KIND, STEP, Big, T>(d, w, O, batch, stream);
-    if (s == 1) return product_launch<KIND, STEP, Mid, T>(d, w, O, batch, stream);
-    return product_launch<KIND, STEP, Small, T>(d, w, O, batch, stream);
+    if (c.shape == 0) return product_launch<KIND, STEP, Big, T>(d, c.cut, w, O, batch, stream);
+    if (c.shape == 1) return product_launch<KIND, STEP, Mid, T>(d, c.cut, w, O, batch, stream);
+    return product_launch<KIND, STEP, Small, T>(d, c.cut, w, O, batch, stream);
 }
 
 struct Problem {
@@ -498,14 +464,20 @@ gett_status_t orthogonalize_typed(const Problem &P, Stack<const T> G, Stack<T> O
     if (P.batch * startM * startN >= INT32_MAX || P.batch * blocks >= INT32_MAX ||
         copies >= INT32_MAX)
         return GETT_ERROR_NOT_SUPPORTED;
-    SliceNeed need;
-    add_need<kGram>(need, P.batch, m, m, panelsX);
-    add_need<kPoly>(need, P.batch, m, m, panelsS);
-    add_need<kUpdate>(need, P.batch, m, n, panelsS);
+    // without a quintic term to speak of S^2 is not needed
+    const bool quintic = fabs(P.c) * 0x1p40 > fabs(P.b);
+    const Choice gram = choose<KIND, kGram>(P.batch, m, m, panelsX);
+    const Choice quad = choose<KIND, kPoly>(P.batch, m, m, quintic ? panelsS : 0);
+    const Choice update = choose<KIND, kUpdate>(P.batch, m, n, panelsS);
+    int64_t slotBytes = 0, counters = 0;
+    for (const Choice *c : {&gram, &quad, &update}) {
+        slotBytes = slotBytes > c->slotBytes ? slotBytes : c->slotBytes;
+        counters = counters > c->cut.shared() ? counters : c->cut.shared();
+    }
     Partials w;
     const int64_t matrices = head + P.batch * (X + 2 * XT + 2 * SS);
-    const gett_status_t ws = stream_workspace(P.stream, (uint64_t)need.counters,
-                                              (uint64_t)(matrices + need.slots), w);
+    const gett_status_t ws = stream_workspace(P.stream, (uint64_t)counters,
+                                              (uint64_t)(matrices + slotBytes), w);
     if (ws != GETT_SUCCESS) return ws;
     const Workspace slots = {reinterpret_cast<float *>(static_cast<char *>(w.tiles) + matrices),
                              w.counters};
@@ -539,17 +511,15 @@ gett_status_t orthogonalize_typed(const Problem &P, Stack<const T> G, Stack<T> O
         d.out = d.outT = s;
         d.stackOut = d.stackOutT = SS;
         d.factor = kDown;
-        e = product<KIND, kGram, T>(d, slots, none, P.batch, P.stream);
+        e = product<KIND, kGram, T>(d, gram, slots, none, P.batch, P.stream);
         if (e != hipSuccess) return GETT_ERROR_HIP;
         d.P = d.Q = d.addend = s;
         d.stackP = d.stackQ = SS;
-        // without a quintic term to speak of no product is needed
-        const bool quintic = fabs(P.c) * 0x1p40 > fabs(P.b);
         d.panels = quintic ? (int)panelsS : 0;
         d.out = d.outT = poly;
         d.factor = (float)(quintic ? P.c * kDown : P.b);
         d.ratio = (float)(quintic ? P.b / (P.c * kDown) : 1.0);
-        e = product<KIND, kPoly, T>(d, slots, none, P.batch, P.stream);
+        e = product<KIND, kPoly, T>(d, quad, slots, none, P.batch, P.stream);
         if (e != hipSuccess) return GETT_ERROR_HIP;
         d.P = poly;
         d.Q = xt;
@@ -562,8 +532,8 @@ gett_status_t orthogonalize_typed(const Problem &P, Stack<const T> G, Stack<T> O
         d.panels = (int)panelsS;
         d.factor = kDown;
         d.ratio = (float)P.a * kUp;
-        e = i + 1 < P.steps ? product<KIND, kUpdate, T>(d, slots, none, P.batch, P.stream)
-                            : product<KIND, kLast, T>(d, slots, O, P.batch, P.stream);
+        e = i + 1 < P.steps ? product<KIND, kUpdate, T>(d, update, slots, none, P.batch, P.stream)
+                            : product<KIND, kLast, T>(d, update, slots, O, P.batch, P.stream);
         if (e != hipSuccess) return GETT_ERROR_HIP;
         std::swap(xt, xt2);
     }

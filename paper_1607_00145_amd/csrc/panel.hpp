@@ -503,21 +503,41 @@ __device__ __forceinline__ bool panel_join(Panel<KIND, S> &p, const PanelGrid &d
     return true;
 }
 
-// Host: how a launch of `tiles` tiles is shared, with `slots` workgroups
-// resident at once.  Whole rounds of tiles stay whole; the tiles of a last,
-// incomplete round are cut so that their slices fill it (at most eight, of two
-// panels or more each: beyond, the sums cost what the shorter runs save).
+// Host: how the tiles of a launch are shared.  Whole rounds of tiles (as many as
+// are resident at once) stay whole; the tiles of a last, incomplete round may
+// be cut so that their slices fill it.  us per panel and round, with the CUs
+// full and with one workgroup each, and for the join of s slices, measured: the
+// products of 4096 x 4096 (Big, Mid) and 517 x 1000 (Small).
 struct PanelCut {
-    int64_t full, slices, blocks;
+    int64_t full = 0, slices = 1, blocks = 0;
+    double us = 1e300;
+    int64_t shared() const { return slices > 1 ? (blocks - full) / slices : 0; }
 };
-inline PanelCut panel_cut(int64_t tiles, int64_t slots, int64_t panels)
+constexpr int64_t kPanelCus = 256;
+template <typename S> PanelCut panel_cut(int kind, int64_t tiles, int64_t panels)
 {
-    const int64_t rest = tiles % slots;
-    int64_t s = rest ? slots / rest : 1;
-    s = s < panels / 2 ? s : panels / 2;
-    s = s < 8 ? s : 8;
-    if (s < 2) return {tiles, 1, tiles};
-    return {tiles - rest, s, tiles - rest + rest * s};
+    constexpr bool big = S::BM == 256, mid = S::BM == 128;
+    constexpr int64_t slots = (big ? 1 : 2) * kPanelCus;
+    const double full = kind == kPanelSplit ? (big ? 2.3 : mid ? 1.2 : 0.45)
+                        : kind == kPanelMx  ? (big ? 2.1 : mid ? 1.2 : 0.45)
+                                            : (big ? 1.7 : mid ? 1.0 : 0.40);
+    const double alone = big ? full : kind == kPanelSplit ? (mid ? 1.0 : 0.30) : (mid ? 0.75 : 0.25);
+    const double join = big ? 15 : mid ? 8 : 6, joinEach = big ? 6 : mid ? 1.5 : 0.3;
+    const int64_t rounds = tiles / slots, rest = tiles % slots;
+    PanelCut best;
+    for (int64_t s = 1; s <= 16; ++s) {
+        if (s > 1 && (rest * s > slots || panels < 2 * s)) break;
+        double t = rounds * panels * full;
+        if (rest) t += (double)((panels + s - 1) / s) * (rest * s <= kPanelCus ? alone : full);
+        if (s > 1) t += join + joinEach * s;
+        if (t < best.us) {
+            best.full = s > 1 ? tiles - rest : tiles;
+            best.slices = s;
+            best.blocks = best.full + (s > 1 ? rest * s : 0);
+            best.us = t;
+        }
+    }
+    return best;
 }
 
 // Fills in a grid; false where it has too many workgroups for a launch.
