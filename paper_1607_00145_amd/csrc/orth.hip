@@ -203,8 +203,44 @@ struct ProductArgs {
     const char *addend;         // Poly: S; Update, Last: X; [row][col] as `out`
     char *out, *outT;           // [row][col], and its transpose
     int64_t stackOut, stackOutT;
-    float factor, ratio;        // out = factor * (product + ratio * addend)
+    float factor, scale;        // out = factor * product + scale * addend
 };
+
+// Passes in which a tile's panels, [panel][row][128 bytes], go through LDS.
+template <int KIND, typename S, bool ACROSS> constexpr int image_passes()
+{
+    constexpr int ROWS = ACROSS ? S::BN : S::BM, COLS = ACROSS ? S::BM : S::BN;
+    constexpr int FIT = S::lds(KIND) / (ROWS * 128), ALL = COLS / panel_elements<KIND>();
+    return FIT < ALL ? ALL / FIT : 1;
+}
+
+// Small tiles have LDS to spare for the addend, which then arrives with the
+// first panels; large ones load it after the sums, where panels were.
+template <typename S> constexpr bool kAddendEarly = S::BM == 64;
+
+// Starts the loads of a tile's panels of a matrix of `rows` rows and `panels`
+// panels, as the LDS image of pass `pass`.  Outside the matrix any of its
+// values will do: what becomes of them is replaced by zeros.
+template <int KIND, typename S>
+__device__ __forceinline__ void load_panels(const Panel<KIND, S> &p, char *image, const char *from,
+                                            int rows, int panels, int row0, int col0, int pass)
+{
+    constexpr int E = panel_elements<KIND>();
+    constexpr int PP = S::BN / E / (kAddendEarly<S> ? 1 : image_passes<KIND, S, false>());
+    const int lane = (int)threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+#pragma unroll
+    for (int u = 0; u < PP * S::BM / 8 / (S::THREADS / 64); ++u) {
+        const int k = u * (S::THREADS / 64) + wave;   // eight rows of a panel
+        const int panel = k / (S::BM / 8), row = row0 + k % (S::BM / 8) * 8 + (lane >> 3);
+        int to = col0 / E + pass * PP + panel;
+        to = to < panels ? to : panels - 1;
+        const char *src = from + ((int64_t)to * rows + (row < rows ? row : rows - 1)) * 128 +
+                          (lane & 7) * 16;
+        __builtin_amdgcn_global_load_lds((matrix_global *)src, (matrix_lds *)(image + k * 1024), 16, 0,
+                                         0);
+    }
+}
 
 // Writes a tile's accumulators (held values) to panels at `out`, a matrix of
 // `rows` rows and `panels` panels, as [row][col] or ACROSS as its transpose,
@@ -218,7 +254,7 @@ __device__ __forceinline__ void store_panels(Panel<KIND, S> &p, char *lds, char 
     constexpr int E = panel_elements<KIND>();
     constexpr int ROWS = ACROSS ? S::BN : S::BM, COLS = ACROSS ? S::BM : S::BN;
     constexpr int FR = ACROSS ? S::FN : S::FM, FC = ACROSS ? S::FM : S::FN;   // runs of a lane
-    constexpr int FIT = S::lds(KIND) / (ROWS * 128), ALL = COLS / E, PP = FIT < ALL ? FIT : ALL;
+    constexpr int ALL = COLS / E, PP = ALL / image_passes<KIND, S, ACROSS>();
     static_assert(ALL % PP == 0 && (PP * E) % (32 * FC) == 0, "a wavefront's columns in one pass");
     const int tid = (int)threadIdx.x;
     const int mine = (ACROSS ? p.wm : p.wn) * 32 * FC;   // this wavefront's first column
@@ -291,42 +327,52 @@ __global__ __launch_bounds__(S::THREADS) void orth_product_kernel(ProductArgs d,
     Panel<KIND, S> p;
     p.init();
     const int col = B.row0 + p.col(0), padN = padded<KIND>(d.n);
-    if constexpr (STEP != kGram) {
-        // the sums start from the addend: its loads overlap those of the
-        // first panels and need no registers of their own
-        const char *addend = d.addend + z * d.stackOut;
-        if (w.slice == 0 && p.group == 0) {
-            // (outside the matrix any of its values will do: the results there
-            // are replaced)
-            const int c = col < padN ? col : padN - FN;
-#pragma unroll
-            for (int e = 0; e < 16; ++e)
-#pragma unroll
-                for (int i = 0; i < FM; ++i) {
-                    const int row = A.row0 + p.row(i, e);
-                    float x[FN];
-                    load_run<KIND, FN>(addend + at<KIND>(d.m, row < d.m ? row : d.m - 1, c), x);
-#pragma unroll
-                    for (int j = 0; j < FN; ++j) p.acc[i][j][e] = d.ratio * x[j];
-                }
-        }
-    }
+    const char *addend = STEP == kGram ? nullptr : d.addend + z * d.stackOut;
+    const int panelsN = padN / panel_elements<KIND>();
+    if constexpr (STEP != kGram && kAddendEarly<S>)
+        load_panels<KIND, S>(p, dyn_lds + S::lds(KIND), addend, d.m, panelsN, A.row0, B.row0, 0);
     p.run(dyn_lds, A, B, w.t0, w.t1);
+    __builtin_amdgcn_s_waitcnt(7 << 4 | 15 << 8);   // vmcnt 0 (the addend, if no panel came)
     __syncthreads();
     if (!panel_join<KIND, S>(p, grid, w, dyn_lds)) return;
 
     // rows and columns of the padding become zeros
+    constexpr int PASSES = STEP == kGram || kAddendEarly<S> ? 1 : image_passes<KIND, S, false>();
 #pragma unroll
-    for (int e = 0; e < 16; ++e)
+    for (int pass = 0; pass < PASSES; ++pass) {
+        const char *image = dyn_lds + (kAddendEarly<S> ? S::lds(KIND) : 0);
+        if constexpr (STEP != kGram && !kAddendEarly<S>) {
+            __syncthreads();
+            load_panels<KIND, S>(p, dyn_lds, addend, d.m, panelsN, A.row0, B.row0, pass);
+            __builtin_amdgcn_s_waitcnt(7 << 4 | 15 << 8);   // vmcnt 0
+            __syncthreads();
+        }
+        constexpr int SPAN = S::BN / PASSES;   // columns of a pass
+        if (PASSES > 1 && p.wn * 32 * FN / SPAN != pass) continue;
 #pragma unroll
-        for (int i = 0; i < FM; ++i)
+        for (int e = 0; e < 16; ++e) {
 #pragma unroll
-            for (int j = 0; j < FN; ++j)
-                p.acc[i][j][e] = A.row0 + p.row(i, e) < d.m && col + j < d.n
-                                     ? d.factor * p.acc[i][j][e]
-                                     : 0.0f;
+            for (int i = 0; i < FM; ++i) {
+                float x[FN] = {};
+                if constexpr (STEP != kGram) {
+                    const int c = p.col(0) - pass * SPAN;
+                    load_run<KIND, FN>(image + at<KIND>(S::BM, p.row(i, e), c), x);
+                }
+#pragma unroll
+                for (int j = 0; j < FN; ++j) {
+                    float v = d.factor * p.acc[i][j][e];
+                    if constexpr (STEP != kGram) v += d.scale * x[j];
+                    p.acc[i][j][e] = A.row0 + p.row(i, e) < d.m && col + j < d.n ? v : 0.0f;
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j) asm volatile("" : "+v"(p.acc[i][j]));   // computed here
     if constexpr (STEP != kLast) {
-        const int panelsN = padN / panel_elements<KIND>();
         store_panels<KIND, S, false>(p, dyn_lds, d.out + z * d.stackOut, d.m, panelsN, A.row0, B.row0);
         // the other orientation: X^T, or the mirrored tile
         if (!kSymmetric || tm != tn)
@@ -334,13 +380,12 @@ __global__ __launch_bounds__(S::THREADS) void orth_product_kernel(ProductArgs d,
                                         padded<KIND>(d.m) / panel_elements<KIND>(), B.row0, A.row0);
     } else if (p.group > 0) {
     } else if (O.si != 1 || O.sk == 1) {
-        T *own = O.p + z * O.sb + (A.row0 + p.row(0, 0)) * O.si + col * O.sk;
+        // a lane's rows: four times FM in a row, then as many are another's
+        T *o = O.p + z * O.sb + (A.row0 + p.row(0, 0)) * O.si + col * O.sk;
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
 #pragma unroll
             for (int i = 0; i < FM; ++i) {
-                const int down = p.row(i, e) - p.row(0, 0);
-                T *o = own + down * O.si;
                 if (A.row0 + p.row(i, e) < d.m) {
                     if (O.sk == 1 && col + FN <= d.n) {
                         Run<T, FN> v;
@@ -353,7 +398,10 @@ __global__ __launch_bounds__(S::THREADS) void orth_product_kernel(ProductArgs d,
                             if (col + j < d.n) o[j * O.sk] = from_float<T>(p.acc[i][j][e] * kDown);
                     }
                 }
+                o += O.si;
+                asm volatile("" : "+v"(o));   // one pointer, not one per row
             }
+            if (e % 4 == 3) o += 4 * FM * O.si;
             __builtin_amdgcn_sched_barrier(0);
         }
     } else {   // neighbours in memory run along the rows, FM of which a lane holds
@@ -421,13 +469,15 @@ hipError_t product_launch(const ProductArgs &d, const PanelCut &c, const Workspa
                           const Stack<T> &O, int64_t batch, hipStream_t stream)
 {
     constexpr auto k = orth_product_kernel<KIND, STEP, S, T>;
-    const hipError_t e = allow_dynamic_lds<k>(S::lds(KIND));
+    constexpr int lds = S::lds(KIND) + (STEP != kGram && kAddendEarly<S>
+                                            ? S::TILE * (KIND == kPanelSplit ? 4 : 2) : 0);
+    const hipError_t e = allow_dynamic_lds<k>(lds);
     if (e != hipSuccess) return e;
     PanelGrid g;
     if (!panel_grid(g, batch, (d.m + S::BM - 1) / S::BM, (d.n + S::BN - 1) / S::BN,
                     tile_count<STEP>(S::BM, d.m, d.n), c, d.panels, w.slots, w.counters))
         return hipErrorInvalidValue;
-    hipLaunchKernelGGL(k, dim3((unsigned)c.blocks), dim3(S::THREADS), S::lds(KIND), stream, d, g, O);
+    hipLaunchKernelGGL(k, dim3((unsigned)c.blocks), dim3(S::THREADS), lds, stream, d, g, O);
     return hipGetLastError();
 }
 
@@ -517,8 +567,8 @@ gett_status_t orthogonalize_typed(const Problem &P, Stack<const T> G, Stack<T> O
         d.stackP = d.stackQ = SS;
         d.panels = quintic ? (int)panelsS : 0;
         d.out = d.outT = poly;
-        d.factor = (float)(quintic ? P.c * kDown : P.b);
-        d.ratio = (float)(quintic ? P.b / (P.c * kDown) : 1.0);
+        d.factor = (float)(P.c * kDown);
+        d.scale = (float)P.b;
         e = product<KIND, kPoly, T>(d, quad, slots, none, P.batch, P.stream);
         if (e != hipSuccess) return GETT_ERROR_HIP;
         d.P = poly;
@@ -531,7 +581,7 @@ gett_status_t orthogonalize_typed(const Problem &P, Stack<const T> G, Stack<T> O
         d.stackOutT = XT;
         d.panels = (int)panelsS;
         d.factor = kDown;
-        d.ratio = (float)P.a * kUp;
+        d.scale = (float)P.a;
         e = i + 1 < P.steps ? product<KIND, kUpdate, T>(d, update, slots, none, P.batch, P.stream)
                             : product<KIND, kLast, T>(d, update, slots, O, P.batch, P.stream);
         if (e != hipSuccess) return GETT_ERROR_HIP;
