@@ -10,6 +10,7 @@
  *   gett_mx_dequantize   the values a packed matrix stands for
  *   gett_mx_contract     C <- alpha * A * B^T + beta * C, A and B packed
  *   gett_mx_apply        the same with a float A that is quantised in the call
+ *   gett_mx_linear, gett_mx_linear_grad   a linear layer of a training step
  *   gett_orthogonalize   Newton-Schulz steps on a stack of matrices
  *
  * Element types are those of gett_dtype_t and GETT_BFLOAT16 / GETT_FLOAT16.
@@ -135,6 +136,39 @@ gett_status_t gett_mx_apply(int64_t m, int64_t n, int64_t k, double alpha, gett_
                             const void *codes_B, const void *scales_B, double beta,
                             gett_dtype_t dtype, void *C, int64_t stride_m, int64_t stride_n,
                             void *stream);
+
+/*
+ * gett_mx_linear -- Y <- Q(X) Q(W)^T, both quantised in the call, for training.
+ *
+ *   X   m x k, W   n x k, Y   m x n in X's type.
+ *   codes_xt, scales_xt   X^T packed (gett_mx_size(k, m)) as
+ *   codes_wt, scales_wt   and W^T packed (gett_mx_size(k, n)): what
+ *                         gett_mx_linear_grad needs, or NULL where not wanted.
+ *
+ * The same results as gett_mx_quantize and gett_mx_contract in fewer calls and
+ * launches.  Errors as for those; outputs must not overlap one another or an
+ * input.
+ */
+gett_status_t gett_mx_linear(int64_t m, int64_t n, int64_t k, gett_dtype_t dtype_X, const void *X,
+                             int64_t stride_xm, int64_t stride_xk, gett_dtype_t dtype_W,
+                             const void *W, int64_t stride_wn, int64_t stride_wk, void *Y,
+                             int64_t stride_ym, int64_t stride_yn, void *codes_xt,
+                             void *scales_xt, void *codes_wt, void *scales_wt, void *stream);
+
+/*
+ * gett_mx_linear_grad -- the gradients of gett_mx_linear,
+ *     dX <- Q(dY) Q(W^T)^T   (m x k, in dY's type),
+ *     dW <- Q(dY^T) Q(X^T)^T (n x k, in dtype_W),
+ * each product's operands packed along the direction it sums over; the
+ * gradient of the rounding itself is taken as one.  dX or dW may be NULL where
+ * not wanted (dX needs W^T, dW needs X^T).  Errors as for gett_mx_linear.
+ */
+gett_status_t gett_mx_linear_grad(int64_t m, int64_t n, int64_t k, gett_dtype_t dtype_Y,
+                                  const void *dY, int64_t stride_ym, int64_t stride_yn,
+                                  const void *codes_xt, const void *scales_xt,
+                                  const void *codes_wt, const void *scales_wt, void *dX,
+                                  int64_t stride_xm, int64_t stride_xk, gett_dtype_t dtype_W,
+                                  void *dW, int64_t stride_wn, int64_t stride_wk, void *stream);
 
 /*
  * gett_orthogonalize -- O <- the Newton-Schulz iterate of G, per matrix.

@@ -455,5 +455,6 @@ def contract(expr: str, A, B, C=None, alpha: float = 1.0, beta: float = 0.0, out
 
 # the matrix operators of include/gett_matrix.h
 from .matrix import (GETT_BFLOAT16, GETT_FLOAT16, MXTensor, gett_mx_apply,  # noqa: E402
-                     gett_mx_contract, gett_mx_dequantize, gett_mx_quantize, gett_mx_size,
+                     gett_mx_contract, gett_mx_dequantize, gett_mx_linear, gett_mx_linear_grad,
+                     gett_mx_quantize, gett_mx_size,
                      gett_orthogonalize, mx_linear, mx_matmul, mx_quantize, orthogonalize)

@@ -15,7 +15,9 @@
 // (unrounded, in X's own type) and a lane takes 32 rows of one column; four
 // lanes take one column's four blocks, so 64 bytes of a row of codes_t leave
 // together.  Scales are gathered in LDS and leave in runs of 512 bytes.
+#include "kernel.hpp"
 #include "matrix.hpp"
+#include "mx.hpp"
 
 namespace gett {
 namespace {
@@ -49,20 +51,40 @@ template <typename T> __device__ __forceinline__ int tile_at(int r, int c)
     return r * kT + (r >> 5) * (32 / (int)sizeof(T)) + c;
 }
 
-// `wide`: columns are neighbours in memory (stride_col 1).
+// One matrix to pack; tiles of columns and their reciprocal.  `wide`: columns
+// are neighbours in memory (stride_col 1).
+template <typename T> struct Job {
+    const T *X;
+    int64_t sr, sc;
+    int rows, cols, tilesC, blocks;
+    Recip tilesInv;
+    bool wide;
+    uint8_t *codes, *scales, *codesT, *scalesT;
+};
+
+// Workgroups of the first matrix, then those of the second (if there is one).
 template <typename T, bool ROWS, bool COLS>
-__global__ __launch_bounds__(kThreads) void mx_quantize_kernel(
-    const T *__restrict__ X, int64_t sr, int64_t sc, int rows, int cols, int tilesC, bool wide,
-    uint8_t *__restrict__ codes, uint8_t *__restrict__ scales, uint8_t *__restrict__ codesT,
-    uint8_t *__restrict__ scalesT)
+__global__ __launch_bounds__(kThreads) void mx_quantize_kernel(Job<T> first, Job<T> second)
 {
+    const bool is2 = (int)blockIdx.x >= first.blocks;
+    const T *const X = is2 ? second.X : first.X;
+    const int64_t sr = is2 ? second.sr : first.sr, sc = is2 ? second.sc : first.sc;
+    const int rows = is2 ? second.rows : first.rows, cols = is2 ? second.cols : first.cols;
+    const int tilesC = is2 ? second.tilesC : first.tilesC;
+    const bool wide = is2 ? second.wide : first.wide;
+    uint8_t *const codes = is2 ? second.codes : first.codes;
+    uint8_t *const scales = is2 ? second.scales : first.scales;
+    uint8_t *const codesT = is2 ? second.codesT : first.codesT;
+    uint8_t *const scalesT = is2 ? second.scalesT : first.scalesT;
+    const int block = (int)blockIdx.x - (is2 ? first.blocks : 0);
     __shared__ __attribute__((aligned(16))) T tile[COLS ? kT * kT + 3 * (32 / sizeof(T)) : 1];
     // [row or column][block]
     __shared__ __attribute__((aligned(16))) uint8_t sRow[ROWS ? kT : 1][4];
     __shared__ __attribute__((aligned(16))) uint8_t sCol[COLS ? kT : 1][4];
 
     const int tid = (int)threadIdx.x;
-    const int tr = (int)blockIdx.x / tilesC, tc = (int)blockIdx.x % tilesC;
+    const int tr = (int)quotient((uint32_t)block, tilesC, is2 ? second.tilesInv : first.tilesInv);
+    const int tc = block - tr * tilesC;
     const int row0 = tr * kT, col0 = tc * kT;
     const int tilesK = (int)mx_tiles(cols), tilesKT = (int)mx_tiles(rows);
     // this tile's columns (rows) lie inside the padded row of codes (codes_t)
@@ -200,24 +222,44 @@ __global__ __launch_bounds__(kThreads) void mx_dequantize_kernel(
     }
 }
 
-template <typename T>
-hipError_t quantize_typed(int64_t rows, int64_t cols, const void *X, int64_t sr, int64_t sc,
-                          uint8_t *codes, uint8_t *scales, uint8_t *codesT, uint8_t *scalesT,
-                          unsigned blocks, int tilesC, hipStream_t stream)
+// A job in kernel terms: rows are the direction of the larger stride.
+template <typename T> Job<T> job_of(QuantizeJob q)
 {
-    const T *x = static_cast<const T *>(X);
-    const int r = (int)rows, c = (int)cols;
-    const bool wide = sc == 1;
-    if (codes && codesT)
-        hipLaunchKernelGGL((mx_quantize_kernel<T, true, true>), dim3(blocks), dim3(kThreads), 0,
-                           stream, x, sr, sc, r, c, tilesC, wide, codes, scales, codesT, scalesT);
-    else if (codes)
-        hipLaunchKernelGGL((mx_quantize_kernel<T, true, false>), dim3(blocks), dim3(kThreads), 0,
-                           stream, x, sr, sc, r, c, tilesC, wide, codes, scales, codesT, scalesT);
+    if (q.sr == 1 && q.sc != 1) {   // the transpose is read along its rows
+        std::swap(q.rows, q.cols);
+        std::swap(q.sr, q.sc);
+        std::swap(q.codes, q.codesT);
+        std::swap(q.scales, q.scalesT);
+    }
+    // enough tiles for X and for the padding of the packed rows
+    const int64_t tilesR = q.codesT ? 2 * mx_tiles(q.rows) : (q.rows + kT - 1) / kT;
+    const int64_t tilesC = q.codes ? 2 * mx_tiles(q.cols) : (q.cols + kT - 1) / kT;
+    const int64_t blocks = tilesR * tilesC < INT32_MAX / 2 ? tilesR * tilesC : 0;
+    return {static_cast<const T *>(q.X), q.sr, q.sc, (int)q.rows, (int)q.cols, (int)tilesC,
+            (int)blocks, recip(tilesC), q.sc == 1, static_cast<uint8_t *>(q.codes),
+            static_cast<uint8_t *>(q.scales), static_cast<uint8_t *>(q.codesT),
+            static_cast<uint8_t *>(q.scalesT)};
+}
+
+template <typename T>
+gett_status_t quantize_typed(const QuantizeJob *q, int n, hipStream_t stream)
+{
+    const Job<T> a = job_of<T>(q[0]);
+    Job<T> b = {};
+    if (n == 2) b = job_of<T>(q[1]);
+    if (a.blocks == 0 || (n == 2 && b.blocks == 0)) return GETT_ERROR_NOT_SUPPORTED;
+    if (n == 2 && (!a.codes != !b.codes || !a.codesT != !b.codesT)) {   // one launch each
+        const gett_status_t st = quantize_typed<T>(q, 1, stream);
+        return st == GETT_SUCCESS ? quantize_typed<T>(q + 1, 1, stream) : st;
+    }
+    const dim3 grid((unsigned)(a.blocks + b.blocks)), block(kThreads);
+    if (a.codes && a.codesT)
+        hipLaunchKernelGGL((mx_quantize_kernel<T, true, true>), grid, block, 0, stream, a, b);
+    else if (a.codes)
+        hipLaunchKernelGGL((mx_quantize_kernel<T, true, false>), grid, block, 0, stream, a, b);
     else
-        hipLaunchKernelGGL((mx_quantize_kernel<T, false, true>), dim3(blocks), dim3(kThreads), 0,
-                           stream, x, sr, sc, r, c, tilesC, wide, codes, scales, codesT, scalesT);
-    return hipGetLastError();
+        hipLaunchKernelGGL((mx_quantize_kernel<T, false, true>), grid, block, 0, stream, a, b);
+    return hipGetLastError() == hipSuccess ? GETT_SUCCESS : GETT_ERROR_HIP;
 }
 
 template <typename T>
@@ -231,51 +273,18 @@ hipError_t dequantize_typed(int64_t rows, int64_t cols, const void *codes, const
     return hipGetLastError();
 }
 
-// status of a matrix argument: extents, strides, pointer
-gett_status_t matrix_ok(gett_dtype_t dtype, int64_t rows, int64_t cols, const void *X, int64_t sr,
-                        int64_t sc)
-{
-    if (!float_type(dtype) || rows < 0 || cols < 0 || sr < 1 || sc < 1)
-        return GETT_ERROR_INVALID_VALUE;
-    if (rows > 0 && cols > 0 && (!X || (uintptr_t)X % type_size(dtype)))
-        return GETT_ERROR_INVALID_VALUE;
-    return GETT_SUCCESS;
-}
-
 }  // namespace
 
-bool packed_ok(const void *codes, const void *scales)
+gett_status_t quantize_launch(gett_dtype_t dtype, const QuantizeJob *q, int n, hipStream_t stream)
 {
-    return codes && scales && (uintptr_t)codes % 16 == 0 && (uintptr_t)scales % 16 == 0;
-}
-
-gett_status_t quantize_launch(gett_dtype_t dtype, int64_t rows, int64_t cols, const void *X,
-                              int64_t sr, int64_t sc, void *codes, void *scales, void *codesT,
-                              void *scalesT, hipStream_t stream)
-{
-    if (rows == 0 || cols == 0) return GETT_SUCCESS;
-    if (sr == 1 && sc != 1) {   // the transpose is read along its rows
-        std::swap(rows, cols);
-        std::swap(sr, sc);
-        std::swap(codes, codesT);
-        std::swap(scales, scalesT);
-    }
-    // enough tiles for X and for the padding of the packed rows
-    const int64_t tilesR = codesT ? 2 * mx_tiles(rows) : (rows + kT - 1) / kT;
-    const int64_t tilesC = codes ? 2 * mx_tiles(cols) : (cols + kT - 1) / kT;
-    if (tilesR * tilesC >= INT32_MAX) return GETT_ERROR_NOT_SUPPORTED;
-    const unsigned blocks = (unsigned)(tilesR * tilesC);
-    uint8_t *c = static_cast<uint8_t *>(codes), *s = static_cast<uint8_t *>(scales);
-    uint8_t *ct = static_cast<uint8_t *>(codesT), *st = static_cast<uint8_t *>(scalesT);
-    hipError_t e;
-    if (dtype == GETT_FLOAT32)
-        e = quantize_typed<float>(rows, cols, X, sr, sc, c, s, ct, st, blocks, (int)tilesC, stream);
-    else if (dtype == GETT_BFLOAT16)
-        e = quantize_typed<bf16>(rows, cols, X, sr, sc, c, s, ct, st, blocks, (int)tilesC, stream);
-    else
-        e = quantize_typed<_Float16>(rows, cols, X, sr, sc, c, s, ct, st, blocks, (int)tilesC,
-                                     stream);
-    return e == hipSuccess ? GETT_SUCCESS : GETT_ERROR_HIP;
+    QuantizeJob some[2];
+    int m = 0;
+    for (int i = 0; i < n; ++i)
+        if (q[i].rows > 0 && q[i].cols > 0) some[m++] = q[i];
+    if (m == 0) return GETT_SUCCESS;
+    if (dtype == GETT_FLOAT32) return quantize_typed<float>(some, m, stream);
+    if (dtype == GETT_BFLOAT16) return quantize_typed<bf16>(some, m, stream);
+    return quantize_typed<_Float16>(some, m, stream);
 }
 
 }  // namespace gett
@@ -314,8 +323,8 @@ gett_status_t gett_mx_quantize(gett_dtype_t dtype, int64_t rows, int64_t cols, c
     for (int i = 0; i < 5; ++i)
         for (int j = i + 1; j < 5; ++j)
             if (p[i] && p[j] && overlaps(p[i], n[i], p[j], n[j])) return GETT_ERROR_INVALID_VALUE;
-    return quantize_launch(dtype, rows, cols, X, stride_row, stride_col, codes, scales, codes_t,
-                           scales_t, static_cast<hipStream_t>(stream));
+    const QuantizeJob q = {rows, cols, X, stride_row, stride_col, codes, scales, codes_t, scales_t};
+    return quantize_launch(dtype, &q, 1, static_cast<hipStream_t>(stream));
 }
 
 gett_status_t gett_mx_dequantize(gett_dtype_t dtype, int64_t rows, int64_t cols,

@@ -8,16 +8,12 @@
 // into the registers that the MFMA reads (a lane's two pieces of a panel are
 // 32 bytes of one row), so no byte waits for a barrier, and the eight partial
 // results are summed in wavefront order through LDS.
-#include "matrix.hpp"
 #include "launch.hpp"
+#include "matrix.hpp"
+#include "mx.hpp"
 #include "panel.hpp"
 
 namespace gett {
-
-bool packed_ok(const void *codes, const void *scales);
-gett_status_t quantize_launch(gett_dtype_t dtype, int64_t rows, int64_t cols, const void *X,
-                              int64_t sr, int64_t sc, void *codes, void *scales, void *codesT,
-                              void *scalesT, hipStream_t stream);
 
 namespace {
 
@@ -59,13 +55,25 @@ __device__ __forceinline__ void store_row(const Result<T> &o, int row, int col, 
 
 // ------------------------------------------------------------------- tiles ---
 
+// One product: its operands, its share of the launch and its result.
+template <typename T> struct TileJob {
+    PanelOperand A, B;
+    PanelGrid grid;
+    Result<T> o;
+    int blocks;
+};
+
+// Workgroups of the first product, then those of the second (if there is one).
 template <typename T, typename S>
-__global__ __launch_bounds__(S::THREADS) void mx_tile_kernel(PanelOperand A, PanelOperand B,
-                                                            PanelGrid grid, Result<T> o)
+__global__ __launch_bounds__(S::THREADS) void mx_tile_kernel(TileJob<T> first, TileJob<T> second)
 {
     extern __shared__ __attribute__((aligned(256))) char dyn_lds[];
+    const bool is2 = (int)blockIdx.x >= first.blocks;
+    PanelOperand A = is2 ? second.A : first.A, B = is2 ? second.B : first.B;
+    const PanelGrid grid = is2 ? second.grid : first.grid;
+    const Result<T> o = is2 ? second.o : first.o;
     int tm, tn;
-    const PanelItem w = panel_item(grid, (int)blockIdx.x);
+    const PanelItem w = panel_item(grid, (int)blockIdx.x - (is2 ? first.blocks : 0));
     panel_tile(grid, w.tile, tm, tn);
     A.row0 = tm * S::BM;
     B.row0 = tn * S::BN;
@@ -113,19 +121,16 @@ TilePlan tile_plan(int64_t m, int64_t n, int64_t panels)
     return p;
 }
 
-template <typename T, typename S>
-hipError_t tile_launch(const PanelOperand &A, const PanelOperand &B, int panels, const TilePlan &p,
-                       float *slots, int *counters, const Result<T> &o, hipStream_t stream)
+template <typename T, typename S> hipError_t tile_launch(const TileJob<T> *j, int n, hipStream_t stream)
 {
     constexpr auto k = mx_tile_kernel<T, S>;
     const hipError_t e = allow_dynamic_lds<k>(S::lds(kPanelMx));
     if (e != hipSuccess) return e;
-    const int64_t tilesM = (o.m + S::BM - 1) / S::BM, tilesN = (o.n + S::BN - 1) / S::BN;
-    PanelGrid g;
-    if (!panel_grid(g, 1, tilesM, tilesN, tilesM * tilesN, p.cut, panels, slots, counters))
-        return hipErrorInvalidValue;
-    hipLaunchKernelGGL(k, dim3((unsigned)p.cut.blocks), dim3(S::THREADS), S::lds(kPanelMx), stream,
-                       A, B, g, o);
+    TileJob<T> none = {};
+    const int64_t blocks = (int64_t)j[0].blocks + (n == 2 ? j[1].blocks : 0);
+    if (blocks >= INT32_MAX) return hipErrorInvalidValue;
+    hipLaunchKernelGGL(k, dim3((unsigned)blocks), dim3(S::THREADS), S::lds(kPanelMx), stream, j[0],
+                       n == 2 ? j[1] : none);
     return hipGetLastError();
 }
 
@@ -295,86 +300,127 @@ struct Packed {
     int64_t rows;
 };
 
-// Few rows go their own way; tiles get slots for shared sums behind the
-// `before` bytes of the stream's workspace that the caller has in use.
-bool few_rows(int64_t m, int64_t k) { return k > 0 && m <= 32; }
-
-template <typename T>
-hipError_t contract_typed(const Packed &A, const Packed &B, int64_t k, const TilePlan &plan,
-                          float *slots, int *counters, const Result<T> &o, hipStream_t stream)
-{
-    const int panels = (int)mx_tiles(k);
-    const uint8_t *ca = static_cast<const uint8_t *>(A.codes);
-    const uint8_t *sa = static_cast<const uint8_t *>(A.scales);
-    const uint8_t *cb = static_cast<const uint8_t *>(B.codes);
-    const uint8_t *sb = static_cast<const uint8_t *>(B.scales);
-    if (few_rows(o.m, k))
-        return o.m <= 16 ? few_launch<T, FewPacked<1>, 1>({ca, sa, o.m}, cb, sb, panels, o, stream)
-                         : few_launch<T, FewPacked<2>, 2>({ca, sa, o.m}, cb, sb, panels, o, stream);
-    const PanelOperand pa = {ca, sa, o.m, 0}, pb = {cb, sb, o.n, 0};
-    if (plan.shape == 0)
-        return tile_launch<T, Big>(pa, pb, panels, plan, slots, counters, o, stream);
-    if (plan.shape == 1)
-        return tile_launch<T, Mid>(pa, pb, panels, plan, slots, counters, o, stream);
-    return tile_launch<T, Small>(pa, pb, panels, plan, slots, counters, o, stream);
-}
-
-template <typename T>
-Result<T> result(void *C, int64_t sm, int64_t sn, int64_t m, int64_t n, double alpha, double beta)
-{
-    return Result<T>{static_cast<T *>(C), sm, sn, (int)m, (int)n, (float)alpha, (float)beta};
-}
-
-// What a product of m x k by n x k needs of the workspace, with C's neighbours
-// along n (or exchanged).
-struct Need {
-    bool swapped;
+// A product of m x k by n x k: operands (exchanged where C's neighbours lie
+// along m: C^T = B A^T), result and plan; few rows need no tiles.  The plan
+// depends on sizes and strides alone: a call whose operands go to the workspace
+// makes its products without pointers, to size it, and then again with them.
+struct Product {
+    Packed A, B;
+    int64_t k;
+    void *C;
+    int64_t sm, sn;
+    bool few;
     TilePlan plan;
 };
-Need need_of(int64_t m, int64_t n, int64_t k, int64_t sm, int64_t sn)
+Product product_of(Packed A, Packed B, int64_t k, void *C, int64_t sm, int64_t sn)
 {
-    Need w = {};
-    w.swapped = sm == 1 && sn != 1;   // C's neighbours lie along m: C^T = B A^T
-    if (w.swapped) std::swap(m, n);
-    if (!few_rows(m, k)) w.plan = tile_plan(m, n, mx_tiles(k));
-    return w;
+    Product p = {A, B, k, C, sm, sn, false, {}};
+    if (sm == 1 && sn != 1) {
+        std::swap(p.A, p.B);
+        std::swap(p.sm, p.sn);
+    }
+    p.few = k > 0 && p.A.rows <= 32;
+    if (!p.few) p.plan = tile_plan(p.A.rows, p.B.rows, mx_tiles(k));
+    return p;
 }
 
-gett_status_t contract_launch(Packed A, Packed B, int64_t k, const Need &need, float *slots,
-                              int *counters, double alpha, double beta, gett_dtype_t dtype, void *C,
-                              int64_t sm, int64_t sn, hipStream_t stream)
+template <typename T> Result<T> result(const Product &p, double alpha, double beta)
 {
-    if (need.swapped) {
-        std::swap(A, B);
-        std::swap(sm, sn);
+    return {static_cast<T *>(p.C), p.sm, p.sn, (int)p.A.rows, (int)p.B.rows, (float)alpha,
+            (float)beta};
+}
+
+template <typename T>
+hipError_t few_packed(const Product &p, double alpha, double beta, hipStream_t stream)
+{
+    const int panels = (int)mx_tiles(p.k), m = (int)p.A.rows;
+    const uint8_t *ca = static_cast<const uint8_t *>(p.A.codes);
+    const uint8_t *sa = static_cast<const uint8_t *>(p.A.scales);
+    const Result<T> o = result<T>(p, alpha, beta);
+    return m <= 16 ? few_launch<T, FewPacked<1>, 1>({ca, sa, m}, p.B.codes, p.B.scales, panels, o, stream)
+                   : few_launch<T, FewPacked<2>, 2>({ca, sa, m}, p.B.codes, p.B.scales, panels, o, stream);
+}
+
+// One or two products of one result type; slots for shared sums lie at `slots`
+// (the second product's behind the first's), counters likewise.
+template <typename T>
+hipError_t contract_typed(const Product *p, int n, float *slots, int *counters, double alpha,
+                          double beta, hipStream_t stream)
+{
+    TileJob<T> jobs[2];
+    for (int i = 0; i < n; ++i) {
+        if (p[i].few) {
+            const hipError_t e = few_packed<T>(p[i], alpha, beta, stream);
+            if (e != hipSuccess) return e;
+            continue;
+        }
+        const TilePlan &plan = p[i].plan;
+        const int64_t edge = plan.shape == 0 ? Big::BM : plan.shape == 1 ? Mid::BM : Small::BM;
+        const int64_t tm = (p[i].A.rows + edge - 1) / edge, tn = (p[i].B.rows + edge - 1) / edge;
+        TileJob<T> &j = jobs[i];
+        j.A = {static_cast<const uint8_t *>(p[i].A.codes),
+               static_cast<const uint8_t *>(p[i].A.scales), (int)p[i].A.rows, 0};
+        j.B = {static_cast<const uint8_t *>(p[i].B.codes),
+               static_cast<const uint8_t *>(p[i].B.scales), (int)p[i].B.rows, 0};
+        j.o = result<T>(p[i], alpha, beta);
+        j.blocks = (int)plan.cut.blocks;
+        if (!panel_grid(j.grid, 1, tm, tn, tm * tn, plan.cut, (int)mx_tiles(p[i].k), slots, counters))
+            return hipErrorInvalidValue;
+        slots += plan.slotBytes / 4;
+        counters += plan.counters;
     }
-    const int64_t m = A.rows, n = B.rows;
-    hipError_t e;
-    if (dtype == GETT_FLOAT32)
-        e = contract_typed<float>(A, B, k, need.plan, slots, counters,
-                                  result<float>(C, sm, sn, m, n, alpha, beta), stream);
-    else if (dtype == GETT_BFLOAT16)
-        e = contract_typed<bf16>(A, B, k, need.plan, slots, counters,
-                                 result<bf16>(C, sm, sn, m, n, alpha, beta), stream);
-    else
-        e = contract_typed<_Float16>(A, B, k, need.plan, slots, counters,
-                                     result<_Float16>(C, sm, sn, m, n, alpha, beta), stream);
+    auto launch = [&](const TileJob<T> *j, int count, int shape) {
+        return shape == 0   ? tile_launch<T, Big>(j, count, stream)
+               : shape == 1 ? tile_launch<T, Mid>(j, count, stream)
+                            : tile_launch<T, Small>(j, count, stream);
+    };
+    if (n == 2 && !p[0].few && !p[1].few && p[0].plan.shape == p[1].plan.shape)
+        return launch(jobs, 2, p[0].plan.shape);
+    for (int i = 0; i < n; ++i)
+        if (!p[i].few) {
+            const hipError_t e = launch(jobs + i, 1, p[i].plan.shape);
+            if (e != hipSuccess) return e;
+        }
+    return hipSuccess;
+}
+
+gett_status_t contract_launch(const Product *p, int n, float *slots, int *counters, double alpha,
+                              double beta, gett_dtype_t dtype, hipStream_t stream)
+{
+    const hipError_t e =
+        dtype == GETT_FLOAT32    ? contract_typed<float>(p, n, slots, counters, alpha, beta, stream)
+        : dtype == GETT_BFLOAT16 ? contract_typed<bf16>(p, n, slots, counters, alpha, beta, stream)
+                                 : contract_typed<_Float16>(p, n, slots, counters, alpha, beta, stream);
     return e == hipSuccess ? GETT_SUCCESS : GETT_ERROR_HIP;
 }
 
-// the whole call: the product alone
+// The stream's workspace for a call: `before` bytes of its own, then the slots
+// of its products.
+gett_status_t product_workspace(const Product *p, int n, int64_t before, hipStream_t stream,
+                                Partials &w)
+{
+    int64_t bytes = before, counters = 0;
+    for (int i = 0; i < n; ++i) {
+        bytes += p[i].plan.slotBytes;
+        counters += p[i].plan.counters;
+    }
+    return bytes == 0 ? GETT_SUCCESS
+                      : stream_workspace(stream, (uint64_t)counters, (uint64_t)bytes, w);
+}
+float *slots_of(const Partials &w, int64_t before)
+{
+    return reinterpret_cast<float *>(static_cast<char *>(w.tiles) + before);
+}
+
+// the whole call: one product of packed operands
 gett_status_t contract(const Packed &A, const Packed &B, int64_t k, double alpha, double beta,
                        gett_dtype_t dtype, void *C, int64_t sm, int64_t sn, hipStream_t stream)
 {
-    const Need need = need_of(A.rows, B.rows, k, sm, sn);
+    const Product p = product_of(A, B, k, C, sm, sn);
     Partials w;
-    if (need.plan.slotBytes > 0) {
-        const gett_status_t ws = stream_workspace(stream, (uint64_t)need.plan.counters,
-                                                  (uint64_t)need.plan.slotBytes, w);
-        if (ws != GETT_SUCCESS) return ws;
-    }
-    return contract_launch(A, B, k, need, static_cast<float *>(w.tiles), w.counters, alpha, beta,
-                           dtype, C, sm, sn, stream);
+    const gett_status_t ws = product_workspace(&p, 1, 0, stream, w);
+    if (ws != GETT_SUCCESS) return ws;
+    return contract_launch(&p, 1, slots_of(w, 0), w.counters, alpha, beta, dtype, stream);
 }
 
 template <typename TA, typename T>
@@ -391,6 +437,12 @@ hipError_t few_float_of(gett_dtype_t dtypeA, const void *A, int64_t sam, int64_t
     if (dtypeA == GETT_FLOAT32) return few_float<float, T>(A, sam, sak, k, B, o, stream);
     if (dtypeA == GETT_BFLOAT16) return few_float<bf16, T>(A, sam, sak, k, B, o, stream);
     return few_float<_Float16, T>(A, sam, sak, k, B, o, stream);
+}
+
+template <typename T>
+Result<T> few_result(void *C, int64_t sm, int64_t sn, int64_t m, int64_t n, double alpha, double beta)
+{
+    return {static_cast<T *>(C), sm, sn, (int)m, (int)n, (float)alpha, (float)beta};
 }
 
 // C's arguments; `C` may be null where C is empty
@@ -463,34 +515,160 @@ gett_status_t gett_mx_apply(int64_t m, int64_t n, int64_t k, double alpha, gett_
     if (overlaps(C, bytesC, A, bytesA) || !clear_of(C, bytesC, codes_B, scales_B, n, k))
         return GETT_ERROR_INVALID_VALUE;
     if (m <= 16) {
-        const Packed B = {codes_B, scales_B, n};
+        const Packed W = {codes_B, scales_B, n};
         hipError_t e;
         if (dtype == GETT_FLOAT32)
-            e = few_float_of<float>(dtype_A, A, stride_am, stride_ak, k, B,
-                                    result<float>(C, stride_m, stride_n, m, n, alpha, beta), s);
+            e = few_float_of<float>(dtype_A, A, stride_am, stride_ak, k, W,
+                                    few_result<float>(C, stride_m, stride_n, m, n, alpha, beta), s);
         else if (dtype == GETT_BFLOAT16)
-            e = few_float_of<bf16>(dtype_A, A, stride_am, stride_ak, k, B,
-                                   result<bf16>(C, stride_m, stride_n, m, n, alpha, beta), s);
+            e = few_float_of<bf16>(dtype_A, A, stride_am, stride_ak, k, W,
+                                   few_result<bf16>(C, stride_m, stride_n, m, n, alpha, beta), s);
         else
-            e = few_float_of<_Float16>(dtype_A, A, stride_am, stride_ak, k, B,
-                                       result<_Float16>(C, stride_m, stride_n, m, n, alpha, beta),
+            e = few_float_of<_Float16>(dtype_A, A, stride_am, stride_ak, k, W,
+                                       few_result<_Float16>(C, stride_m, stride_n, m, n, alpha, beta),
                                        s);
         return e == hipSuccess ? GETT_SUCCESS : GETT_ERROR_HIP;
     }
     // A's packed copy and the slots of shared sums, in the stream's workspace.
     // The hold lasts until both launches are enqueued.
     const int64_t codeBytes = mx_code_bytes(m, k), packed = codeBytes + mx_scale_bytes(m, k);
-    const Need need = need_of(m, n, k, stride_m, stride_n);
+    const Packed B = {codes_B, scales_B, n};
+    Product p = product_of({nullptr, nullptr, m}, B, k, C, stride_m, stride_n);
     Partials w;
-    gett_status_t ws = stream_workspace(s, (uint64_t)need.plan.counters,
-                                        (uint64_t)(packed + need.plan.slotBytes), w);
+    gett_status_t ws = product_workspace(&p, 1, packed, s, w);
     if (ws != GETT_SUCCESS) return ws;
     char *codes = static_cast<char *>(w.tiles), *scales = codes + codeBytes;
-    ws = quantize_launch(dtype_A, m, k, A, stride_am, stride_ak, codes, scales, nullptr, nullptr, s);
+    p = product_of({codes, scales, m}, B, k, C, stride_m, stride_n);
+    const QuantizeJob q = {m, k, A, stride_am, stride_ak, codes, scales, nullptr, nullptr};
+    ws = quantize_launch(dtype_A, &q, 1, s);
     if (ws != GETT_SUCCESS) return ws;
-    return contract_launch({codes, scales, m}, {codes_B, scales_B, n}, k, need,
-                           reinterpret_cast<float *>(codes + packed), w.counters, alpha, beta, dtype,
-                           C, stride_m, stride_n, s);
+    return contract_launch(&p, 1, slots_of(w, packed), w.counters, alpha, beta, dtype, s);
+}
+
+gett_status_t gett_mx_linear(int64_t m, int64_t n, int64_t k, gett_dtype_t dtype_X, const void *X,
+                             int64_t stride_xm, int64_t stride_xk, gett_dtype_t dtype_W,
+                             const void *W, int64_t stride_wn, int64_t stride_wk, void *Y,
+                             int64_t stride_ym, int64_t stride_yn, void *codes_xt,
+                             void *scales_xt, void *codes_wt, void *scales_wt, void *stream)
+{
+    using namespace gett;
+    gett_status_t st = matrix_ok(dtype_X, m, k, X, stride_xm, stride_xk);
+    if (st == GETT_SUCCESS) st = matrix_ok(dtype_W, n, k, W, stride_wn, stride_wk);
+    if (st == GETT_SUCCESS) st = result_ok(m, n, k, dtype_X, Y, stride_ym, stride_yn);
+    if (st != GETT_SUCCESS) return st;
+    const bool xt = codes_xt || scales_xt, wt = codes_wt || scales_wt;
+    if ((xt && !packed_ok(codes_xt, scales_xt)) || (wt && !packed_ok(codes_wt, scales_wt)))
+        return GETT_ERROR_INVALID_VALUE;
+    if ((xt && m >= kMaxCols) || (wt && n >= kMaxCols)) return GETT_ERROR_NOT_SUPPORTED;
+    // every output clear of the inputs and of the other outputs
+    struct Range {
+        const void *p;
+        int64_t n;
+    };
+    auto whole = [](gett_dtype_t t, int64_t r, int64_t c, const void *p, int64_t sr, int64_t sc) {
+        return Range{r > 0 && c > 0 ? p : nullptr, r > 0 && c > 0 ? span_bytes(r, c, sr, sc, type_size(t)) : 0};
+    };
+    const Range out[5] = {whole(dtype_X, m, n, Y, stride_ym, stride_yn),
+                          {codes_xt, mx_code_bytes(k, m)}, {scales_xt, mx_scale_bytes(k, m)},
+                          {codes_wt, mx_code_bytes(k, n)}, {scales_wt, mx_scale_bytes(k, n)}};
+    const Range in[2] = {whole(dtype_X, m, k, X, stride_xm, stride_xk),
+                         whole(dtype_W, n, k, W, stride_wn, stride_wk)};
+    if (in[0].n < 0 || in[1].n < 0) return GETT_ERROR_NOT_SUPPORTED;
+    for (int i = 0; i < 5; ++i) {
+        for (int j = i + 1; j < 5; ++j)
+            if (out[i].p && out[j].p && overlaps(out[i].p, out[i].n, out[j].p, out[j].n))
+                return GETT_ERROR_INVALID_VALUE;
+        for (const Range &x : in)
+            if (out[i].p && x.p && overlaps(out[i].p, out[i].n, x.p, x.n))
+                return GETT_ERROR_INVALID_VALUE;
+    }
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    const int64_t cx = mx_code_bytes(m, k), px = cx + mx_scale_bytes(m, k);
+    const int64_t cw = mx_code_bytes(n, k), pw = cw + mx_scale_bytes(n, k);
+    Product p = product_of({nullptr, nullptr, m}, {nullptr, nullptr, n}, k, Y, stride_ym, stride_yn);
+    Partials w;
+    gett_status_t ws = product_workspace(&p, 1, px + pw, s, w);
+    if (ws != GETT_SUCCESS) return ws;
+    char *x = static_cast<char *>(w.tiles), *y = x + px;
+    p = product_of({x, x + cx, m}, {y, y + cw, n}, k, Y, stride_ym, stride_yn);
+    const QuantizeJob q[2] = {
+        {m, k, X, stride_xm, stride_xk, x, x + cx, codes_xt, scales_xt},
+        {n, k, W, stride_wn, stride_wk, y, y + cw, codes_wt, scales_wt}};
+    if (dtype_X == dtype_W) {
+        ws = quantize_launch(dtype_X, q, 2, s);
+    } else {
+        ws = quantize_launch(dtype_X, q, 1, s);
+        if (ws == GETT_SUCCESS) ws = quantize_launch(dtype_W, q + 1, 1, s);
+    }
+    if (ws != GETT_SUCCESS || m == 0 || n == 0) return ws;
+    return contract_launch(&p, 1, slots_of(w, px + pw), w.counters, k > 0 ? 1.0 : 0.0, 0.0, dtype_X, s);
+}
+
+gett_status_t gett_mx_linear_grad(int64_t m, int64_t n, int64_t k, gett_dtype_t dtype_Y,
+                                  const void *dY, int64_t stride_ym, int64_t stride_yn,
+                                  const void *codes_xt, const void *scales_xt,
+                                  const void *codes_wt, const void *scales_wt, void *dX,
+                                  int64_t stride_xm, int64_t stride_xk, gett_dtype_t dtype_W,
+                                  void *dW, int64_t stride_wn, int64_t stride_wk, void *stream)
+{
+    using namespace gett;
+    gett_status_t st = matrix_ok(dtype_Y, m, n, dY, stride_ym, stride_yn);
+    if (st != GETT_SUCCESS) return st;
+    if (!float_type(dtype_W) || k < 0) return GETT_ERROR_INVALID_VALUE;
+    if (!dX && !dW) return m > 0 && n > 0 && k > 0 ? GETT_ERROR_INVALID_VALUE : GETT_SUCCESS;
+    if (dX) st = result_ok(m, k, n, dtype_Y, dX, stride_xm, stride_xk);
+    if (dW && st == GETT_SUCCESS) st = result_ok(n, k, m, dtype_W, dW, stride_wn, stride_wk);
+    if (st != GETT_SUCCESS) return st;
+    const bool sum = m > 0 && n > 0 && k > 0;
+    if (sum && ((dX && !packed_ok(codes_wt, scales_wt)) || (dW && !packed_ok(codes_xt, scales_xt))))
+        return GETT_ERROR_INVALID_VALUE;
+    const int64_t bytesY = sum ? span_bytes(m, n, stride_ym, stride_yn, type_size(dtype_Y)) : 0;
+    const int64_t bytesX = m > 0 && k > 0 && dX ? span_bytes(m, k, stride_xm, stride_xk, type_size(dtype_Y)) : 0;
+    const int64_t bytesW = n > 0 && k > 0 && dW ? span_bytes(n, k, stride_wn, stride_wk, type_size(dtype_W)) : 0;
+    if (bytesY < 0) return GETT_ERROR_NOT_SUPPORTED;
+    if (bytesX && bytesW && overlaps(dX, bytesX, dW, bytesW)) return GETT_ERROR_INVALID_VALUE;
+    for (int i = 0; i < 2 && sum; ++i) {
+        const void *o = i ? dW : dX;
+        const int64_t bytes = i ? bytesW : bytesX;
+        if (!o) continue;
+        if (overlaps(o, bytes, dY, bytesY) || (dX && !clear_of(o, bytes, codes_wt, scales_wt, k, n)) ||
+            (dW && !clear_of(o, bytes, codes_xt, scales_xt, k, m)))
+            return GETT_ERROR_INVALID_VALUE;
+    }
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    // dX = dY W: sums over n;  dW = dY^T X: sums over m
+    const int64_t cd = mx_code_bytes(m, n), pd = dX ? cd + mx_scale_bytes(m, n) : 0;
+    const int64_t ct = mx_code_bytes(n, m), pt = dW ? ct + mx_scale_bytes(n, m) : 0;
+    const bool wantX = dX && m > 0 && k > 0, wantW = dW && n > 0 && k > 0;
+    if (!wantX && !wantW) return GETT_SUCCESS;
+    const int count = wantX && wantW ? 2 : 1;
+    Product p[2];
+    auto make = [&](const char *d, const char *t) {
+        int i = 0;
+        if (wantX)
+            p[i++] = product_of({d, d + cd, m}, {codes_wt, scales_wt, k}, n, dX, stride_xm, stride_xk);
+        if (wantW)
+            p[i] = product_of({t, t + ct, n}, {codes_xt, scales_xt, k}, m, dW, stride_wn, stride_wk);
+    };
+    make(nullptr, nullptr);
+    Partials w;
+    gett_status_t ws = product_workspace(p, count, pd + pt, s, w);
+    if (ws != GETT_SUCCESS) return ws;
+    char *d = static_cast<char *>(w.tiles), *t = d + pd;
+    make(d, t);
+    if (sum) {
+        const QuantizeJob q = {m, n, dY, stride_ym, stride_yn, wantX ? d : nullptr, wantX ? d + cd : nullptr,
+                               wantW ? t : nullptr, wantW ? t + ct : nullptr};
+        ws = quantize_launch(dtype_Y, &q, 1, s);
+        if (ws != GETT_SUCCESS) return ws;
+    }
+    if (dtype_W == dtype_Y || count == 1)
+        return contract_launch(p, count, slots_of(w, pd + pt), w.counters, 1.0, 0.0,
+                               wantX ? dtype_Y : dtype_W, s);
+    ws = contract_launch(p, 1, slots_of(w, pd + pt), w.counters, 1.0, 0.0, dtype_Y, s);
+    if (ws != GETT_SUCCESS) return ws;
+    return contract_launch(p + 1, 1, slots_of(w, pd + pt + p[0].plan.slotBytes),
+                           w.counters + p[0].plan.counters, 1.0, 0.0, dtype_W, s);
 }
 
 }  // extern "C"

@@ -36,6 +36,10 @@ def _lib():
                 ("gett_mx_dequantize", [i, i64, i64, p, p, p, i64, i64, p]),
                 ("gett_mx_contract", [i64, i64, i64, d, p, p, p, p, d, i, p, i64, i64, p]),
                 ("gett_mx_apply", [i64, i64, i64, d, i, p, i64, i64, p, p, d, i, p, i64, i64, p]),
+                ("gett_mx_linear", [i64, i64, i64, i, p, i64, i64, i, p, i64, i64, p, i64, i64, p,
+                                    p, p, p, p]),
+                ("gett_mx_linear_grad", [i64, i64, i64, i, p, i64, i64, p, p, p, p, p, i64, i64, i,
+                                         p, i64, i64, p]),
                 ("gett_orthogonalize", [i, i64, i64, i64, p, i64, i64, i64, d, d, d, d, i, p, i64,
                                         i64, i64, p])):
             f = getattr(lib, name)
@@ -92,17 +96,50 @@ def gett_orthogonalize(dtype: int, batch: int, rows: int, cols: int, G: int, str
                                      ostride_row, ostride_col, stream or None)
 
 
-# ------------------------------------------------------ torch convenience ---
+def gett_mx_linear(m: int, n: int, k: int, dtype_X: int, X: int, stride_xm: int, stride_xk: int,
+                   dtype_W: int, W: int, stride_wn: int, stride_wk: int, Y: int, stride_ym: int,
+                   stride_yn: int, codes_xt: int, scales_xt: int, codes_wt: int, scales_wt: int,
+                   stream: int = 0) -> int:
+    return _lib().gett_mx_linear(m, n, k, dtype_X, X or None, stride_xm, stride_xk, dtype_W,
+                                 W or None, stride_wn, stride_wk, Y or None, stride_ym, stride_yn,
+                                 codes_xt or None, scales_xt or None, codes_wt or None,
+                                 scales_wt or None, stream or None)
 
-_codes = None
+
+def gett_mx_linear_grad(m: int, n: int, k: int, dtype_Y: int, dY: int, stride_ym: int,
+                        stride_yn: int, codes_xt: int, scales_xt: int, codes_wt: int,
+                        scales_wt: int, dX: int, stride_xm: int, stride_xk: int, dtype_W: int,
+                        dW: int, stride_wn: int, stride_wk: int, stream: int = 0) -> int:
+    return _lib().gett_mx_linear_grad(m, n, k, dtype_Y, dY or None, stride_ym, stride_yn,
+                                      codes_xt or None, scales_xt or None, codes_wt or None,
+                                      scales_wt or None, dX or None, stride_xm, stride_xk, dtype_W,
+                                      dW or None, stride_wn, stride_wk, stream or None)
+
+
+# ------------------------------------------------------ torch convenience ---
+#
+# A call is a few microseconds of host time, as long as a small matrix's
+# kernel: torch is looked up once, tensors are compared as torch hands them
+# out, a packed matrix is one allocation whose parts are made into tensors
+# when asked for, and the C functions are called directly.
+
+_torch = None
+_codes = {}
+
+
+def _start():
+    """torch and the element types' codes, on the first use."""
+    global _torch
+    import torch
+    _codes.update({torch.float32: GETT_FLOAT32, torch.bfloat16: GETT_BFLOAT16,
+                   torch.float16: GETT_FLOAT16})
+    _torch = torch
+    _lib()
 
 
 def _code(dtype) -> int:
-    global _codes
-    if _codes is None:
-        import torch
-        _codes = {torch.float32: GETT_FLOAT32, torch.bfloat16: GETT_BFLOAT16,
-                  torch.float16: GETT_FLOAT16}
+    if _torch is None:
+        _start()
     c = _codes.get(dtype)
     if c is None:
         raise TypeError(f"unsupported dtype {dtype}: float32, bfloat16 or float16 only")
@@ -112,6 +149,20 @@ def _code(dtype) -> int:
 def _device(name, t):
     if not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
+
+
+def _matrix(name, t):
+    """Element type code, rows, columns and strides of a device matrix."""
+    shape = t.shape
+    if len(shape) != 2:
+        raise ValueError(f"{name} must be a matrix")
+    code = _code(t.dtype)
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    (r, c), (sr, sc) = shape, t.stride()
+    if sr < 1 or sc < 1 or r < 2 or c < 2:
+        sr, sc = _strides(t)
+    return code, r, c, sr, sc
 
 
 def _strides(t):
@@ -124,12 +175,17 @@ def _strides(t):
     return (sr if r > 1 else max(c, 1)), (sc if c > 1 else 1)
 
 
+def _sizes(rows, cols):
+    t = (cols + 255) >> 8
+    return rows * t * 128, t * 8 * ((rows + 15) & -16)
+
+
 class MXTensor:
     """A rows x cols matrix in microscaled 4 bits, packed along its columns.
 
     ``codes`` and ``scales`` are uint8 device tensors of gett_mx_size's bytes."""
 
-    __slots__ = ("rows", "cols", "codes", "scales")
+    __slots__ = ("rows", "cols", "_buffer", "_at", "_codes", "_scales")
 
     def __init__(self, rows: int, cols: int, codes, scales):
         c, s = _sizes(rows, cols)
@@ -137,39 +193,56 @@ class MXTensor:
             if t.numel() * t.element_size() != n or not t.is_contiguous():
                 raise ValueError(f"{name} must hold {n} contiguous bytes")
             _device(name, t)
-        self.rows, self.cols, self.codes, self.scales = rows, cols, codes, scales
+        self.rows, self.cols = rows, cols
+        self._buffer, self._at = (codes, scales), None
+        self._codes, self._scales = codes.data_ptr(), scales.data_ptr()
 
     @property
     def shape(self):
         return (self.rows, self.cols)
 
+    @property
+    def device(self):
+        return (self._buffer[0] if self._at is None else self._buffer).device
+
+    @property
+    def codes(self):
+        if self._at is None:
+            return self._buffer[0]
+        return self._buffer[self._at:self._at + _sizes(self.rows, self.cols)[0]]
+
+    @property
+    def scales(self):
+        if self._at is None:
+            return self._buffer[1]
+        c, s = _sizes(self.rows, self.cols)
+        return self._buffer[self._at + c:self._at + c + s]
+
     def dequantize(self, dtype=None, out=None):
         """The values, as float32 unless `dtype` or `out` says otherwise."""
-        import torch
+        r, c = self.rows, self.cols
         if out is None:
-            out = torch.empty((self.rows, self.cols), dtype=dtype or torch.float32,
-                              device=self.codes.device)
-        elif out.shape != self.shape or (dtype is not None and out.dtype != dtype):
-            raise ValueError("out differs in shape or dtype")
-        code = _code(out.dtype)
-        _device("out", out)
-        sr, sc = _strides(out)
-        st = _lib().gett_mx_dequantize(code, self.rows, self.cols, self.codes.data_ptr(),
-                                       self.scales.data_ptr(), out.data_ptr(), sr, sc,
+            if _torch is None:
+                _start()
+            dtype = dtype or _torch.float32
+            code = _code(dtype)
+            out = _torch.empty((r, c), dtype=dtype, device=self.device)
+            sr, sc = c or 1, 1
+        else:
+            if tuple(out.shape) != (r, c) or (dtype is not None and out.dtype != dtype):
+                raise ValueError("out differs in shape or dtype")
+            code, _, _, sr, sc = _matrix("out", out)
+        st = _bound.gett_mx_dequantize(code, r, c, self._codes, self._scales, out.data_ptr(), sr, sc,
                                        _package._current_stream())
         if st != 0:
             raise GettError(st, "gett_mx_dequantize")
         return out
 
 
-def _sizes(rows, cols):
-    t = (cols + 255) // 256
-    return rows * t * 128, t * 8 * ((rows + 15) // 16 * 16)
-
-
-def _packed(rows, cols, codes, scales):
+def _packed(rows, cols, buffer, at, codes, scales):
+    """A packed matrix at byte `at` of a buffer; addresses of its parts."""
     q = MXTensor.__new__(MXTensor)
-    q.rows, q.cols, q.codes, q.scales = rows, cols, codes, scales
+    q.rows, q.cols, q._buffer, q._at, q._codes, q._scales = rows, cols, buffer, at, codes, scales
     return q
 
 
@@ -177,33 +250,31 @@ def mx_quantize(x, along: str = "cols"):
     """Pack a matrix: ``"cols"`` along its columns (x as an operand of x @ w.T),
     ``"rows"`` along its rows (its transpose as an operand), ``"both"`` in one
     pass, as a pair."""
-    import torch
     if along not in ("cols", "rows", "both"):
         raise ValueError("along must be 'cols', 'rows' or 'both'")
-    if x.dim() != 2:
-        raise ValueError("a matrix is needed")
-    code = _code(x.dtype)
-    _device("x", x)
-    r, c = x.shape
-    sr, sc = _strides(x)
-    n, s = _sizes(r, c) if along != "rows" else (0, 0)
-    nt, st_ = _sizes(c, r) if along != "cols" else (0, 0)
+    code, r, c, sr, sc = _matrix("x", x)
     # one allocation; every part a multiple of 16 bytes
-    buf = torch.empty(n + s + nt + st_, dtype=torch.uint8, device=x.device)
+    n = s = nt = sn = 0
+    if along != "rows":
+        n, s = _sizes(r, c)
+    if along != "cols":
+        nt, sn = _sizes(c, r)
+    buf = _torch.empty(n + s + nt + sn, dtype=_torch.uint8, device=x.device)
     p = buf.data_ptr()
-    st = _lib().gett_mx_quantize(code, r, c, x.data_ptr(), sr, sc,
-                                 p if along != "rows" else None,
-                                 p + n if along != "rows" else None,
-                                 p + n + s if along != "cols" else None,
-                                 p + n + s + nt if along != "cols" else None, _package._current_stream())
+    codes = scales = codes_t = scales_t = None
+    if along != "rows":
+        codes, scales = p, p + n
+    if along != "cols":
+        codes_t = p + n + s
+        scales_t = codes_t + nt
+    st = _bound.gett_mx_quantize(code, r, c, x.data_ptr(), sr, sc, codes, scales, codes_t, scales_t,
+                                 _package._current_stream())
     if st != 0:
         raise GettError(st, "gett_mx_quantize")
-    out = []
-    if along != "rows":
-        out.append(_packed(r, c, buf[:n], buf[n:n + s]))
-    if along != "cols":
-        out.append(_packed(c, r, buf[n + s:n + s + nt], buf[n + s + nt:]))
-    return tuple(out) if along == "both" else out[0]
+    if along == "cols":
+        return _packed(r, c, buf, 0, codes, scales)
+    t = _packed(c, r, buf, n + s, codes_t, scales_t)
+    return t if along == "rows" else (_packed(r, c, buf, 0, codes, scales), t)
 
 
 def mx_matmul(a, b, C=None, alpha: float = 1.0, beta: float = 0.0, dtype=None):
@@ -211,41 +282,62 @@ def mx_matmul(a, b, C=None, alpha: float = 1.0, beta: float = 0.0, dtype=None):
     that is packed or a float matrix, which is quantised in the call.  Without C
     a new row-major one is returned, in `dtype` (default: a's, float32 for a
     packed a)."""
-    import torch
     if not isinstance(b, MXTensor):
         raise TypeError("b must be packed (mx_quantize)")
     packed = isinstance(a, MXTensor)
-    if not packed:
-        if a.dim() != 2:
-            raise ValueError("a matrix is needed")
-        _device("a", a)
-    (m, k), n = a.shape, b.rows
+    if packed:
+        m, k = a.rows, a.cols
+    else:
+        code_a, m, k, sr, sc = _matrix("a", a)
+    n = b.rows
     if k != b.cols:
         raise ValueError(f"a has {k} columns, b {b.cols}")
     if C is None:
         if beta != 0:
             raise ValueError("beta != 0 needs C")
-        C = torch.empty((m, n), dtype=dtype or (torch.float32 if packed else a.dtype),
-                        device=b.codes.device)
-    elif C.shape != (m, n) or (dtype is not None and C.dtype != dtype):
-        raise ValueError("C differs in shape or dtype")
-    _device("C", C)
-    code = _code(C.dtype)
-    sm, sn = _strides(C)
-    if packed:
-        st = _lib().gett_mx_contract(m, n, k, alpha, a.codes.data_ptr(), a.scales.data_ptr(),
-                                     b.codes.data_ptr(), b.scales.data_ptr(), beta, code,
-                                     C.data_ptr(), sm, sn, _package._current_stream())
-        if st != 0:
-            raise GettError(st, "gett_mx_contract")
+        if _torch is None:
+            _start()
+        if dtype is None:
+            dtype = _torch.float32 if packed else a.dtype
+        code, sm, sn = _code(dtype), n or 1, 1
+        C = _torch.empty((m, n), dtype=dtype, device=b.device)
     else:
-        sr, sc = _strides(a)
-        st = _lib().gett_mx_apply(m, n, k, alpha, _code(a.dtype), a.data_ptr(), sr, sc,
-                                  b.codes.data_ptr(), b.scales.data_ptr(), beta, code,
-                                  C.data_ptr(), sm, sn, _package._current_stream())
-        if st != 0:
-            raise GettError(st, "gett_mx_apply")
+        if tuple(C.shape) != (m, n) or (dtype is not None and C.dtype != dtype):
+            raise ValueError("C differs in shape or dtype")
+        code, _, _, sm, sn = _matrix("C", C)
+    if packed:
+        st = _bound.gett_mx_contract(m, n, k, alpha, a._codes, a._scales, b._codes, b._scales, beta,
+                                     code, C.data_ptr(), sm, sn, _package._current_stream())
+    else:
+        st = _bound.gett_mx_apply(m, n, k, alpha, code_a, a.data_ptr(), sr, sc, b._codes, b._scales,
+                                  beta, code, C.data_ptr(), sm, sn, _package._current_stream())
+    if st != 0:
+        raise GettError(st, "gett_mx_contract" if packed else "gett_mx_apply")
     return C
+
+
+def _linear_forward(x, w, save_x, save_w):
+    """y, and the packed x^T and w^T that are asked for: (buffer, addresses)."""
+    cx, m, k, sxm, sxk = _matrix("x", x)
+    cw, n, kw, swn, swk = _matrix("w", w)
+    if kw != k:
+        raise ValueError(f"x has {k} columns, w {kw}")
+    y = _torch.empty((m, n), dtype=x.dtype, device=x.device)
+    buf = xt = xs = wt = ws = None
+    a, b = _sizes(k, m) if save_x else (0, 0)
+    c, d = _sizes(k, n) if save_w else (0, 0)
+    if save_x or save_w:
+        buf = _torch.empty(a + b + c + d, dtype=_torch.uint8, device=x.device)
+        p = buf.data_ptr()
+        if save_x:
+            xt, xs = p, p + a
+        if save_w:
+            wt, ws = p + a + b, p + a + b + c
+    st = _bound.gett_mx_linear(m, n, k, cx, x.data_ptr(), sxm, sxk, cw, w.data_ptr(), swn, swk,
+                               y.data_ptr(), n or 1, 1, xt, xs, wt, ws, _package._current_stream())
+    if st != 0:
+        raise GettError(st, "gett_mx_linear")
+    return y, (buf, xt, xs, wt, ws)
 
 
 _function = None
@@ -255,7 +347,7 @@ def _linear_function():
     global _function
     if _function is not None:
         return _function
-    import torch
+    torch = _torch
 
     class MXLinear(torch.autograd.Function):
         """y = Q(x) Q(w)^T; dx = Q(dy) Q(w^T)^T, dw = Q(dy^T) Q(x^T)^T: every
@@ -265,25 +357,27 @@ def _linear_function():
         @staticmethod
         def forward(ctx, x, w):
             need_x, need_w = ctx.needs_input_grad
-            xq = mx_quantize(x, "both" if need_w else "cols")
-            wq = mx_quantize(w, "both" if need_x else "cols")
-            xq, ctx.xt = xq if need_w else (xq, None)
-            wq, ctx.wt = wq if need_x else (wq, None)
-            ctx.types = x.dtype, w.dtype
-            return mx_matmul(xq, wq, dtype=x.dtype)
+            y, ctx.packed = _linear_forward(x, w, need_w, need_x)
+            ctx.sizes = x.shape[0], w.shape[0], x.shape[1], x.dtype, w.dtype
+            return y
 
         @staticmethod
         @torch.autograd.function.once_differentiable
         def backward(ctx, dy):
             need_x, need_w = ctx.needs_input_grad
-            if not (need_x or need_w):
-                return None, None
+            m, n, k, tx, tw = ctx.sizes
             if dy.stride(0) < 1 or dy.stride(1) < 1:
                 dy = dy.contiguous()   # the gradient of a sum is broadcast
-            dq = mx_quantize(dy, "both" if need_x and need_w else "cols" if need_x else "rows")
-            d, dt = dq if need_x and need_w else (dq, dq)
-            dx = mx_matmul(d, ctx.wt, dtype=ctx.types[0]) if need_x else None
-            dw = mx_matmul(dt, ctx.xt, dtype=ctx.types[1]) if need_w else None
+            code, _, _, sm, sn = _matrix("dy", dy)
+            _, xt, xs, wt, ws = ctx.packed
+            dx = torch.empty((m, k), dtype=tx, device=dy.device) if need_x else None
+            dw = torch.empty((n, k), dtype=tw, device=dy.device) if need_w else None
+            st = _bound.gett_mx_linear_grad(
+                m, n, k, code, dy.data_ptr(), sm, sn, xt, xs, wt, ws,
+                dx.data_ptr() if need_x else None, k or 1, 1, _codes[tw],
+                dw.data_ptr() if need_w else None, k or 1, 1, _package._current_stream())
+            if st != 0:
+                raise GettError(st, "gett_mx_linear_grad")
             return dx, dw
 
     _function = MXLinear
@@ -295,15 +389,16 @@ def mx_linear(x, w):
 
     `w` is a float n x k weight (differentiable, as is `x`: gradients are
     products in 4 bits as well) or a packed one, for serving."""
-    k = x.shape[-1]
-    flat = x.reshape(-1, k)
+    shape = x.shape
+    flat = x if len(shape) == 2 else x.reshape(-1, shape[-1])
     if isinstance(w, MXTensor):
         y = mx_matmul(flat, w)
-    else:
-        if w.dim() != 2 or w.shape[1] != k:
-            raise ValueError(f"x has {k} columns, w is {tuple(w.shape)}")
+    elif _code(x.dtype) is not None and _torch.is_grad_enabled() and (x.requires_grad or
+                                                                      w.requires_grad):
         y = _linear_function().apply(flat, w)
-    return y.reshape(*x.shape[:-1], y.shape[1])
+    else:
+        y = _linear_forward(flat, w, False, False)[0]
+    return y if len(shape) == 2 else y.reshape(*shape[:-1], y.shape[1])
 
 
 def orthogonalize(G, steps: int = 5, coefficients=(3.4445, -4.7750, 2.0315), eps: float = 1e-7,
@@ -311,13 +406,12 @@ def orthogonalize(G, steps: int = 5, coefficients=(3.4445, -4.7750, 2.0315), eps
     """`steps` Newton-Schulz steps X <- a X + (b S + c S^2) X, S = X X^T, from
     G / (|G| + eps), for a matrix or a stack [..., rows, cols] of them; `out`
     may be G."""
-    import torch
     if G.dim() < 2:
         raise ValueError("a matrix or a stack of matrices is needed")
     code = _code(G.dtype)
     _device("G", G)
     if out is None:
-        out = torch.empty(G.shape, dtype=G.dtype, device=G.device)
+        out = _torch.empty(G.shape, dtype=G.dtype, device=G.device)
     elif out.shape != G.shape or out.dtype != G.dtype:
         raise ValueError("out differs in shape or dtype")
     else:
@@ -331,13 +425,13 @@ def orthogonalize(G, steps: int = 5, coefficients=(3.4445, -4.7750, 2.0315), eps
             try:
                 o = out.view(-1, *out.shape[-2:])
             except RuntimeError:   # a stack without one stride
-                copy = o = torch.empty(g.shape, dtype=G.dtype, device=G.device)
+                copy = o = _torch.empty(g.shape, dtype=G.dtype, device=G.device)
     n, r, c = g.shape
     if n > 1 and (g.stride(0) < 1 or o.stride(0) < 1):
         raise ValueError("a broadcast (zero-stride) stack: copy it first")
     (gr, gc), (orow, oc) = _strides(g), _strides(o)
     a, b, cc = coefficients
-    st = _lib().gett_orthogonalize(code, n, r, c, g.data_ptr(), g.stride(0), gr, gc, a, b, cc, eps,
+    st = _bound.gett_orthogonalize(code, n, r, c, g.data_ptr(), g.stride(0), gr, gc, a, b, cc, eps,
                                    int(steps), o.data_ptr(), o.stride(0), orow, oc,
                                    _package._current_stream())
     if st != 0:

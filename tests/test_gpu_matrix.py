@@ -333,6 +333,75 @@ def test_linear_needs_only_what_it_is_asked_for(gpu):
         assert (xa.grad is not None) == a and (wb.grad is not None) == b
 
 
+def test_linear_of_two_types_and_layouts(gpu):
+    """x, w and dy in layouts and types of their own; the gradients come in
+    the types of what they are the gradients of."""
+    rng = np.random.default_rng(12)
+    for tx, tw, kx, kw, ky in (("bfloat16", "float32", "transposed", "slice", "dense"),
+                               ("float16", "bfloat16", "strided", "transposed", "transposed"),
+                               ("float32", "float32", "slice", "dense", "strided")):
+        x, w = matrix(rng, 150, 90, tx, kx, 0.1), matrix(rng, 70, 90, tw, kw, 0.1)
+        dy = matrix(rng, 150, 70, tx, ky, 0.1)
+        x.requires_grad_()
+        w.requires_grad_()
+        y = g.mx_linear(x, w)
+        y.backward(dy)
+        assert x.grad.dtype == x.dtype and w.grad.dtype == w.dtype
+        X, W, DY = host(x.detach()), host(w.detach()), host(dy)
+        product_close(host(y.detach()), mx_values(X), mx_values(W), tx)
+        product_close(host(x.grad), mx_values(DY), mx_values(W.T), tx)
+        product_close(host(w.grad), mx_values(DY.T), mx_values(X.T), tw)
+
+
+def test_linear_into_given_memory(gpu):
+    """gett_mx_linear and its gradient into column-major results (the products
+    exchange their operands)."""
+    import torch
+    rng = np.random.default_rng(13)
+    m, n, k = 140, 200, 260
+    x, w, dy = (matrix(rng, *s, "float32", scale=0.1) for s in ((m, k), (n, k), (m, n)))
+    (c1, s1), (c2, s2) = g.gett_mx_size(k, m)[1:], g.gett_mx_size(k, n)[1:]
+    parts = [torch.empty(b, dtype=torch.uint8, device="cuda") for b in (c1, s1, c2, s2)]
+    p = [t.data_ptr() for t in parts]
+    y, dx, dw = (torch.empty(c, r, device="cuda").t() for r, c in ((m, n), (m, k), (n, k)))
+    stream = torch.cuda.current_stream().cuda_stream
+    assert g.gett_mx_linear(m, n, k, 0, x.data_ptr(), k, 1, 0, w.data_ptr(), k, 1, y.data_ptr(), 1,
+                            m, *p, stream) == 0
+    assert g.gett_mx_linear_grad(m, n, k, 0, dy.data_ptr(), n, 1, *p, dx.data_ptr(), 1, m, 0,
+                                 dw.data_ptr(), 1, n, stream) == 0
+    X, W, DY = host(x), host(w), host(dy)
+    product_close(host(y), mx_values(X), mx_values(W), "float32")
+    product_close(host(dx), mx_values(DY), mx_values(W.T), "float32")
+    product_close(host(dw), mx_values(DY.T), mx_values(X.T), "float32")
+
+
+@pytest.mark.parametrize("m,n,k", [(0, 5, 7), (5, 0, 7), (5, 7, 0)])
+def test_linear_of_empty_matrices(gpu, m, n, k):
+    import torch
+    x = torch.randn(m, k, device="cuda", requires_grad=True)
+    w = torch.randn(n, k, device="cuda", requires_grad=True)
+    y = g.mx_linear(x, w)
+    assert y.shape == (m, n) and (y == 0).all()
+    y.backward(torch.ones_like(y))
+    assert (x.grad == 0).all() and (w.grad == 0).all()
+
+
+@pytest.mark.parametrize("m,n,k", [(2000, 300, 280), (3000, 40, 600), (20, 3000, 30)])
+def test_linear_steps_of_uneven_sizes(gpu, m, n, k):
+    """The gradients' two products take tiles of different sizes, or one of
+    them none."""
+    rng = np.random.default_rng(m)
+    x, w, dy = (matrix(rng, *s, "bfloat16", scale=0.1) for s in ((m, k), (n, k), (m, n)))
+    x.requires_grad_()
+    w.requires_grad_()
+    y = g.mx_linear(x, w)
+    y.backward(dy)
+    X, W, DY = host(x.detach()), host(w.detach()), host(dy)
+    product_close(host(y.detach()), mx_values(X), mx_values(W), "bfloat16")
+    product_close(host(x.grad), mx_values(DY), mx_values(W.T), "bfloat16")
+    product_close(host(w.grad), mx_values(DY.T), mx_values(X.T), "bfloat16")
+
+
 # -------------------------------------------------------- orthogonalisation ---
 
 def orth_tolerance(dtype, steps):

@@ -20,8 +20,9 @@ def test_every_declared_function_is_exported_and_bound():
     text = open(os.path.join(ROOT, "include", "gett_matrix.h")).read()
     text = re.sub(r"/\*.*?\*/", "", text, flags=re.S)
     names = sorted(set(re.findall(r"\b(gett_\w+)\s*\(", text)))
-    assert names == ["gett_mx_apply", "gett_mx_contract", "gett_mx_dequantize", "gett_mx_quantize",
-                     "gett_mx_size", "gett_orthogonalize"]
+    assert names == ["gett_mx_apply", "gett_mx_contract", "gett_mx_dequantize", "gett_mx_linear",
+                     "gett_mx_linear_grad", "gett_mx_quantize", "gett_mx_size",
+                     "gett_orthogonalize"]
     out = subprocess.run(["nm", "-D", "--defined-only", g.LIB_PATH], capture_output=True,
                          text=True).stdout
     for n in names:
@@ -121,6 +122,40 @@ def test_apply_refusals(change, status):
     a.update(change)
     assert g.gett_mx_apply(a["m"], a["n"], a["k"], 1.0, a["ta"], a["A"], a["sam"], a["sak"],
                            a["cb"], a["sb"], 0.0, a["dtype"], a["C"], a["sm"], a["sn"]) == status
+
+
+LINEAR = dict(m=8, n=16, k=64, tx=F32, X=P, sxm=64, sxk=1, tw=F32, W=2 * P, swn=64, swk=1, Y=3 * P,
+              sym=16, syn=1, cx=4 * P, sx=5 * P, cw=6 * P, sw=7 * P)
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(tx=1), VALUE), (dict(tw=9), VALUE), (dict(m=-1), VALUE), (dict(k=-1), VALUE),
+    (dict(X=0), VALUE), (dict(W=2 * P + 2), VALUE), (dict(Y=0), VALUE), (dict(sxm=0), VALUE),
+    (dict(cx=0), VALUE), (dict(sw=0), VALUE), (dict(cw=6 * P + 8), VALUE), (dict(Y=P), VALUE),
+    (dict(Y=2 * P + 64), VALUE), (dict(cx=2 * P), VALUE), (dict(cw=4 * P), VALUE),
+    (dict(sw=3 * P), VALUE), (dict(sym=15), UNSUPPORTED), (dict(k=1 << 24), UNSUPPORTED),
+    (dict(m=1 << 25, sxm=1 << 24, Y=1 << 62), UNSUPPORTED), (dict(m=1 << 30), UNSUPPORTED)])
+def test_linear_refusals(change, status):
+    a = dict(LINEAR)
+    a.update(change)
+    assert g.gett_mx_linear(a["m"], a["n"], a["k"], a["tx"], a["X"], a["sxm"], a["sxk"], a["tw"],
+                            a["W"], a["swn"], a["swk"], a["Y"], a["sym"], a["syn"], a["cx"], a["sx"],
+                            a["cw"], a["sw"]) == status
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(tx=1), VALUE), (dict(tw=9), VALUE), (dict(n=-1), VALUE), (dict(k=-1), VALUE),
+    (dict(Y=0), VALUE), (dict(sym=0), VALUE), (dict(X=0, W=0), VALUE), (dict(X=P + 1), VALUE),
+    (dict(cx=0), VALUE), (dict(cw=0), VALUE), (dict(sw=7 * P + 8), VALUE), (dict(X=3 * P), VALUE),
+    (dict(W=3 * P + 32), VALUE), (dict(X=2 * P), VALUE), (dict(X=6 * P), VALUE),
+    (dict(W=5 * P), VALUE), (dict(sxm=63), UNSUPPORTED), (dict(swk=2), UNSUPPORTED),
+    (dict(n=1 << 24), UNSUPPORTED)])
+def test_linear_grad_refusals(change, status):
+    a = dict(LINEAR)
+    a.update(change)
+    assert g.gett_mx_linear_grad(a["m"], a["n"], a["k"], a["tx"], a["Y"], a["sym"], a["syn"],
+                                 a["cx"], a["sx"], a["cw"], a["sw"], a["X"], a["sxm"], a["sxk"],
+                                 a["tw"], a["W"], a["swn"], a["swk"]) == status
 
 
 @pytest.mark.parametrize("change,status", [
