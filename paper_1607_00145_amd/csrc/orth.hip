@@ -498,10 +498,242 @@ struct Problem {
     hipStream_t stream;
 };
 
+// ------------------------------------------------------------ small matrices ---
+//
+// A matrix whose X, X^T and S fit the 160 KB of a CU goes through all steps in
+// one workgroup: no launch and no memory between them.  Rows are padded to 32
+// (zeros, which stay zeros) and lie 16 bytes more than their length apart, so
+// that sixteen rows' pieces fall on different banks.  A wavefront takes blocks of
+// 32 x 32 of a product in turn; a lane then holds column r and four times
+// four neighbouring rows: the transpose is written in vectors, X itself value
+// by value.  B takes S's place: the blocks wait in registers until all have
+// read S (kSmallBlocks a wavefront at most).
+
+constexpr int kSmallWaves = 8;
+constexpr int kSmallBlocks = 2;
+constexpr int kSmallLds = 160 * 1024 - 256;
+
+template <int KIND> __host__ __device__ constexpr int number_bytes() { return KIND == kPanelSplit ? 4 : 2; }
+template <int KIND> __host__ __device__ inline int small_pitch(int k) { return k * number_bytes<KIND>() + 16; }
+template <int KIND> int64_t small_lds(int64_t m, int64_t n)
+{
+    const int64_t mp = (m + 31) / 32 * 32, np = (n + 31) / 32 * 32;
+    return mp * small_pitch<KIND>((int)np) + (np + mp) * small_pitch<KIND>((int)mp);
+}
+template <int KIND> bool small_fits(int64_t m, int64_t n)
+{
+    const int64_t mb = (m + 31) / 32;
+    return m <= 1024 && n <= 4096 && mb * mb <= kSmallWaves * kSmallBlocks &&
+           small_lds<KIND>(m, n) <= kSmallLds;
+}
+
+// the byte of number k in its row
+template <int KIND> __device__ __forceinline__ int small_at(int k)
+{
+    return KIND == kPanelSplit ? (k >> 3) * 32 + (k & 7) * 2 : k * 2;
+}
+template <int KIND> __device__ __forceinline__ f16v small_block(const char *a, const char *b, int k)
+{
+    f16v acc;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc[e] = 0.0f;
+    constexpr int GROUP = KIND == kPanelSplit ? 32 : 16;   // bytes of eight numbers
+#pragma unroll 2
+    for (int t = 0; t < k / 16; ++t) {
+        const i4 ah = *reinterpret_cast<const i4 *>(a + 2 * t * GROUP);
+        const i4 bh = *reinterpret_cast<const i4 *>(b + 2 * t * GROUP);
+        acc = mfma_half(ah, bh, acc);
+        if constexpr (KIND == kPanelSplit) {
+            const i4 al = *reinterpret_cast<const i4 *>(a + 2 * t * GROUP + 16);
+            const i4 bl = *reinterpret_cast<const i4 *>(b + 2 * t * GROUP + 16);
+            acc = mfma_half(ah, bl, acc);
+            acc = mfma_half(al, bh, acc);
+        }
+    }
+    return acc;
+}
+
+template <typename T, int KIND>
+__global__ __launch_bounds__(kSmallWaves * 64) void orth_small_kernel(Stack<const T> G, Stack<T> O,
+                                                                      int m, int n, double eps,
+                                                                      int steps, float ca, float cb,
+                                                                      float cc)
+{
+    extern __shared__ __attribute__((aligned(256))) char dyn_lds[];
+    __shared__ double sums[kSmallWaves];
+    constexpr int THREADS = kSmallWaves * 64;
+    const int tid = (int)threadIdx.x, lane = tid & 63, r = tid & 31, h = (tid >> 5) & 1;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int mp = (m + 31) & ~31, np = (n + 31) & ~31, mb = mp / 32, nb = np / 32;
+    const int pX = small_pitch<KIND>(np), pS = small_pitch<KIND>(mp);
+    char *const X = dyn_lds, *const XT = X + mp * pX, *const S = XT + np * pS;
+    constexpr int GROUP = KIND == kPanelSplit ? 32 : 16;
+    const T *g = G.p + (int64_t)blockIdx.x * G.sb;
+
+    // the norm, and all of the matrices zero
+    const bool along = G.sk <= G.si;
+    const int inner = along ? n : m, outer = along ? m : n;
+    const int64_t so = along ? G.si : G.sk, si = along ? G.sk : G.si;
+    double sum = 0.0;
+    for (int o = wave; o < outer; o += kSmallWaves)
+        for (int i = lane; i < inner; i += 64) {
+            const double v = (double)to_float(g[o * so + i * si]);
+            sum += v * v;
+        }
+    const i4 zero = {0, 0, 0, 0};
+    for (int i = tid; i < (mp * pX + (np + mp) * pS) / 16; i += THREADS)
+        reinterpret_cast<i4 *>(dyn_lds)[i] = zero;
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
+    if (lane == 0) sums[wave] = sum;
+    __syncthreads();
+    sum = 0.0;
+#pragma unroll
+    for (int w = 0; w < kSmallWaves; ++w) sum += sums[w];
+    const double scale =
+        sum < (double)INFINITY ? (double)kUp / (sqrt(sum) + eps) : (double)NAN;
+    for (int o = wave; o < outer; o += kSmallWaves)
+        for (int i = lane; i < inner; i += 64) {
+            const float v = (float)((double)to_float(g[o * so + i * si]) * scale);
+            const int row = along ? o : i, col = along ? i : o;
+            store_run<KIND, 1>(X + row * pX + small_at<KIND>(col), &v);
+            store_run<KIND, 1>(XT + col * pS + small_at<KIND>(row), &v);
+        }
+    __syncthreads();
+
+    const auto writes = [&](char *M, int pitch, int row0, int col0, const f16v &v) {
+        // the transpose: four times four neighbours of a row
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const float x[4] = {v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
+            store_run<KIND, 4>(M + (col0 + r) * pitch + small_at<KIND>(row0 + 8 * q + 4 * h), x);
+        }
+    };
+    for (int step = 0; step < steps; ++step) {
+        const bool last = step + 1 == steps;
+        for (int b = wave; b < mb * mb; b += kSmallWaves) {   // S = X X^T
+            const int bi = b / mb, bj = b - bi * mb;
+            f16v v = small_block<KIND>(X + (bi * 32 + r) * pX + h * GROUP,
+                                       X + (bj * 32 + r) * pX + h * GROUP, np);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) v[e] *= kDown;
+            writes(S, pS, bi * 32, bj * 32, v);
+        }
+        __syncthreads();
+        f16v poly[kSmallBlocks];   // B = b S + c S^2
+#pragma unroll
+        for (int u = 0; u < kSmallBlocks; ++u) {
+            const int b = wave + u * kSmallWaves;
+            if (b >= mb * mb) break;
+            const int bi = b / mb, bj = b - bi * mb;
+            poly[u] = small_block<KIND>(S + (bi * 32 + r) * pS + h * GROUP,
+                                        S + (bj * 32 + r) * pS + h * GROUP, mp);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                float x[4];   // S is symmetric: its column r
+                load_run<KIND, 4>(S + (bj * 32 + r) * pS + small_at<KIND>(bi * 32 + 8 * q + 4 * h), x);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    poly[u][4 * q + e] = cb * x[e] + cc * kDown * poly[u][4 * q + e];
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < kSmallBlocks; ++u) {
+            const int b = wave + u * kSmallWaves;
+            if (b >= mb * mb) break;
+            const int bi = b / mb, bj = b - bi * mb;
+            writes(S, pS, bi * 32, bj * 32, poly[u]);
+        }
+        __syncthreads();
+        // X <- a X + B X, a block of columns (all of its rows) at a time: the
+        // wavefront that reads these rows of X^T, into registers, writes them
+        constexpr int KS = 8;   // steps of 16 numbers: m <= 128
+        for (int bj = wave; bj < nb; bj += kSmallWaves) {
+            char *const column = XT + (bj * 32 + r) * pS;
+            i4 bh[KS], bl[KIND == kPanelSplit ? KS : 1];
+#pragma unroll
+            for (int t = 0; t < KS; ++t)
+                if (t < mp / 16) {
+                    bh[t] = *reinterpret_cast<const i4 *>(column + (2 * t + h) * GROUP);
+                    if constexpr (KIND == kPanelSplit)
+                        bl[t] = *reinterpret_cast<const i4 *>(column + (2 * t + h) * GROUP + 16);
+                }
+            const int col = bj * 32 + r;
+            T *const o = O.p + (int64_t)blockIdx.x * O.sb + col * O.sk;
+#pragma unroll 1
+            for (int bi = 0; bi < mb; ++bi) {
+                // the rows' offsets are made here, not kept through the steps
+                int px = pX;
+                int64_t down = O.si;
+                asm volatile("" : "+s"(px), "+s"(down));
+                const char *const a = S + (bi * 32 + r) * pS + h * GROUP;
+                f16v v;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) v[e] = 0.0f;
+#pragma unroll
+                for (int t = 0; t < KS; ++t)
+                    if (t < mp / 16) {
+                        const i4 ah = *reinterpret_cast<const i4 *>(a + 2 * t * GROUP);
+                        v = mfma_half(ah, bh[t], v);
+                        if constexpr (KIND == kPanelSplit) {
+                            const i4 al = *reinterpret_cast<const i4 *>(a + 2 * t * GROUP + 16);
+                            v = mfma_half(ah, bl[t], v);
+                            v = mfma_half(al, bh[t], v);
+                        }
+                    }
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    float x[4];
+                    load_run<KIND, 4>(column + small_at<KIND>(bi * 32 + 8 * q + 4 * h), x);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[4 * q + e] = ca * x[e] + kDown * v[4 * q + e];
+                }
+                const int row0 = bi * 32 + 4 * h;
+                if (!last) {
+                    writes(XT, pS, bi * 32, bj * 32, v);
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const float x = v[e];
+                        store_run<KIND, 1>(X + (row0 + 8 * (e >> 2) + (e & 3)) * px + small_at<KIND>(col), &x);
+                    }
+                } else if (col < n) {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const int row = row0 + 8 * (e >> 2) + (e & 3);
+                        if (row < m) o[row * down] = from_float<T>(v[e] * kDown);
+                    }
+                }
+            }
+        }
+        __syncthreads();
+    }
+    if (steps == 0)
+        for (int o = wave; o < m; o += kSmallWaves)
+            for (int i = lane; i < n; i += 64) {
+                float v;
+                load_run<KIND, 1>(X + o * pX + small_at<KIND>(i), &v);
+                O.p[(int64_t)blockIdx.x * O.sb + o * O.si + i * O.sk] = from_float<T>(v * kDown);
+            }
+}
+
+template <typename T, int KIND>
+gett_status_t small_launch(const Problem &P, const Stack<const T> &G, const Stack<T> &O)
+{
+    constexpr auto k = orth_small_kernel<T, KIND>;
+    if (allow_dynamic_lds<k>(kSmallLds) != hipSuccess) return GETT_ERROR_HIP;
+    hipLaunchKernelGGL(k, dim3((unsigned)P.batch), dim3(kSmallWaves * 64),
+                       (size_t)small_lds<KIND>(P.m, P.n), P.stream, G, O, P.m, P.n, P.eps, P.steps,
+                       (float)P.a, (float)P.b, (float)P.c);
+    return hipGetLastError() == hipSuccess ? GETT_SUCCESS : GETT_ERROR_HIP;
+}
+
+
 template <typename T, int KIND>
 gett_status_t orthogonalize_typed(const Problem &P, Stack<const T> G, Stack<T> O)
 {
     const int m = P.m, n = P.n;
+    if (small_fits<KIND>(m, n)) return small_launch<T, KIND>(P, G, O);
     const int64_t panelsX = panel_count<KIND>(n), panelsS = panel_count<KIND>(m);
     const int64_t X = m * panelsX * 128, XT = n * panelsS * 128, SS = m * panelsS * 128;
     // the norm reads along the smaller stride
