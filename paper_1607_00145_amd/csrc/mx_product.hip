@@ -176,31 +176,44 @@ template <typename TA> struct FewFloat {
     __device__ __forceinline__ void load(Frag &f, int t, int r, int q) const
     {
         f.s[0] = 0;
+        f.v[0][0] = f.v[0][1] = i4{0, 0, 0, 0};
+        if (r >= m) return;
+        const int k0 = t * kTileK + q * 64;
+        const TA *p = A + (int64_t)r * sm + (int64_t)k0 * sk;
+        if (sk == 1 && (t + 1) * kTileK <= k) {   // the same for all lanes
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-            float x[32];
-            const int k0 = t * kTileK + q * 64 + b * 32, left = r < m ? k - k0 : 0;
-            const TA *p = A + (int64_t)r * sm + (int64_t)k0 * sk;
-            if (sk == 1 && left >= 32) {
+            for (int b = 0; b < 2; ++b) {
+                float x[32];
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
-                    const Run<TA, 8> v = *reinterpret_cast<const Run<TA, 8> *>(p + 8 * c);
+                    const Run<TA, 8> v = *reinterpret_cast<const Run<TA, 8> *>(p + 32 * b + 8 * c);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) x[8 * c + i] = to_float(v.v[i]);
                 }
-            } else {
-#pragma unroll
-                for (int i = 0; i < 32; ++i) x[i] = i < left ? to_float(p[i * sk]) : 0.0f;
+                pack(f, b, x);
             }
-            uint32_t top = 0;
+        } else {
+#pragma unroll 1
+            for (int b = 0; b < 2; ++b) {
+                float x[32];
 #pragma unroll
-            for (int i = 0; i < 32; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
-            const uint32_t sb = scale_byte(top);
-            const float s = scale_value(sb);
-#pragma unroll
-            for (int c = 0; c < 4; ++c) f.v[0][b][c] = (int)codes8(x + 8 * c, s);
-            f.s[0] |= (int)(sb << (8 * b));
+                for (int i = 0; i < 32; ++i)
+                    x[i] = k0 + 32 * b + i < k ? to_float(p[(32 * b + i) * sk]) : 0.0f;
+                if (b == 0) pack(f, 0, x);
+                else pack(f, 1, x);
+            }
         }
+    }
+    static __device__ __forceinline__ void pack(Frag &f, int b, const float *x)
+    {
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
+        const uint32_t sb = scale_byte(top);
+        const float s = scale_value(sb);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) f.v[0][b][c] = (int)codes8(x + 8 * c, s);
+        f.s[0] |= (int)(sb << (8 * b));
     }
 };
 
