@@ -9,12 +9,12 @@
 // conversion instruction for two values.
 //
 // Bound: memory.  X is read once, also where both orientations are packed: a
-// workgroup takes a 128 x 128 tile; each lane loads eight neighbours of a
+// workgroup takes a tile (128 x 128; 32 x 512 where only rows are packed); each lane loads eight neighbours of a
 // row, four lanes hold a block, and the maximum crosses them in two
 // exchanges.  For the transposed packing the tile passes through LDS
 // (unrounded, in X's own type) and a lane takes 32 rows of one column; four
 // lanes take one column's four blocks, so 64 bytes of a row of codes_t leave
-// together.  Scales are gathered in LDS and leave in runs of 512 bytes.
+// together.  Scales are gathered in LDS and leave in whole runs.
 #include "kernel.hpp"
 #include "matrix.hpp"
 #include "mx.hpp"
@@ -22,11 +22,19 @@
 namespace gett {
 namespace {
 
-constexpr int kT = 128;         // tile edge
+constexpr int kT = 128;         // edge of a square tile
 constexpr int kThreads = 256;
 constexpr int kChunk = 8;       // neighbours of a row one lane takes
-constexpr int kRowsPass = kThreads / (kT / kChunk);   // 16 rows per pass
-constexpr int kPasses = kT / kRowsPass;
+
+// Tiles: 128 x 128 where columns are packed (four blocks of each column); 32 x
+// 512 where only rows are read or written, so that a wavefront's access is one
+// row's 512 neighbours.
+template <bool COLS> struct Tile {
+    static constexpr int R = COLS ? kT : 32, C = COLS ? kT : 512;
+    static constexpr int LANES = C / kChunk;             // lanes of a row
+    static constexpr int ROWS = kThreads / LANES;        // rows of a pass
+    static constexpr int PASSES = R / ROWS;
+};
 
 __device__ __forceinline__ uint32_t quad_max(uint32_t v)
 {
@@ -41,6 +49,25 @@ __device__ __forceinline__ uint32_t magnitude(float x) { return __float_as_uint(
 __device__ __forceinline__ int64_t code_offset(int rows, int r, int c)
 {
     return ((int64_t)(c / kTileK) * rows + r) * kTileBytes + (c % kTileK) / 2;
+}
+
+// The tile of workgroup `block` of `blocks`: ids of one XCD (workgroups go round
+// the eight) are neighbours, in pairs of rows where there are such, so that the
+// two tiles that share a line of 128 bytes of codes meet in one L2.
+__device__ __forceinline__ void tile_of(int block, int blocks, int tilesC, Recip tilesInv, int &tr,
+                                        int &tc)
+{
+    const int per = blocks >> 3;
+    const int id = block < per * 8 ? (block & 7) * per + (block >> 3) : block;
+    const int pair = (int)quotient((uint32_t)(id >> 1), tilesC, tilesInv);
+    const int inPair = id - 2 * pair * tilesC, left = blocks - 2 * pair * tilesC;
+    if (left >= 2 * tilesC) {
+        tr = 2 * pair + (inPair & 1);
+        tc = inPair >> 1;
+    } else {   // a last single row
+        tr = 2 * pair;
+        tc = inPair;
+    }
 }
 
 // LDS address (elements) of tile element (r, c): rows follow one another,
@@ -78,24 +105,26 @@ __global__ __launch_bounds__(kThreads) void mx_quantize_kernel(Job<T> first, Job
     uint8_t *const scalesT = is2 ? second.scalesT : first.scalesT;
     const int block = (int)blockIdx.x - (is2 ? first.blocks : 0);
     __shared__ __attribute__((aligned(16))) T tile[COLS ? kT * kT + 3 * (32 / sizeof(T)) : 1];
-    // [row or column][block]
-    __shared__ __attribute__((aligned(16))) uint8_t sRow[ROWS ? kT : 1][4];
+    typedef Tile<COLS> Q;
+    // [128 columns][row][block], and [column][block]
+    __shared__ __attribute__((aligned(16))) uint8_t sRow[ROWS ? Q::C / 128 : 1][ROWS ? Q::R : 1][4];
     __shared__ __attribute__((aligned(16))) uint8_t sCol[COLS ? kT : 1][4];
 
     const int tid = (int)threadIdx.x;
-    const int tr = (int)quotient((uint32_t)block, tilesC, is2 ? second.tilesInv : first.tilesInv);
-    const int tc = block - tr * tilesC;
-    const int row0 = tr * kT, col0 = tc * kT;
+    int tr, tc;
+    tile_of(block, is2 ? second.blocks : first.blocks, tilesC,
+            is2 ? second.tilesInv : first.tilesInv, tr, tc);
+    const int row0 = tr * Q::R, col0 = tc * Q::C;
     const int tilesK = (int)mx_tiles(cols), tilesKT = (int)mx_tiles(rows);
     // this tile's columns (rows) lie inside the padded row of codes (codes_t)
-    const bool inRow = ROWS && col0 < tilesK * kTileK, inCol = COLS && row0 < tilesKT * kTileK;
+    const int c8 = (tid % Q::LANES) * kChunk, r0 = tid / Q::LANES;
+    const bool inRow = ROWS && col0 + c8 < tilesK * kTileK, inCol = COLS && row0 < tilesKT * kTileK;
 
-    const int c8 = (tid % (kT / kChunk)) * kChunk, r0 = tid / (kT / kChunk);
     const int left = cols - (col0 + c8);   // columns of this lane's chunk inside X
-    T x[kPasses][kChunk];
+    T x[Q::PASSES][kChunk];
 #pragma unroll
-    for (int p = 0; p < kPasses; ++p) {
-        const int r = row0 + r0 + p * kRowsPass;
+    for (int p = 0; p < Q::PASSES; ++p) {
+        const int r = row0 + r0 + p * Q::ROWS;
         const T *src = X + (int64_t)r * sr + (int64_t)(col0 + c8) * sc;
         if (r < rows && left >= kChunk && wide) {
             const Run<T, kChunk> v = *reinterpret_cast<const Run<T, kChunk> *>(src);
@@ -111,8 +140,8 @@ __global__ __launch_bounds__(kThreads) void mx_quantize_kernel(Job<T> first, Job
         }
     }
 #pragma unroll
-    for (int p = 0; p < kPasses; ++p) {
-        const int lr = r0 + p * kRowsPass;
+    for (int p = 0; p < Q::PASSES; ++p) {
+        const int lr = r0 + p * Q::ROWS;
         if constexpr (COLS) {
 #pragma unroll
             for (int i = 0; i < kChunk; ++i) tile[tile_at<T>(lr, c8) + i] = x[p][i];
@@ -129,7 +158,7 @@ __global__ __launch_bounds__(kThreads) void mx_quantize_kernel(Job<T> first, Job
             const uint32_t q = codes8(f, scale_value(sb));
             if (inRow && row0 + lr < rows)
                 *reinterpret_cast<uint32_t *>(codes + code_offset(rows, row0 + lr, col0 + c8)) = q;
-            if ((tid & 3) == 0) sRow[lr][c8 >> 5] = (uint8_t)sb;
+            if ((tid & 3) == 0) sRow[c8 >> 7][lr][(c8 >> 5) & 3] = (uint8_t)sb;
         }
     }
     __syncthreads();
@@ -155,12 +184,12 @@ __global__ __launch_bounds__(kThreads) void mx_quantize_kernel(Job<T> first, Job
         }
         __syncthreads();
     }
-    // scales: a run of 512 bytes, one 16-byte piece (four rows) a thread
+    // scales: 512 bytes, one 16-byte piece (four rows) a thread
     if constexpr (ROWS) {
-        const int r = tid * 4, R = (int)mx_scale_rows(rows);
-        if (tid < 32 && inRow && row0 + r < R)
-            *reinterpret_cast<i4 *>(scales + ((int64_t)(col0 / kT) * R + row0 + r) * 4) =
-                *reinterpret_cast<const i4 *>(&sRow[r][0]);
+        const int r = tid * 4 % Q::R, part = tid * 4 / Q::R, R = (int)mx_scale_rows(rows);
+        if (tid < 32 && col0 + part * kT < tilesK * kTileK && row0 + r < R)
+            *reinterpret_cast<i4 *>(scales + ((int64_t)(col0 / kT + part) * R + row0 + r) * 4) =
+                *reinterpret_cast<const i4 *>(&sRow[part][r][0]);
     }
     if constexpr (COLS) {
         const int c = (tid - 64) * 4, R = (int)mx_scale_rows(cols);   // another wavefront
@@ -170,35 +199,41 @@ __global__ __launch_bounds__(kThreads) void mx_quantize_kernel(Job<T> first, Job
     }
 }
 
-// A workgroup writes a 128 x 128 tile of values; `wide` as above.
+// A workgroup writes a 32 x 512 tile of values; `wide` as above.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void mx_dequantize_kernel(
     const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales, int rows, int cols,
-    int tilesC, bool wide, T *__restrict__ X, int64_t sr, int64_t sc)
+    int tilesC, Recip tilesInv, bool wide, T *__restrict__ X, int64_t sr, int64_t sc)
 {
-    __shared__ __attribute__((aligned(16))) uint8_t sRow[kT][4];
+    typedef Tile<false> Q;
+    __shared__ __attribute__((aligned(16))) uint8_t sRow[Q::C / 128][Q::R][4];
     const int tid = (int)threadIdx.x;
-    const int row0 = (int)blockIdx.x / tilesC * kT, col0 = (int)blockIdx.x % tilesC * kT;
+    int tr, tc;
+    tile_of((int)blockIdx.x, (int)gridDim.x, tilesC, tilesInv, tr, tc);
+    const int row0 = tr * Q::R, col0 = tc * Q::C;
     const int R = (int)mx_scale_rows(rows);
-    const int c8 = (tid % (kT / kChunk)) * kChunk, r0 = tid / (kT / kChunk);
+    const int c8 = (tid % Q::LANES) * kChunk, r0 = tid / Q::LANES;
     const int left = cols - (col0 + c8);
-    uint32_t q[kPasses];
+    uint32_t q[Q::PASSES];
 #pragma unroll
-    for (int p = 0; p < kPasses; ++p) {
-        const int r = row0 + r0 + p * kRowsPass;
+    for (int p = 0; p < Q::PASSES; ++p) {
+        const int r = row0 + r0 + p * Q::ROWS;
         q[p] = 0;
         if (r < rows && left > 0)
             q[p] = *reinterpret_cast<const uint32_t *>(codes + code_offset(rows, r, col0 + c8));
     }
-    if (tid < 32 && row0 + tid * 4 < R)
-        *reinterpret_cast<i4 *>(&sRow[tid * 4][0]) =
-            *reinterpret_cast<const i4 *>(scales + ((int64_t)(col0 / kT) * R + row0 + tid * 4) * 4);
+    {
+        const int r = tid * 4 % Q::R, part = tid * 4 / Q::R;
+        if (tid < 32 && col0 + part * kT < cols && row0 + r < R)
+            *reinterpret_cast<i4 *>(&sRow[part][r][0]) = *reinterpret_cast<const i4 *>(
+                scales + ((int64_t)(col0 / kT + part) * R + row0 + r) * 4);
+    }
     __syncthreads();
 #pragma unroll
-    for (int p = 0; p < kPasses; ++p) {
-        const int lr = r0 + p * kRowsPass, r = row0 + lr;
+    for (int p = 0; p < Q::PASSES; ++p) {
+        const int lr = r0 + p * Q::ROWS, r = row0 + lr;
         if (r >= rows || left <= 0) continue;
-        const uint32_t sb = sRow[lr][c8 >> 5];
+        const uint32_t sb = sRow[c8 >> 7][lr][(c8 >> 5) & 3];
         const float s = scale_value(sb);
         float f[kChunk];
         const f2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q[p], s, 0);
@@ -232,8 +267,10 @@ template <typename T> Job<T> job_of(QuantizeJob q)
         std::swap(q.scales, q.scalesT);
     }
     // enough tiles for X and for the padding of the packed rows
-    const int64_t tilesR = q.codesT ? 2 * mx_tiles(q.rows) : (q.rows + kT - 1) / kT;
-    const int64_t tilesC = q.codes ? 2 * mx_tiles(q.cols) : (q.cols + kT - 1) / kT;
+    const int64_t R = q.codesT ? Tile<true>::R : Tile<false>::R;
+    const int64_t C = q.codesT ? Tile<true>::C : Tile<false>::C;
+    const int64_t tilesR = ((q.codesT ? mx_tiles(q.rows) * kTileK : q.rows) + R - 1) / R;
+    const int64_t tilesC = ((q.codes ? mx_tiles(q.cols) * kTileK : q.cols) + C - 1) / C;
     const int64_t blocks = tilesR * tilesC < INT32_MAX / 2 ? tilesR * tilesC : 0;
     return {static_cast<const T *>(q.X), q.sr, q.sc, (int)q.rows, (int)q.cols, (int)tilesC,
             (int)blocks, recip(tilesC), q.sc == 1, static_cast<uint8_t *>(q.codes),
@@ -269,7 +306,8 @@ hipError_t dequantize_typed(int64_t rows, int64_t cols, const void *codes, const
 {
     hipLaunchKernelGGL((mx_dequantize_kernel<T>), dim3(blocks), dim3(kThreads), 0, stream,
                        static_cast<const uint8_t *>(codes), static_cast<const uint8_t *>(scales),
-                       (int)rows, (int)cols, tilesC, sc == 1, static_cast<T *>(X), sr, sc);
+                       (int)rows, (int)cols, tilesC, recip(tilesC), sc == 1, static_cast<T *>(X), sr,
+                       sc);
     return hipGetLastError();
 }
 
@@ -343,7 +381,8 @@ gett_status_t gett_mx_dequantize(gett_dtype_t dtype, int64_t rows, int64_t cols,
     if (overlaps(X, span, codes, mx_code_bytes(rows, cols)) ||
         overlaps(X, span, scales, mx_scale_bytes(rows, cols)))
         return GETT_ERROR_INVALID_VALUE;
-    const int64_t tilesC = (cols + kT - 1) / kT, tiles = (rows + kT - 1) / kT * tilesC;
+    const int64_t tilesC = (cols + Tile<false>::C - 1) / Tile<false>::C;
+    const int64_t tiles = (rows + Tile<false>::R - 1) / Tile<false>::R * tilesC;
     if (tiles >= INT32_MAX) return GETT_ERROR_NOT_SUPPORTED;
     hipStream_t s = static_cast<hipStream_t>(stream);
     hipError_t e;
