@@ -78,6 +78,48 @@ template <typename T> __device__ __forceinline__ int tile_at(int r, int c)
     return r * kT + (r >> 5) * (32 / (int)sizeof(T)) + c;
 }
 
+// 16 bytes at an address that is a multiple of 4 or 2
+typedef i4 Piece4 __attribute__((aligned(4)));
+typedef i4 Piece2 __attribute__((aligned(2)));
+
+// Eight neighbours of a row, as they lie in memory (at any element's address).
+template <typename T> struct Chunk {
+    static constexpr int N = (int)sizeof(T) / 2;   // 16-byte pieces
+    typedef typename std::conditional<sizeof(T) == 4, Piece4, Piece2>::type Piece;
+    i4 v[N];
+    __device__ __forceinline__ void load(const T *p)
+    {
+        // read once: past the caches' least recently used lines (51 us where
+        // ordinary loads took 58 for 268 MB beside a quarter of that in stores)
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            v[i] = __builtin_nontemporal_load(reinterpret_cast<const Piece *>(p) + i);
+    }
+    __device__ __forceinline__ void set(const T *p) { __builtin_memcpy(v, p, sizeof(v)); }
+    __device__ __forceinline__ void clear()
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = i4{0, 0, 0, 0};
+    }
+    __device__ __forceinline__ void store(T *lds) const   // 16-byte aligned
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i) reinterpret_cast<i4 *>(lds)[i] = v[i];
+    }
+    __device__ __forceinline__ float at(int i) const
+    {
+        if constexpr (sizeof(T) == 4) {
+            return __int_as_float(v[i >> 2][i & 3]);
+        } else {
+            const uint32_t w = (uint32_t)v[0][i >> 1];
+            if constexpr (std::is_same<T, bf16>::value)
+                return __uint_as_float(i & 1 ? w & 0xffff0000u : w << 16);
+            else
+                return (float)__builtin_bit_cast(_Float16, (uint16_t)(i & 1 ? w >> 16 : w & 0xffffu));
+        }
+    }
+};
+
 // One matrix to pack; tiles of columns and their reciprocal.  `wide`: columns
 // are neighbours in memory (stride_col 1).
 template <typename T> struct Job {
@@ -120,38 +162,43 @@ __global__ __launch_bounds__(kThreads) void mx_quantize_kernel(Job<T> first, Job
     const int c8 = (tid % Q::LANES) * kChunk, r0 = tid / Q::LANES;
     const bool inRow = ROWS && col0 + c8 < tilesK * kTileK, inCol = COLS && row0 < tilesKT * kTileK;
 
+    // All passes' loads, with nothing between them.  Rows past the last read it
+    // again (their codes are not stored; for the columns they become zeros), and
+    // so do chunks past the last column or across it, which are replaced.
     const int left = cols - (col0 + c8);   // columns of this lane's chunk inside X
-    T x[Q::PASSES][kChunk];
+    Chunk<T> x[Q::PASSES];
+    if (wide && cols >= kChunk) {
+        const int c = left >= kChunk ? col0 + c8 : cols - kChunk;
 #pragma unroll
-    for (int p = 0; p < Q::PASSES; ++p) {
-        const int r = row0 + r0 + p * Q::ROWS;
-        const T *src = X + (int64_t)r * sr + (int64_t)(col0 + c8) * sc;
-        if (r < rows && left >= kChunk && wide) {
-            const Run<T, kChunk> v = *reinterpret_cast<const Run<T, kChunk> *>(src);
+        for (int p = 0; p < Q::PASSES; ++p) {
+            const int r = row0 + r0 + p * Q::ROWS;
+            x[p].load(X + (int64_t)(r < rows ? r : rows - 1) * sr + c);
+        }
+    }
+    if (!wide || left < kChunk) {
 #pragma unroll
-            for (int i = 0; i < kChunk; ++i) x[p][i] = v.v[i];
-        } else {
+        for (int p = 0; p < Q::PASSES; ++p) {
+            const int r = row0 + r0 + p * Q::ROWS;
+            const T *src = X + (int64_t)(r < rows ? r : rows - 1) * sr + (int64_t)(col0 + c8) * sc;
+            T v[kChunk];
 #pragma unroll
-            for (int i = 0; i < kChunk; ++i) x[p][i] = from_float<T>(0.0f);
-            if (r < rows)
-#pragma unroll
-                for (int i = 0; i < kChunk; ++i)
-                    if (i < left) x[p][i] = src[i * sc];
+            for (int i = 0; i < kChunk; ++i) v[i] = i < left ? src[i * sc] : from_float<T>(0.0f);
+            x[p].set(v);
         }
     }
 #pragma unroll
     for (int p = 0; p < Q::PASSES; ++p) {
         const int lr = r0 + p * Q::ROWS;
         if constexpr (COLS) {
-#pragma unroll
-            for (int i = 0; i < kChunk; ++i) tile[tile_at<T>(lr, c8) + i] = x[p][i];
+            if (row0 + lr >= rows) x[p].clear();
+            x[p].store(tile + tile_at<T>(lr, c8));
         }
         if constexpr (ROWS) {
             float f[kChunk];
             uint32_t top = 0;
 #pragma unroll
             for (int i = 0; i < kChunk; ++i) {
-                f[i] = to_float(x[p][i]);
+                f[i] = x[p].at(i);
                 top = max(top, magnitude(f[i]));
             }
             const uint32_t sb = scale_byte(quad_max(top));
@@ -199,11 +246,14 @@ __global__ __launch_bounds__(kThreads) void mx_quantize_kernel(Job<T> first, Job
     }
 }
 
+// Values of more than this pass the L2s (32 MB) by; fewer may be wanted there.
+constexpr int64_t kStreamBytes = 32 << 20;
+
 // A workgroup writes a 32 x 512 tile of values; `wide` as above.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void mx_dequantize_kernel(
     const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales, int rows, int cols,
-    int tilesC, Recip tilesInv, bool wide, T *__restrict__ X, int64_t sr, int64_t sc)
+    int tilesC, Recip tilesInv, bool wide, bool stream, T *__restrict__ X, int64_t sr, int64_t sc)
 {
     typedef Tile<false> Q;
     __shared__ __attribute__((aligned(16))) uint8_t sRow[Q::C / 128][Q::R][4];
@@ -242,17 +292,24 @@ __global__ __launch_bounds__(kThreads) void mx_dequantize_kernel(
         const f2 d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q[p], s, 3);
         f[0] = a[0], f[1] = a[1], f[2] = b[0], f[3] = b[1];
         f[4] = c[0], f[5] = c[1], f[6] = d[0], f[7] = d[1];
-        Run<T, kChunk> v;
+        T v[kChunk];
 #pragma unroll
         for (int i = 0; i < kChunk; ++i)
-            v.v[i] = from_float<T>(sb == 255 ? __uint_as_float(0x7fc00000u) : f[i]);
+            v[i] = from_float<T>(sb == 255 ? __uint_as_float(0x7fc00000u) : f[i]);
         T *dst = X + (int64_t)r * sr + (int64_t)(col0 + c8) * sc;
         if (wide && left >= kChunk) {
-            *reinterpret_cast<Run<T, kChunk> *>(dst) = v;
+            Chunk<T> c;
+            c.set(v);
+#pragma unroll
+            for (int i = 0; i < Chunk<T>::N; ++i) {
+                typename Chunk<T>::Piece *at = reinterpret_cast<typename Chunk<T>::Piece *>(dst) + i;
+                if (stream) __builtin_nontemporal_store(c.v[i], at);
+                else *at = c.v[i];
+            }
         } else {
 #pragma unroll
             for (int i = 0; i < kChunk; ++i)
-                if (i < left) dst[i * sc] = v.v[i];
+                if (i < left) dst[i * sc] = v[i];
         }
     }
 }
@@ -306,8 +363,8 @@ hipError_t dequantize_typed(int64_t rows, int64_t cols, const void *codes, const
 {
     hipLaunchKernelGGL((mx_dequantize_kernel<T>), dim3(blocks), dim3(kThreads), 0, stream,
                        static_cast<const uint8_t *>(codes), static_cast<const uint8_t *>(scales),
-                       (int)rows, (int)cols, tilesC, recip(tilesC), sc == 1, static_cast<T *>(X), sr,
-                       sc);
+                       (int)rows, (int)cols, tilesC, recip(tilesC), sc == 1,
+                       rows * cols * (int64_t)sizeof(T) > kStreamBytes, static_cast<T *>(X), sr, sc);
     return hipGetLastError();
 }
 
