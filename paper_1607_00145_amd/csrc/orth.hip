@@ -34,7 +34,7 @@ namespace {
 
 constexpr float kUp = 4096.0f, kDown = 1.0f / 4096.0f;   // halves hold 2^12 x
 constexpr int kNormThreads = 256;
-constexpr int kNormBlocks = 256;   // at most, per matrix; one partial sum each
+constexpr int kNormBlocks = 1024;   // at most, per matrix; one partial sum each
 
 // ----------------------------------------------------------------- storage ---
 
@@ -97,36 +97,48 @@ template <typename T> struct Stack {
     int64_t sb, si, sk;
 };
 
+// the sum over a workgroup, in a fixed order; `lds` holds one value a wavefront
 __device__ __forceinline__ double block_sum(double v, double *lds)
 {
-    const int tid = (int)threadIdx.x;
-    lds[tid] = v;
-    __syncthreads();
 #pragma unroll
-    for (int n = kNormThreads / 2; n > 0; n >>= 1) {
-        if (tid < n) lds[tid] += lds[tid + n];
-        __syncthreads();
-    }
-    return lds[0];
+    for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d);
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+    __syncthreads();
+    double sum = 0.0;
+#pragma unroll
+    for (int w = 0; w < kNormThreads / 64; ++w) sum += lds[w];
+    return sum;
 }
 
 // partial[z][block] = sum of squares of rows block, block + blocks, ... where
-// `rows` is the direction of the larger stride
+// `rows` is the direction of the larger stride; bound by reading G
 template <typename T>
 __global__ __launch_bounds__(kNormThreads) void orth_norm_kernel(Stack<const T> G, int rows,
                                                                  int cols, int blocks,
-                                                                 double *partial)
+                                                                 Recip blocksInv, double *partial)
 {
-    __shared__ double lds[kNormThreads];
-    const int z = (int)blockIdx.x / blocks, b = (int)blockIdx.x % blocks;
+    __shared__ double lds[kNormThreads / 64];
+    const int z = (int)quotient(blockIdx.x, blocks, blocksInv), b = (int)blockIdx.x - z * blocks;
     const T *p = G.p + z * G.sb;
+    constexpr int N = 16 / (int)sizeof(T);   // values of 16 bytes
     double s = 0.0;
-    for (int i = b; i < rows; i += blocks)
+    for (int i = b; i < rows; i += blocks) {
+        const T *row = p + i * G.si;
+        const int whole = G.sk == 1 ? cols / N : 0;
 #pragma unroll 4
-        for (int k = (int)threadIdx.x; k < cols; k += kNormThreads) {
-            const double v = (double)to_float(p[i * G.si + k * G.sk]);
-            s += v * v;
+        for (int k = (int)threadIdx.x; k < whole; k += kNormThreads) {
+            const Run<T, N> v = *reinterpret_cast<const Run<T, N> *>(row + k * N);
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                const double x = (double)to_float(v.v[j]);
+                s += x * x;
+            }
         }
+        for (int k = whole * N + (int)threadIdx.x; k < cols; k += kNormThreads) {
+            const double x = (double)to_float(row[k * G.sk]);
+            s += x * x;
+        }
+    }
     s = block_sum(s, lds);
     if (threadIdx.x == 0) partial[(int64_t)z * blocks + b] = s;
 }
@@ -135,29 +147,37 @@ __global__ __launch_bounds__(kNormThreads) void orth_norm_kernel(Stack<const T> 
 constexpr int kStart = 64;
 template <typename T, int KIND>
 __global__ __launch_bounds__(kNormThreads) void orth_start_kernel(
-    Stack<const T> G, int m, int n, int tilesM, int tilesN, const double *partial, int blocks,
-    double eps, char *X, char *XT, int64_t stackX, int64_t stackXT)
+    Stack<const T> G, int m, int n, int tiles, Recip tilesInv, int tilesN, Recip tilesNInv,
+    const double *partial, int blocks, double eps, char *X, char *XT, int64_t stackX, int64_t stackXT)
 {
-    __shared__ double lds[kNormThreads];
+    __shared__ double lds[kNormThreads / 64];
     __shared__ float tile[kStart][kStart + 1];
     const int tid = (int)threadIdx.x;
-    const int tiles = tilesM * tilesN, z = (int)blockIdx.x / tiles, t = (int)blockIdx.x % tiles;
-    const int i0 = t / tilesN * kStart, k0 = t % tilesN * kStart;
-    const double sum = block_sum(tid < blocks ? partial[(int64_t)z * blocks + tid] : 0.0, lds);
+    const int z = (int)quotient(blockIdx.x, tiles, tilesInv), t = (int)blockIdx.x - z * tiles;
+    const int tm = (int)quotient((uint32_t)t, tilesN, tilesNInv);
+    const int i0 = tm * kStart, k0 = (t - tm * tilesN) * kStart;
+    // the tile's loads are on their way while the norm is summed
+    const T *g = G.p + z * G.sb;
+    const bool along = G.sk <= G.si;   // neighbouring lanes take neighbours in memory
+    constexpr int U = kStart * kStart / kNormThreads;
+    T x[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int e = u * kNormThreads + tid, a = e / kStart, b = e % kStart;
+        const int i = i0 + (along ? a : b), k = k0 + (along ? b : a);
+        x[u] = g[(i < m ? i : m - 1) * G.si + (k < n ? k : n - 1) * G.sk];
+    }
+    double sum = 0.0;
+    for (int b = tid; b < blocks; b += kNormThreads) sum += partial[(int64_t)z * blocks + b];
+    sum = block_sum(sum, lds);
     // an infinity or a NaN anywhere makes the whole matrix NaN
     const double scale =
         sum < (double)INFINITY ? (double)kUp / (sqrt(sum) + eps) : (double)NAN;
-    const T *g = G.p + z * G.sb;
-    const bool along = G.sk <= G.si;   // neighbouring lanes take neighbours in memory
-#pragma unroll 4
-    for (int u = 0; u < kStart * kStart / kNormThreads; ++u) {
-        const int e = u * kNormThreads + tid;
-        const int a = e / kStart, b = e % kStart;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int e = u * kNormThreads + tid, a = e / kStart, b = e % kStart;
         const int i = along ? a : b, k = along ? b : a;
-        float v = 0.0f;
-        if (i0 + i < m && k0 + k < n)
-            v = (float)((double)to_float(g[(i0 + i) * G.si + (k0 + k) * G.sk]) * scale);
-        tile[i][k] = v;
+        tile[i][k] = i0 + i < m && k0 + k < n ? (float)((double)to_float(x[u]) * scale) : 0.0f;
     }
     __syncthreads();
 #pragma unroll
@@ -770,12 +790,13 @@ gett_status_t orthogonalize_typed(const Problem &P, Stack<const T> G, Stack<T> O
     Stack<const T> g = G;
     if (!along) std::swap(g.si, g.sk);
     hipLaunchKernelGGL((orth_norm_kernel<T>), dim3((unsigned)(P.batch * blocks)),
-                       dim3(kNormThreads), 0, P.stream, g, outer, inner, blocks, partial);
+                       dim3(kNormThreads), 0, P.stream, g, outer, inner, blocks, recip(blocks),
+                       partial);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return GETT_ERROR_HIP;
     hipLaunchKernelGGL((orth_start_kernel<T, KIND>), dim3((unsigned)(P.batch * startM * startN)),
-                       dim3(kNormThreads), 0, P.stream, G, m, n, (int)startM, (int)startN, partial,
-                       blocks, P.eps, x, xt, X, XT);
+                       dim3(kNormThreads), 0, P.stream, G, m, n, (int)(startM * startN),
+                       recip(startM * startN), (int)startN, recip(startN), partial, blocks, P.eps, x, xt, X, XT);
     e = hipGetLastError();
     if (e != hipSuccess) return GETT_ERROR_HIP;
     if (P.steps == 0) {
