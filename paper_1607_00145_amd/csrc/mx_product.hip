@@ -81,7 +81,7 @@ __global__ __launch_bounds__(S::THREADS) void mx_tile_kernel(TileJob<T> first, T
     p.init();
     p.run(dyn_lds, A, B, w.t0, w.t1);
     __syncthreads();
-    if (!panel_join<kPanelMx, S>(p, grid, w, dyn_lds) || p.group > 0) return;
+    if (!panel_join<kPanelMx, S>(p, grid, w, dyn_lds)) return;
 #pragma unroll
     for (int e = 0; e < 16; ++e)
 #pragma unroll

@@ -281,7 +281,7 @@ __device__ __forceinline__ void store_panels(Panel<KIND, S> &p, char *lds, char 
 #pragma unroll
     for (int pass = 0; pass < ALL / PP; ++pass) {
         __syncthreads();
-        if (p.group == 0 && mine / (PP * E) == pass) {
+        if (mine / (PP * E) == pass) {
             // each pass rounds anew: the compiler would round all values once
             // and keep the parts, twice the registers, in scratch memory
 #pragma unroll
@@ -358,7 +358,7 @@ __global__ __launch_bounds__(S::THREADS) void orth_product_kernel(ProductArgs d,
 
     // rows and columns of the padding become zeros
     constexpr int PASSES = STEP == kGram || kAddendEarly<S> ? 1 : image_passes<KIND, S, false>();
-#pragma unroll
+#pragma unroll 1
     for (int pass = 0; pass < PASSES; ++pass) {
         const char *image = dyn_lds + (kAddendEarly<S> ? S::lds(KIND) : 0);
         if constexpr (STEP != kGram && !kAddendEarly<S>) {
@@ -398,7 +398,6 @@ __global__ __launch_bounds__(S::THREADS) void orth_product_kernel(ProductArgs d,
         if (!kSymmetric || tm != tn)
             store_panels<KIND, S, true>(p, dyn_lds, d.outT + z * d.stackOutT, d.n,
                                         padded<KIND>(d.m) / panel_elements<KIND>(), B.row0, A.row0);
-    } else if (p.group > 0) {
     } else if (O.si != 1 || O.sk == 1) {
         // a lane's rows: four times FM in a row, then as many are another's
         T *o = O.p + z * O.sb + (A.row0 + p.row(0, 0)) * O.si + col * O.sk;

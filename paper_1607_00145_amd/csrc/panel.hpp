@@ -2,9 +2,9 @@
 // acc[i][j] = sum over K of row i of one operand times row j of another.
 //
 // Both operands are cut along K into panels of 128 bytes a row; a panel's rows
-// follow one another in memory, panel after panel (row after row, the rows of
-// a panel would lie a power of two apart and share few L2 channels: 181 us for
-// the half-precision product 4096^3 that takes XXX this way).  A row's 128 bytes
+// follow one another in memory, panel after panel, so that an instruction's loads
+// are one run of 1 KB (row after row, the rows of a panel lie a power of two
+// apart: 2 to 5 % more for a 4096 x 4096 update).  A row's 128 bytes
 // are eight 16-byte pieces, taken as four slabs of two pieces, slab s the
 // pieces s and s + 4.  One MFMA 32 x 32 takes a slab of 32 rows of each operand
 // (16 bytes a lane: lane l gives row l % 32, piece 4 (l / 32) + s), whatever
@@ -67,12 +67,11 @@ template <int N, int I = 0, typename F> __device__ __forceinline__ void static_f
     }
 }
 
-template <int FM_, int FN_, int WM_, int WN_, int NS_, int KG_ = 1> struct PanelShape {
+template <int FM_, int FN_, int WM_, int WN_, int NS_> struct PanelShape {
     static constexpr int FM = FM_, FN = FN_, WM = WM_, WN = WN_;   // fragments, wavefronts
     static constexpr int NS = NS_;                                 // stages
     static constexpr int BM = 32 * FM * WM, BN = 32 * FN * WN;
-    static constexpr int KG = KG_;                                 // groups that share K
-    static constexpr int NW = WM * WN, THREADS = 64 * NW * KG;     // wavefronts of a group
+    static constexpr int NW = WM * WN, THREADS = 64 * NW;
     static constexpr int DATA = (BM + BN) * 128;      // bytes of a stage without scales
     static constexpr int SCALES = (BM + BN) * 8;      // of its scales
     static constexpr int J = DATA / 1024 / NW;        // load instructions a wavefront per panel
@@ -80,8 +79,7 @@ template <int FM_, int FN_, int WM_, int WN_, int NS_, int KG_ = 1> struct Panel
     static constexpr int TILE = BM * BN;              // elements
     static_assert((BM / 8) % NW == 0 && (BN / 8) % NW == 0, "whole instructions per operand");
     static_assert(SCALES % (256 * NW) == 0 && BM % 64 == 0 && BN % 64 == 0, "64 scale words each");
-    static constexpr int lds(int kind) { return KG * NS * (DATA + (kind == kPanelMx ? SCALES : 0)); }
-    static_assert(KG == 1 || (KG - 1) * TILE * 4 <= KG * NS * DATA, "the groups' sums fit");
+    static constexpr int lds(int kind) { return NS * (DATA + (kind == kPanelMx ? SCALES : 0)); }
 };
 
 // One operand of a tile: rows [row0, row0 + tile rows) of a matrix of `rows`
@@ -91,21 +89,20 @@ struct PanelOperand {
     const uint8_t *data;     // panel 0, row 0
     const uint8_t *scales;   // Mx: the packed scales
     int rows, row0;
-    // rows row0 ... of panel t, and nothing behind the panel's last row (of a
-    // panel that is not `there`, nothing: zeros are read); the scale words of
-    // half h likewise
-    __device__ __forceinline__ __amdgpu_buffer_rsrc_t panel(int t, bool there) const
+    // rows row0 ... of panel t, and nothing behind the panel's last row; the
+    // scale words of half h likewise
+    __device__ __forceinline__ __amdgpu_buffer_rsrc_t panel(int t) const
     {
         const uint8_t *p = data + ((int64_t)t * rows + row0) * 128;
-        const int64_t bytes = there ? (int64_t)(rows - row0) * 128 : 0;
+        const int64_t bytes = (int64_t)(rows - row0) * 128;
         return __builtin_amdgcn_make_buffer_rsrc(
             const_cast<uint8_t *>(p), 0, (int)(uint32_t)(bytes < 0xffffffffll ? bytes : 0xffffffffll),
             0x00027000);
     }
-    __device__ __forceinline__ __amdgpu_buffer_rsrc_t words(int t, int half, int64_t R, bool there) const
+    __device__ __forceinline__ __amdgpu_buffer_rsrc_t words(int t, int half, int64_t R) const
     {
         const uint8_t *p = scales + (((int64_t)t * 2 + half) * R + row0) * 4;
-        const int64_t bytes = there ? (R - row0) * 4 : 0;
+        const int64_t bytes = (R - row0) * 4;
         return __builtin_amdgcn_make_buffer_rsrc(
             const_cast<uint8_t *>(p), 0, (int)(uint32_t)(bytes < 0xffffffffll ? bytes : 0xffffffffll),
             0x00027000);
@@ -141,16 +138,16 @@ template <int F> __device__ __forceinline__ int panel_place(int p, int r)
 template <int KIND, typename S> struct Panel {
     static constexpr int FM = S::FM, FN = S::FN, NS = S::NS;
     static constexpr int STAGE = S::DATA + (KIND == kPanelMx ? S::SCALES : 0);
-    static constexpr int G = KIND == kPanelSplit ? 2 : 1;   // slabs read together
+    // Slabs read together.  One block of 32 x 32 a wavefront has too few MFMAs
+    // in a slab to cover the reads of the next: it reads whole panels.
+    static constexpr int G = FM * FN == 1 ? 4 : KIND == kPanelSplit ? 2 : 1;
     f16v acc[FM][FN];
-    int r, h, wm, wn, group;
+    int r, h, wm, wn;
 
     __device__ __forceinline__ void init()
     {
         const int tid = (int)threadIdx.x;
-        const int all = __builtin_amdgcn_readfirstlane(tid >> 6);
-        group = S::KG == 1 ? 0 : all / S::NW;
-        const int wave = S::KG == 1 ? all : all % S::NW;
+        const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
         r = tid & 31;
         h = (tid >> 5) & 1;
         wm = wave / S::WN;
@@ -169,17 +166,13 @@ template <int KIND, typename S> struct Panel {
     }
     __device__ __forceinline__ int col(int j) const { return wn * 32 * FN + FN * r + j; }
 
-    // panels [t0, t1) of both operands; `lds` holds S::lds(KIND) bytes.  With
-    // several groups, group g takes panels t0 + g, t0 + g + KG, ... in stages of
-    // its own (all go through the same number of barriers), and group 0 ends
-    // with the sum; the others have nothing.
-    __device__ __forceinline__ void run(char *all, const PanelOperand &A, const PanelOperand &B,
+    // panels [t0, t1) of both operands; `lds` holds S::lds(KIND) bytes.
+    __device__ __forceinline__ void run(char *lds, const PanelOperand &A, const PanelOperand &B,
                                         int t0, int t1)
     {
-        char *lds = all + group * NS * STAGE;
         constexpr int NW = S::NW, J = S::J, JA = S::BM / 8 / NW;
         const int lane = (int)threadIdx.x & 63;
-        const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) - group * NW;
+        const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
         // this lane's piece of each load: 16 places of a pair of rows
         uint32_t off[J];
 #pragma unroll
@@ -193,10 +186,9 @@ template <int KIND, typename S> struct Panel {
             off[j] = (uint32_t)(row < last ? row : last) * 128 + (uint32_t)(p & 7) * 16;
         }
         // buffer loads: a lane's offset stays, the panel's base is a scalar
-        int at = t0 + group;
+        int at = t0;
         auto issue = [&](int stage) {
-            const bool there = S::KG == 1 || at < t1;
-            const __amdgpu_buffer_rsrc_t ra = A.panel(at, there), rb = B.panel(at, there);
+            const __amdgpu_buffer_rsrc_t ra = A.panel(at), rb = B.panel(at);
             char *base = lds + stage * STAGE;
 #pragma unroll
             for (int j = 0; j < J; ++j) {
@@ -215,12 +207,12 @@ template <int KIND, typename S> struct Panel {
                     const int v = isA ? u : u - S::BM / 32, per = (isA ? S::BM : S::BN) / 64;
                     const int half = v / per, first = (v - half * per) * 64;
                     const __amdgpu_buffer_rsrc_t rs =
-                        isA ? A.words(at, half, RA, there) : B.words(at, half, RB, there);
+                        isA ? A.words(at, half, RA) : B.words(at, half, RB);
                     __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (matrix_lds *)(base + S::DATA + u * 256),
                                                              4, (first + lane) * 4, 0, 0, 0);
                 }
             }
-            at += S::KG;
+            ++at;
         };
 
         // LDS reads: rows F r + i of the wavefront's part, piece 4 h + s.  The
@@ -265,29 +257,29 @@ template <int KIND, typename S> struct Panel {
                         lds + (atB ^ ((8 * (j & 1) + s + g) * 16)) + (j >> 1) * 256);
             }
         };
-        auto mma = [&](int set, auto slab) {
-            constexpr int s = decltype(slab)::value;
+        auto mma = [&](int set, auto slab) {   // slabs [slab, slab + G)
+            static_for<G>([&](auto gc) {
+                constexpr int g = decltype(gc)::value, s = decltype(slab)::value + g;
+                auto each = [&](int ga, int gb) {
 #pragma unroll
-            for (int i = 0; i < FM; ++i)
+                    for (int i = 0; i < FM; ++i)
 #pragma unroll
-                for (int j = 0; j < FN; ++j) {
-                    if constexpr (KIND == kPanelMx)
-                        acc[i][j] = mfma_mx32<s>(a[set][0][i], b[set][0][j], acc[i][j], sa[i], sb[j]);
-                    else
-                        acc[i][j] = mfma_half(a[set][0][i], b[set][0][j], acc[i][j]);
+                        for (int j = 0; j < FN; ++j) {
+                            if constexpr (KIND == kPanelMx)
+                                acc[i][j] = mfma_mx32<s>(a[set][ga][i], b[set][gb][j], acc[i][j],
+                                                         sa[i], sb[j]);
+                            else
+                                acc[i][j] = mfma_half(a[set][ga][i], b[set][gb][j], acc[i][j]);
+                        }
+                };
+                if constexpr (KIND != kPanelSplit) {
+                    each(g, g);
+                } else if constexpr (g % 2 == 0) {
+                    each(g, g);
+                    each(g, g + 1);
+                    each(g + 1, g);
                 }
-            if constexpr (KIND == kPanelSplit) {
-#pragma unroll
-                for (int i = 0; i < FM; ++i)
-#pragma unroll
-                    for (int j = 0; j < FN; ++j)
-                        acc[i][j] = mfma_half(a[set][0][i], b[set][1][j], acc[i][j]);
-#pragma unroll
-                for (int i = 0; i < FM; ++i)
-#pragma unroll
-                    for (int j = 0; j < FN; ++j)
-                        acc[i][j] = mfma_half(a[set][1][i], b[set][0][j], acc[i][j]);
-            }
+            });
         };
         // no fence: a release would wait for the loads in flight as well
         auto barrier = []() { asm volatile("s_barrier" ::: "memory"); };
@@ -300,7 +292,7 @@ template <int KIND, typename S> struct Panel {
         constexpr int kAll = wait_for(0), kFirst = wait_for((NS - 1) * LOADS);
         constexpr int kNext = wait_for((NS - 2) * LOADS);
 
-        const int n = (t1 - t0 + S::KG - 1) / S::KG;
+        const int n = t1 - t0;
         if (n <= 0) return;
 #pragma unroll
         for (int i = 0; i < NS; ++i)
@@ -311,26 +303,33 @@ template <int KIND, typename S> struct Panel {
         at_stage(0);
         read(0, 0);
         int stage = 0;
-        // one panel; `more`: another follows, `load`: and one is loaded
-        auto panel = [&](auto more, auto load) {
+        // one panel, whose first slabs are in set `set0`; `more`: another follows,
+        // `load`: one is loaded (a bool: perhaps)
+        auto panel = [&](auto more, auto load, auto set0) {
+            constexpr bool steady = std::is_same<decltype(load), std::true_type>::value;
+            constexpr bool perhaps = std::is_same<decltype(load), bool>::value;
             scales(stage);
             static_for<STEPS>([&](auto step) {
-                constexpr int s = decltype(step)::value;
+                constexpr int s = decltype(step)::value, set = (decltype(set0)::value + s) & 1;
                 if constexpr (s + 1 < STEPS) {
-                    read((s + 1) & 1, (s + 1) * G);
+                    read(set ^ 1, (s + 1) * G);
                 } else if constexpr (more) {
-                    __builtin_amdgcn_s_waitcnt(load ? kNext : kAll);   // t + 1 loaded, t read
+                    __builtin_amdgcn_s_waitcnt(steady ? kNext : kAll);   // t + 1 loaded, t read
                     barrier();
-                    if constexpr (load) issue(stage);
+                    if constexpr (steady) {
+                        issue(stage);
+                    } else if constexpr (perhaps) {
+                        if (load) issue(stage);
+                    }
                     stage = stage + 1 == NS ? 0 : stage + 1;
                     at_stage(stage);
-                    read((s + 1) & 1, 0);
+                    read(set ^ 1, 0);
                 }
-                mma(s & 1, std::integral_constant<int, s * G>{});
+                mma(set, std::integral_constant<int, s * G>{});
                 // the reads of one group lie among the first MFMAs of the one
                 // before, and stay there
                 constexpr int READS = G * (FM + FN);
-                constexpr int MFMAS = FM * FN * (KIND == kPanelSplit ? 3 : 1);
+                constexpr int MFMAS = FM * FN * (KIND == kPanelSplit ? 3 * G / 2 : G);
                 if constexpr (s + 1 < STEPS || more) {
                     static_for<(READS < MFMAS ? READS : MFMAS)>([](auto ic) {
                         constexpr int i = decltype(ic)::value;
@@ -343,33 +342,28 @@ template <int KIND, typename S> struct Panel {
         };
         const std::true_type yes;
         const std::false_type no;
+        const std::integral_constant<int, 0> even;
+        const std::integral_constant<int, STEPS % 2> odd;   // the next panel's set
         int t = 0;
-        for (; t + NS < n; ++t) panel(yes, yes);
-        for (; t + 1 < n; ++t) panel(yes, no);
-        panel(no, no);
-        if constexpr (S::KG > 1) {
-            float *sums = reinterpret_cast<float *>(all) + ((int)threadIdx.x & (64 * NW - 1));
-            __syncthreads();
-#pragma unroll
-            for (int i = 0; i < FM; ++i)
-#pragma unroll
-                for (int j = 0; j < FN; ++j)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        float *at = sums + ((i * FN + j) * 16 + e) * 64 * NW;
-                        if (group > 0) at[(group - 1) * S::TILE] = acc[i][j][e];
-                    }
-            __syncthreads();
-            if (group == 0) {
-#pragma unroll
-                for (int g = 0; g < S::KG - 1; ++g)
-#pragma unroll
-                    for (int i = 0; i < FM; ++i)
-#pragma unroll
-                        for (int j = 0; j < FN; ++j)
-#pragma unroll
-                            for (int e = 0; e < 16; ++e)
-                                acc[i][j][e] += sums[((i * FN + j) * 16 + e) * 64 * NW + g * S::TILE];
+        if constexpr (STEPS % 2 == 0) {
+            // (no branch inside a panel: across one, the sums would be copied)
+            for (; t + NS < n; ++t) panel(yes, yes, even);
+            for (; t + 1 < n; ++t) panel(yes, no, even);
+            panel(no, no, even);
+        } else {
+            for (; t + NS + 1 < n; t += 2) {
+                panel(yes, yes, even);
+                panel(yes, yes, odd);
+            }
+            for (; t + 2 < n; t += 2) {
+                panel(yes, t + NS < n, even);
+                panel(yes, t + 1 + NS < n, odd);
+            }
+            if (t + 1 < n) {
+                panel(yes, t + NS < n, even);
+                panel(no, no, odd);
+            } else {
+                panel(no, no, even);
             }
         }
     }
@@ -452,18 +446,17 @@ __device__ __forceinline__ bool panel_join(Panel<KIND, S> &p, const PanelGrid &d
 {
     if (w.shared < 0) return true;
     const int tid = (int)threadIdx.x;
-    constexpr int N = 64 * S::NW;   // threads that hold sums
-    float *first = d.slots + (int64_t)w.shared * d.slices * S::TILE + (tid & (N - 1));
+    constexpr int N = S::THREADS;
+    float *first = d.slots + (int64_t)w.shared * d.slices * S::TILE + tid;
     float *own = first + (int64_t)w.slice * S::TILE;
-    if (p.group == 0)
 #pragma unroll
-        for (int i = 0; i < S::FM; ++i)
+    for (int i = 0; i < S::FM; ++i)
 #pragma unroll
-            for (int j = 0; j < S::FN; ++j)
+        for (int j = 0; j < S::FN; ++j)
 #pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    __hip_atomic_store(own + ((i * S::FN + j) * 16 + e) * N, p.acc[i][j][e],
-                                       __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            for (int e = 0; e < 16; ++e)
+                __hip_atomic_store(own + ((i * S::FN + j) * 16 + e) * N, p.acc[i][j][e],
+                                   __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     __builtin_amdgcn_s_waitcnt(7 << 4 | 15 << 8);   // vmcnt 0: the stores are done
     __syncthreads();
     int *last = reinterpret_cast<int *>(lds);
@@ -474,31 +467,29 @@ __device__ __forceinline__ bool panel_join(Panel<KIND, S> &p, const PanelGrid &d
     if (!*last) return false;
     if (tid == 0)
         __hip_atomic_store(d.counters + w.shared, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    if (p.group == 0)
 #pragma unroll
-        for (int i = 0; i < S::FM; ++i)
+    for (int i = 0; i < S::FM; ++i)
 #pragma unroll
-            for (int j = 0; j < S::FN; ++j) {
-                const float *at = first + (i * S::FN + j) * 16 * N;
-                for (int s0 = 0; s0 < d.slices; s0 += 2) {   // two slices' loads together
-                    float v[2][16];
+        for (int j = 0; j < S::FN; ++j) {
+            const float *at = first + (i * S::FN + j) * 16 * N;
+            for (int s0 = 0; s0 < d.slices; s0 += 2) {   // two slices' loads together
+                float v[2][16];
 #pragma unroll
-                    for (int s = 0; s < 2; ++s)
-                        if (s0 + s < d.slices)
+                for (int s = 0; s < 2; ++s)
+                    if (s0 + s < d.slices)
 #pragma unroll
-                            for (int e = 0; e < 16; ++e)
-                                v[s][e] = __hip_atomic_load(at + (int64_t)(s0 + s) * S::TILE + e * N,
-                                                            __ATOMIC_RELAXED,
-                                                            __HIP_MEMORY_SCOPE_AGENT);
+                        for (int e = 0; e < 16; ++e)
+                            v[s][e] = __hip_atomic_load(at + (int64_t)(s0 + s) * S::TILE + e * N,
+                                                        __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 #pragma unroll
-                    for (int s = 0; s < 2; ++s)
-                        if (s0 + s < d.slices)
+                for (int s = 0; s < 2; ++s)
+                    if (s0 + s < d.slices)
 #pragma unroll
-                            for (int e = 0; e < 16; ++e)
-                                p.acc[i][j][e] = s0 + s == 0 ? v[s][e] : p.acc[i][j][e] + v[s][e];
-                }
-                __builtin_amdgcn_sched_barrier(0);
+                        for (int e = 0; e < 16; ++e)
+                            p.acc[i][j][e] = s0 + s == 0 ? v[s][e] : p.acc[i][j][e] + v[s][e];
             }
+            __builtin_amdgcn_sched_barrier(0);
+        }
     __syncthreads();   // everyone has read `last`
     return true;
 }
