@@ -362,24 +362,29 @@ def _linear_function():
             return y
 
         @staticmethod
-        @torch.autograd.function.once_differentiable
         def backward(ctx, dy):
-            need_x, need_w = ctx.needs_input_grad
-            m, n, k, tx, tw = ctx.sizes
-            if dy.stride(0) < 1 or dy.stride(1) < 1:
-                dy = dy.contiguous()   # the gradient of a sum is broadcast
-            code, _, _, sm, sn = _matrix("dy", dy)
-            _, xt, xs, wt, ws = ctx.packed
-            dx = torch.empty((m, k), dtype=tx, device=dy.device) if need_x else None
-            dw = torch.empty((n, k), dtype=tw, device=dy.device) if need_w else None
-            st = _bound.gett_mx_linear_grad(
-                m, n, k, code, dy.data_ptr(), sm, sn, xt, xs, wt, ws,
-                dx.data_ptr() if need_x else None, k or 1, 1, _codes[tw],
-                dw.data_ptr() if need_w else None, k or 1, 1, _package._current_stream())
-            if st != 0:
-                raise GettError(st, "gett_mx_linear_grad")
-            return dx, dw
+            # the decorated form refuses a second derivative; nobody can ask for
+            # one where gradients are not recorded, and it costs 4 us of host time
+            return recorded(ctx, dy) if torch.is_grad_enabled() else gradients(ctx, dy)
 
+    def gradients(ctx, dy):
+        need_x, need_w = ctx.needs_input_grad
+        m, n, k, tx, tw = ctx.sizes
+        if dy.stride(0) < 1 or dy.stride(1) < 1:
+            dy = dy.contiguous()   # the gradient of a sum is broadcast
+        code, _, _, sm, sn = _matrix("dy", dy)
+        _, xt, xs, wt, ws = ctx.packed
+        dx = torch.empty((m, k), dtype=tx, device=dy.device) if need_x else None
+        dw = torch.empty((n, k), dtype=tw, device=dy.device) if need_w else None
+        st = _bound.gett_mx_linear_grad(
+            m, n, k, code, dy.data_ptr(), sm, sn, xt, xs, wt, ws,
+            dx.data_ptr() if need_x else None, k or 1, 1, _codes[tw],
+            dw.data_ptr() if need_w else None, k or 1, 1, _package._current_stream())
+        if st != 0:
+            raise GettError(st, "gett_mx_linear_grad")
+        return dx, dw
+
+    recorded = torch.autograd.function.once_differentiable(gradients)
     _function = MXLinear
     return _function
 

@@ -577,3 +577,15 @@ def test_offsets_beyond_32_bits(gpu):
     a = g.mx_quantize(torch.randn(40, 64, device="cuda"))
     b = g.mx_quantize(torch.randn(5, 64, device="cuda"))
     assert torch.equal(g.mx_matmul(a, b, C), g.mx_matmul(a, b, dtype=torch.bfloat16))
+
+
+def test_linear_refuses_a_second_derivative(gpu):
+    import torch
+    x = torch.randn(9, 40, device=gpu, requires_grad=True)
+    w = torch.randn(7, 40, device=gpu, requires_grad=True)
+    y = g.mx_linear(x, w)
+    first, = torch.autograd.grad(y, x, torch.ones_like(y), retain_graph=True)
+    dx, = torch.autograd.grad(y, x, torch.ones_like(y, requires_grad=True), create_graph=True)
+    assert torch.equal(first, dx)
+    with pytest.raises(RuntimeError):
+        dx.sum().backward()
