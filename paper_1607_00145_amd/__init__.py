@@ -8,6 +8,9 @@ used for device memory and streams only.
     import torch, paper_1607_00145_amd as gett
     p = gett.Plan("C[a,b,c] = A[a,k,c] * B[k,b]", C=c, A=a, B=b)
     p(a, b, c, alpha=1.0, beta=0.0)          # enqueued on torch's current stream
+
+``matrix`` has the matrix operators for training and serving in 4 bits
+(``include/gett_matrix.h``); its names are the package's too.
 """
 from __future__ import annotations
 
