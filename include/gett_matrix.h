@@ -197,9 +197,9 @@ gett_status_t gett_mx_linear_grad(int64_t m, int64_t n, int64_t k, gett_dtype_t 
  * matrix makes that matrix NaN.  Errors: GETT_ERROR_INVALID_VALUE (unknown
  * dtype, negative extent or steps, stride < 1, eps negative or NaN, a
  * coefficient that is not finite, null or misaligned pointer, overlap),
- * GETT_ERROR_NOT_SUPPORTED (see above; rows or cols of 2^20 and more, steps above 1000; strides
- * that map two elements to one address; batch x tiles beyond a launch),
- * GETT_ERROR_HIP.
+ * GETT_ERROR_NOT_SUPPORTED (see above; rows or cols of 2^20 and more, steps
+ * above 1000; strides that map two elements to one address; batch x tiles
+ * beyond a launch), GETT_ERROR_HIP.
  */
 gett_status_t gett_orthogonalize(gett_dtype_t dtype, int64_t batch, int64_t rows, int64_t cols,
                                  const void *G, int64_t stride_batch, int64_t stride_row,

@@ -2,12 +2,19 @@
 //     C[m, n] <- alpha * sum_k A[m, k] B[n, k] + beta * C[m, n],
 // and of float rows, quantised on the way, with a packed matrix.
 //
-// Many rows: tiles of C, the operands' panels through LDS (panel.hpp).
-// Few rows: bound by B's bytes.  A workgroup takes 32 rows of B (32 columns
+// Many rows: tiles of C, the operands' panels through LDS (panel.hpp).  Bound:
+// the card's power under the matrix instructions; 8192 x 8192 x 8192 into bf16
+// takes 255 us (4.3 PFLOP/s; the instructions alone, on random operands in
+// registers, reach 6.2).  A tile's results go out as they lie, FN neighbours
+// a lane.
+// Few rows (up to 32): bound by B's bytes, and below some 16 MB of them by the
+// launch and two memory latencies.  A workgroup takes 32 rows of B (32 columns
 // of C) and its wavefronts every eighth panel; B goes from memory straight
 // into the registers that the MFMA reads (a lane's two pieces of a panel are
 // 32 bytes of one row), so no byte waits for a barrier, and the eight partial
-// results are summed in wavefront order through LDS.
+// results are summed in wavefront order through LDS.  8192 x 4096 (17.8 MB)
+// with 16 packed rows takes 5.4 us (as tiles 7.6), with 32 rows 6.6 (8.0),
+// with one bf16 row packed on its way 6.6.
 #include "launch.hpp"
 #include "matrix.hpp"
 #include "mx.hpp"
@@ -193,12 +200,19 @@ template <typename TA> struct FewFloat {
                 pack(f, b, x);
             }
         } else {
+            // element by element, columns past the last read as the last and
+            // replaced: no branches, so that a block's loads go out together
 #pragma unroll 1
             for (int b = 0; b < 2; ++b) {
+                const int left = k - (k0 + 32 * b) - 1;   // the last column's place
+                if (left < 0) break;                      // (zeros)
+                const TA *q = p + 32 * b * sk;
+                TA v[32];
+#pragma unroll
+                for (int i = 0; i < 32; ++i) v[i] = q[(i < left ? i : left) * sk];
                 float x[32];
 #pragma unroll
-                for (int i = 0; i < 32; ++i)
-                    x[i] = k0 + 32 * b + i < k ? to_float(p[(32 * b + i) * sk]) : 0.0f;
+                for (int i = 0; i < 32; ++i) x[i] = i <= left ? to_float(v[i]) : 0.0f;
                 if (b == 0) pack(f, 0, x);
                 else pack(f, 1, x);
             }
@@ -217,7 +231,7 @@ template <typename TA> struct FewFloat {
     }
 };
 
-// `deep`: panels whose loads are in flight together
+// DEEP: panels of a wavefront whose loads are in flight together
 template <typename T, typename LA, int FM, int DEEP>
 __global__ __launch_bounds__(kFewWaves * 64) void mx_few_kernel(LA A, const uint8_t *codesB,
                                                                const uint8_t *scalesB, int panels,
@@ -452,6 +466,16 @@ hipError_t few_float_of(gett_dtype_t dtypeA, const void *A, int64_t sam, int64_t
     return few_float<_Float16, T>(A, sam, sak, k, B, o, stream);
 }
 
+// Whether a float A of m rows is packed inside its product with an n x k B:
+// every workgroup then packs all of A again, but a launch is saved.  us in
+// one launch and in two, bf16: 8192 x 4096, 1 row 6.6 / 7.4, 16 rows 8.2 /
+// 8.6; 515 x 1000, 1 row 5.5 / 6.8; 2048 x 2048, 16 rows 5.2 / 6.9; 8192 x
+// 8192, 8 rows 11.9 / 12.4, 12 rows 13.3 / 12.7, 16 rows 14.6 / 13.0.
+bool packs_inside(int64_t m, int64_t n, int64_t k)
+{
+    return m <= 8 || (m <= 16 && n * k <= (int64_t)1 << 25);
+}
+
 template <typename T>
 Result<T> few_result(void *C, int64_t sm, int64_t sn, int64_t m, int64_t n, double alpha, double beta)
 {
@@ -527,7 +551,7 @@ gett_status_t gett_mx_apply(int64_t m, int64_t n, int64_t k, double alpha, gett_
     if (bytesA < 0) return GETT_ERROR_NOT_SUPPORTED;
     if (overlaps(C, bytesC, A, bytesA) || !clear_of(C, bytesC, codes_B, scales_B, n, k))
         return GETT_ERROR_INVALID_VALUE;
-    if (m <= 16) {
+    if (packs_inside(m, n, k)) {
         const Packed W = {codes_B, scales_B, n};
         hipError_t e;
         if (dtype == GETT_FLOAT32)

@@ -3,10 +3,18 @@
 //     X_0 = G / (|G| + eps);   S = X X^T;   B = b S + c S^2;   X <- a X + B X
 //
 // X is held with its shorter side as rows (m <= n), so S and B are m x m.
-// Bound: matrix instructions, 2 m n + 4 m (m + n) ... per step; S and S^2 are
-// symmetric, so only the tiles on and below the diagonal are computed and the
-// others mirrored: m^2 n + m^3 + 2 m^2 n multiplications' flops per step
-// instead of 2 m^2 n + 2 m^3 + 2 m^2 n.
+// Bound: matrix instructions.  S and S^2 are symmetric, so only the tiles on
+// and below the diagonal are computed and the others mirrored: m^2 n + m^3 +
+// 2 m^2 n operations per step instead of 2 m^2 n + 2 m^3 + 2 m^2 n, each three
+// MFMA operations where numbers are held in two parts.
+//
+// 4096 x 4096, five steps, float: 3.74 ms; a step's three products 200-214,
+// 200-215 and 363-394 us (1.0 to 1.1 PFLOP/s of MFMA operations; the update's
+// panels alone, without reading the addend and writing both orientations, 1.2),
+// the norm 13.5 and the start 41-47.  bf16: 1.64 ms; 102, 104 and 150.
+// Mid-sized matrices are chains of launches: 15 products of 6 to 8 us at 517 x
+// 1000, of which three are the launch and the rest loads, a short K and the
+// stores, each waiting for the one before.
 //
 // Numbers.  |X| <= 1 at the start and every singular value stays below 3
 // (gett_orthogonalize refuses other polynomials), so all entries of X, S and
@@ -520,13 +528,19 @@ struct Problem {
 // ------------------------------------------------------------ small matrices ---
 //
 // A matrix whose X, X^T and S fit the 160 KB of a CU goes through all steps in
-// one workgroup: no launch and no memory between them.  Rows are padded to 32
-// (zeros, which stay zeros) and lie 16 bytes more than their length apart, so
-// that sixteen rows' pieces fall on different banks.  A wavefront takes blocks of
-// 32 x 32 of a product in turn; a lane then holds column r and four times
-// four neighbouring rows: the transpose is written in vectors, X itself value
-// by value.  B takes S's place: the blocks wait in registers until all have
-// read S (kSmallBlocks a wavefront at most).
+// one workgroup: no launch and no memory between them.  us so and by launches
+// (in a graph, without the host's time for 17 launches): 12 x 64 x 128 floats
+// 30 / 74, bf16 21 / 61; 16 x 128 x 128 floats 87 / 88, bf16 42 / 69; 600 x 64 x
+// 128 floats 94 / 229; 32 x 1000 floats 92 / 91, bf16 53 / 69.  Bound: the
+// latency of each step's three products, of the LDS accesses between them and
+// of their barriers.
+//
+// Rows are padded to 32 (zeros, which stay zeros) and lie 16 bytes more than
+// their length apart, so that sixteen rows' pieces fall on different banks.  A
+// wavefront takes blocks of 32 x 32 of a product in turn; a lane then holds
+// column r and four times four neighbouring rows: the transpose is written in
+// vectors, X itself value by value.  B takes S's place: the blocks wait in
+// registers until all have read S (kSmallBlocks a wavefront at most).
 
 constexpr int kSmallWaves = 8;
 constexpr int kSmallBlocks = 2;
