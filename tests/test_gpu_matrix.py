@@ -589,3 +589,12 @@ def test_linear_refuses_a_second_derivative(gpu):
     assert torch.equal(first, dx)
     with pytest.raises(RuntimeError):
         dx.sum().backward()
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("shape", [(600, 600), (1100, 1210), (2310, 2200)])
+def test_orthogonalize_many_tiles(gpu, shape, dtype):
+    """Several bands of tile rows, the last one incomplete."""
+    rng = np.random.default_rng(sum(shape))
+    G = stack(rng, shape, dtype)
+    orth_close(g.orthogonalize(G, steps=2), G, dtype, steps=2)
