@@ -12,9 +12,9 @@
 // 200-215 and 363-394 us (1.0 to 1.1 PFLOP/s of MFMA operations; the update's
 // panels alone, without reading the addend and writing both orientations, 1.2),
 // the norm 13.5 and the start 41-47.  bf16: 1.64 ms; 102, 104 and 150.
-// Mid-sized matrices are chains of launches: 15 products of 6 to 8 us at 517 x
-// 1000, of which three are the launch and the rest loads, a short K and the
-// stores, each waiting for the one before.
+// Mid-sized matrices are chains of launches: 15 products of 5 to 8 us at 517 x
+// 1000 (bf16, 104 us in all), of which three are the launch and the rest loads,
+// a short K and the stores, each waiting for the one before.
 //
 // Numbers.  |X| <= 1 at the start and every singular value stays below 3
 // (gett_orthogonalize refuses other polynomials), so all entries of X, S and
@@ -456,6 +456,152 @@ __global__ __launch_bounds__(S::THREADS) void orth_product_kernel(ProductArgs d,
     }
 }
 
+// ------------------------------------------------------------ short products ---
+//
+// A product of few tiles is a chain of latencies, not of work.  Here a
+// workgroup takes a block of 32 x 32 results and each of its eight wavefronts
+// every eighth panel, through LDS of its own: all of a wavefront's loads are in
+// flight together, and no barrier comes before the eight partial results are
+// summed, in wavefront order, through LDS.
+
+constexpr int kShortWaves = 8;
+constexpr int kShortDeep = 2;   // panels of a wavefront in flight
+constexpr int kShortE = 32, kShortThreads = 64 * kShortWaves;
+constexpr int kShortOwn = kShortDeep * 2 * kShortE * 128;   // LDS of a wavefront
+constexpr int kShortPitch = kShortE + 2, kShortAcross = kShortE + 1;
+constexpr int kShortLds = kShortWaves * kShortOwn + kShortE * kShortAcross * 4;
+
+template <int KIND, int STEP, typename T>
+__global__ __launch_bounds__(kShortThreads) void orth_short_kernel(ProductArgs d, PanelGrid grid,
+                                                                   Stack<T> O)
+{
+    extern __shared__ __attribute__((aligned(256))) char dyn_lds[];
+    constexpr int E = kShortE, W = kShortWaves, DEEP = kShortDeep, N = E * E / kShortThreads;
+    constexpr bool kSymmetric = STEP == kGram || STEP == kPoly;
+    const int tid = (int)threadIdx.x, lane = tid & 63, r = tid & 31, h = (tid >> 5) & 1;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    char *const own = dyn_lds + wave * kShortOwn;
+    float *const turned = reinterpret_cast<float *>(dyn_lds + W * kShortOwn);
+    int tm, tn;
+    const PanelItem w = panel_item(grid, (int)blockIdx.x);
+    const int z = w.z;
+    if constexpr (kSymmetric) panel_triangle(w.tile, tm, tn);
+    else panel_tile(grid, w.tile, tm, tn);
+    const int row0 = tm * E, col0 = tn * E, padM = padded<KIND>(d.m), padN = padded<KIND>(d.n);
+
+    // a lane's 16 bytes of each load of eight rows: piece p of row r lies at
+    // place p ^ (r / 2 mod 8) of its row; rows past the last read it again, and
+    // their results are not stored
+    const char *from[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+        const int lr = u % 4 * 8 + (lane >> 3), piece = (lane & 7) ^ (lr >> 1 & 7);
+        const int row = (u < 4 ? row0 : col0) + lr, rows = u < 4 ? d.m : d.n;
+        from[u] = (u < 4 ? d.P + z * d.stackP : d.Q + z * d.stackQ) +
+                  (int64_t)(row < rows ? row : rows - 1) * 128 + piece * 16;
+    }
+    // the results that this lane sums, and the addend's numbers there
+    const int lr = tid / (E / N), lc = tid % (E / N) * N, row = row0 + lr, col = col0 + lc;
+    float x[N] = {};
+    if constexpr (STEP != kGram)
+        if (row < d.m && col < padN)
+            load_run<KIND, N>(d.addend + z * d.stackOut + at<KIND>(d.m, row, col), x);
+
+    f16v acc;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc[e] = 0.0f;
+    for (int t0 = wave; t0 < d.panels; t0 += W * DEEP) {
+#pragma unroll
+        for (int u = 0; u < DEEP; ++u) {
+            const int t = t0 + u * W;
+            if (t < d.panels) {
+#pragma unroll
+                for (int v = 0; v < 8; ++v)
+                    __builtin_amdgcn_global_load_lds(
+                        (matrix_global *)(from[v] + (int64_t)t * (v < 4 ? d.m : d.n) * 128),
+                        (matrix_lds *)(own + (u * 8 + v) * 1024), 16, 0, 0);
+            }
+        }
+        __builtin_amdgcn_s_waitcnt(7 << 4 | 15 << 8);   // vmcnt 0
+        asm volatile("" ::: "memory");
+#pragma unroll
+        for (int u = 0; u < DEEP; ++u) {
+            if (t0 + u * W >= d.panels) break;
+            i4 a[4], b[4];
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                const int place = (4 * h + s) ^ (r >> 1 & 7);
+                a[s] = *reinterpret_cast<const i4 *>(own + u * 8192 + r * 128 + place * 16);
+                b[s] = *reinterpret_cast<const i4 *>(own + u * 8192 + 4096 + r * 128 + place * 16);
+            }
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                if constexpr (KIND == kPanelHalf) {
+                    acc = mfma_half(a[s], b[s], acc);
+                } else if (s % 2 == 0) {
+                    acc = mfma_half(a[s], b[s], acc);
+                    acc = mfma_half(a[s], b[s + 1], acc);
+                    acc = mfma_half(a[s + 1], b[s], acc);
+                }
+            }
+        }
+        __builtin_amdgcn_s_waitcnt(0);   // own LDS has been read
+        asm volatile("" ::: "memory");
+    }
+    float *const mine = reinterpret_cast<float *>(own);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) mine[(8 * (e >> 2) + 4 * h + (e & 3)) * kShortPitch + r] = acc[e];
+    __syncthreads();
+
+    // rows and columns of the padding become zeros
+    float v[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = 0.0f;
+#pragma unroll
+    for (int p = 0; p < W; ++p)
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            v[i] += reinterpret_cast<const float *>(dyn_lds + p * kShortOwn)[lr * kShortPitch + lc + i];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        v[i] = d.factor * v[i];
+        if constexpr (STEP != kGram) v[i] += d.scale * x[i];
+        if (row >= d.m || col + i >= d.n) v[i] = 0.0f;
+    }
+    // the other orientation: X^T or the mirrored block; for a result whose
+    // neighbours in memory lie along its rows, the only one
+    const bool turn = STEP == kLast ? O.si == 1 && O.sk != 1 : !kSymmetric || tm != tn;
+    if (turn) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) turned[lr * kShortAcross + lc + i] = v[i];
+        __syncthreads();
+    }
+    const int trow = row0 + lc, tcol = col0 + lr;   // of N neighbours of a column
+    float y[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) y[i] = turn ? turned[(lc + i) * kShortAcross + lr] : 0.0f;
+    if constexpr (STEP != kLast) {
+        if (row < d.m && col < padN)
+            store_run<KIND, N>(d.out + z * d.stackOut + at<KIND>(d.m, row, col), v);
+        if (turn && tcol < d.n && trow < padM)
+            store_run<KIND, N>(d.outT + z * d.stackOutT + at<KIND>(d.n, tcol, trow), y);
+    } else {
+        const int er = turn ? trow : row, ec = turn ? tcol : col;   // first of the N
+        const int left = turn ? (ec < d.n ? d.m - er : 0) : (er < d.m ? d.n - ec : 0);
+        T *const o = O.p + z * O.sb + er * O.si + ec * O.sk;
+        Run<T, N> out;
+#pragma unroll
+        for (int i = 0; i < N; ++i) out.v[i] = from_float<T>((turn ? y[i] : v[i]) * kDown);
+        if (left >= N && (turn || O.sk == 1)) {
+            *reinterpret_cast<Run<T, N> *>(o) = out;
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (i < left) o[i * (turn ? O.si : O.sk)] = out.v[i];
+        }
+    }
+}
+
 // Square tiles (the symmetric products mirror them).
 typedef PanelShape<2, 4, 4, 2, 2> Big;
 typedef PanelShape<2, 2, 2, 2, 2> Mid;
@@ -467,22 +613,43 @@ template <int STEP> int64_t tile_count(int64_t edge, int64_t m, int64_t n)
     return STEP == kGram || STEP == kPoly ? tm * (tm + 1) / 2 : tm * tn;
 }
 
-// The tiles of one product: 0 Big, 1 Mid, 2 Small, and how they are shared.
+// The tiles of one product: 0 Big, 1 Mid, 2 Small, 3 a short product's blocks,
+// and how they are shared.
 struct Choice {
     int shape;
     PanelCut cut;
     int64_t slotBytes;
 };
+// blocks of a short product; they write the padding of the last panels too
+template <int KIND, int STEP> int64_t short_count(int64_t m, int64_t n)
+{
+    return tile_count<STEP>(kShortE, padded<KIND>((int)m), padded<KIND>((int)n));
+}
+// Its price beside panel_cut's, which leave out a launch's fixed time: that is
+// 2 us shorter here, and a wavefront's panels in flight together take 1.8.  us
+// as tiles of 64 x 64 and here: 160 x 160 floats, S 6.0 / 4.2, update 6.9 / 4.4;
+// 517 x 1000, S 11.7 / 6.8, S^2 9.4 / 6.0, bf16 7.3 / 5.7 and 6.9 / 4.8; 256 x
+// 2048, S 12.1 / 9.9.  With more blocks than CUs the tiles' fewer loads win: S
+// of 1024 x 1024 11.4 / 15.6, the update of 517 x 1000 12.1 / 14.2.
+PanelCut short_cut(int64_t blocks, int64_t panels)
+{
+    PanelCut c;
+    c.full = c.blocks = blocks;
+    const int64_t together = kShortWaves * kShortDeep;
+    if (blocks <= kPanelCus) c.us = 1.8 * (double)((panels + together - 1) / together) - 2.0;
+    return c;
+}
 template <int KIND, int STEP> Choice choose(int64_t batch, int64_t m, int64_t n, int64_t panels)
 {
-    const PanelCut c[3] = {
+    const PanelCut c[4] = {
         panel_cut<Big>(KIND, batch * tile_count<STEP>(Big::BM, m, n), panels),
         panel_cut<Mid>(KIND, batch * tile_count<STEP>(Mid::BM, m, n), panels),
-        panel_cut<Small>(KIND, batch * tile_count<STEP>(Small::BM, m, n), panels)};
+        panel_cut<Small>(KIND, batch * tile_count<STEP>(Small::BM, m, n), panels),
+        short_cut(batch * short_count<KIND, STEP>(m, n), panels)};
     int s = 0;
-    for (int i = 1; i < 3; ++i)
+    for (int i = 1; i < 4; ++i)
         if (c[i].us < c[s].us) s = i;
-    const int64_t tile[3] = {Big::TILE, Mid::TILE, Small::TILE};
+    const int64_t tile[4] = {Big::TILE, Mid::TILE, Small::TILE, 0};
     return {s, c[s], c[s].shared() * c[s].slices * tile[s] * 4};
 }
 
@@ -509,12 +676,29 @@ hipError_t product_launch(const ProductArgs &d, const PanelCut &c, const Workspa
 }
 
 template <int KIND, int STEP, typename T>
+hipError_t short_launch(const ProductArgs &d, const PanelCut &c, const Stack<T> &O, int64_t batch,
+                        hipStream_t stream)
+{
+    constexpr auto k = orth_short_kernel<KIND, STEP, T>;
+    const hipError_t e = allow_dynamic_lds<k>(kShortLds);
+    if (e != hipSuccess) return e;
+    PanelGrid g;
+    if (!panel_grid(g, batch, (padded<KIND>(d.m) + kShortE - 1) / kShortE,
+                    (padded<KIND>(d.n) + kShortE - 1) / kShortE, short_count<KIND, STEP>(d.m, d.n), c,
+                    d.panels, nullptr, nullptr))
+        return hipErrorInvalidValue;
+    hipLaunchKernelGGL(k, dim3((unsigned)c.blocks), dim3(kShortThreads), kShortLds, stream, d, g, O);
+    return hipGetLastError();
+}
+
+template <int KIND, int STEP, typename T>
 hipError_t product(const ProductArgs &d, const Choice &c, const Workspace &w, const Stack<T> &O,
                    int64_t batch, hipStream_t stream)
 {
     if (c.shape == 0) return product_launch<KIND, STEP, Big, T>(d, c.cut, w, O, batch, stream);
     if (c.shape == 1) return product_launch<KIND, STEP, Mid, T>(d, c.cut, w, O, batch, stream);
-    return product_launch<KIND, STEP, Small, T>(d, c.cut, w, O, batch, stream);
+    if (c.shape == 2) return product_launch<KIND, STEP, Small, T>(d, c.cut, w, O, batch, stream);
+    return short_launch<KIND, STEP, T>(d, c.cut, O, batch, stream);
 }
 
 struct Problem {
@@ -530,10 +714,9 @@ struct Problem {
 // A matrix whose X, X^T and S fit the 160 KB of a CU goes through all steps in
 // one workgroup: no launch and no memory between them.  us so and by launches
 // (in a graph, without the host's time for 17 launches): 12 x 64 x 128 floats
-// 30 / 74, bf16 21 / 61; 16 x 128 x 128 floats 87 / 88, bf16 42 / 69; 600 x 64 x
-// 128 floats 94 / 229; 32 x 1000 floats 92 / 91, bf16 53 / 69.  Bound: the
-// latency of each step's three products, of the LDS accesses between them and
-// of their barriers.
+// 30 / 58, bf16 21 / 56; 16 x 128 x 128 bf16 42 / 55; 32 x 1000 bf16 53 / 57; 600 x
+// 64 x 128 floats 94 / 227.  Bound: the latency of each step's three products,
+// of the LDS accesses between them and of their barriers.
 //
 // Rows are padded to 32 (zeros, which stay zeros) and lie 16 bytes more than
 // their length apart, so that sixteen rows' pieces fall on different banks.  A

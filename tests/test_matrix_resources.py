@@ -12,7 +12,7 @@ from test_kernel_resources import LLVM, code_objects
 
 KERNELS = ["mx_quantize_kernel", "mx_dequantize_kernel", "mx_tile_kernel", "mx_few_kernel",
            "orth_norm_kernel", "orth_start_kernel", "orth_copy_kernel", "orth_product_kernel",
-           "orth_small_kernel"]
+           "orth_short_kernel", "orth_small_kernel"]
 
 
 @pytest.fixture(scope="module")
