@@ -460,14 +460,14 @@ __global__ __launch_bounds__(S::THREADS) void orth_product_kernel(ProductArgs d,
 //
 // A product of few tiles is a chain of latencies, not of work.  Here a
 // workgroup takes a block of 32 x 32 results and each of its eight wavefronts
-// every eighth panel, through LDS of its own: all of a wavefront's loads are in
-// flight together, and no barrier comes before the eight partial results are
-// summed, in wavefront order, through LDS.
+// every eighth panel, through LDS of its own: eight panels' loads are in flight
+// together, and no barrier comes before the eight partial results are summed,
+// in wavefront order, through LDS.  (Two panels a wavefront in flight leave
+// room for one workgroup on a CU instead of two: 256 x 2048, S 9.9 us for 8.4.)
 
 constexpr int kShortWaves = 8;
-constexpr int kShortDeep = 2;   // panels of a wavefront in flight
 constexpr int kShortE = 32, kShortThreads = 64 * kShortWaves;
-constexpr int kShortOwn = kShortDeep * 2 * kShortE * 128;   // LDS of a wavefront
+constexpr int kShortOwn = 2 * kShortE * 128;   // LDS of a wavefront
 constexpr int kShortPitch = kShortE + 2, kShortAcross = kShortE + 1;
 constexpr int kShortLds = kShortWaves * kShortOwn + kShortE * kShortAcross * 4;
 
@@ -476,7 +476,7 @@ __global__ __launch_bounds__(kShortThreads) void orth_short_kernel(ProductArgs d
                                                                    Stack<T> O)
 {
     extern __shared__ __attribute__((aligned(256))) char dyn_lds[];
-    constexpr int E = kShortE, W = kShortWaves, DEEP = kShortDeep, N = E * E / kShortThreads;
+    constexpr int E = kShortE, W = kShortWaves, N = E * E / kShortThreads;
     constexpr bool kSymmetric = STEP == kGram || STEP == kPoly;
     const int tid = (int)threadIdx.x, lane = tid & 63, r = tid & 31, h = (tid >> 5) & 1;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -510,39 +510,29 @@ __global__ __launch_bounds__(kShortThreads) void orth_short_kernel(ProductArgs d
     f16v acc;
 #pragma unroll
     for (int e = 0; e < 16; ++e) acc[e] = 0.0f;
-    for (int t0 = wave; t0 < d.panels; t0 += W * DEEP) {
+    for (int t = wave; t < d.panels; t += W) {
 #pragma unroll
-        for (int u = 0; u < DEEP; ++u) {
-            const int t = t0 + u * W;
-            if (t < d.panels) {
-#pragma unroll
-                for (int v = 0; v < 8; ++v)
-                    __builtin_amdgcn_global_load_lds(
-                        (matrix_global *)(from[v] + (int64_t)t * (v < 4 ? d.m : d.n) * 128),
-                        (matrix_lds *)(own + (u * 8 + v) * 1024), 16, 0, 0);
-            }
-        }
+        for (int u = 0; u < 8; ++u)
+            __builtin_amdgcn_global_load_lds(
+                (matrix_global *)(from[u] + (int64_t)t * (u < 4 ? d.m : d.n) * 128),
+                (matrix_lds *)(own + u * 1024), 16, 0, 0);
         __builtin_amdgcn_s_waitcnt(7 << 4 | 15 << 8);   // vmcnt 0
         asm volatile("" ::: "memory");
+        i4 a[4], b[4];
 #pragma unroll
-        for (int u = 0; u < DEEP; ++u) {
-            if (t0 + u * W >= d.panels) break;
-            i4 a[4], b[4];
+        for (int s = 0; s < 4; ++s) {
+            const int place = (4 * h + s) ^ (r >> 1 & 7);
+            a[s] = *reinterpret_cast<const i4 *>(own + r * 128 + place * 16);
+            b[s] = *reinterpret_cast<const i4 *>(own + 4096 + r * 128 + place * 16);
+        }
 #pragma unroll
-            for (int s = 0; s < 4; ++s) {
-                const int place = (4 * h + s) ^ (r >> 1 & 7);
-                a[s] = *reinterpret_cast<const i4 *>(own + u * 8192 + r * 128 + place * 16);
-                b[s] = *reinterpret_cast<const i4 *>(own + u * 8192 + 4096 + r * 128 + place * 16);
-            }
-#pragma unroll
-            for (int s = 0; s < 4; ++s) {
-                if constexpr (KIND == kPanelHalf) {
-                    acc = mfma_half(a[s], b[s], acc);
-                } else if (s % 2 == 0) {
-                    acc = mfma_half(a[s], b[s], acc);
-                    acc = mfma_half(a[s], b[s + 1], acc);
-                    acc = mfma_half(a[s + 1], b[s], acc);
-                }
+        for (int s = 0; s < 4; ++s) {
+            if constexpr (KIND == kPanelHalf) {
+                acc = mfma_half(a[s], b[s], acc);
+            } else if (s % 2 == 0) {
+                acc = mfma_half(a[s], b[s], acc);
+                acc = mfma_half(a[s], b[s + 1], acc);
+                acc = mfma_half(a[s + 1], b[s], acc);
             }
         }
         __builtin_amdgcn_s_waitcnt(0);   // own LDS has been read
@@ -626,17 +616,18 @@ template <int KIND, int STEP> int64_t short_count(int64_t m, int64_t n)
     return tile_count<STEP>(kShortE, padded<KIND>((int)m), padded<KIND>((int)n));
 }
 // Its price beside panel_cut's, which leave out a launch's fixed time: that is
-// 2 us shorter here, and a wavefront's panels in flight together take 1.8.  us
-// as tiles of 64 x 64 and here: 160 x 160 floats, S 6.0 / 4.2, update 6.9 / 4.4;
-// 517 x 1000, S 11.7 / 6.8, S^2 9.4 / 6.0, bf16 7.3 / 5.7 and 6.9 / 4.8; 256 x
-// 2048, S 12.1 / 9.9.  With more blocks than CUs the tiles' fewer loads win: S
-// of 1024 x 1024 11.4 / 15.6, the update of 517 x 1000 12.1 / 14.2.
+// 1.3 us shorter here, and a wavefront's panel takes 0.65, with two workgroups
+// on a CU 1.6.  us as tiles of 64 x 64 and here: 160 x 160 floats, S 5.8 / 4.2,
+// update 6.9 / 4.2; 517 x 1000, S 11.4 / 7.1, S^2 9.5 / 5.2, bf16 7.3 / 5.1 and
+// 6.8 / 4.8; 256 x 2048, S 11.3 / 8.4, update 8.7 / 8.1; 768 x 768, S 10.2 / 8.5.
+// With more blocks than are resident the tiles' fewer loads win: S of 1024 x
+// 1024 11.2 / 12.1, the update of 517 x 1000 11.6 / 12.0 and bf16 8.6 / 9.4.
 PanelCut short_cut(int64_t blocks, int64_t panels)
 {
     PanelCut c;
     c.full = c.blocks = blocks;
-    const int64_t together = kShortWaves * kShortDeep;
-    if (blocks <= kPanelCus) c.us = 1.8 * (double)((panels + together - 1) / together) - 2.0;
+    const double each = (double)((panels + kShortWaves - 1) / kShortWaves);
+    if (blocks <= 2 * kPanelCus) c.us = (blocks <= kPanelCus ? 0.65 : 1.6) * each - 1.3;
     return c;
 }
 template <int KIND, int STEP> Choice choose(int64_t batch, int64_t m, int64_t n, int64_t panels)
