@@ -13,7 +13,7 @@
 // panels alone, without reading the addend and writing both orientations, 1.2),
 // the norm 13.5 and the start 41-47.  bf16: 1.64 ms; 102, 104 and 150.
 // Mid-sized matrices are chains of launches: 15 products of 5 to 8 us at 517 x
-// 1000 (bf16, 104 us in all), of which three are the launch and the rest loads,
+// 1000 (bf16, 102 us in all), of which three are the launch and the rest loads,
 // a short K and the stores, each waiting for the one before.
 //
 // Numbers.  |X| <= 1 at the start and every singular value stays below 3
@@ -22,9 +22,12 @@
 // entries down to 2^-26 normal.  A float matrix is held as two halves, hi +
 // lo (22 bits; products in panel.hpp, sums in 32 bits): the result is as close
 // to the 64-bit one as that of products in 32 bits (1.5e-6 of its norm for
-// both at 512 x 517) at a fifth of their price.  For bf16 one half is held:
-// 1.3e-3 of the norm, below the 1.7e-3 that rounding the result to bf16
-// costs anyway.
+// both at 512 x 517) at a fifth of their price.  For bf16 one half is held
+// where the shorter side is above 256: 1.1e-3 to 1.5e-3 of the norm, below the
+// 1.7e-3 that rounding the result to bf16 costs anyway.  With fewer rows fewer
+// roundings average out (2.9e-3 at 16 x 64 and 3.6e-3 at 16 x 4000 with the result's own,
+// up to 4.7e-3), while latency bounds the time: two halves there, 64 x 64 in 25 us
+// instead of 17, 128 x 128 in 56 instead of 42.
 //
 // Every product has K along the rows of both operands: S from X, S^2 from S
 // (symmetric), B X from B and X^T.  So X is kept in both orientations, and
@@ -41,6 +44,7 @@ namespace gett {
 namespace {
 
 constexpr float kUp = 4096.0f, kDown = 1.0f / 4096.0f;   // halves hold 2^12 x
+constexpr int kTwoPartRows = 256;   // bf16: two parts up to here
 constexpr int kNormThreads = 256;
 constexpr int kNormBlocks = 1024;   // at most, per matrix; one partial sum each
 
@@ -705,8 +709,7 @@ struct Problem {
 // A matrix whose X, X^T and S fit the 160 KB of a CU goes through all steps in
 // one workgroup: no launch and no memory between them.  us so and by launches
 // (in a graph, without the host's time for 17 launches): 12 x 64 x 128 floats
-// 30 / 58, bf16 21 / 56; 16 x 128 x 128 bf16 42 / 55; 32 x 1000 bf16 53 / 57; 600 x
-// 64 x 128 floats 94 / 227.  Bound: the latency of each step's three products,
+// 30 / 58, 64 x 64 25 / 55, 600 x 64 x 128 94 / 227.  Bound: the latency of each step's three products,
 // of the LDS accesses between them and of their barriers.
 //
 // Rows are padded to 32 (zeros, which stay zeros) and lie 16 bytes more than
@@ -720,47 +723,44 @@ constexpr int kSmallWaves = 8;
 constexpr int kSmallBlocks = 2;
 constexpr int kSmallLds = 160 * 1024 - 256;
 
-template <int KIND> __host__ __device__ constexpr int number_bytes() { return KIND == kPanelSplit ? 4 : 2; }
-template <int KIND> __host__ __device__ inline int small_pitch(int k) { return k * number_bytes<KIND>() + 16; }
-template <int KIND> int64_t small_lds(int64_t m, int64_t n)
+__host__ __device__ inline int small_pitch(int k) { return k * 4 + 16; }
+inline int64_t small_lds(int64_t m, int64_t n)
 {
     const int64_t mp = (m + 31) / 32 * 32, np = (n + 31) / 32 * 32;
-    return mp * small_pitch<KIND>((int)np) + (np + mp) * small_pitch<KIND>((int)mp);
+    return mp * small_pitch((int)np) + (np + mp) * small_pitch((int)mp);
 }
-template <int KIND> bool small_fits(int64_t m, int64_t n)
+inline bool small_fits(int64_t m, int64_t n)
 {
     const int64_t mb = (m + 31) / 32;
     return m <= 1024 && n <= 4096 && mb * mb <= kSmallWaves * kSmallBlocks &&
-           small_lds<KIND>(m, n) <= kSmallLds;
+           small_lds(m, n) <= kSmallLds;
 }
 
 // the byte of number k in its row
-template <int KIND> __device__ __forceinline__ int small_at(int k)
+__device__ __forceinline__ int small_at(int k)
 {
-    return KIND == kPanelSplit ? (k >> 3) * 32 + (k & 7) * 2 : k * 2;
+    return (k >> 3) * 32 + (k & 7) * 2;
 }
-template <int KIND> __device__ __forceinline__ f16v small_block(const char *a, const char *b, int k)
+__device__ __forceinline__ f16v small_block(const char *a, const char *b, int k)
 {
     f16v acc;
 #pragma unroll
     for (int e = 0; e < 16; ++e) acc[e] = 0.0f;
-    constexpr int GROUP = KIND == kPanelSplit ? 32 : 16;   // bytes of eight numbers
+    constexpr int GROUP = 32;   // bytes of eight numbers, their high parts first
 #pragma unroll 2
     for (int t = 0; t < k / 16; ++t) {
         const i4 ah = *reinterpret_cast<const i4 *>(a + 2 * t * GROUP);
         const i4 bh = *reinterpret_cast<const i4 *>(b + 2 * t * GROUP);
         acc = mfma_half(ah, bh, acc);
-        if constexpr (KIND == kPanelSplit) {
-            const i4 al = *reinterpret_cast<const i4 *>(a + 2 * t * GROUP + 16);
-            const i4 bl = *reinterpret_cast<const i4 *>(b + 2 * t * GROUP + 16);
-            acc = mfma_half(ah, bl, acc);
-            acc = mfma_half(al, bh, acc);
-        }
+        const i4 al = *reinterpret_cast<const i4 *>(a + 2 * t * GROUP + 16);
+        const i4 bl = *reinterpret_cast<const i4 *>(b + 2 * t * GROUP + 16);
+        acc = mfma_half(ah, bl, acc);
+        acc = mfma_half(al, bh, acc);
     }
     return acc;
 }
 
-template <typename T, int KIND>
+template <typename T>
 __global__ __launch_bounds__(kSmallWaves * 64) void orth_small_kernel(Stack<const T> G, Stack<T> O,
                                                                       int m, int n, double eps,
                                                                       int steps, float ca, float cb,
@@ -772,9 +772,9 @@ __global__ __launch_bounds__(kSmallWaves * 64) void orth_small_kernel(Stack<cons
     const int tid = (int)threadIdx.x, lane = tid & 63, r = tid & 31, h = (tid >> 5) & 1;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int mp = (m + 31) & ~31, np = (n + 31) & ~31, mb = mp / 32, nb = np / 32;
-    const int pX = small_pitch<KIND>(np), pS = small_pitch<KIND>(mp);
+    const int pX = small_pitch(np), pS = small_pitch(mp);
     char *const X = dyn_lds, *const XT = X + mp * pX, *const S = XT + np * pS;
-    constexpr int GROUP = KIND == kPanelSplit ? 32 : 16;
+    constexpr int GROUP = 32;
     const T *g = G.p + (int64_t)blockIdx.x * G.sb;
 
     // the norm, and all of the matrices zero
@@ -803,8 +803,8 @@ __global__ __launch_bounds__(kSmallWaves * 64) void orth_small_kernel(Stack<cons
         for (int i = lane; i < inner; i += 64) {
             const float v = (float)((double)to_float(g[o * so + i * si]) * scale);
             const int row = along ? o : i, col = along ? i : o;
-            store_run<KIND, 1>(X + row * pX + small_at<KIND>(col), &v);
-            store_run<KIND, 1>(XT + col * pS + small_at<KIND>(row), &v);
+            store_run<kPanelSplit, 1>(X + row * pX + small_at(col), &v);
+            store_run<kPanelSplit, 1>(XT + col * pS + small_at(row), &v);
         }
     __syncthreads();
 
@@ -813,14 +813,14 @@ __global__ __launch_bounds__(kSmallWaves * 64) void orth_small_kernel(Stack<cons
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             const float x[4] = {v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
-            store_run<KIND, 4>(M + (col0 + r) * pitch + small_at<KIND>(row0 + 8 * q + 4 * h), x);
+            store_run<kPanelSplit, 4>(M + (col0 + r) * pitch + small_at(row0 + 8 * q + 4 * h), x);
         }
     };
     for (int step = 0; step < steps; ++step) {
         const bool last = step + 1 == steps;
         for (int b = wave; b < mb * mb; b += kSmallWaves) {   // S = X X^T
             const int bi = b / mb, bj = b - bi * mb;
-            f16v v = small_block<KIND>(X + (bi * 32 + r) * pX + h * GROUP,
+            f16v v = small_block(X + (bi * 32 + r) * pX + h * GROUP,
                                        X + (bj * 32 + r) * pX + h * GROUP, np);
 #pragma unroll
             for (int e = 0; e < 16; ++e) v[e] *= kDown;
@@ -833,12 +833,12 @@ __global__ __launch_bounds__(kSmallWaves * 64) void orth_small_kernel(Stack<cons
             const int b = wave + u * kSmallWaves;
             if (b >= mb * mb) break;
             const int bi = b / mb, bj = b - bi * mb;
-            poly[u] = small_block<KIND>(S + (bi * 32 + r) * pS + h * GROUP,
+            poly[u] = small_block(S + (bi * 32 + r) * pS + h * GROUP,
                                         S + (bj * 32 + r) * pS + h * GROUP, mp);
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 float x[4];   // S is symmetric: its column r
-                load_run<KIND, 4>(S + (bj * 32 + r) * pS + small_at<KIND>(bi * 32 + 8 * q + 4 * h), x);
+                load_run<kPanelSplit, 4>(S + (bj * 32 + r) * pS + small_at(bi * 32 + 8 * q + 4 * h), x);
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
                     poly[u][4 * q + e] = cb * x[e] + cc * kDown * poly[u][4 * q + e];
@@ -858,13 +858,12 @@ __global__ __launch_bounds__(kSmallWaves * 64) void orth_small_kernel(Stack<cons
         constexpr int KS = 8;   // steps of 16 numbers: m <= 128
         for (int bj = wave; bj < nb; bj += kSmallWaves) {
             char *const column = XT + (bj * 32 + r) * pS;
-            i4 bh[KS], bl[KIND == kPanelSplit ? KS : 1];
+            i4 bh[KS], bl[KS];
 #pragma unroll
             for (int t = 0; t < KS; ++t)
                 if (t < mp / 16) {
                     bh[t] = *reinterpret_cast<const i4 *>(column + (2 * t + h) * GROUP);
-                    if constexpr (KIND == kPanelSplit)
-                        bl[t] = *reinterpret_cast<const i4 *>(column + (2 * t + h) * GROUP + 16);
+                    bl[t] = *reinterpret_cast<const i4 *>(column + (2 * t + h) * GROUP + 16);
                 }
             const int col = bj * 32 + r;
             T *const o = O.p + (int64_t)blockIdx.x * O.sb + col * O.sk;
@@ -883,16 +882,14 @@ __global__ __launch_bounds__(kSmallWaves * 64) void orth_small_kernel(Stack<cons
                     if (t < mp / 16) {
                         const i4 ah = *reinterpret_cast<const i4 *>(a + 2 * t * GROUP);
                         v = mfma_half(ah, bh[t], v);
-                        if constexpr (KIND == kPanelSplit) {
-                            const i4 al = *reinterpret_cast<const i4 *>(a + 2 * t * GROUP + 16);
-                            v = mfma_half(ah, bl[t], v);
-                            v = mfma_half(al, bh[t], v);
-                        }
+                        const i4 al = *reinterpret_cast<const i4 *>(a + 2 * t * GROUP + 16);
+                        v = mfma_half(ah, bl[t], v);
+                        v = mfma_half(al, bh[t], v);
                     }
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     float x[4];
-                    load_run<KIND, 4>(column + small_at<KIND>(bi * 32 + 8 * q + 4 * h), x);
+                    load_run<kPanelSplit, 4>(column + small_at(bi * 32 + 8 * q + 4 * h), x);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) v[4 * q + e] = ca * x[e] + kDown * v[4 * q + e];
                 }
@@ -902,7 +899,7 @@ __global__ __launch_bounds__(kSmallWaves * 64) void orth_small_kernel(Stack<cons
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
                         const float x = v[e];
-                        store_run<KIND, 1>(X + (row0 + 8 * (e >> 2) + (e & 3)) * px + small_at<KIND>(col), &x);
+                        store_run<kPanelSplit, 1>(X + (row0 + 8 * (e >> 2) + (e & 3)) * px + small_at(col), &x);
                     }
                 } else if (col < n) {
 #pragma unroll
@@ -919,18 +916,18 @@ __global__ __launch_bounds__(kSmallWaves * 64) void orth_small_kernel(Stack<cons
         for (int o = wave; o < m; o += kSmallWaves)
             for (int i = lane; i < n; i += 64) {
                 float v;
-                load_run<KIND, 1>(X + o * pX + small_at<KIND>(i), &v);
+                load_run<kPanelSplit, 1>(X + o * pX + small_at(i), &v);
                 O.p[(int64_t)blockIdx.x * O.sb + o * O.si + i * O.sk] = from_float<T>(v * kDown);
             }
 }
 
-template <typename T, int KIND>
+template <typename T>
 gett_status_t small_launch(const Problem &P, const Stack<const T> &G, const Stack<T> &O)
 {
-    constexpr auto k = orth_small_kernel<T, KIND>;
+    constexpr auto k = orth_small_kernel<T>;
     if (allow_dynamic_lds<k>(kSmallLds) != hipSuccess) return GETT_ERROR_HIP;
     hipLaunchKernelGGL(k, dim3((unsigned)P.batch), dim3(kSmallWaves * 64),
-                       (size_t)small_lds<KIND>(P.m, P.n), P.stream, G, O, P.m, P.n, P.eps, P.steps,
+                       (size_t)small_lds(P.m, P.n), P.stream, G, O, P.m, P.n, P.eps, P.steps,
                        (float)P.a, (float)P.b, (float)P.c);
     return hipGetLastError() == hipSuccess ? GETT_SUCCESS : GETT_ERROR_HIP;
 }
@@ -940,7 +937,8 @@ template <typename T, int KIND>
 gett_status_t orthogonalize_typed(const Problem &P, Stack<const T> G, Stack<T> O)
 {
     const int m = P.m, n = P.n;
-    if (small_fits<KIND>(m, n)) return small_launch<T, KIND>(P, G, O);
+    if constexpr (KIND == kPanelSplit)   // (one part means more rows than fit)
+        if (small_fits(m, n)) return small_launch<T>(P, G, O);
     const int64_t panelsX = panel_count<KIND>(n), panelsS = panel_count<KIND>(m);
     const int64_t X = m * panelsX * 128, XT = n * panelsS * 128, SS = m * panelsS * 128;
     // the norm reads along the smaller stride
@@ -1132,9 +1130,10 @@ gett_status_t gett_orthogonalize(gett_dtype_t dtype, int64_t batch, int64_t rows
         return orthogonalize_typed<_Float16, kPanelSplit>(
             P, {static_cast<const _Float16 *>(G), stride_batch, stride_row, stride_col},
             {static_cast<_Float16 *>(O), ostride_batch, ostride_row, ostride_col});
-    return orthogonalize_typed<bf16, kPanelHalf>(
-        P, {static_cast<const bf16 *>(G), stride_batch, stride_row, stride_col},
-        {static_cast<bf16 *>(O), ostride_batch, ostride_row, ostride_col});
+    const Stack<const bf16> g = {static_cast<const bf16 *>(G), stride_batch, stride_row, stride_col};
+    const Stack<bf16> o = {static_cast<bf16 *>(O), ostride_batch, ostride_row, ostride_col};
+    return P.m <= kTwoPartRows ? orthogonalize_typed<bf16, kPanelSplit>(P, g, o)
+                               : orthogonalize_typed<bf16, kPanelHalf>(P, g, o);
 }
 
 }  // extern "C"

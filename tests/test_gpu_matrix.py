@@ -598,3 +598,14 @@ def test_orthogonalize_many_tiles(gpu, shape, dtype):
     rng = np.random.default_rng(sum(shape))
     G = stack(rng, shape, dtype)
     orth_close(g.orthogonalize(G, steps=2), G, dtype, steps=2)
+
+
+@pytest.mark.parametrize("shape", [(16, 16), (4000, 16), (64, 64), (130, 200), (256, 700)])
+def test_orthogonalize_few_rows_in_two_parts(gpu, shape):
+    """bf16 with a short side of 256 at most: two parts, so the result's own
+    rounding (half a unit of each entry) is all that is left beside them."""
+    rng = np.random.default_rng(sum(shape))
+    G = stack(rng, shape, "bfloat16")
+    got, ref = host(g.orthogonalize(G)), newton_schulz(host(G), 5, MUON, 1e-7)
+    err = np.linalg.norm(got - ref) / np.linalg.norm(ref)
+    assert err <= 12 * 5 * 2.0 ** -22 + HALF_ULP["bfloat16"]
