@@ -25,9 +25,9 @@
 // both at 512 x 517) at a fifth of their price.  For bf16 one half is held
 // where the shorter side is above 256: 1.1e-3 to 1.5e-3 of the norm, below the
 // 1.7e-3 that rounding the result to bf16 costs anyway.  With fewer rows fewer
-// roundings average out (2.9e-3 at 16 x 64 and 3.6e-3 at 16 x 4000 with the result's own,
-// up to 4.7e-3), while latency bounds the time: two halves there, 64 x 64 in 25 us
-// instead of 17, 128 x 128 in 56 instead of 42.
+// roundings average out (with the result's own 2.9e-3 at 16 x 64, 3.6e-3 at 16
+// x 4000, 4.7e-3 at 16 x 16), while latency bounds the time: two halves there,
+// 64 x 64 in 25 us instead of 17, 128 x 128 in 56 instead of 42.
 //
 // Every product has K along the rows of both operands: S from X, S^2 from S
 // (symmetric), B X from B and X^T.  So X is kept in both orientations, and
