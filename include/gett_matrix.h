@@ -191,10 +191,8 @@ gett_status_t gett_mx_linear_grad(int64_t m, int64_t n, int64_t k, gett_dtype_t 
  *   steps     0 to 1000.
  *
  * O may be G itself (same pointer and strides); otherwise they must not
- * overlap.  Products are formed from 16-bit parts with sums in 32 bits: two
- * parts (22 bits) for GETT_FLOAT32 and GETT_FLOAT16 and, where rows or cols are
- * 256 at most, GETT_BFLOAT16; one part (11 bits) for larger matrices of
- * GETT_BFLOAT16, whose own 8 bits are coarser.  A NaN or an infinity in a
+ * overlap.  Iterates are held in two 16-bit parts (22 bits) for every dtype, with
+ * sums in 32 bits, and the result is rounded once.  A NaN or an infinity in a
  * matrix makes that matrix NaN.  Errors: GETT_ERROR_INVALID_VALUE (unknown
  * dtype, negative extent or steps, stride < 1, eps negative or NaN, a
  * coefficient that is not finite, null or misaligned pointer, overlap),

@@ -8,26 +8,22 @@
 // 2 m^2 n operations per step instead of 2 m^2 n + 2 m^3 + 2 m^2 n, each three
 // MFMA operations where numbers are held in two parts.
 //
-// 4096 x 4096, five steps, float: 3.74 ms; a step's three products 200-214,
+// 4096 x 4096, five steps: 3.74 ms; a step's three products 200-214,
 // 200-215 and 363-394 us (1.0 to 1.1 PFLOP/s of MFMA operations; the update's
 // panels alone, without reading the addend and writing both orientations, 1.2),
-// the norm 13.5 and the start 41-47.  bf16: 1.64 ms; 102, 104 and 150.
-// Mid-sized matrices are chains of launches: 15 products of 5 to 8 us at 517 x
-// 1000 (bf16, 102 us in all), of which three are the launch and the rest loads,
-// a short K and the stores, each waiting for the one before.
+// the norm 13.5 and the start 41-47.
+// Mid-sized matrices are chains of launches, each a load latency, a short K and
+// the stores, waiting for the one before.
 //
 // Numbers.  |X| <= 1 at the start and every singular value stays below 3
 // (gett_orthogonalize refuses other polynomials), so all entries of X, S and
 // B are below 15 and fit a half after multiplication by 2^12, which keeps
-// entries down to 2^-26 normal.  A float matrix is held as two halves, hi +
-// lo (22 bits; products in panel.hpp, sums in 32 bits): the result is as close
-// to the 64-bit one as that of products in 32 bits (1.5e-6 of its norm for
-// both at 512 x 517) at a fifth of their price.  For bf16 one half is held
-// where the shorter side is above 256: 1.1e-3 to 1.5e-3 of the norm, below the
-// 1.7e-3 that rounding the result to bf16 costs anyway.  With fewer rows fewer
-// roundings average out (with the result's own 2.9e-3 at 16 x 64, 3.6e-3 at 16
-// x 4000, 4.7e-3 at 16 x 16), while latency bounds the time: two halves there,
-// 64 x 64 in 25 us instead of 17, 128 x 128 in 56 instead of 42.
+// entries down to 2^-26 normal.  A matrix is held as two halves, hi + lo (22
+// bits; products in panel.hpp, sums in 32 bits), for every type: the result is
+// as close to the 64-bit one as that of products in 32 bits (1.5e-6 of its norm
+// for both at 512 x 517).  One half would not do for bf16 either: its fifteen
+// roundings leave 1.1e-3 to 2.9e-3 of the norm beside the 1.7e-3 that rounding
+// the result costs.
 //
 // Every product has K along the rows of both operands: S from X, S^2 from S
 // (symmetric), B X from B and X^T.  So X is kept in both orientations, and
@@ -44,61 +40,44 @@ namespace gett {
 namespace {
 
 constexpr float kUp = 4096.0f, kDown = 1.0f / 4096.0f;   // halves hold 2^12 x
-constexpr int kTwoPartRows = 256;   // bf16: two parts up to here
 constexpr int kNormThreads = 256;
 constexpr int kNormBlocks = 1024;   // at most, per matrix; one partial sum each
 
 // ----------------------------------------------------------------- storage ---
 
-// Numbers of one panel: Half 64 halves; Split 32, the high parts of eight
-// numbers and then their low parts (slab 0 takes the even pieces of a panel,
-// slab 1 the odd ones).
-template <int KIND> __host__ __device__ constexpr int panel_elements() { return KIND == kPanelSplit ? 32 : 64; }
-template <int KIND> inline int64_t panel_count(int64_t k)
-{
-    const int e = panel_elements<KIND>();
-    return (k + e - 1) / e;
-}
+// Numbers of one panel: the high parts of eight and then their low parts (slab
+// 0 takes the even pieces of a panel, slab 1 the odd ones).
+constexpr int kNumbers = 32;
+__host__ __device__ inline int64_t panel_count(int64_t k) { return (k + kNumbers - 1) / kNumbers; }
 // columns of a row, padding included
-template <int KIND> __host__ __device__ inline int padded(int k)
-{
-    const int e = panel_elements<KIND>();
-    return (k + e - 1) / e * e;
-}
+__host__ __device__ inline int padded(int k) { return (int)panel_count(k) * kNumbers; }
+// the byte of number k in its panel
+__host__ __device__ constexpr int in_panel(int k) { return (k >> 3) * 32 + (k & 7) * 2; }
 // the byte of column k of a row in a matrix of `rows` rows
-template <int KIND> __device__ __forceinline__ int64_t at(int rows, int row, int k)
+__device__ __forceinline__ int64_t at(int rows, int row, int k)
 {
-    const int e = panel_elements<KIND>(), in = k % e;
-    return ((int64_t)(k / e) * rows + row) * 128 +
-           (KIND == kPanelSplit ? (in >> 3) * 32 + (in & 7) * 2 : in * 2);
+    return ((int64_t)(k / kNumbers) * rows + row) * 128 + in_panel(k % kNumbers);
 }
 
 // N neighbours (N divides 8 and the column): held values are 2^12 x
-template <int KIND, int N> __device__ __forceinline__ void store_run(char *p, const float *v)
+template <int N> __device__ __forceinline__ void store_run(char *p, const float *v)
 {
     typedef _Float16 vec __attribute__((ext_vector_type(N)));
-    vec hi;
+    vec hi, lo;
 #pragma unroll
     for (int i = 0; i < N; ++i) hi[i] = (_Float16)v[i];
-    *reinterpret_cast<vec *>(p) = hi;
-    if constexpr (KIND == kPanelSplit) {
-        vec lo;
 #pragma unroll
-        for (int i = 0; i < N; ++i) lo[i] = (_Float16)(v[i] - (float)hi[i]);
-        *reinterpret_cast<vec *>(p + 16) = lo;
-    }
+    for (int i = 0; i < N; ++i) lo[i] = (_Float16)(v[i] - (float)hi[i]);
+    *reinterpret_cast<vec *>(p) = hi;
+    *reinterpret_cast<vec *>(p + 16) = lo;
 }
-template <int KIND, int N> __device__ __forceinline__ void load_run(const char *p, float *v)
+template <int N> __device__ __forceinline__ void load_run(const char *p, float *v)
 {
     typedef _Float16 vec __attribute__((ext_vector_type(N)));
     const vec hi = *reinterpret_cast<const vec *>(p);
+    const vec lo = *reinterpret_cast<const vec *>(p + 16);
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = (float)hi[i];
-    if constexpr (KIND == kPanelSplit) {
-        const vec lo = *reinterpret_cast<const vec *>(p + 16);
-#pragma unroll
-        for (int i = 0; i < N; ++i) v[i] += (float)lo[i];
-    }
+    for (int i = 0; i < N; ++i) v[i] = (float)hi[i] + (float)lo[i];
 }
 
 // ------------------------------------------------------------ norm and start ---
@@ -157,7 +136,7 @@ __global__ __launch_bounds__(kNormThreads) void orth_norm_kernel(Stack<const T> 
 
 // X_0 in both orientations, a 64 x 64 tile a workgroup
 constexpr int kStart = 64;
-template <typename T, int KIND>
+template <typename T>
 __global__ __launch_bounds__(kNormThreads) void orth_start_kernel(
     Stack<const T> G, int m, int n, int tiles, Recip tilesInv, int tilesN, Recip tilesNInv,
     const double *partial, int blocks, double eps, char *X, char *XT, int64_t stackX, int64_t stackXT)
@@ -197,21 +176,21 @@ __global__ __launch_bounds__(kNormThreads) void orth_start_kernel(
         const int e = u * kNormThreads + tid;
         const int a = e / (kStart / 8), c = e % (kStart / 8) * 8;
         float v[8];
-        if (i0 + a < m && k0 + c < padded<KIND>(n)) {
+        if (i0 + a < m && k0 + c < padded(n)) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = tile[a][c + i];
-            store_run<KIND, 8>(X + z * stackX + at<KIND>(m, i0 + a, k0 + c), v);
+            store_run<8>(X + z * stackX + at(m, i0 + a, k0 + c), v);
         }
-        if (k0 + a < n && i0 + c < padded<KIND>(m)) {
+        if (k0 + a < n && i0 + c < padded(m)) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = tile[c + i][a];
-            store_run<KIND, 8>(XT + z * stackXT + at<KIND>(n, k0 + a, i0 + c), v);
+            store_run<8>(XT + z * stackXT + at(n, k0 + a, i0 + c), v);
         }
     }
 }
 
 // O = X_0 (no steps)
-template <typename T, int KIND>
+template <typename T>
 __global__ __launch_bounds__(256) void orth_copy_kernel(const char *X, int64_t stackX, int m, int n,
                                                         Stack<T> O, int64_t total)
 {
@@ -220,7 +199,7 @@ __global__ __launch_bounds__(256) void orth_copy_kernel(const char *X, int64_t s
     const int64_t z = e / ((int64_t)m * n), rest = e % ((int64_t)m * n);
     const int i = (int)(rest / n), k = (int)(rest % n);
     float v;
-    load_run<KIND, 1>(X + z * stackX + at<KIND>(m, i, k), &v);
+    load_run<1>(X + z * stackX + at(m, i, k), &v);
     O.p[z * O.sb + i * O.si + k * O.sk] = from_float<T>(v * kDown);
 }
 
@@ -239,10 +218,10 @@ struct ProductArgs {
 };
 
 // Passes in which a tile's panels, [panel][row][128 bytes], go through LDS.
-template <int KIND, typename S, bool ACROSS> constexpr int image_passes()
+template <typename S, bool ACROSS> constexpr int image_passes()
 {
     constexpr int ROWS = ACROSS ? S::BN : S::BM, COLS = ACROSS ? S::BM : S::BN;
-    constexpr int FIT = S::lds(KIND) / (ROWS * 128), ALL = COLS / panel_elements<KIND>();
+    constexpr int FIT = S::lds(kPanelSplit) / (ROWS * 128), ALL = COLS / kNumbers;
     return FIT < ALL ? ALL / FIT : 1;
 }
 
@@ -253,12 +232,13 @@ template <typename S> constexpr bool kAddendEarly = S::BM == 64;
 // Starts the loads of a tile's panels of a matrix of `rows` rows and `panels`
 // panels, as the LDS image of pass `pass`.  Outside the matrix any of its
 // values will do: what becomes of them is replaced by zeros.
-template <int KIND, typename S>
-__device__ __forceinline__ void load_panels(const Panel<KIND, S> &p, char *image, const char *from,
-                                            int rows, int panels, int row0, int col0, int pass)
+template <typename S>
+__device__ __forceinline__ void load_panels(const Panel<kPanelSplit, S> &p, char *image,
+                                            const char *from, int rows, int panels, int row0,
+                                            int col0, int pass)
 {
-    constexpr int E = panel_elements<KIND>();
-    constexpr int PP = S::BN / E / (kAddendEarly<S> ? 1 : image_passes<KIND, S, false>());
+    constexpr int E = kNumbers;
+    constexpr int PP = S::BN / E / (kAddendEarly<S> ? 1 : image_passes<S, false>());
     const int lane = (int)threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
 #pragma unroll
@@ -279,14 +259,14 @@ __device__ __forceinline__ void load_panels(const Panel<KIND, S> &p, char *image
 // `row0` / `col0` being the tile's first row and column there.  The lanes'
 // runs are a few elements of many rows, so they are put in order in LDS, the
 // panels' image: every store of a wavefront then covers 1 KB.
-template <int KIND, typename S, bool ACROSS>
-__device__ __forceinline__ void store_panels(Panel<KIND, S> &p, char *lds, char *out,
+template <typename S, bool ACROSS>
+__device__ __forceinline__ void store_panels(Panel<kPanelSplit, S> &p, char *lds, char *out,
                                              int rows, int panels, int row0, int col0)
 {
-    constexpr int E = panel_elements<KIND>();
+    constexpr int E = kNumbers;
     constexpr int ROWS = ACROSS ? S::BN : S::BM, COLS = ACROSS ? S::BM : S::BN;
     constexpr int FR = ACROSS ? S::FN : S::FM, FC = ACROSS ? S::FM : S::FN;   // runs of a lane
-    constexpr int ALL = COLS / E, PP = ALL / image_passes<KIND, S, ACROSS>();
+    constexpr int ALL = COLS / E, PP = ALL / image_passes<S, ACROSS>();
     static_assert(ALL % PP == 0 && (PP * E) % (32 * FC) == 0, "a wavefront's columns in one pass");
     const int tid = (int)threadIdx.x;
     const int mine = (ACROSS ? p.wm : p.wn) * 32 * FC;   // this wavefront's first column
@@ -307,7 +287,7 @@ __device__ __forceinline__ void store_panels(Panel<KIND, S> &p, char *lds, char 
                     const int row = ACROSS ? p.col(f) : p.row(f, e);
                     const int col = (ACROSS ? p.row(0, e) : p.col(0)) - pass * PP * E;
                     const int in = col % E;
-                    const int byte = KIND == kPanelSplit ? (in >> 3) * 32 + (in & 7) * 2 : in * 2;
+                    const int byte = in_panel(in);
                     // pieces of a row lie by an exclusive or, so that the lanes'
                     // rows, a power of two apart, fall on different banks
                     const int x = row / FR & 7;
@@ -321,9 +301,8 @@ __device__ __forceinline__ void store_panels(Panel<KIND, S> &p, char *lds, char 
                         lo[c] = (_Float16)(v - (float)hi[c]);
                     }
                     *reinterpret_cast<vec *>(at) = hi;
-                    if constexpr (KIND == kPanelSplit)
-                        *reinterpret_cast<vec *>(lds + (col / E * ROWS + row) * 128 +
-                                                 (((byte >> 4) + 1 ^ x) << 4) + (byte & 15)) = lo;
+                    *reinterpret_cast<vec *>(lds + (col / E * ROWS + row) * 128 +
+                                             (((byte >> 4) + 1 ^ x) << 4) + (byte & 15)) = lo;
                 }
                 __builtin_amdgcn_sched_barrier(0);   // no registers for many addresses
             }
@@ -340,7 +319,7 @@ __device__ __forceinline__ void store_panels(Panel<KIND, S> &p, char *lds, char 
     }
 }
 
-template <int KIND, int STEP, typename S, typename T>
+template <int STEP, typename S, typename T>
 __global__ __launch_bounds__(S::THREADS) void orth_product_kernel(ProductArgs d, PanelGrid grid,
                                                                   Stack<T> O)
 {
@@ -356,26 +335,26 @@ __global__ __launch_bounds__(S::THREADS) void orth_product_kernel(ProductArgs d,
                             tm * S::BM};
     const PanelOperand B = {reinterpret_cast<const uint8_t *>(d.Q) + z * d.stackQ, nullptr, d.n,
                             tn * S::BN};
-    Panel<KIND, S> p;
+    Panel<kPanelSplit, S> p;
     p.init();
-    const int col = B.row0 + p.col(0), padN = padded<KIND>(d.n);
+    const int col = B.row0 + p.col(0), padN = padded(d.n);
     const char *addend = STEP == kGram ? nullptr : d.addend + z * d.stackOut;
-    const int panelsN = padN / panel_elements<KIND>();
+    const int panelsN = padN / kNumbers;
     if constexpr (STEP != kGram && kAddendEarly<S>)
-        load_panels<KIND, S>(p, dyn_lds + S::lds(KIND), addend, d.m, panelsN, A.row0, B.row0, 0);
+        load_panels<S>(p, dyn_lds + S::lds(kPanelSplit), addend, d.m, panelsN, A.row0, B.row0, 0);
     p.run(dyn_lds, A, B, w.t0, w.t1);
     __builtin_amdgcn_s_waitcnt(7 << 4 | 15 << 8);   // vmcnt 0 (the addend, if no panel came)
     __syncthreads();
-    if (!panel_join<KIND, S>(p, grid, w, dyn_lds)) return;
+    if (!panel_join<kPanelSplit, S>(p, grid, w, dyn_lds)) return;
 
     // rows and columns of the padding become zeros
-    constexpr int PASSES = STEP == kGram || kAddendEarly<S> ? 1 : image_passes<KIND, S, false>();
+    constexpr int PASSES = STEP == kGram || kAddendEarly<S> ? 1 : image_passes<S, false>();
 #pragma unroll 1
     for (int pass = 0; pass < PASSES; ++pass) {
-        const char *image = dyn_lds + (kAddendEarly<S> ? S::lds(KIND) : 0);
+        const char *image = dyn_lds + (kAddendEarly<S> ? S::lds(kPanelSplit) : 0);
         if constexpr (STEP != kGram && !kAddendEarly<S>) {
             __syncthreads();
-            load_panels<KIND, S>(p, dyn_lds, addend, d.m, panelsN, A.row0, B.row0, pass);
+            load_panels<S>(p, dyn_lds, addend, d.m, panelsN, A.row0, B.row0, pass);
             __builtin_amdgcn_s_waitcnt(7 << 4 | 15 << 8);   // vmcnt 0
             __syncthreads();
         }
@@ -388,7 +367,7 @@ __global__ __launch_bounds__(S::THREADS) void orth_product_kernel(ProductArgs d,
                 float x[FN] = {};
                 if constexpr (STEP != kGram) {
                     const int c = p.col(0) - pass * SPAN;
-                    load_run<KIND, FN>(image + at<KIND>(S::BM, p.row(i, e), c), x);
+                    load_run<FN>(image + at(S::BM, p.row(i, e), c), x);
                 }
 #pragma unroll
                 for (int j = 0; j < FN; ++j) {
@@ -405,11 +384,11 @@ __global__ __launch_bounds__(S::THREADS) void orth_product_kernel(ProductArgs d,
 #pragma unroll
         for (int j = 0; j < FN; ++j) asm volatile("" : "+v"(p.acc[i][j]));   // computed here
     if constexpr (STEP != kLast) {
-        store_panels<KIND, S, false>(p, dyn_lds, d.out + z * d.stackOut, d.m, panelsN, A.row0, B.row0);
+        store_panels<S, false>(p, dyn_lds, d.out + z * d.stackOut, d.m, panelsN, A.row0, B.row0);
         // the other orientation: X^T, or the mirrored tile
         if (!kSymmetric || tm != tn)
-            store_panels<KIND, S, true>(p, dyn_lds, d.outT + z * d.stackOutT, d.n,
-                                        padded<KIND>(d.m) / panel_elements<KIND>(), B.row0, A.row0);
+            store_panels<S, true>(p, dyn_lds, d.outT + z * d.stackOutT, d.n, padded(d.m) / kNumbers,
+                                  B.row0, A.row0);
     } else if (O.si != 1 || O.sk == 1) {
         // a lane's rows: four times FM in a row, then as many are another's
         T *o = O.p + z * O.sb + (A.row0 + p.row(0, 0)) * O.si + col * O.sk;
@@ -475,7 +454,7 @@ constexpr int kShortOwn = 2 * kShortE * 128;   // LDS of a wavefront
 constexpr int kShortPitch = kShortE + 2, kShortAcross = kShortE + 1;
 constexpr int kShortLds = kShortWaves * kShortOwn + kShortE * kShortAcross * 4;
 
-template <int KIND, int STEP, typename T>
+template <int STEP, typename T>
 __global__ __launch_bounds__(kShortThreads) void orth_short_kernel(ProductArgs d, PanelGrid grid,
                                                                    Stack<T> O)
 {
@@ -491,7 +470,7 @@ __global__ __launch_bounds__(kShortThreads) void orth_short_kernel(ProductArgs d
     const int z = w.z;
     if constexpr (kSymmetric) panel_triangle(w.tile, tm, tn);
     else panel_tile(grid, w.tile, tm, tn);
-    const int row0 = tm * E, col0 = tn * E, padM = padded<KIND>(d.m), padN = padded<KIND>(d.n);
+    const int row0 = tm * E, col0 = tn * E, padM = padded(d.m), padN = padded(d.n);
 
     // a lane's 16 bytes of each load of eight rows: piece p of row r lies at
     // place p ^ (r / 2 mod 8) of its row; rows past the last read it again, and
@@ -509,7 +488,7 @@ __global__ __launch_bounds__(kShortThreads) void orth_short_kernel(ProductArgs d
     float x[N] = {};
     if constexpr (STEP != kGram)
         if (row < d.m && col < padN)
-            load_run<KIND, N>(d.addend + z * d.stackOut + at<KIND>(d.m, row, col), x);
+            load_run<N>(d.addend + z * d.stackOut + at(d.m, row, col), x);
 
     f16v acc;
 #pragma unroll
@@ -531,9 +510,7 @@ __global__ __launch_bounds__(kShortThreads) void orth_short_kernel(ProductArgs d
         }
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
-            if constexpr (KIND == kPanelHalf) {
-                acc = mfma_half(a[s], b[s], acc);
-            } else if (s % 2 == 0) {
+            if (s % 2 == 0) {
                 acc = mfma_half(a[s], b[s], acc);
                 acc = mfma_half(a[s], b[s + 1], acc);
                 acc = mfma_half(a[s + 1], b[s], acc);
@@ -576,9 +553,9 @@ __global__ __launch_bounds__(kShortThreads) void orth_short_kernel(ProductArgs d
     for (int i = 0; i < N; ++i) y[i] = turn ? turned[(lc + i) * kShortAcross + lr] : 0.0f;
     if constexpr (STEP != kLast) {
         if (row < d.m && col < padN)
-            store_run<KIND, N>(d.out + z * d.stackOut + at<KIND>(d.m, row, col), v);
+            store_run<N>(d.out + z * d.stackOut + at(d.m, row, col), v);
         if (turn && tcol < d.n && trow < padM)
-            store_run<KIND, N>(d.outT + z * d.stackOutT + at<KIND>(d.n, tcol, trow), y);
+            store_run<N>(d.outT + z * d.stackOutT + at(d.n, tcol, trow), y);
     } else {
         const int er = turn ? trow : row, ec = turn ? tcol : col;   // first of the N
         const int left = turn ? (ec < d.n ? d.m - er : 0) : (er < d.m ? d.n - ec : 0);
@@ -614,18 +591,13 @@ struct Choice {
     PanelCut cut;
     int64_t slotBytes;
 };
-// blocks of a short product; they write the padding of the last panels too
-template <int KIND, int STEP> int64_t short_count(int64_t m, int64_t n)
-{
-    return tile_count<STEP>(kShortE, padded<KIND>((int)m), padded<KIND>((int)n));
-}
-// Its price beside panel_cut's, which leave out a launch's fixed time: that is
-// 1.3 us shorter here, and a wavefront's panel takes 0.65, with two workgroups
-// on a CU 1.6.  us as tiles of 64 x 64 and here: 160 x 160 floats, S 5.8 / 4.2,
-// update 6.9 / 4.2; 517 x 1000, S 11.4 / 7.1, S^2 9.5 / 5.2, bf16 7.3 / 5.1 and
-// 6.8 / 4.8; 256 x 2048, S 11.3 / 8.4, update 8.7 / 8.1; 768 x 768, S 10.2 / 8.5.
-// With more blocks than are resident the tiles' fewer loads win: S of 1024 x
-// 1024 11.2 / 12.1, the update of 517 x 1000 11.6 / 12.0 and bf16 8.6 / 9.4.
+// A short product's price beside panel_cut's, which leave out a launch's fixed
+// time: that is 1.3 us shorter here, and a wavefront's panel takes 0.65, with two
+// workgroups on a CU 1.6.  us as tiles of 64 x 64 and here: 160 x 160, S 5.8 /
+// 4.2, update 6.9 / 4.2; 517 x 1000, S 11.4 / 7.1, S^2 9.5 / 5.2; 256 x 2048, S
+// 11.3 / 8.4, update 8.7 / 8.1; 768 x 768, S 10.2 / 8.5.  With more blocks than
+// are resident the tiles' fewer loads win: S of 1024 x 1024 11.2 / 12.1, the
+// update of 517 x 1000 11.6 / 12.0.
 PanelCut short_cut(int64_t blocks, int64_t panels)
 {
     PanelCut c;
@@ -634,13 +606,13 @@ PanelCut short_cut(int64_t blocks, int64_t panels)
     if (blocks <= 2 * kPanelCus) c.us = (blocks <= kPanelCus ? 0.65 : 1.6) * each - 1.3;
     return c;
 }
-template <int KIND, int STEP> Choice choose(int64_t batch, int64_t m, int64_t n, int64_t panels)
+template <int STEP> Choice choose(int64_t batch, int64_t m, int64_t n, int64_t panels)
 {
     const PanelCut c[4] = {
-        panel_cut<Big>(KIND, batch * tile_count<STEP>(Big::BM, m, n), panels),
-        panel_cut<Mid>(KIND, batch * tile_count<STEP>(Mid::BM, m, n), panels),
-        panel_cut<Small>(KIND, batch * tile_count<STEP>(Small::BM, m, n), panels),
-        short_cut(batch * short_count<KIND, STEP>(m, n), panels)};
+        panel_cut<Big>(kPanelSplit, batch * tile_count<STEP>(Big::BM, m, n), panels),
+        panel_cut<Mid>(kPanelSplit, batch * tile_count<STEP>(Mid::BM, m, n), panels),
+        panel_cut<Small>(kPanelSplit, batch * tile_count<STEP>(Small::BM, m, n), panels),
+        short_cut(batch * tile_count<STEP>(kShortE, m, n), panels)};
     int s = 0;
     for (int i = 1; i < 4; ++i)
         if (c[i].us < c[s].us) s = i;
@@ -653,13 +625,12 @@ struct Workspace {
     int *counters;
 };
 
-template <int KIND, int STEP, typename S, typename T>
+template <int STEP, typename S, typename T>
 hipError_t product_launch(const ProductArgs &d, const PanelCut &c, const Workspace &w,
                           const Stack<T> &O, int64_t batch, hipStream_t stream)
 {
-    constexpr auto k = orth_product_kernel<KIND, STEP, S, T>;
-    constexpr int lds = S::lds(KIND) + (STEP != kGram && kAddendEarly<S>
-                                            ? S::TILE * (KIND == kPanelSplit ? 4 : 2) : 0);
+    constexpr auto k = orth_product_kernel<STEP, S, T>;
+    constexpr int lds = S::lds(kPanelSplit) + (STEP != kGram && kAddendEarly<S> ? S::TILE * 4 : 0);
     const hipError_t e = allow_dynamic_lds<k>(lds);
     if (e != hipSuccess) return e;
     PanelGrid g;
@@ -670,30 +641,29 @@ hipError_t product_launch(const ProductArgs &d, const PanelCut &c, const Workspa
     return hipGetLastError();
 }
 
-template <int KIND, int STEP, typename T>
+template <int STEP, typename T>
 hipError_t short_launch(const ProductArgs &d, const PanelCut &c, const Stack<T> &O, int64_t batch,
                         hipStream_t stream)
 {
-    constexpr auto k = orth_short_kernel<KIND, STEP, T>;
+    constexpr auto k = orth_short_kernel<STEP, T>;
     const hipError_t e = allow_dynamic_lds<k>(kShortLds);
     if (e != hipSuccess) return e;
     PanelGrid g;
-    if (!panel_grid(g, batch, (padded<KIND>(d.m) + kShortE - 1) / kShortE,
-                    (padded<KIND>(d.n) + kShortE - 1) / kShortE, short_count<KIND, STEP>(d.m, d.n), c,
-                    d.panels, nullptr, nullptr))
+    if (!panel_grid(g, batch, (d.m + kShortE - 1) / kShortE, (d.n + kShortE - 1) / kShortE,
+                    tile_count<STEP>(kShortE, d.m, d.n), c, d.panels, nullptr, nullptr))
         return hipErrorInvalidValue;
     hipLaunchKernelGGL(k, dim3((unsigned)c.blocks), dim3(kShortThreads), kShortLds, stream, d, g, O);
     return hipGetLastError();
 }
 
-template <int KIND, int STEP, typename T>
+template <int STEP, typename T>
 hipError_t product(const ProductArgs &d, const Choice &c, const Workspace &w, const Stack<T> &O,
                    int64_t batch, hipStream_t stream)
 {
-    if (c.shape == 0) return product_launch<KIND, STEP, Big, T>(d, c.cut, w, O, batch, stream);
-    if (c.shape == 1) return product_launch<KIND, STEP, Mid, T>(d, c.cut, w, O, batch, stream);
-    if (c.shape == 2) return product_launch<KIND, STEP, Small, T>(d, c.cut, w, O, batch, stream);
-    return short_launch<KIND, STEP, T>(d, c.cut, O, batch, stream);
+    if (c.shape == 0) return product_launch<STEP, Big, T>(d, c.cut, w, O, batch, stream);
+    if (c.shape == 1) return product_launch<STEP, Mid, T>(d, c.cut, w, O, batch, stream);
+    if (c.shape == 2) return product_launch<STEP, Small, T>(d, c.cut, w, O, batch, stream);
+    return short_launch<STEP, T>(d, c.cut, O, batch, stream);
 }
 
 struct Problem {
@@ -736,11 +706,6 @@ inline bool small_fits(int64_t m, int64_t n)
            small_lds(m, n) <= kSmallLds;
 }
 
-// the byte of number k in its row
-__device__ __forceinline__ int small_at(int k)
-{
-    return (k >> 3) * 32 + (k & 7) * 2;
-}
 __device__ __forceinline__ f16v small_block(const char *a, const char *b, int k)
 {
     f16v acc;
@@ -803,8 +768,8 @@ __global__ __launch_bounds__(kSmallWaves * 64) void orth_small_kernel(Stack<cons
         for (int i = lane; i < inner; i += 64) {
             const float v = (float)((double)to_float(g[o * so + i * si]) * scale);
             const int row = along ? o : i, col = along ? i : o;
-            store_run<kPanelSplit, 1>(X + row * pX + small_at(col), &v);
-            store_run<kPanelSplit, 1>(XT + col * pS + small_at(row), &v);
+            store_run<1>(X + row * pX + in_panel(col), &v);
+            store_run<1>(XT + col * pS + in_panel(row), &v);
         }
     __syncthreads();
 
@@ -813,7 +778,7 @@ __global__ __launch_bounds__(kSmallWaves * 64) void orth_small_kernel(Stack<cons
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             const float x[4] = {v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
-            store_run<kPanelSplit, 4>(M + (col0 + r) * pitch + small_at(row0 + 8 * q + 4 * h), x);
+            store_run<4>(M + (col0 + r) * pitch + in_panel(row0 + 8 * q + 4 * h), x);
         }
     };
     for (int step = 0; step < steps; ++step) {
@@ -838,7 +803,7 @@ __global__ __launch_bounds__(kSmallWaves * 64) void orth_small_kernel(Stack<cons
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 float x[4];   // S is symmetric: its column r
-                load_run<kPanelSplit, 4>(S + (bj * 32 + r) * pS + small_at(bi * 32 + 8 * q + 4 * h), x);
+                load_run<4>(S + (bj * 32 + r) * pS + in_panel(bi * 32 + 8 * q + 4 * h), x);
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
                     poly[u][4 * q + e] = cb * x[e] + cc * kDown * poly[u][4 * q + e];
@@ -889,7 +854,7 @@ __global__ __launch_bounds__(kSmallWaves * 64) void orth_small_kernel(Stack<cons
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     float x[4];
-                    load_run<kPanelSplit, 4>(column + small_at(bi * 32 + 8 * q + 4 * h), x);
+                    load_run<4>(column + in_panel(bi * 32 + 8 * q + 4 * h), x);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) v[4 * q + e] = ca * x[e] + kDown * v[4 * q + e];
                 }
@@ -899,7 +864,7 @@ __global__ __launch_bounds__(kSmallWaves * 64) void orth_small_kernel(Stack<cons
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
                         const float x = v[e];
-                        store_run<kPanelSplit, 1>(X + (row0 + 8 * (e >> 2) + (e & 3)) * px + small_at(col), &x);
+                        store_run<1>(X + (row0 + 8 * (e >> 2) + (e & 3)) * px + in_panel(col), &x);
                     }
                 } else if (col < n) {
 #pragma unroll
@@ -916,7 +881,7 @@ __global__ __launch_bounds__(kSmallWaves * 64) void orth_small_kernel(Stack<cons
         for (int o = wave; o < m; o += kSmallWaves)
             for (int i = lane; i < n; i += 64) {
                 float v;
-                load_run<kPanelSplit, 1>(X + o * pX + small_at(i), &v);
+                load_run<1>(X + o * pX + in_panel(i), &v);
                 O.p[(int64_t)blockIdx.x * O.sb + o * O.si + i * O.sk] = from_float<T>(v * kDown);
             }
 }
@@ -933,13 +898,12 @@ gett_status_t small_launch(const Problem &P, const Stack<const T> &G, const Stac
 }
 
 
-template <typename T, int KIND>
+template <typename T>
 gett_status_t orthogonalize_typed(const Problem &P, Stack<const T> G, Stack<T> O)
 {
     const int m = P.m, n = P.n;
-    if constexpr (KIND == kPanelSplit)   // (one part means more rows than fit)
-        if (small_fits(m, n)) return small_launch<T>(P, G, O);
-    const int64_t panelsX = panel_count<KIND>(n), panelsS = panel_count<KIND>(m);
+    if (small_fits(m, n)) return small_launch<T>(P, G, O);
+    const int64_t panelsX = panel_count(n), panelsS = panel_count(m);
     const int64_t X = m * panelsX * 128, XT = n * panelsS * 128, SS = m * panelsS * 128;
     // the norm reads along the smaller stride
     const bool along = G.sk <= G.si;
@@ -953,9 +917,9 @@ gett_status_t orthogonalize_typed(const Problem &P, Stack<const T> G, Stack<T> O
         return GETT_ERROR_NOT_SUPPORTED;
     // without a quintic term to speak of S^2 is not needed
     const bool quintic = fabs(P.c) * 0x1p40 > fabs(P.b);
-    const Choice gram = choose<KIND, kGram>(P.batch, m, m, panelsX);
-    const Choice quad = choose<KIND, kPoly>(P.batch, m, m, quintic ? panelsS : 0);
-    const Choice update = choose<KIND, kUpdate>(P.batch, m, n, panelsS);
+    const Choice gram = choose<kGram>(P.batch, m, m, panelsX);
+    const Choice quad = choose<kPoly>(P.batch, m, m, quintic ? panelsS : 0);
+    const Choice update = choose<kUpdate>(P.batch, m, n, panelsS);
     int64_t slotBytes = 0, counters = 0;
     for (const Choice *c : {&gram, &quad, &update}) {
         slotBytes = slotBytes > c->slotBytes ? slotBytes : c->slotBytes;
@@ -979,13 +943,13 @@ gett_status_t orthogonalize_typed(const Problem &P, Stack<const T> G, Stack<T> O
                        partial);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return GETT_ERROR_HIP;
-    hipLaunchKernelGGL((orth_start_kernel<T, KIND>), dim3((unsigned)(P.batch * startM * startN)),
+    hipLaunchKernelGGL((orth_start_kernel<T>), dim3((unsigned)(P.batch * startM * startN)),
                        dim3(kNormThreads), 0, P.stream, G, m, n, (int)(startM * startN),
                        recip(startM * startN), (int)startN, recip(startN), partial, blocks, P.eps, x, xt, X, XT);
     e = hipGetLastError();
     if (e != hipSuccess) return GETT_ERROR_HIP;
     if (P.steps == 0) {
-        hipLaunchKernelGGL((orth_copy_kernel<T, KIND>), dim3((unsigned)copies), dim3(256), 0,
+        hipLaunchKernelGGL((orth_copy_kernel<T>), dim3((unsigned)copies), dim3(256), 0,
                            P.stream, x, X, m, n, O, (int64_t)m * n * P.batch);
         return hipGetLastError() == hipSuccess ? GETT_SUCCESS : GETT_ERROR_HIP;
     }
@@ -999,7 +963,7 @@ gett_status_t orthogonalize_typed(const Problem &P, Stack<const T> G, Stack<T> O
         d.out = d.outT = s;
         d.stackOut = d.stackOutT = SS;
         d.factor = kDown;
-        e = product<KIND, kGram, T>(d, gram, slots, none, P.batch, P.stream);
+        e = product<kGram, T>(d, gram, slots, none, P.batch, P.stream);
         if (e != hipSuccess) return GETT_ERROR_HIP;
         d.P = d.Q = d.addend = s;
         d.stackP = d.stackQ = SS;
@@ -1007,7 +971,7 @@ gett_status_t orthogonalize_typed(const Problem &P, Stack<const T> G, Stack<T> O
         d.out = d.outT = poly;
         d.factor = (float)(P.c * kDown);
         d.scale = (float)P.b;
-        e = product<KIND, kPoly, T>(d, quad, slots, none, P.batch, P.stream);
+        e = product<kPoly, T>(d, quad, slots, none, P.batch, P.stream);
         if (e != hipSuccess) return GETT_ERROR_HIP;
         d.P = poly;
         d.Q = xt;
@@ -1020,8 +984,8 @@ gett_status_t orthogonalize_typed(const Problem &P, Stack<const T> G, Stack<T> O
         d.panels = (int)panelsS;
         d.factor = kDown;
         d.scale = (float)P.a;
-        e = i + 1 < P.steps ? product<KIND, kUpdate, T>(d, update, slots, none, P.batch, P.stream)
-                            : product<KIND, kLast, T>(d, update, slots, O, P.batch, P.stream);
+        e = i + 1 < P.steps ? product<kUpdate, T>(d, update, slots, none, P.batch, P.stream)
+                            : product<kLast, T>(d, update, slots, O, P.batch, P.stream);
         if (e != hipSuccess) return GETT_ERROR_HIP;
         std::swap(xt, xt2);
     }
@@ -1123,17 +1087,16 @@ gett_status_t gett_orthogonalize(gett_dtype_t dtype, int64_t batch, int64_t rows
         std::swap(ostride_row, ostride_col);
     }
     if (dtype == GETT_FLOAT32)
-        return orthogonalize_typed<float, kPanelSplit>(
+        return orthogonalize_typed<float>(
             P, {static_cast<const float *>(G), stride_batch, stride_row, stride_col},
             {static_cast<float *>(O), ostride_batch, ostride_row, ostride_col});
     if (dtype == GETT_FLOAT16)
-        return orthogonalize_typed<_Float16, kPanelSplit>(
+        return orthogonalize_typed<_Float16>(
             P, {static_cast<const _Float16 *>(G), stride_batch, stride_row, stride_col},
             {static_cast<_Float16 *>(O), ostride_batch, ostride_row, ostride_col});
-    const Stack<const bf16> g = {static_cast<const bf16 *>(G), stride_batch, stride_row, stride_col};
-    const Stack<bf16> o = {static_cast<bf16 *>(O), ostride_batch, ostride_row, ostride_col};
-    return P.m <= kTwoPartRows ? orthogonalize_typed<bf16, kPanelSplit>(P, g, o)
-                               : orthogonalize_typed<bf16, kPanelHalf>(P, g, o);
+    return orthogonalize_typed<bf16>(
+        P, {static_cast<const bf16 *>(G), stride_batch, stride_row, stride_col},
+        {static_cast<bf16 *>(O), ostride_batch, ostride_row, ostride_col});
 }
 
 }  // extern "C"

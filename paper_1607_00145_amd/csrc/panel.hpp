@@ -11,12 +11,11 @@
 // the bytes stand for:
 //   Mx     64 4-bit numbers a slab, and a scale per piece (32 numbers):
 //          v_mfma_scale 32x32x64;
-//   Half   16 halves a slab: v_mfma 32x32x16 f16;
 //   Split  numbers in two parts (x = hi + lo, 22 bits), eight high parts in an
 //          even piece and their low parts in the odd piece after it: slabs 2 j
 //          and 2 j + 1 give hi hi' + hi lo' + lo hi', three MFMAs; lo lo' is
 //          below the sums' own rounding.
-// All of them take as long for 32 bytes of their rows, so one tile geometry
+// Both take as long for 32 bytes of their rows, so one tile geometry
 // serves them.  (32 x 32 and not 16 x 16: from one wavefront per SIMD the
 // instructions alone reach 9.3 PFLOP/s in 4 bits and 2.4 in halves, the 16 x 16
 // ones 5.5 and 1.5.)
@@ -57,7 +56,7 @@ namespace gett {
 typedef __attribute__((address_space(1))) void matrix_global;
 typedef __attribute__((address_space(3))) void matrix_lds;
 
-enum PanelKind { kPanelMx, kPanelHalf, kPanelSplit };
+enum PanelKind { kPanelMx, kPanelSplit };
 
 template <int N, int I = 0, typename F> __device__ __forceinline__ void static_for(F &&f)
 {
@@ -272,7 +271,7 @@ template <int KIND, typename S> struct Panel {
                                 acc[i][j] = mfma_half(a[set][ga][i], b[set][gb][j], acc[i][j]);
                         }
                 };
-                if constexpr (KIND != kPanelSplit) {
+                if constexpr (KIND == kPanelMx) {
                     each(g, g);
                 } else if constexpr (g % 2 == 0) {
                     each(g, g);
@@ -509,9 +508,7 @@ template <typename S> PanelCut panel_cut(int kind, int64_t tiles, int64_t panels
 {
     constexpr bool big = S::BM == 256, mid = S::BM == 128;
     constexpr int64_t slots = (big ? 1 : 2) * kPanelCus;
-    const double full = kind == kPanelSplit ? (big ? 2.3 : mid ? 1.2 : 0.45)
-                        : kind == kPanelMx  ? (big ? 2.1 : mid ? 1.2 : 0.45)
-                                            : (big ? 1.7 : mid ? 1.0 : 0.40);
+    const double full = big ? (kind == kPanelSplit ? 2.3 : 2.1) : mid ? 1.2 : 0.45;
     const double alone = big ? full : kind == kPanelSplit ? (mid ? 1.0 : 0.30) : (mid ? 0.75 : 0.25);
     const double join = big ? 15 : mid ? 8 : 6, joinEach = big ? 6 : mid ? 1.5 : 0.3;
     const int64_t rounds = tiles / slots, rest = tiles % slots;

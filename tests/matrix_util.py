@@ -55,3 +55,42 @@ def newton_schulz(G, steps, coefficients, eps):
                 X = a * X + X @ (b * S + c * (S @ S))
         out[i] = X
     return out
+
+
+def to_bfloat16(x):
+    """x rounded to the nearest number of bfloat16 (8 significant bits)."""
+    f, e = np.frexp(np.asarray(x, dtype=np.float64))
+    return np.ldexp(np.rint(f * 256.0), e - 8)
+
+
+def held(x, parts):
+    """2^12 x as one or two 16-bit floats hold it: the nearest half, and for two
+    parts the nearest half of what is left."""
+    up = np.asarray(x, dtype=np.float64) * 4096.0
+    hi = up.astype(np.float16).astype(np.float64)
+    lo = (up - hi).astype(np.float16).astype(np.float64) if parts == 2 else 0.0
+    return (hi + lo) / 4096.0
+
+
+def newton_schulz_held(G, steps, coefficients, eps, parts):
+    """newton_schulz of one matrix (rows <= cols) whose iterates, S and b S + c
+    S^2 are held in parts; everything between them in 64 bits."""
+    a, b, c = coefficients
+    G = np.asarray(G, dtype=np.float64)
+    X = held(G / (math.sqrt(float((G ** 2).sum())) + eps), parts)
+    for i in range(steps):
+        S = held(X @ X.T, parts)
+        B = held(b * S + c * (S @ S), parts)
+        X = a * X + B @ X
+        if i + 1 < steps:
+            X = held(X, parts)
+    return X
+
+
+def bfloat16_bound(ref, steps):
+    """Bound of |got - ref| / |ref| where got is rounded to bfloat16 from numbers
+    within d = 12 steps 2^-22 of ref (two parts): a number's distance to the
+    type's grid changes by no more than the number does, so rounding costs what
+    it costs ref, and d; d itself comes on top."""
+    norm = np.linalg.norm(ref)
+    return np.linalg.norm(to_bfloat16(ref) - ref) / norm + 2 * 12 * max(steps, 1) * 2.0 ** -22
