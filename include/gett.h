@@ -190,8 +190,11 @@ gett_status_t gett_plan(gett_plan_t *plan, gett_dtype_t dtype,
  * call on the same stream, or use gett_contract_noalloc.  Calls on one stream
  * share its buffers: they run in order, and the launches of one call are
  * enqueued together also when several host threads call on that stream; calls
- * on different streams use different ones.  Errors: GETT_ERROR_HIP also when
- * that allocation fails; GETT_ERROR_NOT_SUPPORTED, with nothing enqueued, when
+ * on different streams use different ones.  A graph goes on using the buffers
+ * of the stream it was captured on: they stay allocated until the process ends,
+ * also when a later call on that stream gets larger ones, and a replay has to be
+ * ordered with that stream's other calls (on that stream, or by events).
+ * Errors: GETT_ERROR_HIP also when that allocation fails; GETT_ERROR_NOT_SUPPORTED, with nothing enqueued, when
  * it would have to happen while `stream` is capturing a graph.
  */
 gett_status_t gett_contract(const gett_plan_t plan, double alpha, const void *A, const void *B,

@@ -23,7 +23,11 @@
  * library's own, one per device and stream, as for gett_contract: a call that
  * needs more than the stream's workspace holds allocates, which is refused
  * with GETT_ERROR_NOT_SUPPORTED, nothing enqueued, while `stream` captures a
- * graph (run the call eagerly on that stream first).
+ * graph (run the call eagerly on that stream first).  A graph goes on using the
+ * workspace of the stream it was captured on, which is left to it when a later
+ * call gets a larger one; a replay has to be ordered with that stream's other
+ * calls (on that stream, or by events), as calls from several streams would be
+ * that share a workspace.
  *
  * The packed format ("MX4").  A matrix of `rows` x `cols` is packed along its
  * columns, the direction a product sums over.  Each run of 32 neighbours

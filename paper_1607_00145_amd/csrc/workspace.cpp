@@ -6,11 +6,16 @@
 // allocated and left at zero by every launch that uses them, and the
 // partial-tile slots, which need no initial value.  Launches on one stream
 // run in order and a call holds the pair until its launches are enqueued, so
-// they can share it; launches on different streams get different pairs.  A buffer grows when a plan needs more: the stream is
-// synchronised first (queued work may still use the old one).  Growth is
+// they can share it; launches on different streams get different pairs.
+//
+// A buffer grows when a call needs more: the stream is synchronised first
+// (queued work may still use the old one) and the old buffer freed.  Growth is
 // refused (GETT_ERROR_NOT_SUPPORTED, nothing enqueued) while the stream is
-// capturing a graph -- an eager call of the plan on that stream beforehand
-// allocates what the captured calls use.
+// capturing a graph -- an eager call on that stream beforehand allocates what
+// the captured calls use.  A buffer that a captured call was given belongs to
+// that graph from then on, whose kernels hold its address: when the stream needs
+// a larger one it is left allocated, until the process ends (when the last graph
+// that holds it goes cannot be seen from here).
 #include <hip/hip_runtime_api.h>
 #include <stdint.h>
 
@@ -23,11 +28,13 @@
 namespace gett {
 namespace {
 
+struct Buffer {
+    void *p = nullptr;
+    uint64_t bytes = 0;
+    bool inGraph = false;   // a captured call was given it
+};
 struct Buffers {
-    void *counters = nullptr;
-    uint64_t counterBytes = 0;
-    void *tiles = nullptr;
-    uint64_t tileBytes = 0;
+    Buffer counters, tiles;
     std::mutex use;   // held by the call that is enqueuing its launches
 };
 
@@ -35,6 +42,20 @@ std::mutex g_mutex;   // of the map; its entries stay where they are
 std::map<std::pair<int, hipStream_t>, Buffers> g_buffers;
 
 uint64_t round_up(uint64_t n) { return (n + 4095) / 4096 * 4096; }
+
+// A new buffer in place of one that nothing enqueued uses any more.
+gett_status_t grow(Buffer &b, uint64_t bytes)
+{
+    if (b.p && !b.inGraph && hipFree(b.p) != hipSuccess) return GETT_ERROR_HIP;
+    b = Buffer{};
+    const uint64_t n = round_up(bytes);
+    if (hipMalloc(&b.p, n) != hipSuccess) {
+        b.p = nullptr;
+        return GETT_ERROR_HIP;
+    }
+    b.bytes = n;
+    return GETT_SUCCESS;
+}
 
 }  // namespace
 
@@ -51,42 +72,38 @@ gett_status_t stream_workspace(hipStream_t stream, uint64_t counters, uint64_t t
     Buffers &b = *found;
     out.hold = std::unique_lock<std::mutex>(b.use);
     const uint64_t cBytes = counters * sizeof(int);
-    const bool growC = cBytes > b.counterBytes, growT = tileBytes > b.tileBytes;
-    if (growC || growT) {
-        hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
-        if (hipStreamIsCapturing(stream, &cap) != hipSuccess) return GETT_ERROR_HIP;
-        if (cap != hipStreamCaptureStatusNone) return GETT_ERROR_NOT_SUPPORTED;
+    const bool growC = cBytes > b.counters.bytes, growT = tileBytes > b.tiles.bytes;
+    hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
+    if (hipStreamIsCapturing(stream, &cap) != hipSuccess) {
+        if (growC || growT) return GETT_ERROR_HIP;
+        (void)hipGetLastError();   // no capture of this stream; its launches say the rest
+        cap = hipStreamCaptureStatusNone;
     }
-    if ((growC && b.counters) || (growT && b.tiles)) {
+    const bool capturing = cap != hipStreamCaptureStatusNone;
+    if (capturing && (growC || growT)) return GETT_ERROR_NOT_SUPPORTED;
+    if ((growC && b.counters.p) || (growT && b.tiles.p)) {
         // queued launches on this stream may still use the old buffers
         if (hipStreamSynchronize(stream) != hipSuccess) return GETT_ERROR_HIP;
     }
     if (growC) {
-        if (b.counters && hipFree(b.counters) != hipSuccess) return GETT_ERROR_HIP;
-        b.counters = nullptr;
-        b.counterBytes = 0;
-        const uint64_t n = round_up(cBytes);
-        if (hipMalloc(&b.counters, n) != hipSuccess) {
-            b.counters = nullptr;
+        const gett_status_t st = grow(b.counters, cBytes);
+        if (st != GETT_SUCCESS) return st;
+        // ordered before the launches that follow on this stream
+        if (hipMemsetAsync(b.counters.p, 0, b.counters.bytes, stream) != hipSuccess) {
+            b.counters.bytes = 0;   // (not zeroed: never handed out)
             return GETT_ERROR_HIP;
         }
-        // ordered before the launches that follow on this stream
-        if (hipMemsetAsync(b.counters, 0, n, stream) != hipSuccess) return GETT_ERROR_HIP;
-        b.counterBytes = n;
     }
     if (growT) {
-        if (b.tiles && hipFree(b.tiles) != hipSuccess) return GETT_ERROR_HIP;
-        b.tiles = nullptr;
-        b.tileBytes = 0;
-        const uint64_t n = round_up(tileBytes);
-        if (hipMalloc(&b.tiles, n) != hipSuccess) {
-            b.tiles = nullptr;
-            return GETT_ERROR_HIP;
-        }
-        b.tileBytes = n;
+        const gett_status_t st = grow(b.tiles, tileBytes);
+        if (st != GETT_SUCCESS) return st;
     }
-    out.counters = static_cast<int *>(b.counters);
-    out.tiles = b.tiles;
+    if (capturing) {
+        b.counters.inGraph |= cBytes > 0;
+        b.tiles.inGraph |= tileBytes > 0;
+    }
+    out.counters = static_cast<int *>(b.counters.p);
+    out.tiles = b.tiles.p;
     return GETT_SUCCESS;
 }
 
