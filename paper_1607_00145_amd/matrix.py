@@ -165,6 +165,14 @@ def _matrix(name, t):
     return code, r, c, sr, sc
 
 
+def _no_gradient(what, *tensors):
+    """Refuses tensors whose gradient would be lost in silence."""
+    for t in tensors:
+        if t.requires_grad and _torch.is_grad_enabled():
+            raise RuntimeError(f"{what} has no gradient: detach its tensors or call it under "
+                               "torch.no_grad() (mx_linear with a float weight has one)")
+
+
 def _strides(t):
     """(row, column) strides of the last two directions; one of extent one may
     carry any (torch leaves what it likes there, 0 included)."""
@@ -232,6 +240,7 @@ class MXTensor:
             if tuple(out.shape) != (r, c) or (dtype is not None and out.dtype != dtype):
                 raise ValueError("out differs in shape or dtype")
             code, _, _, sr, sc = _matrix("out", out)
+            _no_gradient("dequantize", out)
         st = _bound.gett_mx_dequantize(code, r, c, self._codes, self._scales, out.data_ptr(), sr, sc,
                                        _package._current_stream())
         if st != 0:
@@ -249,7 +258,7 @@ def _packed(rows, cols, buffer, at, codes, scales):
 def mx_quantize(x, along: str = "cols"):
     """Pack a matrix: ``"cols"`` along its columns (x as an operand of x @ w.T),
     ``"rows"`` along its rows (its transpose as an operand), ``"both"`` in one
-    pass, as a pair."""
+    pass, as a pair.  A packed matrix carries no gradient."""
     if along not in ("cols", "rows", "both"):
         raise ValueError("along must be 'cols', 'rows' or 'both'")
     code, r, c, sr, sc = _matrix("x", x)
@@ -281,7 +290,8 @@ def mx_matmul(a, b, C=None, alpha: float = 1.0, beta: float = 0.0, dtype=None):
     """C <- alpha * a @ b.T + beta * C for a packed `b` (n x k) and an `a` (m x k)
     that is packed or a float matrix, which is quantised in the call.  Without C
     a new row-major one is returned, in `dtype` (default: a's, float32 for a
-    packed a)."""
+    packed a).  It has no gradient and refuses tensors that require one while
+    gradients are recorded."""
     if not isinstance(b, MXTensor):
         raise TypeError("b must be packed (mx_quantize)")
     packed = isinstance(a, MXTensor)
@@ -289,6 +299,7 @@ def mx_matmul(a, b, C=None, alpha: float = 1.0, beta: float = 0.0, dtype=None):
         m, k = a.rows, a.cols
     else:
         code_a, m, k, sr, sc = _matrix("a", a)
+        _no_gradient("mx_matmul", a)
     n = b.rows
     if k != b.cols:
         raise ValueError(f"a has {k} columns, b {b.cols}")
@@ -305,6 +316,7 @@ def mx_matmul(a, b, C=None, alpha: float = 1.0, beta: float = 0.0, dtype=None):
         if tuple(C.shape) != (m, n) or (dtype is not None and C.dtype != dtype):
             raise ValueError("C differs in shape or dtype")
         code, _, _, sm, sn = _matrix("C", C)
+        _no_gradient("mx_matmul", C)
     if packed:
         st = _bound.gett_mx_contract(m, n, k, alpha, a._codes, a._scales, b._codes, b._scales, beta,
                                      code, C.data_ptr(), sm, sn, _package._current_stream())
@@ -393,7 +405,9 @@ def mx_linear(x, w):
     """x @ w.T over the last dimension with both operands rounded to 4 bits.
 
     `w` is a float n x k weight (differentiable, as is `x`: gradients are
-    products in 4 bits as well) or a packed one, for serving."""
+    products in 4 bits as well) or a packed one, for serving: that form keeps
+    nothing that x's gradient could be formed from, and refuses an x that
+    requires one while gradients are recorded."""
     shape = x.shape
     flat = x if len(shape) == 2 else x.reshape(-1, shape[-1])
     if isinstance(w, MXTensor):
@@ -410,7 +424,8 @@ def orthogonalize(G, steps: int = 5, coefficients=(3.4445, -4.7750, 2.0315), eps
                   out=None):
     """`steps` Newton-Schulz steps X <- a X + (b S + c S^2) X, S = X X^T, from
     G / (|G| + eps), for a matrix or a stack [..., rows, cols] of them; `out`
-    may be G."""
+    may be G.  It has no gradient and refuses tensors that require one while
+    gradients are recorded."""
     if G.dim() < 2:
         raise ValueError("a matrix or a stack of matrices is needed")
     code = _code(G.dtype)
@@ -421,6 +436,7 @@ def orthogonalize(G, steps: int = 5, coefficients=(3.4445, -4.7750, 2.0315), eps
         raise ValueError("out differs in shape or dtype")
     else:
         _device("out", out)
+    _no_gradient("orthogonalize", G, out)
     g, o, copy = G, out, None
     if G.dim() != 3:
         g = G.unsqueeze(0) if G.dim() == 2 else G.reshape(-1, *G.shape[-2:])
