@@ -328,28 +328,34 @@ def mx_matmul(a, b, C=None, alpha: float = 1.0, beta: float = 0.0, dtype=None):
     return C
 
 
+def _addresses(parts, buffer):
+    """Addresses of a buffer's parts; None for one that is not there."""
+    if buffer is None:
+        return parts
+    p = buffer.data_ptr()
+    return [None if at is None else p + at for at in parts]
+
+
 def _linear_forward(x, w, save_x, save_w):
-    """y, and the packed x^T and w^T that are asked for: (buffer, addresses)."""
+    """y, and what a backward pass needs of it: a buffer with the packed x^T and
+    w^T that are asked for, and where in it the codes and scales of each lie."""
     cx, m, k, sxm, sxk = _matrix("x", x)
     cw, n, kw, swn, swk = _matrix("w", w)
     if kw != k:
         raise ValueError(f"x has {k} columns, w {kw}")
     y = _torch.empty((m, n), dtype=x.dtype, device=x.device)
-    buf = xt = xs = wt = ws = None
-    a, b = _sizes(k, m) if save_x else (0, 0)
+    a, b = _sizes(k, m) if save_x else (0, 0)      # multiples of 16 bytes
     c, d = _sizes(k, n) if save_w else (0, 0)
+    parts = ([0, a] if save_x else [None, None]) + ([a + b, a + b + c] if save_w else [None, None])
+    buf = None
     if save_x or save_w:
         buf = _torch.empty(a + b + c + d, dtype=_torch.uint8, device=x.device)
-        p = buf.data_ptr()
-        if save_x:
-            xt, xs = p, p + a
-        if save_w:
-            wt, ws = p + a + b, p + a + b + c
+    xt, xs, wt, ws = _addresses(parts, buf)
     st = _bound.gett_mx_linear(m, n, k, cx, x.data_ptr(), sxm, sxk, cw, w.data_ptr(), swn, swk,
                                y.data_ptr(), n or 1, 1, xt, xs, wt, ws, _package._current_stream())
     if st != 0:
         raise GettError(st, "gett_mx_linear")
-    return y, (buf, xt, xs, wt, ws)
+    return y, buf, parts
 
 
 _function = None
@@ -369,7 +375,8 @@ def _linear_function():
         @staticmethod
         def forward(ctx, x, w):
             need_x, need_w = ctx.needs_input_grad
-            y, ctx.packed = _linear_forward(x, w, need_w, need_x)
+            y, buf, ctx.parts = _linear_forward(x, w, need_w, need_x)
+            ctx.save_for_backward(buf)   # freed with the graph; hooks and checkpoints see it
             ctx.sizes = x.shape[0], w.shape[0], x.shape[1], x.dtype, w.dtype
             return y
 
@@ -385,7 +392,8 @@ def _linear_function():
         if dy.stride(0) < 1 or dy.stride(1) < 1:
             dy = dy.contiguous()   # the gradient of a sum is broadcast
         code, _, _, sm, sn = _matrix("dy", dy)
-        _, xt, xs, wt, ws = ctx.packed
+        buf, = ctx.saved_tensors
+        xt, xs, wt, ws = _addresses(ctx.parts, buf)
         dx = torch.empty((m, k), dtype=tx, device=dy.device) if need_x else None
         dw = torch.empty((n, k), dtype=tw, device=dy.device) if need_w else None
         st = _bound.gett_mx_linear_grad(

@@ -30,3 +30,74 @@ def test_a_gradient_is_refused_where_there_is_none(gpu):
     assert torch.equal(g.mx_linear(xg.detach(), wq), g.mx_matmul(x, wq))
     # a weight may be packed while it is trained: the packed copy is no tensor
     assert g.mx_quantize(xg).shape == (6, 64)
+
+
+def layer(gpu, m=40, n=48, k=64):
+    import torch
+    x = torch.randn(m, k, device=gpu, requires_grad=True)
+    w = torch.randn(n, k, device=gpu, requires_grad=True)
+    return x, w
+
+
+def test_a_second_backward_needs_retain_graph(gpu):
+    import torch
+    x, w = layer(gpu)
+    y = g.mx_linear(x, w)
+    y.sum().backward(retain_graph=True)
+    first = x.grad.clone(), w.grad.clone()
+    x.grad = w.grad = None
+    y.sum().backward()
+    assert torch.equal(x.grad, first[0]) and torch.equal(w.grad, first[1])
+    with pytest.raises(RuntimeError, match="second time"):
+        y.sum().backward()
+
+
+def test_what_backward_needs_is_freed_after_it(gpu):
+    """Also while the result, and with it the graph's node, lives on."""
+    import torch
+    x, w = layer(gpu, 2048, 1024, 4096)
+    y = g.mx_linear(x, w)
+    torch.cuda.synchronize()
+    with_saved = torch.cuda.memory_allocated()
+    y.sum().backward()
+    x.grad = w.grad = None
+    torch.cuda.synchronize()
+    packed = sum(sum(g.gett_mx_size(4096, r)[1:]) for r in (2048, 1024))
+    assert y.grad_fn is not None
+    assert with_saved - torch.cuda.memory_allocated() >= packed
+
+
+def test_saved_tensor_hooks_see_the_packed_operands(gpu):
+    """Kept on the host between the passes: the same gradients."""
+    import torch
+    for need_x, need_w in ((True, True), (True, False), (False, True)):
+        x, w = layer(gpu)
+        x.requires_grad_(need_x)
+        w.requires_grad_(need_w)
+        wanted = [t for t in (x, w) if t.requires_grad]
+        dy = torch.randn(40, 48, device=gpu)
+        want = torch.autograd.grad(g.mx_linear(x, w), wanted, dy)
+        with torch.autograd.graph.save_on_cpu():
+            y = g.mx_linear(x, w)
+        got = torch.autograd.grad(y, wanted, dy)
+        for a, b in zip(got, want):
+            assert torch.equal(a, b)
+        count = []
+        with torch.autograd.graph.saved_tensors_hooks(lambda t: count.append(t.numel()) or t,
+                                                      lambda t: t):
+            g.mx_linear(x, w)
+        # x^T is what dw needs, w^T what dx needs
+        sizes = [sum(g.gett_mx_size(64, r)[1:]) for r, kept in ((40, need_w), (48, need_x)) if kept]
+        assert sum(count) >= sum(sizes)
+
+
+def test_checkpointing_recomputes_the_packed_operands(gpu):
+    import torch
+    from torch.utils.checkpoint import checkpoint
+    x, w = layer(gpu)
+    dy = torch.randn(40, 48, device=gpu)
+    want = torch.autograd.grad(g.mx_linear(x, w), (x, w), dy)
+    y = checkpoint(g.mx_linear, x, w, use_reentrant=False)
+    got = torch.autograd.grad(y, (x, w), dy)
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
