@@ -7,7 +7,7 @@
 
 The ``gett_*`` functions carry the names of the C interface and only marshal
 arguments; the others are a convenience over torch device tensors, enqueued on
-torch's current stream.
+torch's current stream of the device that they lie on.
 """
 from __future__ import annotations
 
@@ -124,13 +124,15 @@ def gett_mx_linear_grad(m: int, n: int, k: int, dtype_Y: int, dY: int, stride_ym
 # when asked for, and the C functions are called directly.
 
 _torch = None
+_current_device = None
 _codes = {}
 
 
 def _start():
     """torch and the element types' codes, on the first use."""
-    global _torch
+    global _torch, _current_device
     import torch
+    _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
     _codes.update({torch.float32: GETT_FLOAT32, torch.bfloat16: GETT_BFLOAT16,
                    torch.float16: GETT_FLOAT16})
     _torch = torch
@@ -149,6 +151,17 @@ def _code(dtype) -> int:
 def _device(name, t):
     if not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
+
+
+def _elsewhere(first, *others):
+    """Makes current the device that all of a call's tensors (or None) lie on,
+    where it is not: the call is then made again (the library launches and keeps
+    its workspace on the current device).  None where it is."""
+    i = first.get_device()
+    for t in others:
+        if t is not None and t.get_device() != i:
+            raise ValueError("the tensors lie on different devices")
+    return None if i == _current_device() else _torch.cuda.device(i)
 
 
 def _matrix(name, t):
@@ -193,7 +206,7 @@ class MXTensor:
 
     ``codes`` and ``scales`` are uint8 device tensors of gett_mx_size's bytes."""
 
-    __slots__ = ("rows", "cols", "_buffer", "_at", "_codes", "_scales")
+    __slots__ = ("rows", "cols", "_buffer", "_at", "_codes", "_scales", "_device")
 
     def __init__(self, rows: int, cols: int, codes, scales):
         c, s = _sizes(rows, cols)
@@ -201,9 +214,16 @@ class MXTensor:
             if t.numel() * t.element_size() != n or not t.is_contiguous():
                 raise ValueError(f"{name} must hold {n} contiguous bytes")
             _device(name, t)
+        if codes.get_device() != scales.get_device():
+            raise ValueError("codes and scales lie on different devices")
         self.rows, self.cols = rows, cols
         self._buffer, self._at = (codes, scales), None
         self._codes, self._scales = codes.data_ptr(), scales.data_ptr()
+        self._device = codes.get_device()
+
+    def get_device(self):
+        """The index of the device that it lies on, as a tensor's."""
+        return self._device
 
     @property
     def shape(self):
@@ -229,9 +249,14 @@ class MXTensor:
     def dequantize(self, dtype=None, out=None):
         """The values, as float32 unless `dtype` or `out` says otherwise."""
         r, c = self.rows, self.cols
+        if _torch is None:
+            _start()
+        if out is not None or self._device != _current_device():
+            there = _elsewhere(self, out)
+            if there is not None:
+                with there:
+                    return self.dequantize(dtype, out)
         if out is None:
-            if _torch is None:
-                _start()
             dtype = dtype or _torch.float32
             code = _code(dtype)
             out = _torch.empty((r, c), dtype=dtype, device=self.device)
@@ -248,10 +273,11 @@ class MXTensor:
         return out
 
 
-def _packed(rows, cols, buffer, at, codes, scales):
+def _packed(rows, cols, device, buffer, at, codes, scales):
     """A packed matrix at byte `at` of a buffer; addresses of its parts."""
     q = MXTensor.__new__(MXTensor)
-    q.rows, q.cols, q._buffer, q._at, q._codes, q._scales = rows, cols, buffer, at, codes, scales
+    q.rows, q.cols, q._device, q._buffer, q._at = rows, cols, device, buffer, at
+    q._codes, q._scales = codes, scales
     return q
 
 
@@ -262,6 +288,10 @@ def mx_quantize(x, along: str = "cols"):
     if along not in ("cols", "rows", "both"):
         raise ValueError("along must be 'cols', 'rows' or 'both'")
     code, r, c, sr, sc = _matrix("x", x)
+    i = x.get_device()
+    if i != _current_device():
+        with _elsewhere(x):
+            return mx_quantize(x, along)
     # one allocation; every part a multiple of 16 bytes
     n = s = nt = sn = 0
     if along != "rows":
@@ -281,9 +311,9 @@ def mx_quantize(x, along: str = "cols"):
     if st != 0:
         raise GettError(st, "gett_mx_quantize")
     if along == "cols":
-        return _packed(r, c, buf, 0, codes, scales)
-    t = _packed(c, r, buf, n + s, codes_t, scales_t)
-    return t if along == "rows" else (_packed(r, c, buf, 0, codes, scales), t)
+        return _packed(r, c, i, buf, 0, codes, scales)
+    t = _packed(c, r, i, buf, n + s, codes_t, scales_t)
+    return t if along == "rows" else (_packed(r, c, i, buf, 0, codes, scales), t)
 
 
 def mx_matmul(a, b, C=None, alpha: float = 1.0, beta: float = 0.0, dtype=None):
@@ -299,15 +329,21 @@ def mx_matmul(a, b, C=None, alpha: float = 1.0, beta: float = 0.0, dtype=None):
         m, k = a.rows, a.cols
     else:
         code_a, m, k, sr, sc = _matrix("a", a)
-        _no_gradient("mx_matmul", a)
+        if a.requires_grad:
+            _no_gradient("mx_matmul", a)
     n = b.rows
     if k != b.cols:
         raise ValueError(f"a has {k} columns, b {b.cols}")
+    if _torch is None:
+        _start()
+    if C is not None or not b._device == a.get_device() == _current_device():
+        there = _elsewhere(a, b, C)
+        if there is not None:
+            with there:
+                return mx_matmul(a, b, C, alpha, beta, dtype)
     if C is None:
         if beta != 0:
             raise ValueError("beta != 0 needs C")
-        if _torch is None:
-            _start()
         if dtype is None:
             dtype = _torch.float32 if packed else a.dtype
         code, sm, sn = _code(dtype), n or 1, 1
@@ -343,6 +379,10 @@ def _linear_forward(x, w, save_x, save_w):
     cw, n, kw, swn, swk = _matrix("w", w)
     if kw != k:
         raise ValueError(f"x has {k} columns, w {kw}")
+    there = _elsewhere(x, w)
+    if there is not None:
+        with there:
+            return _linear_forward(x, w, save_x, save_w)
     y = _torch.empty((m, n), dtype=x.dtype, device=x.device)
     a, b = _sizes(k, m) if save_x else (0, 0)      # multiples of 16 bytes
     c, d = _sizes(k, n) if save_w else (0, 0)
@@ -438,6 +478,10 @@ def orthogonalize(G, steps: int = 5, coefficients=(3.4445, -4.7750, 2.0315), eps
         raise ValueError("a matrix or a stack of matrices is needed")
     code = _code(G.dtype)
     _device("G", G)
+    there = _elsewhere(G, out)
+    if there is not None:
+        with there:
+            return orthogonalize(G, steps, coefficients, eps, out)
     if out is None:
         out = _torch.empty(G.shape, dtype=G.dtype, device=G.device)
     elif out.shape != G.shape or out.dtype != G.dtype:

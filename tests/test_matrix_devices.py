@@ -1,0 +1,90 @@
+"""Which device a matrix operator runs on, without a GPU: the tensors are CPU
+tensors that claim to lie on a device, and the library's functions a record."""
+import contextlib
+import types
+
+import pytest
+import torch
+
+import paper_1607_00145_amd as g
+from paper_1607_00145_amd import matrix
+
+
+class On:
+    """A CPU tensor that claims to lie on device `index`."""
+
+    is_cuda = True
+
+    def __init__(self, index, *shape, dtype=torch.float32):
+        self._t, self._index = torch.zeros(*shape, dtype=dtype), index
+
+    def get_device(self):
+        return self._index
+
+    def __getattr__(self, name):
+        return getattr(self._t, name)
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    """Records (function, device that is current) of each call; device 0 at first."""
+    now, made = [0], []
+
+    class Library:
+        def __getattr__(self, name):
+            return lambda *args: made.append((name, now[0])) or 0
+
+    @contextlib.contextmanager
+    def device(index):
+        before, now[0] = now[0], index
+        yield
+        now[0] = before
+
+    matrix._start()
+    monkeypatch.setattr(matrix, "_bound", Library())
+    monkeypatch.setattr(matrix, "_current_device", lambda: now[0], raising=False)
+    monkeypatch.setattr(matrix._package, "_current_stream", lambda: 0)
+    monkeypatch.setattr(torch.cuda, "device", device)
+    return made
+
+
+def packed(index, rows, cols):
+    c, s = matrix._sizes(rows, cols)
+    return g.MXTensor(rows, cols, On(index, c, dtype=torch.uint8), On(index, s, dtype=torch.uint8))
+
+
+def every_call(i, j):
+    """Each operator with one tensor on device i and the others on j."""
+    x, w, q, C, O = On(i, 6, 64), On(j, 48, 64), packed(j, 48, 64), On(j, 6, 48), On(j, 6, 64)
+    return [("gett_mx_apply", lambda: g.mx_matmul(x, q)),
+            ("gett_mx_apply", lambda: g.mx_matmul(On(j, 6, 64), q, On(i, 6, 48))),
+            ("gett_mx_contract", lambda: g.mx_matmul(packed(i, 6, 64), q)),
+            ("gett_mx_contract", lambda: g.mx_matmul(packed(j, 6, 64), q, On(i, 6, 48))),
+            ("gett_mx_apply", lambda: g.mx_linear(x, q)),
+            ("gett_mx_linear", lambda: g.mx_linear(x, w)),
+            ("gett_orthogonalize", lambda: g.orthogonalize(x, out=O)),
+            ("gett_mx_dequantize", lambda: packed(i, 6, 64).dequantize(out=O))]
+
+
+@pytest.mark.parametrize("i,j", [(0, 1), (1, 0), (1, 2)])
+def test_tensors_of_two_devices_are_refused(calls, i, j):
+    for _, call in every_call(i, j):
+        with pytest.raises(ValueError, match="device"):
+            call()
+    c, s = matrix._sizes(6, 64)
+    with pytest.raises(ValueError, match="device"):
+        g.MXTensor(6, 64, On(i, c, dtype=torch.uint8), On(j, s, dtype=torch.uint8))
+    assert calls == []
+
+
+@pytest.mark.parametrize("index", [0, 1])
+def test_calls_run_on_their_tensors_device(calls, index):
+    every = every_call(index, index) + [
+        ("gett_mx_quantize", lambda: g.mx_quantize(On(index, 6, 64), "both")),
+        ("gett_orthogonalize", lambda: g.orthogonalize(On(index, 2, 6, 64))),
+        ("gett_mx_dequantize", lambda: packed(index, 6, 64).dequantize())]
+    for name, call in every:
+        call()
+        assert calls == [(name, index)]
+        calls.clear()
+    assert matrix._current_device() == 0
