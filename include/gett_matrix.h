@@ -187,7 +187,8 @@ gett_status_t gett_mx_linear_grad(int64_t m, int64_t n, int64_t k, gett_dtype_t 
  *
  *   dtype     of G and O: GETT_FLOAT32, GETT_BFLOAT16 or GETT_FLOAT16.
  *   batch     matrices in the stack (stride_batch between them, >= 1; any
- *             value when batch is 1).
+ *             value when batch is 1).  They may interleave in memory, as the
+ *             column slices of a wide matrix do.
  *   a, b, c   the polynomial.  Coefficients for which a singular value may
  *             pass 3, or b s^2 + c s^4 may pass 15, within the steps
  *             are refused (GETT_ERROR_NOT_SUPPORTED): the iterates are kept

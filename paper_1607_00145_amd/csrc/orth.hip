@@ -1073,9 +1073,10 @@ gett_status_t gett_orthogonalize(gett_dtype_t dtype, int64_t batch, int64_t rows
     const int64_t spanG = span_bytes(batch, oneG / item, stride_batch, 1, item);
     const int64_t spanO = span_bytes(batch, oneO / item, ostride_batch, 1, item);
     if (spanG < 0 || spanO < 0) return GETT_ERROR_NOT_SUPPORTED;
-    if (!matrix_injective(rows, cols, ostride_row, ostride_col) ||
-        (batch > 1 && (__int128)ostride_batch * item < oneO))
-        return GETT_ERROR_NOT_SUPPORTED;
+    // (matrices may interleave, as the column slices of a weight's heads do)
+    const int64_t extents[3] = {batch, rows, cols};
+    const int64_t strides[3] = {ostride_batch, ostride_row, ostride_col};
+    if (!strides_injective(3, extents, strides)) return GETT_ERROR_NOT_SUPPORTED;
     const bool same = G == O && stride_row == ostride_row && stride_col == ostride_col &&
                       stride_batch == ostride_batch;
     if (!same && overlaps(G, spanG, O, spanO)) return GETT_ERROR_INVALID_VALUE;
