@@ -12,6 +12,7 @@ torch's current stream of the device that they lie on.
 from __future__ import annotations
 
 import ctypes
+import math
 import sys
 
 from . import GETT_FLOAT32, GettError, load_library
@@ -457,7 +458,9 @@ def mx_linear(x, w):
     nothing that x's gradient could be formed from, and refuses an x that
     requires one while gradients are recorded."""
     shape = x.shape
-    flat = x if len(shape) == 2 else x.reshape(-1, shape[-1])
+    if not shape:
+        raise ValueError("x must have a dimension")
+    flat = x if len(shape) == 2 else x.reshape(math.prod(shape[:-1]), shape[-1])
     if isinstance(w, MXTensor):
         y = mx_matmul(flat, w)
     elif _code(x.dtype) is not None and _torch.is_grad_enabled() and (x.requires_grad or
@@ -490,15 +493,15 @@ def orthogonalize(G, steps: int = 5, coefficients=(3.4445, -4.7750, 2.0315), eps
         _device("out", out)
     _no_gradient("orthogonalize", G, out)
     g, o, copy = G, out, None
-    if G.dim() != 3:
-        g = G.unsqueeze(0) if G.dim() == 2 else G.reshape(-1, *G.shape[-2:])
-        if G.dim() == 2:
-            o = out.unsqueeze(0)
-        else:
-            try:
-                o = out.view(-1, *out.shape[-2:])
-            except RuntimeError:   # a stack without one stride
-                copy = o = _torch.empty(g.shape, dtype=G.dtype, device=G.device)
+    if G.dim() == 2:
+        g, o = G.unsqueeze(0), out.unsqueeze(0)
+    elif G.dim() != 3:
+        stack = (math.prod(G.shape[:-2]), *G.shape[-2:])
+        g = G.reshape(stack)
+        try:
+            o = out.view(stack)
+        except RuntimeError:   # a stack without one stride
+            copy = o = _torch.empty(stack, dtype=G.dtype, device=G.device)
     n, r, c = g.shape
     if n > 1 and (g.stride(0) < 1 or o.stride(0) < 1):
         raise ValueError("a broadcast (zero-stride) stack: copy it first")

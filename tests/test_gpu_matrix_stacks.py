@@ -39,3 +39,36 @@ def test_overlapping_stacks_are_refused(gpu):
         O = buf.as_strided(shape, stride)
         with pytest.raises(g.GettError):
             g.orthogonalize(torch.randn(shape, device=gpu), out=O)
+
+
+@pytest.mark.parametrize("shape", [(0, 5, 7), (3, 0, 7), (3, 5, 0), (2, 3, 0, 5), (2, 3, 5, 0),
+                                   (2, 0, 4, 5), (0, 0, 4, 5)])
+def test_empty_stacks(gpu, shape):
+    import torch
+    G = torch.randn(shape, device=gpu)
+    assert g.orthogonalize(G).shape == shape
+    assert g.orthogonalize(G, out=G) is G
+    strided = torch.randn(*shape[:-1], 2 * shape[-1] + 1, device=gpu)[..., :2 * shape[-1]:2]
+    assert g.orthogonalize(strided).shape == shape
+
+
+@pytest.mark.parametrize("shape", [(2, 3, 0), (2, 0, 8), (0, 3, 8), (2, 0, 0), (0,)])
+def test_linear_of_empty_leading_dimensions(gpu, shape):
+    """As for two dimensions: a sum over nothing is zero."""
+    import torch
+    x = torch.randn(shape, device=gpu)
+    w = torch.randn(6, shape[-1], device=gpu)
+    for y in (g.mx_linear(x, w), g.mx_linear(x, g.mx_quantize(w))):
+        assert y.shape == (*shape[:-1], 6) and (y == 0).all()
+    x.requires_grad_()
+    w.requires_grad_()
+    g.mx_linear(x, w).sum().backward()
+    assert x.grad.shape == x.shape and (w.grad == 0).all()
+
+
+def test_linear_of_a_vector(gpu):
+    import torch
+    x, w = torch.randn(64, device=gpu), torch.randn(48, 64, device=gpu)
+    assert torch.equal(g.mx_linear(x, w), g.mx_linear(x[None], w)[0])
+    with pytest.raises(ValueError):
+        g.mx_linear(x[0], w)
