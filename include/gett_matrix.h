@@ -19,7 +19,8 @@
  * entry points describe tensors the same way).
  *
  * Calls enqueue work on `stream` (a hipStream_t, NULL: the default stream)
- * and return.  Errors are statuses; nothing is thrown.  Workspaces are the
+ * and return.  Errors are statuses; nothing is thrown.  Extents that need more
+ * threads than a launch has (2^32) are GETT_ERROR_NOT_SUPPORTED.  Workspaces are the
  * library's own, one per device and stream, as for gett_contract: a call that
  * needs more than the stream's workspace holds allocates, which is refused
  * with GETT_ERROR_NOT_SUPPORTED, nothing enqueued, while `stream` captures a

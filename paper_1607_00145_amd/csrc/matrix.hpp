@@ -44,6 +44,12 @@ inline bool matrix_injective(int64_t rows, int64_t cols, int64_t sr, int64_t sc)
     return (__int128)inner * (extent - 1) < outer;
 }
 
+// A launch has fewer than 2^32 threads.
+inline bool fits_launch(int64_t blocks, int64_t threads)
+{
+    return blocks < ((int64_t)1 << 32) / threads;
+}
+
 // ------------------------------------------------------------ packed format ---
 
 constexpr int kTileK = 256;    // columns of one tile: 128 bytes of codes, 8 scales a row

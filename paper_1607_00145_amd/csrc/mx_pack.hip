@@ -325,7 +325,7 @@ template <typename T> Job<T> job_of(QuantizeJob q)
     const int64_t C = q.codesT ? Tile<true>::C : Tile<false>::C;
     const int64_t tilesR = ((q.codesT ? mx_tiles(q.rows) * kTileK : q.rows) + R - 1) / R;
     const int64_t tilesC = ((q.codes ? mx_tiles(q.cols) * kTileK : q.cols) + C - 1) / C;
-    const int64_t blocks = tilesR * tilesC < INT32_MAX / 2 ? tilesR * tilesC : 0;
+    const int64_t blocks = fits_launch(tilesR * tilesC, kThreads) ? tilesR * tilesC : 0;
     return {static_cast<const T *>(q.X), q.sr, q.sc, (int)q.rows, (int)q.cols, (int)tilesC,
             (int)blocks, recip(tilesC), q.sc == 1, static_cast<uint8_t *>(q.codes),
             static_cast<uint8_t *>(q.scales), static_cast<uint8_t *>(q.codesT),
@@ -339,7 +339,8 @@ gett_status_t quantize_typed(const QuantizeJob *q, int n, hipStream_t stream)
     Job<T> b = {};
     if (n == 2) b = job_of<T>(q[1]);
     if (a.blocks == 0 || (n == 2 && b.blocks == 0)) return GETT_ERROR_NOT_SUPPORTED;
-    if (n == 2 && (!a.codes != !b.codes || !a.codesT != !b.codesT)) {   // one launch each
+    if (n == 2 && (!a.codes != !b.codes || !a.codesT != !b.codesT ||
+                   !fits_launch((int64_t)a.blocks + b.blocks, kThreads))) {   // one launch each
         const gett_status_t st = quantize_typed<T>(q, 1, stream);
         return st == GETT_SUCCESS ? quantize_typed<T>(q + 1, 1, stream) : st;
     }
@@ -437,7 +438,7 @@ gett_status_t gett_mx_dequantize(gett_dtype_t dtype, int64_t rows, int64_t cols,
         return GETT_ERROR_INVALID_VALUE;
     const int64_t tilesC = (cols + Tile<false>::C - 1) / Tile<false>::C;
     const int64_t tiles = (rows + Tile<false>::R - 1) / Tile<false>::R * tilesC;
-    if (tiles >= INT32_MAX) return GETT_ERROR_NOT_SUPPORTED;
+    if (!fits_launch(tiles, kThreads)) return GETT_ERROR_NOT_SUPPORTED;
     hipStream_t s = static_cast<hipStream_t>(stream);
     hipError_t e;
     if (dtype == GETT_FLOAT32)

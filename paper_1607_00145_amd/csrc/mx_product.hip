@@ -135,7 +135,6 @@ template <typename T, typename S> hipError_t tile_launch(const TileJob<T> *j, in
     if (e != hipSuccess) return e;
     TileJob<T> none = {};
     const int64_t blocks = (int64_t)j[0].blocks + (n == 2 ? j[1].blocks : 0);
-    if (blocks >= INT32_MAX) return hipErrorInvalidValue;
     hipLaunchKernelGGL(k, dim3((unsigned)blocks), dim3(S::THREADS), S::lds(kPanelMx), stream, j[0],
                        n == 2 ? j[1] : none);
     return hipGetLastError();
@@ -401,7 +400,8 @@ hipError_t contract_typed(const Product *p, int n, float *slots, int *counters, 
                : shape == 1 ? tile_launch<T, Mid>(j, count, stream)
                             : tile_launch<T, Small>(j, count, stream);
     };
-    if (n == 2 && !p[0].few && !p[1].few && p[0].plan.shape == p[1].plan.shape)
+    if (n == 2 && !p[0].few && !p[1].few && p[0].plan.shape == p[1].plan.shape &&
+        fits_launch((int64_t)jobs[0].blocks + jobs[1].blocks, Big::THREADS))
         return launch(jobs, 2, p[0].plan.shape);
     for (int i = 0; i < n; ++i)
         if (!p[i].few) {
@@ -421,13 +421,26 @@ gett_status_t contract_launch(const Product *p, int n, float *slots, int *counte
     return e == hipSuccess ? GETT_SUCCESS : GETT_ERROR_HIP;
 }
 
+// Whether a product goes into one launch.
+bool launchable(const Product &p)
+{
+    if (p.few) return fits_launch((p.B.rows + kFewCols - 1) / kFewCols, kFewWaves * 64);
+    const int64_t edge = p.plan.shape == 0 ? Big::BM : p.plan.shape == 1 ? Mid::BM : Small::BM;
+    const int64_t tm = (p.A.rows + edge - 1) / edge, tn = (p.B.rows + edge - 1) / edge;
+    PanelGrid g;
+    return panel_grid(g, 1, tm, tn, tm * tn, p.plan.cut, (int)mx_tiles(p.k), nullptr, nullptr) &&
+           fits_launch(p.plan.cut.blocks, p.plan.shape == 0 ? Big::THREADS : Mid::THREADS);
+}
+
 // The stream's workspace for a call: `before` bytes of its own, then the slots
-// of its products.
+// of its products; refused, before anything is enqueued, where a product has too
+// many tiles for a launch.
 gett_status_t product_workspace(const Product *p, int n, int64_t before, hipStream_t stream,
                                 Partials &w)
 {
     int64_t bytes = before, counters = 0;
     for (int i = 0; i < n; ++i) {
+        if (!launchable(p[i])) return GETT_ERROR_NOT_SUPPORTED;
         bytes += p[i].plan.slotBytes;
         counters += p[i].plan.counters;
     }
@@ -552,6 +565,7 @@ gett_status_t gett_mx_apply(int64_t m, int64_t n, int64_t k, double alpha, gett_
     if (overlaps(C, bytesC, A, bytesA) || !clear_of(C, bytesC, codes_B, scales_B, n, k))
         return GETT_ERROR_INVALID_VALUE;
     if (packs_inside(m, n, k)) {
+        if (!fits_launch((n + kFewCols - 1) / kFewCols, kFewWaves * 64)) return GETT_ERROR_NOT_SUPPORTED;
         const Packed W = {codes_B, scales_B, n};
         hipError_t e;
         if (dtype == GETT_FLOAT32)

@@ -590,6 +590,7 @@ struct Choice {
     int shape;
     PanelCut cut;
     int64_t slotBytes;
+    bool launchable;   // not too many tiles for a launch
 };
 // A short product's price beside panel_cut's, which leave out a launch's fixed
 // time: that is 1.3 us shorter here, and a wavefront's panel takes 0.65, with two
@@ -617,7 +618,13 @@ template <int STEP> Choice choose(int64_t batch, int64_t m, int64_t n, int64_t p
     for (int i = 1; i < 4; ++i)
         if (c[i].us < c[s].us) s = i;
     const int64_t tile[4] = {Big::TILE, Mid::TILE, Small::TILE, 0};
-    return {s, c[s], c[s].shared() * c[s].slices * tile[s] * 4};
+    const int64_t edge[4] = {Big::BM, Mid::BM, Small::BM, kShortE};
+    const int64_t threads[4] = {Big::THREADS, Mid::THREADS, Small::THREADS, kShortThreads};
+    PanelGrid g;
+    const bool ok = panel_grid(g, batch, (m + edge[s] - 1) / edge[s], (n + edge[s] - 1) / edge[s],
+                               tile_count<STEP>(edge[s], m, n), c[s], (int)panels, nullptr, nullptr);
+    return {s, c[s], c[s].shared() * c[s].slices * tile[s] * 4,
+            ok && fits_launch(c[s].blocks, threads[s])};
 }
 
 struct Workspace {
@@ -890,6 +897,7 @@ template <typename T>
 gett_status_t small_launch(const Problem &P, const Stack<const T> &G, const Stack<T> &O)
 {
     constexpr auto k = orth_small_kernel<T>;
+    if (!fits_launch(P.batch, kSmallWaves * 64)) return GETT_ERROR_NOT_SUPPORTED;
     if (allow_dynamic_lds<k>(kSmallLds) != hipSuccess) return GETT_ERROR_HIP;
     hipLaunchKernelGGL(k, dim3((unsigned)P.batch), dim3(kSmallWaves * 64),
                        (size_t)small_lds(P.m, P.n), P.stream, G, O, P.m, P.n, P.eps, P.steps,
@@ -912,8 +920,8 @@ gett_status_t orthogonalize_typed(const Problem &P, Stack<const T> G, Stack<T> O
     const int64_t head = (P.batch * blocks * 8 + 255) / 256 * 256;
     const int64_t startM = (m + kStart - 1) / kStart, startN = (n + kStart - 1) / kStart;
     const int64_t copies = ((int64_t)m * n * P.batch + 255) / 256;
-    if (P.batch * startM * startN >= INT32_MAX || P.batch * blocks >= INT32_MAX ||
-        copies >= INT32_MAX)
+    if (!fits_launch(P.batch * startM * startN, kNormThreads) ||
+        !fits_launch(P.batch * blocks, kNormThreads) || !fits_launch(copies, 256))
         return GETT_ERROR_NOT_SUPPORTED;
     // without a quintic term to speak of S^2 is not needed
     const bool quintic = fabs(P.c) * 0x1p40 > fabs(P.b);
@@ -922,6 +930,7 @@ gett_status_t orthogonalize_typed(const Problem &P, Stack<const T> G, Stack<T> O
     const Choice update = choose<kUpdate>(P.batch, m, n, panelsS);
     int64_t slotBytes = 0, counters = 0;
     for (const Choice *c : {&gram, &quad, &update}) {
+        if (P.steps > 0 && !c->launchable) return GETT_ERROR_NOT_SUPPORTED;
         slotBytes = slotBytes > c->slotBytes ? slotBytes : c->slotBytes;
         counters = counters > c->cut.shared() ? counters : c->cut.shared();
     }
