@@ -1085,7 +1085,11 @@ gett_status_t gett_orthogonalize(gett_dtype_t dtype, int64_t batch, int64_t rows
     // (matrices may interleave, as the column slices of a weight's heads do)
     const int64_t extents[3] = {batch, rows, cols};
     const int64_t strides[3] = {ostride_batch, ostride_row, ostride_col};
-    if (!strides_injective(3, extents, strides)) return GETT_ERROR_NOT_SUPPORTED;
+    try {   // (it takes a little host memory)
+        if (!strides_injective(3, extents, strides)) return GETT_ERROR_NOT_SUPPORTED;
+    } catch (...) {
+        return GETT_ERROR_ALLOC;
+    }
     const bool same = G == O && stride_row == ostride_row && stride_col == ostride_col &&
                       stride_batch == ostride_batch;
     if (!same && overlaps(G, spanG, O, spanO)) return GETT_ERROR_INVALID_VALUE;

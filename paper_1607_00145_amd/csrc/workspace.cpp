@@ -65,9 +65,11 @@ gett_status_t stream_workspace(hipStream_t stream, uint64_t counters, uint64_t t
     int dev = 0;
     if (hipGetDevice(&dev) != hipSuccess) return GETT_ERROR_HIP;
     Buffers *found;
-    {
+    try {   // (a new entry takes host memory)
         std::lock_guard<std::mutex> lock(g_mutex);
         found = &g_buffers[{dev, stream}];
+    } catch (...) {
+        return GETT_ERROR_ALLOC;
     }
     Buffers &b = *found;
     out.hold = std::unique_lock<std::mutex>(b.use);

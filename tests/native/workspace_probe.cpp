@@ -4,7 +4,9 @@
 #include <hip/hip_runtime_api.h>
 #include <stdint.h>
 #include <stdio.h>
+#include <stdlib.h>
 
+#include <new>
 #include <set>
 
 #include "plan.hpp"
@@ -13,7 +15,17 @@ namespace {
 std::set<void *> g_live;
 int g_synced = 0;
 hipStreamCaptureStatus g_capture = hipStreamCaptureStatusNone;
+bool g_memory = true;   // false: host allocations fail
 }  // namespace
+
+void *operator new(size_t n)
+{
+    void *p = g_memory ? malloc(n) : nullptr;
+    if (!p) throw std::bad_alloc();
+    return p;
+}
+void operator delete(void *p) noexcept { free(p); }
+void operator delete(void *p, size_t) noexcept { free(p); }
 
 extern "C" {
 hipError_t hipGetDevice(int *d)
@@ -110,5 +122,15 @@ int main()
     Got refused = ask(3, 8, 1 << 26, true), same = ask(3, 8, 1 << 24);
     check("growth inside a capture is refused", refused.status == GETT_ERROR_NOT_SUPPORTED &&
                                                     same.tiles == more.tiles && live(same.tiles));
+
+    // no host memory for a new stream's entry: a status, not an exception
+    gett_status_t none = GETT_SUCCESS;
+    g_memory = false;
+    try {
+        none = ask(4, 8, 1 << 20).status;
+    } catch (...) {
+    }
+    g_memory = true;
+    check("no host memory is a status", none == GETT_ERROR_ALLOC);
     return g_failed != 0;
 }
