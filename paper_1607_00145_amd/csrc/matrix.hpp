@@ -115,3 +115,17 @@ __device__ __forceinline__ uint32_t codes8(const float *x, float scale)
 }
 
 }  // namespace gett
+
+// Which kernels a call takes, from sizes alone (no HIP call): for tests, which
+// assert that they run the variant that they mean to.  Exported, but not part of
+// gett_matrix.h.
+extern "C" {
+// of a product of packed matrices into a row-major C (few rows: edge 0)
+struct gett_tiles {
+    int64_t edge, slices, shared, workgroups;   // slices of each shared tile
+};
+void gett_mx_tiles(int64_t m, int64_t n, int64_t k, struct gett_tiles *out);
+// of S, b S + c S^2 and the update; edge 32: blocks whose wavefronts share K;
+// edge 0: the whole matrix in one workgroup
+void gett_orthogonalize_tiles(int64_t batch, int64_t rows, int64_t cols, struct gett_tiles out[3]);
+}

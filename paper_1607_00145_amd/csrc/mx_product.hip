@@ -521,6 +521,16 @@ bool clear_of(const void *C, int64_t bytesC, const void *codes, const void *scal
 
 extern "C" {
 
+void gett_mx_tiles(int64_t m, int64_t n, int64_t k, struct gett_tiles *out)
+{
+    using namespace gett;
+    const Product p = product_of({nullptr, nullptr, m}, {nullptr, nullptr, n}, k, nullptr, n, 1);
+    const PanelCut &c = p.plan.cut;
+    if (p.few) *out = {0, 1, 0, (n + kFewCols - 1) / kFewCols};
+    else *out = {p.plan.shape == 0 ? Big::BM : p.plan.shape == 1 ? Mid::BM : Small::BM, c.slices,
+                 c.shared(), c.blocks};
+}
+
 gett_status_t gett_mx_contract(int64_t m, int64_t n, int64_t k, double alpha,
                                const void *codes_A, const void *scales_A, const void *codes_B,
                                const void *scales_B, double beta, gett_dtype_t dtype, void *C,

@@ -1056,6 +1056,23 @@ bool orth_in_range(double a, double b, double c, int steps)
 
 extern "C" {
 
+void gett_orthogonalize_tiles(int64_t batch, int64_t rows, int64_t cols, struct gett_tiles out[3])
+{
+    using namespace gett;
+    const int64_t m = rows < cols ? rows : cols, n = rows < cols ? cols : rows;
+    if (small_fits(m, n)) {
+        out[0] = out[1] = out[2] = {0, 1, 0, batch};
+        return;
+    }
+    const auto put = [](const auto &c) -> gett_tiles {
+        const int64_t edge[4] = {Big::BM, Mid::BM, Small::BM, kShortE};
+        return {edge[c.shape], c.cut.slices, c.cut.shared(), c.cut.blocks};
+    };
+    out[0] = put(choose<kGram>(batch, m, m, panel_count(n)));
+    out[1] = put(choose<kPoly>(batch, m, m, panel_count(m)));
+    out[2] = put(choose<kUpdate>(batch, m, n, panel_count(m)));
+}
+
 gett_status_t gett_orthogonalize(gett_dtype_t dtype, int64_t batch, int64_t rows, int64_t cols,
                                  const void *G, int64_t stride_batch, int64_t stride_row,
                                  int64_t stride_col, double a, double b, double c, double eps,
