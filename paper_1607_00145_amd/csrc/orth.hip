@@ -21,7 +21,10 @@
 // entries down to 2^-26 normal.  A matrix is held as two halves, hi + lo (22
 // bits; products in panel.hpp, sums in 32 bits), for every type: the result is
 // as close to the 64-bit one as that of products in 32 bits (1.5e-6 of its norm
-// for both at 512 x 517).  One half would not do for bf16 either: its fifteen
+// for both at 512 x 517).  The low part's grid ends at 2^-36, which the steps
+// magnify by a^steps in the directions of small numbers: beside one element 1e6
+// times the others the error is 1.5e-6 where 32 bits leave 2e-7 (512 x 512).  A
+// third part would cost three more products.  One half would not do for bf16 either: its fifteen
 // roundings leave 1.1e-3 to 2.9e-3 of the norm beside the 1.7e-3 that rounding
 // the result costs.
 //
