@@ -154,6 +154,12 @@ def _device(name, t):
         raise ValueError(f"{name} must be a device tensor")
 
 
+def _written(t):
+    """Tells autograd that a given tensor's values have changed."""
+    if not t.is_inference():
+        _torch.autograd.graph.increment_version(t)
+
+
 def _elsewhere(first, *others):
     """Makes current the device that all of a call's tensors (or None) lie on,
     where it is not: the call is then made again (the library launches and keeps
@@ -257,7 +263,8 @@ class MXTensor:
             if there is not None:
                 with there:
                     return self.dequantize(dtype, out)
-        if out is None:
+        given = out is not None
+        if not given:
             dtype = dtype or _torch.float32
             code = _code(dtype)
             out = _torch.empty((r, c), dtype=dtype, device=self.device)
@@ -271,6 +278,8 @@ class MXTensor:
                                        _package._current_stream())
         if st != 0:
             raise GettError(st, "gett_mx_dequantize")
+        if given:
+            _written(out)
         return out
 
 
@@ -342,7 +351,8 @@ def mx_matmul(a, b, C=None, alpha: float = 1.0, beta: float = 0.0, dtype=None):
         if there is not None:
             with there:
                 return mx_matmul(a, b, C, alpha, beta, dtype)
-    if C is None:
+    given = C is not None
+    if not given:
         if beta != 0:
             raise ValueError("beta != 0 needs C")
         if dtype is None:
@@ -362,6 +372,8 @@ def mx_matmul(a, b, C=None, alpha: float = 1.0, beta: float = 0.0, dtype=None):
                                   beta, code, C.data_ptr(), sm, sn, _package._current_stream())
     if st != 0:
         raise GettError(st, "gett_mx_contract" if packed else "gett_mx_apply")
+    if given:
+        _written(C)
     return C
 
 
@@ -485,7 +497,8 @@ def orthogonalize(G, steps: int = 5, coefficients=(3.4445, -4.7750, 2.0315), eps
     if there is not None:
         with there:
             return orthogonalize(G, steps, coefficients, eps, out)
-    if out is None:
+    given = out is not None
+    if not given:
         out = _torch.empty(G.shape, dtype=G.dtype, device=G.device)
     elif out.shape != G.shape or out.dtype != G.dtype:
         raise ValueError("out differs in shape or dtype")
@@ -514,4 +527,6 @@ def orthogonalize(G, steps: int = 5, coefficients=(3.4445, -4.7750, 2.0315), eps
         raise GettError(st, "gett_orthogonalize")
     if copy is not None:
         out.copy_(copy.view(out.shape))
+    elif given:
+        _written(out)
     return out

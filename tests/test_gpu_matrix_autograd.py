@@ -101,3 +101,24 @@ def test_checkpointing_recomputes_the_packed_operands(gpu):
     got = torch.autograd.grad(y, (x, w), dy)
     for a, b in zip(got, want):
         assert torch.equal(a, b)
+
+
+def test_results_written_into_a_saved_tensor_are_noticed(gpu):
+    """As torch's own operations in place: a backward pass that needs the old
+    values says that they are gone."""
+    import torch
+    a, b = torch.randn(40, 64, device=gpu), g.mx_quantize(torch.randn(48, 64, device=gpu))
+    q, G = g.mx_quantize(a), torch.randn(40, 64, device=gpu)
+    writes = [((40, 48), lambda t: g.mx_matmul(a, b, t)), ((40, 48), lambda t: g.mx_matmul(q, b, t, beta=1.0)),
+              ((40, 64), lambda t: q.dequantize(out=t)), ((40, 64), lambda t: g.orthogonalize(G, out=t)),
+              ((40, 64), lambda t: g.orthogonalize(t, out=t)),
+              ((2, 20, 64), lambda t: g.orthogonalize(t, out=t))]
+    for shape, write in writes:
+        t = torch.randn(shape, device=gpu)
+        v = torch.randn(shape, device=gpu, requires_grad=True)
+        y = (t * v).sum()
+        write(t)
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            y.backward()
+        with torch.inference_mode():      # tensors without a version
+            write(torch.zeros(shape, device=gpu))
