@@ -44,6 +44,7 @@ def calls(monkeypatch):
     monkeypatch.setattr(matrix, "_bound", Library())
     monkeypatch.setattr(matrix, "_current_device", lambda: now[0], raising=False)
     monkeypatch.setattr(matrix._package, "_current_stream", lambda: 0)
+    monkeypatch.setattr(matrix, "_written", lambda t: None)   # (they are no tensors)
     monkeypatch.setattr(torch.cuda, "device", device)
     return made
 
