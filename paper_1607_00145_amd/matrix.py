@@ -13,11 +13,8 @@ from __future__ import annotations
 
 import ctypes
 import math
-import sys
 
 from . import GETT_FLOAT32, GettError, load_library
-
-_package = sys.modules[__package__]   # its _current_stream rebinds itself on the first call
 
 GETT_BFLOAT16 = 2
 GETT_FLOAT16 = 3
@@ -125,15 +122,18 @@ def gett_mx_linear_grad(m: int, n: int, k: int, dtype_Y: int, dY: int, stride_ym
 # when asked for, and the C functions are called directly.
 
 _torch = None
-_current_device = None
+_current_device = _stream = None   # the current device; torch's current stream on one
 _codes = {}
 
 
 def _start():
     """torch and the element types' codes, on the first use."""
-    global _torch, _current_device
+    global _torch, _current_device, _stream
     import torch
-    _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+    c = torch._C
+    _current_device = getattr(c, "_cuda_getDevice", torch.cuda.current_device)
+    _stream = getattr(c, "_cuda_getCurrentRawStream",
+                      lambda device: torch.cuda.current_stream(device).cuda_stream)
     _codes.update({torch.float32: GETT_FLOAT32, torch.bfloat16: GETT_BFLOAT16,
                    torch.float16: GETT_FLOAT16})
     _torch = torch
@@ -258,7 +258,8 @@ class MXTensor:
         r, c = self.rows, self.cols
         if _torch is None:
             _start()
-        if out is not None or self._device != _current_device():
+        i = self._device
+        if out is not None or i != _current_device():
             there = _elsewhere(self, out)
             if there is not None:
                 with there:
@@ -275,7 +276,7 @@ class MXTensor:
             code, _, _, sr, sc = _matrix("out", out)
             _no_gradient("dequantize", out)
         st = _bound.gett_mx_dequantize(code, r, c, self._codes, self._scales, out.data_ptr(), sr, sc,
-                                       _package._current_stream())
+                                       _stream(i))
         if st != 0:
             raise GettError(st, "gett_mx_dequantize")
         if given:
@@ -317,7 +318,7 @@ def mx_quantize(x, along: str = "cols"):
         codes_t = p + n + s
         scales_t = codes_t + nt
     st = _bound.gett_mx_quantize(code, r, c, x.data_ptr(), sr, sc, codes, scales, codes_t, scales_t,
-                                 _package._current_stream())
+                                 _stream(i))
     if st != 0:
         raise GettError(st, "gett_mx_quantize")
     if along == "cols":
@@ -346,7 +347,8 @@ def mx_matmul(a, b, C=None, alpha: float = 1.0, beta: float = 0.0, dtype=None):
         raise ValueError(f"a has {k} columns, b {b.cols}")
     if _torch is None:
         _start()
-    if C is not None or not b._device == a.get_device() == _current_device():
+    i = b._device
+    if C is not None or not i == a.get_device() == _current_device():
         there = _elsewhere(a, b, C)
         if there is not None:
             with there:
@@ -366,10 +368,10 @@ def mx_matmul(a, b, C=None, alpha: float = 1.0, beta: float = 0.0, dtype=None):
         _no_gradient("mx_matmul", C)
     if packed:
         st = _bound.gett_mx_contract(m, n, k, alpha, a._codes, a._scales, b._codes, b._scales, beta,
-                                     code, C.data_ptr(), sm, sn, _package._current_stream())
+                                     code, C.data_ptr(), sm, sn, _stream(i))
     else:
         st = _bound.gett_mx_apply(m, n, k, alpha, code_a, a.data_ptr(), sr, sc, b._codes, b._scales,
-                                  beta, code, C.data_ptr(), sm, sn, _package._current_stream())
+                                  beta, code, C.data_ptr(), sm, sn, _stream(i))
     if st != 0:
         raise GettError(st, "gett_mx_contract" if packed else "gett_mx_apply")
     if given:
@@ -405,7 +407,7 @@ def _linear_forward(x, w, save_x, save_w):
         buf = _torch.empty(a + b + c + d, dtype=_torch.uint8, device=x.device)
     xt, xs, wt, ws = _addresses(parts, buf)
     st = _bound.gett_mx_linear(m, n, k, cx, x.data_ptr(), sxm, sxk, cw, w.data_ptr(), swn, swk,
-                               y.data_ptr(), n or 1, 1, xt, xs, wt, ws, _package._current_stream())
+                               y.data_ptr(), n or 1, 1, xt, xs, wt, ws, _stream(x.get_device()))
     if st != 0:
         raise GettError(st, "gett_mx_linear")
     return y, buf, parts
@@ -452,7 +454,7 @@ def _linear_function():
         st = _bound.gett_mx_linear_grad(
             m, n, k, code, dy.data_ptr(), sm, sn, xt, xs, wt, ws,
             dx.data_ptr() if need_x else None, k or 1, 1, _codes[tw],
-            dw.data_ptr() if need_w else None, k or 1, 1, _package._current_stream())
+            dw.data_ptr() if need_w else None, k or 1, 1, _stream(dy.get_device()))
         if st != 0:
             raise GettError(st, "gett_mx_linear_grad")
         return dx, dw
@@ -522,7 +524,7 @@ def orthogonalize(G, steps: int = 5, coefficients=(3.4445, -4.7750, 2.0315), eps
     a, b, cc = coefficients
     st = _bound.gett_orthogonalize(code, n, r, c, g.data_ptr(), g.stride(0), gr, gc, a, b, cc, eps,
                                    int(steps), o.data_ptr(), o.stride(0), orow, oc,
-                                   _package._current_stream())
+                                   _stream(G.get_device()))
     if st != 0:
         raise GettError(st, "gett_orthogonalize")
     if copy is not None:

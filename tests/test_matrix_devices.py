@@ -32,7 +32,11 @@ def calls(monkeypatch):
 
     class Library:
         def __getattr__(self, name):
-            return lambda *args: made.append((name, now[0])) or 0
+            def call(*args):
+                assert args[-1] == 100 + now[0]      # the stream is the device's own
+                made.append((name, now[0]))
+                return 0
+            return call
 
     @contextlib.contextmanager
     def device(index):
@@ -43,7 +47,7 @@ def calls(monkeypatch):
     matrix._start()
     monkeypatch.setattr(matrix, "_bound", Library())
     monkeypatch.setattr(matrix, "_current_device", lambda: now[0], raising=False)
-    monkeypatch.setattr(matrix._package, "_current_stream", lambda: 0)
+    monkeypatch.setattr(matrix, "_stream", lambda index: 100 + index)
     monkeypatch.setattr(matrix, "_written", lambda t: None)   # (they are no tensors)
     monkeypatch.setattr(torch.cuda, "device", device)
     return made
