@@ -28,7 +28,13 @@
  * workspace of the stream it was captured on, which is left to it when a later
  * call gets a larger one; a replay has to be ordered with that stream's other
  * calls (on that stream, or by events), as calls from several streams would be
- * that share a workspace.
+ * that share a workspace.  A workspace is kept until the process ends, at the size
+ * of the largest call on its stream: 17/32 byte for each number that
+ * gett_mx_apply (more than 16 rows, or more than 8 of a large product),
+ * gett_mx_linear (X and W) and gett_mx_linear_grad (dY, twice) pack; for
+ * gett_orthogonalize, unless one workgroup takes a whole matrix, 12 rows cols + 8
+ * min(rows, cols)^2 bytes a matrix (335 MB for 4096 x 4096); and up to 64 MB
+ * for each product whose sums several workgroups share.
  *
  * The packed format ("MX4").  A matrix of `rows` x `cols` is packed along its
  * columns, the direction a product sums over.  Each run of 32 neighbours

@@ -3,9 +3,11 @@
 // and of float rows, quantised on the way, with a packed matrix.
 //
 // Many rows: tiles of C, the operands' panels through LDS (panel.hpp).  Bound:
-// the card's power under the matrix instructions; 8192 x 8192 x 8192 into bf16
-// takes 255 us (4.3 PFLOP/s; the instructions alone, on random operands in
-// registers, reach 6.2).  A tile's results go out as they lie, FN neighbours
+// the matrix units, busy for 54 % of the cycles of a clock that falls to 1.74 GHz;
+// 8192 x 8192 x 8192 into bf16 takes 253-263 us by card (4.2-4.3 PFLOP/s; the
+// instructions alone, on random operands in registers, reach 6.2).  Between few
+// rows and large tiles, tiles of 64 x 64 take their panels one after the other, on
+// few CUs: 48 x 1024 x 8192 12.9 us, 64 x 8192 x 4096 8.9.  A tile's results go out as they lie, FN neighbours
 // a lane.
 // Few rows (up to 32): bound by B's bytes, and below some 16 MB of them by the
 // launch and two memory latencies.  A workgroup takes 32 rows of B (32 columns

@@ -6,14 +6,15 @@
 // Bound: matrix instructions.  S and S^2 are symmetric, so only the tiles on
 // and below the diagonal are computed and the others mirrored: m^2 n + m^3 +
 // 2 m^2 n operations per step instead of 2 m^2 n + 2 m^3 + 2 m^2 n, each three
-// MFMA operations where numbers are held in two parts.
+// MFMA operations, since numbers are held in two parts.
 //
-// 4096 x 4096, five steps: 3.74 ms; a step's three products 200-214,
-// 200-215 and 363-394 us (1.0 to 1.1 PFLOP/s of MFMA operations; the update's
-// panels alone, without reading the addend and writing both orientations, 1.2),
-// the norm 13.5 and the start 41-47.
-// Mid-sized matrices are chains of launches, each a load latency, a short K and
-// the stores, waiting for the one before.
+// 4096 x 4096, five steps: 3.64-3.81 ms by card, in every type; a step's three
+// products 193-214, 195-215 and 346-394 us (1.0 to 1.2 PFLOP/s of MFMA operations;
+// the update's panels alone, without reading the addend and writing both
+// orientations, 1.2), the norm 13.5 and the start 41-47.
+// Mid-sized matrices are chains of 17 launches, each a load latency, a short K and
+// the stores, waiting for the one before: 517 x 1000 129 us, products of 5 to 12;
+// 1024 x 1024 189, 2048 x 2048 800-890.
 //
 // Numbers.  |X| <= 1 at the start and every singular value stays below 3
 // (gett_orthogonalize refuses other polynomials), so all entries of X, S and
@@ -24,9 +25,9 @@
 // for both at 512 x 517).  The low part's grid ends at 2^-36, which the steps
 // magnify by a^steps in the directions of small numbers: beside one element 1e6
 // times the others the error is 1.5e-6 where 32 bits leave 2e-7 (512 x 512).  A
-// third part would cost three more products.  One half would not do for bf16 either: its fifteen
-// roundings leave 1.1e-3 to 2.9e-3 of the norm beside the 1.7e-3 that rounding
-// the result costs.
+// third part would cost three more products.  One half would not do for bf16
+// either: 4096 x 4096 would take 1.6 ms, but its fifteen roundings leave 1.1e-3 to
+// 2.9e-3 of the norm beside the 1.7e-3 that rounding the result costs.
 //
 // Every product has K along the rows of both operands: S from X, S^2 from S
 // (symmetric), B X from B and X^T.  So X is kept in both orientations, and
@@ -687,10 +688,14 @@ struct Problem {
 // ------------------------------------------------------------ small matrices ---
 //
 // A matrix whose X, X^T and S fit the 160 KB of a CU goes through all steps in
-// one workgroup: no launch and no memory between them.  us so and by launches
-// (in a graph, without the host's time for 17 launches): 12 x 64 x 128 floats
-// 30 / 58, 64 x 64 25 / 55, 600 x 64 x 128 94 / 227.  Bound: the latency of each step's three products,
-// of the LDS accesses between them and of their barriers.
+// one workgroup: no launch and no memory between them.  That wins up to the edge of
+// what fits, for one matrix and for many; us so and by launches (in a graph,
+// without the host's time for 17 launches), floats, bf16 the same within 6 %:
+// 64 x 64 24 / 51, 12 x 64 x 128 30 / 55, and at the edge 32 x 576 49 / 54, 64 x 256
+// 41 / 55, 96 x 128 47 / 55; 12 of these 50 / 58, 41 / 58, 49 / 57; 200 of them 55 /
+// 156, 46 / 146, 54 / 188; 600 of them 169 / 384, 135 / 312, 154 / 396.  Bound: the
+// latency of each step's three products, of the LDS accesses between them and of
+// their barriers.
 //
 // Rows are padded to 32 (zeros, which stay zeros) and lie 16 bytes more than
 // their length apart, so that sixteen rows' pieces fall on different banks.  A
@@ -1040,7 +1045,7 @@ double largest_poly(double b, double c, double x1)
 
 }  // namespace
 
-// Singular values stay within the halves' range (orth.hip, Numbers); 1 % for
+// Singular values stay within the halves' range (Numbers, above); 1 % for
 // the products' rounding.
 bool orth_in_range(double a, double b, double c, int steps)
 {

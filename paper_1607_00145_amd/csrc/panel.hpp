@@ -42,9 +42,11 @@
 // Two stages do for the large tiles (three or four: the same time within 2 %);
 // small tiles, whose panels take less than a load's latency, have four.
 //
-// The large tiles are bound by the card's power: with the instructions alone
-// and operands of random bits the clock falls until they make 6.2 PFLOP/s in
-// 4 bits and 1.6 in halves.
+// Two things keep the large tiles from the instructions' peak, 10 PFLOP/s in 4 bits
+// and 2.5 in halves: the clock, 1.67-1.89 GHz under them where 2.4 is the highest (the
+// card's power; the instructions alone, on operands of random bits, make 6.2 and 1.6),
+// and the matrix units, which are busy for 50-54 % (4 bits) and 58-64 % (two parts) of
+// the cycles: eight wavefronts read LDS and wait at one barrier together.
 #pragma once
 #include <type_traits>
 
