@@ -1,6 +1,6 @@
 """What becomes of the per-stream workspace that a captured graph points at
-when a later call needs more, and its errors (csrc/workspace.cpp, built here with g++ against a
-record of its HIP calls; no GPU)."""
+when a later call needs more, and its errors (csrc/workspace.cpp, built here
+with g++ against a record of its HIP calls; no GPU)."""
 import os
 import subprocess
 
