@@ -10,7 +10,8 @@ used for device memory and streams only.
     p(a, b, c, alpha=1.0, beta=0.0)          # enqueued on torch's current stream
 
 ``matrix`` has the matrix operators for training and serving in 4 bits
-(``include/gett_matrix.h``); its names are the package's too.
+(``include/gett_matrix.h``), ``layers`` those of a feed-forward layer in 16 and
+32 bits (``include/gett_layers.h``); their names are the package's too.
 """
 from __future__ import annotations
 
@@ -461,3 +462,9 @@ from .matrix import (GETT_BFLOAT16, GETT_FLOAT16, MXTensor, gett_mx_apply,  # no
                      gett_mx_contract, gett_mx_dequantize, gett_mx_linear, gett_mx_linear_grad,
                      gett_mx_quantize, gett_mx_size,
                      gett_orthogonalize, mx_linear, mx_matmul, mx_quantize, orthogonalize)
+
+# the operators of include/gett_layers.h
+from .layers import (Routing, combine, dropout, expert_linear, gett_combine,  # noqa: E402
+                     gett_combine_grad, gett_dropout, gett_dropout_t, gett_experts,
+                     gett_experts_grad, gett_linear, gett_linear_grad, gett_route, gett_route_grad,
+                     linear, route)

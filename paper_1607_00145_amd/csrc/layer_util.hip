@@ -1,0 +1,273 @@
+// layer_util.hip -- the passes around the products of product.hpp, all bound by
+// the bytes that they move: copies onto the 16-byte grid, the gradient of an
+// epilogue, sums of columns, sums of the experts' rows.
+#include "layer_util.hpp"
+
+namespace gett {
+
+namespace {
+
+// --------------------------------------------------------------------- copy ---
+
+// Piece after piece of 16 bytes of a copy with rows of `ld` numbers, zeros behind a
+// row's last column.  A row of the copy is row order[.] / choices of the source where
+// there is an order (rows of no expert stay unwritten; nothing reads them).
+template <typename T>
+__global__ __launch_bounds__(256) void layer_copy_kernel(CopyJob j)
+{
+    constexpr int EP = 16 / sizeof(T);
+    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (id >= (int64_t)j.rows * j.pieces) return;
+    const int64_t row = id < INT32_MAX ? quotient((uint32_t)id, j.pieces, j.piecesInv) : id / j.pieces;
+    const int col = (int)(id - row * j.pieces) * EP;
+    int64_t from = row;
+    if (j.order) {
+        const int32_t r = j.order[row];
+        if (r < 0) return;
+        from = quotient(min((uint32_t)r, (uint32_t)j.rows - 1), j.choices, j.choicesInv);
+    }
+    int64_t at = from * j.ld;
+    if (j.perMatrix) {
+        const int64_t z = quotient((uint32_t)row, j.perMatrix, j.perMatrixInv);
+        at = z * j.step + (row - z * j.perMatrix) * j.ld;
+    }
+    const T *src = reinterpret_cast<const T *>(j.src) + at + col;
+    Run<T, EP> v;
+    if (col + EP <= j.cols) {
+        v = *reinterpret_cast<const Run<T, EP> *>(src);
+    } else {
+#pragma unroll
+        for (int i = 0; i < EP; ++i) v.v[i] = col + i < j.cols ? src[i] : from_float<T>(0.0f);
+    }
+    *reinterpret_cast<i4 *>(reinterpret_cast<T *>(j.dst) + row * j.pieces * EP + col) =
+        __builtin_bit_cast(i4, v);
+}
+
+// ------------------------------------------------------- epilogue's gradient ---
+
+constexpr int kSlopeRows = 64;   // rows of a workgroup
+constexpr int kSlopeCols = 256;  // columns: 32 lanes of eight
+
+// dz = dropout(dy) act'(z), written with zeros behind the last column, and the sums
+// of each column over the workgroup's rows: eight rows at a time, the eight
+// partial sums of a column added in the same order each time.
+template <typename T>
+__global__ __launch_bounds__(256) void layer_slope_kernel(SlopeJob j)
+{
+    __shared__ float sums[8][kSlopeCols];
+    const int lane = (int)threadIdx.x & 31, strip = (int)threadIdx.x >> 5;
+    const int slot = (int)quotient(blockIdx.x, j.across, j.acrossInv);
+    int begin = slot * kSlopeRows, end = j.m;
+    if (j.offsets) {
+        const int e = expert_of_slot<kSlopeRows>(j.offsets, j.experts, j.m, slot);
+        const int b = expert_offset(j.offsets, e, j.m);
+        begin = b + (slot - (b / kSlopeRows + e)) * kSlopeRows;
+        end = e == j.experts ? 0 : expert_offset(j.offsets, e + 1, j.m);   // (none behind the last)
+    }
+    if (begin + kSlopeRows < end) end = begin + kSlopeRows;
+    const int col0 = ((int)blockIdx.x - slot * j.across) * kSlopeCols, col = col0 + lane * 8;
+    const int left = j.n - col;
+    const uint64_t key = j.drop.cut ? j.drop.key() : 0;
+    float total[8] = {};
+    if (left > 0) {
+        for (int row = begin + strip; row < end; row += 8) {
+            float v[8];
+            load8(reinterpret_cast<const T *>(j.dY) + row * j.ldy + col, left, v);
+            if (j.activation != GETT_ACTIVATION_NONE) {
+                float z[8];
+                load8(reinterpret_cast<const T *>(j.Z) + row * j.ldz + col, left, z);
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (i < left) v[i] *= slope(j.activation, z[i]);
+            }
+            // (last: what is dropped is zero, whatever it was)
+            if (j.drop.cut) drop8(v, j.drop, key, (uint32_t)row, (uint32_t)col);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) total[i] += v[i];
+            if (j.dZ)
+                store8(reinterpret_cast<T *>(j.dZ) + row * j.ldd + col,
+                       j.ldd - col < 8 ? (int)(j.ldd - col) : 8, v);
+        }
+    }
+    if (!j.sums) return;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sums[strip][lane * 8 + i] = total[i];
+    __syncthreads();
+    const int c = col0 + (int)threadIdx.x;
+    if (c >= j.n) return;
+    float t = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) t += sums[i][threadIdx.x];
+    j.sums[(int64_t)slot * j.n + c] = t;
+}
+
+// A column's sum over the workgroups of layer_slope_kernel, of each expert.  Four
+// running sums, added in a fixed order.
+template <typename T>
+__global__ __launch_bounds__(256) void layer_sums_kernel(SlopeJob j, T *out)
+{
+    const int c = (int)blockIdx.x * 256 + (int)threadIdx.x, e = (int)blockIdx.y;
+    if (c >= j.n) return;
+    int first = 0, count = (j.m + kSlopeRows - 1) / kSlopeRows;
+    if (j.offsets) {
+        const int b = expert_offset(j.offsets, e, j.m), f = expert_offset(j.offsets, e + 1, j.m);
+        first = b / kSlopeRows + e;
+        count = f > b ? (f - b + kSlopeRows - 1) / kSlopeRows : 0;
+    }
+    const float *p = j.sums + (int64_t)first * j.n + c;
+    float t[4] = {};
+    int i = 0;
+    for (; i + 4 <= count; i += 4)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) t[x] += p[(int64_t)(i + x) * j.n];
+    for (; i < count; ++i) t[0] += p[(int64_t)i * j.n];
+    out[(int64_t)e * j.n + c] = from_float<T>((t[0] + t[1]) + (t[2] + t[3]));
+}
+
+// ------------------------------------------------------------------ combine ---
+
+// Y[t] = residual[t] + sum_j weights[t, j] H[place[t, j]], eight columns a lane, in
+// rising j.  H in T or, for sums of gradients, in 32 bits.
+template <typename T, typename H, typename W>
+__global__ __launch_bounds__(256) void combine_kernel(CombineJob j)
+{
+    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (id >= (int64_t)j.tokens * j.runs) return;
+    const int64_t t = id < INT32_MAX ? quotient((uint32_t)id, j.runs, j.runsInv) : id / j.runs;
+    const int col = (int)(id - t * j.runs) * 8, left = j.cols - col;
+    const uint32_t rows = (uint32_t)j.tokens * j.k;
+    float v[8] = {};
+    if (j.residual) load8(reinterpret_cast<const T *>(j.residual) + t * j.ldr + col, left, v);
+    for (int i = 0; i < j.k; ++i) {
+        const uint32_t p = (uint32_t)j.place[t * j.k + i];
+        if (p >= rows) continue;
+        const float w = j.weights ? to_float(reinterpret_cast<const W *>(j.weights)[t * j.k + i]) : 1.0f;
+        float x[8];
+        load8(reinterpret_cast<const H *>(j.H) + (int64_t)p * j.ldh + col, left, x);
+#pragma unroll
+        for (int c = 0; c < 8; ++c) v[c] += w * x[c];
+    }
+    store8(reinterpret_cast<T *>(j.Y) + t * j.ldy + col, left, v);
+}
+
+// A wavefront for each row (t, i): dH[place] = w dY[t] and dw = dY[t] . H[place]; and
+// the row of dH with the wavefront's own number is set to zero where it is no
+// expert's.
+template <typename T, typename W>
+__global__ __launch_bounds__(256) void combine_grad_kernel(CombineGradJob j)
+{
+    const int lane = (int)threadIdx.x & 63;
+    const uint32_t rows = (uint32_t)j.tokens * j.k;
+    const uint32_t r = blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (r >= rows) return;
+    T *dH = reinterpret_cast<T *>(j.dH);
+    if (dH && (int64_t)r >= expert_offset(j.offsets, j.experts, (int)rows)) {
+        const float zero[8] = {};
+        for (int c = lane * 8; c < j.cols; c += 512) store8(dH + r * j.ldd + c, j.cols - c, zero);
+    }
+    const uint32_t p = (uint32_t)j.place[r];
+    float sum = 0.0f;
+    if (p < rows) {
+        const T *dY = reinterpret_cast<const T *>(j.dY) + quotient(r, j.k, j.kInv) * j.ldy;
+        const float w = dH ? to_float(reinterpret_cast<const W *>(j.weights)[r]) : 0.0f;
+        for (int c = lane * 8; c < j.cols; c += 512) {
+            float g[8];
+            load8(dY + c, j.cols - c, g);
+            if (j.dweights) {
+                float x[8];
+                load8(reinterpret_cast<const T *>(j.H) + p * j.ldh + c, j.cols - c, x);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) sum += g[i] * x[i];
+            }
+            if (dH) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) g[i] *= w;
+                store8(dH + p * j.ldd + c, j.cols - c, g);
+            }
+        }
+    }
+    if (!j.dweights) return;
+#pragma unroll
+    for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
+    if (lane == 0) reinterpret_cast<W *>(j.dweights)[r] = from_float<W>(sum);
+}
+
+}  // namespace
+
+// ---------------------------------------------------------------- launchers ---
+
+gett_status_t copy_launch(gett_dtype_t t, const CopyJob &j, hipStream_t s)
+{
+    const int64_t n = (int64_t)j.rows * j.pieces;
+    if (n == 0) return GETT_SUCCESS;
+    if (!fits_launch((n + 255) / 256, 256)) return GETT_ERROR_NOT_SUPPORTED;
+    return with_type(t, [&](auto v) {
+        hipLaunchKernelGGL(layer_copy_kernel<decltype(v)>, dim3((unsigned)((n + 255) / 256)), dim3(256),
+                           0, s, j);
+        return launched(hipGetLastError());
+    });
+}
+
+int64_t slope_slots(int64_t m, int experts)
+{
+    return experts ? m / kSlopeRows + experts + 1 : (m + kSlopeRows - 1) / kSlopeRows;
+}
+gett_status_t slope_launch(gett_dtype_t t, SlopeJob j, hipStream_t s)
+{
+    const int64_t slots = slope_slots(j.m, j.offsets ? j.experts : 0);
+    const int64_t across = (j.n + kSlopeCols - 1) / kSlopeCols;
+    if (slots == 0 || across == 0) return GETT_SUCCESS;
+    if (!fits_launch(slots * across, 256)) return GETT_ERROR_NOT_SUPPORTED;
+    j.across = (int)across;
+    j.acrossInv = recip(across);
+    return with_type(t, [&](auto v) {
+        hipLaunchKernelGGL(layer_slope_kernel<decltype(v)>, dim3((unsigned)(slots * across)),
+                           dim3(256), 0, s, j);
+        return launched(hipGetLastError());
+    });
+}
+gett_status_t sums_launch(gett_dtype_t t, const SlopeJob &j, void *out, hipStream_t s)
+{
+    return with_type(t, [&](auto v) {
+        typedef decltype(v) T;
+        hipLaunchKernelGGL(layer_sums_kernel<T>,
+                           dim3((unsigned)((j.n + 255) / 256), (unsigned)(j.offsets ? j.experts : 1)),
+                           dim3(256), 0, s, j, static_cast<T *>(out));
+        return launched(hipGetLastError());
+    });
+}
+
+gett_status_t combine_launch(gett_dtype_t t, gett_dtype_t tH, gett_dtype_t tw, const CombineJob &j,
+                             hipStream_t s)
+{
+    const int64_t n = (int64_t)j.tokens * j.runs;
+    if (n == 0) return GETT_SUCCESS;
+    if (!fits_launch((n + 255) / 256, 256)) return GETT_ERROR_NOT_SUPPORTED;
+    return with_type(t, [&](auto v) {
+        typedef decltype(v) T;
+        auto launch = [&](auto h, auto w) {
+            hipLaunchKernelGGL((combine_kernel<T, decltype(h), decltype(w)>),
+                               dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, j);
+            return launched(hipGetLastError());
+        };
+        if (tH != t) return launch(float(), float());
+        return tw == t ? launch(T(), T()) : launch(T(), float());
+    });
+}
+gett_status_t combine_grad_launch(gett_dtype_t t, gett_dtype_t tw, const CombineGradJob &j, hipStream_t s)
+{
+    const int64_t n = (int64_t)j.tokens * j.k;
+    if (n == 0) return GETT_SUCCESS;
+    if (!fits_launch((n + 3) / 4, 256)) return GETT_ERROR_NOT_SUPPORTED;
+    return with_type(t, [&](auto v) {
+        typedef decltype(v) T;
+        auto launch = [&](auto w) {
+            hipLaunchKernelGGL((combine_grad_kernel<T, decltype(w)>), dim3((unsigned)((n + 3) / 4)),
+                               dim3(256), 0, s, j);
+            return launched(hipGetLastError());
+        };
+        return tw == t ? launch(T()) : launch(float());
+    });
+}
+
+}  // namespace gett

@@ -1,0 +1,143 @@
+// layer_util.hpp -- jobs of layer_util.hip's passes.
+#pragma once
+#include "product.hpp"
+
+namespace gett {
+
+// rows x cols numbers -> a copy on the 16-byte grid, `pieces` pieces a row
+struct CopyJob {
+    const void *src;
+    void *dst;
+    int64_t ld;              // of the source, elements
+    int rows, cols, pieces;
+    Recip piecesInv;
+    const int32_t *order;    // rows by expert of `choices` rows a token, or nullptr
+    int choices;
+    Recip choicesInv;
+    int perMatrix;           // rows of one of several matrices `step` apart (0: one matrix)
+    Recip perMatrixInv;
+    int64_t step;
+};
+gett_status_t copy_launch(gett_dtype_t t, const CopyJob &j, hipStream_t s);
+
+// dZ (or nullptr) and, per workgroup row (slot), the sums of its columns (or nullptr)
+struct SlopeJob {
+    const void *dY, *Z;
+    void *dZ;
+    float *sums;
+    int64_t ldy, ldz, ldd;
+    int m, n;
+    int activation;
+    Drop drop;
+    const int32_t *offsets;  // rows by expert, or nullptr
+    int experts;
+    int across;              // workgroups along the columns (set by the launch)
+    Recip acrossInv;
+};
+int64_t slope_slots(int64_t m, int experts);   // experts 0: no offsets
+gett_status_t slope_launch(gett_dtype_t t, SlopeJob j, hipStream_t s);
+gett_status_t sums_launch(gett_dtype_t t, const SlopeJob &j, void *out, hipStream_t s);
+
+struct CombineJob {
+    const void *H, *weights, *residual;
+    void *Y;
+    const int32_t *place;
+    int64_t ldh, ldr, ldy;
+    int tokens, k, cols, runs;   // runs of eight columns
+    Recip runsInv;
+};
+gett_status_t combine_launch(gett_dtype_t t, gett_dtype_t tH, gett_dtype_t tw, const CombineJob &j,
+                             hipStream_t s);
+
+struct CombineGradJob {
+    const void *dY, *H, *weights;
+    void *dH, *dweights;
+    const int32_t *place, *offsets;
+    int64_t ldy, ldh, ldd;
+    int tokens, k, cols, experts;
+    Recip kInv;
+};
+gett_status_t combine_grad_launch(gett_dtype_t t, gett_dtype_t tw, const CombineGradJob &j, hipStream_t s);
+
+gett_status_t product_launch_f32(ProductForm form, ProductGroups groups, ProductArgs g, hipStream_t s);
+gett_status_t product_launch_bf16(ProductForm form, ProductGroups groups, ProductArgs g, hipStream_t s);
+gett_status_t product_launch_f16(ProductForm form, ProductGroups groups, ProductArgs g, hipStream_t s);
+inline gett_status_t product_launch_of(gett_dtype_t t, ProductForm form, ProductGroups groups,
+                                       const ProductArgs &g, hipStream_t s)
+{
+    if (t == GETT_FLOAT32) return product_launch_f32(form, groups, g, s);
+    return t == GETT_BFLOAT16 ? product_launch_bf16(form, groups, g, s)
+                              : product_launch_f16(form, groups, g, s);
+}
+
+// ----------------------------------------------------------- host helpers ---
+
+// Parts of a stream's workspace, each on the 256-byte grid.
+struct Arena {
+    uint64_t bytes = 0;
+    int64_t take(int64_t n)
+    {
+        const int64_t at = (int64_t)bytes;
+        bytes += (uint64_t)round_up(n, 256);
+        return at;
+    }
+};
+
+// A matrix as an operand of a product: as it lies, or copied onto the 16-byte grid
+// with rows of `width` numbers, zeros behind the last column.
+struct Operand {
+    const char *p;
+    int64_t ld;        // bytes
+    int width;         // numbers of a row that may be read
+    int64_t copyAt;    // in the workspace, -1: not copied
+};
+inline int64_t piece_numbers(gett_dtype_t t) { return 16 / type_size(t); }
+// A tile's rows are reached by 32-bit offsets: 256 rows 16 MB apart at most.
+constexpr int64_t kDirectStride = (int64_t)1 << 24;
+inline bool on_grid(gett_dtype_t t, int64_t rows, int64_t cols, const void *p, int64_t stride)
+{
+    const int64_t item = type_size(t);
+    return (uintptr_t)p % 16 == 0 && cols % piece_numbers(t) == 0 &&
+           (rows <= 1 || (stride * item % 16 == 0 && stride * item < kDirectStride));
+}
+inline Operand operand_of(gett_dtype_t t, int64_t rows, int64_t cols, const void *p, int64_t stride,
+                          bool direct, Arena &a, int64_t copyRows)
+{
+    const int64_t item = type_size(t), width = round_up(cols, piece_numbers(t));
+    if (rows == 0 || cols == 0) return {nullptr, 16, 0, -1};
+    if (direct)
+        return {static_cast<const char *>(p), (rows > 1 ? stride : cols) * item, (int)cols, -1};
+    return {nullptr, width * item, (int)width, a.take(copyRows * width * item)};
+}
+
+// Enqueues the copy of an operand that is not on the grid, into its workspace.
+inline gett_status_t place_copy(gett_dtype_t t, Operand &o, const Partials &hold, int64_t rows,
+                                int64_t cols, const void *p, int64_t stride, hipStream_t s,
+                                const int32_t *order = nullptr, int choices = 1, int64_t perMatrix = 0,
+                                int64_t step = 0)
+{
+    if (o.copyAt < 0) return GETT_SUCCESS;
+    char *to = static_cast<char *>(hold.tiles) + o.copyAt;
+    o.p = to;
+    const int64_t pieces = o.width / piece_numbers(t);
+    const CopyJob j = {p, to, rows > 1 ? stride : cols, (int)rows, (int)cols, (int)pieces,
+                       recip(pieces), order, choices, recip(choices), (int)perMatrix,
+                       recip(perMatrix > 0 ? perMatrix : 1), step};
+    return copy_launch(t, j, s);
+}
+
+// A product's operands and sizes; its form and result are the caller's to fill in.
+inline ProductArgs product_args(const Operand &M, const Operand &N, int64_t m, int64_t n, int64_t k)
+{
+    ProductArgs g = {};
+    g.M = M.p;
+    g.N = N.p;
+    g.ldm = M.ld;
+    g.ldn = N.ld;
+    g.m = (int)m;
+    g.n = (int)n;
+    g.k = (int)k;
+    return g;
+}
+
+}  // namespace gett

@@ -1,0 +1,171 @@
+// layers.hpp -- what the operators of gett_layers.h share: their random numbers,
+// activations, argument checks and vectors.
+#pragma once
+#include "gett_layers.h"
+#include "kernel.hpp"
+#include "matrix.hpp"
+
+namespace gett {
+
+// ------------------------------------------------------------------ dropout ---
+
+// A call's dropout as its kernels take it; cut 0: none.
+struct Drop {
+    uint32_t cut;
+    float scale;
+    uint64_t seed, offset;
+    const int64_t *seedAt;   // device, or nullptr
+    __device__ __forceinline__ uint64_t key() const { return seedAt ? (uint64_t)*seedAt : seed; }
+};
+
+inline bool drop_ok(const gett_dropout_t *d)
+{
+    return !d || (d->p >= 0.0 && d->p <= 1.0 && (uintptr_t)d->seed_device % 8 == 0);
+}
+inline Drop drop_of(const gett_dropout_t *d)
+{
+    if (!d) return {0, 1.0f, 0, 0, nullptr};
+    const double t = __builtin_nearbyint(d->p * 65536.0);
+    return {(uint32_t)t, t < 65536.0 ? (float)(65536.0 / (65536.0 - t)) : 0.0f, d->seed, d->offset,
+            d->seed_device};
+}
+
+// The block of counter {c0, c1, offset}: 10 rounds, of which each multiplies two
+// words by constants and exchanges the halves of the products, and a key that
+// moves by its Weyl constants.
+__device__ __forceinline__ void philox(uint32_t c0, uint32_t c1, uint64_t offset, uint64_t key,
+                                       uint32_t out[4])
+{
+    uint32_t c2 = (uint32_t)offset, c3 = (uint32_t)(offset >> 32);
+    uint32_t k0 = (uint32_t)key, k1 = (uint32_t)(key >> 32);
+#pragma unroll
+    for (int i = 0; i < 10; ++i) {
+        const uint64_t p = (uint64_t)0xD2511F53u * c0, q = (uint64_t)0xCD9E8D57u * c2;
+        c0 = (uint32_t)(q >> 32) ^ c1 ^ k0;
+        c2 = (uint32_t)(p >> 32) ^ c3 ^ k1;
+        c1 = (uint32_t)q;
+        c3 = (uint32_t)p;
+        k0 += 0x9E3779B9u;
+        k1 += 0xBB67AE85u;
+    }
+    out[0] = c0;
+    out[1] = c1;
+    out[2] = c2;
+    out[3] = c3;
+}
+
+// Eight neighbours of one row, from a column that is a multiple of 8.  A block
+// of random bits serves the eight of them (16 bits each: with 32 the generator, and
+// not memory, would be what bounds a 16-bit dropout).
+__device__ __forceinline__ void drop8(float v[8], const Drop &d, uint64_t key, uint32_t row, uint32_t col)
+{
+    uint32_t w[4];
+    philox(col >> 3, row, d.offset, key, w);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        v[2 * i] = (w[i] & 0xffff) >= d.cut ? v[2 * i] * d.scale : 0.0f;
+        v[2 * i + 1] = (w[i] >> 16) >= d.cut ? v[2 * i + 1] * d.scale : 0.0f;
+    }
+}
+
+// -------------------------------------------------------------- activations ---
+
+__device__ __forceinline__ float activate(int kind, float z)
+{
+    if (kind == GETT_ACTIVATION_RELU) return z > 0.0f || z != z ? z : 0.0f;
+    if (kind == GETT_ACTIVATION_GELU) return 0.5f * z * (1.0f + erff(z * 0.70710678f));
+    if (kind == GETT_ACTIVATION_SILU) return z / (1.0f + expf(-z));
+    return z;
+}
+__device__ __forceinline__ float slope(int kind, float z)
+{
+    if (kind == GETT_ACTIVATION_RELU) return z > 0.0f ? 1.0f : z != z ? z : 0.0f;
+    if (kind == GETT_ACTIVATION_GELU)
+        return 0.5f * (1.0f + erff(z * 0.70710678f)) + z * 0.39894228f * expf(-0.5f * z * z);
+    if (kind == GETT_ACTIVATION_SILU) {
+        const float s = 1.0f / (1.0f + expf(-z));
+        return s * (1.0f + z * (1.0f - s));
+    }
+    return 1.0f;
+}
+
+// ------------------------------------------------------------------ vectors ---
+
+// `left` of eight neighbours (0 for the others), and back
+template <typename T> __device__ __forceinline__ void load8(const T *p, int left, float v[8])
+{
+    if (left >= 8) {
+        const Run<T, 8> r = *reinterpret_cast<const Run<T, 8> *>(p);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = to_float(r.v[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i < left ? to_float(p[i]) : 0.0f;
+    }
+}
+template <typename T> __device__ __forceinline__ void store8(T *p, int left, const float v[8])
+{
+    if (left >= 8) {
+        Run<T, 8> r;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) r.v[i] = from_float<T>(v[i]);
+        *reinterpret_cast<Run<T, 8> *>(p) = r;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < left) p[i] = from_float<T>(v[i]);
+    }
+}
+
+// ------------------------------------------------------------- host checks ---
+
+constexpr int64_t kLayerRows = (int64_t)1 << 31;   // rows of a matrix, exclusive
+constexpr int64_t kLayerCols = (int64_t)1 << 21;   // columns, exclusive
+constexpr int kMostExperts = 1024, kMostChoices = 32;
+
+// One matrix argument of a call: what it may overlap, and whether it is there.
+struct Extent {
+    const char *p;
+    int64_t bytes;
+};
+inline gett_status_t layer_matrix(gett_dtype_t t, int64_t rows, int64_t cols, const void *p,
+                                  int64_t stride, Extent &e)
+{
+    e = {nullptr, 0};
+    if (rows < 0 || cols < 0) return GETT_ERROR_INVALID_VALUE;
+    if (rows >= kLayerRows || cols >= kLayerCols) return GETT_ERROR_NOT_SUPPORTED;
+    if (rows == 0 || cols == 0) return GETT_SUCCESS;
+    if (rows > 1 && stride < cols) return GETT_ERROR_INVALID_VALUE;
+    if (!p || (uintptr_t)p % type_size(t)) return GETT_ERROR_INVALID_VALUE;
+    const int64_t n = span_bytes(rows, cols, rows > 1 ? stride : cols, 1, type_size(t));
+    if (n < 0) return GETT_ERROR_NOT_SUPPORTED;
+    e = {static_cast<const char *>(p), n};
+    return GETT_SUCCESS;
+}
+// a list of `n` items of `item` bytes
+inline gett_status_t layer_list(int64_t n, int64_t item, const void *p, Extent &e)
+{
+    e = {nullptr, 0};
+    if (n <= 0) return GETT_SUCCESS;
+    if (!p || (uintptr_t)p % item) return GETT_ERROR_INVALID_VALUE;
+    e = {static_cast<const char *>(p), n * item};
+    return GETT_SUCCESS;
+}
+inline bool apart(const Extent &a, const Extent &b)
+{
+    return !a.bytes || !b.bytes || a.p + a.bytes <= b.p || b.p + b.bytes <= a.p;
+}
+inline bool activation_ok(int a) { return a >= GETT_ACTIVATION_NONE && a <= GETT_ACTIVATION_SILU; }
+
+inline int64_t round_up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
+inline gett_status_t launched(hipError_t e) { return e == hipSuccess ? GETT_SUCCESS : GETT_ERROR_HIP; }
+
+// Calls f with a value of the element type.
+template <typename F> auto with_type(gett_dtype_t t, F &&f)
+{
+    if (t == GETT_FLOAT32) return f(float());
+    if (t == GETT_BFLOAT16) return f(bf16());
+    return f(_Float16());
+}
+
+}  // namespace gett
