@@ -118,7 +118,8 @@ gett_status_t gett_experts(gett_dtype_t dtype, int64_t tokens, int k, int expert
     }
     g.out = {static_cast<const char *>(bias), nullptr, static_cast<char *>(Z), static_cast<char *>(Y), 0,
              stride_z, stride_y, activation, 0, {}};
-    return product_launch_of(dtype, kRowsRows, kByRows, g, s);
+    return product_launch_of(dtype, kRowsRows, kByRows, g, product_plan(dtype, kByRows, rows, n, width, experts),
+                             hold, 0, s);
 }
 
 gett_status_t gett_experts_grad(gett_dtype_t dtype, int64_t tokens, int k, int experts, int64_t n,
@@ -200,7 +201,8 @@ gett_status_t gett_experts_grad(gett_dtype_t dtype, int64_t tokens, int k, int e
         g.out.Y = gather ? ws + partsAt : static_cast<char *>(dX);
         g.out.ldy = gather ? width : stride_dx;
         g.out.wide = gather ? 1 : 0;
-        st = product_launch_of(dtype, kRowsColumns, kByRows, g, s);
+        st = product_launch_of(dtype, kRowsColumns, kByRows, g,
+                               product_plan(dtype, kByRows, rows, width, n, experts), hold, 0, s);
         if (st == GETT_SUCCESS && gather) {
             const int64_t runs = (width + 7) / 8;
             const CombineJob c = {ws + partsAt, nullptr, nullptr, dX, place, width, 0, stride_dx,
@@ -217,7 +219,8 @@ gett_status_t gett_experts_grad(gett_dtype_t dtype, int64_t tokens, int k, int e
         g.offsets = offsets;
         g.out.Y = static_cast<char *>(dW);
         g.out.ldy = width;
-        st = product_launch_of(dtype, kColumnsColumns, kByK, g, s);
+        st = product_launch_of(dtype, kColumnsColumns, kByK, g,
+                               product_plan(dtype, kByK, n, width, rows, experts), hold, 0, s);
     }
     return st;
 }

@@ -59,15 +59,24 @@ struct CombineGradJob {
 };
 gett_status_t combine_grad_launch(gett_dtype_t t, gett_dtype_t tw, const CombineGradJob &j, hipStream_t s);
 
-gett_status_t product_launch_f32(ProductForm form, ProductGroups groups, ProductArgs g, hipStream_t s);
-gett_status_t product_launch_bf16(ProductForm form, ProductGroups groups, ProductArgs g, hipStream_t s);
-gett_status_t product_launch_f16(ProductForm form, ProductGroups groups, ProductArgs g, hipStream_t s);
+gett_status_t product_launch_f32(ProductForm form, ProductGroups groups, const ProductArgs &g,
+                                 const ProductPlan &p, hipStream_t s);
+gett_status_t product_launch_bf16(ProductForm form, ProductGroups groups, const ProductArgs &g,
+                                  const ProductPlan &p, hipStream_t s);
+gett_status_t product_launch_f16(ProductForm form, ProductGroups groups, const ProductArgs &g,
+                                 const ProductPlan &p, hipStream_t s);
+// Slots and counters of a shared sum begin at `slots` of the workspace.
 inline gett_status_t product_launch_of(gett_dtype_t t, ProductForm form, ProductGroups groups,
-                                       const ProductArgs &g, hipStream_t s)
+                                       ProductArgs g, const ProductPlan &p, const Partials &hold,
+                                       int64_t slots, hipStream_t s)
 {
-    if (t == GETT_FLOAT32) return product_launch_f32(form, groups, g, s);
-    return t == GETT_BFLOAT16 ? product_launch_bf16(form, groups, g, s)
-                              : product_launch_f16(form, groups, g, s);
+    if (p.slices > 1) {
+        g.slots = reinterpret_cast<float *>(static_cast<char *>(hold.tiles) + slots);
+        g.counters = hold.counters;
+    }
+    if (t == GETT_FLOAT32) return product_launch_f32(form, groups, g, p, s);
+    return t == GETT_BFLOAT16 ? product_launch_bf16(form, groups, g, p, s)
+                              : product_launch_f16(form, groups, g, p, s);
 }
 
 // ----------------------------------------------------------- host helpers ---

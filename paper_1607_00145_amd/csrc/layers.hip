@@ -75,9 +75,11 @@ gett_status_t gett_linear(gett_dtype_t dtype, int64_t m, int64_t n, int64_t k, c
     const bool gridX = on_grid(dtype, m, k, X, stride_x), gridW = on_grid(dtype, n, k, W, stride_w);
     Operand ox = operand_of(dtype, m, k, X, stride_x, gridX, arena, m);
     Operand ow = operand_of(dtype, n, k, W, stride_w, gridW, arena, n);
+    const ProductPlan plan = product_plan(dtype, kWhole, m, n, k, 0);
+    const int64_t slots = arena.take(plan.slotBytes);
     Partials hold;
     if (arena.bytes) {
-        st = stream_workspace(s, 0, arena.bytes, hold);
+        st = stream_workspace(s, (uint64_t)plan.counters, arena.bytes, hold);
         if (st != GETT_SUCCESS) return st;
         st = place_copy(dtype, ox, hold, m, k, X, stride_x, s);
         if (st == GETT_SUCCESS) st = place_copy(dtype, ow, hold, n, k, W, stride_w, s);
@@ -89,7 +91,7 @@ gett_status_t gett_linear(gett_dtype_t dtype, int64_t m, int64_t n, int64_t k, c
     g.out = {static_cast<const char *>(bias), static_cast<const char *>(residual),
              static_cast<char *>(Z), static_cast<char *>(Y), stride_r, stride_z, stride_y, activation, 0,
              drop_of(drop)};
-    return product_launch_of(dtype, kRowsRows, kWhole, g, s);
+    return product_launch_of(dtype, kRowsRows, kWhole, g, plan, hold, slots, s);
 }
 
 gett_status_t gett_linear_grad(gett_dtype_t dtype, int64_t m, int64_t n, int64_t k, const void *dY,
@@ -130,9 +132,15 @@ gett_status_t gett_linear_grad(gett_dtype_t dtype, int64_t m, int64_t n, int64_t
     if (ew.bytes) ox = operand_of(dtype, m, k, X, stride_x, on_grid(dtype, m, k, X, stride_x), arena, m);
     if (ex.bytes) ow = operand_of(dtype, n, k, W, stride_w, on_grid(dtype, n, k, W, stride_w), arena, n);
     const int64_t sumsAt = sum ? arena.take(slope_slots(m, 0) * n * 4) : -1;
+    ProductPlan px = {}, pw = {};
+    if (ex.bytes) px = product_plan(dtype, kWhole, m, k, n, 0);
+    if (ew.bytes) pw = product_plan(dtype, kWhole, n, k, m, 0);
+    // (one after the other, in the same slots)
+    const int64_t slots = arena.take(px.slotBytes > pw.slotBytes ? px.slotBytes : pw.slotBytes);
     Partials hold;
     if (arena.bytes) {
-        st = stream_workspace(s, 0, arena.bytes, hold);
+        st = stream_workspace(s, (uint64_t)(px.counters > pw.counters ? px.counters : pw.counters),
+                              arena.bytes, hold);
         if (st != GETT_SUCCESS) return st;
     }
     char *ws = static_cast<char *>(hold.tiles);
@@ -153,7 +161,7 @@ gett_status_t gett_linear_grad(gett_dtype_t dtype, int64_t m, int64_t n, int64_t
         g.fullN = ow.width;
         g.out.Y = static_cast<char *>(dX);
         g.out.ldy = stride_dx;
-        st = product_launch_of(dtype, kRowsColumns, kWhole, g, s);
+        st = product_launch_of(dtype, kRowsColumns, kWhole, g, px, hold, slots, s);
     }
     if (st == GETT_SUCCESS && ew.bytes) {
         ProductArgs g = product_args(oz, ox, n, k, m);
@@ -161,7 +169,7 @@ gett_status_t gett_linear_grad(gett_dtype_t dtype, int64_t m, int64_t n, int64_t
         g.fullN = ox.width;
         g.out.Y = static_cast<char *>(dW);
         g.out.ldy = stride_dw;
-        st = product_launch_of(dtype, kColumnsColumns, kWhole, g, s);
+        st = product_launch_of(dtype, kColumnsColumns, kWhole, g, pw, hold, slots, s);
     }
     return st;
 }

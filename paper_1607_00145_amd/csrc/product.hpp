@@ -24,14 +24,15 @@
 // sixteen times as long as the ones in 16 bits, and LDS has the time).
 //
 // N comes first in the instruction, so that a lane's results are of one row i
-// and of columns j that follow one another; which row of N is which row of an
-// instruction's operand is chosen so that the results of two instructions make
-// runs of eight columns: 16 bytes of a 16-bit C, and one block of random bits.
+// and of four columns j that follow one another: they go to LDS in vectors, and from
+// there to the epilogue in runs of eight columns, which are 16 bytes of a 16-bit C
+// and one block of random bits.
 #pragma once
 #include <type_traits>
 
 #include "layers.hpp"
 #include "panel.hpp"
+#include "product_plan.hpp"
 
 namespace gett {
 
@@ -64,8 +65,13 @@ struct ProductArgs {
     int fullM, fullN;       // rows of a column operand that may be read (m, n rounded up where
                             // they are zeros)
     int kM, kN;             // K of the operands that may be read
-    int tilesM, tilesN;
-    Recip tilesMInv, tilesNInv;
+    int tiles, tilesM, tilesN, bandRows;   // bandRows: of tiles, all experts' together
+    Recip tilesMInv, bandInv;
+    int full, slices;       // tiles from `full` on are shared by `slices` workgroups each,
+    Recip slicesInv;        // units: full + the others' slices
+    int units;
+    float *slots;
+    int *counters;
     int experts;
     const int32_t *offsets; // device, experts + 1
     const int32_t *order;   // device: M's rows are those of order[.] / choices, or nullptr
@@ -74,27 +80,39 @@ struct ProductArgs {
     Epilogue out;
 };
 
-enum ProductForm { kRowsRows, kRowsColumns, kColumnsColumns };
-enum ProductGroups { kWhole, kByRows, kByK };
-
 template <int FM_, int FN_, int WM_, int WN_, int NS_> struct ProductShape {
     static constexpr int FM = FM_, FN = FN_, WM = WM_, WN = WN_, NS = NS_;
     static constexpr int BM = 32 * FM * WM, BN = 32 * FN * WN;
     static constexpr int NW = WM * WN, THREADS = 64 * NW;
     static constexpr int STAGE = (BM + BN) * 128;
     static constexpr int JA = BM / 8 / NW, JB = BN / 8 / NW, J = JA + JB;   // loads a lane
-    static constexpr int LDS = NS * STAGE;
-    static_assert(FN % 2 == 0 && (FM & (FM - 1)) == 0 && (FN & (FN - 1)) == 0, "runs of eight");
+    static constexpr int W = 32 * FN;                   // columns of a wavefront
+    static constexpr int RESULTS = 16 * W * 4;          // of LDS a wavefront, for its results
+    static constexpr int LDS = NS * STAGE + NW * RESULTS;
+    static_assert((FM & (FM - 1)) == 0 && (FN & (FN - 1)) == 0, "addresses by exclusive or");
     static_assert(JA * 8 * NW == BM && JB * 8 * NW == BN, "whole instructions");
     static_assert((NS - 1) * J < 64, "vmcnt");
-    static_assert(LDS >= NW * 32 * 32 * FN * 4, "results");
 };
 
 constexpr uint32_t kNowhere = 0xfffffff0u;   // behind every buffer: such a load gives zeros
 
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t whole_buffer(const char *p)
+// A buffer from p on, as the instruction takes it; p is the same in all lanes.
+__device__ __forceinline__ i4 whole_buffer(const char *p)
 {
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(p), 0, (int)kNowhere, 0x00027000);
+    const uint64_t a = (uint64_t)p;
+    return i4{__builtin_amdgcn_readfirstlane((int)(uint32_t)a),
+              __builtin_amdgcn_readfirstlane((int)(uint32_t)(a >> 32)), (int)kNowhere, 0x00027000};
+}
+// 16 bytes a lane straight into LDS, 1 KB from `at` on.  Written out, and not by the
+// builtin: after that the compiler lets the first ds_read_tr16 wait for every load on
+// its way, since it cannot tell their addresses apart (the builtin, 8192 x 8192 x
+// 4096 in bf16: 600 us for dw).  It has no result in registers; the compiler's own
+// waits count it as younger than what they wait for, or wait longer.  (m0 cannot be
+// named as overwritten; nothing else in these kernels takes it.)
+__device__ __forceinline__ void load_to_lds(i4 buffer, uint32_t offset, uint32_t at)
+{
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds"
+                 :: "v"(offset), "s"(buffer), "s"(at) : "memory");
 }
 
 typedef short s4 __attribute__((ext_vector_type(4)));
@@ -128,7 +146,7 @@ template <typename T, bool MCOL, bool NCOL, typename S> struct Product {
     f16v acc[FM][FN];
     int q, h, wm, wn;
 
-    __device__ __forceinline__ void init()
+    __device__ __forceinline__ void locate()
     {
         const int tid = (int)threadIdx.x;
         const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -136,6 +154,9 @@ template <typename T, bool MCOL, bool NCOL, typename S> struct Product {
         h = (tid >> 5) & 1;
         wm = wave / S::WN;
         wn = wave % S::WN;
+    }
+    __device__ __forceinline__ void clear()
+    {
 #pragma unroll
         for (int i = 0; i < FM; ++i)
 #pragma unroll
@@ -143,12 +164,12 @@ template <typename T, bool MCOL, bool NCOL, typename S> struct Product {
 #pragma unroll
                 for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
     }
-    // acc[i][2 u + x][4 a + y] is that of row 32 i + q and column 64 u + 16 a + 8 h +
-    // 4 x + y of the wavefront's part.
+    // acc[i][f][4 a + y] is that of row 32 i + q and column 32 f + 8 a + 4 h + y of the
+    // wavefront's part.
 
     // Where a lane's 16 bytes of load j lie: k or piece that decides whether they
     // are within K (`at`), and the offset from the panel's first byte.
-    template <bool COL, int B, bool ISN, typename Row>
+    template <bool COL, int B, typename Row>
     __device__ __forceinline__ static void place(const Side &x, int j, int wave, int lane, Row rowOffset,
                                                  uint32_t &off, int &at)
     {
@@ -161,74 +182,100 @@ template <typename T, bool MCOL, bool NCOL, typename S> struct Product {
             off = piece * EP < x.count ? (uint32_t)(k * x.ld) + piece * 16 : kNowhere;
         } else {
             const int r = L >> 3, pl = L & 7;
-            const int piece = pl ^ (ISN ? ((r >> 1) & 1) | ((r >> 3) & 3) << 1 : (r >> 1) & 7);
+            const int piece = pl ^ ((r >> 1) & 7);
             at = piece * EP;
             off = r < x.count ? rowOffset(r) + piece * 16 : kNowhere;
         }
     }
 
-    // The panels of K = [0, extent) of both sides; `lds` holds S::LDS bytes.
-    template <typename RowM>
-    __device__ __forceinline__ void run(char *lds, const Side &M, const Side &N, RowM rowM, int panels)
+    // Loads on their way to LDS: what a lane fetches of each panel, and the next
+    // panel.  In the order of issue a stage's J loads follow one another.
+    uint32_t off[S::J];
+    int at[S::J];
+    const char *pm, *pn;
+    int64_t stepM, stepN;
+    int leftM, leftN, panels;
+    uint32_t ldsAt;
+
+    i4 rm, rn;
+    uint32_t to;
+    __device__ __forceinline__ void issue_begin(int stage)
     {
-        constexpr int NW = S::NW, J = S::J, JA = S::JA;
+        rm = whole_buffer(pm);
+        rn = whole_buffer(pn);
+        to = ldsAt + stage * S::STAGE;
+    }
+    __device__ __forceinline__ void issue_one(int j)
+    {
+        const bool isM = j < S::JA;
+        const uint32_t o = at[j] < (isM ? leftM : leftN) ? off[j] : kNowhere;
+        load_to_lds(isM ? rm : rn, o,
+                    to + (isM ? 0 : S::BM * 128) + (isM ? j : j - S::JA) * S::NW * 1024);
+    }
+    __device__ __forceinline__ void issue_end()
+    {
+        pm += stepM;
+        pn += stepN;
+        leftM -= KP;
+        leftN -= KP;
+    }
+    // Takes a tile and sends the loads of its first panels; nobody reads LDS any more.
+    template <typename RowM>
+    __device__ __forceinline__ void begin(char *lds, const Side &M, const Side &N, RowM rowM, int count)
+    {
         const int lane = (int)threadIdx.x & 63;
         const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-        uint32_t off[J];
-        int at[J];
 #pragma unroll
-        for (int j = 0; j < J; ++j) {
-            if (j < JA)
-                place<MCOL, S::BM, false>(M, j, wave, lane, rowM, off[j], at[j]);
+        for (int j = 0; j < S::J; ++j) {
+            if (j < S::JA)
+                place<MCOL, S::BM>(M, j, wave, lane, rowM, off[j], at[j]);
             else
-                place<NCOL, S::BN, true>(N, j - JA, wave, lane,
+                place<NCOL, S::BN>(N, j - S::JA, wave, lane,
                                          [&](int r) { return (uint32_t)(r * N.ld); }, off[j], at[j]);
         }
-        const int64_t stepM = MCOL ? KP * M.ld : 128, stepN = NCOL ? KP * N.ld : 128;
-        const char *pm = M.p, *pn = N.p;
-        int leftM = M.extent, leftN = N.extent;
-        auto issue = [&](int stage) {
-            const __amdgpu_buffer_rsrc_t rm = whole_buffer(pm), rn = whole_buffer(pn);
-            char *base = lds + stage * S::STAGE;
+        stepM = MCOL ? KP * M.ld : 128;
+        stepN = NCOL ? KP * N.ld : 128;
+        pm = M.p;
+        pn = N.p;
+        ldsAt = (uint32_t)(uintptr_t)(matrix_lds *)lds + wave * 1024;
+        leftM = M.extent;
+        leftN = N.extent;
+        panels = count;
 #pragma unroll
-            for (int j = 0; j < J; ++j) {
-                const bool isM = j < JA;
-                char *dst = base + (isM ? 0 : S::BM * 128) + ((isM ? j : j - JA) * NW + wave) * 1024;
-                const uint32_t o = at[j] < (isM ? leftM : leftN) ? off[j] : kNowhere;
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(isM ? rm : rn, (matrix_lds *)dst, 16, (int)o,
-                                                         0, 0, 0);
+        for (int i = 0; i < NS; ++i)
+            if (i < panels) {
+                issue_begin(i);
+#pragma unroll
+                for (int j = 0; j < S::J; ++j) issue_one(j);
+                issue_end();
             }
-            pm += stepM;
-            pn += stepN;
-            leftM -= KP;
-            leftN -= KP;
-        };
+    }
 
+    // The sums over the panels of the tile that was begun; at least `after` stores
+    // were issued since.
+    template <int AFTER> __device__ __forceinline__ void run(char *lds, bool after)
+    {
+        constexpr int J = S::J;
+        const int lane = (int)threadIdx.x & 63;
         // A lane's own address in a stage for fragment 0 and slab 0; the others are
         // that, exclusive or (and plus) constants.
         const int j4 = lane & 3, k4 = (lane >> 2) & 3, g2 = (lane >> 4) & 1;
-        int ownM, ownN;
-        if constexpr (!MCOL) {
-            ownM = (wm * 32 * FM + q) * 128 + ((4 * h) ^ ((q >> 1) & 7)) * 16;
-        } else if constexpr (sizeof(T) == 2) {
-            constexpr int PR = S::BM / EP;
-            const int piece = wm * 4 * FM + 2 * g2 + (j4 >> 1);
-            ownM = (32 * h + k4) * PR * 16 + (piece ^ (4 * k4 & (PR - 1))) * 16 + (j4 & 1) * 8;
-        } else {
-            ownM = 16 * h * S::BM * 4 + (wm * 32 * FM + q) * 4;
-        }
-        const int nq = 16 * (q >> 3) + 8 * ((q >> 2) & 1) + (q & 3);   // row of N of fragment 0
-        if constexpr (!NCOL) {
-            ownN = (wn * 32 * FN + nq) * 128 +
-                   ((4 * h) ^ (((q >> 1) & 1) | ((q >> 2) & 1) << 1 | ((q >> 3) & 1) << 2)) * 16;
-        } else if constexpr (sizeof(T) == 2) {
-            constexpr int PR = S::BN / EP;
-            const int piece = wn * 4 * FN + 4 * g2 + j4;
-            ownN = (32 * h + k4) * PR * 16 + (piece ^ (4 * k4 & (PR - 1))) * 16;
-        } else {
-            ownN = 16 * h * S::BN * 4 + (wn * 32 * FN + nq) * 4;
-        }
-        ownN += S::BM * 128;
+        auto own = [&](auto column, auto size, int first) {
+            constexpr int B = decltype(size)::value;
+            if constexpr (!decltype(column)::value) {
+                return (first + q) * 128 + ((4 * h) ^ ((q >> 1) & 7)) * 16;
+            } else if constexpr (sizeof(T) == 2) {
+                constexpr int PR = B / EP;
+                const int piece = first / EP + 2 * g2 + (j4 >> 1);
+                return (32 * h + k4) * PR * 16 + (piece ^ (4 * k4 & (PR - 1))) * 16 + (j4 & 1) * 8;
+            } else {
+                return 16 * h * B * 4 + (first + q) * 4;
+            }
+        };
+        const int ownM = own(std::bool_constant<MCOL>{}, std::integral_constant<int, S::BM>{},
+                             wm * 32 * FM);
+        const int ownN = S::BM * 128 + own(std::bool_constant<NCOL>{},
+                                           std::integral_constant<int, S::BN>{}, wn * 32 * FN);
         int atM = ownM, atN = ownN;
         auto at_stage = [&](int stage) {
             atM = ownM + stage * S::STAGE;
@@ -243,45 +290,33 @@ template <typename T, bool MCOL, bool NCOL, typename S> struct Product {
             return __builtin_bit_cast(i4, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
         };
         i4 a[2][FM], b[2][FN];
-        auto read = [&](int set, int s) {
+        auto fragment = [&](auto column, auto size, int own, int s, int i) {
+            constexpr int B = decltype(size)::value;
+            if constexpr (!decltype(column)::value) {
+                return *reinterpret_cast<const i4 *>(lds + (own ^ (s * 16)) + i * 4096);
+            } else if constexpr (sizeof(T) == 2) {
+                constexpr int KB = B * 2;      // bytes of one k
+                const int x = (own ^ (i * 64)) + 8 * s * KB;
+                return join(quad(x), quad(x + 4 * KB));
+            } else {
+                i4 v;
 #pragma unroll
-            for (int i = 0; i < FM; ++i) {
-                if constexpr (!MCOL) {
-                    a[set][i] = *reinterpret_cast<const i4 *>(lds + (atM ^ (s * 16)) + i * 4096);
-                } else if constexpr (sizeof(T) == 2) {
-                    constexpr int KB = S::BM * 2;      // bytes of one k
-                    const int x = (atM ^ (i * 64)) + 8 * s * KB;
-                    a[set][i] = join(quad(x), quad(x + 4 * KB));
-                } else {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        a[set][i][j] = *reinterpret_cast<const int *>(
-                            lds + atM + (4 * s + j) * S::BM * 4 + i * 128);
-                }
-            }
-#pragma unroll
-            for (int f = 0; f < FN; ++f) {
-                if constexpr (!NCOL) {
-                    b[set][f] = *reinterpret_cast<const i4 *>(lds + (atN ^ (s * 16)) +
-                                                             (64 * (f >> 1) + 4 * (f & 1)) * 128);
-                } else if constexpr (sizeof(T) == 2) {
-                    constexpr int KB = S::BN * 2;
-                    const int x = (atN ^ (128 * (f >> 1))) + 8 * (f & 1) + 8 * s * KB;
-                    b[set][f] = join(quad(x), quad(x + 4 * KB));
-                } else {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        b[set][f][j] = *reinterpret_cast<const int *>(
-                            lds + atN + (4 * s + j) * S::BN * 4 + (64 * (f >> 1) + 4 * (f & 1)) * 4);
-                }
+                for (int j = 0; j < 4; ++j)
+                    v[j] = *reinterpret_cast<const int *>(lds + own + (4 * s + j) * B * 4 + i * 128);
+                return v;
             }
         };
-        auto mma = [&](int set) {
-#pragma unroll
-            for (int i = 0; i < FM; ++i)
-#pragma unroll
-                for (int f = 0; f < FN; ++f)
-                    acc[i][f] = product_mfma<T>(b[set][f], a[set][i], acc[i][f]);
+        auto read_m = [&](int set, int s, int i) {
+            a[set][i] = fragment(std::bool_constant<MCOL>{}, std::integral_constant<int, S::BM>{}, atM, s, i);
+        };
+        auto read_n = [&](int set, int s, int f) {
+            b[set][f] = fragment(std::bool_constant<NCOL>{}, std::integral_constant<int, S::BN>{}, atN, s, f);
+        };
+        // the x-th fragment of a slab, in the order that the MFMAs want them
+        auto read_one = [&](int set, int s, int x) {
+            if (x == 0) read_m(set, s, 0);
+            else if (x <= FN) read_n(set, s, x - 1);
+            else read_m(set, s, x - FN);
         };
         // no fence: a release would wait for the loads in flight as well
         auto barrier = []() { asm volatile("s_barrier" ::: "memory"); };
@@ -291,39 +326,54 @@ template <typename T, bool MCOL, bool NCOL, typename S> struct Product {
         constexpr int kNext = wait_for((NS - 2) * J);
 
         if (panels <= 0) return;
-#pragma unroll
-        for (int i = 0; i < NS; ++i)
-            if (i < panels) issue(i);
-        if (panels >= NS) __builtin_amdgcn_s_waitcnt(kFirst);
-        else __builtin_amdgcn_s_waitcnt(kAll);
+        constexpr int kFirst2 = wait_for((NS - 1) * J + AFTER);
+        if (panels < NS) __builtin_amdgcn_s_waitcnt(kAll);
+        else if (after) __builtin_amdgcn_s_waitcnt(kFirst2);
+        else __builtin_amdgcn_s_waitcnt(kFirst);
         barrier();
         at_stage(0);
-        read(0, 0);
+        constexpr int READS = FM + FN, MFMAS = FM * FN;
+#pragma unroll
+        for (int x = 0; x < READS; ++x) read_one(0, 0, x);
         int stage = 0;
         // While a panel is multiplied the next NS - 1 are on their way; one barrier a
-        // panel, after its last LDS read and before its last MFMAs.
+        // panel, after its last LDS read and before its last MFMAs.  The order is
+        // written out: between two MFMAs a fragment of the next slab is read, and in
+        // the last slab the loads go out as well, so that the matrix unit waits for
+        // neither to be issued.
         auto panel = [&](auto more, auto load) {
             static_for<4>([&](auto step) {
                 constexpr int s = decltype(step)::value, set = s & 1;
-                if constexpr (s < 3) {
-                    read(set ^ 1, s + 1);
-                } else if constexpr (more) {
+                constexpr bool last = s == 3, reads = !last || more, loads = last && load;
+                if constexpr (last && more) {
                     __builtin_amdgcn_s_waitcnt(load ? kNext : kAll);   // the next is there
                     barrier();
-                    if constexpr (load) issue(stage);
+                    if constexpr (loads) issue_begin(stage);
                     stage = stage + 1 == NS ? 0 : stage + 1;
                     at_stage(stage);
-                    read(set ^ 1, 0);
                 }
-                mma(set);
-                __builtin_amdgcn_sched_barrier(0);
+                static_for<MFMAS>([&](auto xc) {
+                    constexpr int x = decltype(xc)::value, i = x / FN, f = x % FN;
+                    constexpr int r0 = x * READS / MFMAS, r1 = (x + 1) * READS / MFMAS;
+                    constexpr int l0 = x * J / MFMAS, l1 = (x + 1) * J / MFMAS;
+                    if constexpr (reads)
+                        static_for<r1 - r0>([&](auto y) {
+                            read_one(set ^ 1, last ? 0 : s + 1, r0 + decltype(y)::value);
+                        });
+                    acc[i][f] = product_mfma<T>(b[set][f], a[set][i], acc[i][f]);
+                    if constexpr (loads)
+                        static_for<l1 - l0>([&](auto y) { issue_one(l0 + decltype(y)::value); });
+                    __builtin_amdgcn_sched_barrier(0);
+                });
+                if constexpr (loads) issue_end();
             });
         };
         const std::true_type yes;
         const std::false_type no;
+        const int n = panels;
         int t = 0;
-        for (; t + NS < panels; ++t) panel(yes, yes);
-        for (; t + 1 < panels; ++t) panel(yes, no);
+        for (; t + NS < n; ++t) panel(yes, yes);
+        for (; t + 1 < n; ++t) panel(yes, no);
         panel(no, no);
     }
 };
@@ -383,63 +433,151 @@ __device__ __forceinline__ int expert_of_slot(const int32_t *offsets, int expert
     return found - 1;   // expert 0's first is 0
 }
 
+// A workgroup's tile: rows and columns of C, the expert, and its share of K.
+struct TileAt {
+    int row0, rows, col0, e, first, sum;
+    bool empty;          // rows of no expert
+    int shared, slice;   // number among the shared tiles (-1: whole), slice
+};
+
+// Unit `id` of the launch; false where nothing is to be done.  Workgroups go round
+// the eight XCDs, each with an L2 of its own: the ids of one XCD are made neighbours,
+// and neighbours walk bands of four tile rows, so that the tiles that are on an XCD
+// together share operands.
+template <typename S>
+__device__ __forceinline__ bool product_tile(const ProductArgs &g, int groups, int id, TileAt &t)
+{
+    t.shared = -1;
+    t.slice = 0;
+    if (id >= g.full) {
+        const int u = id - g.full;
+        t.shared = (int)quotient((uint32_t)u, g.slices, g.slicesInv);
+        t.slice = u - t.shared * g.slices;
+        id = g.full + t.shared;
+    } else if (id < (g.full & ~7)) {
+        id = (id & 7) * (g.full >> 3) + (id >> 3);
+    }
+    const int inBand = 4 * g.tilesN;
+    const int band = (int)quotient((uint32_t)id, inBand, g.bandInv), rest = id - band * inBand;
+    const int height = min(g.bandRows - 4 * band, 4);
+    const int tn = height == 4 ? rest >> 2 : height == 3 ? (int)__umulhi((uint32_t)rest, 0x55555556u)
+                                                         : rest >> (height - 1);
+    int tm = 4 * band + rest - tn * height;
+    t.col0 = tn * S::BN;
+    t.rows = g.m;
+    t.first = 0;
+    t.sum = g.k;
+    t.e = 0;
+    t.empty = false;
+    if (groups == kByRows) {
+        const int e = __builtin_amdgcn_readfirstlane(
+            expert_of_slot<S::BM>(g.offsets, g.experts, g.m, tm));
+        const int begin = expert_offset(g.offsets, e, g.m);
+        t.e = e;
+        t.empty = e == g.experts;
+        t.rows = t.empty ? g.m : expert_offset(g.offsets, e + 1, g.m);
+        t.row0 = begin + (tm - (begin / S::BM + e)) * S::BM;
+        return t.row0 < t.rows;
+    }
+    if (groups == kByK) {
+        t.e = (int)quotient((uint32_t)tm, g.tilesM, g.tilesMInv);
+        tm -= t.e * g.tilesM;
+        t.first = expert_offset(g.offsets, t.e, g.k);
+        t.sum = expert_offset(g.offsets, t.e + 1, g.k) - t.first;
+    }
+    t.row0 = tm * S::BM;
+    return true;
+}
+
+// Adds up a shared tile; true for the workgroup that holds the sum.  The slices' sums
+// go to slots in device memory in lane order (device-scope accesses, which pass by
+// the XCD's own L2), and the last to arrive adds them in slice order: results do not
+// depend on who that is.  Counters are zero between launches.
+template <typename T, bool MCOL, bool NCOL, typename S>
+__device__ __forceinline__ bool product_join(Product<T, MCOL, NCOL, S> &p, const ProductArgs &g,
+                                             const TileAt &t, char *lds)
+{
+    const int tid = (int)threadIdx.x;
+    constexpr int N = S::THREADS, TILE = S::BM * S::BN;
+    float *first = g.slots + (int64_t)t.shared * g.slices * TILE + tid;
+    float *own = first + (int64_t)t.slice * TILE;
+    static_for<S::FM * S::FN>([&](auto xc) {
+        constexpr int x = decltype(xc)::value;
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+            __hip_atomic_store(own + (x * 16 + e) * N, p.acc[x / S::FN][x % S::FN][e], __ATOMIC_RELAXED,
+                               __HIP_MEMORY_SCOPE_AGENT);
+    });
+    __builtin_amdgcn_s_waitcnt(7 << 4 | 15 << 8);   // vmcnt 0: the stores are done
+    __syncthreads();
+    int *last = reinterpret_cast<int *>(lds);
+    if (tid == 0)
+        *last = __hip_atomic_fetch_add(g.counters + t.shared, 1, __ATOMIC_RELAXED,
+                                       __HIP_MEMORY_SCOPE_AGENT) == g.slices - 1;
+    __syncthreads();
+    const bool mine = *last;
+    __syncthreads();   // everyone has read it
+    if (!mine) return false;
+    if (tid == 0)
+        __hip_atomic_store(g.counters + t.shared, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    static_for<S::FM * S::FN>([&](auto xc) {
+        constexpr int x = decltype(xc)::value;
+        f16v &acc = p.acc[x / S::FN][x % S::FN];
+        for (int s0 = 0; s0 < g.slices; s0 += 2) {   // two slices' loads together
+            float v[2][16];
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+                if (s0 + s < g.slices)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        v[s][e] = __hip_atomic_load(first + (int64_t)(s0 + s) * TILE + (x * 16 + e) * N,
+                                                    __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+                if (s0 + s < g.slices)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) acc[e] = s0 + s == 0 ? v[s][e] : acc[e] + v[s][e];
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    });
+    return true;
+}
+
+// Workgroups take tile after tile.  A tile's loads begin before the results of the
+// one before are written: its first panels arrive while those leave.
 template <typename T, ProductForm FORM, typename S>
 __global__ __launch_bounds__(S::THREADS) void product_kernel(ProductArgs g, int groups)
 {
     extern __shared__ __attribute__((aligned(256))) char dyn_lds[];
     constexpr bool MCOL = FORM == kColumnsColumns, NCOL = FORM != kRowsRows;
     constexpr int KP = 128 / (int)sizeof(T);
-    const int bid = (int)blockIdx.x;
-    int tm = (int)quotient((uint32_t)bid, g.tilesN, g.tilesNInv);
-    const int tn = bid - tm * g.tilesN;
-    // rows of M and of C, K, and the expert's share of them
-    int row0 = 0, rows = g.m, first = 0, sum = g.k, e = 0;
-    bool empty = false;
-    if (groups == kByRows) {
-        e = expert_of_slot<S::BM>(g.offsets, g.experts, g.m, tm);
-        e = __builtin_amdgcn_readfirstlane(e);
-        const int begin = expert_offset(g.offsets, e, g.m);
-        rows = e == g.experts ? g.m : expert_offset(g.offsets, e + 1, g.m);
-        row0 = begin + (tm - (begin / S::BM + e)) * S::BM;
-        empty = e == g.experts;
-    } else if (groups == kByK) {
-        e = (int)quotient((uint32_t)tm, g.tilesM, g.tilesMInv);
-        tm -= e * g.tilesM;
-        first = expert_offset(g.offsets, e, g.k);
-        sum = expert_offset(g.offsets, e + 1, g.k) - first;
-        row0 = tm * S::BM;
-    } else {
-        row0 = tm * S::BM;
-    }
-    if (row0 >= rows) return;
-    const int col0 = tn * S::BN;
     Product<T, MCOL, NCOL, S> p;
-    p.init();
-    if (!empty) {
+    p.locate();
+    auto begin = [&](const TileAt &t) {
         const bool gathered = FORM == kRowsRows && g.order;
         Side M, N;
         M.ld = g.ldm;
         N.ld = g.ldn;
-        N.p = g.N + (groups == kByRows ? (int64_t)e * g.stepN : 0);
+        N.p = g.N + (groups == kByRows ? (int64_t)t.e * g.stepN : 0);
         if constexpr (MCOL) {
-            M.p = g.M + (int64_t)first * g.ldm + (int64_t)row0 * sizeof(T);
-            M.count = g.fullM - row0;
-            M.extent = sum;
+            M.p = g.M + (int64_t)t.first * g.ldm + (int64_t)t.row0 * sizeof(T);
+            M.count = g.fullM - t.row0;
+            M.extent = t.sum;
         } else {
-            M.p = g.M + (gathered ? 0 : (int64_t)row0 * g.ldm);
-            M.count = rows - row0;
+            M.p = g.M + (gathered ? 0 : (int64_t)t.row0 * g.ldm);
+            M.count = t.rows - t.row0;
             M.extent = g.kM;
         }
         if constexpr (NCOL) {
-            N.p += (int64_t)first * g.ldn + (int64_t)col0 * sizeof(T);
-            N.count = g.fullN - col0;
-            N.extent = sum;
+            N.p += (int64_t)t.first * g.ldn + (int64_t)t.col0 * sizeof(T);
+            N.count = g.fullN - t.col0;
+            N.extent = t.sum;
         } else {
-            N.p += (int64_t)col0 * g.ldn;
-            N.count = g.n - col0;
+            N.p += (int64_t)t.col0 * g.ldn;
+            N.count = g.n - t.col0;
             N.extent = g.kN;
         }
-        const int32_t *order = g.order + (gathered ? row0 : 0);
+        const int32_t *order = g.order + (gathered ? t.row0 : 0);
         auto rowM = [&](int r) {
             if (FORM == kRowsRows && gathered) {
                 const uint32_t id = min((uint32_t)order[r], (uint32_t)g.m - 1);
@@ -447,49 +585,84 @@ __global__ __launch_bounds__(S::THREADS) void product_kernel(ProductArgs g, int 
             }
             return (uint32_t)(r * g.ldm);
         };
-        p.run(dyn_lds, M, N, rowM, (sum + KP - 1) / KP);
-    }
-    Epilogue o = g.out;
-    if (groups == kByRows && o.bias) o.bias += (int64_t)e * g.n * sizeof(T);
-    if (groups == kByK) o.Y += (int64_t)e * g.stepN * (o.wide ? 4 : sizeof(T));
-    if (empty) {
-        o.bias = nullptr;
-        o.activation = GETT_ACTIVATION_NONE;
-    }
-    const uint64_t key = o.drop.cut ? o.drop.key() : 0;
-    // The results go through LDS, 32 rows of a wavefront at a time, so that one
-    // loop (and not one copy of the epilogue for each register) takes them, whole
-    // lines of C each time.  Piece x of row r lies at x ^ (r % 16).
-    constexpr int W = 32 * S::FN;                 // columns of a wavefront
-    const int lane = (int)threadIdx.x & 63;
-    char *mine = dyn_lds + (p.wm * S::WN + p.wn) * 32 * W * 4;
-    __syncthreads();
-    static_for<S::FM>([&](auto ic) {
-        constexpr int i = decltype(ic)::value;
-#pragma unroll
-        for (int u = 0; u < S::FN / 2; ++u)
-#pragma unroll
-            for (int a = 0; a < 4; ++a)
-#pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    const int piece = 16 * u + 4 * a + 2 * p.h + x;
-                    const f16v &c = p.acc[i][2 * u + x];
-                    *reinterpret_cast<f4 *>(mine + p.q * W * 4 + (piece ^ (p.q & 15)) * 16) =
-                        f4{c[4 * a], c[4 * a + 1], c[4 * a + 2], c[4 * a + 3]};
-                }
-        constexpr int PER = W / 8, ROWS = 64 / PER;   // runs of a row, rows a pass
-        const int run = lane % PER, first = lane / PER;
-        const int c = col0 + p.wn * W + 8 * run;
-#pragma unroll 1
-        for (int r = first; r < 32; r += ROWS) {
-            const int row = row0 + p.wm * 32 * S::FM + 32 * i + r;
-            if (row >= rows) break;
-            const f4 lo = *reinterpret_cast<const f4 *>(mine + r * W * 4 + ((2 * run) ^ (r & 15)) * 16);
-            const f4 hi = *reinterpret_cast<const f4 *>(mine + r * W * 4 + ((2 * run + 1) ^ (r & 15)) * 16);
-            float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-            product_store<T>(o, key, row, c, g.n - c, v);
+        int panels = t.empty ? 0 : (t.sum + KP - 1) / KP;
+        if (t.shared >= 0) {
+            const int t0 = (int)quotient((uint32_t)(panels * t.slice), g.slices, g.slicesInv);
+            panels = (int)quotient((uint32_t)(panels * (t.slice + 1)), g.slices, g.slicesInv) - t0;
+            M.p += t0 * (MCOL ? KP * M.ld : 128);
+            N.p += t0 * (NCOL ? KP * N.ld : 128);
+            M.extent -= t0 * KP;
+            N.extent -= t0 * KP;
         }
-    });
+        p.begin(dyn_lds, M, N, rowM, panels);
+    };
+    const uint64_t key = g.out.drop.cut ? g.out.drop.key() : 0;
+    const int lane = (int)threadIdx.x & 63;
+    char *mine = dyn_lds + S::NS * S::STAGE + (p.wm * S::WN + p.wn) * S::RESULTS;
+    int id = (int)blockIdx.x;
+    TileAt t;
+    bool there = false;
+    for (; id < g.units && !there; id += (int)gridDim.x) there = product_tile<S>(g, groups, id, t);
+    if (!there) return;
+    begin(t);
+    bool after = false;   // a whole tile's stores came after the loads
+    while (true) {
+        constexpr int STORES = S::FM * S::FN * (sizeof(T) == 2 ? 2 : 4);
+        p.clear();
+        p.template run<(S::NS - 1) * S::J + STORES < 64 ? STORES : 0>(dyn_lds, after);
+        __syncthreads();
+        TileAt now = t;
+        there = false;
+        for (; id < g.units && !there; id += (int)gridDim.x) there = product_tile<S>(g, groups, id, t);
+        if (there) begin(t);
+        after = false;
+        if (now.shared >= 0 &&
+            !product_join<T, MCOL, NCOL, S>(p, g, now, dyn_lds + S::NS * S::STAGE)) {
+            if (!there) return;
+            continue;
+        }
+        Epilogue o = g.out;
+        if (groups == kByRows && o.bias) o.bias += (int64_t)now.e * g.n * sizeof(T);
+        if (groups == kByK) o.Y += (int64_t)now.e * g.stepN * (o.wide ? 4 : sizeof(T));
+        if (now.empty) {
+            o.bias = nullptr;
+            o.activation = GETT_ACTIVATION_NONE;
+        }
+        after = now.row0 + S::BM <= now.rows && now.col0 + S::BN <= g.n;
+        // The results go through LDS, 16 rows of a wavefront at a time, so that one
+        // loop (and not one copy of the epilogue for each register) takes them, whole
+        // lines of C each time.  Piece x of row r lies at x ^ r % 16.
+        constexpr int W = S::W, PER = W / 8, ROWS = 64 / PER;   // runs of a row, rows a pass
+        constexpr int SWAP = W / 4 < 16 ? W / 4 - 1 : 15;
+        const int run = lane % PER, rowIn = lane / PER;
+        const int c = now.col0 + p.wn * W + 8 * run;
+#pragma unroll 1
+        for (int step = 0; step < 2 * S::FM; ++step) {
+            static_for<S::FM>([&](auto ic) {
+                constexpr int i = decltype(ic)::value;
+                if (step >> 1 != i || p.q >> 4 != (step & 1)) return;
+#pragma unroll
+                for (int f = 0; f < S::FN; ++f)
+#pragma unroll
+                    for (int a = 0; a < 4; ++a) {
+                        const int piece = 8 * f + 2 * a + p.h;
+                        const f16v &v = p.acc[i][f];
+                        *reinterpret_cast<f4 *>(mine + (p.q & 15) * W * 4 +
+                                                (piece ^ (p.q & SWAP)) * 16) =
+                            f4{v[4 * a], v[4 * a + 1], v[4 * a + 2], v[4 * a + 3]};
+                    }
+            });
+            const int first = now.row0 + p.wm * 32 * S::FM + 16 * step;
+#pragma unroll
+            for (int r = rowIn; r < rowIn + 16; r += ROWS) {
+                const f4 lo = *reinterpret_cast<const f4 *>(mine + r * W * 4 + ((2 * run) ^ (r & SWAP)) * 16);
+                const f4 hi = *reinterpret_cast<const f4 *>(mine + r * W * 4 + ((2 * run + 1) ^ (r & SWAP)) * 16);
+                float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+                if (first + r < now.rows) product_store<T>(o, key, first + r, c, g.n - c, v);
+            }
+        }
+        if (!there) return;
+    }
 }
 
 }  // namespace gett

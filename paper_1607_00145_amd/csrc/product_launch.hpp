@@ -1,44 +1,58 @@
-// product_launch.hpp -- which tiles a product of product.hpp takes, and its
-// launch; included by one .hip file per element type.
+// product_launch.hpp -- the launch of a product of product.hpp; included by one .hip
+// file per element type.
 #pragma once
 #include "launch.hpp"
-#include "product.hpp"
+#include "layer_util.hpp"
 
 namespace gett {
 
-
 template <typename T, ProductForm FORM, typename S>
-gett_status_t product_tiles(ProductGroups groups, ProductArgs g, hipStream_t s)
+gett_status_t product_tiles(ProductGroups groups, ProductArgs g, const ProductPlan &p, hipStream_t s)
 {
-    int64_t tm = (g.m + S::BM - 1) / S::BM;
-    const int64_t tn = (g.n + S::BN - 1) / S::BN;
-    g.tilesM = (int)tm;
-    g.tilesMInv = recip(tm);
-    if (groups == kByRows) tm = g.m / S::BM + g.experts + 1;
-    if (groups == kByK) tm *= g.experts;
-    if (!fits_launch(tm * tn, S::THREADS)) return GETT_ERROR_NOT_SUPPORTED;
-    g.tilesN = (int)tn;
-    g.tilesNInv = recip(tn);
+    // (ids are below 2^31 with a grid's stride added)
+    if (p.units >= INT32_MAX / 2 || p.tiles >= INT32_MAX / 2 || 4 * p.tilesN >= INT32_MAX ||
+        p.slices * ((int64_t)g.k * (int)sizeof(T) / 128 + 1) >= INT32_MAX)
+        return GETT_ERROR_NOT_SUPPORTED;
+    g.tiles = (int)p.tiles;
+    g.tilesM = (int)p.tilesM;
+    g.tilesN = (int)p.tilesN;
+    g.bandRows = (int)p.bandRows;
+    g.tilesMInv = recip(p.tilesM);
+    g.bandInv = recip(4 * p.tilesN);
+    g.full = (int)p.full;
+    g.slices = (int)p.slices;
+    g.slicesInv = recip(p.slices);
+    g.units = (int)p.units;
     constexpr auto kernel = product_kernel<T, FORM, S>;
     if (allow_dynamic_lds<kernel>(S::LDS) != hipSuccess) return GETT_ERROR_HIP;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(tm * tn)), dim3(S::THREADS), S::LDS, s, g, (int)groups);
+    const unsigned blocks = persistent_grid<kernel>(S::THREADS, (unsigned)g.units, S::LDS);
+    if (blocks == 0) return GETT_ERROR_HIP;
+    hipLaunchKernelGGL(kernel, dim3(blocks), dim3(S::THREADS), S::LDS, s, g, (int)groups);
     return launched(hipGetLastError());
 }
 
+// Eight wavefronts of 128 x 64 (one workgroup a CU: its LDS); four of 64 x 64 and of
+// 32 x 32 (two a CU).
+typedef ProductShape<4, 2, 2, 4, 2> ProductBig;
 typedef ProductShape<2, 2, 2, 2, 2> ProductMid;
+typedef ProductShape<1, 1, 2, 2, 4> ProductSmall;
 
 template <typename T, ProductForm FORM>
-gett_status_t product_form(ProductGroups groups, const ProductArgs &g, hipStream_t s)
+gett_status_t product_form(ProductGroups groups, const ProductArgs &g, const ProductPlan &p, hipStream_t s)
 {
-    return product_tiles<T, FORM, ProductMid>(groups, g, s);
+    if constexpr (sizeof(T) == 2)   // (in 32 bits the middle ones are bound by the instructions)
+        if (p.shape == 0) return product_tiles<T, FORM, ProductBig>(groups, g, p, s);
+    if (p.shape == 1) return product_tiles<T, FORM, ProductMid>(groups, g, p, s);
+    return product_tiles<T, FORM, ProductSmall>(groups, g, p, s);
 }
 
 template <typename T>
-gett_status_t product_launch(ProductForm form, ProductGroups groups, const ProductArgs &g, hipStream_t s)
+gett_status_t product_launch(ProductForm form, ProductGroups groups, const ProductArgs &g,
+                             const ProductPlan &p, hipStream_t s)
 {
-    if (form == kRowsRows) return product_form<T, kRowsRows>(groups, g, s);
-    if (form == kRowsColumns) return product_form<T, kRowsColumns>(groups, g, s);
-    return product_form<T, kColumnsColumns>(groups, g, s);
+    if (form == kRowsRows) return product_form<T, kRowsRows>(groups, g, p, s);
+    if (form == kRowsColumns) return product_form<T, kRowsColumns>(groups, g, p, s);
+    return product_form<T, kColumnsColumns>(groups, g, p, s);
 }
 
 }  // namespace gett

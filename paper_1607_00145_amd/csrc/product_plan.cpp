@@ -1,0 +1,106 @@
+// product_plan.cpp -- which tiles a product of product.hpp takes, and how many
+// workgroups share one.
+//
+// A launch lasts as many rounds as its tiles fill the workgroups that are resident
+// at once, each as long as its panels and a fixed part (first loads, results).  Tiles
+// of a last, incomplete round may be cut along K so that their slices fill it, which
+// costs a trip of the partial sums through memory.  The smallest estimate wins.
+//
+// us per panel with the CUs full and with one workgroup each, per tile, and for a
+// join of s slices, measured: the products of 8192 x 8192 x 4096, 1023 x 515 x 1000 and
+// 200 x 4096 x 4096.
+#include "product_plan.hpp"
+
+#include "layers.hpp"
+
+namespace gett {
+
+namespace {
+
+struct ShapeCost {
+    int edge;          // rows and columns of a tile
+    int perCu;         // workgroups resident
+    double full, alone, tile, join, joinEach;
+};
+constexpr ShapeCost kCost16[3] = {{256, 1, 1.50, 1.50, 12.0, 15.0, 6.0},
+                                  {128, 2, 1.00, 0.60, 5.0, 8.0, 1.5},
+                                  {64, 2, 0.45, 0.30, 3.0, 5.0, 0.3}};
+constexpr ShapeCost kCost32[3] = {{256, 1, 1e6, 1e6, 0.0, 0.0, 0.0},
+                                  {128, 2, 3.60, 1.90, 5.0, 8.0, 1.5},
+                                  {64, 2, 1.00, 0.55, 3.0, 5.0, 0.3}};
+constexpr int64_t kCus = 256;
+
+}  // namespace
+
+ProductPlan product_plan(gett_dtype_t dtype, ProductGroups groups, int64_t m, int64_t n, int64_t k,
+                         int64_t experts)
+{
+    const int64_t KP = 128 / type_size(dtype);
+    ProductPlan best = {};
+    double least = 1e300;
+    for (int shape = 0; shape < 3; ++shape) {
+        const ShapeCost &c = dtype == GETT_FLOAT32 ? kCost32[shape] : kCost16[shape];
+        ProductPlan p = {};
+        p.shape = shape;
+        p.tilesM = (m + c.edge - 1) / c.edge;
+        p.tilesN = (n + c.edge - 1) / c.edge;
+        p.bandRows = p.tilesM;
+        int64_t panels = (k + KP - 1) / KP;
+        double tiles = (double)(p.tilesM * p.tilesN);
+        if (groups == kByRows) {
+            // as many tiles as any split among the experts needs; about so many of them
+            // hold rows
+            p.bandRows = m / c.edge + experts + 1;
+            const double used = (double)(experts < m ? experts : m);
+            tiles = (double)m / c.edge + used / 2;
+            tiles = (tiles > used ? tiles : used) * (double)p.tilesN;
+        } else if (groups == kByK) {
+            p.bandRows = p.tilesM * experts;
+            tiles *= (double)experts;
+            panels = (panels + experts - 1) / experts;
+        }
+        p.tiles = p.full = p.units = p.bandRows * p.tilesN;
+        p.slices = 1;
+        const double slots = (double)(kCus * c.perCu);
+        if (groups != kWhole) {
+            const double rounds = tiles / slots;
+            const double part = tiles <= kCus ? c.alone : c.full;
+            // (the experts' tiles differ and even out over the rounds)
+            const double us = (rounds < 1 ? 1 : rounds) * ((double)panels * part + c.tile);
+            if (us < least) {
+                least = us;
+                best = p;
+            }
+            continue;
+        }
+        const int64_t all = kCus * c.perCu, rounds = p.tiles / all, rest = p.tiles % all;
+        for (int64_t s = 1; s <= 16; ++s) {
+            if (s > 1 && (rest == 0 || rest * s > all || panels < 2 * s)) break;
+            double us = (double)rounds * ((double)panels * c.full + c.tile);
+            if (rest)
+                us += (double)((panels + s - 1) / s) * (rest * s <= kCus ? c.alone : c.full) + c.tile;
+            if (s > 1) us += c.join + c.joinEach * (double)s;
+            if (us >= least) continue;
+            least = us;
+            best = p;
+            best.slices = s;
+            best.full = s > 1 ? p.tiles - rest : p.tiles;
+            best.units = best.full + (s > 1 ? rest * s : 0);
+            best.counters = s > 1 ? rest : 0;
+            best.slotBytes = s > 1 ? rest * s * c.edge * c.edge * 4 : 0;
+        }
+    }
+    return best;
+}
+
+}  // namespace gett
+
+extern "C" void gett_product_tiles(gett_dtype_t dtype, int64_t m, int64_t n, int64_t k,
+                                   struct gett_tiles *out)
+{
+    const gett::ProductPlan p = gett::product_plan(dtype, gett::kWhole, m, n, k, 0);
+    out->edge = 256 >> p.shape;
+    out->slices = p.slices;
+    out->shared = p.counters;
+    out->workgroups = p.units;
+}
