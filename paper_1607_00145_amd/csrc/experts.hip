@@ -43,10 +43,11 @@ struct WeightsOperand {
     int64_t step;   // bytes
 };
 WeightsOperand weights_operand(gett_dtype_t t, int64_t experts, int64_t n, int64_t width, const void *W,
-                               int64_t stride, int64_t step, Arena &a)
+                               int64_t stride, int64_t step, bool anywhere, Arena &a)
 {
     const int64_t item = type_size(t);
-    const bool direct = on_grid(t, n, width, W, stride) && (experts == 1 || step * item % 16 == 0);
+    const bool direct = anywhere || (on_grid(t, n, width, W, stride) &&
+                                     (experts == 1 || step * item % 16 == 0));
     WeightsOperand w = {operand_of(t, n, width, W, stride, direct, a, experts * n), 0};
     w.step = w.o.copyAt >= 0 ? n * w.o.ld : step * item;
     return w;
@@ -91,11 +92,12 @@ gett_status_t gett_experts(gett_dtype_t dtype, int64_t tokens, int k, int expert
     hipStream_t s = static_cast<hipStream_t>(stream);
     // rows that are gathered in the product are reached by 32-bit offsets
     const int64_t reach = tokens * stride_x * type_size(dtype);
-    const bool gridX = on_grid(dtype, gather ? tokens : rows, width, X, stride_x) &&
-                       (!gather || reach < 0xffff0000ll);
+    const bool few = product_is_few(kByRows, rows);   // (at any address)
+    const bool gridX = few || (on_grid(dtype, gather ? tokens : rows, width, X, stride_x) &&
+                               (!gather || reach < 0xffff0000ll));
     Arena arena;
     Operand ox = operand_of(dtype, gather ? tokens : rows, width, X, stride_x, gridX, arena, rows);
-    WeightsOperand ow = weights_operand(dtype, experts, n, width, W, stride_w, stride_we, arena);
+    WeightsOperand ow = weights_operand(dtype, experts, n, width, W, stride_w, stride_we, few, arena);
     Partials hold;
     if (arena.bytes) {
         st = stream_workspace(s, 0, arena.bytes, hold);
@@ -118,8 +120,10 @@ gett_status_t gett_experts(gett_dtype_t dtype, int64_t tokens, int k, int expert
     }
     g.out = {static_cast<const char *>(bias), nullptr, static_cast<char *>(Z), static_cast<char *>(Y), 0,
              stride_z, stride_y, activation, 0, {}};
-    return product_launch_of(dtype, kRowsRows, kByRows, g, product_plan(dtype, kByRows, rows, n, width, experts),
-                             hold, 0, s);
+    ProductPlan plan = {};
+    if (few) plan.shape = kFewRows;
+    else plan = product_plan(dtype, kByRows, rows, n, width, experts);
+    return product_launch_of(dtype, kRowsRows, kByRows, g, plan, hold, 0, s);
 }
 
 gett_status_t gett_experts_grad(gett_dtype_t dtype, int64_t tokens, int k, int experts, int64_t n,
@@ -168,7 +172,7 @@ gett_status_t gett_experts_grad(gett_dtype_t dtype, int64_t tokens, int k, int e
     if (ew.bytes)
         ox = operand_of(dtype, rows, width, X, stride_x,
                         !gather && on_grid(dtype, rows, width, X, stride_x), arena, rows);
-    if (ex.bytes) ow = weights_operand(dtype, experts, n, width, W, stride_w, stride_we, arena);
+    if (ex.bytes) ow = weights_operand(dtype, experts, n, width, W, stride_w, stride_we, false, arena);
     const int64_t sumsAt = sum ? arena.take(slope_slots(rows, experts) * n * 4) : -1;
     // the rows' gradients, which a token sums in 32 bits
     const int64_t partsAt = ex.bytes && gather ? arena.take(rows * width * 4) : -1;

@@ -72,10 +72,15 @@ gett_status_t gett_linear(gett_dtype_t dtype, int64_t m, int64_t n, int64_t k, c
         return GETT_ERROR_INVALID_VALUE;
     hipStream_t s = static_cast<hipStream_t>(stream);
     Arena arena;
-    const bool gridX = on_grid(dtype, m, k, X, stride_x), gridW = on_grid(dtype, n, k, W, stride_w);
+    // (few rows are taken at any address)
+    const bool few = product_is_few(kWhole, m);
+    const bool gridX = few || on_grid(dtype, m, k, X, stride_x);
+    const bool gridW = few || on_grid(dtype, n, k, W, stride_w);
     Operand ox = operand_of(dtype, m, k, X, stride_x, gridX, arena, m);
     Operand ow = operand_of(dtype, n, k, W, stride_w, gridW, arena, n);
-    const ProductPlan plan = product_plan(dtype, kWhole, m, n, k, 0);
+    ProductPlan plan = {};
+    if (few) plan.shape = kFewRows;
+    else plan = product_plan(dtype, kWhole, m, n, k, 0);
     const int64_t slots = arena.take(plan.slotBytes);
     Partials hold;
     if (arena.bytes) {

@@ -3,6 +3,7 @@
 #pragma once
 #include "launch.hpp"
 #include "layer_util.hpp"
+#include "product_few.hpp"
 
 namespace gett {
 
@@ -37,6 +38,30 @@ typedef ProductShape<4, 2, 2, 4, 2> ProductBig;
 typedef ProductShape<2, 2, 2, 2, 2> ProductMid;
 typedef ProductShape<1, 1, 2, 2, 4> ProductSmall;
 
+// Few rows: a workgroup for 32 columns and, of experts, for each row that may be an
+// expert's first.
+template <typename T>
+gett_status_t product_few(ProductGroups groups, ProductArgs g, hipStream_t s)
+{
+    const int m = g.m;
+    const int64_t tn = ((int64_t)g.n + kFewCols32 - 1) / kFewCols32;
+    const int64_t blocks = tn * (groups == kByRows ? g.m : 1);
+    if (!fits_launch(blocks, 1024)) return GETT_ERROR_NOT_SUPPORTED;
+    g.tilesN = (int)tn;
+    g.bandInv = recip(tn);
+    auto launch = [&](auto kernel, int threads) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(threads), 0, s, g, (int)groups);
+        return launched(hipGetLastError());
+    };
+    // (experts: rows that share one read its weights once each, from the XCD's cache)
+    if (groups == kByRows && m <= 2 * g.experts) return launch(product_row_kernel<T, 1>, 64 * kRowWaves);
+    if (groups == kWhole && m == 1) return launch(product_row_kernel<T, 1>, 64 * kRowWaves);
+    if (groups == kWhole && m == 2) return launch(product_row_kernel<T, 2>, 64 * kRowWaves);
+    if (groups == kWhole && m <= 4) return launch(product_row_kernel<T, 4>, 64 * kRowWaves);
+    if (groups == kWhole && m > 32) return launch(product_few_kernel<T, 2, 8>, 512);
+    return launch(product_few_kernel<T, 1, 8>, 512);
+}
+
 template <typename T, ProductForm FORM>
 gett_status_t product_form(ProductGroups groups, const ProductArgs &g, const ProductPlan &p, hipStream_t s)
 {
@@ -50,6 +75,8 @@ template <typename T>
 gett_status_t product_launch(ProductForm form, ProductGroups groups, const ProductArgs &g,
                              const ProductPlan &p, hipStream_t s)
 {
+    if (p.shape == kFewRows)
+        return product_few<T>(groups, g, s);
     if (form == kRowsRows) return product_form<T, kRowsRows>(groups, g, p, s);
     if (form == kRowsColumns) return product_form<T, kRowsColumns>(groups, g, p, s);
     return product_form<T, kColumnsColumns>(groups, g, p, s);

@@ -32,6 +32,8 @@ constexpr int64_t kCus = 256;
 
 }  // namespace
 
+bool product_is_few(ProductGroups groups, int64_t m) { return groups != kByK && m <= 64; }
+
 ProductPlan product_plan(gett_dtype_t dtype, ProductGroups groups, int64_t m, int64_t n, int64_t k,
                          int64_t experts)
 {
@@ -98,6 +100,10 @@ ProductPlan product_plan(gett_dtype_t dtype, ProductGroups groups, int64_t m, in
 extern "C" void gett_product_tiles(gett_dtype_t dtype, int64_t m, int64_t n, int64_t k,
                                    struct gett_tiles *out)
 {
+    if (gett::product_is_few(gett::kWhole, m)) {
+        *out = {0, 1, 0, (n + 31) / 32};
+        return;
+    }
     const gett::ProductPlan p = gett::product_plan(dtype, gett::kWhole, m, n, k, 0);
     out->edge = 256 >> p.shape;
     out->slices = p.slices;

@@ -9,8 +9,14 @@ namespace gett {
 enum ProductForm { kRowsRows, kRowsColumns, kColumnsColumns };
 enum ProductGroups { kWhole, kByRows, kByK };
 
+constexpr int kFewRows = 3;   // product_few.hpp
+
+// Whether rows x N^T is one of few rows: y = x w^T of up to 64 rows, or of so many
+// rows of experts in all.
+bool product_is_few(ProductGroups groups, int64_t m);
+
 struct ProductPlan {
-    int shape;                                  // tiles of 256 >> shape
+    int shape;                                  // tiles of 256 >> shape, or kFewRows
     int64_t tilesM, tilesN, bandRows, tiles;    // bandRows: rows of tiles of all experts
     int64_t full, slices, units;                // tiles from `full` on: `slices` workgroups
     int64_t counters, slotBytes;                // of the workspace
