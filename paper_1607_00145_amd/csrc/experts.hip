@@ -173,7 +173,7 @@ gett_status_t gett_experts_grad(gett_dtype_t dtype, int64_t tokens, int k, int e
         ox = operand_of(dtype, rows, width, X, stride_x,
                         !gather && on_grid(dtype, rows, width, X, stride_x), arena, rows);
     if (ex.bytes) ow = weights_operand(dtype, experts, n, width, W, stride_w, stride_we, false, arena);
-    const int64_t sumsAt = sum ? arena.take(slope_slots(rows, experts) * n * 4) : -1;
+    const int64_t sumsAt = sum ? arena.take(slope_slots(rows, n, experts) * n * 4) : -1;
     // the rows' gradients, which a token sums in 32 bits
     const int64_t partsAt = ex.bytes && gather ? arena.take(rows * width * 4) : -1;
     Partials hold;
@@ -183,7 +183,7 @@ gett_status_t gett_experts_grad(gett_dtype_t dtype, int64_t tokens, int k, int e
     }
     char *ws = static_cast<char *>(hold.tiles);
     SlopeJob j = {dY, Z, nullptr, sum ? reinterpret_cast<float *>(ws + sumsAt) : nullptr, stride_dy,
-                  stride_z, 0, (int)rows, (int)n, activation, {}, offsets, experts, 0, {}};
+                  stride_z, 0, (int)rows, (int)n, activation, {}, offsets, experts, 0, 0, {}};
     if (oz.copyAt >= 0) {
         oz.p = ws + oz.copyAt;
         j.dZ = ws + oz.copyAt;

@@ -45,48 +45,80 @@ __global__ __launch_bounds__(256) void layer_copy_kernel(CopyJob j)
 
 // ------------------------------------------------------- epilogue's gradient ---
 
-constexpr int kSlopeRows = 64;   // rows of a workgroup
-constexpr int kSlopeCols = 256;  // columns: 32 lanes of eight
+constexpr int kSlopeCols = 256;  // columns of a workgroup: 32 lanes of eight
+
+// Rows of a workgroup: as many as leave four workgroups a CU, between 8 and 64 (1023 x
+// 515 in 32 bits, of 64 rows each 25 us, of 8 rows 5).
+int slope_log2(int64_t m, int64_t n)
+{
+    const int64_t across = (n + kSlopeCols - 1) / kSlopeCols;
+    int l = 3;
+    while (l < 6 && (m >> (l + 1)) * across >= 1024) ++l;
+    return l;
+}
+
+// The slots (runs of 1 << shift rows) of expert e begin with offsets[e] >> shift, plus e.
+__device__ __forceinline__ void slope_slots_of(const SlopeJob &j, int e, int &first, int &count)
+{
+    int b = 0, f = j.m;
+    if (j.offsets) {
+        b = expert_offset(j.offsets, e, j.m);
+        f = expert_offset(j.offsets, e + 1, j.m);
+    }
+    first = (b >> j.shift) + e;
+    count = f > b ? (f - b + (1 << j.shift) - 1) >> j.shift : 0;
+}
 
 // dz = dropout(dy) act'(z), written with zeros behind the last column, and the sums
-// of each column over the workgroup's rows: eight rows at a time, the eight
-// partial sums of a column added in the same order each time.
+// of each column over the workgroup's rows: eight rows at a time, two loads each on
+// their way, the eight partial sums of a column added in the same order each time.
 template <typename T>
 __global__ __launch_bounds__(256) void layer_slope_kernel(SlopeJob j)
 {
     __shared__ float sums[8][kSlopeCols];
     const int lane = (int)threadIdx.x & 31, strip = (int)threadIdx.x >> 5;
     const int slot = (int)quotient(blockIdx.x, j.across, j.acrossInv);
-    int begin = slot * kSlopeRows, end = j.m;
+    const int size = 1 << j.shift;
+    int begin = slot << j.shift, end = j.m;
     if (j.offsets) {
-        const int e = expert_of_slot<kSlopeRows>(j.offsets, j.experts, j.m, slot);
+        const int e = expert_of_slot(j.offsets, j.experts, j.m, slot, j.shift);
         const int b = expert_offset(j.offsets, e, j.m);
-        begin = b + (slot - (b / kSlopeRows + e)) * kSlopeRows;
+        begin = b + (slot - ((b >> j.shift) + e)) * size;
         end = e == j.experts ? 0 : expert_offset(j.offsets, e + 1, j.m);   // (none behind the last)
     }
-    if (begin + kSlopeRows < end) end = begin + kSlopeRows;
+    if (begin + size < end) end = begin + size;
     const int col0 = ((int)blockIdx.x - slot * j.across) * kSlopeCols, col = col0 + lane * 8;
     const int left = j.n - col;
     const uint64_t key = j.drop.cut ? j.drop.key() : 0;
+    const bool active = j.activation != GETT_ACTIVATION_NONE;
     float total[8] = {};
     if (left > 0) {
-        for (int row = begin + strip; row < end; row += 8) {
-            float v[8];
-            load8(reinterpret_cast<const T *>(j.dY) + row * j.ldy + col, left, v);
-            if (j.activation != GETT_ACTIVATION_NONE) {
-                float z[8];
-                load8(reinterpret_cast<const T *>(j.Z) + row * j.ldz + col, left, z);
+        for (int row0 = begin + strip; row0 < end; row0 += 16) {
+            float v[2][8], z[2][8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (i < left) v[i] *= slope(j.activation, z[i]);
+            for (int x = 0; x < 2; ++x)
+                if (row0 + 8 * x < end) {
+                    load8(reinterpret_cast<const T *>(j.dY) + (row0 + 8 * x) * j.ldy + col, left, v[x]);
+                    if (active)
+                        load8(reinterpret_cast<const T *>(j.Z) + (row0 + 8 * x) * j.ldz + col, left, z[x]);
+                }
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const int row = row0 + 8 * x;
+                if (row >= end) break;
+                if (active) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        if (i < left) v[x][i] *= slope(j.activation, z[x][i]);
+                }
+                // (last: what is dropped is zero, whatever it was)
+                if (j.drop.cut) drop8(v[x], j.drop, key, (uint32_t)row, (uint32_t)col);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) total[i] += v[x][i];
+                if (j.dZ)
+                    store8(reinterpret_cast<T *>(j.dZ) + row * j.ldd + col,
+                           j.ldd - col < 8 ? (int)(j.ldd - col) : 8, v[x]);
             }
-            // (last: what is dropped is zero, whatever it was)
-            if (j.drop.cut) drop8(v, j.drop, key, (uint32_t)row, (uint32_t)col);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) total[i] += v[i];
-            if (j.dZ)
-                store8(reinterpret_cast<T *>(j.dZ) + row * j.ldd + col,
-                       j.ldd - col < 8 ? (int)(j.ldd - col) : 8, v);
         }
     }
     if (!j.sums) return;
@@ -101,27 +133,34 @@ __global__ __launch_bounds__(256) void layer_slope_kernel(SlopeJob j)
     j.sums[(int64_t)slot * j.n + c] = t;
 }
 
-// A column's sum over the workgroups of layer_slope_kernel, of each expert.  Four
-// running sums, added in a fixed order.
+// A column's sum over the slots of each expert: 32 columns a workgroup, eight strips of
+// every eighth slot, added in a fixed order.
 template <typename T>
 __global__ __launch_bounds__(256) void layer_sums_kernel(SlopeJob j, T *out)
 {
-    const int c = (int)blockIdx.x * 256 + (int)threadIdx.x, e = (int)blockIdx.y;
-    if (c >= j.n) return;
-    int first = 0, count = (j.m + kSlopeRows - 1) / kSlopeRows;
-    if (j.offsets) {
-        const int b = expert_offset(j.offsets, e, j.m), f = expert_offset(j.offsets, e + 1, j.m);
-        first = b / kSlopeRows + e;
-        count = f > b ? (f - b + kSlopeRows - 1) / kSlopeRows : 0;
+    __shared__ float sums[8][32];
+    const int lane = (int)threadIdx.x & 31, strip = (int)threadIdx.x >> 5;
+    const int e = (int)quotient(blockIdx.x, j.across, j.acrossInv);
+    const int c = ((int)blockIdx.x - e * j.across) * 32 + lane;
+    int first, count;
+    slope_slots_of(j, e, first, count);
+    float t[2] = {};
+    if (c < j.n) {
+        const float *p = j.sums + (int64_t)first * j.n + c;
+        int i = strip;
+        for (; i + 8 < count; i += 16) {
+            t[0] += p[(int64_t)i * j.n];
+            t[1] += p[(int64_t)(i + 8) * j.n];
+        }
+        if (i < count) t[0] += p[(int64_t)i * j.n];
     }
-    const float *p = j.sums + (int64_t)first * j.n + c;
-    float t[4] = {};
-    int i = 0;
-    for (; i + 4 <= count; i += 4)
+    sums[strip][lane] = t[0] + t[1];
+    __syncthreads();
+    if (strip || c >= j.n) return;
+    float v = 0.0f;
 #pragma unroll
-        for (int x = 0; x < 4; ++x) t[x] += p[(int64_t)(i + x) * j.n];
-    for (; i < count; ++i) t[0] += p[(int64_t)i * j.n];
-    out[(int64_t)e * j.n + c] = from_float<T>((t[0] + t[1]) + (t[2] + t[3]));
+    for (int i = 0; i < 8; ++i) v += sums[i][lane];
+    out[(int64_t)e * j.n + c] = from_float<T>(v);
 }
 
 // ------------------------------------------------------------------ combine ---
@@ -138,14 +177,26 @@ __global__ __launch_bounds__(256) void combine_kernel(CombineJob j)
     const uint32_t rows = (uint32_t)j.tokens * j.k;
     float v[8] = {};
     if (j.residual) load8(reinterpret_cast<const T *>(j.residual) + t * j.ldr + col, left, v);
-    for (int i = 0; i < j.k; ++i) {
-        const uint32_t p = (uint32_t)j.place[t * j.k + i];
-        if (p >= rows) continue;
-        const float w = j.weights ? to_float(reinterpret_cast<const W *>(j.weights)[t * j.k + i]) : 1.0f;
-        float x[8];
-        load8(reinterpret_cast<const H *>(j.H) + (int64_t)p * j.ldh + col, left, x);
+    // four rows on their way (one after the other, eight take 5 us of latencies)
+    for (int i0 = 0; i0 < j.k; i0 += 4) {
+        uint32_t p[4];
+        float w[4], x[4][8];
 #pragma unroll
-        for (int c = 0; c < 8; ++c) v[c] += w * x[c];
+        for (int i = 0; i < 4; ++i) {
+            const bool there = i0 + i < j.k;
+            p[i] = there ? (uint32_t)j.place[t * j.k + i0 + i] : rows;
+            w[i] = there && j.weights ? to_float(reinterpret_cast<const W *>(j.weights)[t * j.k + i0 + i])
+                                      : 1.0f;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (p[i] < rows)
+                load8(reinterpret_cast<const H *>(j.H) + (int64_t)p[i] * j.ldh + col, left, x[i]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (p[i] < rows)
+#pragma unroll
+                for (int c = 0; c < 8; ++c) v[c] += w[i] * x[i][c];
     }
     store8(reinterpret_cast<T *>(j.Y) + t * j.ldy + col, left, v);
 }
@@ -208,16 +259,18 @@ gett_status_t copy_launch(gett_dtype_t t, const CopyJob &j, hipStream_t s)
     });
 }
 
-int64_t slope_slots(int64_t m, int experts)
+int64_t slope_slots(int64_t m, int64_t n, int experts)
 {
-    return experts ? m / kSlopeRows + experts + 1 : (m + kSlopeRows - 1) / kSlopeRows;
+    const int l = slope_log2(m, n);
+    return experts ? (m >> l) + experts + 1 : (m + (1 << l) - 1) >> l;
 }
 gett_status_t slope_launch(gett_dtype_t t, SlopeJob j, hipStream_t s)
 {
-    const int64_t slots = slope_slots(j.m, j.offsets ? j.experts : 0);
+    const int64_t slots = slope_slots(j.m, j.n, j.offsets ? j.experts : 0);
     const int64_t across = (j.n + kSlopeCols - 1) / kSlopeCols;
     if (slots == 0 || across == 0) return GETT_SUCCESS;
     if (!fits_launch(slots * across, 256)) return GETT_ERROR_NOT_SUPPORTED;
+    j.shift = slope_log2(j.m, j.n);
     j.across = (int)across;
     j.acrossInv = recip(across);
     return with_type(t, [&](auto v) {
@@ -226,13 +279,18 @@ gett_status_t slope_launch(gett_dtype_t t, SlopeJob j, hipStream_t s)
         return launched(hipGetLastError());
     });
 }
-gett_status_t sums_launch(gett_dtype_t t, const SlopeJob &j, void *out, hipStream_t s)
+gett_status_t sums_launch(gett_dtype_t t, SlopeJob j, void *out, hipStream_t s)
 {
+    const int64_t across = (j.n + 31) / 32, blocks = across * (j.offsets ? j.experts : 1);
+    if (blocks == 0) return GETT_SUCCESS;
+    if (!fits_launch(blocks, 256)) return GETT_ERROR_NOT_SUPPORTED;
+    j.shift = slope_log2(j.m, j.n);
+    j.across = (int)across;
+    j.acrossInv = recip(across);
     return with_type(t, [&](auto v) {
         typedef decltype(v) T;
-        hipLaunchKernelGGL(layer_sums_kernel<T>,
-                           dim3((unsigned)((j.n + 255) / 256), (unsigned)(j.offsets ? j.experts : 1)),
-                           dim3(256), 0, s, j, static_cast<T *>(out));
+        hipLaunchKernelGGL(layer_sums_kernel<T>, dim3((unsigned)blocks), dim3(256), 0, s, j,
+                           static_cast<T *>(out));
         return launched(hipGetLastError());
     });
 }

@@ -31,12 +31,12 @@ struct SlopeJob {
     Drop drop;
     const int32_t *offsets;  // rows by expert, or nullptr
     int experts;
-    int across;              // workgroups along the columns (set by the launch)
+    int across, shift;       // workgroups along the columns, rows of one (set by the launch)
     Recip acrossInv;
 };
-int64_t slope_slots(int64_t m, int experts);   // experts 0: no offsets
+int64_t slope_slots(int64_t m, int64_t n, int experts);   // experts 0: no offsets
 gett_status_t slope_launch(gett_dtype_t t, SlopeJob j, hipStream_t s);
-gett_status_t sums_launch(gett_dtype_t t, const SlopeJob &j, void *out, hipStream_t s);
+gett_status_t sums_launch(gett_dtype_t t, SlopeJob j, void *out, hipStream_t s);
 
 struct CombineJob {
     const void *H, *weights, *residual;

@@ -136,7 +136,7 @@ gett_status_t gett_linear_grad(gett_dtype_t dtype, int64_t m, int64_t n, int64_t
     Operand ox = {nullptr, 16, 0, -1}, ow = ox;
     if (ew.bytes) ox = operand_of(dtype, m, k, X, stride_x, on_grid(dtype, m, k, X, stride_x), arena, m);
     if (ex.bytes) ow = operand_of(dtype, n, k, W, stride_w, on_grid(dtype, n, k, W, stride_w), arena, n);
-    const int64_t sumsAt = sum ? arena.take(slope_slots(m, 0) * n * 4) : -1;
+    const int64_t sumsAt = sum ? arena.take(slope_slots(m, n, 0) * n * 4) : -1;
     ProductPlan px = {}, pw = {};
     if (ex.bytes) px = product_plan(dtype, kWhole, m, k, n, 0);
     if (ew.bytes) pw = product_plan(dtype, kWhole, n, k, m, 0);
@@ -150,7 +150,7 @@ gett_status_t gett_linear_grad(gett_dtype_t dtype, int64_t m, int64_t n, int64_t
     }
     char *ws = static_cast<char *>(hold.tiles);
     SlopeJob j = {dY, Z, nullptr, sum ? reinterpret_cast<float *>(ws + sumsAt) : nullptr, stride_dy,
-                  stride_z, 0, (int)m, (int)n, activation, d, nullptr, 0, 0, {}};
+                  stride_z, 0, (int)m, (int)n, activation, d, nullptr, 0, 0, 0, {}};
     if (oz.copyAt >= 0) {
         oz.p = ws + oz.copyAt;
         j.dZ = ws + oz.copyAt;

@@ -414,18 +414,18 @@ __device__ __forceinline__ int expert_offset(const int32_t *offsets, int e, int 
     return v < 0 ? 0 : v > rows ? rows : v;
 }
 
-// Tiles of BM rows of a list of experts.  Expert e's begin with number
-// offsets[e] / BM + e, which leaves each as many as it needs and needs no table:
+// Tiles of 1 << shift rows of a list of experts.  Expert e's begin with number
+// (offsets[e] >> shift) + e, which leaves each as many as it needs and needs no table:
 // the last e whose first is not behind `slot`.  What lies behind the last expert's
 // rows counts as one more expert.
-template <int BM>
-__device__ __forceinline__ int expert_of_slot(const int32_t *offsets, int experts, int rows, int slot)
+__device__ __forceinline__ int expert_of_slot(const int32_t *offsets, int experts, int rows, int slot,
+                                              int shift)
 {
     const int lane = (int)threadIdx.x & 63;
     int found = 0;
     for (int e0 = 0; e0 <= experts; e0 += 64) {
         const int e = e0 + lane;
-        const bool before = e <= experts && expert_offset(offsets, e < experts ? e : experts, rows) / BM + e <= slot;
+        const bool before = e <= experts && (expert_offset(offsets, e < experts ? e : experts, rows) >> shift) + e <= slot;
         const int n = __popcll(__ballot(before));
         found += n;
         if (n < 64) break;
@@ -471,7 +471,7 @@ __device__ __forceinline__ bool product_tile(const ProductArgs &g, int groups, i
     t.empty = false;
     if (groups == kByRows) {
         const int e = __builtin_amdgcn_readfirstlane(
-            expert_of_slot<S::BM>(g.offsets, g.experts, g.m, tm));
+            expert_of_slot(g.offsets, g.experts, g.m, tm, __builtin_ctz(S::BM)));
         const int begin = expert_offset(g.offsets, e, g.m);
         t.e = e;
         t.empty = e == g.experts;
