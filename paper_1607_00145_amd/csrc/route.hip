@@ -1,11 +1,16 @@
 // route.hip -- the choice of experts and the order of the chosen rows.
 //
-// A wavefront takes a token: lane l holds the experts l, l + 64, ...; the k largest
-// are taken one by one (k is small), each the largest of the lanes' largest.  The
-// order of the rows by expert is a stable counting sort: chunks of 1024 rows are
-// counted, the counts summed over the chunks, and each chunk writes its rows, with no
-// atomics whose order could show.  Up to 1024 rows it is one launch of one
-// workgroup in all.
+// A wavefront takes a token; the k largest are taken one by one (k is small), each the
+// largest of the lanes' largest, of equal ones the lowest.  What is compared is held
+// in 64 bits, as whole numbers of the same order whose halves go through the
+// wavefront one after the other (DPP: no trip through LDS).  (Choosing in 32 bits, and
+// again in 64 where a bound of the error does not decide, was no faster: one token in
+// a hundred is enough for every workgroup to wait for one.)
+//
+// The order of the rows by expert is a stable counting sort: chunks of whole tokens,
+// up to 512 rows, are chosen and counted in one launch, the counts summed over the
+// chunks, and each chunk writes its rows, with no atomics whose order could show.  Up
+// to 512 rows it is one launch of one workgroup in all.
 #include "launch.hpp"
 #include "layer_util.hpp"
 
@@ -13,7 +18,8 @@ namespace gett {
 
 namespace {
 
-constexpr int kChunk = 1024;   // rows (token, choice) that a workgroup orders
+constexpr int kChunk = 512;       // rows (token, choice) of a workgroup, at most
+constexpr int kThreads = 1024;
 
 struct RouteJob {
     const void *logits;
@@ -23,8 +29,8 @@ struct RouteJob {
     double scale;
     float *weights;
     int32_t *index, *order, *offsets, *place;
-    int32_t *counts;   // chunks x experts
-    int chunks;
+    int32_t *counts;   // experts x chunks, then the experts' totals
+    int chunks, chunkTokens;
 };
 
 // A larger one first, of equal ones the lower index; -inf is nothing.
@@ -58,133 +64,282 @@ __device__ __forceinline__ float wave_max(float v)
     return v;
 }
 
-// One token; `keys` holds `experts` doubles of LDS of the wavefront's own.
-template <typename T, int PER>
-__device__ __forceinline__ void choose(const RouteJob &j, int64_t token, double *keys)
+// One token in 64 bits: lane l sees to the experts l, l + 64, ... and the groups l,
+// l + 64, ...  `keys` holds `experts` doubles of LDS of the wavefront's own.  Nearly
+// never run: small, not fast.
+template <typename T>
+__device__ __forceinline__ void choose_exactly(const RouteJob &j, int64_t token, double *keys)
 {
     const int lane = (int)threadIdx.x & 63;
     const double none = -__builtin_huge_val();
+    const float least = -__builtin_huge_valf();
+    const bool soft = j.scoring == GETT_SCORE_SOFTMAX, plain = !j.bias && j.groups == 1;
     const T *row = reinterpret_cast<const T *>(j.logits) + token * j.ld;
-    float x[PER];
     bool nan = false;
-    float most = -__builtin_huge_valf();
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        const int e = i * 64 + lane;
-        x[i] = e < j.experts ? to_float(row[e]) : -__builtin_huge_valf();
-        if (x[i] != x[i]) {
-            nan = true;
-            x[i] = -__builtin_huge_valf();
-        }
-        most = fmaxf(most, x[i]);
+    float most = least;
+    for (int e = lane; e < j.experts; e += 64) {
+        const float x = to_float(row[e]);
+        nan |= x != x;
+        most = fmaxf(most, x);   // (a NaN is passed over)
     }
     nan = __any(nan);
     most = wave_max(most);
-    // scores in 64 bits
-    double s[PER], total = 0.0;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        if (j.scoring == GETT_SCORE_SOFTMAX) {
-            s[i] = x[i] == -__builtin_huge_valf() ? 0.0 : exp((double)x[i] - (double)most);
-            total += s[i];
-        } else {
-            s[i] = 1.0 / (1.0 + exp(-(double)x[i]));
+    double total = 1.0;
+    if (soft) {
+        total = 0.0;
+        for (int e = lane; e < j.experts; e += 64) {
+            const float x = to_float(row[e]);
+            if (x > least) total += exp((double)x - (double)most);
         }
-    }
-    if (j.scoring == GETT_SCORE_SOFTMAX) {
         total = wave_sum(total);
-#pragma unroll
-        for (int i = 0; i < PER; ++i) s[i] /= total;
     }
-    // choices
-    const bool plain = !j.bias && j.groups == 1;
-    double key[PER];
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        const int e = i * 64 + lane;
+    auto score_of = [&](float x) {
+        return soft ? exp((double)x - (double)most) / total : 1.0 / (1.0 + exp(-(double)x));
+    };
+    for (int e = lane; e < j.experts; e += 64) {
+        const float x = to_float(row[e]);
         double c = none;
-        if (e < j.experts && x[i] != -__builtin_huge_valf()) {
-            c = plain ? (double)x[i] : j.bias ? s[i] + (double)j.bias[e] : s[i];
-            if (c != c) c = none;
-        }
-        key[i] = c;
+        if (x > least) c = plain ? (double)x : j.bias ? score_of(x) + (double)j.bias[e] : score_of(x);
+        keys[e] = c != c ? none : c;
     }
     if (j.groups > 1) {
-#pragma unroll
-        for (int i = 0; i < PER; ++i)
-            if (i * 64 + lane < j.experts) keys[i * 64 + lane] = key[i];
         const int size = j.experts / j.groups;
-        // lane g holds the groups g, g + 64, ...
-        double score[PER];
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const int g = i * 64 + lane;
-            double a = none, b = none;
-            if (g < j.groups)
-                for (int e = g * size; e < (g + 1) * size; ++e) {
-                    const double v = keys[e];
-                    if (v > a) {
-                        b = a;
-                        a = v;
-                    } else if (v > b) {
-                        b = v;
-                    }
-                }
-            score[i] = b > none ? a + b : a;
-        }
         uint32_t open = 0;   // of this lane's groups
         for (int r = 0; r < j.topGroups; ++r) {
-            Best b = {none, INT32_MAX};
-#pragma unroll
-            for (int i = 0; i < PER; ++i) b.take(score[i], i * 64 + lane);
-            b = wave_best(b);
-            if (b.key == none) break;
-#pragma unroll
-            for (int i = 0; i < PER; ++i)
-                if (b.at == i * 64 + lane) {
-                    open |= 1u << i;
-                    score[i] = none;
+            Best best = {none, INT32_MAX};
+            for (int g = lane; g < j.groups; g += 64) {
+                if (open >> (g >> 6) & 1) continue;
+                double a = none, b = none;
+                for (int e = g * size; e < (g + 1) * size; ++e) {
+                    const double v = keys[e];
+                    b = v > a ? a : v > b ? v : b;
+                    a = v > a ? v : a;
                 }
+                best.take(b > none ? a + b : a, g);
+            }
+            best = wave_best(best);
+            if (best.key == none) break;
+            if ((best.at & 63) == lane) open |= 1u << (best.at >> 6);
         }
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const int e = i * 64 + lane, g = e < j.experts ? e / size : 0;
+        for (int e0 = 0; e0 < j.experts; e0 += 64) {
+            const int e = e0 + lane, g = e < j.experts ? e / size : 0;
             const uint32_t bits = __shfl(open, g & 63);
-            if (!(bits >> (g >> 6) & 1)) key[i] = none;
+            if (e < j.experts && !(bits >> (g >> 6) & 1)) keys[e] = none;
         }
     }
     // the k largest: lane r keeps the r-th
     int mine = -1;
-    double score = 0.0, sum = 0.0;
     for (int r = 0; r < j.k; ++r) {
-        Best b = {none, INT32_MAX};
-#pragma unroll
-        for (int i = 0; i < PER; ++i) b.take(key[i], i * 64 + lane);
-        b = wave_best(b);
-        if (b.key == none) break;
-        double v = 0.0;
-#pragma unroll
-        for (int i = 0; i < PER; ++i)
-            if (b.at == i * 64 + lane) {
-                v = s[i];
-                key[i] = none;
-            }
-        v = __shfl(v, b.at & 63);
-        sum += v;
-        if (lane == r) {
-            mine = b.at;
-            score = v;
-        }
+        Best best = {none, INT32_MAX};
+        for (int e = lane; e < j.experts; e += 64) best.take(keys[e], e);
+        best = wave_best(best);
+        if (best.key == none) break;
+        if ((best.at & 63) == lane) keys[best.at] = none;
+        if (lane == r) mine = best.at;
+    }
+    const double score = mine >= 0 ? score_of(to_float(row[mine])) : 0.0;
+    double w = score;
+    if (j.renormalize) {
+        const double sum = wave_sum(score);
+        w = sum > 0.0 || sum != sum ? score / sum : 0.0;
     }
     if (lane < j.k) {
-        double w = score;
-        if (j.renormalize) w = sum > 0.0 || sum != sum ? score / sum : 0.0;
         float out = mine < 0 ? 0.0f : (float)(w * j.scale);
-        if (nan || (j.scoring == GETT_SCORE_SOFTMAX && most == __builtin_huge_valf()))
-            out = __builtin_nanf("");
+        if (nan || (soft && most == __builtin_huge_valf())) out = __builtin_nanf("");
         j.weights[token * j.k + lane] = out;
         j.index[token * j.k + lane] = mine;
     }
+}
+
+// The largest of the lanes' values.
+__device__ __forceinline__ uint32_t wave_max_u32(uint32_t v)
+{
+    auto step = [&](auto ctrl) {
+        v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, decltype(ctrl)::value, 0xf, 0xf, false));
+    };
+    step(std::integral_constant<int, 0x111>{});   // from the lane 1, 2, 4, 8 before in the row
+    step(std::integral_constant<int, 0x112>{});
+    step(std::integral_constant<int, 0x114>{});
+    step(std::integral_constant<int, 0x118>{});
+    step(std::integral_constant<int, 0x142>{});   // from the last lane of the row before,
+    step(std::integral_constant<int, 0x143>{});   // and of the half before
+    return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
+}
+// Numbers as whole numbers of the same order (no NaN, -0 made 0); 0 is less than all.
+__device__ __forceinline__ uint64_t ordered(double d)
+{
+    const uint64_t b = (uint64_t)__double_as_longlong(d + 0.0);
+    return b ^ (b >> 63 ? ~0ull : 1ull << 63);
+}
+__device__ __forceinline__ double from_ordered(uint64_t u)
+{
+    return __longlong_as_double((long long)(u ^ (u >> 63 ? 1ull << 63 : ~0ull)));
+}
+// The largest of the lanes' N values each, in halves: which lane has it, and where; of
+// equal ones the lowest lane's lowest.  False where all are 0.  The low halves are only
+// looked at where the high ones do not decide.
+template <int N>
+__device__ __forceinline__ bool pick(const uint32_t (&high)[N], const uint32_t (&low)[N], int &lane, int &at)
+{
+    uint32_t local = high[0];
+#pragma unroll
+    for (int i = 1; i < N; ++i) local = max(local, high[i]);
+    const uint32_t most = wave_max_u32(local);
+    if (most == 0) return false;
+    uint64_t has[N], any = 0;
+    int count = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        has[i] = __ballot(high[i] == most);
+        any |= has[i];
+        count += __popcll(has[i]);
+    }
+    if (count > 1) {
+        uint32_t l = 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) l = max(l, high[i] == most ? low[i] : 0);
+        l = wave_max_u32(l);
+        any = 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            has[i] = __ballot(high[i] == most && low[i] == l);
+            any |= has[i];
+        }
+    }
+    lane = __ffsll((unsigned long long)any) - 1;
+    at = 0;
+#pragma unroll
+    for (int i = N - 1; i >= 0; --i)
+        if (has[i] >> lane & 1) at = i;
+    return true;
+}
+
+// One token whose logits and biases are numbers: lane l holds the experts PER l ... PER l
+// + PER - 1, a group has a power of two of lanes.  False where that is not so (nothing
+// is written then).
+template <typename T, int PER>
+__device__ __forceinline__ bool choose_quickly(const RouteJob &j, int64_t token)
+{
+    const int lane = (int)threadIdx.x & 63;
+    const float none = -__builtin_huge_valf();
+    const bool soft = j.scoring == GETT_SCORE_SOFTMAX, plain = !j.bias && j.groups == 1;
+    const int size = j.experts / j.groups, lanes = size / PER;   // lanes of a group
+    if (j.groups > 1 && (size % PER || (lanes & (lanes - 1)))) return false;
+    const T *row = reinterpret_cast<const T *>(j.logits) + token * j.ld + lane * PER;
+    float x[PER], most = none;
+    bool odd = false;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const bool there = lane * PER + i < j.experts;
+        x[i] = there ? to_float(row[i]) : none;
+        odd |= x[i] != x[i] || x[i] == __builtin_huge_valf();
+        most = fmaxf(most, x[i]);
+    }
+    uint64_t key[PER];
+    double total = 1.0;
+    if (soft) most = wave_max(most);
+    if (plain) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) key[i] = x[i] == none ? 0 : ordered((double)x[i]);
+    }
+    if (!plain || (soft && !j.renormalize)) {   // scores, or their sum
+        double s[PER];
+        if (soft) {
+            total = 0.0;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                s[i] = x[i] == none ? 0.0 : exp((double)x[i] - (double)most);
+                total += s[i];
+            }
+            total = wave_sum(total);
+        }
+        if (!plain) {
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                double c = soft ? s[i] / total : 1.0 / (1.0 + exp(-(double)x[i]));
+                if (j.bias) {
+                    const float bias = lane * PER + i < j.experts ? j.bias[lane * PER + i] : 0.0f;
+                    odd |= !(fabsf(bias) < __builtin_huge_valf());
+                    c += (double)bias;
+                }
+                key[i] = x[i] == none ? 0 : ordered(c);
+            }
+        }
+    }
+    if (__any(odd)) return false;
+    if (j.groups > 1) {
+        // the two largest of each group
+        uint64_t a = 0, b = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            b = max(b, min(a, key[i]));
+            a = max(a, key[i]);
+        }
+        for (int d = 1; d < lanes; d <<= 1) {
+            const uint64_t a2 = __shfl_xor(a, d), b2 = __shfl_xor(b, d);
+            b = max(min(a, a2), max(b, b2));
+            a = max(a, a2);
+        }
+        uint64_t sum = a == 0 ? 0 : ordered(b ? from_ordered(a) + from_ordered(b) : from_ordered(a));
+        if (lane * PER >= j.experts || lane & (lanes - 1)) sum = 0;   // a group's first lane has it
+        uint32_t high[1] = {(uint32_t)(sum >> 32)}, low[1] = {(uint32_t)sum};
+        bool open = false;
+        for (int r = 0; r < j.topGroups; ++r) {
+            int first, at;
+            if (!pick<1>(high, low, first, at)) break;
+            open |= lane >= first && lane < first + lanes;
+            if (lane == first) high[0] = 0;
+        }
+        if (!open) {
+#pragma unroll
+            for (int i = 0; i < PER; ++i) key[i] = 0;
+        }
+    }
+    uint32_t high[PER], low[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        high[i] = (uint32_t)(key[i] >> 32);
+        low[i] = (uint32_t)key[i];
+    }
+    int mine = -1;
+    float chosen = 0.0f;
+    for (int r = 0; r < j.k; ++r) {
+        int from, at;
+        if (!pick<PER>(high, low, from, at)) break;
+        float v = x[0];
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            if (i == at) v = x[i];
+            if (i == at && lane == from) high[i] = 0;
+        }
+        v = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), from));
+        if (lane == r) {
+            mine = from * PER + at;
+            chosen = v;
+        }
+    }
+    double score = 0.0;
+    if (mine >= 0)
+        score = soft ? exp((double)chosen - (double)most) / total : 1.0 / (1.0 + exp(-(double)chosen));
+    double w = score;
+    if (j.renormalize) {
+        const double sum = wave_sum(score);
+        w = sum > 0.0 ? score / sum : 0.0;
+    }
+    if (lane < j.k) {
+        j.weights[token * j.k + lane] = mine < 0 ? 0.0f : (float)(w * j.scale);
+        j.index[token * j.k + lane] = mine;
+    }
+    return true;
+}
+
+template <typename T, int PER>
+__device__ __forceinline__ void choose(const RouteJob &j, int64_t token, double *keys)
+{
+    if constexpr (PER <= 8) {   // (of 1024 experts a lane's sixteen do not fit the registers)
+        if (choose_quickly<T, PER>(j, token)) return;
+    }
+    choose_exactly<T>(j, token, keys);
 }
 
 // The lanes of a wavefront that have the same e, 0 <= e < 1024.
@@ -199,16 +354,15 @@ __device__ __forceinline__ uint64_t same_lanes(int e)
     return m;
 }
 
-// Writes a chunk's rows.  `waves` holds 16 x experts counts; base[e] is where the
-// chunk's rows of expert e begin.
-__device__ __forceinline__ void place_chunk(const RouteJob &j, int chunk, int32_t *waves,
-                                            const int32_t *base)
+// Writes a chunk's rows, those from row0 on.  `waves` holds 8 x experts counts; base[e]
+// is where the chunk's rows of expert e begin.
+__device__ __forceinline__ void place_rows(const RouteJob &j, int row0, int rows, int32_t *waves,
+                                           const int32_t *base)
 {
-    const int rows = j.tokens * j.k;
-    const int r = chunk * kChunk + (int)threadIdx.x, lane = (int)threadIdx.x & 63;
-    const int wave = (int)threadIdx.x >> 6;
-    const int e = r < rows ? j.index[r] : -1;
-    for (int i = (int)threadIdx.x; i < 16 * j.experts; i += kChunk) waves[i] = 0;
+    const int tid = (int)threadIdx.x, r = row0 + tid, lane = tid & 63, wave = tid >> 6;
+    const bool there = tid < kChunk && tid < rows;
+    const int e = there ? j.index[r] : -1;
+    for (int i = tid; i < kChunk / 64 * j.experts; i += kThreads) waves[i] = 0;
     __syncthreads();
     const uint64_t alike = same_lanes(e < 0 ? 0 : e) & __ballot(e >= 0);
     const int rank = __popcll(alike & ((1ull << lane) - 1));
@@ -219,23 +373,27 @@ __device__ __forceinline__ void place_chunk(const RouteJob &j, int chunk, int32_
         for (int w = 0; w < wave; ++w) at += waves[w * j.experts + e];
         j.order[at] = r;
         j.place[r] = at;
-    } else if (r < rows) {
+    } else if (there) {
         j.place[r] = -1;
     }
 }
 
-// Rows of a chunk per expert.
-__device__ __forceinline__ void count_chunk(const RouteJob &j, int chunk, int32_t *counts)
+// Chooses for a chunk's tokens and counts their rows per expert.
+template <typename T, int PER>
+__device__ __forceinline__ void choose_rows(const RouteJob &j, int token0, int tokens, double *keys,
+                                            int32_t *counts)
 {
-    for (int i = (int)threadIdx.x; i < j.experts; i += kChunk) counts[i] = 0;
-    __syncthreads();
-    const int r = chunk * kChunk + (int)threadIdx.x;
-    const int e = r < j.tokens * j.k ? j.index[r] : -1;
+    const int tid = (int)threadIdx.x, wave = tid >> 6;
+    for (int i = tid; i < j.experts; i += kThreads) counts[i] = 0;
+    for (int t = wave; t < tokens; t += kThreads / 64)
+        choose<T, PER>(j, token0 + t, keys + wave * j.experts);
+    __syncthreads();   // (drains the stores, which this workgroup reads back)
+    const int e = tid < tokens * j.k ? j.index[(int64_t)token0 * j.k + tid] : -1;
     if (e >= 0) atomicAdd(&counts[e], 1);   // (whole numbers: in any order the same)
     __syncthreads();
 }
 
-// counts[experts] -> where each begins, and offsets[experts] last; 1024 threads.
+// Where the rows of this thread's expert begin, from the number of each; 1024 threads.
 __device__ __forceinline__ int scan_experts(int count, int32_t *lds)
 {
     const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
@@ -254,61 +412,70 @@ __device__ __forceinline__ int scan_experts(int count, int32_t *lds)
 }
 
 template <typename T, int PER>
-__global__ __launch_bounds__(256) void route_choose_kernel(RouteJob j)
+__global__ __launch_bounds__(kThreads) void route_choose_kernel(RouteJob j)
 {
-    __shared__ double keys[4][64 * PER];
-    const int64_t token = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (token < j.tokens) choose<T, PER>(j, token, keys[threadIdx.x >> 6]);
-}
-
-__global__ __launch_bounds__(kChunk) void route_count_kernel(RouteJob j)
-{
+    extern __shared__ __attribute__((aligned(256))) char dyn_lds[];
     __shared__ int32_t counts[kMostExperts];
-    count_chunk(j, (int)blockIdx.x, counts);
-    for (int i = (int)threadIdx.x; i < j.experts; i += kChunk)
-        j.counts[(int64_t)blockIdx.x * j.experts + i] = counts[i];
+    const int token0 = (int)blockIdx.x * j.chunkTokens, tokens = min(j.tokens - token0, j.chunkTokens);
+    choose_rows<T, PER>(j, token0, tokens, reinterpret_cast<double *>(dyn_lds), counts);
+    for (int i = (int)threadIdx.x; i < j.experts; i += kThreads)
+        j.counts[(int64_t)i * j.chunks + blockIdx.x] = counts[i];
 }
 
-// Counts of the chunks -> where each chunk's rows of each expert begin.
-__global__ __launch_bounds__(kChunk) void route_scan_kernel(RouteJob j)
+// A wavefront for an expert: its rows before each chunk, and in all.
+__global__ __launch_bounds__(256) void route_scan_kernel(RouteJob j)
 {
-    __shared__ int32_t lds[16];
-    const int e = (int)threadIdx.x;
-    int total = 0;
-    if (e < j.experts)
-        for (int c = 0; c < j.chunks; ++c) total += j.counts[(int64_t)c * j.experts + e];
-    int at = scan_experts(total, lds);
+    const int lane = (int)threadIdx.x & 63, e = (int)blockIdx.x * 4 + ((int)threadIdx.x >> 6);
     if (e >= j.experts) return;
-    j.offsets[e] = at;
-    if (e == j.experts - 1) j.offsets[j.experts] = at + total;
-    for (int c = 0; c < j.chunks; ++c) {
-        const int n = j.counts[(int64_t)c * j.experts + e];
-        j.counts[(int64_t)c * j.experts + e] = at;
-        at += n;
+    int32_t *counts = j.counts + (int64_t)e * j.chunks;
+    int before = 0;
+    for (int c0 = 0; c0 < j.chunks; c0 += 64) {
+        const int n = c0 + lane < j.chunks ? counts[c0 + lane] : 0;
+        int v = n;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int o = __shfl_up(v, d);
+            if (lane >= d) v += o;
+        }
+        if (c0 + lane < j.chunks) counts[c0 + lane] = before + v - n;
+        before += __shfl(v, 63);
     }
+    if (lane == 0) j.counts[(int64_t)j.experts * j.chunks + e] = before;
 }
 
-__global__ __launch_bounds__(kChunk) void route_place_kernel(RouteJob j)
+__global__ __launch_bounds__(kThreads) void route_place_kernel(RouteJob j)
 {
     extern __shared__ int32_t waves[];
-    place_chunk(j, (int)blockIdx.x, waves, j.counts + (int64_t)blockIdx.x * j.experts);
-    const int r = (int)blockIdx.x * kChunk + (int)threadIdx.x;
-    if (r < j.tokens * j.k && r >= j.offsets[j.experts]) j.order[r] = -1;
+    __shared__ int32_t base[kMostExperts];
+    __shared__ int32_t lds[16];
+    __shared__ int live;
+    const int e = (int)threadIdx.x;
+    const int n = e < j.experts ? j.counts[(int64_t)j.experts * j.chunks + e] : 0;
+    const int at = scan_experts(n, lds);
+    if (e < j.experts) {
+        base[e] = at + j.counts[(int64_t)e * j.chunks + blockIdx.x];
+        if (blockIdx.x == 0) j.offsets[e] = at;
+    }
+    if (e == j.experts - 1) {
+        live = at + n;
+        if (blockIdx.x == 0) j.offsets[j.experts] = at + n;
+    }
+    __syncthreads();
+    const int token0 = (int)blockIdx.x * j.chunkTokens, tokens = min(j.tokens - token0, j.chunkTokens);
+    place_rows(j, token0 * j.k, tokens * j.k, waves, base);
+    const int r = token0 * j.k + (int)threadIdx.x;
+    if ((int)threadIdx.x < tokens * j.k && r >= live) j.order[r] = -1;
 }
 
-// Everything, for up to 1024 rows.
+// Everything, for up to 512 rows.
 template <typename T, int PER>
-__global__ __launch_bounds__(kChunk) void route_small_kernel(RouteJob j)
+__global__ __launch_bounds__(kThreads) void route_small_kernel(RouteJob j)
 {
     extern __shared__ __attribute__((aligned(256))) char dyn_lds[];
     __shared__ int32_t counts[kMostExperts];
     __shared__ int32_t lds[16];
-    __shared__ int total;
-    const int wave = (int)threadIdx.x >> 6;
-    double *keys = reinterpret_cast<double *>(dyn_lds) + wave * j.experts;
-    for (int t = wave; t < j.tokens; t += 16) choose<T, PER>(j, t, keys);
-    __syncthreads();   // (drains the stores, which this workgroup reads back)
-    count_chunk(j, 0, counts);
+    __shared__ int live;
+    choose_rows<T, PER>(j, 0, j.tokens, reinterpret_cast<double *>(dyn_lds), counts);
     const int e = (int)threadIdx.x;
     const int n = e < j.experts ? counts[e] : 0;
     const int at = scan_experts(n, lds);
@@ -318,12 +485,12 @@ __global__ __launch_bounds__(kChunk) void route_small_kernel(RouteJob j)
     }
     if (e == j.experts - 1) {
         j.offsets[j.experts] = at + n;
-        total = at + n;
+        live = at + n;
     }
     __syncthreads();
-    place_chunk(j, 0, reinterpret_cast<int32_t *>(dyn_lds), counts);
+    place_rows(j, 0, j.tokens * j.k, reinterpret_cast<int32_t *>(dyn_lds), counts);
     const int r = (int)threadIdx.x;
-    if (r < j.tokens * j.k && r >= total) j.order[r] = -1;
+    if (r < j.tokens * j.k && r >= live) j.order[r] = -1;
 }
 
 // ----------------------------------------------------------------- gradient ---
@@ -338,10 +505,12 @@ struct RouteGradJob {
     const float *dweights;
 };
 
-// With c the chosen scores and w = scale c / sum c (or scale c), g = scale dweights:
-//     renormalised  dc = (g - sum(g c) / sum c) / sum c
+// With c the chosen scores, w = scale c / sum c (or scale c) and g = scale dweights:
+//     renormalised  dc = (g - sum(g c) / sum c) / sum c, otherwise g
 //     softmax       dx = s (ds - sum(ds s)),  sigmoid  dx = ds s (1 - s)
-// where ds is dc at the chosen experts and 0 elsewhere.
+// where ds is dc at the chosen experts and 0 elsewhere.  The sum over ds s is zero
+// where the weights are renormalised: only a softmax that is not has a gradient
+// outside the chosen, and needs their scores.
 template <typename T, int PER>
 __global__ __launch_bounds__(256) void route_grad_kernel(RouteGradJob j)
 {
@@ -351,66 +520,52 @@ __global__ __launch_bounds__(256) void route_grad_kernel(RouteGradJob j)
     if (token >= j.tokens) return;
     float *ds = spread[threadIdx.x >> 6];
     const T *row = reinterpret_cast<const T *>(j.logits) + token * j.ld;
-    float x[PER], most = -__builtin_huge_valf();
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        const int e = i * 64 + lane;
-        x[i] = e < j.experts ? to_float(row[e]) : -__builtin_huge_valf();
-        most = fmaxf(most, x[i]);
-        if (e < j.experts) ds[e] = 0.0f;
-    }
-    most = wave_max(most);
-    double s[PER], total = 0.0;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        if (j.scoring == GETT_SCORE_SOFTMAX) {
-            s[i] = x[i] == -__builtin_huge_valf() ? 0.0 : exp((double)x[i] - (double)most);
-            total += s[i];
-        } else {
-            s[i] = 1.0 / (1.0 + exp(-(double)x[i]));
-        }
-    }
-    if (j.scoring == GETT_SCORE_SOFTMAX) {
-        total = wave_sum(total);
-#pragma unroll
-        for (int i = 0; i < PER; ++i) s[i] = total > 0.0 || total != total ? s[i] / total : 0.0;
-    }
-    // lane r: the r-th choice and its score
+    const bool soft = j.scoring == GETT_SCORE_SOFTMAX, dense = soft && !j.renormalize;
+    // lane r: the r-th choice, its logit and its gradient
     int at = lane < j.k ? j.index[token * j.k + lane] : -1;
     if (at >= j.experts) at = -1;
-    double c = 0.0;
-    for (int r = 0; r < j.k; ++r) {
-        const int e = __shfl(at, r);
-        double v = 0.0;
-#pragma unroll
-        for (int i = 0; i < PER; ++i)
-            if (e >= 0 && i == e >> 6) v = s[i];
-        v = __shfl(v, e & 63);
-        if (lane == r && e >= 0) c = v;
-    }
+    const float chosen = at >= 0 ? to_float(row[at]) : -__builtin_huge_valf();
     double g = at >= 0 ? j.scale * (double)j.dweights[token * j.k + lane] : 0.0;
+    double s[PER], total = 1.0, rest = 0.0;
+    float most = soft ? wave_max(chosen) : 0.0f;
+    if (dense) {
+        float x[PER];
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int e = i * 64 + lane;
+            x[i] = e < j.experts ? to_float(row[e]) : -__builtin_huge_valf();
+            most = fmaxf(most, x[i]);
+        }
+        most = wave_max(most);
+        total = 0.0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            s[i] = x[i] == -__builtin_huge_valf() ? 0.0 : exp((double)x[i] - (double)most);
+            total += s[i];
+        }
+        total = wave_sum(total);
+    }
+    double c = 0.0;
+    if (at >= 0) c = soft ? exp((double)chosen - (double)most) / total : 1.0 / (1.0 + exp(-(double)chosen));
+    double mine;
     if (j.renormalize) {
         const double sum = wave_sum(c), dot = wave_sum(g * c);
-        g = at >= 0 && (sum > 0.0 || sum != sum) ? (g - dot / sum) / sum : 0.0;
-    }
-    // sum(ds s), which the renormalised gradient has at zero
-    const double dot = j.scoring == GETT_SCORE_SOFTMAX ? wave_sum(at >= 0 ? g * c : 0.0) : 0.0;
-    // the chosen experts' own values, in 64 bits until here
-    T *out = reinterpret_cast<T *>(j.dlogits) + token * j.ldd;
-    if (at >= 0)
-        ds[at] = (float)(j.scoring == GETT_SCORE_SOFTMAX ? c * (g - dot) : g * c * (1.0 - c));
-    uint32_t chosen = 0;
-    for (int r = 0; r < j.k; ++r) {
-        const int e = __shfl(at, r);
-        if (e >= 0 && (e & 63) == lane) chosen |= 1u << (e >> 6);
+        mine = sum > 0.0 || sum != sum ? (g - dot / sum) / sum * c : 0.0;
+        if (!soft) mine *= 1.0 - c;
+    } else if (soft) {
+        rest = wave_sum(g * c);
+        mine = c * (g - rest);
+    } else {
+        mine = g * c * (1.0 - c);
     }
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        const int e = i * 64 + lane;
-        if (e >= j.experts) continue;
-        const float rest = j.scoring == GETT_SCORE_SOFTMAX ? (float)(-s[i] * dot) : 0.0f;
-        out[e] = from_float<T>(chosen >> i & 1 ? ds[e] : rest);
-    }
+    for (int i = 0; i < PER; ++i)
+        if (i * 64 + lane < j.experts) ds[i * 64 + lane] = dense ? (float)(-s[i] / total * rest) : 0.0f;
+    if (at >= 0) ds[at] = (float)mine;
+    T *out = reinterpret_cast<T *>(j.dlogits) + token * j.ldd;
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+        if (i * 64 + lane < j.experts) out[i * 64 + lane] = from_float<T>(ds[i * 64 + lane]);
 }
 
 // f(an integral constant of the experts a lane holds)
@@ -429,7 +584,7 @@ gett_status_t route_ok(gett_dtype_t dtype, int64_t tokens, int experts, int k, i
         (scoring != GETT_SCORE_SOFTMAX && scoring != GETT_SCORE_SIGMOID))
         return GETT_ERROR_INVALID_VALUE;
     if (experts > kMostExperts || k > kMostChoices || tokens >= kLayerRows ||
-        tokens * k >= INT32_MAX - kChunk)
+        tokens * k >= INT32_MAX - 2 * kChunk)
         return GETT_ERROR_NOT_SUPPORTED;
     return GETT_SUCCESS;
 }
@@ -466,38 +621,38 @@ gett_status_t gett_route(gett_dtype_t dtype, int64_t tokens, int experts, int k,
             if (!apart(out[i], out[j])) return GETT_ERROR_INVALID_VALUE;
     }
     hipStream_t s = static_cast<hipStream_t>(stream);
-    const int64_t chunks = (rows + kChunk - 1) / kChunk;
+    const int64_t chunkTokens = kChunk / k, chunks = (tokens + chunkTokens - 1) / chunkTokens;
     RouteJob j = {logits, stride, bias, (int)tokens, experts, k, scoring, groups, top_groups, renormalize,
-                  scale, weights, index, order, offsets, place, nullptr, (int)chunks};
-    // 16 counts, or doubles, an expert
-    const size_t countBytes = 16 * (size_t)experts * 4, keyBytes = 16 * (size_t)experts * 8;
-    if (chunks <= 1)
-        return with_experts(experts, [&](auto per) {
-            return with_type(dtype, [&](auto v) {
-                constexpr auto kernel = route_small_kernel<decltype(v), decltype(per)::value>;
-                if (allow_dynamic_lds<kernel>(16 * 64 * decltype(per)::value * 8) != hipSuccess)
-                    return GETT_ERROR_HIP;
-                hipLaunchKernelGGL(kernel, dim3(1), dim3(kChunk), keyBytes, s, j);
-                return launched(hipGetLastError());
-            });
-        });
-    if (!fits_launch(chunks, kChunk)) return GETT_ERROR_NOT_SUPPORTED;
+                  scale, weights, index, order, offsets, place, nullptr, (int)chunks, (int)chunkTokens};
+    // a double an expert for each wavefront, and counts
+    const size_t lds = kThreads / 64 * (size_t)experts * 8, countBytes = kChunk / 64 * (size_t)experts * 4;
+    const bool small = chunks <= 1;
     Partials hold;
-    st = stream_workspace(s, 0, (uint64_t)chunks * experts * 4, hold);
-    if (st != GETT_SUCCESS) return st;
-    j.counts = static_cast<int32_t *>(hold.tiles);
+    if (!small) {
+        if (!fits_launch(chunks, kThreads)) return GETT_ERROR_NOT_SUPPORTED;
+        st = stream_workspace(s, 0, ((uint64_t)chunks + 1) * experts * 4, hold);
+        if (st != GETT_SUCCESS) return st;
+        j.counts = static_cast<int32_t *>(hold.tiles);
+    }
     st = with_experts(experts, [&](auto per) {
         return with_type(dtype, [&](auto v) {
-            hipLaunchKernelGGL((route_choose_kernel<decltype(v), decltype(per)::value>),
-                               dim3((unsigned)((tokens + 3) / 4)), dim3(256), 0, s, j);
+            constexpr int PER = decltype(per)::value;
+            constexpr size_t most = kThreads / 64 * 64 * PER * 8;
+            if (small) {
+                constexpr auto kernel = route_small_kernel<decltype(v), PER>;
+                if (allow_dynamic_lds<kernel>(most) != hipSuccess) return GETT_ERROR_HIP;
+                hipLaunchKernelGGL(kernel, dim3(1), dim3(kThreads), lds, s, j);
+            } else {
+                constexpr auto kernel = route_choose_kernel<decltype(v), PER>;
+                if (allow_dynamic_lds<kernel>(most) != hipSuccess) return GETT_ERROR_HIP;
+                hipLaunchKernelGGL(kernel, dim3((unsigned)chunks), dim3(kThreads), lds, s, j);
+            }
             return launched(hipGetLastError());
         });
     });
-    if (st != GETT_SUCCESS) return st;
-    hipLaunchKernelGGL(route_count_kernel, dim3((unsigned)chunks), dim3(kChunk), 0, s, j);
-    hipLaunchKernelGGL(route_scan_kernel, dim3(1), dim3(kChunk), 0, s, j);
-    if (allow_dynamic_lds<route_place_kernel>(16 * kMostExperts * 4) != hipSuccess) return GETT_ERROR_HIP;
-    hipLaunchKernelGGL(route_place_kernel, dim3((unsigned)chunks), dim3(kChunk), countBytes, s, j);
+    if (st != GETT_SUCCESS || small) return st;
+    hipLaunchKernelGGL(route_scan_kernel, dim3((unsigned)((experts + 3) / 4)), dim3(256), 0, s, j);
+    hipLaunchKernelGGL(route_place_kernel, dim3((unsigned)chunks), dim3(kThreads), countBytes, s, j);
     return launched(hipGetLastError());
 }
 
