@@ -54,18 +54,63 @@ __device__ __forceinline__ void philox(uint32_t c0, uint32_t c1, uint64_t offset
     out[3] = c3;
 }
 
+// philox for one c0 and many c1: what of the first three rounds does not depend on c1
+// (four of twenty products) is kept.
+struct PhiloxColumn {
+    uint32_t a, b, c, d, e;
+    uint32_t k0, k1;
+};
+__device__ __forceinline__ PhiloxColumn philox_column(uint32_t c0, uint64_t offset, uint64_t key)
+{
+    constexpr uint32_t W0 = 0x9E3779B9u, W1 = 0xBB67AE85u;
+    constexpr uint64_t M0 = 0xD2511F53u, M1 = 0xCD9E8D57u;
+    const uint32_t k0 = (uint32_t)key, k1 = (uint32_t)(key >> 32);
+    const uint64_t p1 = M0 * c0, q1 = M1 * (uint32_t)offset;
+    const uint32_t c2 = (uint32_t)(p1 >> 32) ^ (uint32_t)(offset >> 32) ^ k1;
+    const uint64_t q2 = M1 * c2;
+    const uint64_t p3 = M0 * ((uint32_t)(q2 >> 32) ^ (uint32_t)q1 ^ (k0 + W0));
+    return {(uint32_t)(q1 >> 32) ^ k0, (uint32_t)p1 ^ (k1 + W1), (uint32_t)q2 ^ (k0 + 2 * W0),
+            (uint32_t)(p3 >> 32) ^ (k1 + 2 * W1), (uint32_t)p3, k0 + 3 * W0, k1 + 3 * W1};
+}
+__device__ __forceinline__ void philox_row(const PhiloxColumn &s, uint32_t c1, uint32_t out[4])
+{
+    constexpr uint64_t M0 = 0xD2511F53u, M1 = 0xCD9E8D57u;
+    const uint64_t p2 = M0 * (c1 ^ s.a);
+    const uint64_t q3 = M1 * ((uint32_t)(p2 >> 32) ^ s.b);
+    uint32_t c0 = (uint32_t)(q3 >> 32) ^ s.c, c2 = s.d ^ (uint32_t)p2;
+    uint32_t c1_ = (uint32_t)q3, c3 = s.e, k0 = s.k0, k1 = s.k1;
+#pragma unroll
+    for (int i = 3; i < 10; ++i) {
+        const uint64_t p = M0 * c0, q = M1 * c2;
+        c0 = (uint32_t)(q >> 32) ^ c1_ ^ k0;
+        c2 = (uint32_t)(p >> 32) ^ c3 ^ k1;
+        c1_ = (uint32_t)q;
+        c3 = (uint32_t)p;
+        k0 += 0x9E3779B9u;
+        k1 += 0xBB67AE85u;
+    }
+    out[0] = c0;
+    out[1] = c1_;
+    out[2] = c2;
+    out[3] = c3;
+}
+
 // Eight neighbours of one row, from a column that is a multiple of 8.  A block
 // of random bits serves the eight of them (16 bits each: with 32 the generator, and
 // not memory, would be what bounds a 16-bit dropout).
-__device__ __forceinline__ void drop8(float v[8], const Drop &d, uint64_t key, uint32_t row, uint32_t col)
+__device__ __forceinline__ void drop8(float v[8], const Drop &d, const uint32_t w[4])
 {
-    uint32_t w[4];
-    philox(col >> 3, row, d.offset, key, w);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         v[2 * i] = (w[i] & 0xffff) >= d.cut ? v[2 * i] * d.scale : 0.0f;
         v[2 * i + 1] = (w[i] >> 16) >= d.cut ? v[2 * i + 1] * d.scale : 0.0f;
     }
+}
+__device__ __forceinline__ void drop8(float v[8], const Drop &d, uint64_t key, uint32_t row, uint32_t col)
+{
+    uint32_t w[4];
+    philox(col >> 3, row, d.offset, key, w);
+    drop8(v, d, w);
 }
 
 // -------------------------------------------------------------- activations ---
@@ -125,6 +170,18 @@ template <typename T> __device__ __forceinline__ void load8(const T *p, int left
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = i < left ? to_float(p[i]) : 0.0f;
     }
+}
+// the same as they lie in memory
+template <typename T> __device__ __forceinline__ Run<T, 8> raw8(const T *p, int left)
+{
+    Run<T, 8> r;
+    if (left >= 8) {
+        r = *reinterpret_cast<const Run<T, 8> *>(p);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) r.v[i] = i < left ? p[i] : from_float<T>(0.0f);
+    }
+    return r;
 }
 template <typename T> __device__ __forceinline__ void store8(T *p, int left, const float v[8])
 {

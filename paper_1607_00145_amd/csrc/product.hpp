@@ -380,31 +380,42 @@ template <typename T, bool MCOL, bool NCOL, typename S> struct Product {
 
 // ------------------------------------------------------------------- kernel ---
 
+// Eight sums of a row -> the result: v += bias; Z; activation; dropout (its bits in w);
+// v += residual; Y.
 template <typename T>
-__device__ __forceinline__ void product_store(const Epilogue &o, uint64_t key, int64_t row, int col,
-                                              int left, float v[8])
+__device__ __forceinline__ void product_finish(const Epilogue &o, int64_t row, int col, int left, float v[8],
+                                               const Run<T, 8> &bias, const Run<T, 8> &residual,
+                                               const uint32_t w[4])
 {
-    if (left <= 0) return;
     if (o.bias) {
-        float x[8];
-        load8(reinterpret_cast<const T *>(o.bias) + col, left, x);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] += x[i];
+        for (int i = 0; i < 8; ++i) v[i] += to_float(bias.v[i]);
     }
     if (o.Z) store8(reinterpret_cast<T *>(o.Z) + row * o.ldz + col, left, v);
     if (o.activation != GETT_ACTIVATION_NONE) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = activate(o.activation, v[i]);
     }
-    if (o.drop.cut) drop8(v, o.drop, key, (uint32_t)row, (uint32_t)col);
+    if (o.drop.cut) drop8(v, o.drop, w);
     if (o.residual) {
-        float x[8];
-        load8(reinterpret_cast<const T *>(o.residual) + row * o.ldr + col, left, x);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] += x[i];
+        for (int i = 0; i < 8; ++i) v[i] += to_float(residual.v[i]);
     }
     if (o.wide) store8(reinterpret_cast<float *>(o.Y) + row * o.ldy + col, left, v);
     else store8(reinterpret_cast<T *>(o.Y) + row * o.ldy + col, left, v);
+}
+// The same where rows come one by one.
+template <typename T>
+__device__ __forceinline__ void product_store(const Epilogue &o, uint64_t key, int64_t row, int col,
+                                              int left, float v[8])
+{
+    if (left <= 0) return;
+    Run<T, 8> bias = {}, residual = {};
+    uint32_t w[4] = {};
+    if (o.bias) bias = raw8(reinterpret_cast<const T *>(o.bias) + col, left);
+    if (o.residual) residual = raw8(reinterpret_cast<const T *>(o.residual) + row * o.ldr + col, left);
+    if (o.drop.cut) philox((uint32_t)col >> 3, (uint32_t)row, o.drop.offset, key, w);
+    product_finish<T>(o, row, col, left, v, bias, residual, w);
 }
 
 // offsets[e], brought into [0, rows]
@@ -622,6 +633,12 @@ __global__ __launch_bounds__(S::THREADS) void product_kernel(ProductArgs g, int 
             continue;
         }
         Epilogue o = g.out;
+        if constexpr (FORM != kRowsRows) {   // gradients are the sums themselves
+            o.bias = o.residual = nullptr;
+            o.Z = nullptr;
+            o.activation = GETT_ACTIVATION_NONE;
+            o.drop.cut = 0;
+        }
         if (groups == kByRows && o.bias) o.bias += (int64_t)now.e * g.n * sizeof(T);
         if (groups == kByK) o.Y += (int64_t)now.e * g.stepN * (o.wide ? 4 : sizeof(T));
         if (now.empty) {
@@ -631,13 +648,30 @@ __global__ __launch_bounds__(S::THREADS) void product_kernel(ProductArgs g, int 
         after = now.row0 + S::BM <= now.rows && now.col0 + S::BN <= g.n;
         // The results go through LDS, 16 rows of a wavefront at a time, so that one
         // loop (and not one copy of the epilogue for each register) takes them, whole
-        // lines of C each time.  Piece x of row r lies at x ^ r % 16.
+        // lines of C each time.  Piece x of row r lies at x ^ r.  A step's rows of
+        // the residual are on their way a step before (with each waiting for its own,
+        // 8192 x 8192 x 4096 with all of the epilogue takes 625 us, without it 450).
         constexpr int W = S::W, PER = W / 8, ROWS = 64 / PER;   // runs of a row, rows a pass
+        constexpr int PASSES = 16 / ROWS, STEPS = 2 * S::FM;
         constexpr int SWAP = W / 4 < 16 ? W / 4 - 1 : 15;
         const int run = lane % PER, rowIn = lane / PER;
-        const int c = now.col0 + p.wn * W + 8 * run;
+        const int c = now.col0 + p.wn * W + 8 * run, left = g.n - c;
+        const int row0 = now.row0 + p.wm * 32 * S::FM + rowIn;
+        Run<T, 8> bias = {}, ahead[PASSES] = {};
+        PhiloxColumn column = {};
+        if (o.bias && left > 0) bias = raw8(reinterpret_cast<const T *>(o.bias) + c, left);
+        if (o.drop.cut) column = philox_column((uint32_t)c >> 3, o.drop.offset, key);
+        auto fetch = [&](int step) {
+#pragma unroll
+            for (int y = 0; y < PASSES; ++y) {
+                const int64_t row = row0 + 16 * step + ROWS * y;
+                if (o.residual && left > 0 && row < now.rows)
+                    ahead[y] = raw8(reinterpret_cast<const T *>(o.residual) + row * o.ldr + c, left);
+            }
+        };
+        fetch(0);
 #pragma unroll 1
-        for (int step = 0; step < 2 * S::FM; ++step) {
+        for (int step = 0; step < STEPS; ++step) {
             static_for<S::FM>([&](auto ic) {
                 constexpr int i = decltype(ic)::value;
                 if (step >> 1 != i || p.q >> 4 != (step & 1)) return;
@@ -652,13 +686,28 @@ __global__ __launch_bounds__(S::THREADS) void product_kernel(ProductArgs g, int 
                             f4{v[4 * a], v[4 * a + 1], v[4 * a + 2], v[4 * a + 3]};
                     }
             });
-            const int first = now.row0 + p.wm * 32 * S::FM + 16 * step;
+            Run<T, 8> residual[PASSES];
+            float v[PASSES][8];
 #pragma unroll
-            for (int r = rowIn; r < rowIn + 16; r += ROWS) {
+            for (int y = 0; y < PASSES; ++y) {
+                const int r = rowIn + ROWS * y;
                 const f4 lo = *reinterpret_cast<const f4 *>(mine + r * W * 4 + ((2 * run) ^ (r & SWAP)) * 16);
                 const f4 hi = *reinterpret_cast<const f4 *>(mine + r * W * 4 + ((2 * run + 1) ^ (r & SWAP)) * 16);
-                float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-                if (first + r < now.rows) product_store<T>(o, key, first + r, c, g.n - c, v);
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    v[y][x] = lo[x];
+                    v[y][4 + x] = hi[x];
+                }
+                residual[y] = ahead[y];
+            }
+            if (step + 1 < STEPS) fetch(step + 1);
+#pragma unroll
+            for (int y = 0; y < PASSES; ++y) {
+                const int row = row0 + 16 * step + ROWS * y;
+                if (row >= now.rows || left <= 0) continue;
+                uint32_t w[4] = {};
+                if (o.drop.cut) philox_row(column, (uint32_t)row, w);
+                product_finish<T>(o, row, c, left, v[y], bias, residual[y], w);
             }
         }
         if (!there) return;
