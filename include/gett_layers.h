@@ -31,7 +31,7 @@
  * Errors of every call: GETT_ERROR_INVALID_VALUE (unknown dtype, activation or
  * scoring, a negative extent, a stride smaller than the columns, a null or
  * misaligned pointer, an overlap, a probability outside [0, 1]),
- * GETT_ERROR_NOT_SUPPORTED (rows of 2^31 and more, columns of 2^21 and more, a
+ * GETT_ERROR_NOT_SUPPORTED (rows of 2^30 and more, columns of 2^21 and more, a
  * launch or an operand too large), GETT_ERROR_HIP, GETT_ERROR_ALLOC.  Extents of
  * zero enqueue what remains to be written; pointers of empty tensors are not
  * looked at.
@@ -136,7 +136,7 @@ gett_status_t gett_linear_grad(gett_dtype_t dtype, int64_t m, int64_t n, int64_t
  *   place    tokens x k int32: where `order` has the row (-1: nowhere).
  *
  * GETT_ERROR_NOT_SUPPORTED for more than 1024 experts, k > 32, or tokens * k of
- * 2^31 and more; GETT_ERROR_INVALID_VALUE where groups do not divide the experts or
+ * 2^30 and more (of the other calls with tokens, too); GETT_ERROR_INVALID_VALUE where groups do not divide the experts or
  * top_groups of them hold fewer than k.
  */
 #define GETT_SCORE_SOFTMAX 0

@@ -18,8 +18,7 @@ struct ExpertSizes {
 gett_status_t sizes_ok(gett_dtype_t dtype, int64_t tokens, int k, int experts)
 {
     if (!float_type(dtype) || tokens < 0 || k < 1 || experts < 1) return GETT_ERROR_INVALID_VALUE;
-    if (tokens >= kLayerRows || experts > kMostExperts || k > kMostChoices ||
-        tokens * k >= INT32_MAX)
+    if (tokens >= kLayerRows || experts > kMostExperts || k > kMostChoices || tokens * k >= kLayerRows)
         return GETT_ERROR_NOT_SUPPORTED;
     return GETT_SUCCESS;
 }

@@ -199,7 +199,7 @@ template <typename T> __device__ __forceinline__ void store8(T *p, int left, con
 
 // ------------------------------------------------------------- host checks ---
 
-constexpr int64_t kLayerRows = (int64_t)1 << 31;   // rows of a matrix, exclusive
+constexpr int64_t kLayerRows = (int64_t)1 << 30;   // rows of a matrix, exclusive
 constexpr int64_t kLayerCols = (int64_t)1 << 21;   // columns, exclusive
 constexpr int kMostExperts = 1024, kMostChoices = 32;
 

@@ -167,31 +167,37 @@ template <typename T, bool MCOL, bool NCOL, typename S> struct Product {
     // acc[i][f][4 a + y] is that of row 32 i + q and column 32 f + 8 a + 4 h + y of the
     // wavefront's part.
 
-    // Where a lane's 16 bytes of load j lie: k or piece that decides whether they
-    // are within K (`at`), and the offset from the panel's first byte.
+    // A lane's 16 bytes of load j: the number along K that decides whether they are
+    // within it is `first` and j times `step` ...
+    template <bool COL, int B> struct Along {
+        static constexpr int PR = B / EP;          // pieces of one k of columns
+        static constexpr int step = COL ? S::NW * 64 / PR : 0;
+        static_assert(COL ? S::NW * 64 % PR == 0 : S::NW % 2 == 0, "the same for every load");
+        static __device__ __forceinline__ int first(int wave, int lane)
+        {
+            return COL ? (wave * 64 + lane) / PR : ((lane & 7) ^ ((wave * 8 + (lane >> 3)) >> 1 & 7)) * EP;
+        }
+    };
+    // ... and this their offset from the panel's first byte.
     template <bool COL, int B, typename Row>
-    __device__ __forceinline__ static void place(const Side &x, int j, int wave, int lane, Row rowOffset,
-                                                 uint32_t &off, int &at)
+    __device__ __forceinline__ static uint32_t place(const Side &x, int j, int wave, int lane, Row rowOffset)
     {
         const int L = (j * S::NW + wave) * 64 + lane;
         if constexpr (COL) {
-            constexpr int PR = B / EP;             // pieces of one k
+            constexpr int PR = B / EP;
             const int k = L / PR, pl = L % PR;
             const int piece = sizeof(T) == 2 ? pl ^ (4 * (k & 3) & (PR - 1)) : pl;
-            at = k;
-            off = piece * EP < x.count ? (uint32_t)(k * x.ld) + piece * 16 : kNowhere;
+            return piece * EP < x.count ? (uint32_t)(k * x.ld) + piece * 16 : kNowhere;
         } else {
-            const int r = L >> 3, pl = L & 7;
-            const int piece = pl ^ ((r >> 1) & 7);
-            at = piece * EP;
-            off = r < x.count ? rowOffset(r) + piece * 16 : kNowhere;
+            const int r = L >> 3, piece = (L & 7) ^ ((r >> 1) & 7);
+            return r < x.count ? rowOffset(r) + piece * 16 : kNowhere;
         }
     }
 
     // Loads on their way to LDS: what a lane fetches of each panel, and the next
     // panel.  In the order of issue a stage's J loads follow one another.
     uint32_t off[S::J];
-    int at[S::J];
+    int alongM, alongN;
     const char *pm, *pn;
     int64_t stepM, stepN;
     int leftM, leftN, panels;
@@ -208,7 +214,9 @@ template <typename T, bool MCOL, bool NCOL, typename S> struct Product {
     __device__ __forceinline__ void issue_one(int j)
     {
         const bool isM = j < S::JA;
-        const uint32_t o = at[j] < (isM ? leftM : leftN) ? off[j] : kNowhere;
+        const int at = isM ? alongM + j * Along<MCOL, S::BM>::step
+                           : alongN + (j - S::JA) * Along<NCOL, S::BN>::step;
+        const uint32_t o = at < (isM ? leftM : leftN) ? off[j] : kNowhere;
         load_to_lds(isM ? rm : rn, o,
                     to + (isM ? 0 : S::BM * 128) + (isM ? j : j - S::JA) * S::NW * 1024);
     }
@@ -227,12 +235,12 @@ template <typename T, bool MCOL, bool NCOL, typename S> struct Product {
         const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
 #pragma unroll
         for (int j = 0; j < S::J; ++j) {
-            if (j < S::JA)
-                place<MCOL, S::BM>(M, j, wave, lane, rowM, off[j], at[j]);
-            else
-                place<NCOL, S::BN>(N, j - S::JA, wave, lane,
-                                         [&](int r) { return (uint32_t)(r * N.ld); }, off[j], at[j]);
+            off[j] = j < S::JA ? place<MCOL, S::BM>(M, j, wave, lane, rowM)
+                               : place<NCOL, S::BN>(N, j - S::JA, wave, lane,
+                                                    [&](int r) { return (uint32_t)(r * N.ld); });
         }
+        alongM = Along<MCOL, S::BM>::first(wave, lane);
+        alongN = Along<NCOL, S::BN>::first(wave, lane);
         stepM = MCOL ? KP * M.ld : 128;
         stepN = NCOL ? KP * N.ld : 128;
         pm = M.p;
@@ -289,7 +297,11 @@ template <typename T, bool MCOL, bool NCOL, typename S> struct Product {
         auto join = [](s4 a, s4 b) {
             return __builtin_bit_cast(i4, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
         };
-        i4 a[2][FM], b[2][FN];
+        // Slabs read together.  One block of 32 x 32 a wavefront has too few MFMAs in a
+        // slab to cover the reads of the next: it reads whole panels where it is alone on
+        // its CU.
+        constexpr int G = FM * FN == 1 && NS == 8 ? 4 : 1, STEPS = 4 / G;
+        i4 a[2][G][FM], b[2][G][FN];
         auto fragment = [&](auto column, auto size, int own, int s, int i) {
             constexpr int B = decltype(size)::value;
             if constexpr (!decltype(column)::value) {
@@ -306,17 +318,18 @@ template <typename T, bool MCOL, bool NCOL, typename S> struct Product {
                 return v;
             }
         };
-        auto read_m = [&](int set, int s, int i) {
-            a[set][i] = fragment(std::bool_constant<MCOL>{}, std::integral_constant<int, S::BM>{}, atM, s, i);
+        auto read_m = [&](int set, int g, int s, int i) {
+            a[set][g][i] = fragment(std::bool_constant<MCOL>{}, std::integral_constant<int, S::BM>{}, atM, s + g, i);
         };
-        auto read_n = [&](int set, int s, int f) {
-            b[set][f] = fragment(std::bool_constant<NCOL>{}, std::integral_constant<int, S::BN>{}, atN, s, f);
+        auto read_n = [&](int set, int g, int s, int f) {
+            b[set][g][f] = fragment(std::bool_constant<NCOL>{}, std::integral_constant<int, S::BN>{}, atN, s + g, f);
         };
-        // the x-th fragment of a slab, in the order that the MFMAs want them
+        // the x-th fragment of a group of slabs, in the order that the MFMAs want them
         auto read_one = [&](int set, int s, int x) {
-            if (x == 0) read_m(set, s, 0);
-            else if (x <= FN) read_n(set, s, x - 1);
-            else read_m(set, s, x - FN);
+            const int g = x / (FM + FN), y = x - g * (FM + FN);
+            if (y == 0) read_m(set, g, s, 0);
+            else if (y <= FN) read_n(set, g, s, y - 1);
+            else read_m(set, g, s, y - FN);
         };
         // no fence: a release would wait for the loads in flight as well
         auto barrier = []() { asm volatile("s_barrier" ::: "memory"); };
@@ -332,7 +345,7 @@ template <typename T, bool MCOL, bool NCOL, typename S> struct Product {
         else __builtin_amdgcn_s_waitcnt(kFirst);
         barrier();
         at_stage(0);
-        constexpr int READS = FM + FN, MFMAS = FM * FN;
+        constexpr int READS = G * (FM + FN), MFMAS = G * FM * FN;
 #pragma unroll
         for (int x = 0; x < READS; ++x) read_one(0, 0, x);
         int stage = 0;
@@ -341,10 +354,10 @@ template <typename T, bool MCOL, bool NCOL, typename S> struct Product {
         // written out: between two MFMAs a fragment of the next slab is read, and in
         // the last slab the loads go out as well, so that the matrix unit waits for
         // neither to be issued.
-        auto panel = [&](auto more, auto load) {
-            static_for<4>([&](auto step) {
-                constexpr int s = decltype(step)::value, set = s & 1;
-                constexpr bool last = s == 3, reads = !last || more, loads = last && load;
+        auto panel = [&](auto more, auto load, auto set0) {
+            static_for<STEPS>([&](auto step) {
+                constexpr int s = decltype(step)::value, set = (decltype(set0)::value + s) & 1;
+                constexpr bool last = s == STEPS - 1, reads = !last || more, loads = last && load;
                 if constexpr (last && more) {
                     __builtin_amdgcn_s_waitcnt(load ? kNext : kAll);   // the next is there
                     barrier();
@@ -353,16 +366,17 @@ template <typename T, bool MCOL, bool NCOL, typename S> struct Product {
                     at_stage(stage);
                 }
                 static_for<MFMAS>([&](auto xc) {
-                    constexpr int x = decltype(xc)::value, i = x / FN, f = x % FN;
+                    constexpr int x = decltype(xc)::value, y = x / (FM * FN);
+                    constexpr int i = x % (FM * FN) / FN, f = x % FN;
                     constexpr int r0 = x * READS / MFMAS, r1 = (x + 1) * READS / MFMAS;
                     constexpr int l0 = x * J / MFMAS, l1 = (x + 1) * J / MFMAS;
                     if constexpr (reads)
-                        static_for<r1 - r0>([&](auto y) {
-                            read_one(set ^ 1, last ? 0 : s + 1, r0 + decltype(y)::value);
+                        static_for<r1 - r0>([&](auto z) {
+                            read_one(set ^ 1, last ? 0 : (s + 1) * G, r0 + decltype(z)::value);
                         });
-                    acc[i][f] = product_mfma<T>(b[set][f], a[set][i], acc[i][f]);
+                    acc[i][f] = product_mfma<T>(b[set][y][f], a[set][y][i], acc[i][f]);
                     if constexpr (loads)
-                        static_for<l1 - l0>([&](auto y) { issue_one(l0 + decltype(y)::value); });
+                        static_for<l1 - l0>([&](auto z) { issue_one(l0 + decltype(z)::value); });
                     __builtin_amdgcn_sched_barrier(0);
                 });
                 if constexpr (loads) issue_end();
@@ -370,11 +384,46 @@ template <typename T, bool MCOL, bool NCOL, typename S> struct Product {
         };
         const std::true_type yes;
         const std::false_type no;
+        const std::integral_constant<int, 0> even;
+        const std::integral_constant<int, 1> odd;
         const int n = panels;
         int t = 0;
-        for (; t + NS < n; ++t) panel(yes, yes);
-        for (; t + 1 < n; ++t) panel(yes, no);
-        panel(no, no);
+        if constexpr (STEPS % 2 == 0) {
+            for (; t + NS < n; ++t) panel(yes, yes, even);
+            for (; t + 1 < n; ++t) panel(yes, no, even);
+            panel(no, no, even);
+        } else {
+            // (the next panel is in the other set)
+            for (; t + NS + 1 < n; t += 2) {
+                panel(yes, yes, even);
+                panel(yes, yes, odd);
+            }
+            if (t + NS < n) {
+                panel(yes, yes, even);
+                ++t;
+                for (; t + 2 < n; t += 2) {
+                    panel(yes, no, odd);
+                    panel(yes, no, even);
+                }
+                if (t + 1 < n) {
+                    panel(yes, no, odd);
+                    panel(no, no, even);
+                } else {
+                    panel(no, no, odd);
+                }
+            } else {
+                for (; t + 2 < n; t += 2) {
+                    panel(yes, no, even);
+                    panel(yes, no, odd);
+                }
+                if (t + 1 < n) {
+                    panel(yes, no, even);
+                    panel(no, no, odd);
+                } else {
+                    panel(no, no, even);
+                }
+            }
+        }
     }
 };
 
@@ -508,7 +557,8 @@ template <typename T, bool MCOL, bool NCOL, typename S>
 __device__ __forceinline__ bool product_join(Product<T, MCOL, NCOL, S> &p, const ProductArgs &g,
                                              const TileAt &t, char *lds)
 {
-    const int tid = (int)threadIdx.x;
+    int tid = (int)threadIdx.x;
+    asm volatile("" : "+v"(tid));   // (addresses made here, and not kept through all tiles)
     constexpr int N = S::THREADS, TILE = S::BM * S::BN;
     float *first = g.slots + (int64_t)t.shared * g.slices * TILE + tid;
     float *own = first + (int64_t)t.slice * TILE;

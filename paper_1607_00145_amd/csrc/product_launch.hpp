@@ -37,6 +37,10 @@ gett_status_t product_tiles(ProductGroups groups, ProductArgs g, const ProductPl
 typedef ProductShape<4, 2, 2, 4, 2> ProductBig;
 typedef ProductShape<2, 2, 2, 2, 2> ProductMid;
 typedef ProductShape<1, 1, 2, 2, 4> ProductSmall;
+// The same, one a CU: of few tiles each is alone on its CU and may have all of the
+// LDS, with more panels on their way.
+typedef ProductShape<2, 2, 2, 2, 4> ProductMidDeep;
+typedef ProductShape<1, 1, 2, 2, 8> ProductSmallDeep;
 
 // Few rows: a workgroup for 32 columns and, of experts, for each row that may be an
 // expert's first.
@@ -67,7 +71,10 @@ gett_status_t product_form(ProductGroups groups, const ProductArgs &g, const Pro
 {
     if constexpr (sizeof(T) == 2)   // (in 32 bits the middle ones are bound by the instructions)
         if (p.shape == 0) return product_tiles<T, FORM, ProductBig>(groups, g, p, s);
+    const bool deep = p.units <= kProductCus;
+    if (p.shape == 1 && deep) return product_tiles<T, FORM, ProductMidDeep>(groups, g, p, s);
     if (p.shape == 1) return product_tiles<T, FORM, ProductMid>(groups, g, p, s);
+    if (deep) return product_tiles<T, FORM, ProductSmallDeep>(groups, g, p, s);
     return product_tiles<T, FORM, ProductSmall>(groups, g, p, s);
 }
 

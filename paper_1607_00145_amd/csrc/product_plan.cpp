@@ -22,13 +22,13 @@ struct ShapeCost {
     int perCu;         // workgroups resident
     double full, alone, tile, join, joinEach;
 };
-constexpr ShapeCost kCost16[3] = {{256, 1, 1.50, 1.50, 12.0, 15.0, 6.0},
-                                  {128, 2, 1.00, 0.60, 5.0, 8.0, 1.5},
-                                  {64, 2, 0.45, 0.30, 3.0, 5.0, 0.3}};
+constexpr ShapeCost kCost16[3] = {{256, 1, 1.50, 1.20, 9.0, 15.0, 6.0},
+                                  {128, 2, 1.00, 0.50, 4.0, 9.0, 2.5},
+                                  {64, 2, 0.42, 0.27, 2.5, 3.5, 0.5}};
 constexpr ShapeCost kCost32[3] = {{256, 1, 1e6, 1e6, 0.0, 0.0, 0.0},
-                                  {128, 2, 3.60, 1.90, 5.0, 8.0, 1.5},
-                                  {64, 2, 1.00, 0.55, 3.0, 5.0, 0.3}};
-constexpr int64_t kCus = 256;
+                                  {128, 2, 3.90, 2.05, 4.0, 9.0, 2.5},
+                                  {64, 2, 1.05, 0.60, 2.5, 3.5, 0.5}};
+constexpr int64_t kCus = kProductCus;
 
 }  // namespace
 

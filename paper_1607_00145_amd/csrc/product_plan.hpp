@@ -10,6 +10,7 @@ enum ProductForm { kRowsRows, kRowsColumns, kColumnsColumns };
 enum ProductGroups { kWhole, kByRows, kByK };
 
 constexpr int kFewRows = 3;   // product_few.hpp
+constexpr int64_t kProductCus = 256;
 
 // Whether rows x N^T is one of few rows: y = x w^T of up to 64 rows, or of so many
 // rows of experts in all.

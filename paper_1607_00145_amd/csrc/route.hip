@@ -583,8 +583,7 @@ gett_status_t route_ok(gett_dtype_t dtype, int64_t tokens, int experts, int k, i
     if (!float_type(dtype) || tokens < 0 || experts < 1 || k < 1 || k > experts ||
         (scoring != GETT_SCORE_SOFTMAX && scoring != GETT_SCORE_SIGMOID))
         return GETT_ERROR_INVALID_VALUE;
-    if (experts > kMostExperts || k > kMostChoices || tokens >= kLayerRows ||
-        tokens * k >= INT32_MAX - 2 * kChunk)
+    if (experts > kMostExperts || k > kMostChoices || tokens >= kLayerRows || tokens * k >= kLayerRows)
         return GETT_ERROR_NOT_SUPPORTED;
     return GETT_SUCCESS;
 }

@@ -472,6 +472,8 @@ def linear(x, w, bias=None, activation=None, residual=None, p: float = 0.0, seed
         residual = _flat("residual", residual)
     drop = _drop(p, seed, offset)
     seed = None if drop is None else drop[3]
+    _m._device("x", x)
+    _m._device("w", w)
     if _records(x, w, bias, residual):
         y = _function("linear").apply(flat, w, bias, residual, seed, code, drop)
     else:
