@@ -25,7 +25,7 @@ struct ShapeCost {
 constexpr ShapeCost kCost16[3] = {{256, 1, 1.50, 1.20, 9.0, 15.0, 6.0},
                                   {128, 2, 1.00, 0.50, 4.0, 9.0, 2.5},
                                   {64, 2, 0.42, 0.27, 2.5, 3.5, 0.5}};
-constexpr ShapeCost kCost32[3] = {{256, 1, 1e6, 1e6, 0.0, 0.0, 0.0},
+constexpr ShapeCost kCost32[3] = {{},   // (none: the middle ones are bound by the instructions)
                                   {128, 2, 3.90, 2.05, 4.0, 9.0, 2.5},
                                   {64, 2, 1.05, 0.60, 2.5, 3.5, 0.5}};
 constexpr int64_t kCus = kProductCus;
@@ -41,6 +41,7 @@ ProductPlan product_plan(gett_dtype_t dtype, ProductGroups groups, int64_t m, in
     ProductPlan best = {};
     double least = 1e300;
     for (int shape = 0; shape < 3; ++shape) {
+        if (dtype == GETT_FLOAT32 && shape == 0) continue;
         const ShapeCost &c = dtype == GETT_FLOAT32 ? kCost32[shape] : kCost16[shape];
         ProductPlan p = {};
         p.shape = shape;

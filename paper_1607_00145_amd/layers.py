@@ -254,13 +254,33 @@ def _function(name):
 def _make_functions():
     torch = _m._torch
 
-    def once(gradients):
-        # the decorated form refuses a second derivative; nobody can ask for one
-        # where gradients are not recorded, and it costs host time
-        recorded = torch.autograd.function.once_differentiable(gradients)
+    class Refused(torch.autograd.Function):
+        """The gradients as they are; differentiating them raises."""
 
+        @staticmethod
+        def forward(ctx, *values):
+            return tuple(v.view_as(v) for v in values)
+
+        @staticmethod
+        def backward(ctx, *_):
+            raise RuntimeError("the layers' operators have no second derivatives")
+
+    def once(gradients):
+        # Where gradients are recorded on the way back, somebody may ask for second
+        # derivatives: what depends on the gradients then raises, even where the
+        # gradient that came in is a constant.
         def backward(ctx, *dy):
-            return (recorded if torch.is_grad_enabled() else gradients)(ctx, *dy)
+            if not torch.is_grad_enabled():
+                return gradients(ctx, *dy)
+            with torch.no_grad():
+                out = gradients(ctx, *dy)
+            out = out if isinstance(out, tuple) else (out,)
+            there = [i for i, v in enumerate(out) if v is not None]
+            marked = Refused.apply(*(out[i].detach().requires_grad_() for i in there))
+            result = list(out)
+            for i, v in zip(there, marked):
+                result[i] = v
+            return tuple(result)
         return staticmethod(backward)
 
     class Dropout(torch.autograd.Function):

@@ -219,6 +219,12 @@ def test_tiles_by_size(dtype, m, n, k, edge):
     assert product_tiles(dtype, m, n, k).edge == edge
 
 
+def test_no_tiles_of_256_in_32_bits():
+    for k in (0, 1, 64, 4096):
+        for m in (65, 100, 8192, 100000):
+            assert product_tiles(F32, m, m, k).edge in (64, 128)
+
+
 @pytest.mark.parametrize("m,n,k", [(65, 4096, 4096), (1023, 515, 1000), (300, 300, 8192), (2100, 2100, 4096)])
 @pytest.mark.parametrize("dtype", [F32, BF16])
 def test_shared_tiles_fit_their_counters(dtype, m, n, k):
