@@ -279,7 +279,7 @@ gett_status_t gett_combine_grad(gett_dtype_t dtype, int64_t tokens, int k, int64
         if (!apart(eh, e) || !apart(ew, e)) return GETT_ERROR_INVALID_VALUE;
     if (!apart(eh, ew)) return GETT_ERROR_INVALID_VALUE;
     const CombineGradJob j = {dY, H, weights, eh.bytes ? dH : nullptr, dweights, place, offsets, stride_dy,
-                              stride_h, stride_dh, (int)tokens, k, (int)cols, experts, recip(k)};
+                              stride_h, stride_dh, (int)tokens, k, (int)cols, experts};
     return combine_grad_launch(dtype, dtype_w, j, static_cast<hipStream_t>(stream));
 }
 

@@ -55,7 +55,6 @@ struct CombineGradJob {
     const int32_t *place, *offsets;
     int64_t ldy, ldh, ldd;
     int tokens, k, cols, experts;
-    Recip kInv;
 };
 gett_status_t combine_grad_launch(gett_dtype_t t, gett_dtype_t tw, const CombineGradJob &j, hipStream_t s);
 
