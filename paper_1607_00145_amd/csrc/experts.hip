@@ -175,6 +175,13 @@ gett_status_t gett_experts_grad(gett_dtype_t dtype, int64_t tokens, int k, int e
     const int64_t sumsAt = sum ? arena.take(slope_slots(rows, n, experts) * n * 4) : -1;
     // the rows' gradients, which a token sums in 32 bits
     const int64_t partsAt = ex.bytes && gather ? arena.take(rows * width * 4) : -1;
+    BackwardProducts both;
+    both.wantX = ex.bytes;
+    both.wantW = ew.bytes;
+    both.groupsX = kByRows;
+    both.groupsW = kByK;
+    if (both.wantX) both.px = product_plan(dtype, kByRows, rows, width, n, experts);
+    if (both.wantW) both.pw = product_plan(dtype, kByK, n, width, rows, experts);
     Partials hold;
     if (arena.bytes) {
         st = stream_workspace(s, 0, arena.bytes, hold);
@@ -194,36 +201,29 @@ gett_status_t gett_experts_grad(gett_dtype_t dtype, int64_t tokens, int k, int e
         st = place_copy(dtype, ox, hold, rows, width, X, stride_x, s, gather ? order : nullptr, k);
     if (st == GETT_SUCCESS)
         st = place_weights(dtype, ow, hold, experts, n, width, W, stride_w, stride_we, s);
-    if (st == GETT_SUCCESS && ex.bytes) {
-        ProductArgs g = product_args(oz, ow.o, rows, width, n);
-        g.kM = oz.width;
-        g.fullN = ow.o.width;
-        g.stepN = ow.step;
-        g.experts = experts;
-        g.offsets = offsets;
-        g.out.Y = gather ? ws + partsAt : static_cast<char *>(dX);
-        g.out.ldy = gather ? width : stride_dx;
-        g.out.wide = gather ? 1 : 0;
-        st = product_launch_of(dtype, kRowsColumns, kByRows, g,
-                               product_plan(dtype, kByRows, rows, width, n, experts), hold, 0, s);
-        if (st == GETT_SUCCESS && gather) {
-            const int64_t runs = (width + 7) / 8;
-            const CombineJob c = {ws + partsAt, nullptr, nullptr, dX, place, width, 0, stride_dx,
-                                  (int)tokens, k, (int)width, (int)runs, recip(runs)};
-            st = combine_launch(dtype, GETT_FLOAT32, GETT_FLOAT32, c, s);
-        }
-    }
-    if (st == GETT_SUCCESS && ew.bytes) {
-        ProductArgs g = product_args(oz, ox, n, width, rows);
-        g.fullM = oz.width;
-        g.fullN = ox.width;
-        g.stepN = n * width;
-        g.experts = experts;
-        g.offsets = offsets;
-        g.out.Y = static_cast<char *>(dW);
-        g.out.ldy = width;
-        st = product_launch_of(dtype, kColumnsColumns, kByK, g,
-                               product_plan(dtype, kByK, n, width, rows, experts), hold, 0, s);
+    if (st != GETT_SUCCESS) return st;
+    ProductArgs &gx = both.x, &gw = both.w;
+    gx = product_args(oz, ow.o, rows, width, n);
+    gx.kM = oz.width;
+    gx.fullN = ow.o.width;
+    gx.stepN = ow.step;
+    gx.out.Y = gather ? ws + partsAt : static_cast<char *>(dX);
+    gx.out.ldy = gather ? width : stride_dx;
+    gx.out.wide = gather ? 1 : 0;
+    gw = product_args(oz, ox, n, width, rows);
+    gw.fullM = oz.width;
+    gw.fullN = ox.width;
+    gw.stepN = n * width;
+    gw.out.Y = static_cast<char *>(dW);
+    gw.out.ldy = width;
+    gx.experts = gw.experts = experts;
+    gx.offsets = gw.offsets = offsets;
+    st = both.launch(dtype, hold, 0, s);
+    if (st == GETT_SUCCESS && ex.bytes && gather) {
+        const int64_t runs = (width + 7) / 8;
+        const CombineJob c = {ws + partsAt, nullptr, nullptr, dX, place, width, 0, stride_dx,
+                              (int)tokens, k, (int)width, (int)runs, recip(runs)};
+        st = combine_launch(dtype, GETT_FLOAT32, GETT_FLOAT32, c, s);
     }
     return st;
 }

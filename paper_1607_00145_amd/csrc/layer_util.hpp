@@ -64,7 +64,23 @@ gett_status_t product_launch_bf16(ProductForm form, ProductGroups groups, const 
                                   const ProductPlan &p, hipStream_t s);
 gett_status_t product_launch_f16(ProductForm form, ProductGroups groups, const ProductArgs &g,
                                  const ProductPlan &p, hipStream_t s);
-// Slots and counters of a shared sum begin at `slots` of the workspace.
+gett_status_t product_pair_f32(const ProductArgs &x, ProductGroups groupsX, const ProductPlan &px,
+                               const ProductArgs &w, ProductGroups groupsW, const ProductPlan &pw,
+                               hipStream_t s);
+gett_status_t product_pair_bf16(const ProductArgs &x, ProductGroups groupsX, const ProductPlan &px,
+                                const ProductArgs &w, ProductGroups groupsW, const ProductPlan &pw,
+                                hipStream_t s);
+gett_status_t product_pair_f16(const ProductArgs &x, ProductGroups groupsX, const ProductPlan &px,
+                               const ProductArgs &w, ProductGroups groupsW, const ProductPlan &pw,
+                               hipStream_t s);
+inline gett_status_t product_launch_one(gett_dtype_t t, ProductForm form, ProductGroups groups,
+                                        const ProductArgs &g, const ProductPlan &p, hipStream_t s)
+{
+    if (t == GETT_FLOAT32) return product_launch_f32(form, groups, g, p, s);
+    return t == GETT_BFLOAT16 ? product_launch_bf16(form, groups, g, p, s)
+                              : product_launch_f16(form, groups, g, p, s);
+}
+// Slots of a shared sum begin at `slots` of the workspace.
 inline gett_status_t product_launch_of(gett_dtype_t t, ProductForm form, ProductGroups groups,
                                        ProductArgs g, const ProductPlan &p, const Partials &hold,
                                        int64_t slots, hipStream_t s)
@@ -73,10 +89,38 @@ inline gett_status_t product_launch_of(gett_dtype_t t, ProductForm form, Product
         g.slots = reinterpret_cast<float *>(static_cast<char *>(hold.tiles) + slots);
         g.counters = hold.counters;
     }
-    if (t == GETT_FLOAT32) return product_launch_f32(form, groups, g, p, s);
-    return t == GETT_BFLOAT16 ? product_launch_bf16(form, groups, g, p, s)
-                              : product_launch_f16(form, groups, g, p, s);
+    return product_launch_one(t, form, groups, g, p, s);
 }
+
+// The products dX = dz w and dW = dz^T x of a backward pass, one or both.  Of tiles of
+// the same size they are one launch.
+struct BackwardProducts {
+    ProductArgs x = {}, w = {};
+    ProductGroups groupsX = kWhole, groupsW = kWhole;
+    ProductPlan px = {}, pw = {};
+    bool wantX = false, wantW = false;
+    int64_t slotBytes() const { return px.slotBytes + pw.slotBytes; }
+    uint64_t counters() const { return (uint64_t)(px.counters + pw.counters); }
+    gett_status_t launch(gett_dtype_t t, const Partials &hold, int64_t slots, hipStream_t s)
+    {
+        auto share = [&](ProductArgs &g, const ProductPlan &p, int64_t at, int64_t counter) {
+            if (p.slices <= 1) return;
+            g.slots = reinterpret_cast<float *>(static_cast<char *>(hold.tiles) + slots + at);
+            g.counters = hold.counters + counter;
+        };
+        share(x, px, 0, 0);
+        share(w, pw, px.slotBytes, px.counters);
+        if (wantX && wantW && px.shape == pw.shape) {
+            if (t == GETT_FLOAT32) return product_pair_f32(x, groupsX, px, w, groupsW, pw, s);
+            return t == GETT_BFLOAT16 ? product_pair_bf16(x, groupsX, px, w, groupsW, pw, s)
+                                      : product_pair_f16(x, groupsX, px, w, groupsW, pw, s);
+        }
+        gett_status_t st = GETT_SUCCESS;
+        if (wantX) st = product_launch_one(t, kRowsColumns, groupsX, x, px, s);
+        if (wantW && st == GETT_SUCCESS) st = product_launch_one(t, kColumnsColumns, groupsW, w, pw, s);
+        return st;
+    }
+};
 
 // ----------------------------------------------------------- host helpers ---
 

@@ -137,15 +137,15 @@ gett_status_t gett_linear_grad(gett_dtype_t dtype, int64_t m, int64_t n, int64_t
     if (ew.bytes) ox = operand_of(dtype, m, k, X, stride_x, on_grid(dtype, m, k, X, stride_x), arena, m);
     if (ex.bytes) ow = operand_of(dtype, n, k, W, stride_w, on_grid(dtype, n, k, W, stride_w), arena, n);
     const int64_t sumsAt = sum ? arena.take(slope_slots(m, n, 0) * n * 4) : -1;
-    ProductPlan px = {}, pw = {};
-    if (ex.bytes) px = product_plan(dtype, kWhole, m, k, n, 0);
-    if (ew.bytes) pw = product_plan(dtype, kWhole, n, k, m, 0);
-    // (one after the other, in the same slots)
-    const int64_t slots = arena.take(px.slotBytes > pw.slotBytes ? px.slotBytes : pw.slotBytes);
+    BackwardProducts both;
+    both.wantX = ex.bytes;
+    both.wantW = ew.bytes;
+    if (both.wantX) both.px = product_plan(dtype, kWhole, m, k, n, 0);
+    if (both.wantW) both.pw = product_plan(dtype, kWhole, n, k, m, 0);
+    const int64_t slots = arena.take(both.slotBytes());
     Partials hold;
     if (arena.bytes) {
-        st = stream_workspace(s, (uint64_t)(px.counters > pw.counters ? px.counters : pw.counters),
-                              arena.bytes, hold);
+        st = stream_workspace(s, both.counters(), arena.bytes, hold);
         if (st != GETT_SUCCESS) return st;
     }
     char *ws = static_cast<char *>(hold.tiles);
@@ -160,23 +160,19 @@ gett_status_t gett_linear_grad(gett_dtype_t dtype, int64_t m, int64_t n, int64_t
     if (st == GETT_SUCCESS && sum) st = sums_launch(dtype, j, dbias, s);
     if (st == GETT_SUCCESS) st = place_copy(dtype, ox, hold, m, k, X, stride_x, s);
     if (st == GETT_SUCCESS) st = place_copy(dtype, ow, hold, n, k, W, stride_w, s);
-    if (st == GETT_SUCCESS && ex.bytes) {
-        ProductArgs g = product_args(oz, ow, m, k, n);
-        g.kM = oz.width;
-        g.fullN = ow.width;
-        g.out.Y = static_cast<char *>(dX);
-        g.out.ldy = stride_dx;
-        st = product_launch_of(dtype, kRowsColumns, kWhole, g, px, hold, slots, s);
-    }
-    if (st == GETT_SUCCESS && ew.bytes) {
-        ProductArgs g = product_args(oz, ox, n, k, m);
-        g.fullM = oz.width;
-        g.fullN = ox.width;
-        g.out.Y = static_cast<char *>(dW);
-        g.out.ldy = stride_dw;
-        st = product_launch_of(dtype, kColumnsColumns, kWhole, g, pw, hold, slots, s);
-    }
-    return st;
+    if (st != GETT_SUCCESS) return st;
+    ProductArgs &gx = both.x, &gw = both.w;
+    gx = product_args(oz, ow, m, k, n);
+    gx.kM = oz.width;
+    gx.fullN = ow.width;
+    gx.out.Y = static_cast<char *>(dX);
+    gx.out.ldy = stride_dx;
+    gw = product_args(oz, ox, n, k, m);
+    gw.fullM = oz.width;
+    gw.fullN = ox.width;
+    gw.out.Y = static_cast<char *>(dW);
+    gw.out.ldy = stride_dw;
+    return both.launch(dtype, hold, slots, s);
 }
 
 }  // extern "C"

@@ -607,9 +607,9 @@ __device__ __forceinline__ bool product_join(Product<T, MCOL, NCOL, S> &p, const
 // Workgroups take tile after tile.  A tile's loads begin before the results of the
 // one before are written: its first panels arrive while those leave.
 template <typename T, ProductForm FORM, typename S>
-__global__ __launch_bounds__(S::THREADS) void product_kernel(ProductArgs g, int groups)
+__device__ __forceinline__ void product_work(const ProductArgs &g, int groups, int id, int stride,
+                                             char *dyn_lds)
 {
-    extern __shared__ __attribute__((aligned(256))) char dyn_lds[];
     constexpr bool MCOL = FORM == kColumnsColumns, NCOL = FORM != kRowsRows;
     constexpr int KP = 128 / (int)sizeof(T);
     Product<T, MCOL, NCOL, S> p;
@@ -660,10 +660,9 @@ __global__ __launch_bounds__(S::THREADS) void product_kernel(ProductArgs g, int 
     const uint64_t key = g.out.drop.cut ? g.out.drop.key() : 0;
     const int lane = (int)threadIdx.x & 63;
     char *mine = dyn_lds + S::NS * S::STAGE + (p.wm * S::WN + p.wn) * S::RESULTS;
-    int id = (int)blockIdx.x;
     TileAt t;
     bool there = false;
-    for (; id < g.units && !there; id += (int)gridDim.x) there = product_tile<S>(g, groups, id, t);
+    for (; id < g.units && !there; id += stride) there = product_tile<S>(g, groups, id, t);
     if (!there) return;
     begin(t);
     bool after = false;   // a whole tile's stores came after the loads
@@ -674,7 +673,7 @@ __global__ __launch_bounds__(S::THREADS) void product_kernel(ProductArgs g, int 
         __syncthreads();
         TileAt now = t;
         there = false;
-        for (; id < g.units && !there; id += (int)gridDim.x) there = product_tile<S>(g, groups, id, t);
+        for (; id < g.units && !there; id += stride) there = product_tile<S>(g, groups, id, t);
         if (there) begin(t);
         after = false;
         if (now.shared >= 0 &&
@@ -762,6 +761,25 @@ __global__ __launch_bounds__(S::THREADS) void product_kernel(ProductArgs g, int 
         }
         if (!there) return;
     }
+}
+
+template <typename T, ProductForm FORM, typename S>
+__global__ __launch_bounds__(S::THREADS) void product_kernel(ProductArgs g, int groups)
+{
+    extern __shared__ __attribute__((aligned(256))) char dyn_lds[];
+    product_work<T, FORM, S>(g, groups, (int)blockIdx.x, (int)gridDim.x, dyn_lds);
+}
+
+// The two products of a backward pass in one launch: `blocks` workgroups for dz w, the
+// others for dz^T x.  Those of the second begin where those of the first leave off.
+template <typename T, typename S>
+__global__ __launch_bounds__(S::THREADS) void product_pair_kernel(ProductArgs x, int groupsX, int blocks,
+                                                                  ProductArgs w, int groupsW)
+{
+    extern __shared__ __attribute__((aligned(256))) char dyn_lds[];
+    const int id = (int)blockIdx.x;
+    if (id < blocks) product_work<T, kRowsColumns, S>(x, groupsX, id, blocks, dyn_lds);
+    else product_work<T, kColumnsColumns, S>(w, groupsW, id - blocks, (int)gridDim.x - blocks, dyn_lds);
 }
 
 }  // namespace gett

@@ -7,13 +7,13 @@
 
 namespace gett {
 
-template <typename T, ProductForm FORM, typename S>
-gett_status_t product_tiles(ProductGroups groups, ProductArgs g, const ProductPlan &p, hipStream_t s)
+// Fills in a product's tiles; false where there are too many.
+template <typename T> bool product_fill(ProductArgs &g, const ProductPlan &p)
 {
     // (ids are below 2^31 with a grid's stride added)
     if (p.units >= INT32_MAX / 2 || p.tiles >= INT32_MAX / 2 || 4 * p.tilesN >= INT32_MAX ||
         p.slices * ((int64_t)g.k * (int)sizeof(T) / 128 + 1) >= INT32_MAX)
-        return GETT_ERROR_NOT_SUPPORTED;
+        return false;
     g.tiles = (int)p.tiles;
     g.tilesM = (int)p.tilesM;
     g.tilesN = (int)p.tilesN;
@@ -24,11 +24,33 @@ gett_status_t product_tiles(ProductGroups groups, ProductArgs g, const ProductPl
     g.slices = (int)p.slices;
     g.slicesInv = recip(p.slices);
     g.units = (int)p.units;
+    return true;
+}
+
+template <typename T, ProductForm FORM, typename S>
+gett_status_t product_tiles(ProductGroups groups, ProductArgs g, const ProductPlan &p, hipStream_t s)
+{
+    if (!product_fill<T>(g, p)) return GETT_ERROR_NOT_SUPPORTED;
     constexpr auto kernel = product_kernel<T, FORM, S>;
     if (allow_dynamic_lds<kernel>(S::LDS) != hipSuccess) return GETT_ERROR_HIP;
     const unsigned blocks = persistent_grid<kernel>(S::THREADS, (unsigned)g.units, S::LDS);
     if (blocks == 0) return GETT_ERROR_HIP;
     hipLaunchKernelGGL(kernel, dim3(blocks), dim3(S::THREADS), S::LDS, s, g, (int)groups);
+    return launched(hipGetLastError());
+}
+
+template <typename T, typename S>
+gett_status_t product_pair(ProductArgs x, ProductGroups groupsX, const ProductPlan &px, ProductArgs w,
+                           ProductGroups groupsW, const ProductPlan &pw, hipStream_t s)
+{
+    if (!product_fill<T>(x, px) || !product_fill<T>(w, pw)) return GETT_ERROR_NOT_SUPPORTED;
+    constexpr auto kernel = product_pair_kernel<T, S>;
+    if (allow_dynamic_lds<kernel>(S::LDS) != hipSuccess) return GETT_ERROR_HIP;
+    const unsigned first = persistent_grid<kernel>(S::THREADS, (unsigned)x.units, S::LDS);
+    const unsigned second = persistent_grid<kernel>(S::THREADS, (unsigned)w.units, S::LDS);
+    if (first == 0 || second == 0) return GETT_ERROR_HIP;
+    hipLaunchKernelGGL(kernel, dim3(first + second), dim3(S::THREADS), S::LDS, s, x, (int)groupsX, (int)first,
+                       w, (int)groupsW);
     return launched(hipGetLastError());
 }
 
@@ -87,6 +109,22 @@ gett_status_t product_launch(ProductForm form, ProductGroups groups, const Produ
     if (form == kRowsRows) return product_form<T, kRowsRows>(groups, g, p, s);
     if (form == kRowsColumns) return product_form<T, kRowsColumns>(groups, g, p, s);
     return product_form<T, kColumnsColumns>(groups, g, p, s);
+}
+
+// Both products of a backward pass, of the same tiles.
+template <typename T>
+gett_status_t product_launch_pair(const ProductArgs &x, ProductGroups groupsX, const ProductPlan &px,
+                                  const ProductArgs &w, ProductGroups groupsW, const ProductPlan &pw,
+                                  hipStream_t s)
+{
+    if constexpr (sizeof(T) == 2)
+        if (px.shape == 0) return product_pair<T, ProductBig>(x, groupsX, px, w, groupsW, pw, s);
+    const bool deep = px.units + pw.units <= kProductCus;
+    if (px.shape == 1)
+        return deep ? product_pair<T, ProductMidDeep>(x, groupsX, px, w, groupsW, pw, s)
+                    : product_pair<T, ProductMid>(x, groupsX, px, w, groupsW, pw, s);
+    return deep ? product_pair<T, ProductSmallDeep>(x, groupsX, px, w, groupsW, pw, s)
+                : product_pair<T, ProductSmall>(x, groupsX, px, w, groupsW, pw, s);
 }
 
 }  // namespace gett
