@@ -89,7 +89,8 @@ __global__ __launch_bounds__(256) void layer_slope_kernel(SlopeJob j)
     if (begin + size < end) end = begin + size;
     const int col0 = ((int)blockIdx.x - slot * j.across) * kSlopeCols, col = col0 + lane * 8;
     const int left = j.n - col;
-    const uint64_t key = j.drop.cut ? j.drop.key() : 0;
+    PhiloxColumn random = {};
+    if (j.drop.cut) random = philox_column((uint32_t)col >> 3, j.drop.offset, j.drop.key());
     const bool active = j.activation != GETT_ACTIVATION_NONE;
     float total[8] = {};
     if (left > 0) {
@@ -112,7 +113,11 @@ __global__ __launch_bounds__(256) void layer_slope_kernel(SlopeJob j)
                         if (i < left) v[x][i] *= slope(j.activation, z[x][i]);
                 }
                 // (last: what is dropped is zero, whatever it was)
-                if (j.drop.cut) drop8(v[x], j.drop, key, (uint32_t)row, (uint32_t)col);
+                if (j.drop.cut) {
+                    uint32_t w[4];
+                    philox_row(random, (uint32_t)row, w);
+                    drop8(v[x], j.drop, w);
+                }
 #pragma unroll
                 for (int i = 0; i < 8; ++i) total[i] += v[x][i];
                 if (j.dZ)

@@ -166,11 +166,13 @@ def _rows(name, t, dtype=None):
     Returns it and its row stride."""
     if t.dim() != 2:
         raise ValueError(f"{name} must be a matrix")
-    if dtype is not None and t.dtype != dtype:
+    if dtype is not None and t.dtype is not dtype:
         raise TypeError(f"{name} is {t.dtype}, not {dtype}")
     if not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
     r, c = t.shape
+    if t.is_contiguous():
+        return t, c
     sr, sc = t.stride()
     if (c > 1 and sc != 1) or (r > 1 and sr < c):
         t = t.contiguous()
@@ -302,7 +304,7 @@ def _make_functions():
             need_x, need_w, need_b = ctx.needs_input_grad[:3]
             z = None
             if activation and (need_x or need_w or need_b):
-                z = torch.empty((x.shape[0], w.shape[0]), dtype=x.dtype, device=x.device)
+                z = x.new_empty((x.shape[0], w.shape[0]))
             y = _linear(x, w, bias, residual, seed, activation, drop, z)
             ctx.activation, ctx.drop, ctx.sizes = activation, drop, (x.shape, w.shape)
             ctx.save_for_backward(x if need_w else None, w if need_x else None, z, seed)
@@ -321,19 +323,14 @@ def _make_functions():
 
     class Route(torch.autograd.Function):
         @staticmethod
-        def forward(ctx, logits, how):
-            out = _route(logits, how)
-            ctx.how = how
-            ctx.save_for_backward(logits, out[1])
-            ctx.mark_non_differentiable(*out[1:])
-            ctx.set_materialize_grads(False)
-            return out
+        def forward(ctx, logits, how, lists):
+            ctx.how, ctx.lists = how, lists
+            ctx.save_for_backward(logits)
+            return _route(logits, how, lists)
 
-        def gradients(ctx, dweights, *_):
-            if dweights is None:
-                return None, None
-            logits, index = ctx.saved_tensors
-            return _route_grad(logits, index, dweights, ctx.how), None
+        def gradients(ctx, dweights):
+            logits, = ctx.saved_tensors
+            return _route_grad(logits, ctx.lists, dweights, ctx.how), None, None
 
         backward = once(gradients)
 
@@ -343,17 +340,16 @@ def _make_functions():
             need_x, need_w, need_b = ctx.needs_input_grad[:3]
             z = None
             if activation and (need_x or need_w or need_b):
-                z = torch.empty((routing.tokens * routing.k, w.shape[1]), dtype=x.dtype,
-                                device=x.device)
+                z = x.new_empty((routing.tokens * routing.k, w.shape[1]))
             y = _experts(x, w, bias, routing, activation, gather, z)
             ctx.how = routing.tokens, routing.k, activation, gather, x.shape, w.shape
-            ctx.save_for_backward(x if need_w else None, w if need_x else None, z, routing.order,
-                                  routing.offsets, routing.place)
+            ctx.lists = routing._lists
+            ctx.save_for_backward(x if need_w else None, w if need_x else None, z)
             return y
 
         def gradients(ctx, dy):
-            return (*_experts_grad(dy, *ctx.saved_tensors, ctx.how, *ctx.needs_input_grad[:3]),
-                    None, None, None)
+            return (*_experts_grad(dy, *ctx.saved_tensors, ctx.lists, ctx.how,
+                                   *ctx.needs_input_grad[:3]), None, None, None)
 
         backward = once(gradients)
 
@@ -362,15 +358,15 @@ def _make_functions():
         def forward(ctx, h, weights, residual, routing):
             need_h, need_w = ctx.needs_input_grad[:2]
             ctx.how = routing.tokens, routing.k, routing.experts, h.shape, weights.dtype
-            ctx.save_for_backward(h if need_w else None, weights if need_h else None,
-                                  routing.place, routing.offsets)
+            ctx.lists = routing._lists
+            ctx.save_for_backward(h if need_w else None, weights if need_h else None)
             return _combine(h, weights, residual, routing)
 
         def gradients(ctx, dy):
             need_h, need_w, need_r = ctx.needs_input_grad[:3]
             dh = dw = None
             if need_h or need_w:
-                dh, dw = _combine_grad(dy, *ctx.saved_tensors, ctx.how, need_h, need_w)
+                dh, dw = _combine_grad(dy, *ctx.saved_tensors, ctx.lists, ctx.how, need_h, need_w)
             return dh, dw, dy if need_r else None, None
 
         backward = once(gradients)
@@ -389,10 +385,12 @@ def _dropout(x, drop, seed):
     code = _m._code(x.dtype)
     x, sx = _rows("x", x)
     r, c = x.shape
-    y = _m._torch.empty((r, c), dtype=x.dtype, device=x.device)
+    y = x.new_empty((r, c))
     d = _drop_struct(drop, seed)
-    _checked(_bound.gett_dropout(code, r, c, x.data_ptr(), sx, ctypes.addressof(d), y.data_ptr(),
-                                 c, _m._stream(x.get_device())), "gett_dropout")
+    st = _bound.gett_dropout(code, r, c, x.data_ptr(), sx, ctypes.addressof(d), y.data_ptr(), c,
+                             _m._stream(x.get_device()))
+    if st != 0:
+        raise GettError(st, "gett_dropout")
     return y
 
 
@@ -405,7 +403,8 @@ def dropout(x, p: float, seed, offset: int = 0):
     integer, or an int64 device tensor of one element that is read when the kernel
     runs (a captured graph draws a new mask when it changes between replays; it must
     not change between a call and its gradient)."""
-    torch = _start()
+    if _bound is None:
+        _start()
     flat = _flat("x", x)
     _m._code(x.dtype)
     _m._device("x", x)
@@ -438,11 +437,13 @@ def _linear(x, w, bias, residual, seed, activation, drop, z):
         if tuple(residual.shape) != (m, n):
             raise ValueError("residual differs from the result in shape")
         residual, sr = _rows("residual", residual, dtype)
-    y = _m._torch.empty((m, n), dtype=dtype, device=x.device)
+    y = x.new_empty((m, n))
     d = _drop_struct(drop, seed)
-    _checked(_bound.gett_linear(code, m, n, k, x.data_ptr(), sx, w.data_ptr(), sw, _ptr(bias),
-                                activation, _drop_ref(d), _ptr(residual), sr, _ptr(z), n,
-                                y.data_ptr(), n, _m._stream(x.get_device())), "gett_linear")
+    st = _bound.gett_linear(code, m, n, k, x.data_ptr(), sx, w.data_ptr(), sw, _ptr(bias), activation,
+                            _drop_ref(d), _ptr(residual), sr, _ptr(z), n, y.data_ptr(), n,
+                            _m._stream(x.get_device()))
+    if st != 0:
+        raise GettError(st, "gett_linear")
     return y
 
 
@@ -451,7 +452,6 @@ def _linear_grad(dy, z, x, w, seed, activation, drop, sizes, need_x, need_w, nee
     if there is not None:
         with there:
             return _linear_grad(dy, z, x, w, seed, activation, drop, sizes, need_x, need_w, need_b)
-    torch = _m._torch
     (m, k), (n, _) = sizes
     dtype = dy.dtype
     dy, sy = _rows("dy", dy)
@@ -460,9 +460,9 @@ def _linear_grad(dy, z, x, w, seed, activation, drop, sizes, need_x, need_w, nee
         x, sx = _rows("x", x)
     if need_x:
         w, sw = _rows("w", w)
-    dx = torch.empty((m, k), dtype=dtype, device=dy.device) if need_x else None
-    dw = torch.empty((n, k), dtype=dtype, device=dy.device) if need_w else None
-    db = torch.empty(n, dtype=dtype, device=dy.device) if need_b else None
+    dx = dy.new_empty((m, k)) if need_x else None
+    dw = dy.new_empty((n, k)) if need_w else None
+    db = dy.new_empty(n) if need_b else None
     d = _drop_struct(drop, seed)
     _checked(_bound.gett_linear_grad(
         _m._code(dtype), m, n, k, dy.data_ptr(), sy, _ptr(z), n, _ptr(x) if need_w else None, sx,
@@ -479,7 +479,8 @@ def linear(x, w, bias=None, activation=None, residual=None, p: float = 0.0, seed
     are those of `dropout`.  All tensors have one type; sums and the epilogue are in
     32 bits and rounded once.  Differentiable in x, w, bias and residual: for the
     gradient x @ w.T + bias is kept where there is an activation, and no mask."""
-    _start()
+    if _bound is None:
+        _start()
     _m._code(x.dtype)
     code = _activation(activation)
     flat = _flat("x", x)
@@ -509,51 +510,72 @@ class Routing:
     ``weights`` (float32, differentiable) and ``index`` (int32) are tokens x k;
     ``order`` lists the rows token * k + choice expert after expert (-1 behind the
     last), ``offsets`` says where each expert's begin, ``place`` is where `order`
-    has each row (-1: nowhere)."""
+    has each row (-1: nowhere).  The lists are parts of one tensor, not to be
+    written into."""
 
-    __slots__ = ("tokens", "experts", "k", "weights", "index", "order", "offsets", "place")
+    __slots__ = ("tokens", "experts", "k", "weights", "_lists")
 
-    def __init__(self, tokens, experts, k, weights, index, order, offsets, place):
+    def __init__(self, tokens, experts, k, weights, lists):
         self.tokens, self.experts, self.k = tokens, experts, k
-        self.weights, self.index, self.order = weights, index, order
-        self.offsets, self.place = offsets, place
+        self.weights, self._lists = weights, lists   # index, order, place, offsets
+
+    @property
+    def index(self):
+        t, k = self.tokens, self.k
+        return self._lists.as_strided((t, k), (k, 1), 0)
+
+    @property
+    def order(self):
+        n = self.tokens * self.k
+        return self._lists.as_strided((n,), (1,), n)
+
+    @property
+    def place(self):
+        t, k = self.tokens, self.k
+        return self._lists.as_strided((t, k), (k, 1), 2 * t * k)
+
+    @property
+    def offsets(self):
+        return self._lists.as_strided((self.experts + 1,), (1,), 3 * self.tokens * self.k)
 
 
-def _route(logits, how):
+def _addresses(lists, n):
+    """Of a routing's index, order, place and offsets; n = tokens * k."""
+    p = lists.data_ptr()
+    return p, p + 4 * n, p + 8 * n, p + 12 * n
+
+
+def _route(logits, how, lists):
     there = _m._elsewhere(logits, how[2])
     if there is not None:
         with there:
-            return _route(logits, how)
-    torch = _m._torch
+            return _route(logits, how, lists)
     k, scoring, bias, groups, top_groups, renormalize, scale = how
     logits, stride = _rows("logits", logits)
     t, e = logits.shape
-    # one allocation for the whole numbers, each part of 4 bytes an item
-    whole = torch.empty(3 * t * k + e + 1, dtype=torch.int32, device=logits.device)
-    weights = torch.empty((t, k), dtype=torch.float32, device=logits.device)
-    n = t * k
-    p = whole.data_ptr()
-    _checked(_bound.gett_route(
-        _m._code(logits.dtype), t, e, k, logits.data_ptr(), stride, scoring, _ptr(bias), groups,
-        top_groups, renormalize, scale, weights.data_ptr(), p, p + 4 * n, p + 12 * n, p + 8 * n,
-        _m._stream(logits.get_device())), "gett_route")
-    return (weights, whole[:n].view(t, k), whole[n:2 * n], whole[3 * n:],
-            whole[2 * n:3 * n].view(t, k))
+    weights = logits.new_empty((t, k), dtype=_m._torch.float32)
+    index, order, place, offsets = _addresses(lists, t * k)
+    st = _bound.gett_route(_m._code(logits.dtype), t, e, k, logits.data_ptr(), stride, scoring,
+                           _ptr(bias), groups, top_groups, renormalize, scale, weights.data_ptr(),
+                           index, order, offsets, place, _m._stream(logits.get_device()))
+    if st != 0:
+        raise GettError(st, "gett_route")
+    return weights
 
 
-def _route_grad(logits, index, dweights, how):
+def _route_grad(logits, lists, dweights, how):
     there = _m._elsewhere(logits, dweights)
     if there is not None:
         with there:
-            return _route_grad(logits, index, dweights, how)
+            return _route_grad(logits, lists, dweights, how)
     k, scoring, _, _, _, renormalize, scale = how
-    out = _m._torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
     logits, stride = _rows("logits", logits)
     dweights = dweights.contiguous()
     t, e = logits.shape
+    out = logits.new_empty((t, e))
     _checked(_bound.gett_route_grad(
         _m._code(logits.dtype), t, e, k, logits.data_ptr(), stride, scoring, renormalize, scale,
-        index.data_ptr(), dweights.data_ptr(), out.data_ptr(), e, _m._stream(logits.get_device())),
+        lists.data_ptr(), dweights.data_ptr(), out.data_ptr(), e, _m._stream(logits.get_device())),
         "gett_route_grad")
     return out
 
@@ -568,7 +590,8 @@ def route(logits, k: int, scoring: str = "softmax", bias=None, groups: int = 1,
     are the scores of the chosen, divided by their sum unless `renormalize` is false,
     times `scale`.  Ties go to the lowest index.  An expert whose logit is -inf is never
     chosen: where fewer than k are open the last indices are -1 and their weights 0."""
-    torch = _start()
+    if _bound is None:
+        _start()
     _m._code(logits.dtype)
     if logits.dim() != 2:
         raise ValueError("logits must be a matrix (tokens x experts)")
@@ -576,16 +599,21 @@ def route(logits, k: int, scoring: str = "softmax", bias=None, groups: int = 1,
     if scoring not in SCORES:
         raise ValueError(f"scoring must be one of {sorted(SCORES)}")
     t, e = logits.shape
+    k = int(k)
+    if k < 1 or k > e:
+        raise ValueError(f"k must be in [1, {e}]")
     if bias is not None:
         if _records(bias):
             raise RuntimeError("the bias of the choice has no gradient: detach it")
-        bias = _vector("bias", bias, e, torch.float32)
-    how = (int(k), SCORES[scoring], bias, int(groups),
-           int(groups if top_groups is None else top_groups), int(bool(renormalize)), float(scale))
-    if k < 1 or k > e:
-        raise ValueError(f"k must be in [1, {e}]")
-    out = _function("route").apply(logits, how) if _records(logits) else _route(logits, how)
-    return Routing(t, e, how[0], *out)
+        bias = _vector("bias", bias, e, _m._torch.float32)
+    how = (k, SCORES[scoring], bias, int(groups), int(groups if top_groups is None else top_groups),
+           1 if renormalize else 0, float(scale))
+    lists = logits.new_empty(3 * t * k + e + 1, dtype=_m._torch.int32)
+    if _records(logits):
+        weights = _function("route").apply(logits, how, lists)
+    else:
+        weights = _route(logits, how, lists)
+    return Routing(t, e, k, weights, lists)
 
 
 # experts ---------------------------------------------------------------------
@@ -593,6 +621,8 @@ def route(logits, k: int, scoring: str = "softmax", bias=None, groups: int = 1,
 def _weights3(w):
     """experts x n x width with neighbours along the width: itself or a copy."""
     e, n, c = w.shape
+    if w.is_contiguous():
+        return w, c, n * c
     se, sn, sc = w.stride()
     if (c > 1 and sc != 1) or (n > 1 and sn < c) or (e > 1 and se < 0):
         w = w.contiguous()
@@ -601,7 +631,7 @@ def _weights3(w):
 
 
 def _experts(x, w, bias, routing, activation, gather, z):
-    there = _m._elsewhere(x, w, bias, routing.offsets)
+    there = _m._elsewhere(x, w, bias, routing._lists)
     if there is not None:
         with there:
             return _experts(x, w, bias, routing, activation, gather, z)
@@ -612,20 +642,21 @@ def _experts(x, w, bias, routing, activation, gather, z):
     n, width = w.shape[1], w.shape[2]
     if bias is not None and not bias.is_contiguous():
         bias = bias.contiguous()
-    y = _m._torch.empty((t * k, n), dtype=dtype, device=x.device)
-    _checked(_bound.gett_experts(
-        _m._code(dtype), t, k, e, n, width, x.data_ptr(), sx, int(gather), w.data_ptr(), sw, se,
-        _ptr(bias), activation, routing.order.data_ptr(), routing.offsets.data_ptr(), _ptr(z), n,
-        y.data_ptr(), n, _m._stream(x.get_device())), "gett_experts")
+    y = x.new_empty((t * k, n))
+    _, order, _, offsets = _addresses(routing._lists, t * k)
+    st = _bound.gett_experts(_m._code(dtype), t, k, e, n, width, x.data_ptr(), sx, int(gather),
+                             w.data_ptr(), sw, se, _ptr(bias), activation, order, offsets, _ptr(z), n,
+                             y.data_ptr(), n, _m._stream(x.get_device()))
+    if st != 0:
+        raise GettError(st, "gett_experts")
     return y
 
 
-def _experts_grad(dy, x, w, z, order, offsets, place, how, need_x, need_w, need_b):
+def _experts_grad(dy, x, w, z, lists, how, need_x, need_w, need_b):
     there = _m._elsewhere(dy)
     if there is not None:
         with there:
-            return _experts_grad(dy, x, w, z, order, offsets, place, how, need_x, need_w, need_b)
-    torch = _m._torch
+            return _experts_grad(dy, x, w, z, lists, how, need_x, need_w, need_b)
     t, k, activation, gather, shape_x, shape_w = how
     e, n, width = shape_w
     dtype = dy.dtype
@@ -635,13 +666,14 @@ def _experts_grad(dy, x, w, z, order, offsets, place, how, need_x, need_w, need_
         x, sx = _rows("x", x)
     if need_x:
         w, sw, se = _weights3(w)
-    dx = torch.empty(shape_x, dtype=dtype, device=dy.device) if need_x else None
-    dw = torch.empty(shape_w, dtype=dtype, device=dy.device) if need_w else None
-    db = torch.empty((e, n), dtype=dtype, device=dy.device) if need_b else None
+    dx = dy.new_empty(shape_x) if need_x else None
+    dw = dy.new_empty(shape_w) if need_w else None
+    db = dy.new_empty((e, n)) if need_b else None
+    _, order, place, offsets = _addresses(lists, t * k)
     _checked(_bound.gett_experts_grad(
         _m._code(dtype), t, k, e, n, width, dy.data_ptr(), sy, _ptr(z), n, _ptr(x), sx, int(gather),
-        _ptr(w), sw, se, activation, order.data_ptr(), offsets.data_ptr(), place.data_ptr(),
-        _ptr(dx), width, _ptr(dw), _ptr(db), _m._stream(dy.get_device())), "gett_experts_grad")
+        _ptr(w), sw, se, activation, order, offsets, place, _ptr(dx), width, _ptr(dw), _ptr(db),
+        _m._stream(dy.get_device())), "gett_experts_grad")
     return dx, dw, db
 
 
@@ -652,7 +684,8 @@ def expert_linear(x, w, routing: Routing, bias=None, activation=None, gather: bo
     With `gather` x has a row for each token (tokens x width); otherwise a row for each
     row of the result, as another `expert_linear` returns them.  `w` is experts x n x
     width, `bias` experts x n.  Differentiable in x, w and bias."""
-    _start()
+    if _bound is None:
+        _start()
     _m._code(x.dtype)
     code = _activation(activation)
     _m._device("x", x)
@@ -665,7 +698,7 @@ def expert_linear(x, w, routing: Routing, bias=None, activation=None, gather: bo
         raise ValueError(f"w must be {routing.experts} x n x {x.shape[1]}")
     for name, t in (("w", w), ("bias", bias)):
         if t is not None:
-            if t.dtype != x.dtype:
+            if t.dtype is not x.dtype:
                 raise TypeError(f"{name} is {t.dtype}, not {x.dtype}")
             _m._device(name, t)
     if bias is not None and bias.shape != w.shape[:2]:
@@ -678,7 +711,7 @@ def expert_linear(x, w, routing: Routing, bias=None, activation=None, gather: bo
 # combine ---------------------------------------------------------------------
 
 def _combine(h, weights, residual, routing):
-    there = _m._elsewhere(h, weights, residual, routing.place)
+    there = _m._elsewhere(h, weights, residual, routing._lists)
     if there is not None:
         with there:
             return _combine(h, weights, residual, routing)
@@ -690,20 +723,21 @@ def _combine(h, weights, residual, routing):
     sr = 0
     if residual is not None:
         residual, sr = _rows("residual", residual, dtype)
-    y = _m._torch.empty((t, c), dtype=dtype, device=h.device)
-    _checked(_bound.gett_combine(
-        _m._code(dtype), t, k, c, h.data_ptr(), sh, _m._code(weights.dtype), weights.data_ptr(),
-        routing.place.data_ptr(), _ptr(residual), sr, y.data_ptr(), c,
-        _m._stream(h.get_device())), "gett_combine")
+    y = h.new_empty((t, c))
+    _, _, place, _ = _addresses(routing._lists, t * k)
+    st = _bound.gett_combine(_m._code(dtype), t, k, c, h.data_ptr(), sh, _m._code(weights.dtype),
+                             weights.data_ptr(), place, _ptr(residual), sr, y.data_ptr(), c,
+                             _m._stream(h.get_device()))
+    if st != 0:
+        raise GettError(st, "gett_combine")
     return y
 
 
-def _combine_grad(dy, h, weights, place, offsets, how, need_h, need_w):
+def _combine_grad(dy, h, weights, lists, how, need_h, need_w):
     there = _m._elsewhere(dy)
     if there is not None:
         with there:
-            return _combine_grad(dy, h, weights, place, offsets, how, need_h, need_w)
-    torch = _m._torch
+            return _combine_grad(dy, h, weights, lists, how, need_h, need_w)
     t, k, e, shape, wtype = how
     c = shape[1]
     dy, sy = _rows("dy", dy)
@@ -712,11 +746,12 @@ def _combine_grad(dy, h, weights, place, offsets, how, need_h, need_w):
         h, sh = _rows("h", h)
     if need_h and not weights.is_contiguous():
         weights = weights.contiguous()
-    dh = torch.empty(shape, dtype=dy.dtype, device=dy.device) if need_h else None
-    dw = torch.empty((t, k), dtype=wtype, device=dy.device) if need_w else None
+    dh = dy.new_empty(shape) if need_h else None
+    dw = dy.new_empty((t, k), dtype=wtype) if need_w else None
+    _, _, place, offsets = _addresses(lists, t * k)
     _checked(_bound.gett_combine_grad(
         _m._code(dy.dtype), t, k, c, dy.data_ptr(), sy, _ptr(h), sh, _m._code(wtype),
-        _ptr(weights), place.data_ptr(), e, offsets.data_ptr(), _ptr(dh), c, _ptr(dw),
+        _ptr(weights), place, e, offsets, _ptr(dh), c, _ptr(dw),
         _m._stream(dy.get_device())), "gett_combine_grad")
     return dh, dw
 
@@ -726,7 +761,8 @@ def combine(h, routing: Routing, weights=None, residual=None):
 
     `h` has the rows of `expert_linear`; `weights` are tokens x k, in float32 or h's
     type (default: the routing's).  Differentiable in h, weights and residual."""
-    _start()
+    if _bound is None:
+        _start()
     _m._code(h.dtype)
     _m._device("h", h)
     if weights is None:

@@ -38,9 +38,7 @@ def calls(monkeypatch):
 
 
 def routing(index):
-    i32 = dict(dtype=torch.int32)
-    return g.Routing(6, 3, 2, On(index, 6, 2), On(index, 6, 2, **i32), On(index, 12, **i32),
-                     On(index, 4, **i32), On(index, 6, 2, **i32))
+    return g.Routing(6, 3, 2, On(index, 6, 2), On(index, 3 * 12 + 4, dtype=torch.int32))
 
 
 def every_call(i, j):
