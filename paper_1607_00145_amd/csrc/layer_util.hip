@@ -107,11 +107,7 @@ __global__ __launch_bounds__(256) void layer_slope_kernel(SlopeJob j)
             for (int x = 0; x < 2; ++x) {
                 const int row = row0 + 8 * x;
                 if (row >= end) break;
-                if (active) {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        if (i < left) v[x][i] *= slope(j.activation, z[x][i]);
-                }
+                if (active) slope8(j.activation, v[x], z[x]);   // (zeros behind the last column)
                 // (last: what is dropped is zero, whatever it was)
                 if (j.drop.cut) {
                     uint32_t w[4];

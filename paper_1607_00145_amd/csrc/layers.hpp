@@ -118,43 +118,60 @@ __device__ __forceinline__ void drop8(float v[8], const Drop &d, uint64_t key, u
 // e^x, within two steps for |x| < 100 or so
 __device__ __forceinline__ float quick_exp(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504f); }
 
-// The normal distribution's cdf and e^(-z^2/2), within 1.5e-7: Abramowitz and
-// Stegun, Handbook of Mathematical Functions, 7.1.26,
+// The tail 1 - cdf(|z|) of the normal distribution and e^(-z^2/2), within 0.8e-7:
+// Abramowitz and Stegun, Handbook of Mathematical Functions, 7.1.26,
 //     erfc(x) = (a1 t + ... + a5 t^5) e^(-x^2), t = 1 / (1 + p x), x = |z| / sqrt 2,
 // with halved coefficients.  (The library's erff and expf take three times as long,
 // and an epilogue of 8192 x 8192 results 170 us.)
-__device__ __forceinline__ float normal_cdf(float z, float &e)
+__device__ __forceinline__ float normal_tail(float z, float &e)
 {
-    const float x = fabsf(z) * 0.70710678f;
-    const float t = __builtin_amdgcn_rcpf(1.0f + 0.3275911f * x);
-    e = quick_exp(-x * x);
-    const float half = t * (0.127414796f + t * (-0.142248368f + t * (0.7107068705f +
-                       t * (-0.7265760135f + t * 0.5307027145f)))) * e;
-    return z < 0.0f ? half : 1.0f - half;
+    const float t = __builtin_amdgcn_rcpf(1.0f + 0.23164189f * fabsf(z));
+    e = __builtin_amdgcn_exp2f(z * z * -0.72134752f);
+    return t * (0.127414796f + t * (-0.142248368f + t * (0.7107068705f +
+               t * (-0.7265760135f + t * 0.5307027145f)))) * e;
 }
-__device__ __forceinline__ float activate(int kind, float z)
+__device__ __forceinline__ float gelu(float z)
 {
-    if (kind == GETT_ACTIVATION_RELU) return z > 0.0f || z != z ? z : 0.0f;
-    if (kind == GETT_ACTIVATION_GELU) {
-        float e;
-        return z * normal_cdf(z, e);
-    }
-    if (kind == GETT_ACTIVATION_SILU) return z * __builtin_amdgcn_rcpf(1.0f + quick_exp(-z));
-    return z;
+    // z cdf(z), as max(z, 0) less |z| times the tail; |z| finite: of infinity it is 0
+    float e;
+    const float tail = normal_tail(z, e);
+    const float positive = z < 0.0f ? 0.0f : z;   // (a NaN stays one)
+    return positive - fminf(fabsf(z), 3e38f) * tail;
 }
-__device__ __forceinline__ float slope(int kind, float z)
+__device__ __forceinline__ float gelu_slope(float z)
 {
-    if (kind == GETT_ACTIVATION_RELU) return z > 0.0f ? 1.0f : z != z ? z : 0.0f;
-    if (kind == GETT_ACTIVATION_GELU) {
-        float e;
-        const float cdf = normal_cdf(z, e);
-        return cdf + z * 0.39894228f * e;
-    }
-    if (kind == GETT_ACTIVATION_SILU) {
-        const float s = __builtin_amdgcn_rcpf(1.0f + quick_exp(-z));
-        return s * (1.0f + z * (1.0f - s));
-    }
-    return 1.0f;
+    float e;
+    const float tail = normal_tail(z, e);
+    return (z < 0.0f ? tail : 1.0f - tail) + z * 0.39894228f * e;
+}
+__device__ __forceinline__ float silu(float z) { return z * __builtin_amdgcn_rcpf(1.0f + quick_exp(-z)); }
+__device__ __forceinline__ float silu_slope(float z)
+{
+    const float s = __builtin_amdgcn_rcpf(1.0f + quick_exp(-z));
+    return s * (1.0f + z * (1.0f - s));
+}
+__device__ __forceinline__ float relu(float z) { return z < 0.0f ? 0.0f : z; }
+__device__ __forceinline__ float relu_slope(float z) { return z > 0.0f ? 1.0f : z != z ? z : 0.0f; }
+
+// Eight numbers through one activation: which one is asked once, and the eight chains
+// of dependent instructions run side by side.
+template <typename F> __device__ __forceinline__ void each8(float v[8], const float z[8], F f)
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = f(v[i], z[i]);
+}
+__device__ __forceinline__ void activate8(int kind, float v[8])
+{
+    if (kind == GETT_ACTIVATION_GELU) each8(v, v, [](float, float z) { return gelu(z); });
+    else if (kind == GETT_ACTIVATION_SILU) each8(v, v, [](float, float z) { return silu(z); });
+    else if (kind == GETT_ACTIVATION_RELU) each8(v, v, [](float, float z) { return relu(z); });
+}
+// v times the slope at z
+__device__ __forceinline__ void slope8(int kind, float v[8], const float z[8])
+{
+    if (kind == GETT_ACTIVATION_GELU) each8(v, z, [](float g, float z) { return g * gelu_slope(z); });
+    else if (kind == GETT_ACTIVATION_SILU) each8(v, z, [](float g, float z) { return g * silu_slope(z); });
+    else if (kind == GETT_ACTIVATION_RELU) each8(v, z, [](float g, float z) { return g * relu_slope(z); });
 }
 
 // ------------------------------------------------------------------ vectors ---

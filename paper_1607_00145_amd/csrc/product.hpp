@@ -441,10 +441,7 @@ __device__ __forceinline__ void product_finish(const Epilogue &o, int64_t row, i
         for (int i = 0; i < 8; ++i) v[i] += to_float(bias.v[i]);
     }
     if (o.Z) store8(reinterpret_cast<T *>(o.Z) + row * o.ldz + col, left, v);
-    if (o.activation != GETT_ACTIVATION_NONE) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = activate(o.activation, v[i]);
-    }
+    activate8(o.activation, v);
     if (o.drop.cut) drop8(v, o.drop, w);
     if (o.residual) {
 #pragma unroll
