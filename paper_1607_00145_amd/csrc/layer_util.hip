@@ -34,7 +34,7 @@ __global__ __launch_bounds__(256) void layer_copy_kernel(CopyJob j)
     const T *src = reinterpret_cast<const T *>(j.src) + at + col;
     Run<T, EP> v;
     if (col + EP <= j.cols) {
-        v = *reinterpret_cast<const Run<T, EP> *>(src);
+        v = __builtin_bit_cast(Run<T, EP>, load16(src));
     } else {
 #pragma unroll
         for (int i = 0; i < EP; ++i) v.v[i] = col + i < j.cols ? src[i] : from_float<T>(0.0f);

@@ -176,37 +176,65 @@ __device__ __forceinline__ void slope8(int kind, float v[8], const float z[8])
 
 // ------------------------------------------------------------------ vectors ---
 
-// `left` of eight neighbours (0 for the others), and back
-template <typename T> __device__ __forceinline__ void load8(const T *p, int left, float v[8])
+// Whole vectors at any element address.  (Stored element by element, eight numbers
+// of 16 bits become a store of 12 bytes between two of two.)
+typedef int any16 __attribute__((ext_vector_type(4), aligned(2)));
+typedef float any16f __attribute__((ext_vector_type(4), aligned(4)));
+
+__device__ __forceinline__ i4 load16(const void *p)
 {
-    if (left >= 8) {
-        const Run<T, 8> r = *reinterpret_cast<const Run<T, 8> *>(p);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = to_float(r.v[i]);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = i < left ? to_float(p[i]) : 0.0f;
-    }
+    const any16 w = *reinterpret_cast<const any16 *>(p);
+    return i4{w[0], w[1], w[2], w[3]};
 }
+
+__device__ __forceinline__ int pack2(float a, float b, bf16)
+{
+    typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(int, b2{(__bf16)a, (__bf16)b});
+}
+__device__ __forceinline__ int pack2(float a, float b, _Float16)
+{
+    typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(int, h2{(_Float16)a, (_Float16)b});
+}
+
 // the same as they lie in memory
 template <typename T> __device__ __forceinline__ Run<T, 8> raw8(const T *p, int left)
 {
     Run<T, 8> r;
     if (left >= 8) {
-        r = *reinterpret_cast<const Run<T, 8> *>(p);
+        struct {
+            i4 v[sizeof(T) / 2];
+        } w;
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) w.v[i] = load16(p + i * (16 / sizeof(T)));
+        r = __builtin_bit_cast(Run<T, 8>, w);
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) r.v[i] = i < left ? p[i] : from_float<T>(0.0f);
     }
     return r;
 }
+// `left` of eight neighbours (0 for the others), and back
+template <typename T> __device__ __forceinline__ void load8(const T *p, int left, float v[8])
+{
+    const Run<T, 8> r = raw8(p, left);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = to_float(r.v[i]);
+}
 template <typename T> __device__ __forceinline__ void store8(T *p, int left, const float v[8])
 {
     if (left >= 8) {
-        Run<T, 8> r;
+        if constexpr (sizeof(T) == 4) {
+            any16f *q = reinterpret_cast<any16f *>(p);
+            q[0] = any16f{v[0], v[1], v[2], v[3]};
+            q[1] = any16f{v[4], v[5], v[6], v[7]};
+        } else {
+            any16 w;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) r.v[i] = from_float<T>(v[i]);
-        *reinterpret_cast<Run<T, 8> *>(p) = r;
+            for (int i = 0; i < 4; ++i) w[i] = pack2(v[2 * i], v[2 * i + 1], T());
+            *reinterpret_cast<any16 *>(p) = w;
+        }
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)

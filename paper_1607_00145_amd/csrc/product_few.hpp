@@ -22,7 +22,7 @@ template <typename T> struct Few {
     {
 #pragma unroll
         for (int s = 0; s < 4; ++s)
-            v[s] = __builtin_bit_cast(i4, *reinterpret_cast<const Run<T, EP> *>(row + k + s * EP));
+            v[s] = load16(row + k + s * EP);
     }
     // the same with zeros behind K
     static __device__ __forceinline__ void load_last(const T *row, int k, int extent, i4 v[4])
@@ -223,17 +223,18 @@ __global__ __launch_bounds__(64 * kRowWaves) void product_row_kernel(ProductArgs
     };
     auto some = [&](auto count, int k) {
         constexpr int N_ = decltype(count)::value;
-        Run<T, EP> w[N_][CPW], x[N_][R];
+        typedef Run<T, EP> V;
+        V w[N_][CPW], x[N_][R];
 #pragma unroll
         for (int u = 0; u < N_; ++u)
 #pragma unroll
             for (int c = 0; c < CPW; ++c)
-                w[u][c] = *reinterpret_cast<const Run<T, EP> *>(N[c] + k + u * STEP);
+                w[u][c] = *reinterpret_cast<const V *>(N[c] + k + u * STEP);
 #pragma unroll
         for (int u = 0; u < N_; ++u)
 #pragma unroll
             for (int r = 0; r < R; ++r)
-                x[u][r] = *reinterpret_cast<const Run<T, EP> *>(M[r] + k + u * STEP);
+                x[u][r] = *reinterpret_cast<const V *>(M[r] + k + u * STEP);
 #pragma unroll
         for (int u = 0; u < N_; ++u)
 #pragma unroll
