@@ -91,7 +91,7 @@ gett_status_t gett_experts(gett_dtype_t dtype, int64_t tokens, int k, int expert
     hipStream_t s = static_cast<hipStream_t>(stream);
     // rows that are gathered in the product are reached by 32-bit offsets
     const int64_t reach = tokens * stride_x * type_size(dtype);
-    const bool few = product_is_few(kByRows, rows);   // (at any address)
+    const bool few = product_is_few(dtype, kByRows, rows, n, width);   // (at any address)
     const bool gridX = few || (on_grid(dtype, gather ? tokens : rows, width, X, stride_x) &&
                                (!gather || reach < 0xffff0000ll));
     Arena arena;

@@ -73,7 +73,7 @@ gett_status_t gett_linear(gett_dtype_t dtype, int64_t m, int64_t n, int64_t k, c
     hipStream_t s = static_cast<hipStream_t>(stream);
     Arena arena;
     // (few rows are taken at any address)
-    const bool few = product_is_few(kWhole, m);
+    const bool few = product_is_few(dtype, kWhole, m, n, k);
     const bool gridX = few || on_grid(dtype, m, k, X, stride_x);
     const bool gridW = few || on_grid(dtype, n, k, W, stride_w);
     Operand ox = operand_of(dtype, m, k, X, stride_x, gridX, arena, m);

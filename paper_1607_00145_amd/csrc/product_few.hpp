@@ -13,7 +13,7 @@
 
 namespace gett {
 
-constexpr int kFewCols32 = 32;   // columns of C of a workgroup
+constexpr int kFewCols = 32, kFewWaves = 8;   // columns of C of a workgroup, its wavefronts
 
 template <typename T> struct Few {
     static constexpr int EP = 16 / sizeof(T), KP = 8 * EP;
@@ -38,16 +38,17 @@ template <typename T> struct Few {
     }
 };
 
-template <typename T, int FM, int NW>
-__global__ __launch_bounds__(64 * NW) void product_few_kernel(ProductArgs g, int groups)
+template <typename T>
+__global__ __launch_bounds__(64 * kFewWaves) void product_few_kernel(ProductArgs g, int groups)
 {
     typedef Few<T> F;
+    constexpr int NW = kFewWaves;
     constexpr int ROW = 36;   // floats of a row of partial results: whole vectors, few conflicts
-    __shared__ __attribute__((aligned(16))) float sums[NW][32 * FM][ROW];
+    __shared__ __attribute__((aligned(16))) float sums[NW][32][ROW];
     const int lane = (int)threadIdx.x & 63, q = lane & 31, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int slot = (int)quotient(blockIdx.x, g.tilesN, g.bandInv);
-    const int col0 = ((int)blockIdx.x - slot * g.tilesN) * kFewCols32;
+    const int col0 = ((int)blockIdx.x - slot * g.tilesN) * kFewCols;
     int begin = 0, end = g.m, e = 0;
     if (groups == kByRows) {
         // a workgroup for each row of the list; that of an expert's first row takes the
@@ -81,31 +82,23 @@ __global__ __launch_bounds__(64 * NW) void product_few_kernel(ProductArgs g, int
     // that together they ask all memory channels and not a few (one row of 4096 with
     // 8192 x 4096: 22.8 -> 19.6 us).
     const int turn = panels > 0 ? (int)(blockIdx.x * NW % (unsigned)panels) : 0;
-    for (int row0 = begin; row0 < end; row0 += 32 * FM) {
+    for (int row0 = begin; row0 < end; row0 += 32) {
         // rows that are not there are the last one again: not stored
-        const T *M[FM];
+        int64_t from = min(row0 + q, end - 1);
+        if (g.order && !empty)
+            from = quotient(min((uint32_t)g.order[from], (uint32_t)g.m - 1), g.choices, g.choicesInv);
+        const T *M = reinterpret_cast<const T *>(g.M + (empty ? 0 : from * g.ldm));
+        f16v acc;
 #pragma unroll
-        for (int i = 0; i < FM; ++i) {
-            int64_t from = min(row0 + 32 * i + q, end - 1);
-            if (g.order && !empty)
-                from = quotient(min((uint32_t)g.order[from], (uint32_t)g.m - 1), g.choices, g.choicesInv);
-            M[i] = reinterpret_cast<const T *>(g.M + (empty ? 0 : from * g.ldm));
-        }
-        f16v acc[FM];
+        for (int x = 0; x < 16; ++x) acc[x] = 0.0f;
+        auto multiply = [&](const i4 w[4], const i4 x[4]) {
 #pragma unroll
-        for (int i = 0; i < FM; ++i)
-#pragma unroll
-            for (int x = 0; x < 16; ++x) acc[i][x] = 0.0f;
-        auto multiply = [&](const i4 w[4], const i4 x[FM][4]) {
-#pragma unroll
-            for (int s = 0; s < 4; ++s)
-#pragma unroll
-                for (int i = 0; i < FM; ++i) acc[i] = product_mfma<T>(w[s], x[i][s], acc[i]);
+            for (int s = 0; s < 4; ++s) acc = product_mfma<T>(w[s], x[s], acc);
         };
         // U panels on their way
         auto some = [&](auto count, int t) {
             constexpr int U = decltype(count)::value;
-            i4 w[U][4], x[U][FM][4];
+            i4 w[U][4], x[U][4];
             int k[U];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
@@ -115,35 +108,30 @@ __global__ __launch_bounds__(64 * NW) void product_few_kernel(ProductArgs g, int
                 F::load(N, k[u], w[u]);
             }
 #pragma unroll
-            for (int u = 0; u < U; ++u)
-#pragma unroll
-                for (int i = 0; i < FM; ++i) F::load(M[i], k[u], x[u][i]);
+            for (int u = 0; u < U; ++u) F::load(M, k[u], x[u]);
 #pragma unroll
             for (int u = 0; u < U; ++u) multiply(w[u], x[u]);
         };
-        constexpr int U = FM == 1 ? 4 : 2;
+        constexpr int U = 4;
         int t = wave;
         for (; t + (U - 1) * NW < panels; t += U * NW) some(std::integral_constant<int, U>{}, t);
         for (; t < panels; t += NW) some(std::integral_constant<int, 1>{}, t);
         if (rest && wave == NW - 1) {
-            i4 w[4], x[FM][4];
+            i4 w[4], x[4];
             const int k = panels * F::KP + 4 * h * F::EP;
             F::load_last(N, k, g.k, w);
-#pragma unroll
-            for (int i = 0; i < FM; ++i) F::load_last(M[i], k, g.k, x[i]);
+            F::load_last(M, k, g.k, x);
             multiply(w, x);
         }
         __syncthreads();   // the rows before are read
+        if (row0 + q < end) {
 #pragma unroll
-        for (int i = 0; i < FM; ++i)
-            if (row0 + 32 * i + q < end) {
-#pragma unroll
-                for (int a = 0; a < 4; ++a)
-                    *reinterpret_cast<f4 *>(&sums[wave][32 * i + q][8 * a + 4 * h]) =
-                        f4{acc[i][4 * a], acc[i][4 * a + 1], acc[i][4 * a + 2], acc[i][4 * a + 3]};
-            }
+            for (int a = 0; a < 4; ++a)
+                *reinterpret_cast<f4 *>(&sums[wave][q][8 * a + 4 * h]) =
+                    f4{acc[4 * a], acc[4 * a + 1], acc[4 * a + 2], acc[4 * a + 3]};
+        }
         __syncthreads();
-        const int count = min(32 * FM, end - row0) * 4;   // runs of eight columns
+        const int count = min(32, end - row0) * 4;   // runs of eight columns
         if ((int)threadIdx.x < count) {
             const int r = (int)threadIdx.x >> 2, c = ((int)threadIdx.x & 3) * 8;
             float v[8] = {};
@@ -172,12 +160,12 @@ constexpr int kRowWaves = 16;
 template <typename T, int R>
 __global__ __launch_bounds__(64 * kRowWaves) void product_row_kernel(ProductArgs g, int groups)
 {
-    constexpr int EP = 16 / sizeof(T), STEP = 64 * EP, CPW = kFewCols32 / kRowWaves, U = R == 1 ? 8 : R == 2 ? 4 : 2;
-    __shared__ __attribute__((aligned(16))) float sums[R][kFewCols32];
+    constexpr int EP = 16 / sizeof(T), STEP = 64 * EP, CPW = kFewCols / kRowWaves, U = R == 1 ? 8 : R == 2 ? 4 : 2;
+    __shared__ __attribute__((aligned(16))) float sums[R][kFewCols];
     const int lane = (int)threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int slot = (int)quotient(blockIdx.x, g.tilesN, g.bandInv);
-    const int col0 = ((int)blockIdx.x - slot * g.tilesN) * kFewCols32;
+    const int col0 = ((int)blockIdx.x - slot * g.tilesN) * kFewCols;
     const int row0 = groups == kByRows ? slot : 0;
     int e = 0;
     Epilogue o = g.out;

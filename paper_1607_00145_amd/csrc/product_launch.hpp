@@ -70,7 +70,7 @@ template <typename T>
 gett_status_t product_few(ProductGroups groups, ProductArgs g, hipStream_t s)
 {
     const int m = g.m;
-    const int64_t tn = ((int64_t)g.n + kFewCols32 - 1) / kFewCols32;
+    const int64_t tn = ((int64_t)g.n + kFewCols - 1) / kFewCols;
     const int64_t blocks = tn * (groups == kByRows ? g.m : 1);
     if (!fits_launch(blocks, 1024)) return GETT_ERROR_NOT_SUPPORTED;
     g.tilesN = (int)tn;
@@ -84,8 +84,7 @@ gett_status_t product_few(ProductGroups groups, ProductArgs g, hipStream_t s)
     if (groups == kWhole && m == 1) return launch(product_row_kernel<T, 1>, 64 * kRowWaves);
     if (groups == kWhole && m == 2) return launch(product_row_kernel<T, 2>, 64 * kRowWaves);
     if (groups == kWhole && m <= 4) return launch(product_row_kernel<T, 4>, 64 * kRowWaves);
-    if (groups == kWhole && m > 32) return launch(product_few_kernel<T, 2, 8>, 512);
-    return launch(product_few_kernel<T, 1, 8>, 512);
+    return launch(product_few_kernel<T>, 64 * kFewWaves);
 }
 
 template <typename T, ProductForm FORM>

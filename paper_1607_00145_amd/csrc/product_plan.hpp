@@ -12,9 +12,7 @@ enum ProductGroups { kWhole, kByRows, kByK };
 constexpr int kFewRows = 3;   // product_few.hpp
 constexpr int64_t kProductCus = 256;
 
-// Whether rows x N^T is one of few rows: y = x w^T of up to 64 rows, or of so many
-// rows of experts in all.
-bool product_is_few(ProductGroups groups, int64_t m);
+bool product_is_few(gett_dtype_t dtype, ProductGroups groups, int64_t m, int64_t n, int64_t k);
 
 struct ProductPlan {
     int shape;                                  // tiles of 256 >> shape, or kFewRows

@@ -214,7 +214,8 @@ def product_tiles(dtype, m, n, k):
 
 @pytest.mark.parametrize("dtype,m,n,k,edge", [
     (BF16, 8192, 8192, 4096, 256), (BF16, 1024, 4096, 4096, 128), (BF16, 200, 4096, 4096, 64),
-    (BF16, 64, 4096, 4096, 0), (F32, 8192, 8192, 4096, 128), (F32, 65, 128, 64, 64)])
+    (BF16, 64, 4096, 4096, 64), (BF16, 32, 4096, 4096, 0), (BF16, 32, 512, 4096, 64),
+    (BF16, 4, 512, 4096, 0), (F32, 8192, 8192, 4096, 128), (F32, 65, 128, 64, 64)])
 def test_tiles_by_size(dtype, m, n, k, edge):
     assert product_tiles(dtype, m, n, k).edge == edge
 
