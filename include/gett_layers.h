@@ -119,13 +119,13 @@ gett_status_t gett_linear_grad(gett_dtype_t dtype, int64_t m, int64_t n, int64_t
  *     index   the k open experts of largest choice, largest first; never one of
  *             choice -inf
  *     weights s at these experts; divided by their sum where `renormalize` is not
- *             0; times `scale`
+ *             0 (0 where sigmoids sum to 0 in 64 bits); times `scale`
  *
  * What is compared is held in 64 bits (without a bias and groups the logits are
  * compared themselves); ties go to the lowest index.  Where fewer than k experts
  * are open the last indices are -1 and their weights 0: such a row belongs to no
- * expert.  A NaN counts as -inf in the choice, and one among the logits makes the token's weights NaN,
- * as does a +inf under a softmax.
+ * expert.  A NaN counts as -inf in the choice, and one among the logits makes the
+ * token's weights NaN, as does a +inf under a softmax.
  *
  *   logits   tokens x experts, of type dtype.
  *   bias     experts floats, or NULL.
@@ -136,8 +136,8 @@ gett_status_t gett_linear_grad(gett_dtype_t dtype, int64_t m, int64_t n, int64_t
  *   place    tokens x k int32: where `order` has the row (-1: nowhere).
  *
  * GETT_ERROR_NOT_SUPPORTED for more than 1024 experts, k > 32, or tokens * k of
- * 2^30 and more (of the other calls with tokens, too); GETT_ERROR_INVALID_VALUE where groups do not divide the experts or
- * top_groups of them hold fewer than k.
+ * 2^30 and more (of the other calls with tokens, too); GETT_ERROR_INVALID_VALUE
+ * where groups do not divide the experts or top_groups of them hold fewer than k.
  */
 #define GETT_SCORE_SOFTMAX 0
 #define GETT_SCORE_SIGMOID 1

@@ -93,8 +93,9 @@ __device__ __forceinline__ void choose_exactly(const RouteJob &j, int64_t token,
         }
         total = wave_sum(total);
     }
+    float top = most;
     auto score_of = [&](float x) {
-        return soft ? exp((double)x - (double)most) / total : 1.0 / (1.0 + exp(-(double)x));
+        return soft ? exp((double)x - (double)top) / total : 1.0 / (1.0 + exp(-(double)x));
     };
     for (int e = lane; e < j.experts; e += 64) {
         const float x = to_float(row[e]);
@@ -137,7 +138,9 @@ __device__ __forceinline__ void choose_exactly(const RouteJob &j, int64_t token,
         if ((best.at & 63) == lane) keys[best.at] = none;
         if (lane == r) mine = best.at;
     }
-    const double score = mine >= 0 ? score_of(to_float(row[mine])) : 0.0;
+    const float chosen = mine >= 0 ? to_float(row[mine]) : least;
+    if (soft && j.renormalize) top = wave_max(chosen);   // (as in choose_quickly)
+    const double score = mine >= 0 ? score_of(chosen) : 0.0;
     double w = score;
     if (j.renormalize) {
         const double sum = wave_sum(score);
@@ -318,6 +321,10 @@ __device__ __forceinline__ bool choose_quickly(const RouteJob &j, int64_t token)
             chosen = v;
         }
     }
+    // Of renormalised weights the scores' own sum is no matter: relative to the largest
+    // of the chosen they do not all vanish, as far below the token's largest as a bias
+    // or the groups may have them.  (Without these the two are the same.)
+    if (soft && j.renormalize && !plain) most = wave_max(mine >= 0 ? chosen : none);
     double score = 0.0;
     if (mine >= 0)
         score = soft ? exp((double)chosen - (double)most) / total : 1.0 / (1.0 + exp(-(double)chosen));

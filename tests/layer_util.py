@@ -148,6 +148,8 @@ def route(logits, k, scoring, bias=None, groups=1, top_groups=None, renormalize=
         pick = pick[key[pick] > -np.inf]
         index[i, :len(pick)] = pick
         w = s[pick]
+        if renormalize and len(pick) and scoring == "softmax" and v.max() < np.inf:
+            w = np.exp(v[pick] - v[pick].max())   # (the same ratios, which do not vanish)
         if renormalize and len(pick):
             w = w / w.sum() if w.sum() > 0 or np.isnan(w.sum()) else np.zeros_like(w)
         weights[i, :len(pick)] = w * scale

@@ -210,6 +210,27 @@ def test_route_gradient(gpu, dtype, t, e, k, scoring, biased, groups, kept, reno
     lu.close(dx, ref, err + lu.rounding(ref.abs() + err, dtype))
 
 
+@pytest.mark.parametrize("e,groups", [(8, 1), (8, 2), (9, 3), (1024, 1)])
+def test_route_far_below_the_largest(gpu, e, groups):
+    """The bias or the groups take experts whose scores vanish beside the token's largest:
+    renormalised weights and their gradient are still those of the chosen."""
+    logits = rand(3, 5, e)
+    logits[:, 0] += 2000.0
+    bias = torch.zeros(e)
+    bias[0], bias[e - 2:] = -10.0, 5.0
+    x = logits.to(gpu).requires_grad_()
+    r = g.route(x, 2, bias=bias.to(gpu), groups=groups, top_groups=1)
+    check_route(r, lu.route(logits, 2, "softmax", bias, groups, 1))
+    assert float((r.weights.detach().sum(1) - 1).abs().max()) <= 2 * lu.V
+    dw = rand(4, 5, 2)
+    dx, = torch.autograd.grad(r.weights, x, dw.to(gpu))
+    v = logits.double().requires_grad_()
+    w = torch.softmax(v.gather(1, r.index.cpu().long()), 1)
+    ref, = torch.autograd.grad(w, v, dw.double())
+    err = 4 * lu.V * ref.abs() + 1e-14 * dw.double().abs().sum(1, keepdim=True)
+    lu.close(dx, ref, err + lu.rounding(ref.abs() + err, torch.float32))
+
+
 def test_route_of_no_tokens(gpu):
     r = g.route(torch.empty(0, 8, device=gpu), 2)
     assert r.weights.shape == (0, 2) and r.order.numel() == 0
