@@ -90,7 +90,7 @@ gett_status_t gett_experts(gett_dtype_t dtype, int64_t tokens, int k, int expert
     if (!apart(y, z)) return GETT_ERROR_INVALID_VALUE;
     hipStream_t s = static_cast<hipStream_t>(stream);
     // rows that are gathered in the product are reached by 32-bit offsets
-    const int64_t reach = tokens * stride_x * type_size(dtype);
+    const int64_t reach = tokens > 1 ? tokens * stride_x * type_size(dtype) : 0;
     const bool few = product_is_few(dtype, kByRows, rows, n, width);   // (at any address)
     const bool gridX = few || (on_grid(dtype, gather ? tokens : rows, width, X, stride_x) &&
                                (!gather || reach < 0xffff0000ll));

@@ -487,7 +487,7 @@ __device__ __forceinline__ int expert_of_slot(const int32_t *offsets, int expert
         found += n;
         if (n < 64) break;
     }
-    return found - 1;   // expert 0's first is 0
+    return max(found - 1, 0);   // (expert 0's first is 0, or what lies before it is its own)
 }
 
 // A workgroup's tile: rows and columns of C, the expert, and its share of K.

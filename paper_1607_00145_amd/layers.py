@@ -516,6 +516,9 @@ class Routing:
     __slots__ = ("tokens", "experts", "k", "weights", "_lists")
 
     def __init__(self, tokens, experts, k, weights, lists):
+        if (lists.dtype is not _m._torch.int32 or not lists.is_contiguous()
+                or lists.numel() != 3 * tokens * k + experts + 1):
+            raise ValueError("a Routing is made by route")
         self.tokens, self.experts, self.k = tokens, experts, k
         self.weights, self._lists = weights, lists   # index, order, place, offsets
 

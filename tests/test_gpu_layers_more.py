@@ -210,6 +210,34 @@ def test_expert_strides(gpu, t):
     assert torch.equal(g.combine(h, r), g.combine(h.contiguous(), r))
 
 
+@pytest.mark.parametrize("t,dtype", [(5, torch.float32), (300, torch.float32), (300, torch.bfloat16)])
+def test_offsets_that_begin_late(gpu, t, dtype):
+    """Offsets of a caller's own that begin behind 0: the rows before the first expert's
+    have no meaning, and the others are those of their experts."""
+    e, d, n = 4, 24, 40
+    w, b = rand(1, e, n, d, dtype=dtype).cuda(), rand(2, e, n, dtype=dtype).cuda()
+    r = g.route(rand(3, t, e).cuda(), 1)
+    x = rand(4, t, d, dtype=dtype).cuda()
+    dy = rand(5, t, n, dtype=dtype).cuda()
+    late = min(int(r.offsets[1]), 3)
+    leaves = [v.clone().requires_grad_() for v in (x, w, b)]
+    want = g.expert_linear(leaves[0], leaves[1], r, leaves[2], activation="silu")
+    grads = torch.autograd.grad(want, leaves, dy)
+    r.offsets[0] = late
+    got = g.expert_linear(leaves[0], leaves[1], r, leaves[2], activation="silu")
+    back = torch.autograd.grad(got, leaves, dy)
+    assert torch.equal(got[late:], want[late:])
+    assert torch.equal(back[0][late:], grads[0][late:])
+    assert torch.equal(back[1][1:], grads[1][1:]) and torch.equal(back[2][1:], grads[2][1:])
+
+
+def test_a_routing_is_made_by_route(gpu):
+    r = g.route(rand(1, 6, 4).cuda(), 2)
+    for lists in (r._lists[:-1], r._lists.long(), torch.stack((r._lists, r._lists), 1)[:, 0]):
+        with pytest.raises(ValueError, match="made by route"):
+            g.Routing(6, 4, 2, r.weights, lists)
+
+
 def test_route_of_equal_rows_is_stable(gpu):
     t, e, k = 2000, 16, 4
     r = g.route(torch.zeros(t, e, device="cuda"), k)
