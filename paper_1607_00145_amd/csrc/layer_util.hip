@@ -48,7 +48,7 @@ __global__ __launch_bounds__(256) void layer_copy_kernel(CopyJob j)
 constexpr int kSlopeCols = 256;  // columns of a workgroup: 32 lanes of eight
 
 // Rows of a workgroup: as many as leave four workgroups a CU, between 8 and 64 (1023 x
-// 515 in 32 bits, of 64 rows each 25 us, of 8 rows 5).
+// 515 in 32 bits, of 64 rows each 25 us, of 8 rows 5.5).
 int slope_log2(int64_t m, int64_t n)
 {
     const int64_t across = (n + kSlopeCols - 1) / kSlopeCols;
@@ -72,6 +72,7 @@ __device__ __forceinline__ void slope_slots_of(const SlopeJob &j, int e, int &fi
 // dz = dropout(dy) act'(z), written with zeros behind the last column, and the sums
 // of each column over the workgroup's rows: eight rows at a time, two loads each on
 // their way, the eight partial sums of a column added in the same order each time.
+// Bound by memory: 8192 x 8192 in bf16 with GELU and dropout 87 us (403 MB: 4.6 TB/s).
 template <typename T>
 __global__ __launch_bounds__(256) void layer_slope_kernel(SlopeJob j)
 {
@@ -167,7 +168,8 @@ __global__ __launch_bounds__(256) void layer_sums_kernel(SlopeJob j, T *out)
 // ------------------------------------------------------------------ combine ---
 
 // Y[t] = residual[t] + sum_j weights[t, j] H[place[t, j]], eight columns a lane, in
-// rising j.  H in T or, for sums of gradients, in 32 bits.
+// rising j.  H in T or, for sums of gradients, in 32 bits.  Bound by memory: 8192 x 4
+// rows of 2048 in bf16 32 us (168 MB: 5.2 TB/s), in 32 bits 65 (302 MB: 4.7 TB/s).
 template <typename T, typename H, typename W>
 __global__ __launch_bounds__(256) void combine_kernel(CombineJob j)
 {
@@ -203,8 +205,8 @@ __global__ __launch_bounds__(256) void combine_kernel(CombineJob j)
 }
 
 // A workgroup for a token t: dH[place] = w dY[t] and dw = dY[t] . H[place] for its
-// choices, four rows on their way (a wavefront for each row, and dY[t] read by each:
-// 92 us for 8192 x 4 rows of 2048 in bf16).  The rows of dH with the token's own
+// choices, four rows on their way (8192 x 4 rows of 2048 in bf16: 65 us, 302 MB at
+// 4.6 TB/s; with a wavefront for each row, dY[t] read by each, 92 where this had 84).  The rows of dH with the token's own
 // numbers are set to zero where they are no expert's.
 template <typename T, typename W>
 __global__ __launch_bounds__(256) void combine_grad_kernel(CombineGradJob j)

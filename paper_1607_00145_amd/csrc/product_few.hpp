@@ -1,12 +1,13 @@
 // product_few.hpp -- products of few rows (device code), for single tokens and small
-// batches: C[i, j] = sum over K of M(i, k) N(j, k) with up to 64 rows i, or of every
-// expert's rows where there are few in all.
+// batches: C[i, j] = sum over K of M(i, k) N(j, k) with up to 32 rows i, or of every
+// expert's rows where there are up to 64 in all.
 //
 // Bound by N's bytes, and where these are few by the launch and two memory
 // latencies.  A workgroup takes 32 rows of N (columns of C) and its eight wavefronts
 // every eighth panel of 128 bytes of K; N goes from memory straight into the
 // registers that the MFMA reads, 64 bytes of one row a lane, so that no byte waits for
 // a barrier, and the eight partial results are summed in wavefront order through LDS.
+// 5 to 32 rows with 8192 x 4096 in bf16 take 18 to 22 us (67 MB: 3.1 to 3.7 TB/s).
 // Rows may lie at any element address: nothing is copied first.
 #pragma once
 #include "product.hpp"
@@ -154,7 +155,9 @@ __global__ __launch_bounds__(64 * kFewWaves) void product_few_kernel(ProductArgs
 // of whose 32 rows it would fill one.  A wavefront takes two rows of N whole, 1 KB of one
 // after the other, so that every load is a run of whole lines; its lanes multiply
 // their 16 bytes with x's, and sum up across the wavefront at the end.  The sixteen
-// wavefronts of a workgroup have up to 128 KB on their way.
+// wavefronts of a workgroup have up to 128 KB on their way.  Bound by the weights' bytes:
+// one bf16 row with 8192 x 4096 takes 14 us (4.8 TB/s; 20 us in the kernel above),
+// eight experts of 1024 x 2048 for a token 9 (33 MB, and the launch).
 constexpr int kRowWaves = 16;
 
 template <typename T, int R>

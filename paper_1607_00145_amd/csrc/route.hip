@@ -5,7 +5,10 @@
 // in 64 bits, as whole numbers of the same order whose halves go through the
 // wavefront one after the other (DPP: no trip through LDS).  (Choosing in 32 bits, and
 // again in 64 where a bound of the error does not decide, was no faster: one token in
-// a hundred is enough for every workgroup to wait for one.)
+// a hundred is enough for every workgroup to wait for one.)  16384 tokens of 256
+// experts in 8 groups take 41 us, bound by instructions: four sigmoids a lane in 64 bits
+// and twelve picks one after the other; the bytes (17 MB) would take 3.4.  A single
+// token takes 5.5 us, all latency.
 //
 // The order of the rows by expert is a stable counting sort: chunks of whole tokens,
 // up to 512 rows, are chosen and counted in one launch, the counts summed over the

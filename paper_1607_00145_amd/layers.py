@@ -397,7 +397,7 @@ def _dropout(x, drop, seed):
 def dropout(x, p: float, seed, offset: int = 0):
     """x / (1 - p) where a counter-based generator keeps it and 0 elsewhere.
 
-    `p` is rounded to a multiple of 2^-16.  The mask is a function of `seed`, `offset`
+    With p = 0 it is x itself.  `p` is rounded to a multiple of 2^-16.  The mask is a function of `seed`, `offset`
     and a number's row (over all leading dimensions) and column: a call with the same
     seed and offset has the same mask, and the gradient makes it again.  `seed` is an
     integer, or an int64 device tensor of one element that is read when the kernel
@@ -408,7 +408,9 @@ def dropout(x, p: float, seed, offset: int = 0):
     flat = _flat("x", x)
     _m._code(x.dtype)
     _m._device("x", x)
-    drop = _drop(p, seed, offset) or (0.0, 0, 0, None)
+    drop = _drop(p, seed, offset)
+    if drop is None:
+        return x
     if _records(x):
         y = _function("dropout").apply(flat, drop[3], drop)
     else:

@@ -70,6 +70,18 @@ def test_dropout_strides_and_in_place(gpu):
     assert torch.equal(base[:, :3], rand(3, 50, 131)[:, :3].to(gpu))
 
 
+def test_no_dropout(gpu):
+    """p = 0 is x itself; the C call copies."""
+    x = rand(3, 50, 131).to(gpu).requires_grad_()
+    assert g.dropout(x, 0.0, None) is x
+    with pytest.raises(ValueError):
+        g.dropout(x.detach().cpu(), 0.0, None)
+    y, d = torch.empty_like(x), g.gett_dropout_t(0.0, 0, 0, None)
+    st = g.gett_dropout(g.GETT_FLOAT32, 50, 131, x.data_ptr(), 131, d, y.data_ptr(), 131,
+                        torch.cuda.current_stream().cuda_stream)
+    assert st == 0 and torch.equal(x, y)
+
+
 def test_dropout_seed_on_the_device(gpu):
     x = rand(4, 20, 40).to(gpu)
     seed = torch.tensor([-5], dtype=torch.int64, device=gpu)
