@@ -24,7 +24,10 @@
  * Calls enqueue work on `stream` and return; errors are statuses; workspaces are
  * the library's own, one per device and stream, as gett_matrix.h describes: a
  * call that needs more than the stream's holds allocates, which is refused with
- * GETT_ERROR_NOT_SUPPORTED while the stream captures a graph.  Repeated calls
+ * GETT_ERROR_NOT_SUPPORTED while the stream captures a graph.  They hold the copies
+ * above, dZ of a gradient (unless it is dY itself), the rows of the experts' X and
+ * dX where these are gathered, 4 bytes for each 8 to 64 numbers whose columns are
+ * summed, and up to 64 MB for a product whose sums several workgroups share.  Repeated calls
  * give identical results.  Outputs must not overlap inputs or one another except
  * where it is said.
  *
@@ -45,7 +48,9 @@
 extern "C" {
 #endif
 
-/* Activations: z; max(z, 0); z (1 + erf(z / sqrt 2)) / 2; z / (1 + e^-z). */
+/* Activations: z; max(z, 0); z (1 + erf(z / sqrt 2)) / 2; z / (1 + e^-z).  Values are
+ * within 2^-20 (1 + |z|) |z|, slopes within 2^-20 (1 + |z|); of infinities they are the
+ * limits, of NaN NaN. */
 #define GETT_ACTIVATION_NONE 0
 #define GETT_ACTIVATION_RELU 1
 #define GETT_ACTIVATION_GELU 2

@@ -130,6 +130,10 @@ __device__ __forceinline__ float normal_tail(float z, float &e)
     return t * (0.127414796f + t * (-0.142248368f + t * (0.7107068705f +
                t * (-0.7265760135f + t * 0.5307027145f)))) * e;
 }
+// z, or the number next to an infinity: times 0 it is 0, as the limits are (z of 16 bits
+// is infinite beyond 65504 and its slope 0 or 1).  What NaN becomes does not matter:
+// the other factor is one.
+__device__ __forceinline__ float finite(float z) { return fmaxf(fminf(z, 3e38f), -3e38f); }
 __device__ __forceinline__ float gelu(float z)
 {
     // z cdf(z), as max(z, 0) less |z| times the tail; |z| finite: of infinity it is 0
@@ -142,13 +146,16 @@ __device__ __forceinline__ float gelu_slope(float z)
 {
     float e;
     const float tail = normal_tail(z, e);
-    return (z < 0.0f ? tail : 1.0f - tail) + z * 0.39894228f * e;
+    return (z < 0.0f ? tail : 1.0f - tail) + finite(z) * 0.39894228f * e;
 }
-__device__ __forceinline__ float silu(float z) { return z * __builtin_amdgcn_rcpf(1.0f + quick_exp(-z)); }
+__device__ __forceinline__ float silu(float z)
+{
+    return fmaxf(z, -3e38f) * __builtin_amdgcn_rcpf(1.0f + quick_exp(-z));
+}
 __device__ __forceinline__ float silu_slope(float z)
 {
     const float s = __builtin_amdgcn_rcpf(1.0f + quick_exp(-z));
-    return s * (1.0f + z * (1.0f - s));
+    return s * (1.0f + finite(z) * (1.0f - s));
 }
 __device__ __forceinline__ float relu(float z) { return z < 0.0f ? 0.0f : z; }
 __device__ __forceinline__ float relu_slope(float z) { return z > 0.0f ? 1.0f : z != z ? z : 0.0f; }
