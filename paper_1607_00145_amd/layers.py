@@ -324,13 +324,12 @@ def _make_functions():
     class Route(torch.autograd.Function):
         @staticmethod
         def forward(ctx, logits, how, lists):
-            ctx.how, ctx.lists = how, lists
-            ctx.save_for_backward(logits)
+            ctx.how = how
+            ctx.save_for_backward(logits, lists)
             return _route(logits, how, lists)
 
         def gradients(ctx, dweights):
-            logits, = ctx.saved_tensors
-            return _route_grad(logits, ctx.lists, dweights, ctx.how), None, None
+            return _route_grad(*ctx.saved_tensors, dweights, ctx.how), None, None
 
         backward = once(gradients)
 
@@ -343,13 +342,12 @@ def _make_functions():
                 z = x.new_empty((routing.tokens * routing.k, w.shape[1]))
             y = _experts(x, w, bias, routing, activation, gather, z)
             ctx.how = routing.tokens, routing.k, activation, gather, x.shape, w.shape
-            ctx.lists = routing._lists
-            ctx.save_for_backward(x if need_w else None, w if need_x else None, z)
+            ctx.save_for_backward(x if need_w else None, w if need_x else None, z, routing._lists)
             return y
 
         def gradients(ctx, dy):
-            return (*_experts_grad(dy, *ctx.saved_tensors, ctx.lists, ctx.how,
-                                   *ctx.needs_input_grad[:3]), None, None, None)
+            return (*_experts_grad(dy, *ctx.saved_tensors, ctx.how, *ctx.needs_input_grad[:3]),
+                    None, None, None)
 
         backward = once(gradients)
 
@@ -358,15 +356,15 @@ def _make_functions():
         def forward(ctx, h, weights, residual, routing):
             need_h, need_w = ctx.needs_input_grad[:2]
             ctx.how = routing.tokens, routing.k, routing.experts, h.shape, weights.dtype
-            ctx.lists = routing._lists
-            ctx.save_for_backward(h if need_w else None, weights if need_h else None)
+            ctx.save_for_backward(h if need_w else None, weights if need_h else None,
+                                  routing._lists)
             return _combine(h, weights, residual, routing)
 
         def gradients(ctx, dy):
             need_h, need_w, need_r = ctx.needs_input_grad[:3]
             dh = dw = None
             if need_h or need_w:
-                dh, dw = _combine_grad(dy, *ctx.saved_tensors, ctx.lists, ctx.how, need_h, need_w)
+                dh, dw = _combine_grad(dy, *ctx.saved_tensors, ctx.how, need_h, need_w)
             return dh, dw, dy if need_r else None, None
 
         backward = once(gradients)
@@ -513,7 +511,7 @@ class Routing:
     ``order`` lists the rows token * k + choice expert after expert (-1 behind the
     last), ``offsets`` says where each expert's begin, ``place`` is where `order`
     has each row (-1: nowhere).  The lists are parts of one tensor, not to be
-    written into."""
+    written into (a backward pass raises where they were)."""
 
     __slots__ = ("tokens", "experts", "k", "weights", "_lists")
 

@@ -2,6 +2,7 @@
 tile, shared sums, odd strides and addresses, uneven experts, repeated calls, streams,
 graphs, large offsets, refusals."""
 import math
+import threading
 
 import pytest
 import torch
@@ -246,6 +247,29 @@ def test_route_of_equal_rows_is_stable(gpu):
     assert torch.equal(r.order, rows.t().reshape(-1))
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("m", [3, 20, 150])
+@pytest.mark.parametrize("name", ["relu", "gelu", "silu"])
+def test_activations_of_the_largest_numbers(gpu, dtype, m, name):
+    """Infinities, numbers whose type's z is one, and NaN: values and slopes are the limits."""
+    inf, big = math.inf, torch.finfo(dtype).max
+    z = torch.tensor([inf, -inf, big, -big, math.nan, 1e4, -1e4])[torch.arange(m) % 7]
+    want = torch.where(z > 0, z, torch.zeros(())).to(dtype)
+    slope = (z > 0).to(dtype)
+    want[z.isnan()] = slope[z.isnan()] = math.nan
+    for scale in (1.0, 2.0):                # (of 2 the largest numbers' z is infinite)
+        x = z.to(dtype).cuda()[:, None].requires_grad_()
+        w = torch.full((9, 1), scale, dtype=dtype, device="cuda")
+        y = g.linear(x, w, activation=name)
+        dx, = torch.autograd.grad(y, x, torch.ones_like(y))
+        assert torch.equal(y.isnan().cpu(), want.isnan()[:, None].expand(m, 9))
+        there = ~want.isnan()
+        assert torch.equal(y.cpu()[there], (scale * want)[there, None].expand(-1, 9))
+        assert torch.equal(dx.isnan().cpu()[:, 0], want.isnan())
+        # (bf16 and fp16 hold 18; 1 and 0 are exact)
+        assert torch.equal(dx.cpu()[there, 0], (9 * scale * slope)[there])
+
+
 # calls -----------------------------------------------------------------------
 
 def layer(x, router, w1, w2, wo, seed):
@@ -322,6 +346,59 @@ def test_graph_of_a_training_step(gpu):
         assert all(torch.equal(a, b) for a, b in zip(got, want)), i
         seen.append(got[0])
     assert not torch.equal(seen[0], seen[1])
+
+
+def test_graphs_that_share_a_workspace(gpu):
+    """Two graphs of different sizes on one stream, replayed in turn with eager calls
+    between them."""
+    stream = torch.cuda.Stream()
+    jobs = [layer_inputs(i, t=t) for i, t in ((1, 70), (20, 700))]
+    graphs, out = [], []
+    with torch.cuda.stream(stream):
+        want = [layer(*v, 3) for v in reversed(jobs)][::-1]
+    torch.cuda.synchronize()
+    for v in jobs:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1], stream=stream):
+            out.append(layer(*v, 3))
+    with torch.cuda.stream(stream):
+        for _ in range(3):
+            for i in (0, 1, 1, 0):
+                out[i].zero_()
+                graphs[i].replay()
+                layer(*jobs[1 - i], 3)
+                stream.synchronize()
+                assert torch.equal(out[i], want[i]), i
+
+
+def test_threads_on_one_stream(gpu):
+    """The launches of one call are enqueued together, whoever else calls."""
+    jobs = [layer_inputs(i, t=t, d=61) for i, t in ((1, 160), (20, 700))]
+    want = [layer(*v, 3) for v in jobs]
+    got = [[], []]
+
+    def work(i):
+        for _ in range(10):
+            got[i].append(layer(*jobs[i], 3))
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert len(got[i]) == 10 and all(torch.equal(v, want[i]) for v in got[i])
+
+
+def test_a_routing_that_was_written_into_is_seen(gpu):
+    x, w = rand(1, 6, 16).cuda().requires_grad_(), rand(2, 4, 8, 16).cuda()
+    r = g.route(rand(3, 6, 4).cuda().requires_grad_(), 2)
+    h = g.expert_linear(x, w, r, gather=True)
+    for y in (h, g.combine(h.detach(), r), r.weights):
+        r.offsets[0] = 0
+        with pytest.raises(RuntimeError, match="modified by an inplace"):
+            y.sum().backward(retain_graph=True)
 
 
 def test_capture_that_would_need_memory_is_refused(gpu):
