@@ -93,7 +93,10 @@ gett_status_t gett_experts(gett_dtype_t dtype, int64_t tokens, int k, int expert
     hipStream_t s = static_cast<hipStream_t>(stream);
     // rows that are gathered in the product are reached by 32-bit offsets
     const int64_t reach = tokens > 1 ? tokens * stride_x * type_size(dtype) : 0;
-    const bool few = product_is_few(dtype, kByRows, rows, n, width);   // (at any address)
+    // few rows are taken at any address
+    const bool direct = on_grid(dtype, n, width, W, stride_w) &&
+                        (experts == 1 || stride_we * type_size(dtype) % 16 == 0);
+    const bool few = product_is_few(dtype, kByRows, rows, n, experts, direct);
     const bool gridX = few || (on_grid(dtype, gather ? tokens : rows, width, X, stride_x) &&
                                (!gather || reach < 0xffff0000ll));
     Arena arena;
@@ -123,7 +126,7 @@ gett_status_t gett_experts(gett_dtype_t dtype, int64_t tokens, int k, int expert
              stride_z, stride_y, activation, 0, {}};
     ProductPlan plan = {};
     if (few) plan.shape = kFewRows;
-    else plan = product_plan(dtype, kByRows, rows, n, width, experts);
+    else plan = product_plan(dtype, kRowsRows, kByRows, rows, n, width, experts);
     return product_launch_of(dtype, kRowsRows, kByRows, g, plan, hold, 0, s);
 }
 
@@ -182,8 +185,7 @@ gett_status_t gett_experts_grad(gett_dtype_t dtype, int64_t tokens, int k, int e
     both.wantW = ew.bytes;
     both.groupsX = kByRows;
     both.groupsW = kByK;
-    if (both.wantX) both.px = product_plan(dtype, kByRows, rows, width, n, experts);
-    if (both.wantW) both.pw = product_plan(dtype, kByK, n, width, rows, experts);
+    both.plan(dtype, rows, n, width, experts);
     Partials hold;
     if (arena.bytes) {
         st = stream_workspace(s, 0, arena.bytes, hold);

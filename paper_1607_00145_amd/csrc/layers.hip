@@ -75,14 +75,13 @@ gett_status_t gett_linear(gett_dtype_t dtype, int64_t m, int64_t n, int64_t k, c
     hipStream_t s = static_cast<hipStream_t>(stream);
     Arena arena;
     // (few rows are taken at any address)
-    const bool few = product_is_few(dtype, kWhole, m, n, k);
-    const bool gridX = few || on_grid(dtype, m, k, X, stride_x);
-    const bool gridW = few || on_grid(dtype, n, k, W, stride_w);
+    const bool direct = on_grid(dtype, n, k, W, stride_w), few = product_is_few(dtype, kWhole, m, n, 0, direct);
+    const bool gridX = few || on_grid(dtype, m, k, X, stride_x), gridW = few || direct;
     Operand ox = operand_of(dtype, m, k, X, stride_x, gridX, arena, m);
     Operand ow = operand_of(dtype, n, k, W, stride_w, gridW, arena, n);
     ProductPlan plan = {};
     if (few) plan.shape = kFewRows;
-    else plan = product_plan(dtype, kWhole, m, n, k, 0);
+    else plan = product_plan(dtype, kRowsRows, kWhole, m, n, k, 0);
     const int64_t slots = arena.take(plan.slotBytes);
     Partials hold;
     if (arena.bytes) {
@@ -142,8 +141,7 @@ gett_status_t gett_linear_grad(gett_dtype_t dtype, int64_t m, int64_t n, int64_t
     BackwardProducts both;
     both.wantX = ex.bytes;
     both.wantW = ew.bytes;
-    if (both.wantX) both.px = product_plan(dtype, kWhole, m, k, n, 0);
-    if (both.wantW) both.pw = product_plan(dtype, kWhole, n, k, m, 0);
+    both.plan(dtype, m, n, k, 0);
     const int64_t slots = arena.take(both.slotBytes());
     Partials hold;
     if (arena.bytes) {

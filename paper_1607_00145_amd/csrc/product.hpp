@@ -91,6 +91,7 @@ template <int FM_, int FN_, int WM_, int WN_, int NS_> struct ProductShape {
     static constexpr int FM = FM_, FN = FN_, WM = WM_, WN = WN_, NS = NS_;
     static constexpr int BM = 32 * FM * WM, BN = 32 * FN * WN;
     static constexpr int NW = WM * WN, THREADS = 64 * NW;
+    static constexpr bool SLABS = false;
     static constexpr int STAGE = (BM + BN) * 128;
     static constexpr int JA = BM / 8 / NW, JB = BN / 8 / NW, J = JA + JB;   // loads a lane
     static constexpr int W = 32 * FN;                   // columns of a wavefront
@@ -99,6 +100,16 @@ template <int FM_, int FN_, int WM_, int WN_, int NS_> struct ProductShape {
     static_assert((FM & (FM - 1)) == 0 && (FN & (FN - 1)) == 0, "addresses by exclusive or");
     static_assert(JA * 8 * NW == BM && JB * 8 * NW == BN, "whole instructions");
     static_assert((NS - 1) * J < 64, "vmcnt");
+};
+
+// One block of 32 x 32 for four wavefronts, each of which takes one slab of every panel.
+template <int NS_> struct ProductSlabs {
+    static constexpr int FM = 1, FN = 1, NS = NS_, BM = 32, BN = 32, NW = 4, THREADS = 256;
+    static constexpr bool SLABS = true;
+    static constexpr int STAGE = (BM + BN) * 128, JA = 1, JB = 1, J = 2;
+    static constexpr int ROW = 36;   // floats of a row of partial sums: whole vectors, few conflicts
+    static constexpr int LDS = NS * STAGE;
+    static_assert(LDS >= 4 * 32 * ROW * 4, "the partial sums come where the stages were");
 };
 
 constexpr uint32_t kNowhere = 0xfffffff0u;   // behind every buffer: such a load gives zeros
@@ -151,7 +162,7 @@ template <typename T, bool MCOL, bool NCOL, typename S> struct Product {
     static constexpr int EP = 16 / sizeof(T);      // numbers of a piece
     static constexpr int KP = 8 * EP;              // of a panel
     f16v acc[FM][FN];
-    int q, h, wm, wn;
+    int q, h, wm, wn;       // wm, wn: the wavefront's part of the tile (of slabs: 0, its slab)
 
     __device__ __forceinline__ void locate()
     {
@@ -159,8 +170,13 @@ template <typename T, bool MCOL, bool NCOL, typename S> struct Product {
         const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
         q = tid & 31;
         h = (tid >> 5) & 1;
-        wm = wave / S::WN;
-        wn = wave % S::WN;
+        if constexpr (S::SLABS) {
+            wm = 0;
+            wn = wave;
+        } else {
+            wm = wave / S::WN;
+            wn = wave % S::WN;
+        }
     }
     __device__ __forceinline__ void clear()
     {
@@ -287,10 +303,13 @@ template <typename T, bool MCOL, bool NCOL, typename S> struct Product {
                 return 16 * h * B * 4 + (first + q) * 4;
             }
         };
-        const int ownM = own(std::bool_constant<MCOL>{}, std::integral_constant<int, S::BM>{},
-                             wm * 32 * FM);
-        const int ownN = S::BM * 128 + own(std::bool_constant<NCOL>{},
-                                           std::integral_constant<int, S::BN>{}, wn * 32 * FN);
+        int ownM = own(std::bool_constant<MCOL>{}, std::integral_constant<int, S::BM>{}, wm * 32 * FM);
+        int ownN = S::BM * 128 + own(std::bool_constant<NCOL>{}, std::integral_constant<int, S::BN>{},
+                                     S::SLABS ? 0 : wn * 32 * FN);
+        if constexpr (S::SLABS) {   // (columns: four k of 32 bits, eight of 16)
+            ownM = MCOL ? ownM + wn * S::BM * 16 : ownM ^ wn * 16;
+            ownN = NCOL ? ownN + wn * S::BN * 16 : ownN ^ wn * 16;
+        }
         int atM = ownM, atN = ownN;
         auto at_stage = [&](int stage) {
             atM = ownM + stage * S::STAGE;
@@ -307,7 +326,7 @@ template <typename T, bool MCOL, bool NCOL, typename S> struct Product {
         // Slabs read together.  One block of 32 x 32 a wavefront has too few MFMAs in a
         // slab to cover the reads of the next: it reads whole panels where it is alone on
         // its CU.
-        constexpr int G = FM * FN == 1 && NS == 8 ? 4 : 1, STEPS = 4 / G;
+        constexpr int G = FM * FN == 1 && NS == 8 && !S::SLABS ? 4 : 1, STEPS = S::SLABS ? 1 : 4 / G;
         i4 a[2][G][FM], b[2][G][FN];
         auto fragment = [&](auto column, auto size, int own, int s, int i) {
             constexpr int B = decltype(size)::value;
@@ -608,59 +627,86 @@ __device__ __forceinline__ bool product_join(Product<T, MCOL, NCOL, S> &p, const
     return true;
 }
 
+// Sends the loads of a tile's first panels.
+template <typename T, ProductForm FORM, typename S>
+__device__ __forceinline__ void product_begin(Product<T, FORM == kColumnsColumns, FORM != kRowsRows, S> &p,
+                                              const ProductArgs &g, int groups, const TileAt &t,
+                                              char *dyn_lds)
+{
+    constexpr bool MCOL = FORM == kColumnsColumns, NCOL = FORM != kRowsRows;
+    constexpr int KP = 128 / (int)sizeof(T);
+    const bool gathered = FORM == kRowsRows && g.order;
+    Side M, N;
+    M.ld = g.ldm;
+    N.ld = g.ldn;
+    N.p = g.N + (groups == kByRows ? (int64_t)t.e * g.stepN : 0);
+    if constexpr (MCOL) {
+        M.p = g.M + (int64_t)t.first * g.ldm + (int64_t)t.row0 * sizeof(T);
+        M.count = g.fullM - t.row0;
+        M.extent = t.sum;
+    } else {
+        M.p = g.M + (gathered ? 0 : (int64_t)t.row0 * g.ldm);
+        M.count = t.rows - t.row0;
+        M.extent = g.kM;
+    }
+    if constexpr (NCOL) {
+        N.p += (int64_t)t.first * g.ldn + (int64_t)t.col0 * sizeof(T);
+        N.count = g.fullN - t.col0;
+        N.extent = t.sum;
+    } else {
+        N.p += (int64_t)t.col0 * g.ldn;
+        N.count = g.n - t.col0;
+        N.extent = g.kN;
+    }
+    const int32_t *order = g.order + (gathered ? t.row0 : 0);
+    auto rowM = [&](int r) {
+        if (FORM == kRowsRows && gathered) {
+            const uint32_t id = min((uint32_t)order[r], (uint32_t)g.m - 1);
+            r = (int)quotient(id, g.choices, g.choicesInv);
+        }
+        return (uint32_t)(r * g.ldm);
+    };
+    int panels = t.empty ? 0 : (t.sum + KP - 1) / KP;
+    if (t.shared >= 0) {
+        const int t0 = (int)quotient((uint32_t)(panels * t.slice), g.slices, g.slicesInv);
+        panels = (int)quotient((uint32_t)(panels * (t.slice + 1)), g.slices, g.slicesInv) - t0;
+        M.p += t0 * (MCOL ? KP * M.ld : 128);
+        N.p += t0 * (NCOL ? KP * N.ld : 128);
+        M.extent -= t0 * KP;
+        N.extent -= t0 * KP;
+    }
+    p.begin(dyn_lds, M, N, rowM, panels);
+}
+
+// A tile's epilogue.
+template <typename T, ProductForm FORM>
+__device__ __forceinline__ Epilogue product_epilogue(const ProductArgs &g, int groups, const TileAt &t)
+{
+    Epilogue o = g.out;
+    if constexpr (FORM != kRowsRows) {   // gradients are the sums themselves
+        o.bias = o.residual = nullptr;
+        o.Z = nullptr;
+        o.activation = GETT_ACTIVATION_NONE;
+        o.drop.cut = 0;
+    }
+    if (groups == kByRows && o.bias) o.bias += (int64_t)t.e * g.n * sizeof(T);
+    if (groups == kByK) o.Y += (int64_t)t.e * g.stepN * (o.wide ? 4 : sizeof(T));
+    if (t.empty) {
+        o.bias = nullptr;
+        o.activation = GETT_ACTIVATION_NONE;
+    }
+    return o;
+}
+
 // Workgroups take tile after tile.  A tile's loads begin before the results of the
 // one before are written: its first panels arrive while those leave.
 template <typename T, ProductForm FORM, typename S>
 __device__ __forceinline__ void product_work(const ProductArgs &g, int groups, int id, int stride,
                                              char *dyn_lds)
 {
-    constexpr bool MCOL = FORM == kColumnsColumns, NCOL = FORM != kRowsRows;
-    constexpr int KP = 128 / (int)sizeof(T);
-    Product<T, MCOL, NCOL, S> p;
+    Product<T, FORM == kColumnsColumns, FORM != kRowsRows, S> p;
     p.locate();
-    auto begin = [&](const TileAt &t) {
-        const bool gathered = FORM == kRowsRows && g.order;
-        Side M, N;
-        M.ld = g.ldm;
-        N.ld = g.ldn;
-        N.p = g.N + (groups == kByRows ? (int64_t)t.e * g.stepN : 0);
-        if constexpr (MCOL) {
-            M.p = g.M + (int64_t)t.first * g.ldm + (int64_t)t.row0 * sizeof(T);
-            M.count = g.fullM - t.row0;
-            M.extent = t.sum;
-        } else {
-            M.p = g.M + (gathered ? 0 : (int64_t)t.row0 * g.ldm);
-            M.count = t.rows - t.row0;
-            M.extent = g.kM;
-        }
-        if constexpr (NCOL) {
-            N.p += (int64_t)t.first * g.ldn + (int64_t)t.col0 * sizeof(T);
-            N.count = g.fullN - t.col0;
-            N.extent = t.sum;
-        } else {
-            N.p += (int64_t)t.col0 * g.ldn;
-            N.count = g.n - t.col0;
-            N.extent = g.kN;
-        }
-        const int32_t *order = g.order + (gathered ? t.row0 : 0);
-        auto rowM = [&](int r) {
-            if (FORM == kRowsRows && gathered) {
-                const uint32_t id = min((uint32_t)order[r], (uint32_t)g.m - 1);
-                r = (int)quotient(id, g.choices, g.choicesInv);
-            }
-            return (uint32_t)(r * g.ldm);
-        };
-        int panels = t.empty ? 0 : (t.sum + KP - 1) / KP;
-        if (t.shared >= 0) {
-            const int t0 = (int)quotient((uint32_t)(panels * t.slice), g.slices, g.slicesInv);
-            panels = (int)quotient((uint32_t)(panels * (t.slice + 1)), g.slices, g.slicesInv) - t0;
-            M.p += t0 * (MCOL ? KP * M.ld : 128);
-            N.p += t0 * (NCOL ? KP * N.ld : 128);
-            M.extent -= t0 * KP;
-            N.extent -= t0 * KP;
-        }
-        p.begin(dyn_lds, M, N, rowM, panels);
-    };
+    auto begin = [&](const TileAt &t) { product_begin<T, FORM, S>(p, g, groups, t, dyn_lds); };
     const uint64_t key = g.out.drop.cut ? g.out.drop.key() : 0;
     const int lane = (int)threadIdx.x & 63;
     char *mine = dyn_lds + S::NS * S::STAGE + (p.wm * S::WN + p.wn) * S::RESULTS;
@@ -681,23 +727,11 @@ __device__ __forceinline__ void product_work(const ProductArgs &g, int groups, i
         if (there) begin(t);
         after = false;
         if (now.shared >= 0 &&
-            !product_join<T, MCOL, NCOL, S>(p, g, now, dyn_lds + S::NS * S::STAGE)) {
+            !product_join(p, g, now, dyn_lds + S::NS * S::STAGE)) {
             if (!there) return;
             continue;
         }
-        Epilogue o = g.out;
-        if constexpr (FORM != kRowsRows) {   // gradients are the sums themselves
-            o.bias = o.residual = nullptr;
-            o.Z = nullptr;
-            o.activation = GETT_ACTIVATION_NONE;
-            o.drop.cut = 0;
-        }
-        if (groups == kByRows && o.bias) o.bias += (int64_t)now.e * g.n * sizeof(T);
-        if (groups == kByK) o.Y += (int64_t)now.e * g.stepN * (o.wide ? 4 : sizeof(T));
-        if (now.empty) {
-            o.bias = nullptr;
-            o.activation = GETT_ACTIVATION_NONE;
-        }
+        const Epilogue o = product_epilogue<T, FORM>(g, groups, now);
         after = now.row0 + S::BM <= now.rows && now.col0 + S::BN <= g.n;
         // The results go through LDS, 16 rows of a wavefront at a time, so that one
         // loop (and not one copy of the epilogue for each register) takes them, whole
@@ -768,6 +802,60 @@ __device__ __forceinline__ void product_work(const ProductArgs &g, int groups, i
         }
         if (!there) return;
     }
+}
+
+// A block of 32 x 32 whose wavefronts share K: their four sums are added in the order of
+// the slabs, and a row's runs of eight columns leave from four lanes.
+template <typename T, ProductForm FORM, typename S>
+__device__ __forceinline__ void product_slabs(const ProductArgs &g, int groups, int id, char *dyn_lds)
+{
+    TileAt t;
+    if (!product_tile<S>(g, groups, id, t)) return;
+    Product<T, FORM == kColumnsColumns, FORM != kRowsRows, S> p;
+    p.locate();
+    product_begin<T, FORM, S>(p, g, groups, t, dyn_lds);
+    p.clear();
+    p.template run<0>(dyn_lds, false);
+    __syncthreads();
+    float *sums = reinterpret_cast<float *>(dyn_lds);
+#pragma unroll
+    for (int a = 0; a < 4; ++a) {
+        const f16v &v = p.acc[0][0];
+        *reinterpret_cast<f4 *>(sums + (p.wn * 32 + p.q) * S::ROW + 8 * a + 4 * p.h) =
+            f4{v[4 * a], v[4 * a + 1], v[4 * a + 2], v[4 * a + 3]};
+    }
+    __syncthreads();
+    const int r = (int)threadIdx.x >> 2, c = ((int)threadIdx.x & 3) * 8;
+    if (r >= 32 || t.row0 + r >= t.rows) return;
+    float v[8] = {};
+#pragma unroll
+    for (int y = 0; y < 4; ++y) {
+        const f4 lo = *reinterpret_cast<const f4 *>(sums + (y * 32 + r) * S::ROW + c);
+        const f4 hi = *reinterpret_cast<const f4 *>(sums + (y * 32 + r) * S::ROW + c + 4);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            v[i] += lo[i];
+            v[4 + i] += hi[i];
+        }
+    }
+    const Epilogue o = product_epilogue<T, FORM>(g, groups, t);
+    product_store<T>(o, o.drop.cut ? o.drop.key() : 0, t.row0 + r, t.col0 + c, g.n - t.col0 - c, v);
+}
+
+template <typename T, ProductForm FORM, typename S>
+__global__ __launch_bounds__(S::THREADS) void product_slabs_kernel(ProductArgs g, int groups)
+{
+    extern __shared__ __attribute__((aligned(256))) char dyn_lds[];
+    product_slabs<T, FORM, S>(g, groups, (int)blockIdx.x, dyn_lds);
+}
+template <typename T, typename S>
+__global__ __launch_bounds__(S::THREADS) void product_slabs_pair_kernel(ProductArgs x, int groupsX, int blocks,
+                                                                        ProductArgs w, int groupsW)
+{
+    extern __shared__ __attribute__((aligned(256))) char dyn_lds[];
+    const int id = (int)blockIdx.x;
+    if (id < blocks) product_slabs<T, kRowsColumns, S>(x, groupsX, id, dyn_lds);
+    else product_slabs<T, kColumnsColumns, S>(w, groupsW, id - blocks, dyn_lds);
 }
 
 template <typename T, ProductForm FORM, typename S>

@@ -63,6 +63,7 @@ typedef ProductShape<1, 1, 2, 2, 4> ProductSmall;
 // LDS, with more panels on their way.
 typedef ProductShape<2, 2, 2, 2, 4> ProductMidDeep;
 typedef ProductShape<1, 1, 2, 2, 8> ProductSmallDeep;
+typedef ProductSlabs<4> ProductBlocks;
 
 // Few rows: a workgroup for 32 columns and, of experts, for each row that may be an
 // expert's first.
@@ -88,8 +89,19 @@ gett_status_t product_few(ProductGroups groups, ProductArgs g, hipStream_t s)
 }
 
 template <typename T, ProductForm FORM>
+gett_status_t product_slabs_one(ProductGroups groups, ProductArgs g, const ProductPlan &p, hipStream_t s)
+{
+    typedef ProductBlocks S;
+    if (!product_fill<T>(g, p) || !fits_launch(p.units, S::THREADS)) return GETT_ERROR_NOT_SUPPORTED;
+    hipLaunchKernelGGL((product_slabs_kernel<T, FORM, S>), dim3((unsigned)g.units), dim3(S::THREADS), S::LDS, s,
+                       g, (int)groups);
+    return launched(hipGetLastError());
+}
+
+template <typename T, ProductForm FORM>
 gett_status_t product_form(ProductGroups groups, const ProductArgs &g, const ProductPlan &p, hipStream_t s)
 {
+    if (p.shape == kSlabs) return product_slabs_one<T, FORM>(groups, g, p, s);
     if constexpr (sizeof(T) == 2)   // (in 32 bits the middle ones are bound by the instructions)
         if (p.shape == 0) return product_tiles<T, FORM, ProductBig>(groups, g, p, s);
     const bool deep = p.units <= kProductCus;
@@ -118,6 +130,15 @@ gett_status_t product_launch_pair(const ProductArgs &x, ProductGroups groupsX, c
 {
     if constexpr (sizeof(T) == 2)
         if (px.shape == 0) return product_pair<T, ProductBig>(x, groupsX, px, w, groupsW, pw, s);
+    if (px.shape == kSlabs) {
+        typedef ProductBlocks S;
+        ProductArgs gx = x, gw = w;
+        if (!product_fill<T>(gx, px) || !product_fill<T>(gw, pw) || !fits_launch(px.units + pw.units, S::THREADS))
+            return GETT_ERROR_NOT_SUPPORTED;
+        hipLaunchKernelGGL((product_slabs_pair_kernel<T, S>), dim3((unsigned)(gx.units + gw.units)),
+                           dim3(S::THREADS), S::LDS, s, gx, (int)groupsX, gx.units, gw, (int)groupsW);
+        return launched(hipGetLastError());
+    }
     const bool deep = px.units + pw.units <= kProductCus;
     if (px.shape == 1)
         return deep ? product_pair<T, ProductMidDeep>(x, groupsX, px, w, groupsW, pw, s)

@@ -8,7 +8,8 @@
 //
 // us per panel with the CUs full and with one workgroup each, per tile, and for a
 // join of s slices, measured: the products of 8192 x 8192 x 4096, 1023 x 515 x 1000 and
-// 200 x 4096 x 4096.
+// 200 x 4096 x 4096; of blocks of 32 those of 2048 x 1024 x 1024, 128 x 2048 x 2048, 512 x
+// 512 x 4096 and 2048 x 2048 x 128.
 #include "product_plan.hpp"
 
 #include "layers.hpp"
@@ -28,30 +29,51 @@ constexpr ShapeCost kCost16[3] = {{256, 1, 1.50, 1.20, 9.0, 15.0, 6.0},
 constexpr ShapeCost kCost32[3] = {{},   // (none: the middle ones are bound by the instructions)
                                   {128, 2, 3.90, 2.05, 4.0, 9.0, 2.5},
                                   {64, 2, 1.05, 0.60, 2.5, 3.5, 0.5}};
+// Blocks of 32 x 32 by the form (a k of 32 columns of 16 bits is half a line).  us, tiles of
+// 64 against blocks: 128 x 2048 x 2048 bf16 11.5, 6.9 and fp32 19.5, 14.7; 1023 x 515 x 1000
+// fp32 21.1, 14.0; 2048 x 1024 x 1024 bf16 11.5, 14.0, dw 10.8, 22.0.
+constexpr ShapeCost kBlocks16[3] = {{32, 4, 0.33, 0.094, 1.5, 0, 0},
+                                    {32, 4, 0.42, 0.094, 1.5, 0, 0},
+                                    {32, 4, 0.60, 0.140, 1.5, 0, 0}};
+constexpr ShapeCost kBlocks32 = {32, 4, 0.58, 0.171, 1.4, 0, 0};
 constexpr int64_t kCus = kProductCus;
+
+// a panel's time with so many workgroups at once
+double panel_us(const ShapeCost &c, int64_t units)
+{
+    const double us = c.full * (double)((units + kCus - 1) / kCus) / c.perCu;
+    return us < c.alone ? c.alone : us > c.full ? c.full : us;
+}
 
 }  // namespace
 
-// y = x w^T of up to 32 rows (and of up to 64 rows of experts in all), unless a long sum
-// of few columns leaves most CUs without work: tiles share it.  us, few rows against
-// tiles, of 32 rows: 8192 x 4096 bf16 21.8, 18.1 (16 rows 19.0, 17.8; 5 rows 17.9,
-// 17.7), fp32 35.8, 42.6; 4096 x 1024 7.2, 8.1; 512 x 4096 17.6, 10.2; of 64 rows 8192 x
-// 4096 30.7, 18.1.
-bool product_is_few(gett_dtype_t dtype, ProductGroups groups, int64_t m, int64_t n, int64_t k)
+// y = x w^T of so few rows that a wavefront takes rows of w whole: up to 2 in 16 bits,
+// unless the blocks of 32 columns keep every CU busy, and up to 4 in 32 bits; of experts
+// up to two rows each.  us, rows of w against blocks: 1 row with 2048 x 2048 bf16 4.7, 6.4,
+// 8192 x 4096 14.2, 11.9; 3 rows with 2048 x 2048 bf16 7.4, 6.5, fp32 9.5, 14.5; 16 and 64
+// rows of 64 experts of 1024 x 2048 bf16 11.8, 19.4 and 40.7, 31.4, fp32 21.5, 72.4 and 74,
+// 88.  Where w would have to be copied onto the 16-byte grid, up to 32 rows (of experts
+// 64) take it as it lies: 18 rows of 12 experts of 333 x 500 bf16 4.8, 11.6.
+bool product_is_few(gett_dtype_t dtype, ProductGroups groups, int64_t m, int64_t n, int64_t experts,
+                    bool grid)
 {
-    if (groups == kByRows) return m <= 64;
-    return m <= 4 || (m <= 32 && (n > 1024 || k * type_size(dtype) <= 4096));
+    const bool half = type_size(dtype) == 2;
+    if (!grid) return m <= (groups == kByRows ? 64 : 32);
+    if (groups == kByRows) return m <= 2 * experts && m <= (half ? 32 : 64);
+    return half ? m <= 2 && n < 32 * kCus : m <= 4;
 }
 
-ProductPlan product_plan(gett_dtype_t dtype, ProductGroups groups, int64_t m, int64_t n, int64_t k,
-                         int64_t experts)
+ProductPlan product_plan(gett_dtype_t dtype, ProductForm form, ProductGroups groups, int64_t m, int64_t n,
+                         int64_t k, int64_t experts, int only)
 {
     const int64_t KP = 128 / type_size(dtype);
     ProductPlan best = {};
-    double least = 1e300;
-    for (int shape = 0; shape < 3; ++shape) {
+    best.us = 1e300;
+    for (int shape = 0; shape <= kSlabs; ++shape) {
         if (dtype == GETT_FLOAT32 && shape == 0) continue;
-        const ShapeCost &c = dtype == GETT_FLOAT32 ? kCost32[shape] : kCost16[shape];
+        if (only >= 0 && shape != only) continue;
+        const ShapeCost &c = dtype == GETT_FLOAT32 ? (shape == kSlabs ? kBlocks32 : kCost32[shape])
+                                                   : (shape == kSlabs ? kBlocks16[form] : kCost16[shape]);
         ProductPlan p = {};
         p.shape = shape;
         p.tilesM = (m + c.edge - 1) / c.edge;
@@ -73,27 +95,21 @@ ProductPlan product_plan(gett_dtype_t dtype, ProductGroups groups, int64_t m, in
         }
         p.tiles = p.full = p.units = p.bandRows * p.tilesN;
         p.slices = 1;
-        const double slots = (double)(kCus * c.perCu);
+        const int64_t all = kCus * c.perCu;
         if (groups != kWhole) {
-            const double rounds = tiles / slots;
-            const double part = tiles <= kCus ? c.alone : c.full;
+            const double rounds = tiles / (double)all;
             // (the experts' tiles differ and even out over the rounds)
-            const double us = (rounds < 1 ? 1 : rounds) * ((double)panels * part + c.tile);
-            if (us < least) {
-                least = us;
-                best = p;
-            }
+            p.us = (rounds < 1 ? 1 : rounds) * ((double)panels * panel_us(c, (int64_t)tiles) + c.tile);
+            if (p.us < best.us) best = p;
             continue;
         }
-        const int64_t all = kCus * c.perCu, rounds = p.tiles / all, rest = p.tiles % all;
+        const int64_t rounds = p.tiles / all, rest = p.tiles % all;
         for (int64_t s = 1; s <= 16; ++s) {
-            if (s > 1 && (rest == 0 || rest * s > all || panels < 2 * s)) break;
-            double us = (double)rounds * ((double)panels * c.full + c.tile);
-            if (rest)
-                us += (double)((panels + s - 1) / s) * (rest * s <= kCus ? c.alone : c.full) + c.tile;
-            if (s > 1) us += c.join + c.joinEach * (double)s;
-            if (us >= least) continue;
-            least = us;
+            if (s > 1 && (shape == kSlabs || rest == 0 || rest * s > all || panels < 2 * s)) break;
+            p.us = (double)rounds * ((double)panels * c.full + c.tile);
+            if (rest) p.us += (double)((panels + s - 1) / s) * panel_us(c, rest * s) + c.tile;
+            if (s > 1) p.us += c.join + c.joinEach * (double)s;
+            if (p.us >= best.us) continue;
             best = p;
             best.slices = s;
             best.full = s > 1 ? p.tiles - rest : p.tiles;
@@ -110,11 +126,11 @@ ProductPlan product_plan(gett_dtype_t dtype, ProductGroups groups, int64_t m, in
 extern "C" void gett_product_tiles(gett_dtype_t dtype, int64_t m, int64_t n, int64_t k,
                                    struct gett_tiles *out)
 {
-    if (gett::product_is_few(dtype, gett::kWhole, m, n, k)) {
+    if (gett::product_is_few(dtype, gett::kWhole, m, n, 0, true)) {
         *out = {0, 1, 0, (n + 31) / 32};
         return;
     }
-    const gett::ProductPlan p = gett::product_plan(dtype, gett::kWhole, m, n, k, 0);
+    const gett::ProductPlan p = gett::product_plan(dtype, gett::kRowsRows, gett::kWhole, m, n, k, 0);
     out->edge = 256 >> p.shape;
     out->slices = p.slices;
     out->shared = p.counters;

@@ -17,15 +17,18 @@ TYPES = [torch.float32, torch.bfloat16, torch.float16]
 CODES = {torch.float32: g.GETT_FLOAT32, torch.bfloat16: g.GETT_BFLOAT16, torch.float16: g.GETT_FLOAT16}
 
 # m, n, k and what they have to take: the tiles' edge, whether sums are shared, and
-# whether workgroups are alone on a CU (-1), two a CU (0) or take several tiles (1)
-TILES16 = [(4372, 2693, 72, 256, False, -1), (8300, 7900, 328, 256, False, 1),
-           (2973, 666, 40, 128, False, -1), (3237, 1229, 40, 128, False, 0), (3085, 2579, 40, 128, False, 1),
-           (86, 228, 40, 64, False, -1), (270, 3492, 40, 64, False, 0), (3789, 1070, 520, 64, False, 1),
-           (146, 52, 2056, 64, True, -1), (3167, 65, 4104, 64, True, 0)]
-TILES32 = [(2696, 707, 40, 128, False, -1), (2377, 1689, 40, 128, False, 0), (2525, 3276, 40, 128, False, 1),
-           (922, 1102, 4104, 128, True, 0), (4420, 195, 2056, 128, True, -1), (3820, 4384, 520, 128, True, 1),
-           (201, 145, 40, 64, False, -1), (2817, 321, 40, 64, False, 0), (458, 4338, 72, 64, False, 1),
-           (74, 62, 1032, 64, True, -1), (87, 3166, 1032, 64, True, 0), (2362, 850, 520, 64, True, 1)]
+# whether workgroups are alone on a CU (-1), all resident at once (0) or more (1)
+TILES16 = [(4372, 2693, 72, 256, False, -1), (8300, 7900, 328, 256, False, 1), (4487, 4507, 4104, 256, True, 1),
+           (1122, 1805, 40, 128, False, -1), (3237, 1229, 40, 128, False, 0), (3085, 2579, 40, 128, False, 1),
+           (2317, 3380, 4104, 128, True, 1),
+           (4897, 130, 1032, 64, False, -1), (260, 3645, 40, 64, False, 0), (3789, 1070, 520, 64, False, 1),
+           (4151, 97, 4104, 64, True, 0),
+           (86, 228, 40, 32, False, -1), (270, 3492, 40, 32, False, 0), (2973, 666, 40, 32, False, 1)]
+TILES32 = [(2502, 1219, 40, 128, False, -1), (2596, 1571, 40, 128, False, 0), (2525, 3276, 40, 128, False, 1),
+           (353, 3403, 4104, 128, True, -1), (609, 2450, 4104, 128, True, 0), (3820, 4384, 520, 128, True, 1),
+           (4914, 291, 40, 64, False, 0), (4708, 790, 40, 64, False, 1),
+           (40, 41, 4104, 64, True, -1), (4355, 39, 2056, 64, True, 0), (3691, 611, 1032, 64, True, 1),
+           (201, 145, 40, 32, False, -1), (922, 1102, 4104, 32, False, 0), (2696, 707, 40, 32, False, 1)]
 
 
 def on_gpu(t):
@@ -55,7 +58,7 @@ def close(got, ref, err, what=""):
                          [(torch.float16, *TILES16[0])] + [(torch.float32, *t) for t in TILES32])
 def test_every_kind_of_tile(gpu, dtype, m, n, k, edge, shared, fill):
     t = product_tiles(CODES[dtype], m, n, k)
-    resident = 256 if edge == 256 else 512
+    resident = {256: 256, 32: 1024}.get(edge, 512)
     assert t.edge == edge and (t.slices > 1) == shared
     assert fill == (-1 if t.workgroups <= 256 else 0 if t.workgroups <= resident else 1)
     x, w = rand(1, m, k, dtype=dtype), rand(2, n, k, dtype=dtype, scale=k ** -0.5)
@@ -78,7 +81,7 @@ def test_every_kind_of_tile(gpu, dtype, m, n, k, edge, shared, fill):
 
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("m", [1, 2, 3, 4, 5, 32, 33, 64, 65])
-@pytest.mark.parametrize("n,k", [(31, 7), (70, 1030), (33, 4104)])
+@pytest.mark.parametrize("n,k", [(31, 7), (70, 1030), (33, 4104), (8200, 72)])
 def test_few_rows(gpu, dtype, m, n, k):
     x, w = rand(m, m, k, dtype=dtype), rand(2, n, k, dtype=dtype, scale=k ** -0.5)
     bias, residual = rand(3, n, dtype=dtype), rand(4, m, n, dtype=dtype)
@@ -93,8 +96,11 @@ def test_strides_and_addresses(gpu, dtype, m):
     wide_x, wide_w = rand(1, m, 215, dtype=dtype).cuda(), rand(2, 90, 300, dtype=dtype).cuda()
     x, w, res = wide_x[:, 3:203], wide_w[:, 7:207], rand(3, 90, m, dtype=dtype).cuda().t()
     bias = rand(4, 1, dtype=dtype).cuda().expand(90)
-    want = g.linear(x.contiguous(), w.contiguous(), bias.contiguous(), residual=res.contiguous())
-    assert torch.equal(g.linear(x, w, bias, residual=res), want)
+    # (few rows of weights at odd addresses are summed in another order than on the grid)
+    want = linear64(x, w, bias, None, res, dtype)
+    close(g.linear(x.contiguous(), w.contiguous(), bias.contiguous(), residual=res.contiguous()), *want)
+    close(g.linear(x, w, bias, residual=res), *want)
+    assert torch.equal(g.linear(x, w, bias, residual=res), g.linear(x, w, bias, residual=res))
     leaves = [v.detach().requires_grad_() for v in (wide_x, wide_w)]
     dy = rand(5, 90, m, dtype=dtype).cuda().t()
     grads = torch.autograd.grad(g.linear(leaves[0][:, 3:203], leaves[1][:, 7:207]), leaves, dy)

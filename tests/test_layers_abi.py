@@ -214,8 +214,9 @@ def product_tiles(dtype, m, n, k):
 
 @pytest.mark.parametrize("dtype,m,n,k,edge", [
     (BF16, 8192, 8192, 4096, 256), (BF16, 1024, 4096, 4096, 128), (BF16, 200, 4096, 4096, 64),
-    (BF16, 64, 4096, 4096, 64), (BF16, 32, 4096, 4096, 0), (BF16, 32, 512, 4096, 64),
-    (BF16, 4, 512, 4096, 0), (F32, 8192, 8192, 4096, 128), (F32, 65, 128, 64, 64)])
+    (BF16, 64, 4096, 4096, 32), (BF16, 3, 512, 4096, 32), (BF16, 2, 512, 4096, 0), (BF16, 1, 8192, 4096, 32),
+    (F32, 8192, 8192, 4096, 128), (F32, 32, 512, 4096, 64), (F32, 65, 128, 64, 32), (F32, 5, 128, 64, 32),
+    (F32, 4, 512, 4096, 0)])
 def test_tiles_by_size(dtype, m, n, k, edge):
     assert product_tiles(dtype, m, n, k).edge == edge
 
@@ -223,7 +224,7 @@ def test_tiles_by_size(dtype, m, n, k, edge):
 def test_no_tiles_of_256_in_32_bits():
     for k in (0, 1, 64, 4096):
         for m in (65, 100, 8192, 100000):
-            assert product_tiles(F32, m, m, k).edge in (64, 128)
+            assert product_tiles(F32, m, m, k).edge in (32, 64, 128)
 
 
 @pytest.mark.parametrize("m,n,k", [(65, 4096, 4096), (1023, 515, 1000), (300, 300, 8192), (2100, 2100, 4096)])

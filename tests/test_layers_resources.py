@@ -10,7 +10,8 @@ import pytest
 import paper_1607_00145_amd as g
 from test_kernel_resources import LLVM, code_objects
 
-KERNELS = ["dropout_kernel", "product_kernel", "product_pair_kernel", "product_few_kernel", "product_row_kernel",
+KERNELS = ["dropout_kernel", "product_kernel", "product_pair_kernel", "product_slabs_kernel",
+           "product_slabs_pair_kernel", "product_few_kernel", "product_row_kernel",
            "layer_copy_kernel", "layer_slope_kernel", "layer_sums_kernel", "combine_kernel",
            "combine_grad_kernel", "route_choose_kernel", "route_small_kernel", "route_scan_kernel",
            "route_place_kernel", "route_grad_kernel"]
