@@ -1,14 +1,15 @@
-// product_few.hpp -- products of few rows (device code), for single tokens and small
-// batches: C[i, j] = sum over K of M(i, k) N(j, k) with up to 32 rows i, or of every
-// expert's rows where there are up to 64 in all.
+// product_few.hpp -- products of few rows (device code) that no tile suits: C[i, j] = sum
+// over K of M(i, k) N(j, k) with rows of N at any address, for up to 32 rows i or up to
+// 64 of all experts together, and of one to four rows (product_is_few says when).
 //
-// Bound by N's bytes, and where these are few by the launch and two memory
-// latencies.  A workgroup takes 32 rows of N (columns of C) and its eight wavefronts
-// every eighth panel of 128 bytes of K; N goes from memory straight into the
-// registers that the MFMA reads, 64 bytes of one row a lane, so that no byte waits for
-// a barrier, and the eight partial results are summed in wavefront order through LDS.
-// 5 to 32 rows with 8192 x 4096 in bf16 take 18 to 22 us (67 MB: 3.1 to 3.7 TB/s).
-// Rows may lie at any element address: nothing is copied first.
+// The first kernel is for N off the 16-byte grid, which tiles would copy first.  Bound by
+// N's bytes, and where these are few by the launch and two memory latencies.  A
+// workgroup takes 32 rows of N (columns of C) and its eight wavefronts every eighth
+// panel of 128 bytes of K; N goes from memory straight into the registers that the
+// MFMA reads, 64 bytes of one row a lane, so that no byte waits for a barrier, and
+// the eight partial results are summed in wavefront order through LDS.  5 to 32 rows
+// with 8192 x 4096 in bf16 take 18 to 22 us (67 MB: 3.1 to 3.7 TB/s; blocks of 32 x 32 take
+// 12, and where N is copied before 30 more).
 #pragma once
 #include "product.hpp"
 
