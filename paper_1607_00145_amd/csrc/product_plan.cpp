@@ -37,6 +37,9 @@ constexpr ShapeCost kBlocks16[3] = {{32, 4, 0.33, 0.094, 1.5, 0, 0},
                                     {32, 4, 0.60, 0.140, 1.5, 0, 0}};
 constexpr ShapeCost kBlocks32 = {32, 4, 0.58, 0.171, 1.4, 0, 0};
 constexpr int64_t kCus = kProductCus;
+// A block is a workgroup of 256 threads, and a launch has fewer than 2^32 threads also
+// where it takes two products; the other shapes' workgroups take tile after tile.
+constexpr int64_t kMostBlocks = (int64_t)1 << 22;
 
 // a panel's time with so many workgroups at once
 double panel_us(const ShapeCost &c, int64_t units)
@@ -95,6 +98,7 @@ ProductPlan product_plan(gett_dtype_t dtype, ProductForm form, ProductGroups gro
         }
         p.tiles = p.full = p.units = p.bandRows * p.tilesN;
         p.slices = 1;
+        if (shape == kSlabs && p.units > kMostBlocks) continue;
         const int64_t all = kCus * c.perCu;
         if (groups != kWhole) {
             const double rounds = tiles / (double)all;

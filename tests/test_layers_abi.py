@@ -227,6 +227,15 @@ def test_no_tiles_of_256_in_32_bits():
             assert product_tiles(F32, m, m, k).edge in (32, 64, 128)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_products_of_any_size_fit_a_launch(dtype):
+    """Blocks of 32 x 32 are workgroups of their own: no more than a launch has threads for."""
+    for m in (1 << 20, (1 << 27) + 5, (1 << 30) - 1):
+        for n, k in ((1, 1), (16, 16), (33, 64)):
+            t = product_tiles(dtype, m, n, k)
+            assert t.edge > 32 or t.workgroups <= 1 << 22, (m, n, k)
+
+
 @pytest.mark.parametrize("m,n,k", [(65, 4096, 4096), (1023, 515, 1000), (300, 300, 8192), (2100, 2100, 4096)])
 @pytest.mark.parametrize("dtype", [F32, BF16])
 def test_shared_tiles_fit_their_counters(dtype, m, n, k):
