@@ -87,13 +87,14 @@ struct ProductArgs {
     Epilogue out;
 };
 
-template <int FM_, int FN_, int WM_, int WN_, int NS_> struct ProductShape {
-    static constexpr int FM = FM_, FN = FN_, WM = WM_, WN = WN_, NS = NS_;
+// FM x FN blocks of 32 x 32 for each of WM x WN wavefronts, NS stages of P panels.
+template <int FM_, int FN_, int WM_, int WN_, int NS_, int P_ = 1> struct ProductShape {
+    static constexpr int FM = FM_, FN = FN_, WM = WM_, WN = WN_, NS = NS_, P = P_;
     static constexpr int BM = 32 * FM * WM, BN = 32 * FN * WN;
     static constexpr int NW = WM * WN, THREADS = 64 * NW;
     static constexpr bool SLABS = false;
-    static constexpr int STAGE = (BM + BN) * 128;
-    static constexpr int JA = BM / 8 / NW, JB = BN / 8 / NW, J = JA + JB;   // loads a lane
+    static constexpr int PANEL = (BM + BN) * 128, STAGE = P * PANEL;
+    static constexpr int JA = BM / 8 / NW, JB = BN / 8 / NW, JP = JA + JB, J = P * JP;   // loads a lane
     static constexpr int W = 32 * FN;                   // columns of a wavefront
     static constexpr int RESULTS = 16 * W * 4;          // of LDS a wavefront, for its results
     static constexpr int LDS = NS * STAGE + NW * RESULTS;
@@ -103,14 +104,15 @@ template <int FM_, int FN_, int WM_, int WN_, int NS_> struct ProductShape {
 };
 
 // One block of 32 x 32 for four wavefronts, each of which takes one slab of every panel,
-// four workgroups a CU: for products that have too few larger tiles to fill the card.
-// Bound by a barrier and the LDS latency behind it, 0.09 us a panel (fp32 0.17, of
-// which the MFMAs have 0.12), until several are on a CU; eight stages in the place of
-// four, and the epilogue's operands fetched before the panels, changed nothing.
-template <int NS_> struct ProductSlabs {
-    static constexpr int FM = 1, FN = 1, NS = NS_, BM = 32, BN = 32, NW = 4, THREADS = 256;
+// three workgroups a CU: for products that have too few larger tiles to fill the card.
+// Bound by a barrier and the LDS latency behind it, 0.13 us a stage of two panels (fp32
+// 0.33, of which the MFMAs have 0.25), until several are on a CU.  (Stages of one panel,
+// four of them: 512 x 512 x 4096 in bf16 10.4 us, where this takes 8.5; eight of them, or
+// the epilogue's operands fetched before the panels, were not better.)
+struct ProductSlabs {
+    static constexpr int FM = 1, FN = 1, NS = 3, P = 2, BM = 32, BN = 32, NW = 4, THREADS = 256;
     static constexpr bool SLABS = true;
-    static constexpr int STAGE = (BM + BN) * 128, JA = 1, JB = 1, J = 2;
+    static constexpr int PANEL = (BM + BN) * 128, STAGE = P * PANEL, JA = 1, JB = 1, JP = 2, J = P * JP;
     static constexpr int ROW = 36;   // floats of a row of partial sums: whole vectors, few conflicts
     static constexpr int LDS = NS * STAGE;
     static_assert(LDS >= 4 * 32 * ROW * 4, "the partial sums come where the stages were");
@@ -223,7 +225,7 @@ template <typename T, bool MCOL, bool NCOL, typename S> struct Product {
 
     // Loads on their way to LDS: what a lane fetches of each panel, and the next
     // panel.  In the order of issue a stage's J loads follow one another.
-    uint32_t off[S::J];
+    uint32_t off[S::JP], panelM, panelN;
     int alongM, alongN;
     const char *pm, *pn;
     int64_t stepM, stepN;
@@ -240,19 +242,23 @@ template <typename T, bool MCOL, bool NCOL, typename S> struct Product {
     }
     __device__ __forceinline__ void issue_one(int j)
     {
+        const int panel = j / S::JP;
+        j -= panel * S::JP;
         const bool isM = j < S::JA;
-        const int at = isM ? alongM + j * Along<MCOL, S::BM>::step
-                           : alongN + (j - S::JA) * Along<NCOL, S::BN>::step;
-        const uint32_t o = at < (isM ? leftM : leftN) ? off[j] : kNowhere;
-        load_to_lds(isM ? rm : rn, o,
-                    to + (isM ? 0 : S::BM * 128) + (isM ? j : j - S::JA) * S::NW * 1024);
+        const int at = panel * KP + (isM ? alongM + j * Along<MCOL, S::BM>::step
+                                         : alongN + (j - S::JA) * Along<NCOL, S::BN>::step);
+        uint32_t o = off[j];
+        if (panel) o = o == kNowhere ? o : o + panel * (isM ? panelM : panelN);
+        o = at < (isM ? leftM : leftN) ? o : kNowhere;
+        load_to_lds(isM ? rm : rn, o, to + panel * S::PANEL + (isM ? 0 : S::BM * 128) +
+                                          (isM ? j : j - S::JA) * S::NW * 1024);
     }
     __device__ __forceinline__ void issue_end()
     {
         pm += stepM;
         pn += stepN;
-        leftM -= KP;
-        leftN -= KP;
+        leftM -= S::P * KP;
+        leftN -= S::P * KP;
     }
     // Takes a tile and sends the loads of its first panels; nobody reads LDS any more.
     template <typename RowM>
@@ -261,15 +267,17 @@ template <typename T, bool MCOL, bool NCOL, typename S> struct Product {
         const int lane = (int)threadIdx.x & 63;
         const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
 #pragma unroll
-        for (int j = 0; j < S::J; ++j) {
+        for (int j = 0; j < S::JP; ++j) {
             off[j] = j < S::JA ? place<MCOL, S::BM>(M, j, wave, lane, rowM)
                                : place<NCOL, S::BN>(N, j - S::JA, wave, lane,
                                                     [&](int r) { return (uint32_t)(r * N.ld); });
         }
         alongM = Along<MCOL, S::BM>::first(wave, lane);
         alongN = Along<NCOL, S::BN>::first(wave, lane);
-        stepM = MCOL ? KP * M.ld : 128;
-        stepN = NCOL ? KP * N.ld : 128;
+        stepM = MCOL ? S::P * KP * M.ld : S::P * 128;
+        stepN = NCOL ? S::P * KP * N.ld : S::P * 128;
+        panelM = (uint32_t)(stepM / S::P);
+        panelN = (uint32_t)(stepN / S::P);
         pm = M.p;
         pn = N.p;
         ldsAt = (uint32_t)(uintptr_t)(matrix_lds *)lds + wave * 1024;
@@ -328,12 +336,14 @@ template <typename T, bool MCOL, bool NCOL, typename S> struct Product {
             return __builtin_bit_cast(i4, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
         };
         // Slabs read together.  One block of 32 x 32 a wavefront has too few MFMAs in a
-        // slab to cover the reads of the next: it reads whole panels where it is alone on
+        // slab to cover the reads of the next: it reads whole stages where it is alone on
         // its CU.
-        constexpr int G = FM * FN == 1 && NS == 8 && !S::SLABS ? 4 : 1, STEPS = S::SLABS ? 1 : 4 / G;
+        constexpr int G = S::SLABS ? S::P : S::P > 1 ? 4 * S::P : 1, STEPS = S::SLABS ? 1 : 4 * S::P / G;
         i4 a[2][G][FM], b[2][G][FN];
         auto fragment = [&](auto column, auto size, int own, int s, int i) {
             constexpr int B = decltype(size)::value;
+            own += (S::SLABS ? s : s / 4) * S::PANEL;
+            s = S::SLABS ? 0 : s % 4;
             if constexpr (!decltype(column)::value) {
                 return *reinterpret_cast<const i4 *>(lds + (own ^ (s * 16)) + i * 4096);
             } else if constexpr (sizeof(T) == 2) {
@@ -638,7 +648,7 @@ __device__ __forceinline__ void product_begin(Product<T, FORM == kColumnsColumns
                                               char *dyn_lds)
 {
     constexpr bool MCOL = FORM == kColumnsColumns, NCOL = FORM != kRowsRows;
-    constexpr int KP = 128 / (int)sizeof(T);
+    constexpr int KP = S::P * 128 / (int)sizeof(T);   // of a stage
     const bool gathered = FORM == kRowsRows && g.order;
     Side M, N;
     M.ld = g.ldm;
@@ -674,8 +684,8 @@ __device__ __forceinline__ void product_begin(Product<T, FORM == kColumnsColumns
     if (t.shared >= 0) {
         const int t0 = (int)quotient((uint32_t)(panels * t.slice), g.slices, g.slicesInv);
         panels = (int)quotient((uint32_t)(panels * (t.slice + 1)), g.slices, g.slicesInv) - t0;
-        M.p += t0 * (MCOL ? KP * M.ld : 128);
-        N.p += t0 * (NCOL ? KP * N.ld : 128);
+        M.p += t0 * (MCOL ? KP * M.ld : S::P * 128);
+        N.p += t0 * (NCOL ? KP * N.ld : S::P * 128);
         M.extent -= t0 * KP;
         N.extent -= t0 * KP;
     }

@@ -60,10 +60,10 @@ typedef ProductShape<4, 2, 2, 4, 2> ProductBig;
 typedef ProductShape<2, 2, 2, 2, 2> ProductMid;
 typedef ProductShape<1, 1, 2, 2, 4> ProductSmall;
 // The same, one a CU: of few tiles each is alone on its CU and may have all of the
-// LDS, with more panels on their way.
+// LDS, with more panels on their way (the small ones with two for each barrier: 200 x
+// 4096 x 4096 in bf16 18.3 -> 16.9 us).
 typedef ProductShape<2, 2, 2, 2, 4> ProductMidDeep;
-typedef ProductShape<1, 1, 2, 2, 8> ProductSmallDeep;
-typedef ProductSlabs<4> ProductBlocks;
+typedef ProductShape<1, 1, 2, 2, 4, 2> ProductSmallDeep;
 
 // Few rows: a workgroup for 32 columns and, of experts, for each row that may be an
 // expert's first.
@@ -91,7 +91,7 @@ gett_status_t product_few(ProductGroups groups, ProductArgs g, hipStream_t s)
 template <typename T, ProductForm FORM>
 gett_status_t product_slabs_one(ProductGroups groups, ProductArgs g, const ProductPlan &p, hipStream_t s)
 {
-    typedef ProductBlocks S;
+    typedef ProductSlabs S;
     if (!product_fill<T>(g, p) || !fits_launch(p.units, S::THREADS)) return GETT_ERROR_NOT_SUPPORTED;
     hipLaunchKernelGGL((product_slabs_kernel<T, FORM, S>), dim3((unsigned)g.units), dim3(S::THREADS), S::LDS, s,
                        g, (int)groups);
@@ -131,7 +131,7 @@ gett_status_t product_launch_pair(const ProductArgs &x, ProductGroups groupsX, c
     if constexpr (sizeof(T) == 2)
         if (px.shape == 0) return product_pair<T, ProductBig>(x, groupsX, px, w, groupsW, pw, s);
     if (px.shape == kSlabs) {
-        typedef ProductBlocks S;
+        typedef ProductSlabs S;
         ProductArgs gx = x, gw = w;
         if (!product_fill<T>(gx, px) || !product_fill<T>(gw, pw) || !fits_launch(px.units + pw.units, S::THREADS))
             return GETT_ERROR_NOT_SUPPORTED;

@@ -25,17 +25,17 @@ struct ShapeCost {
 };
 constexpr ShapeCost kCost16[3] = {{256, 1, 1.50, 1.20, 9.0, 15.0, 6.0},
                                   {128, 2, 1.00, 0.50, 4.0, 9.0, 2.5},
-                                  {64, 2, 0.42, 0.27, 2.5, 3.5, 0.5}};
+                                  {64, 2, 0.42, 0.22, 2.5, 3.5, 0.5}};
 constexpr ShapeCost kCost32[3] = {{},   // (none: the middle ones are bound by the instructions)
                                   {128, 2, 3.90, 2.05, 4.0, 9.0, 2.5},
                                   {64, 2, 1.05, 0.60, 2.5, 3.5, 0.5}};
 // Blocks of 32 x 32 by the form (a k of 32 columns of 16 bits is half a line).  us, tiles of
-// 64 against blocks: 128 x 2048 x 2048 bf16 11.5, 6.9 and fp32 19.5, 14.7; 1023 x 515 x 1000
-// fp32 21.1, 14.0; 2048 x 1024 x 1024 bf16 11.5, 14.0, dw 10.8, 22.0.
-constexpr ShapeCost kBlocks16[3] = {{32, 4, 0.33, 0.094, 1.5, 0, 0},
-                                    {32, 4, 0.42, 0.094, 1.5, 0, 0},
-                                    {32, 4, 0.60, 0.140, 1.5, 0, 0}};
-constexpr ShapeCost kBlocks32 = {32, 4, 0.58, 0.171, 1.4, 0, 0};
+// 64 against blocks: 128 x 2048 x 2048 bf16 11.5, 5.9 and fp32 19.5, 13.6; 1024 x 512 x 1000
+// fp32 20.5, 13.5; 2048 x 1024 x 1024 bf16 11.8, 14.0, dw 10.8, 22.0.
+constexpr ShapeCost kBlocks16[3] = {{32, 3, 0.25, 0.065, 1.5, 0, 0},
+                                    {32, 3, 0.32, 0.090, 1.5, 0, 0},
+                                    {32, 3, 0.45, 0.140, 1.5, 0, 0}};
+constexpr ShapeCost kBlocks32 = {32, 3, 0.44, 0.165, 1.4, 0, 0};
 constexpr int64_t kCus = kProductCus;
 // A block is a workgroup of 256 threads, and a launch has fewer than 2^32 threads also
 // where it takes two products; the other shapes' workgroups take tile after tile.
