@@ -17,9 +17,10 @@
  * a call have the call's type unless said otherwise.  Sums, activations and the
  * epilogue are held in 32 bits and rounded once, at the store.  Matrices are
  * row-major with a row stride in elements (at least their columns); rows may be
- * wider apart.  Addresses need only their element's alignment (operands of a
- * product that do not lie on the 16-byte grid, in base, stride and columns, are
- * copied into the stream's workspace first).
+ * wider apart.  Addresses need only their element's alignment: operands of a product
+ * that do not lie on the 16-byte grid, in base, stride and columns, are copied into
+ * the stream's workspace first, unless they are multiplied with few rows (up to 32, of
+ * experts 64), which take them as they lie and may sum in another order.
  *
  * Calls enqueue work on `stream` and return; errors are statuses; workspaces are
  * the library's own, one per device and stream, as gett_matrix.h describes: a
@@ -27,9 +28,9 @@
  * GETT_ERROR_NOT_SUPPORTED while the stream captures a graph.  They hold the copies
  * above, dZ of a gradient (unless it is dY itself), the rows of the experts' X and
  * dX where these are gathered, 4 bytes for each 8 to 64 numbers whose columns are
- * summed, and up to 64 MB for a product whose sums several workgroups share.  Repeated calls
- * give identical results.  Outputs must not overlap inputs or one another except
- * where it is said.
+ * summed, and up to 64 MB for a product whose sums several workgroups share.
+ * Repeated calls give identical results.  Outputs must not overlap inputs or one
+ * another except where it is said.
  *
  * Errors of every call: GETT_ERROR_INVALID_VALUE (unknown dtype, activation or
  * scoring, a negative extent, a stride smaller than the columns, a null or
