@@ -6,10 +6,11 @@
     h = gett.expert_linear(x, w1, r, activation="silu", gather=True)
     y = gett.combine(gett.expert_linear(h, w2, r), r)    # back to tokens
 
-All are differentiable.  The ``gett_*`` functions carry the names of the C
-interface and only marshal arguments; the others are a convenience over torch
-device tensors, enqueued on torch's current stream of the device that they lie
-on.
+All are differentiable, backwards and once: second derivatives raise, and so do
+derivatives forwards and traces (torch.jit.trace, make_fx), which would not see the
+kernels.  The ``gett_*`` functions carry the names of the C interface and only
+marshal arguments; the others are a convenience over torch device tensors, enqueued
+on torch's current stream of the device that they lie on.
 """
 from __future__ import annotations
 
@@ -272,6 +273,7 @@ def _make_functions():
         # derivatives: what depends on the gradients then raises, even where the
         # gradient that came in is a constant.
         def backward(ctx, *dy):
+            _m._eager("a gradient of the layers' operators", *dy)
             if not torch.is_grad_enabled():
                 return gradients(ctx, *dy)
             with torch.no_grad():
@@ -409,6 +411,7 @@ def dropout(x, p: float, seed, offset: int = 0):
     drop = _drop(p, seed, offset)
     if drop is None:
         return x
+    _m._eager("dropout", flat)
     if _records(x):
         y = _function("dropout").apply(flat, drop[3], drop)
     else:
@@ -495,6 +498,7 @@ def linear(x, w, bias=None, activation=None, residual=None, p: float = 0.0, seed
     seed = None if drop is None else drop[3]
     _m._device("x", x)
     _m._device("w", w)
+    _m._eager("linear", flat, w, bias, residual)
     if _records(x, w, bias, residual):
         y = _function("linear").apply(flat, w, bias, residual, seed, code, drop)
     else:
@@ -599,6 +603,7 @@ def route(logits, k: int, scoring: str = "softmax", bias=None, groups: int = 1,
     if logits.dim() != 2:
         raise ValueError("logits must be a matrix (tokens x experts)")
     _m._device("logits", logits)
+    _m._eager("route", logits, bias)
     if scoring not in SCORES:
         raise ValueError(f"scoring must be one of {sorted(SCORES)}")
     t, e = logits.shape
@@ -706,6 +711,7 @@ def expert_linear(x, w, routing: Routing, bias=None, activation=None, gather: bo
             _m._device(name, t)
     if bias is not None and bias.shape != w.shape[:2]:
         raise ValueError(f"bias must be {w.shape[0]} x {w.shape[1]}")
+    _m._eager("expert_linear", x, w, bias)
     if _records(x, w, bias):
         return _function("experts").apply(x, w, bias, routing, code, bool(gather))
     return _experts(x, w, bias, routing, code, bool(gather), None)
@@ -780,6 +786,7 @@ def combine(h, routing: Routing, weights=None, residual=None):
     _m._device("weights", weights)
     if residual is not None and tuple(residual.shape) != (t, h.shape[1]):
         raise ValueError("residual differs from the result in shape")
+    _m._eager("combine", h, weights, residual)
     if _records(h, weights, residual):
         return _function("combine").apply(h, weights, residual, routing)
     return _combine(h, weights, residual, routing)

@@ -123,14 +123,17 @@ def gett_mx_linear_grad(m: int, n: int, k: int, dtype_Y: int, dY: int, stride_ym
 
 _torch = None
 _current_device = _stream = None   # the current device; torch's current stream on one
+_forward = None                    # torch.autograd.forward_ad
 _codes = {}
 
 
 def _start():
     """torch and the element types' codes, on the first use."""
-    global _torch, _current_device, _stream
+    global _torch, _current_device, _stream, _forward
     import torch
+    import torch.autograd.forward_ad
     c = torch._C
+    _forward = torch.autograd.forward_ad
     _current_device = getattr(c, "_cuda_getDevice", torch.cuda.current_device)
     _stream = getattr(c, "_cuda_getCurrentRawStream",
                       lambda device: torch.cuda.current_stream(device).cuda_stream)
@@ -152,6 +155,20 @@ def _code(dtype) -> int:
 def _device(name, t):
     if not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
+
+
+def _eager(what, *tensors):
+    """Refuses what would lose a call in silence: tensors (or None) with a tangent, which
+    the result would not have (a derivative of zero), and traces, which would hold
+    the result's allocation and not the kernels that fill it."""
+    if _forward._current_level >= 0:
+        for t in tensors:
+            if t is not None and _forward.unpack_dual(t).tangent is not None:
+                raise RuntimeError(f"{what} has no derivative forwards")
+    c = _torch._C
+    if c._is_tracing() or (c._len_torch_dispatch_stack()
+                           and c._get_dispatch_mode(c._TorchDispatchModeKey.PROXY) is not None):
+        raise RuntimeError(f"{what} cannot be traced")
 
 
 def _written(t):
@@ -258,6 +275,7 @@ class MXTensor:
         r, c = self.rows, self.cols
         if _torch is None:
             _start()
+        _eager("dequantize", out)
         i = self._device
         if out is not None or i != _current_device():
             there = _elsewhere(self, out)
@@ -299,6 +317,7 @@ def mx_quantize(x, along: str = "cols"):
     if along not in ("cols", "rows", "both"):
         raise ValueError("along must be 'cols', 'rows' or 'both'")
     code, r, c, sr, sc = _matrix("x", x)
+    _eager("mx_quantize")
     i = x.get_device()
     if i != _current_device():
         with _elsewhere(x):
@@ -347,6 +366,7 @@ def mx_matmul(a, b, C=None, alpha: float = 1.0, beta: float = 0.0, dtype=None):
         raise ValueError(f"a has {k} columns, b {b.cols}")
     if _torch is None:
         _start()
+    _eager("mx_matmul", None if packed else a, C)
     i = b._device
     if C is not None or not i == a.get_device() == _current_device():
         there = _elsewhere(a, b, C)
@@ -442,6 +462,7 @@ def _linear_function():
             return recorded(ctx, dy) if torch.is_grad_enabled() else gradients(ctx, dy)
 
     def gradients(ctx, dy):
+        _eager("a gradient of mx_linear", dy)
         need_x, need_w = ctx.needs_input_grad
         m, n, k, tx, tw = ctx.sizes
         if dy.stride(0) < 1 or dy.stride(1) < 1:
@@ -477,11 +498,13 @@ def mx_linear(x, w):
     flat = x if len(shape) == 2 else x.reshape(math.prod(shape[:-1]), shape[-1])
     if isinstance(w, MXTensor):
         y = mx_matmul(flat, w)
-    elif _code(x.dtype) is not None and _torch.is_grad_enabled() and (x.requires_grad or
-                                                                      w.requires_grad):
-        y = _linear_function().apply(flat, w)
     else:
-        y = _linear_forward(flat, w, False, False)[0]
+        _code(x.dtype)
+        _eager("mx_linear", flat, w)
+        if _torch.is_grad_enabled() and (x.requires_grad or w.requires_grad):
+            y = _linear_function().apply(flat, w)
+        else:
+            y = _linear_forward(flat, w, False, False)[0]
     return y if len(shape) == 2 else y.reshape(*shape[:-1], y.shape[1])
 
 
@@ -495,6 +518,7 @@ def orthogonalize(G, steps: int = 5, coefficients=(3.4445, -4.7750, 2.0315), eps
         raise ValueError("a matrix or a stack of matrices is needed")
     code = _code(G.dtype)
     _device("G", G)
+    _eager("orthogonalize", G, out)
     there = _elsewhere(G, out)
     if there is not None:
         with there:
