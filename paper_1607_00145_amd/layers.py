@@ -162,6 +162,17 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
+def _values(t):
+    """t, or a copy where its memory holds other values than it has (torch's lazily
+    negated views: imaginary parts of conjugates, and gradients of such)."""
+    return t.resolve_neg() if t.is_neg() else t
+
+
+def _dense(t):
+    t = _values(t)
+    return t if t.is_contiguous() else t.contiguous()
+
+
 def _rows(name, t, dtype=None):
     """A device matrix whose columns are neighbours in memory: itself, or a copy.
     Returns it and its row stride."""
@@ -171,6 +182,7 @@ def _rows(name, t, dtype=None):
         raise TypeError(f"{name} is {t.dtype}, not {dtype}")
     if not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
+    t = _values(t)
     r, c = t.shape
     if t.is_contiguous():
         return t, c
@@ -188,7 +200,7 @@ def _vector(name, t, n, dtype):
         raise TypeError(f"{name} is {t.dtype}, not {dtype}")
     if not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
-    return t if t.is_contiguous() else t.contiguous()
+    return _dense(t)
 
 
 def _flat(name, x):
@@ -577,7 +589,7 @@ def _route_grad(logits, lists, dweights, how):
             return _route_grad(logits, lists, dweights, how)
     k, scoring, _, _, _, renormalize, scale = how
     logits, stride = _rows("logits", logits)
-    dweights = dweights.contiguous()
+    dweights = _dense(dweights)
     t, e = logits.shape
     out = logits.new_empty((t, e))
     _checked(_bound.gett_route_grad(
@@ -628,6 +640,7 @@ def route(logits, k: int, scoring: str = "softmax", bias=None, groups: int = 1,
 
 def _weights3(w):
     """experts x n x width with neighbours along the width: itself or a copy."""
+    w = _values(w)
     e, n, c = w.shape
     if w.is_contiguous():
         return w, c, n * c
@@ -648,8 +661,8 @@ def _experts(x, w, bias, routing, activation, gather, z):
     x, sx = _rows("x", x)
     w, sw, se = _weights3(w)
     n, width = w.shape[1], w.shape[2]
-    if bias is not None and not bias.is_contiguous():
-        bias = bias.contiguous()
+    if bias is not None:
+        bias = _dense(bias)
     y = x.new_empty((t * k, n))
     _, order, _, offsets = _addresses(routing._lists, t * k)
     st = _bound.gett_experts(_m._code(dtype), t, k, e, n, width, x.data_ptr(), sx, int(gather),
@@ -728,7 +741,7 @@ def _combine(h, weights, residual, routing):
     dtype = h.dtype
     h, sh = _rows("h", h)
     c = h.shape[1]
-    weights = weights if weights.is_contiguous() else weights.contiguous()
+    weights = _dense(weights)
     sr = 0
     if residual is not None:
         residual, sr = _rows("residual", residual, dtype)
@@ -753,8 +766,8 @@ def _combine_grad(dy, h, weights, lists, how, need_h, need_w):
     sh = 0
     if need_w:
         h, sh = _rows("h", h)
-    if need_h and not weights.is_contiguous():
-        weights = weights.contiguous()
+    if need_h:
+        weights = _dense(weights)
     dh = dy.new_empty(shape) if need_h else None
     dw = dy.new_empty((t, k), dtype=wtype) if need_w else None
     _, _, place, offsets = _addresses(lists, t * k)

@@ -196,6 +196,8 @@ def _matrix(name, t):
     code = _code(t.dtype)
     if not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
+    if t.is_neg():
+        raise ValueError(f"{name} is a lazily negated view: resolve_neg() it first")
     (r, c), (sr, sc) = shape, t.stride()
     if sr < 1 or sc < 1 or r < 2 or c < 2:
         sr, sc = _strides(t)
@@ -215,6 +217,8 @@ def _strides(t):
     carry any (torch leaves what it likes there, 0 included)."""
     sr, sc = t.stride()[-2:]
     r, c = t.shape[-2:]
+    if t.is_neg():
+        raise ValueError("a lazily negated view: resolve_neg() it first")
     if r > 1 and sr < 1 or c > 1 and sc < 1:
         raise ValueError("a broadcast (zero-stride) matrix: copy it first")
     return (sr if r > 1 else max(c, 1)), (sc if c > 1 else 1)
@@ -465,6 +469,8 @@ def _linear_function():
         _eager("a gradient of mx_linear", dy)
         need_x, need_w = ctx.needs_input_grad
         m, n, k, tx, tw = ctx.sizes
+        if dy.is_neg():
+            dy = dy.resolve_neg()  # (of a complex number's imaginary part)
         if dy.stride(0) < 1 or dy.stride(1) < 1:
             dy = dy.contiguous()   # the gradient of a sum is broadcast
         code, _, _, sm, sn = _matrix("dy", dy)

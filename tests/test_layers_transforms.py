@@ -19,6 +19,9 @@ class Claims(torch.Tensor):
     def get_device(self):
         return 0
 
+    def resolve_neg(self):
+        return torch.Tensor.resolve_neg(self).as_subclass(Claims)
+
 
 def on(*shape, dtype=torch.float32):
     return torch.zeros(*shape, dtype=dtype).as_subclass(Claims)
@@ -147,3 +150,109 @@ def test_no_dropout_may_be_traced(calls):
         assert g.dropout(d, 0.0, None) is d
     torch.jit.trace(lambda x: g.dropout(x, 0.0, None) + 1, (x,), check_trace=False)
     assert calls == []
+
+
+# lazily negated views ----------------------------------------------------------
+
+def negated(rows, cols, value=2.0):
+    """-value everywhere, as torch hands out imaginary parts of conjugates: memory
+    that holds `value`, its rows apart, and a mark that it is to be negated."""
+    t = torch.complex(torch.zeros(rows, cols), torch.full((rows, cols), value)).conj().imag
+    assert t.is_neg() and bool((t == -value).all())
+    return t
+
+
+def at(address, n):
+    return list((ctypes.c_float * n).from_address(address))
+
+
+def claims(t):
+    return t.as_subclass(Claims)
+
+
+# each float tensor of each call of the library: how it is made of a negated view of
+# the given shape, the function, and which argument is its address
+SEEN = {
+    "dropout": (lambda t: g.dropout(t, 0.5, 1), (4, 1), "gett_dropout", 3),
+    "linear x": (lambda t: g.linear(t, on(8, 1)), (4, 1), "gett_linear", 4),
+    "linear w": (lambda t: g.linear(on(6, 1), t), (4, 1), "gett_linear", 6),
+    "linear bias": (lambda t: g.linear(on(6, 16), on(1, 16), t[0]), (1, 1), "gett_linear", 8),
+    "linear residual": (lambda t: g.linear(on(4, 16), on(1, 16), residual=t), (4, 1), "gett_linear", 11),
+    "route": (lambda t: g.route(t, 1).weights, (4, 1), "gett_route", 4),
+    "route bias": (lambda t: g.route(on(6, 1), 1, bias=t[0]), (1, 1), "gett_route", 7),
+    "expert_linear x": (lambda t: g.expert_linear(t, on(3, 8, 1), routing(), gather=True), (6, 1),
+                        "gett_experts", 6),
+    "expert_linear w": (lambda t: g.expert_linear(on(6, 1), t[:, :, None], routing(), gather=True), (3, 1),
+                        "gett_experts", 9),
+    "expert_linear bias": (lambda t: g.expert_linear(on(6, 16), on(3, 1, 16), routing(), t, gather=True),
+                           (3, 1), "gett_experts", 12),
+    "combine h": (lambda t: g.combine(t, routing()), (12, 1), "gett_combine", 4),
+    "combine weights": (lambda t: g.combine(on(1, 8), g.Routing(1, 3, 1, on(1, 1), on(7, dtype=torch.int32)),
+                                            weights=t), (1, 1), "gett_combine", 7),
+    "combine residual": (lambda t: g.combine(on(12, 1), routing(), residual=t), (6, 1), "gett_combine", 9),
+}
+
+
+@pytest.fixture
+def seen(monkeypatch, calls):
+    """What the functions found at their arguments' addresses when they were called."""
+    found = []
+
+    def library(where, n):
+        class Library:
+            def __getattr__(self, name):
+                def call(*args):
+                    if name == where[0]:
+                        found.append(at(args[where[1]], n))
+                    return 0
+                return call
+        for module in (layers, matrix):
+            monkeypatch.setattr(module, "_bound", Library())
+        return found
+
+    return library
+
+
+@pytest.mark.parametrize("name", SEEN)
+def test_negated_views_are_read_as_their_values(seen, name):
+    call, shape, function, argument = SEEN[name]
+    found = seen((function, argument), 1)
+    call(claims(negated(*shape)))
+    assert found == [[-2.0]]
+
+
+@pytest.mark.parametrize("name,function,argument", [
+    ("dropout", "gett_dropout", 3), ("linear x", "gett_linear_grad", 4), ("linear w", "gett_linear_grad", 4),
+    ("route", "gett_route_grad", 10), ("expert_linear x", "gett_experts_grad", 6),
+    ("combine h", "gett_combine_grad", 4), ("combine weights", "gett_combine_grad", 4)])
+def test_negated_gradients_are_read_as_their_values(seen, name, function, argument):
+    """As they come out of a complex number's gradient."""
+    shape = {"linear w": (1, 16), "combine weights": (6, 2)}.get(name, EVERY[name][1])
+    call = {"linear x": lambda x: g.linear(x, on(1, 16)),
+            "route": lambda x: g.route(x[:1], 1).weights,
+            "expert_linear x": lambda x: g.expert_linear(x, on(3, 1, 16), routing(), gather=True),
+            "combine h": lambda h: g.combine(h[:, :1], routing()),
+            "combine weights": lambda w: g.combine(on(12, 1), routing(), weights=w),
+            "dropout": lambda x: g.dropout(x[:, :1], 0.5, 1)}.get(name, EVERY[name][0])
+    found = seen((function, argument), 1)
+    x = on(*shape).requires_grad_()
+    y = call(x)
+    found.clear()
+    torch.autograd.grad(y, x, claims(negated(*y.shape)))
+    assert found == [[-2.0]]
+
+
+def test_negated_matrices_of_the_4_bit_operators(seen):
+    """Inputs and outputs are refused as broadcast ones are; a gradient is read as its values."""
+    found = seen(("gett_mx_linear_grad", 4), 1)
+    t = claims(negated(6, 64))
+    for call in (lambda: g.mx_quantize(t), lambda: g.mx_matmul(t, packed(48, 64)),
+                 lambda: g.mx_matmul(on(6, 64), packed(64, 64), t), lambda: g.mx_linear(t, on(48, 64)),
+                 lambda: g.mx_linear(on(6, 64), t), lambda: g.orthogonalize(t),
+                 lambda: g.orthogonalize(on(6, 64), out=t), lambda: packed(6, 64).dequantize(out=t)):
+        with pytest.raises(ValueError, match="negated"):
+            call()
+    x = on(6, 64).requires_grad_()
+    y = g.mx_linear(x, on(48, 64))
+    torch.autograd.grad(y, x, claims(negated(6, 48)))
+    assert found == [[-2.0]]
