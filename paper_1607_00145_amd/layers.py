@@ -182,10 +182,10 @@ def _rows(name, t, dtype=None):
         raise TypeError(f"{name} is {t.dtype}, not {dtype}")
     if not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
-    t = _values(t)
     r, c = t.shape
-    if t.is_contiguous():
+    if t.is_contiguous() and (r > 1 or c > 1):   # (a negated view has every second number)
         return t, c
+    t = _values(t)
     sr, sc = t.stride()
     if (c > 1 and sc != 1) or (r > 1 and sr < c):
         t = t.contiguous()
@@ -200,7 +200,7 @@ def _vector(name, t, n, dtype):
         raise TypeError(f"{name} is {t.dtype}, not {dtype}")
     if not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
-    return _dense(t)
+    return t if n > 1 and t.is_contiguous() else _dense(t)
 
 
 def _flat(name, x):
@@ -640,10 +640,10 @@ def route(logits, k: int, scoring: str = "softmax", bias=None, groups: int = 1,
 
 def _weights3(w):
     """experts x n x width with neighbours along the width: itself or a copy."""
-    w = _values(w)
     e, n, c = w.shape
-    if w.is_contiguous():
+    if w.is_contiguous() and (n > 1 or c > 1):
         return w, c, n * c
+    w = _values(w)
     se, sn, sc = w.stride()
     if (c > 1 and sc != 1) or (n > 1 and sn < c) or (e > 1 and se < 0):
         w = w.contiguous()

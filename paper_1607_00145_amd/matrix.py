@@ -123,17 +123,17 @@ def gett_mx_linear_grad(m: int, n: int, k: int, dtype_Y: int, dY: int, stride_ym
 
 _torch = None
 _current_device = _stream = None   # the current device; torch's current stream on one
-_forward = None                    # torch.autograd.forward_ad
+_forward = _tracing = _modes = None   # torch.autograd.forward_ad; whether torch traces, has modes
 _codes = {}
 
 
 def _start():
     """torch and the element types' codes, on the first use."""
-    global _torch, _current_device, _stream, _forward
+    global _torch, _current_device, _stream, _forward, _tracing, _modes
     import torch
     import torch.autograd.forward_ad
     c = torch._C
-    _forward = torch.autograd.forward_ad
+    _forward, _tracing, _modes = torch.autograd.forward_ad, c._is_tracing, c._len_torch_dispatch_stack
     _current_device = getattr(c, "_cuda_getDevice", torch.cuda.current_device)
     _stream = getattr(c, "_cuda_getCurrentRawStream",
                       lambda device: torch.cuda.current_stream(device).cuda_stream)
@@ -161,13 +161,13 @@ def _eager(what, *tensors):
     """Refuses what would lose a call in silence: tensors (or None) with a tangent, which
     the result would not have (a derivative of zero), and traces, which would hold
     the result's allocation and not the kernels that fill it."""
-    if _forward._current_level >= 0:
-        for t in tensors:
-            if t is not None and _forward.unpack_dual(t).tangent is not None:
-                raise RuntimeError(f"{what} has no derivative forwards")
+    if _forward._current_level < 0 and not _tracing() and not _modes():
+        return
+    for t in tensors:
+        if t is not None and _forward.unpack_dual(t).tangent is not None:
+            raise RuntimeError(f"{what} has no derivative forwards")
     c = _torch._C
-    if c._is_tracing() or (c._len_torch_dispatch_stack()
-                           and c._get_dispatch_mode(c._TorchDispatchModeKey.PROXY) is not None):
+    if _tracing() or c._get_dispatch_mode(c._TorchDispatchModeKey.PROXY) is not None:
         raise RuntimeError(f"{what} cannot be traced")
 
 
