@@ -570,7 +570,8 @@ __global__ __launch_bounds__(256) void route_grad_kernel(RouteGradJob j)
     }
 #pragma unroll
     for (int i = 0; i < PER; ++i)
-        if (i * 64 + lane < j.experts) ds[i * 64 + lane] = dense ? (float)(-s[i] / total * rest) : 0.0f;
+        if (i * 64 + lane < j.experts)   // (a total of 0: every logit is -inf)
+            ds[i * 64 + lane] = dense && total != 0.0 ? (float)(-s[i] / total * rest) : 0.0f;
     if (at >= 0) ds[at] = (float)mine;
     T *out = reinterpret_cast<T *>(j.dlogits) + token * j.ldd;
 #pragma unroll
