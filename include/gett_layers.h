@@ -154,7 +154,8 @@ gett_status_t gett_route(gett_dtype_t dtype, int64_t tokens, int experts, int k,
                          void *stream);
 
 /* dlogits <- the gradient of gett_route's weights (the choice is constant), from
- * its logits, its index and dweights (float, tokens x k). */
+ * its logits, its index and dweights (float, tokens x k).  Of a token whose weights
+ * are NaN all are NaN. */
 gett_status_t gett_route_grad(gett_dtype_t dtype, int64_t tokens, int experts, int k,
                               const void *logits, int64_t stride, int scoring, int renormalize,
                               double scale, const int32_t *index, const float *dweights,

@@ -520,7 +520,9 @@ struct RouteGradJob {
 //     softmax       dx = s (ds - sum(ds s)),  sigmoid  dx = ds s (1 - s)
 // where ds is dc at the chosen experts and 0 elsewhere.  The sum over ds s is zero
 // where the weights are renormalised: only a softmax that is not has a gradient
-// outside the chosen, and needs their scores.
+// outside the chosen, and needs their scores.  All logits are read all the same: a NaN
+// among them, or a +inf under a softmax, has made the token's weights NaN wherever it
+// is, and so its gradient is.
 template <typename T, int PER>
 __global__ __launch_bounds__(256) void route_grad_kernel(RouteGradJob j)
 {
@@ -536,16 +538,20 @@ __global__ __launch_bounds__(256) void route_grad_kernel(RouteGradJob j)
     if (at >= j.experts) at = -1;
     const float chosen = at >= 0 ? to_float(row[at]) : -__builtin_huge_valf();
     double g = at >= 0 ? j.scale * (double)j.dweights[token * j.k + lane] : 0.0;
+    float x[PER];
+    bool odd = false;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int e = i * 64 + lane;
+        x[i] = e < j.experts ? to_float(row[e]) : -__builtin_huge_valf();
+        odd |= x[i] != x[i] || (soft && x[i] == __builtin_huge_valf());
+    }
+    const bool nan = __any(odd);
     double s[PER], total = 1.0, rest = 0.0;
     float most = soft ? wave_max(chosen) : 0.0f;
     if (dense) {
-        float x[PER];
 #pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const int e = i * 64 + lane;
-            x[i] = e < j.experts ? to_float(row[e]) : -__builtin_huge_valf();
-            most = fmaxf(most, x[i]);
-        }
+        for (int i = 0; i < PER; ++i) most = fmaxf(most, x[i]);
         most = wave_max(most);
         total = 0.0;
 #pragma unroll
@@ -576,7 +582,8 @@ __global__ __launch_bounds__(256) void route_grad_kernel(RouteGradJob j)
     T *out = reinterpret_cast<T *>(j.dlogits) + token * j.ldd;
 #pragma unroll
     for (int i = 0; i < PER; ++i)
-        if (i * 64 + lane < j.experts) out[i * 64 + lane] = from_float<T>(ds[i * 64 + lane]);
+        if (i * 64 + lane < j.experts)
+            out[i * 64 + lane] = from_float<T>(nan ? __builtin_nanf("") : ds[i * 64 + lane]);
 }
 
 // f(an integral constant of the experts a lane holds)

@@ -31,3 +31,37 @@ def test_route_gradient_of_a_token_without_experts(gpu, dtype, e, scoring, renor
     dx, = torch.autograd.grad(g.route(leaf, k, **how).weights, leaf, dw)
     want, = torch.autograd.grad(g.route(clean, k, **how).weights, clean, dw[1::2])
     assert bool((dx[::2] == 0).all()) and torch.equal(dx[1::2], want)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("e,groups", [(8, 1), (64, 4), (200, 1), (1000, 1)])
+@pytest.mark.parametrize("scoring", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("renormalize", [True, False])
+def test_route_gradient_where_weights_are_nan(gpu, dtype, e, groups, scoring, renormalize):
+    """A token whose weights are NaN has a gradient of NaN, whether or not what makes
+    them so was chosen; the others' is theirs."""
+    inf, k = math.inf, 3
+    x = rand(e, 8, e, dtype=dtype)
+    x[1, 3] = math.nan
+    x[2, e - 1] = inf
+    x[3] = -inf
+    x[4] = math.nan
+    x[5, ::2] = -inf
+    x[6, ::2] = -inf
+    x[6, 1] = math.nan
+    bias = torch.zeros(e)
+    bias[e - 1] = -5.0                      # (of the infinity's expert: not chosen)
+    dw = rand(2, 8, k).to(gpu)
+    how = dict(scoring=scoring, bias=bias.to(gpu), groups=groups, top_groups=max(1, groups // 2),
+               renormalize=renormalize)
+    leaf = x.to(gpu).requires_grad_()
+    r = g.route(leaf, k, **how)
+    dx, = torch.autograd.grad(r.weights, leaf, dw)
+    nan = torch.tensor([False, True, scoring == "softmax", False, True, False, True, False], device=gpu)
+    assert torch.equal(r.weights.isnan(), nan[:, None].expand(8, k))
+    assert torch.equal(dx.isnan(), nan[:, None].expand(8, e))
+    assert not dx[3].any()
+    there = ~nan
+    clean = x.to(gpu)[there].requires_grad_()
+    want, = torch.autograd.grad(g.route(clean, k, **how).weights, clean, dw[there])
+    assert torch.equal(dx[there], want)
