@@ -101,7 +101,8 @@ struct BackwardProducts {
     bool wantX = false, wantW = false;
     // dX is m x k and sums over n, dW n x k and over m.  A launch of one for both saves 2.5
     // us, which may outweigh the better tiles for one of them.  (Both are planned also
-    // where one is wanted: a gradient does not depend on what else is.)
+    // where one is wanted, and shared sums are cut alike however many panels a stage has:
+    // a gradient does not depend on what else is.)
     void plan(gett_dtype_t t, int64_t m, int64_t n, int64_t k, int64_t experts)
     {
         auto of_x = [&](int only) { return product_plan(t, kRowsColumns, groupsX, m, k, n, experts, only); };

@@ -682,8 +682,14 @@ __device__ __forceinline__ void product_begin(Product<T, FORM == kColumnsColumns
     };
     int panels = t.empty ? 0 : (t.sum + KP - 1) / KP;
     if (t.shared >= 0) {
-        const int t0 = (int)quotient((uint32_t)(panels * t.slice), g.slices, g.slicesInv);
-        panels = (int)quotient((uint32_t)(panels * (t.slice + 1)), g.slices, g.slicesInv) - t0;
+        // A gradient in tiles of 64 has stages of one panel or two by how many workgroups
+        // its launch has, the other gradient's among them.  Its slices are whole pairs of
+        // panels in both, so that its sums do not depend on what else is wanted.
+        constexpr int CUT = FORM != kRowsRows && S::BM == 64 ? 2 / S::P : 1;
+        const int cuts = (panels + CUT - 1) / CUT;
+        const int t0 = CUT * (int)quotient((uint32_t)(cuts * t.slice), g.slices, g.slicesInv);
+        const int t1 = CUT * (int)quotient((uint32_t)(cuts * (t.slice + 1)), g.slices, g.slicesInv);
+        panels = min(t1, panels) - t0;
         M.p += t0 * (MCOL ? KP * M.ld : S::P * 128);
         N.p += t0 * (NCOL ? KP * N.ld : S::P * 128);
         M.extent -= t0 * KP;

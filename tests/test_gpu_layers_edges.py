@@ -65,3 +65,27 @@ def test_route_gradient_where_weights_are_nan(gpu, dtype, e, groups, scoring, re
     clean = x.to(gpu)[there].requires_grad_()
     want, = torch.autograd.grad(g.route(clean, k, **how).weights, clean, dw[there])
     assert torch.equal(dx[there], want)
+
+
+# products --------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype,m,n,k", [
+    (torch.bfloat16, 1280, 2560, 256), (torch.float16, 2560, 1280, 256), (torch.bfloat16, 2560, 2560, 128),
+    (torch.bfloat16, 2560, 768, 384), (torch.bfloat16, 1000, 2560, 320), (torch.float32, 640, 1280, 333),
+    (torch.float32, 200, 4096, 200), (torch.bfloat16, 300, 300, 2000), (torch.float32, 1023, 515, 1000)])
+def test_a_gradient_does_not_depend_on_what_else_is_wanted(gpu, dtype, m, n, k):
+    """With w frozen dx is what it is beside dw, bit by bit, whatever tiles the products
+    take and however many workgroups share their sums."""
+    x, w, b = rand(1, m, k, dtype=dtype), rand(2, n, k, dtype=dtype, scale=k ** -0.5), rand(3, n, dtype=dtype)
+    dy = rand(4, m, n, dtype=dtype).to(gpu)
+    tensors = [v.to(gpu) for v in (x, w, b)]
+
+    def gradients(*wanted):
+        leaves = [t.detach().requires_grad_(i in wanted) for i, t in enumerate(tensors)]
+        y = g.linear(*leaves, activation="silu")
+        return torch.autograd.grad(y, [leaves[i] for i in wanted], dy)
+
+    every = gradients(0, 1, 2)
+    for wanted in ((0,), (1,), (2,), (0, 1), (0, 2), (1, 2)):
+        for i, got in zip(wanted, gradients(*wanted)):
+            assert torch.equal(got, every[i]), (wanted, i)
