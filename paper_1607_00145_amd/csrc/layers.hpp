@@ -181,6 +181,16 @@ __device__ __forceinline__ void slope8(int kind, float v[8], const float z[8])
     else if (kind == GETT_ACTIVATION_RELU) each8(v, z, [](float g, float z) { return g * relu_slope(z); });
 }
 
+// Between one lane's store to LDS and another's load of it, in one wavefront: the
+// hardware does its LDS accesses in order, and this keeps the compiler from moving
+// them or from taking a lane's own earlier value.  No instruction of its own.
+__device__ __forceinline__ void wave_exchange()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // ------------------------------------------------------------------ vectors ---
 
 // Whole vectors at any element address.  (Stored element by element, eight numbers

@@ -796,6 +796,7 @@ __device__ __forceinline__ void product_work(const ProductArgs &g, int groups, i
                             f4{v[4 * a], v[4 * a + 1], v[4 * a + 2], v[4 * a + 3]};
                     }
             });
+            wave_exchange();
             Run<T, 8> residual[PASSES];
             float v[PASSES][8];
 #pragma unroll
@@ -810,6 +811,7 @@ __device__ __forceinline__ void product_work(const ProductArgs &g, int groups, i
                 }
                 residual[y] = ahead[y];
             }
+            wave_exchange();   // (all are read)
             if (step + 1 < STEPS) fetch(step + 1);
 #pragma unroll
             for (int y = 0; y < PASSES; ++y) {

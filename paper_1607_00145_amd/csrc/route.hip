@@ -107,6 +107,7 @@ __device__ __forceinline__ void choose_exactly(const RouteJob &j, int64_t token,
         keys[e] = c != c ? none : c;
     }
     if (j.groups > 1) {
+        wave_exchange();   // a group's keys are other lanes' than the group
         const int size = j.experts / j.groups;
         uint32_t open = 0;   // of this lane's groups
         for (int r = 0; r < j.topGroups; ++r) {
@@ -125,6 +126,7 @@ __device__ __forceinline__ void choose_exactly(const RouteJob &j, int64_t token,
             if (best.key == none) break;
             if ((best.at & 63) == lane) open |= 1u << (best.at >> 6);
         }
+        wave_exchange();   // (all are read)
         for (int e0 = 0; e0 < j.experts; e0 += 64) {
             const int e = e0 + lane, g = e < j.experts ? e / size : 0;
             const uint32_t bits = __shfl(open, g & 63);
@@ -578,7 +580,9 @@ __global__ __launch_bounds__(256) void route_grad_kernel(RouteGradJob j)
     for (int i = 0; i < PER; ++i)
         if (i * 64 + lane < j.experts)   // (a total of 0: every logit is -inf)
             ds[i * 64 + lane] = dense && total != 0.0 ? (float)(-s[i] / total * rest) : 0.0f;
+    wave_exchange();
     if (at >= 0) ds[at] = (float)mine;
+    wave_exchange();
     T *out = reinterpret_cast<T *>(j.dlogits) + token * j.ldd;
 #pragma unroll
     for (int i = 0; i < PER; ++i)
