@@ -220,11 +220,11 @@ def _activation(name):
 
 def _drop(p, seed, offset):
     """(p, seed's value, offset, seed's tensor or None) with the checks; None for
-    no dropout."""
+    no dropout, as p is rounded."""
     p = float(p)
     if not 0.0 <= p <= 1.0:
         raise ValueError("p must be in [0, 1]")
-    if p == 0.0:
+    if round(p * 65536) == 0:
         return None
     if seed is None:
         raise ValueError("dropout needs a seed")
@@ -409,9 +409,11 @@ def _dropout(x, drop, seed):
 def dropout(x, p: float, seed, offset: int = 0):
     """x / (1 - p) where a counter-based generator keeps it and 0 elsewhere.
 
-    With p = 0 it is x itself.  `p` is rounded to a multiple of 2^-16.  The mask is a function of `seed`, `offset`
-    and a number's row (over all leading dimensions) and column: a call with the same
-    seed and offset has the same mask, and the gradient makes it again.  `seed` is an
+    `p` is rounded to a multiple of 2^-16.  With p = 0 (up to 2^-17) the result is x
+    itself, not a copy, as torch's own dropout returns it.  The mask is a function of
+    `seed`, `offset` and a number's row (over all leading dimensions) and column: a
+    call with the same seed and offset has the same mask, and the gradient makes it
+    again.  `seed` is an
     integer, or an int64 device tensor of one element that is read when the kernel
     runs (a captured graph draws a new mask when it changes between replays; it must
     not change between a call and its gradient)."""

@@ -89,3 +89,15 @@ def test_a_gradient_does_not_depend_on_what_else_is_wanted(gpu, dtype, m, n, k):
     for wanted in ((0,), (1,), (2,), (0, 1), (0, 2), (1, 2)):
         for i, got in zip(wanted, gradients(*wanted)):
             assert torch.equal(got, every[i]), (wanted, i)
+
+
+@pytest.mark.parametrize("p", [1e-6, 2.0 ** -17])
+def test_a_probability_that_rounds_to_none(gpu, p):
+    """It is p = 0: the same tensor comes back whatever the small number was."""
+    x = rand(1, 20, 40).to(gpu)
+    assert g.dropout(x, p, 5) is x and g.dropout(x, p, None) is x
+    assert g.dropout(x, 2.0 ** -16, 5) is not x
+    leaf = x.clone().requires_grad_()
+    assert g.dropout(leaf, p, 5) is leaf
+    w = rand(2, 30, 40).to(gpu)
+    assert torch.equal(g.linear(x, w, activation="gelu", p=p, seed=3), g.linear(x, w, activation="gelu"))
