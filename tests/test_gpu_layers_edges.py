@@ -91,6 +91,90 @@ def test_a_gradient_does_not_depend_on_what_else_is_wanted(gpu, dtype, m, n, k):
             assert torch.equal(got, every[i]), (wanted, i)
 
 
+def wider(t, more):
+    """A matrix of t's shape in rows that are `more` numbers wider, those of 7."""
+    base = torch.full((t.shape[0], t.shape[1] + more), 7.0, dtype=t.dtype, device=t.device)
+    view = base[:, :t.shape[1]]
+    view.copy_(t)
+    return base, view
+
+
+def drop_of(p, seed):
+    return g.gett_dropout_t(p, seed, 0, None)
+
+
+@pytest.mark.parametrize("more", [0, 5])
+@pytest.mark.parametrize("dtype,m,n,k,edge,shared", [
+    (torch.bfloat16, 8300, 7900, 328, 256, False), (torch.bfloat16, 4487, 4507, 4104, 256, True),
+    (torch.float16, 3085, 2579, 40, 128, False), (torch.bfloat16, 2317, 3380, 4104, 128, True),
+    (torch.float16, 3789, 1070, 520, 64, False), (torch.bfloat16, 4151, 97, 4104, 64, True),
+    (torch.bfloat16, 4165, 197, 328, 32, False), (torch.float32, 2525, 3276, 40, 128, False),
+    (torch.float32, 353, 3403, 4104, 128, True), (torch.float32, 3691, 611, 1032, 64, True),
+    (torch.float32, 201, 145, 40, 32, False), (torch.float16, 1, 700, 264, 0, False),
+    (torch.float32, 3, 700, 261, 0, False)])
+def test_residual_in_place(gpu, dtype, m, n, k, edge, shared, more):
+    """Y may be the residual itself: the same result, bit by bit, in every kind of tile."""
+    t = product_tiles(CODES[dtype], m, n, k)
+    assert t.edge == edge and (t.slices > 1) == shared
+    x, w, bias = (on_gpu(v) for v in (rand(1, m, k, dtype=dtype), rand(2, n, k, dtype=dtype, scale=k ** -0.5),
+                                      rand(3, n, dtype=dtype)))
+    residual = rand(4, m, n, dtype=dtype).to(gpu)
+    want = g.linear(x, w, bias, activation="gelu", residual=residual, p=0.25, seed=9)
+    base, y = wider(residual, more)
+    st = g.gett_linear(CODES[dtype], m, n, k, x.data_ptr(), k, w.data_ptr(), k, bias.data_ptr(), 2,
+                       drop_of(0.25, 9), y.data_ptr(), n + more, 0, n, y.data_ptr(), n + more,
+                       torch.cuda.current_stream().cuda_stream)
+    assert st == 0
+    assert torch.equal(y, want) and bool((base[:, n:] == 7).all())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("m", [5, 32])
+def test_residual_in_place_of_few_rows(gpu, dtype, m):
+    """The same of rows that a weight at an odd address is multiplied with."""
+    n, k = 70, 203
+    x, bias = rand(1, m, k, dtype=dtype).to(gpu), rand(3, n, dtype=dtype).to(gpu)
+    w = rand(2, n, k + 2, dtype=dtype).to(gpu)[:, 1:k + 1]
+    residual = rand(4, m, n, dtype=dtype).to(gpu)
+    want = g.linear(x, w, bias, activation="silu", residual=residual)
+    y = residual.clone()
+    st = g.gett_linear(CODES[dtype], m, n, k, x.data_ptr(), k, w.data_ptr(), k + 2, bias.data_ptr(), 3, None,
+                       y.data_ptr(), n, 0, n, y.data_ptr(), n, torch.cuda.current_stream().cuda_stream)
+    assert st == 0 and torch.equal(y, want)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("t,e,k,cols,more", [(1, 2, 1, 1, 0), (9, 8, 8, 100, 3), (70, 5, 2, 515, 0),
+                                             (333, 40, 6, 1024, 8)])
+def test_combine_in_place(gpu, dtype, t, e, k, cols, more):
+    logits = rand(1, t, e)
+    logits[t // 2] = -math.inf
+    r = g.route(logits.to(gpu), k)
+    h, residual = rand(2, t * k, cols, dtype=dtype).to(gpu), rand(5, t, cols, dtype=dtype).to(gpu)
+    want = g.combine(h, r, residual=residual)
+    base, y = wider(residual, more)
+    st = g.gett_combine(CODES[dtype], t, k, cols, h.data_ptr(), cols, g.GETT_FLOAT32, r.weights.data_ptr(),
+                        r.place.data_ptr(), y.data_ptr(), cols + more, y.data_ptr(), cols + more,
+                        torch.cuda.current_stream().cuda_stream)
+    assert st == 0
+    assert torch.equal(y, want) and bool((base[:, cols:] == 7).all())
+
+
+# dropout ---------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("p", [0.1, 0.3, 0.5])
+def test_dropout_and_its_gradient_number_by_number(gpu, dtype, p):
+    """One product in 32 bits with the mask's factor in 32 bits, rounded once."""
+    rows, cols = 165, 77
+    factor = lu.mask(rows, cols, p, 11, 3).float().to(gpu)
+    x, dy = rand(2, rows, cols, dtype=dtype).to(gpu).requires_grad_(), rand(3, rows, cols, dtype=dtype).to(gpu)
+    y = g.dropout(x, p, 11, 3)
+    dx, = torch.autograd.grad(y, x, dy)
+    assert torch.equal(y.detach(), (x.detach().float() * factor).to(dtype))
+    assert torch.equal(dx, (dy.float() * factor).to(dtype))
+
+
 @pytest.mark.parametrize("p", [1e-6, 2.0 ** -17])
 def test_a_probability_that_rounds_to_none(gpu, p):
     """It is p = 0: the same tensor comes back whatever the small number was."""
