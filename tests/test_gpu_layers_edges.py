@@ -185,3 +185,43 @@ def test_a_probability_that_rounds_to_none(gpu, p):
     assert g.dropout(leaf, p, 5) is leaf
     w = rand(2, 30, 40).to(gpu)
     assert torch.equal(g.linear(x, w, activation="gelu", p=p, seed=3), g.linear(x, w, activation="gelu"))
+
+
+# memory ----------------------------------------------------------------------
+
+@pytest.mark.parametrize("apart", [(1 << 23) - 8, 1 << 23, (1 << 23) + 8])
+def test_rows_far_apart(gpu, apart):
+    """Rows of 16 bits 16 MB apart, about as far as a tile reaches them where they lie."""
+    m, n, k = 260, 40, 72
+    x, w, dy = (rand(i, *s, dtype=torch.bfloat16).to(gpu) for i, s in ((1, (m, k)), (2, (n, k)), (3, (m, n))))
+    far = torch.empty(m * apart, dtype=torch.bfloat16, device=gpu).as_strided((m, k), (apart, 1))
+    far.copy_(x)
+    results = []
+    for v in (x, far):
+        leaves = [v.detach().requires_grad_(), w.detach().requires_grad_()]
+        y = g.linear(*leaves)
+        results.append([y.detach(), *torch.autograd.grad(y, leaves, dy)])
+    assert all(torch.equal(a, b) for a, b in zip(*results))
+    for v in (dy, torch.empty(m * apart, dtype=torch.bfloat16, device=gpu).as_strided((m, n), (apart, 1)).copy_(dy)):
+        leaves = [x.detach().requires_grad_(), w.detach().requires_grad_()]
+        results.append(list(torch.autograd.grad(g.linear(*leaves), leaves, v)))
+    assert all(torch.equal(a, b) for a, b in zip(results[2], results[3]))
+
+
+@pytest.mark.parametrize("t", [(1 << 20) + 3, (1 << 21) - 9])
+def test_gathered_rows_beyond_4_gb(gpu, t):
+    """Tokens of more than 2^32 bytes: the last ones' rows are theirs."""
+    d, n, e = 2048, 24, 3
+    x = torch.empty(t, d, dtype=torch.bfloat16, device=gpu)
+    x[:] = torch.arange(t, device=gpu)[:, None] % 127      # (whole numbers: 16 bits hold them)
+    w = torch.zeros(e, n, d, dtype=torch.bfloat16, device=gpu)
+    w[:, :, 0] = torch.arange(1, e + 1, device=gpu)[:, None]
+    logits = torch.zeros(t, e, device=gpu)
+    logits[torch.arange(t, device=gpu), torch.arange(t, device=gpu) % e] = 5.0
+    r = g.route(logits, 1)
+    y = g.expert_linear(x, w, r, gather=True)
+    back = g.combine(y, r, weights=torch.ones(t, 1, device=gpu))
+    token = torch.arange(t, device=gpu)
+    want = (token % 127).float() * (token % e + 1)
+    # (up to 378: bf16 holds every second one of those beyond 256)
+    assert torch.equal(back.float(), want.to(torch.bfloat16).float()[:, None].expand(t, n))
