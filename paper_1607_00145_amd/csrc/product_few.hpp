@@ -157,8 +157,9 @@ __global__ __launch_bounds__(64 * kFewWaves) void product_few_kernel(ProductArgs
 // after the other, so that every load is a run of whole lines; its lanes multiply
 // their 16 bytes with x's, and sum up across the wavefront at the end.  The sixteen
 // wavefronts of a workgroup have up to 128 KB on their way.  Bound by the weights' bytes:
-// one bf16 row with 8192 x 4096 takes 14 us (4.8 TB/s; 20 us in the kernel above),
-// eight experts of 1024 x 2048 for a token 9 (33 MB, and the launch).
+// eight experts of 1024 x 2048 for a token in bf16 take 9 us (33 MB, and the launch), one
+// row with 2048 x 2048 4.7.  (Where the blocks of 32 columns fill the card they are
+// faster: 8192 x 4096 takes 14 us here, 20 in the kernel above, 12 in those.)
 constexpr int kRowWaves = 16;
 
 template <typename T, int R>

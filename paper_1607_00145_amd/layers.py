@@ -413,10 +413,9 @@ def dropout(x, p: float, seed, offset: int = 0):
     itself, not a copy, as torch's own dropout returns it.  The mask is a function of
     `seed`, `offset` and a number's row (over all leading dimensions) and column: a
     call with the same seed and offset has the same mask, and the gradient makes it
-    again.  `seed` is an
-    integer, or an int64 device tensor of one element that is read when the kernel
-    runs (a captured graph draws a new mask when it changes between replays; it must
-    not change between a call and its gradient)."""
+    again.  `seed` is an integer, or an int64 device tensor of one element that is read
+    when the kernel runs (a captured graph draws a new mask when it changes between
+    replays; it must not change between a call and its gradient)."""
     if _bound is None:
         _start()
     flat = _flat("x", x)
