@@ -150,9 +150,14 @@ def gett_combine_grad(dtype: int, tokens: int, k: int, cols: int, dY: int, strid
 
 # ------------------------------------------------------ torch convenience ---
 
+_forward = _tracing = _modes = None   # as matrix.py has them
+
+
 def _start():
+    global _forward, _tracing, _modes
     if _m._torch is None:
         _m._start()
+    _forward, _tracing, _modes = _m._forward, _m._tracing, _m._modes
     if _bound is None:
         _lib()
     return _m._torch
@@ -285,7 +290,8 @@ def _make_functions():
         # derivatives: what depends on the gradients then raises, even where the
         # gradient that came in is a constant.
         def backward(ctx, *dy):
-            _m._eager("a gradient of the layers' operators", *dy)
+            if _forward._current_level >= 0 or _tracing() or _modes():
+                _m._eager("a gradient of the layers' operators", *dy)
             if not torch.is_grad_enabled():
                 return gradients(ctx, *dy)
             with torch.no_grad():
@@ -416,7 +422,7 @@ def dropout(x, p: float, seed, offset: int = 0):
     again.  `seed` is an integer, or an int64 device tensor of one element that is read
     when the kernel runs (a captured graph draws a new mask when it changes between
     replays; it must not change between a call and its gradient)."""
-    if _bound is None:
+    if _forward is None:
         _start()
     flat = _flat("x", x)
     _m._code(x.dtype)
@@ -424,7 +430,8 @@ def dropout(x, p: float, seed, offset: int = 0):
     drop = _drop(p, seed, offset)
     if drop is None:
         return x
-    _m._eager("dropout", flat)
+    if _forward._current_level >= 0 or _tracing() or _modes():
+        _m._eager("dropout", flat)
     if _records(x):
         y = _function("dropout").apply(flat, drop[3], drop)
     else:
@@ -495,7 +502,7 @@ def linear(x, w, bias=None, activation=None, residual=None, p: float = 0.0, seed
     are those of `dropout`.  All tensors have one type; sums and the epilogue are in
     32 bits and rounded once.  Differentiable in x, w, bias and residual: for the
     gradient x @ w.T + bias is kept where there is an activation, and no mask."""
-    if _bound is None:
+    if _forward is None:
         _start()
     _m._code(x.dtype)
     code = _activation(activation)
@@ -511,7 +518,8 @@ def linear(x, w, bias=None, activation=None, residual=None, p: float = 0.0, seed
     seed = None if drop is None else drop[3]
     _m._device("x", x)
     _m._device("w", w)
-    _m._eager("linear", flat, w, bias, residual)
+    if _forward._current_level >= 0 or _tracing() or _modes():
+        _m._eager("linear", flat, w, bias, residual)
     if _records(x, w, bias, residual):
         y = _function("linear").apply(flat, w, bias, residual, seed, code, drop)
     else:
@@ -610,13 +618,14 @@ def route(logits, k: int, scoring: str = "softmax", bias=None, groups: int = 1,
     are the scores of the chosen, divided by their sum unless `renormalize` is false,
     times `scale`.  Ties go to the lowest index.  An expert whose logit is -inf is never
     chosen: where fewer than k are open the last indices are -1 and their weights 0."""
-    if _bound is None:
+    if _forward is None:
         _start()
     _m._code(logits.dtype)
     if logits.dim() != 2:
         raise ValueError("logits must be a matrix (tokens x experts)")
     _m._device("logits", logits)
-    _m._eager("route", logits, bias)
+    if _forward._current_level >= 0 or _tracing() or _modes():
+        _m._eager("route", logits, bias)
     if scoring not in SCORES:
         raise ValueError(f"scoring must be one of {sorted(SCORES)}")
     t, e = logits.shape
@@ -706,7 +715,7 @@ def expert_linear(x, w, routing: Routing, bias=None, activation=None, gather: bo
     With `gather` x has a row for each token (tokens x width); otherwise a row for each
     row of the result, as another `expert_linear` returns them.  `w` is experts x n x
     width, `bias` experts x n.  Differentiable in x, w and bias."""
-    if _bound is None:
+    if _forward is None:
         _start()
     _m._code(x.dtype)
     code = _activation(activation)
@@ -725,7 +734,8 @@ def expert_linear(x, w, routing: Routing, bias=None, activation=None, gather: bo
             _m._device(name, t)
     if bias is not None and bias.shape != w.shape[:2]:
         raise ValueError(f"bias must be {w.shape[0]} x {w.shape[1]}")
-    _m._eager("expert_linear", x, w, bias)
+    if _forward._current_level >= 0 or _tracing() or _modes():
+        _m._eager("expert_linear", x, w, bias)
     if _records(x, w, bias):
         return _function("experts").apply(x, w, bias, routing, code, bool(gather))
     return _experts(x, w, bias, routing, code, bool(gather), None)
@@ -784,7 +794,7 @@ def combine(h, routing: Routing, weights=None, residual=None):
 
     `h` has the rows of `expert_linear`; `weights` are tokens x k, in float32 or h's
     type (default: the routing's).  Differentiable in h, weights and residual."""
-    if _bound is None:
+    if _forward is None:
         _start()
     _m._code(h.dtype)
     _m._device("h", h)
@@ -800,7 +810,8 @@ def combine(h, routing: Routing, weights=None, residual=None):
     _m._device("weights", weights)
     if residual is not None and tuple(residual.shape) != (t, h.shape[1]):
         raise ValueError("residual differs from the result in shape")
-    _m._eager("combine", h, weights, residual)
+    if _forward._current_level >= 0 or _tracing() or _modes():
+        _m._eager("combine", h, weights, residual)
     if _records(h, weights, residual):
         return _function("combine").apply(h, weights, residual, routing)
     return _combine(h, weights, residual, routing)

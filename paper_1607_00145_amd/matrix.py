@@ -160,9 +160,8 @@ def _device(name, t):
 def _eager(what, *tensors):
     """Refuses what would lose a call in silence: tensors (or None) with a tangent, which
     the result would not have (a derivative of zero), and traces, which would hold
-    the result's allocation and not the kernels that fill it."""
-    if _forward._current_level < 0 and not _tracing() and not _modes():
-        return
+    the result's allocation and not the kernels that fill it.  Callers ask in line
+    whether either may be (a call for that would be 0.2 us of a token's 7.5)."""
     for t in tensors:
         if t is not None and _forward.unpack_dual(t).tangent is not None:
             raise RuntimeError(f"{what} has no derivative forwards")
@@ -196,11 +195,11 @@ def _matrix(name, t):
     code = _code(t.dtype)
     if not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
-    if t.is_neg():
-        raise ValueError(f"{name} is a lazily negated view: resolve_neg() it first")
     (r, c), (sr, sc) = shape, t.stride()
     if sr < 1 or sc < 1 or r < 2 or c < 2:
         sr, sc = _strides(t)
+    elif sc != 1 and sr != 1:
+        _not_negated(t)
     return code, r, c, sr, sc
 
 
@@ -212,13 +211,21 @@ def _no_gradient(what, *tensors):
                                "torch.no_grad() (mx_linear with a float weight has one)")
 
 
+def _not_negated(t):
+    """Refuses torch's lazily negated views, whose memory holds other values than they
+    have: imaginary parts of conjugates, so that no two of their numbers are
+    neighbours."""
+    if t.is_neg():
+        raise ValueError("a lazily negated view: resolve_neg() it first")
+
+
 def _strides(t):
     """(row, column) strides of the last two directions; one of extent one may
     carry any (torch leaves what it likes there, 0 included)."""
     sr, sc = t.stride()[-2:]
     r, c = t.shape[-2:]
-    if t.is_neg():
-        raise ValueError("a lazily negated view: resolve_neg() it first")
+    if (sc != 1 or c == 1) and (sr != 1 or r == 1):
+        _not_negated(t)
     if r > 1 and sr < 1 or c > 1 and sc < 1:
         raise ValueError("a broadcast (zero-stride) matrix: copy it first")
     return (sr if r > 1 else max(c, 1)), (sc if c > 1 else 1)
@@ -279,7 +286,8 @@ class MXTensor:
         r, c = self.rows, self.cols
         if _torch is None:
             _start()
-        _eager("dequantize", out)
+        if _forward._current_level >= 0 or _tracing() or _modes():
+            _eager("dequantize", out)
         i = self._device
         if out is not None or i != _current_device():
             there = _elsewhere(self, out)
@@ -321,7 +329,8 @@ def mx_quantize(x, along: str = "cols"):
     if along not in ("cols", "rows", "both"):
         raise ValueError("along must be 'cols', 'rows' or 'both'")
     code, r, c, sr, sc = _matrix("x", x)
-    _eager("mx_quantize")
+    if _forward._current_level >= 0 or _tracing() or _modes():
+        _eager("mx_quantize")
     i = x.get_device()
     if i != _current_device():
         with _elsewhere(x):
@@ -370,7 +379,8 @@ def mx_matmul(a, b, C=None, alpha: float = 1.0, beta: float = 0.0, dtype=None):
         raise ValueError(f"a has {k} columns, b {b.cols}")
     if _torch is None:
         _start()
-    _eager("mx_matmul", None if packed else a, C)
+    if _forward._current_level >= 0 or _tracing() or _modes():
+        _eager("mx_matmul", None if packed else a, C)
     i = b._device
     if C is not None or not i == a.get_device() == _current_device():
         there = _elsewhere(a, b, C)
@@ -466,7 +476,8 @@ def _linear_function():
             return recorded(ctx, dy) if torch.is_grad_enabled() else gradients(ctx, dy)
 
     def gradients(ctx, dy):
-        _eager("a gradient of mx_linear", dy)
+        if _forward._current_level >= 0 or _tracing() or _modes():
+            _eager("a gradient of mx_linear", dy)
         need_x, need_w = ctx.needs_input_grad
         m, n, k, tx, tw = ctx.sizes
         if dy.is_neg():
@@ -506,7 +517,8 @@ def mx_linear(x, w):
         y = mx_matmul(flat, w)
     else:
         _code(x.dtype)
-        _eager("mx_linear", flat, w)
+        if _forward._current_level >= 0 or _tracing() or _modes():
+            _eager("mx_linear", flat, w)
         if _torch.is_grad_enabled() and (x.requires_grad or w.requires_grad):
             y = _linear_function().apply(flat, w)
         else:
@@ -524,7 +536,8 @@ def orthogonalize(G, steps: int = 5, coefficients=(3.4445, -4.7750, 2.0315), eps
         raise ValueError("a matrix or a stack of matrices is needed")
     code = _code(G.dtype)
     _device("G", G)
-    _eager("orthogonalize", G, out)
+    if _forward._current_level >= 0 or _tracing() or _modes():
+        _eager("orthogonalize", G, out)
     there = _elsewhere(G, out)
     if there is not None:
         with there:

@@ -2,6 +2,9 @@
 traces and lazily negated views.  The tensors are CPU tensors that claim to lie on a
 device, and the library's functions a record."""
 import ctypes
+import os
+import subprocess
+import sys
 
 import pytest
 import torch
@@ -256,3 +259,17 @@ def test_negated_matrices_of_the_4_bit_operators(seen):
     y = g.mx_linear(x, on(48, 64))
     torch.autograd.grad(y, x, claims(negated(6, 48)))
     assert found == [[-2.0]]
+
+
+def test_a_call_of_the_c_interface_first():
+    """It loads the library without torch, which the other calls then look up."""
+    code = ("import paper_1607_00145_amd as g\n"
+            "assert g.gett_dropout(7, 1, 1, 0, 1, None, 0, 1) == 1\n"
+            "import torch\n"
+            "for call in (lambda x: g.dropout(x, 0.5, 1), lambda x: g.linear(x, x), lambda x: g.route(x, 1)):\n"
+            "    try: call(torch.zeros(4, 4))\n"
+            "    except ValueError as e: assert 'device' in str(e)\n"
+            "    else: assert False\n"
+            "assert g.layers._forward is not None and g.layers._tracing is not None\n")
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    subprocess.run([sys.executable, "-c", code], check=True, cwd=root)
