@@ -225,3 +225,149 @@ def test_gathered_rows_beyond_4_gb(gpu, t):
     want = (token % 127).float() * (token % e + 1)
     # (up to 378: bf16 holds every second one of those beyond 256)
     assert torch.equal(back.float(), want.to(torch.bfloat16).float()[:, None].expand(t, n))
+
+
+# one gradient without the others -------------------------------------------------
+
+def subsets(n):
+    return [[i for i in range(n) if bits >> i & 1] for bits in range(1, 1 << n)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("name,p", [(None, 0.0), (None, 0.3), ("gelu", 0.3)])
+@pytest.mark.parametrize("m,n,k", [(1, 24, 40), (37, 51, 29), (300, 136, 264)])
+def test_every_choice_of_gradients(gpu, dtype, name, p, m, n, k):
+    tensors = [v.to(gpu) for v in (rand(1, m, k, dtype=dtype), rand(2, n, k, dtype=dtype, scale=k ** -0.5),
+                                   rand(3, n, dtype=dtype), rand(5, m, n, dtype=dtype))]
+    dy = rand(4, m, n, dtype=dtype).to(gpu)
+
+    def gradients(wanted):
+        leaves = [t.detach().requires_grad_(i in wanted) for i, t in enumerate(tensors)]
+        y = g.linear(*leaves[:3], activation=name, residual=leaves[3], p=p, seed=3)
+        return torch.autograd.grad(y, [leaves[i] for i in wanted], dy)
+
+    every = gradients(range(4))
+    for wanted in subsets(4):
+        assert all(torch.equal(v, every[i]) for i, v in zip(wanted, gradients(wanted))), wanted
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("gather", [True, False])
+@pytest.mark.parametrize("t,e,k,width,n", [(1, 4, 2, 40, 24), (90, 6, 2, 77, 51), (700, 4, 2, 520, 264),
+                                           (2000, 8, 1, 256, 512)])
+def test_every_choice_of_the_experts_gradients(gpu, dtype, gather, t, e, k, width, n):
+    logits = rand(1, t, e)
+    logits[t // 2] = -math.inf
+    r = g.route(logits.to(gpu), k)
+    tensors = [v.to(gpu) for v in (rand(2, t if gather else t * k, width, dtype=dtype),
+                                   rand(3, e, n, width, dtype=dtype, scale=width ** -0.5), rand(4, e, n, dtype=dtype))]
+    dy = rand(5, t * k, n, dtype=dtype).to(gpu)
+
+    def gradients(wanted):
+        leaves = [v.detach().requires_grad_(i in wanted) for i, v in enumerate(tensors)]
+        y = g.expert_linear(leaves[0], leaves[1], r, leaves[2], activation="silu", gather=gather)
+        return torch.autograd.grad(y, [leaves[i] for i in wanted], dy)
+
+    every = gradients(range(3))
+    for wanted in subsets(3):
+        assert all(torch.equal(v, every[i]) for i, v in zip(wanted, gradients(wanted))), wanted
+    h, weights, residual = (rand(i, *s, dtype=dtype).to(gpu) for i, s in ((6, (t * k, n)), (7, (t, k)), (8, (t, n))))
+    back = rand(9, t, n, dtype=dtype).to(gpu)
+
+    def combined(wanted):
+        leaves = [v.detach().requires_grad_(i in wanted) for i, v in enumerate((h, weights, residual))]
+        y = g.combine(leaves[0], r, weights=leaves[1], residual=leaves[2])
+        return torch.autograd.grad(y, [leaves[i] for i in wanted], back)
+
+    every = combined(range(3))
+    for wanted in subsets(3):
+        assert all(torch.equal(v, every[i]) for i, v in zip(wanted, combined(wanted))), wanted
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("gather", [True, False])
+@pytest.mark.parametrize("t,width,n", [(1, 0, 8), (50, 0, 24), (50, 16, 0), (300, 0, 40), (0, 8, 16)])
+def test_experts_of_empty_extents(gpu, dtype, gather, t, width, n):
+    e, k = 3, 2
+    r = g.route(rand(1, t, e).to(gpu), k)
+    x = torch.zeros(t if gather else t * k, width, dtype=dtype, device=gpu).requires_grad_()
+    w = torch.zeros(e, n, width, dtype=dtype, device=gpu).requires_grad_()
+    b = rand(2, e, n, dtype=dtype).to(gpu).requires_grad_()
+    y = g.expert_linear(x, w, r, b, activation="relu", gather=gather)
+    expert = torch.repeat_interleave(torch.arange(e, device=gpu), r.offsets.diff().long())
+    assert torch.equal(y, b.detach().relu()[expert])
+    dx, dw, db = torch.autograd.grad(y, (x, w, b), torch.ones_like(y))
+    assert dx.shape == x.shape and dw.shape == w.shape and not dx.any() and not dw.any()
+    count = r.offsets.diff()[:, None].to(dtype)
+    assert torch.equal(db, torch.where(b.detach() > 0, count, torch.zeros_like(count)))
+    assert torch.equal(g.combine(y, r, weights=torch.ones(t, k, device=gpu)).float(),
+                       torch.zeros(t, n, device=gpu) if not t or not n else
+                       (y.detach().float()[r.place.long()].sum(1).to(dtype).float()))
+
+
+# numbers that are none, in places that do not count -----------------------------
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("gather", [True, False])
+@pytest.mark.parametrize("t,e,k,width,n", [(9, 4, 2, 40, 24), (40, 16, 2, 77, 51), (130, 6, 2, 64, 72),
+                                           (700, 4, 2, 520, 264)])
+def test_nan_of_tokens_without_experts(gpu, dtype, gather, t, e, k, width, n):
+    """Rows of no expert, and gradients of such, are not read into anybody's sums."""
+    logits = rand(1, t, e)
+    logits[1::3] = -math.inf
+    r = g.route(logits.to(gpu), k)
+    live = int(r.offsets[-1])
+    w, b = rand(3, e, n, width, dtype=dtype).to(gpu), rand(4, e, n, dtype=dtype).to(gpu)
+    x, dy = rand(2, t if gather else t * k, width, dtype=dtype).to(gpu), rand(5, t * k, n, dtype=dtype).to(gpu)
+    back = rand(6, t, n, dtype=dtype).to(gpu)
+    results = []
+    for bad in (0.0, math.nan, math.inf):
+        x, dy, back = x.clone(), dy.clone(), back.clone()
+        if gather:
+            x[1::3] = bad
+        else:
+            x[live:] = bad
+        dy[live:] = bad
+        leaves = [v.detach().requires_grad_() for v in (x, w, b)]
+        y = g.expert_linear(leaves[0], leaves[1], r, leaves[2], activation="gelu", gather=gather)
+        out = [y.detach(), *torch.autograd.grad(y, leaves, dy)]
+        h = y.detach().clone()
+        h[live:] = bad
+        back[1::3] = bad
+        more = [h.requires_grad_(), r.weights.detach().requires_grad_()]
+        z = g.combine(more[0], r, weights=more[1])
+        dh, dw = torch.autograd.grad(z, more, back)
+        results.append(out + [z.detach(), dh, dw])
+    for other in results[1:]:
+        for i, (a, c) in enumerate(zip(results[0], other)):
+            assert not c.isnan().any() and torch.equal(a, c), i
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("m,n,k", [(1, 70, 40), (20, 70, 41), (150, 96, 72), (300, 260, 264)])
+def test_nan_of_one_row_stays_in_it(gpu, dtype, m, n, k):
+    x, w, b = rand(1, m, k, dtype=dtype).to(gpu), rand(2, n, k, dtype=dtype).to(gpu), rand(3, n, dtype=dtype).to(gpu)
+    dy, row = rand(4, m, n, dtype=dtype).to(gpu), m // 2
+    want = g.linear(x, w, b, activation="silu")
+    x[row, k - 1] = math.nan
+    leaf = x.requires_grad_()
+    y = g.linear(leaf, w, b, activation="silu")
+    dx, = torch.autograd.grad(y, leaf, dy)
+    others = torch.arange(m, device=gpu) != row
+    assert y[row].isnan().all() and torch.equal(y[others], want[others])
+    assert dx[row].isnan().all() and not dx[others].isnan().any()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("m,n,k", [(1, 70, 40), (20, 70, 41), (300, 260, 264)])
+def test_gradients_that_are_dropped_do_not_count(gpu, dtype, m, n, k):
+    x, w, b = rand(1, m, k, dtype=dtype).to(gpu), rand(2, n, k, dtype=dtype).to(gpu), rand(3, n, dtype=dtype).to(gpu)
+    dy = rand(4, m, n, dtype=dtype).to(gpu)
+    keep = lu.mask(m, n, 0.5, 7, 0).to(gpu) != 0
+    results = []
+    for bad in (0.0, math.nan, math.inf):
+        leaves = [v.detach().requires_grad_() for v in (x, w, b)]
+        y = g.linear(*leaves, activation="gelu", p=0.5, seed=7)
+        results.append(torch.autograd.grad(y, leaves, torch.where(keep, dy, torch.full_like(dy, bad))))
+    for other in results[1:]:
+        assert all(torch.equal(a, c) for a, c in zip(results[0], other))
